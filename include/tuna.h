@@ -504,6 +504,86 @@ int tuna_plan_cuda_error(const tuna_plan_t *plan);
  * barriers of its bulk copies); the receive buffer is then incomplete. */
 int tuna_plan_device_status(tuna_plan_t *plan, int *gave_up);
 
+/*
+ * Mixture-of-experts operators: what stands on either side of a token dispatch.
+ *
+ * Conventions beside those at the top: all arrays are DEVICE memory unless said
+ * otherwise; matrices are row-major with a row pitch (`ld...`) in elements; every call
+ * is asynchronous on `stream` and may be captured into a CUDA graph; calls of zero
+ * tokens or rows launch nothing that reads or writes rows.  Sums, probabilities and
+ * softmax statistics are held in 32 bits.  Workspaces are 256-byte aligned, belong to
+ * one call at a time, and need no initialisation unless the function says so.
+ */
+#define TUNA_DTYPE_F32 0
+#define TUNA_DTYPE_BF16 1
+#define TUNA_DTYPE_E4M3 2 /* 8 bits: 4 of exponent, 3 of fraction, largest value 448 */
+
+#define TUNA_MOE_SOFTMAX 0
+#define TUNA_MOE_SIGMOID 1
+#define TUNA_MOE_MAX_EXPERTS 512
+#define TUNA_MOE_MAX_K 32
+
+/*
+ * tuna_moe_route - the k experts of every token, their weights, and the rows' order.
+ *   logits   tokens x experts, TUNA_DTYPE_F32 or _BF16, pitch ld >= experts.
+ *   ids, weights   tokens x k.  ids[t][0..k) are the experts of the k largest logits of
+ *            the token in falling order, ties to the lower expert.  An expert whose logit
+ *            is -inf or NaN is never chosen; slots left over have id -1 and weight 0, and
+ *            a token whose whole row is masked has nothing but such slots.  (The lowest
+ *            finite value is an ordinary logit.)  Logits of +inf share the softmax.
+ *   scoring  TUNA_MOE_SOFTMAX: softmax over all experts; TUNA_MOE_SIGMOID: 1/(1+exp(-z)).
+ *   renormalize   non-zero: the chosen weights are divided by their sum.  Then all are
+ *            multiplied by `scale`.
+ *   ranks    the tokens are those of `ranks` ranks of tokens / ranks each (a divisor).
+ *            Rows (token, slot) are ordered by rank, expert, token:
+ *   rows     tokens * k: the token of each row in that order (the gather map of
+ *            tuna_plan_set_row_maps when experts are ranks); -1 behind the last row.
+ *   pos      tokens x k: the row of each choice, -1 where the id is -1.
+ *   counts   ranks x experts rows (what tuna_plan_update_counts_device takes when
+ *            experts == ranks); may be NULL.
+ *   offsets  ranks * experts + 1: the first row of each (rank, expert); may be NULL.
+ * Limits (TUNA_ERR_RANGE): experts <= TUNA_MOE_MAX_EXPERTS, k <= TUNA_MOE_MAX_K,
+ * tokens * k <= 2^31, ranks * experts <= 2^20.
+ *
+ * tuna_moe_order - the same order from ids that another router made (ids below 0 or from
+ * `experts` on are left out).  One workspace size for both.
+ *
+ * tuna_moe_route_backward - dlogits (the logits' type) from dweights (tokens x k, f32):
+ * the gradient through scoring, renormalisation and scale; the choice itself is constant.
+ */
+int tuna_moe_order_workspace_bytes(int64_t tokens, int experts, int k, int ranks, size_t *bytes);
+int tuna_moe_route(const void *logits, int dtype, int64_t tokens, int experts, int64_t ld, int k,
+                   int ranks, int scoring, int renormalize, float scale, int32_t *ids,
+                   float *weights, int64_t *counts, int64_t *offsets, int64_t *rows, int64_t *pos,
+                   void *workspace, size_t workspace_bytes, void *stream);
+int tuna_moe_order(const int32_t *ids, int64_t tokens, int experts, int k, int ranks,
+                   int64_t *counts, int64_t *offsets, int64_t *rows, int64_t *pos, void *workspace,
+                   size_t workspace_bytes, void *stream);
+int tuna_moe_route_backward(const void *logits, int dtype, int64_t tokens, int experts, int64_t ld,
+                            int k, int scoring, int renormalize, float scale, const int32_t *ids,
+                            const float *dweights, void *dlogits, int64_t ldd, void *stream);
+
+/*
+ * tuna_moe_combine - out[t] = sum over s of weights[t][s] * y[pos[t][s]], in slot order and
+ * in 32 bits; slots whose pos is outside [0, rows) add nothing.  y: rows x dim, out:
+ * tokens x dim, each f32 or bf16.
+ * tuna_moe_combine_backward - dy[pos[t][s]] = weights[t][s] * dout[t] (y's type; rows that
+ * no pos names are left untouched) and dweights[t][s] = <dout[t], y[pos[t][s]]>.
+ */
+int tuna_moe_combine(const void *y, int y_dtype, int64_t rows, int dim, int64_t ldy,
+                     const float *weights, const int64_t *pos, int64_t tokens, int k, void *out,
+                     int out_dtype, int64_t ldo, void *stream);
+int tuna_moe_combine_backward(const void *dout, int out_dtype, int64_t lddo, const void *y,
+                              int y_dtype, int64_t rows, int dim, int64_t ldy, const float *weights,
+                              const int64_t *pos, int64_t tokens, int k, void *dy, int64_t lddy,
+                              float *dweights, void *stream);
+
+/* Synchronises the device and reports in *gave_up (host) whether a kernel of these operators
+ * abandoned a bounded wait; its outputs are then incomplete.  tuna_ops_cuda_error: the
+ * cudaError_t behind this thread's latest TUNA_ERR_CUDA of these operators. */
+int tuna_ops_device_status(int *gave_up);
+int tuna_ops_cuda_error(void);
+
 /* Static string for a status code. */
 const char *tuna_strerror(int status);
 

@@ -17,6 +17,8 @@ _I64P = ctypes.POINTER(ctypes.c_int64)
 _INTP = ctypes.POINTER(ctypes.c_int)
 _SZP = ctypes.POINTER(ctypes.c_size_t)
 _VP = ctypes.c_void_p
+_I64 = ctypes.c_int64
+_INT = ctypes.c_int
 
 FLAG_DIRECT_TO_R = 0
 FLAG_CLASSIC_ROTATE = 1
@@ -78,6 +80,17 @@ SIGNATURES = {
     "tuna_plan_get_timing": (ctypes.c_int, [_VP, ctypes.c_int, ctypes.POINTER(ctypes.c_double), _I64P, _I64P]),
     "tuna_plan_cuda_error": (ctypes.c_int, [_VP]),
     "tuna_plan_device_status": (ctypes.c_int, [_VP, _INTP]),
+    "tuna_moe_order_workspace_bytes": (ctypes.c_int, [_I64, _INT, _INT, _INT, _SZP]),
+    "tuna_moe_route": (ctypes.c_int, [_VP, _INT, _I64, _INT, _I64] + [_INT] * 4 + [ctypes.c_float] + [_VP] * 7
+                       + [ctypes.c_size_t, _VP]),
+    "tuna_moe_order": (ctypes.c_int, [_VP, _I64, _INT, _INT, _INT] + [_VP] * 5 + [ctypes.c_size_t, _VP]),
+    "tuna_moe_route_backward": (ctypes.c_int, [_VP, _INT, _I64, _INT, _I64, _INT, _INT, _INT, ctypes.c_float, _VP, _VP, _VP,
+                                               _I64, _VP]),
+    "tuna_moe_combine": (ctypes.c_int, [_VP, _INT, _I64, _INT, _I64, _VP, _VP, _I64, _INT, _VP, _INT, _I64, _VP]),
+    "tuna_moe_combine_backward": (ctypes.c_int, [_VP, _INT, _I64, _VP, _INT, _I64, _INT, _I64, _VP, _VP, _I64, _INT, _VP, _I64,
+                                                 _VP, _VP]),
+    "tuna_ops_device_status": (ctypes.c_int, [_INTP]),
+    "tuna_ops_cuda_error": (ctypes.c_int, []),
     "tuna_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "tuna_version": (ctypes.c_int, []),
 }

@@ -1,0 +1,758 @@
+// Router of a mixture-of-experts layer: the k best experts of every token with their
+// weights, the rows' order by expert (the gather map and count matrix that a token
+// dispatch takes), the weighted sum that undoes it, and the gradients of both.
+//
+// All of it is bound by memory, and for a decode step by latency: the logits are read
+// once, everything else is a few bytes a token.
+#include <algorithm>
+#include <mutex>
+
+#include "tuna_ops.cuh"
+
+namespace tuna_ops {
+
+static __device__ int g_gave_up;  // raised by a kernel whose bounded wait ran out
+
+static thread_local int t_cuda_error = 0;
+
+int note_cuda(cudaError_t e) {
+  if (e == cudaSuccess) return TUNA_OK;
+  t_cuda_error = (int)e;
+  return TUNA_ERR_CUDA;
+}
+
+int sm_count() {
+  static std::mutex m;
+  static int count[64] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+  std::lock_guard<std::mutex> lock(m);
+  if (!count[dev] && cudaDeviceGetAttribute(&count[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 148;
+  return count[dev];
+}
+
+int *error_word() {
+  static std::mutex m;
+  static int *at[64] = {};
+  int dev = -1;
+  if (note_cuda(cudaGetDevice(&dev)) || dev < 0 || dev >= 64) return nullptr;
+  std::lock_guard<std::mutex> lock(m);
+  if (!at[dev]) {
+    void *p = nullptr;
+    if (note_cuda(cudaGetSymbolAddress(&p, g_gave_up))) return nullptr;
+    at[dev] = (int *)p;
+  }
+  return at[dev];
+}
+
+namespace {
+
+constexpr int kMaxK = 32;
+constexpr int kTopThreads = 256;
+
+// What a router makes of a logit.  A NaN is a masked place, like -inf: never chosen.
+__device__ __forceinline__ float logit_of(float v) { return v != v ? -INFINITY : v; }
+// exp(z - m) where both may be infinite: the places that hold +inf share the weight.
+__device__ __forceinline__ float exp_of(float z, float m) { return z == m ? 1.0f : expf(z - m); }
+__device__ __forceinline__ float sigmoid_of(float z) { return 1.0f / (1.0f + expf(-z)); }
+
+// A token's logits, VPL a lane in a group of LPT lanes: lane l holds experts l*VPL ...
+template <int VPL, typename T>
+__device__ __forceinline__ void load_logits(const T *row, int first, int experts, bool vec, float (&z)[VPL]) {
+  if (vec && first + VPL <= experts) {
+    load_row(row + first, z);
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) z[i] = logit_of(z[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) z[i] = first + i < experts ? logit_of(to_f32(row[first + i])) : -INFINITY;
+  }
+}
+
+struct RouteArgs {
+  const void *logits;
+  int64_t tokens, ld;
+  int experts, k, scoring, renormalize, vec;
+  float scale;
+  int32_t *ids;
+  float *weights;
+};
+
+// The choice for one token by its group of LPT lanes; lane s of the group leaves with slot s
+// (k <= LPT).  k rounds of an argmax: within a lane over its VPL values, then across lanes by
+// shuffles; ties go to the lower expert because a later one must be strictly larger.
+template <int LPT, int VPL>
+__device__ __forceinline__ void choose(float (&z)[VPL], int lane, int k, int scoring, int renormalize, float scale, int &id, float &weight) {
+  const int first = lane * VPL;
+  uint32_t taken = 0;
+  float mine = -INFINITY, top = -INFINITY;
+  id = -1;
+  for (int s = 0; s < k; ++s) {
+    float best = -INFINITY;
+    int at = 0;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+      if (z[i] > best && !((taken >> i) & 1)) best = z[i], at = i;
+    }
+    int e = first + at;
+#pragma unroll
+    for (int d = 1; d < LPT; d <<= 1) {
+      const float ob = __shfl_xor_sync(~0u, best, d);
+      const int oe = __shfl_xor_sync(~0u, e, d);
+      if (ob > best || (ob == best && oe < e)) best = ob, e = oe;
+    }
+    if (s == 0) top = best;
+    if (best != -INFINITY) {  // (no early end: the other groups of the warp go on with the shuffles)
+      if (e >= first && e < first + VPL) taken |= 1u << (e - first);
+      if (s == lane) id = e, mine = best;
+    }
+  }
+  float w = 0.0f;
+  if (scoring == TUNA_MOE_SIGMOID) {
+    if (id >= 0) w = sigmoid_of(mine);
+  } else if (id >= 0) {
+    w = exp_of(mine, top);
+  }
+  float sum = w;
+  if (!renormalize && scoring == TUNA_MOE_SOFTMAX) {
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) sum += z[i] == -INFINITY ? 0.0f : exp_of(z[i], top);
+  }
+#pragma unroll
+  for (int d = 1; d < LPT; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
+  if (renormalize || scoring == TUNA_MOE_SOFTMAX) w = sum > 0.0f ? w / sum : 0.0f;
+  weight = id >= 0 ? w * scale : 0.0f;
+}
+
+// ---- the rows' order ---------------------------------------------------------------------
+//
+// A stable counting sort of the T k choices by (rank, expert).  The tokens of a rank are cut
+// into chunks; `hist` holds how often each chunk chose each expert.  A block of the order
+// kernel sums the columns of `hist` itself (they come from L2), so that no scan kernel and no
+// third launch is needed, then ranks its own entries: peers of a warp by match, warps by a
+// small table in shared memory.
+
+struct OrderArgs {
+  const int32_t *ids;
+  int64_t tokens;        // in all
+  int64_t rank_tokens;   // of one rank
+  int experts, k, ranks;
+  int chunk;             // tokens a chunk
+  int64_t rank_chunks;   // chunks of one rank
+  int group;             // chunks that one block of the order kernel takes
+  int64_t rank_groups;   // blocks of one rank
+  uint16_t *hist;        // [ranks * rank_chunks][experts]
+  int64_t *counts, *offsets, *rows, *pos;
+};
+
+constexpr int kOrderThreads = 1024, kOrderWarps = kOrderThreads / 32;
+
+// Shared memory of the order step: base[experts] (64 bits), then the warps' tables, then the
+// column sums (64-bit pairs would be wasteful: entries of one call stay below 2^31).
+__host__ __device__ inline size_t order_smem(int experts) {
+  return (size_t)experts * 8 + (size_t)kOrderWarps * experts * 4 + (size_t)experts * 8 + 256;
+}
+
+__device__ __forceinline__ void place_entries(const OrderArgs &o, char *smem, int rank, int64_t first_entry, int64_t last_entry) {
+  // base[e]: the row of the first of this block's entries that chose e
+  int64_t *base = (int64_t *)smem;
+  uint32_t *table = (uint32_t *)(smem + (size_t)o.experts * 16);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t n = last_entry - first_entry;
+  const int64_t per = (n + kOrderWarps - 1) / kOrderWarps;
+  const int64_t a = first_entry + min(n, warp * per), b = first_entry + min(n, (warp + 1) * per);
+  uint32_t *mine = table + (size_t)warp * o.experts;
+  for (int e = threadIdx.x; e < kOrderWarps * o.experts; e += kOrderThreads) table[e] = 0;
+  __syncthreads();
+  for (int64_t i = a; i < b; i += 32) {
+    const int id = i + lane < b ? o.ids[i + lane] : -1;
+    const bool there = id >= 0 && id < o.experts;
+    const uint32_t peers = __match_any_sync(~0u, there ? id : -1);
+    if (there && lane == __ffs(peers) - 1) mine[id] += __popc(peers);
+    __syncwarp();
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < o.experts; e += kOrderThreads) {
+    uint32_t sum = 0;
+    for (int w = 0; w < kOrderWarps; ++w) {
+      const uint32_t c = table[(size_t)w * o.experts + e];
+      table[(size_t)w * o.experts + e] = sum;
+      sum += c;
+    }
+  }
+  __syncthreads();
+  for (int64_t i = a; i < b; i += 32) {
+    const int id = i + lane < b ? o.ids[i + lane] : -1;
+    const bool there = id >= 0 && id < o.experts;
+    const uint32_t peers = __match_any_sync(~0u, there ? id : -1);
+    const int before = __popc(peers & ((1u << lane) - 1));
+    if (there) {
+      const int64_t at = base[id] + mine[id] + before;
+      o.pos[i + lane] = at;
+      o.rows[at] = (i + lane) / o.k;
+    } else if (i + lane < b) {
+      o.pos[i + lane] = -1;
+    }
+    __syncwarp();
+    if (there && lane == __ffs(peers) - 1) mine[id] += __popc(peers);
+    __syncwarp();
+  }
+}
+
+// Exclusive scan of v over the block's threads; *total receives the sum.
+__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t *total) {
+  __shared__ int64_t part[33];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int64_t x = v;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t y = __shfl_up_sync(~0u, x, d);
+    if (lane >= d) x += y;
+  }
+  __syncthreads();
+  if (lane == 31) part[warp] = x;
+  __syncthreads();
+  if (warp == 0) {
+    int64_t p = lane < (int)(blockDim.x >> 5) ? part[lane] : 0;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t y = __shfl_up_sync(~0u, p, d);
+      if (lane >= d) p += y;
+    }
+    part[lane + 1] = p;
+    if (lane == 0) part[0] = 0;
+  }
+  __syncthreads();
+  const int64_t r = x - v + part[warp];
+  *total = part[32];
+  __syncthreads();
+  return r;
+}
+
+// Block (rank, group).  Sums the columns of hist: of all earlier ranks (rows before this
+// rank), of this rank (for the scan over experts) and of this rank's earlier chunks.
+__global__ void __launch_bounds__(kOrderThreads) tuna_order_kernel(OrderArgs o) {
+  extern __shared__ __align__(16) char smem[];
+  wait_previous();
+  allow_next();
+  const int E = o.experts;
+  const int rank = (int)(blockIdx.x / o.rank_groups);
+  const int64_t group = blockIdx.x % o.rank_groups;
+  int64_t *base = (int64_t *)smem;
+  int *total = (int *)(smem + (size_t)E * 8);  // of this rank, per expert
+  int *before = total + E;                     // of this rank's earlier chunks
+  for (int e = threadIdx.x; e < 2 * E; e += kOrderThreads) total[e] = 0;
+  __syncthreads();
+  const int64_t chunks = o.rank_chunks, mine = group * o.group;
+  // threads take (a row of hist, an expert) with the expert along the lanes
+  const int lanes = E >= kOrderThreads ? kOrderThreads : E;
+  const int stripes = kOrderThreads / lanes;
+  const int stripe = threadIdx.x / lanes;
+  int64_t earlier = 0;  // entries of earlier ranks
+  for (int e = threadIdx.x % lanes; e < E && stripe < stripes; e += lanes) {
+    for (int64_t c = stripe; c < rank * chunks; c += stripes) earlier += o.hist[c * E + e];
+    int t = 0, p = 0;
+    const uint16_t *h = o.hist + rank * chunks * E + e;
+#pragma unroll 8
+    for (int64_t c = stripe; c < chunks; c += stripes) {
+      const int v = h[c * E];
+      t += v;
+      p += c < mine ? v : 0;
+    }
+    if (t) atomicAdd(total + e, t);
+    if (p) atomicAdd(before + e, p);
+  }
+  int64_t rows_before;
+  block_scan(earlier, &rows_before);  // (its barriers also cover the sums above)
+  // scan over the experts, kOrderThreads at a time
+  for (int e0 = 0; e0 < E; e0 += kOrderThreads) {
+    const int e = e0 + threadIdx.x;
+    const int64_t t = e < E ? total[e] : 0;
+    int64_t sum;
+    const int64_t x = block_scan(t, &sum) + rows_before;
+    if (e < E) {
+      base[e] = x + before[e];
+      if (group == 0) {
+        if (o.counts) o.counts[(int64_t)rank * E + e] = t;
+        if (o.offsets) {
+          o.offsets[(int64_t)rank * E + e] = x;
+          if (rank == o.ranks - 1 && e == E - 1) o.offsets[(int64_t)o.ranks * E] = x + t;
+        }
+      }
+    }
+    rows_before += sum;
+  }
+  __syncthreads();
+  const int64_t t0 = rank * o.rank_tokens + mine * o.chunk;
+  const int64_t t1 = min((int64_t)(rank + 1) * o.rank_tokens, t0 + (int64_t)o.group * o.chunk);
+  place_entries(o, smem, rank, t0 * o.k, t1 * o.k);
+  // rows that no entry fills (masked choices): -1, written by the last rank's blocks, which know the sum
+  if (rank == o.ranks - 1)
+    for (int64_t j = rows_before + group * kOrderThreads + threadIdx.x; j < o.tokens * o.k; j += o.rank_groups * kOrderThreads) o.rows[j] = -1;
+}
+
+// How often a chunk chose each expert, from ids in memory (a block a chunk).
+__global__ void __launch_bounds__(256) tuna_order_hist_kernel(OrderArgs o) {
+  extern __shared__ int count[];
+  wait_previous();
+  allow_next();
+  for (int e = threadIdx.x; e < o.experts; e += 256) count[e] = 0;
+  __syncthreads();
+  const int64_t rank = blockIdx.x / o.rank_chunks, c = blockIdx.x % o.rank_chunks;
+  const int64_t t0 = rank * o.rank_tokens + c * o.chunk, t1 = min((rank + 1) * o.rank_tokens, t0 + o.chunk);
+  for (int64_t i = t0 * o.k + threadIdx.x; i < t1 * o.k; i += 256) {
+    const int id = o.ids[i];
+    if (id >= 0 && id < o.experts) atomicAdd(count + id, 1);
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < o.experts; e += 256) o.hist[(int64_t)blockIdx.x * o.experts + e] = (uint16_t)count[e];
+}
+
+// The choice for a chunk of tokens (a block a chunk) and its column of hist.
+template <int LPT, int VPL, typename T>
+__global__ void __launch_bounds__(kTopThreads) tuna_route_kernel(RouteArgs a, OrderArgs o) {
+  extern __shared__ int count[];
+  wait_previous();
+  allow_next();
+  for (int e = threadIdx.x; e < a.experts; e += kTopThreads) count[e] = 0;
+  __syncthreads();
+  const int64_t rank = blockIdx.x / o.rank_chunks, c = blockIdx.x % o.rank_chunks;
+  const int64_t t0 = rank * o.rank_tokens + c * o.chunk, t1 = min((rank + 1) * o.rank_tokens, t0 + o.chunk);
+  const int lane = threadIdx.x % LPT;
+  for (int64_t tb = t0; tb < t1; tb += kTopThreads / LPT) {  // (uniform: the shuffles need whole warps)
+    const int64_t t = tb + threadIdx.x / LPT;
+    float z[VPL];
+    if (t < t1) {
+      load_logits(reinterpret_cast<const T *>(a.logits) + t * a.ld, lane * VPL, a.experts, a.vec, z);
+    } else {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) z[i] = -INFINITY;
+    }
+    int id;
+    float w;
+    choose<LPT>(z, lane, a.k, a.scoring, a.renormalize, a.scale, id, w);
+    if (t < t1 && lane < a.k) {
+      a.ids[t * a.k + lane] = id;
+      a.weights[t * a.k + lane] = w;
+      if (id >= 0) atomicAdd(count + id, 1);
+    }
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < a.experts; e += kTopThreads) o.hist[(int64_t)blockIdx.x * a.experts + e] = (uint16_t)count[e];
+}
+
+// Gradient of the weights with respect to the logits; the probabilities are computed anew
+// from the logits (one read of them) instead of being kept by the forward pass.
+//   softmax            dz_e = p_e (g_e - sum_s g_s p_s)          g: dw at the chosen, 0 elsewhere
+//   ... renormalised   dz_s = w_s (g_s - sum_s g_s w_s)          over the chosen alone
+//   sigmoid            dz_s = g_s p_s (1 - p_s)
+//   ... renormalised   dz_s = (g_s - sum_s g_s w_s) / sum p * p_s (1 - p_s)
+struct RouteGradArgs {
+  const void *logits;
+  int64_t tokens, ld, ldd;
+  int experts, k, scoring, renormalize, vec;
+  float scale;
+  const int32_t *ids;
+  const float *dweights;
+  void *dlogits;
+};
+template <int LPT, int VPL, typename T>
+__global__ void __launch_bounds__(kTopThreads) tuna_route_grad_kernel(RouteGradArgs a) {
+  wait_previous();
+  allow_next();
+  const int lane = threadIdx.x % LPT;
+  const int64_t t = (int64_t)blockIdx.x * (kTopThreads / LPT) + threadIdx.x / LPT;
+  const bool there = t < a.tokens;
+  float z[VPL], d[VPL];
+  if (there) {
+    load_logits(reinterpret_cast<const T *>(a.logits) + t * a.ld, lane * VPL, a.experts, a.vec, z);
+  } else {
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) z[i] = -INFINITY;
+  }
+  int id = -1;
+  float g = 0.0f;
+  if (there && lane < a.k) {
+    id = a.ids[t * a.k + lane];
+    if (id >= a.experts) id = -1;
+    g = id < 0 ? 0.0f : a.dweights[t * a.k + lane] * a.scale;
+  }
+  float top = -INFINITY, mine = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < VPL; ++i) top = fmaxf(top, z[i]), d[i] = 0.0f;
+#pragma unroll
+  for (int s = 1; s < LPT; s <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, s));
+  // the chosen logits, from the lanes that hold them
+  for (int s = 0; s < a.k; ++s) {
+    const int e = __shfl_sync(~0u, id, s, LPT);
+    const int owner = e < 0 ? 0 : e / VPL;
+    float v = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i)
+      if (e == lane * VPL + i) v = z[i];
+    v = __shfl_sync(~0u, v, owner, LPT);
+    if (lane == s) mine = e < 0 ? -INFINITY : v;
+  }
+  const bool soft = a.scoring == TUNA_MOE_SOFTMAX;
+  float p = mine == -INFINITY ? 0.0f : soft ? exp_of(mine, top) : sigmoid_of(mine);
+  float sum = p;
+  if (soft && !a.renormalize) {
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) sum += z[i] == -INFINITY ? 0.0f : exp_of(z[i], top);
+  }
+#pragma unroll
+  for (int s = 1; s < LPT; s <<= 1) sum += __shfl_xor_sync(~0u, sum, s);
+  const float over = sum > 0.0f ? 1.0f / sum : 0.0f;
+  const float w = soft || a.renormalize ? (sum > 0.0f ? p / sum : 0.0f) : p;
+  float gw = g * w;
+#pragma unroll
+  for (int s = 1; s < LPT; s <<= 1) gw += __shfl_xor_sync(~0u, gw, s);
+  float mine_d;  // this lane's slot's share
+  if (soft)
+    mine_d = a.renormalize ? w * (g - gw) : w * g;
+  else
+    mine_d = (a.renormalize ? (g - gw) * over : g) * p * (1.0f - p);
+  for (int s = 0; s < a.k; ++s) {
+    const int e = __shfl_sync(~0u, id, s, LPT);
+    const float v = __shfl_sync(~0u, mine_d, s, LPT);
+#pragma unroll
+    for (int i = 0; i < VPL; ++i)
+      if (e == lane * VPL + i) d[i] += v;
+  }
+  if (soft && !a.renormalize) {
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) d[i] -= z[i] == -INFINITY ? 0.0f : (sum > 0.0f ? exp_of(z[i], top) / sum : 0.0f) * gw;
+  }
+  if (!there) return;
+  T *out = reinterpret_cast<T *>(a.dlogits) + t * a.ldd + lane * VPL;
+  if (a.vec && (lane + 1) * VPL <= a.experts) {
+    store_row(out, d);
+  } else {
+#pragma unroll
+    for (int i = 0; i < VPL; ++i)
+      if (lane * VPL + i < a.experts) out[i] = from_f32<T>(d[i]);
+  }
+}
+
+// ---- combine -----------------------------------------------------------------------------
+//
+// out[t] = sum_s w[t,s] y[pos[t,s]], summed in slot order in 32 bits.  Bound by the bytes of
+// y and out: a thread takes 8 columns of a token, 16-byte loads of bf16.
+struct CombineArgs {
+  const void *y, *dout;
+  const float *weights;
+  const int64_t *pos;
+  void *out, *dy;
+  float *dweights;
+  int64_t rows, tokens, ldy, ldo, lddy;
+  int dim, k, vec;
+};
+template <typename TY, typename TO>
+__global__ void __launch_bounds__(256) tuna_combine_kernel(CombineArgs a) {
+  wait_previous();
+  allow_next();
+  const int cols = (a.dim + 7) / 8;
+  const int64_t n = a.tokens * cols;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t t = i / cols;
+    const int c = (int)(i - t * cols) * 8;
+    float acc[8] = {};
+    for (int s = 0; s < a.k; ++s) {
+      const int64_t r = a.pos[t * a.k + s];
+      if (r < 0 || r >= a.rows) continue;
+      const float w = a.weights[t * a.k + s];
+      const TY *y = reinterpret_cast<const TY *>(a.y) + r * a.ldy + c;
+      float v[8];
+      if (a.vec) {
+        load_row(y, v);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c + j < a.dim ? to_f32(y[j]) : 0.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] = fmaf(w, v[j], acc[j]);
+    }
+    TO *out = reinterpret_cast<TO *>(a.out) + t * a.ldo + c;
+    if (a.vec) {
+      store_row(out, acc);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c + j < a.dim) out[j] = from_f32<TO>(acc[j]);
+    }
+  }
+}
+
+// dy[pos[t,s]] = w[t,s] dout[t];  dw[t,s] = <dout[t], y[pos[t,s]]>.  A block a token; the
+// row of dout is read once a slot (from L1 after the first), rows of y once.
+template <typename TY, typename TO>
+__global__ void __launch_bounds__(256) tuna_combine_grad_kernel(CombineArgs a) {
+  __shared__ float part[8];
+  wait_previous();
+  allow_next();
+  for (int64_t t = blockIdx.x; t < a.tokens; t += gridDim.x) {
+    const TO *g = reinterpret_cast<const TO *>(a.dout) + t * a.ldo;
+    for (int s = 0; s < a.k; ++s) {
+      const int64_t r = a.pos[t * a.k + s];
+      const bool there = r >= 0 && r < a.rows;
+      float dot = 0.0f;
+      if (there) {
+        const float w = a.weights[t * a.k + s];
+        const TY *y = reinterpret_cast<const TY *>(a.y) + r * a.ldy;
+        TY *dy = reinterpret_cast<TY *>(a.dy) + r * a.lddy;
+        for (int c = threadIdx.x * 8; c < a.dim; c += 2048) {
+          float gv[8], yv[8];
+          if (a.vec) {
+            load_row(g + c, gv);
+            load_row(y + c, yv);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              gv[j] = c + j < a.dim ? to_f32(g[c + j]) : 0.0f;
+              yv[j] = c + j < a.dim ? to_f32(y[c + j]) : 0.0f;
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) dot = fmaf(gv[j], yv[j], dot), gv[j] *= w;
+          if (a.vec) {
+            store_row(dy + c, gv);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (c + j < a.dim) dy[c + j] = from_f32<TY>(gv[j]);
+          }
+        }
+      }
+#pragma unroll
+      for (int d = 16; d; d >>= 1) dot += __shfl_xor_sync(~0u, dot, d);
+      __syncthreads();
+      if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = dot;
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        float sum = 0.0f;
+        for (int i = 0; i < 8; ++i) sum += part[i];
+        a.dweights[t * a.k + s] = there ? sum : 0.0f;
+      }
+    }
+  }
+}
+
+// ---- host --------------------------------------------------------------------------------
+
+// Chunks of at most 128 tokens, fewer where that fills the GPU better; the blocks of the order
+// kernel take as many chunks as keep their number near one a multiprocessor, since each of them
+// reads the whole table of counts.
+void plan_order(OrderArgs &o, int64_t tokens, int experts, int k, int ranks) {
+  o.tokens = tokens, o.experts = experts, o.k = k, o.ranks = ranks;
+  o.rank_tokens = tokens / ranks;
+  int64_t chunk = 128;
+  while (ceil_div(tokens, chunk) > 2048) chunk *= 2;
+  while (chunk * k > 65535) chunk /= 2;  // 16 bits hold a chunk's count of one expert
+  o.chunk = (int)chunk;
+  o.rank_chunks = ceil_div(o.rank_tokens, chunk);
+  o.group = (int)ceil_div(o.rank_chunks * ranks, 148);
+  o.rank_groups = ceil_div(o.rank_chunks, o.group);
+}
+
+int check_order(int64_t tokens, int experts, int k, int ranks) {
+  if (tokens < 0 || experts < 1 || k < 1 || ranks < 1 || tokens % ranks != 0 || k > experts) return TUNA_ERR_INVALID_ARG;
+  if (experts > TUNA_MOE_MAX_EXPERTS || k > kMaxK || tokens > ((int64_t)1 << 31) / k || (int64_t)ranks > (1 << 20) / experts) return TUNA_ERR_RANGE;
+  return TUNA_OK;
+}
+
+// counts and offsets of a call without tokens
+int zero_order(const OrderArgs &o, int ranks, int experts, cudaStream_t st) {
+  const size_t n = (size_t)ranks * experts;
+  if (o.counts)
+    if (const int rc = note_cuda(cudaMemsetAsync(o.counts, 0, n * 8, st))) return rc;
+  if (o.offsets)
+    if (const int rc = note_cuda(cudaMemsetAsync(o.offsets, 0, (n + 1) * 8, st))) return rc;
+  return TUNA_OK;
+}
+
+int launch_order(const OrderArgs &o, cudaStream_t st) {
+  const size_t smem = order_smem(o.experts);
+  static std::mutex m;
+  static bool set[64] = {};
+  int dev = 0;
+  if (const int rc = note_cuda(cudaGetDevice(&dev))) return rc;
+  {
+    std::lock_guard<std::mutex> lock(m);
+    if (dev < 0 || dev >= 64 || !set[dev]) {
+      if (const int rc = note_cuda(cudaFuncSetAttribute(tuna_order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                        (int)order_smem(TUNA_MOE_MAX_EXPERTS))))
+        return rc;
+      if (dev >= 0 && dev < 64) set[dev] = true;
+    }
+  }
+  return launch(tuna_order_kernel, dim3((unsigned)(o.rank_groups * o.ranks)), kOrderThreads, smem, st, false, o);
+}
+
+// Lanes a token and values a lane: the fewest lanes that hold the experts at 8 values each
+// (one 16-byte load of bf16) and the slots at one a lane.
+template <typename F>
+int by_width(int experts, int k, F f) {
+  if (experts <= 64 && k <= 8) return f.template operator()<8, 8>();
+  if (experts <= 128 && k <= 16) return f.template operator()<16, 8>();
+  if (experts <= 256) return f.template operator()<32, 8>();
+  return f.template operator()<32, 16>();
+}
+template <typename T>
+struct RouteLaunch {
+  const RouteArgs &a;
+  const OrderArgs &o;
+  cudaStream_t st;
+  template <int LPT, int VPL>
+  int operator()() {
+    return launch(tuna_route_kernel<LPT, VPL, T>, dim3((unsigned)(o.rank_chunks * o.ranks)), kTopThreads, (size_t)a.experts * 4, st, false, a, o);
+  }
+};
+template <typename T>
+struct GradLaunch {
+  const RouteGradArgs &a;
+  cudaStream_t st;
+  template <int LPT, int VPL>
+  int operator()() {
+    return launch(tuna_route_grad_kernel<LPT, VPL, T>, dim3((unsigned)ceil_div(a.tokens, kTopThreads / LPT)), kTopThreads, 0, st, false, a);
+  }
+};
+
+size_t dtype_size(int dtype) { return dtype == TUNA_DTYPE_F32 ? 4 : dtype == TUNA_DTYPE_BF16 ? 2 : 0; }
+
+}  // namespace
+
+// The order from ids in memory, for the operators that have them (tuna_moe.cu).
+size_t order_bytes(int64_t tokens, int experts, int k, int ranks) {
+  OrderArgs o = {};
+  plan_order(o, tokens, experts, k, ranks);
+  return (size_t)o.rank_chunks * ranks * experts * 2;
+}
+
+}  // namespace tuna_ops
+
+using namespace tuna_ops;
+
+extern "C" {
+
+int tuna_moe_order_workspace_bytes(int64_t tokens, int experts, int k, int ranks, size_t *bytes) {
+  if (!bytes) return TUNA_ERR_INVALID_ARG;
+  if (const int rc = check_order(tokens, experts, k, ranks)) return rc;
+  *bytes = (order_bytes(tokens, experts, k, ranks) + 255) / 256 * 256;
+  return TUNA_OK;
+}
+
+int tuna_moe_order(const int32_t *ids, int64_t tokens, int experts, int k, int ranks, int64_t *counts, int64_t *offsets,
+                   int64_t *rows, int64_t *pos, void *workspace, size_t workspace_bytes, void *stream) {
+  if (const int rc = check_order(tokens, experts, k, ranks)) return rc;
+  cudaStream_t st = (cudaStream_t)stream;
+  OrderArgs o = {};
+  o.counts = counts, o.offsets = offsets, o.rows = rows, o.pos = pos, o.ids = ids;
+  if (tokens == 0) return zero_order(o, ranks, experts, st);
+  if (!ids || !rows || !pos) return TUNA_ERR_INVALID_ARG;
+  plan_order(o, tokens, experts, k, ranks);
+  if (!workspace || !aligned(workspace, 256) || workspace_bytes < order_bytes(tokens, experts, k, ranks)) return TUNA_ERR_WORKSPACE;
+  o.hist = (uint16_t *)workspace;
+  if (const int rc = launch(tuna_order_hist_kernel, dim3((unsigned)(o.rank_chunks * ranks)), 256, (size_t)experts * 4, st, false, o)) return rc;
+  return launch_order(o, st);
+}
+
+int tuna_moe_route(const void *logits, int dtype, int64_t tokens, int experts, int64_t ld, int k, int ranks, int scoring,
+                   int renormalize, float scale, int32_t *ids, float *weights, int64_t *counts, int64_t *offsets, int64_t *rows,
+                   int64_t *pos, void *workspace, size_t workspace_bytes, void *stream) {
+  if (const int rc = check_order(tokens, experts, k, ranks)) return rc;
+  if (!dtype_size(dtype) || (scoring != TUNA_MOE_SOFTMAX && scoring != TUNA_MOE_SIGMOID) || ld < experts) return TUNA_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  OrderArgs o = {};
+  o.counts = counts, o.offsets = offsets, o.rows = rows, o.pos = pos, o.ids = ids;
+  if (tokens == 0) return zero_order(o, ranks, experts, st);
+  if (!logits || !ids || !weights || !rows || !pos || !aligned(logits, dtype_size(dtype))) return TUNA_ERR_INVALID_ARG;
+  plan_order(o, tokens, experts, k, ranks);
+  if (!workspace || !aligned(workspace, 256) || workspace_bytes < order_bytes(tokens, experts, k, ranks)) return TUNA_ERR_WORKSPACE;
+  o.hist = (uint16_t *)workspace;
+  RouteArgs a = {};
+  a.logits = logits, a.tokens = tokens, a.ld = ld, a.experts = experts, a.k = k;
+  a.scoring = scoring, a.renormalize = renormalize != 0, a.scale = scale, a.ids = ids, a.weights = weights;
+  a.vec = aligned(logits, 16) && ld * dtype_size(dtype) % 16 == 0;
+  const int rc = dtype == TUNA_DTYPE_F32 ? by_width(experts, k, RouteLaunch<float>{a, o, st})
+                                         : by_width(experts, k, RouteLaunch<__nv_bfloat16>{a, o, st});
+  return rc ? rc : launch_order(o, st);
+}
+
+int tuna_moe_route_backward(const void *logits, int dtype, int64_t tokens, int experts, int64_t ld, int k, int scoring,
+                            int renormalize, float scale, const int32_t *ids, const float *dweights, void *dlogits, int64_t ldd,
+                            void *stream) {
+  if (const int rc = check_order(tokens, experts, k, 1)) return rc;
+  if (!dtype_size(dtype) || (scoring != TUNA_MOE_SOFTMAX && scoring != TUNA_MOE_SIGMOID) || ld < experts || ldd < experts) return TUNA_ERR_INVALID_ARG;
+  if (tokens == 0) return TUNA_OK;
+  if (!logits || !ids || !dweights || !dlogits) return TUNA_ERR_INVALID_ARG;
+  const size_t size = dtype_size(dtype);
+  if (!aligned(logits, size) || !aligned(dlogits, size)) return TUNA_ERR_INVALID_ARG;
+  RouteGradArgs a = {};
+  a.logits = logits, a.tokens = tokens, a.ld = ld, a.ldd = ldd, a.experts = experts, a.k = k, a.scoring = scoring;
+  a.renormalize = renormalize != 0, a.scale = scale, a.ids = ids, a.dweights = dweights, a.dlogits = dlogits;
+  a.vec = aligned(logits, 16) && aligned(dlogits, 16) && ld * size % 16 == 0 && ldd * size % 16 == 0;
+  return dtype == TUNA_DTYPE_F32 ? by_width(experts, k, GradLaunch<float>{a, (cudaStream_t)stream})
+                                 : by_width(experts, k, GradLaunch<__nv_bfloat16>{a, (cudaStream_t)stream});
+}
+
+static int check_combine(CombineArgs &a, int y_dtype, int out_dtype) {
+  const size_t sy = dtype_size(y_dtype), so = dtype_size(out_dtype);
+  if (!sy || !so || a.rows < 0 || a.tokens < 0 || a.dim < 0 || a.k < 1 || a.ldy < a.dim || a.ldo < a.dim) return TUNA_ERR_INVALID_ARG;
+  if (a.dim > kMaxDim || a.k > kMaxK || a.tokens > ((int64_t)1 << 31) / a.k) return TUNA_ERR_RANGE;
+  if (a.tokens == 0 || a.dim == 0) return TUNA_OK;
+  if (!a.weights || !a.pos || (a.rows > 0 && !a.y)) return TUNA_ERR_INVALID_ARG;
+  return TUNA_OK;
+}
+
+int tuna_moe_combine(const void *y, int y_dtype, int64_t rows, int dim, int64_t ldy, const float *weights, const int64_t *pos,
+                     int64_t tokens, int k, void *out, int out_dtype, int64_t ldo, void *stream) {
+  CombineArgs a = {};
+  a.y = y, a.weights = weights, a.pos = pos, a.out = out, a.rows = rows, a.tokens = tokens, a.ldy = ldy, a.ldo = ldo, a.dim = dim, a.k = k;
+  if (const int rc = check_combine(a, y_dtype, out_dtype)) return rc;
+  if (tokens == 0 || dim == 0) return TUNA_OK;
+  const size_t sy = dtype_size(y_dtype), so = dtype_size(out_dtype);
+  if (!out || !aligned(y, sy) || !aligned(out, so)) return TUNA_ERR_INVALID_ARG;
+  a.vec = dim % 8 == 0 && aligned(y, 16) && aligned(out, 16) && ldy * sy % 16 == 0 && ldo * so % 16 == 0;
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(tokens * ceil_div(dim, 8), 256), (int64_t)sm_count() * 16));
+  cudaStream_t st = (cudaStream_t)stream;
+  if (y_dtype == TUNA_DTYPE_F32)
+    return out_dtype == TUNA_DTYPE_F32 ? launch(tuna_combine_kernel<float, float>, grid, 256, 0, st, false, a)
+                                       : launch(tuna_combine_kernel<float, __nv_bfloat16>, grid, 256, 0, st, false, a);
+  return out_dtype == TUNA_DTYPE_F32 ? launch(tuna_combine_kernel<__nv_bfloat16, float>, grid, 256, 0, st, false, a)
+                                     : launch(tuna_combine_kernel<__nv_bfloat16, __nv_bfloat16>, grid, 256, 0, st, false, a);
+}
+
+int tuna_moe_combine_backward(const void *dout, int out_dtype, int64_t lddo, const void *y, int y_dtype, int64_t rows, int dim,
+                              int64_t ldy, const float *weights, const int64_t *pos, int64_t tokens, int k, void *dy, int64_t lddy,
+                              float *dweights, void *stream) {
+  CombineArgs a = {};
+  a.y = y, a.dout = dout, a.weights = weights, a.pos = pos, a.dy = dy, a.dweights = dweights;
+  a.rows = rows, a.tokens = tokens, a.ldy = ldy, a.ldo = lddo, a.lddy = lddy, a.dim = dim, a.k = k;
+  if (lddy < dim) return TUNA_ERR_INVALID_ARG;
+  if (const int rc = check_combine(a, y_dtype, out_dtype)) return rc;
+  if (tokens == 0 || dim == 0) return TUNA_OK;
+  const size_t sy = dtype_size(y_dtype), so = dtype_size(out_dtype);
+  if (!dout || !dweights || (rows > 0 && !dy) || !aligned(y, sy) || !aligned(dy, sy) || !aligned(dout, so)) return TUNA_ERR_INVALID_ARG;
+  a.vec = dim % 8 == 0 && aligned(y, 16) && aligned(dy, 16) && aligned(dout, 16) && ldy * sy % 16 == 0 && lddy * sy % 16 == 0 && lddo * so % 16 == 0;
+  const dim3 grid((unsigned)std::min<int64_t>(tokens, (int64_t)sm_count() * 16));
+  cudaStream_t st = (cudaStream_t)stream;
+  if (y_dtype == TUNA_DTYPE_F32)
+    return out_dtype == TUNA_DTYPE_F32 ? launch(tuna_combine_grad_kernel<float, float>, grid, 256, 0, st, false, a)
+                                       : launch(tuna_combine_grad_kernel<float, __nv_bfloat16>, grid, 256, 0, st, false, a);
+  return out_dtype == TUNA_DTYPE_F32 ? launch(tuna_combine_grad_kernel<__nv_bfloat16, float>, grid, 256, 0, st, false, a)
+                                     : launch(tuna_combine_grad_kernel<__nv_bfloat16, __nv_bfloat16>, grid, 256, 0, st, false, a);
+}
+
+int tuna_ops_device_status(int *gave_up) {
+  if (!gave_up) return TUNA_ERR_INVALID_ARG;
+  int *word = error_word();
+  if (!word) return TUNA_ERR_CUDA;
+  if (const int rc = note_cuda(cudaDeviceSynchronize())) return rc;
+  return note_cuda(cudaMemcpy(gave_up, word, sizeof(int), cudaMemcpyDeviceToHost));
+}
+
+int tuna_ops_cuda_error(void) { return t_cuda_error; }
+
+}  // extern "C"
