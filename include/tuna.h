@@ -578,6 +578,41 @@ int tuna_moe_combine_backward(const void *dout, int out_dtype, int64_t lddo, con
                               const int64_t *pos, int64_t tokens, int k, void *dy, int64_t lddy,
                               float *dweights, void *stream);
 
+/*
+ * tuna_fp8_quantize - a matrix to 8 bits with a 32-bit scale for each block.
+ *   block scale s = max(largest |x|, 2^-100) / 448 and q = e4m3(x / s), both divisions
+ *   correctly rounded, halves to even; a block that holds a NaN or an infinity gets the
+ *   scale NaN.  x: rows x cols, f32 or bf16, pitch ldx.
+ *   layout           blocks            q                          scale
+ *   TUNA_FP8_ROWS    1 x 128           rows x cols                [ceil(cols/128)][rows]
+ *   TUNA_FP8_COLUMNS 128 x 1           x^T: cols x rows           [ceil(rows/128)][cols]
+ *   TUNA_FP8_TILES   128 x 128         rows x cols                [ceil(rows/128)][ceil(cols/128)]
+ *   TUNA_FP8_TILES_T 128 x 128         x^T: cols x rows           [ceil(cols/128)][ceil(rows/128)]
+ *   q is 16-byte aligned, its pitch ldq a multiple of 16; rows are written up to the
+ *   next multiple of 16 (with zeros).  Blocks at the edges are smaller.
+ *
+ * tuna_fp8_matmul - out[m][n] = sum over blocks of a_scale * b_scale * (a . b), f32 or bf16.
+ *   a        m x k, e4m3, TUNA_FP8_ROWS scales; b: n x k with TUNA_FP8_TILES scales, or
+ *            with TUNA_FP8_ROWS scales (one group only).  Pitches are multiples of 16.
+ *   A layer y = x w^T and its gradients are the same product on operands quantised along
+ *   the contracted axis:  y = (x ROWS) (w TILES);  dx = (dy ROWS) (w TILES_T);
+ *   dw = (dy COLUMNS) (x COLUMNS with b_layout TUNA_FP8_ROWS).
+ *   groups, offsets   b holds `groups` matrices (n * ldb bytes apart, scales back to back);
+ *            rows [offsets[g], offsets[g+1]) of a meet matrix g (offsets: DEVICE, groups + 1,
+ *            not falling, inside [0, m]).  Rows outside every group are not written.
+ *            offsets NULL: one group of all rows.
+ * Limits (TUNA_ERR_RANGE): groups <= TUNA_MOE_MAX_EXPERTS, n, k <= 2^24, m < 2^31 - 256.
+ */
+#define TUNA_FP8_ROWS 0
+#define TUNA_FP8_COLUMNS 1
+#define TUNA_FP8_TILES 2
+#define TUNA_FP8_TILES_T 3
+int tuna_fp8_quantize(const void *x, int dtype, int64_t rows, int cols, int64_t ldx, int layout,
+                      void *q, int64_t ldq, float *scale, void *stream);
+int tuna_fp8_matmul(const void *a, const float *a_scale, int64_t m, int64_t lda, const void *b,
+                    const float *b_scale, int b_layout, int n, int64_t ldb, int k, int groups,
+                    const int64_t *offsets, void *out, int out_dtype, int64_t ldo, void *stream);
+
 /* Synchronises the device and reports in *gave_up (host) whether a kernel of these operators
  * abandoned a bounded wait; its outputs are then incomplete.  tuna_ops_cuda_error: the
  * cudaError_t behind this thread's latest TUNA_ERR_CUDA of these operators. */

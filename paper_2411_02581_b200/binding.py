@@ -89,6 +89,8 @@ SIGNATURES = {
     "tuna_moe_combine": (ctypes.c_int, [_VP, _INT, _I64, _INT, _I64, _VP, _VP, _I64, _INT, _VP, _INT, _I64, _VP]),
     "tuna_moe_combine_backward": (ctypes.c_int, [_VP, _INT, _I64, _VP, _INT, _I64, _INT, _I64, _VP, _VP, _I64, _INT, _VP, _I64,
                                                  _VP, _VP]),
+    "tuna_fp8_quantize": (ctypes.c_int, [_VP, _INT, _I64, _INT, _I64, _INT, _VP, _I64, _VP, _VP]),
+    "tuna_fp8_matmul": (ctypes.c_int, [_VP, _VP, _I64, _I64, _VP, _VP, _INT, _INT, _I64, _INT, _INT, _VP, _VP, _INT, _I64, _VP]),
     "tuna_ops_device_status": (ctypes.c_int, [_INTP]),
     "tuna_ops_cuda_error": (ctypes.c_int, []),
     "tuna_strerror": (ctypes.c_char_p, [ctypes.c_int]),

@@ -1,0 +1,603 @@
+// Matrix products in 8-bit floating point with a 32-bit scale for each block of 128
+// along the contracted axis, dense and grouped by expert, and the quantisation of their
+// operands.
+//
+//   y[m,n] = sum_b sa[b,m] sb[n or n/128,b] (sum_{k in block b} a[m,k] b[n,k])
+//
+// The inner sum is one accumulation of the tensor cores (exact products of e4m3 values,
+// 32-bit sums); the outer one multiplies by arbitrary 32-bit scales, which the tensor
+// cores cannot do, so every block's accumulator goes through registers: see the product
+// kernel.
+#include <algorithm>
+#include <mutex>
+
+#include "tuna_fp8.h"
+#include "tuna_ops.cuh"
+
+namespace tuna_ops {
+namespace {
+
+// ---- quantisation --------------------------------------------------------------------------
+//
+// Bound by memory: two bytes (bf16) read and one written a value.  Blocks along the row: 8
+// lanes a block of 128 columns, 16 columns a lane (two 16-byte loads of bf16, one 16-byte
+// store), so a warp takes 512 columns of a row and the largest magnitude costs three shuffles.
+struct QuantArgs {
+  const void *x;
+  int64_t rows, ldx, ldq, in_rows;
+  int cols, vec;
+  const int64_t *gather;
+  uint8_t *q;
+  float *scale;
+};
+template <typename T>
+__global__ void __launch_bounds__(256) tuna_quantize_rows_kernel(QuantArgs a) {
+  wait_previous();
+  allow_next();
+  const int parts = (a.cols + 511) / 512;
+  const int lane = threadIdx.x & 31;
+  for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < a.rows * parts; i += (int64_t)gridDim.x * 8) {
+    const int64_t r = i / parts;
+    const int c = (int)(i - r * parts) * 512 + lane * 16;
+    const int64_t from = a.gather ? a.gather[r] : r;
+    const bool there = from >= 0 && from < a.in_rows;
+    const T *x = reinterpret_cast<const T *>(a.x) + (there ? from : 0) * a.ldx + c;
+    float v[16];
+    if (there && a.vec && c + 16 <= a.cols) {
+      load_row(x, v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) v[j] = there && c + j < a.cols ? to_f32(x[j]) : 0.0f;
+    }
+    uint32_t amax = 0;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) amax = max(amax, abs_bits(v[j]));
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) amax = max(amax, __shfl_xor_sync(~0u, amax, d));
+    const float s = fp8_scale(amax);
+    if (c < a.cols) {
+      uint4 u;
+      u.x = fp8_quad(v[0], v[1], v[2], v[3], s), u.y = fp8_quad(v[4], v[5], v[6], v[7], s);
+      u.z = fp8_quad(v[8], v[9], v[10], v[11], s), u.w = fp8_quad(v[12], v[13], v[14], v[15], s);
+      *reinterpret_cast<uint4 *>(a.q + r * a.ldq + c) = u;
+      if (lane % 8 == 0) a.scale[(int64_t)(c / 128) * a.rows + r] = s;
+    }
+  }
+}
+
+// Blocks that span rows: a 128 x 128 tile goes through shared memory.
+enum { kColumns = 1, kTiles = 2, kTilesT = 3 };
+constexpr int kTilePitch = 129;  // words: columns and rows of the tile are both free of bank conflicts
+constexpr size_t kTileSmem = (size_t)128 * kTilePitch * 4;
+template <int MODE, typename T>
+__global__ void __launch_bounds__(256) tuna_quantize_tile_kernel(QuantArgs a) {
+  extern __shared__ float tile[];
+  __shared__ uint32_t part[256];
+  wait_previous();
+  allow_next();
+  const int col_tiles = (a.cols + 127) / 128;
+  const int64_t r0 = (int64_t)(blockIdx.x / col_tiles) * 128;
+  const int c0 = (int)(blockIdx.x % col_tiles) * 128;
+  const int tid = threadIdx.x, lane = tid & 31;
+  uint32_t amax = 0;
+  for (int r = tid >> 5; r < 128; r += 8) {
+    const int c = c0 + lane * 4;
+    const T *x = reinterpret_cast<const T *>(a.x) + (r0 + r) * a.ldx + c;
+    float v[4] = {};
+    if (r0 + r < a.rows) {
+      if (a.vec && c + 4 <= a.cols) {
+        if constexpr (sizeof(T) == 2) {
+          const uint2 u = *reinterpret_cast<const uint2 *>(x);
+          v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xffff0000u);
+          v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xffff0000u);
+        } else {
+          load_row(x, v);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (c + j < a.cols) v[j] = to_f32(x[j]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      tile[r * kTilePitch + lane * 4 + j] = v[j];
+      if (MODE != kColumns) amax = max(amax, abs_bits(v[j]));
+    }
+  }
+  if (MODE != kColumns) {
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) amax = max(amax, __shfl_xor_sync(~0u, amax, d));
+    if (lane == 0) part[tid >> 5] = amax;
+  }
+  __syncthreads();
+  const int i = tid & 127, half = tid >> 7;  // the output row of this tile, and which 64 values of it
+  if (MODE == kColumns) {
+#pragma unroll 16
+    for (int r = 0; r < 64; ++r) amax = max(amax, abs_bits(tile[(half * 64 + r) * kTilePitch + i]));
+    part[tid] = amax;
+    __syncthreads();
+    amax = max(part[i], part[i + 128]);
+  } else {
+    amax = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) amax = max(amax, part[w]);
+  }
+  const float s = fp8_scale(amax);
+  const bool turned = MODE != kTiles;
+  const int64_t out_row = (turned ? c0 : r0) + i, out_rows = turned ? a.cols : a.rows;
+  const int64_t out_col = (turned ? r0 : c0) + half * 64, out_cols = turned ? a.rows : a.cols;
+  if (MODE == kColumns) {
+    if (half == 0 && out_row < out_rows) a.scale[(r0 / 128) * a.cols + out_row] = s;
+  } else if (tid == 0) {
+    a.scale[MODE == kTiles ? (r0 / 128) * col_tiles + c0 / 128 : (c0 / 128) * ((a.rows + 127) / 128) + r0 / 128] = s;
+  }
+  if (out_row >= out_rows) return;
+#pragma unroll
+  for (int j = 0; j < 64; j += 16) {
+    if (out_col + j >= out_cols) break;
+    float v[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = turned ? tile[(half * 64 + j + e) * kTilePitch + i] : tile[i * kTilePitch + half * 64 + j + e];
+    uint4 u;
+    u.x = fp8_quad(v[0], v[1], v[2], v[3], s), u.y = fp8_quad(v[4], v[5], v[6], v[7], s);
+    u.z = fp8_quad(v[8], v[9], v[10], v[11], s), u.w = fp8_quad(v[12], v[13], v[14], v[15], s);
+    *reinterpret_cast<uint4 *>(a.q + out_row * a.ldq + out_col + j) = u;
+  }
+}
+
+// ---- the product -----------------------------------------------------------------------------
+//
+// A persistent block takes tiles of 128 x BN.  One warp copies 128 x 128 blocks of a and BN x
+// 128 blocks of b into a ring of stages; one thread issues the four tensor-core steps of a
+// block into one of two accumulators in tensor memory; eight warps read a finished accumulator
+// back, multiply it by sa * sb and add it to the 32-bit sums they keep in registers (128 a
+// thread at BN = 256), while the tensor cores fill the other one.  At BN = 256 a block keeps
+// the tensor cores busy for 512 cycles and the promotion needs 128 KB of tensor-memory reads
+// and 64 packed multiply-adds a thread, about half of that.
+//
+// With `swiglu` the 256 columns are 2 x (64 gate + 64 up) rows of the two matrices, so that the
+// thread that holds a gate value holds its up value, and a tile is exactly one 128-block of the
+// result: it leaves as e4m3 with its scale, and the 32-bit product never reaches memory.
+struct TileArgs {
+  ProductArgs p;
+  int blocks;   // of k
+  int n_tiles;
+  int *error;
+};
+
+constexpr int kGemmThreads = 384;
+constexpr int kMaxGroups = TUNA_MOE_MAX_EXPERTS;
+
+template <int BN>
+struct Shape {
+  static constexpr int kStages = BN == 256 ? 4 : 6;
+  static constexpr int kStageBytes = 128 * 128 + BN * 128;
+  static constexpr int kCols = BN / 2;  // accumulator columns of a thread
+  // stages, then the groups' tile offsets, a copy of the second operand's scales for each of the
+  // eight warps and two blocks, the rows' largest magnitudes, barriers and flags
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + (kMaxGroups + 4) * 4 + 8 * 2 * 128 * 4 + 256 * 4 + 256;
+};
+
+// Tile t of the walk: the group it is in (never walked backwards), its rows and columns.
+struct Walk {
+  int g = 0;
+  int64_t row, end;  // first row, end of the group's rows
+  int n0;
+};
+__device__ __forceinline__ void walk_to(Walk &w, int64_t t, const TileArgs &a, const int *tile_base, int bn) {
+  while (t >= (int64_t)tile_base[w.g + 1] * a.n_tiles) ++w.g;
+  const int mt = tile_base[w.g + 1] - tile_base[w.g];
+  const int64_t local = t - (int64_t)tile_base[w.g] * a.n_tiles;
+  const int n = (int)(local / mt), m = (int)(local - (int64_t)n * mt);  // rows fastest: blocks that run together share b
+  int64_t begin = 0;
+  w.end = a.p.m;
+  if (a.p.offsets) begin = max(a.p.offsets[w.g], (int64_t)0), w.end = min(a.p.offsets[w.g + 1], a.p.m);
+  w.row = begin + (int64_t)m * 128;
+  w.n0 = n * bn;
+}
+
+template <int BN, bool SWIGLU, bool B_ROWS, typename TO>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+    tuna_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const TileArgs a) {
+  using S = Shape<BN>;
+  extern __shared__ char smem_raw[];
+  char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+  int *tile_base = (int *)(smem + (size_t)S::kStages * S::kStageBytes);
+  float *col_scale = (float *)(tile_base + kMaxGroups + 4);  // [8 warps][2][128]
+  uint32_t *row_amax = (uint32_t *)(col_scale + 2048);       // [256]
+  uint64_t *bars = (uint64_t *)(((uintptr_t)(row_amax + 256) + 7) & ~(uintptr_t)7);
+  volatile int *given_up = (volatile int *)(bars + 2 * S::kStages + 5);
+  volatile int *lost = given_up + 1;  // an eighth of the promotion gave up
+  uint32_t *tmem_at = (uint32_t *)(given_up + 2);
+  const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages, freed = done + 16, drained = freed + 16;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S::kStages; ++s) mbar_init(full + 8 * s, 1), mbar_init(empty + 8 * s, 1);
+    for (int s = 0; s < 2; ++s) mbar_init(done + 8 * s, 1), mbar_init(freed + 8 * s, 8);
+    mbar_init(drained, 1);
+    *given_up = 0, *lost = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 2) tmem_alloc(smem_u32(tmem_at), 2 * BN);
+  wait_previous();
+  allow_next();
+  // tiles of rows before each group
+  if (warp == 1) {
+    int sum = 0;
+    for (int g0 = 0; g0 < a.p.groups; g0 += 32) {
+      const int g = g0 + lane;
+      int64_t rows = 0;
+      if (g < a.p.groups) rows = a.p.offsets ? min(a.p.offsets[g + 1], a.p.m) - max(a.p.offsets[g], (int64_t)0) : a.p.m;
+      const int mt = rows > 0 ? (int)((rows + 127) / 128) : 0;
+      int x = mt;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(~0u, x, d);
+        if (lane >= d) x += y;
+      }
+      if (g < a.p.groups) tile_base[g] = sum + x - mt;
+      sum += __shfl_sync(~0u, x, 31);
+    }
+    if (lane == 0) tile_base[a.p.groups] = sum;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_at;
+  const int64_t tiles = (int64_t)tile_base[a.p.groups] * a.n_tiles;
+  const int blocks = a.blocks;
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp == 0 && lane == 0) {
+      // ---- copies
+      int stage = 0, phase = 0;
+      int64_t issued = 0;
+      Walk w;
+      bool ok = true;
+      for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+        walk_to(w, t, a, tile_base, SWIGLU ? BN / 2 : BN);
+        for (int kb = 0; kb < blocks; ++kb) {
+          if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, given_up))) break;
+          const uint32_t at = smem_u32(smem) + stage * S::kStageBytes, bar = full + 8 * stage;
+          mbar_expect(bar, S::kStageBytes);
+          tma_load_2d(at, &map_a, kb * 128, (int)w.row, bar);
+          if (SWIGLU) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              tma_load_3d(at + 128 * 128 + q * 64 * 128, &map_b, kb * 128, w.n0 + (q >> 1) * 64, w.g * 2 + (q & 1), bar);
+          } else {
+            tma_load_3d(at + 128 * 128, &map_b, kb * 128, w.n0, w.g, bar);
+          }
+          ++issued;
+          if (++stage == S::kStages) stage = 0, phase ^= 1;
+        }
+      }
+      if (!ok) {  // given up: nothing may land in shared memory after the block has gone
+        int never = 0;
+        for (int64_t i = max((int64_t)0, issued - S::kStages); i < issued; ++i)
+          mbar_wait(full + 8 * (int)(i % S::kStages), (uint32_t)((i / S::kStages) & 1), &never);
+      }
+    } else if (warp == 1 && lane == 0) {
+      // ---- tensor cores
+      constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);  // f32 sums of e4m3 products
+      int stage = 0, phase = 0, buf = 0, buf_phase = 0;
+      bool ok = true;
+      for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+        for (int kb = 0; kb < blocks; ++kb) {
+          if (!(ok = mbar_wait(freed + 8 * buf, buf_phase ^ 1, given_up) && mbar_wait(full + 8 * stage, phase, given_up))) break;
+          tc_fence_after();
+          const uint32_t at = smem_u32(smem) + stage * S::kStageBytes;
+          const uint64_t da = tc_desc(at), db = tc_desc(at + 128 * 128);
+#pragma unroll
+          for (int s = 0; s < 4; ++s) tc_mma_fp8(tmem + buf * BN, da + 2 * s, db + 2 * s, idesc, s > 0);  // 32 bytes along k
+          tc_commit(empty + 8 * stage);
+          tc_commit(done + 8 * buf);
+          if (++stage == S::kStages) stage = 0, phase ^= 1;
+          if (++buf == 2) buf = 0, buf_phase ^= 1;
+        }
+      }
+      if (!ok) {
+        int never = 0;
+        tc_commit(drained);
+        mbar_wait(drained, 0, &never);
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    // ---- promotion and results: thread = one row, columns [half * kCols, ...) of the tile
+    const int half = (warp - 4) >> 2, row_in = (warp & 3) * 32 + lane;
+    float *my_scale = col_scale + (warp - 4) * 256;
+    const uint32_t from = tmem + ((uint32_t)((warp & 3) * 32) << 16) + half * S::kCols;
+    int buf = 0, buf_phase = 0;
+    bool ok = true;
+    Walk w;
+    for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+      walk_to(w, t, a, tile_base, SWIGLU ? BN / 2 : BN);
+      const int64_t row = w.row + row_in;
+      const bool there = row < w.end;
+      const float *sa = a.p.sa + (there ? row : w.row);
+      // scales of this thread's columns: one a block of k, or with SWIGLU one for each matrix
+      const int tiles_n = (a.p.n + 127) / 128;
+      const float *sb0 = a.p.sb, *sb1 = a.p.sb;
+      if (SWIGLU) {
+        sb0 += ((int64_t)(w.g * 2) * tiles_n + w.n0 / 128) * blocks;
+        sb1 = sb0 + (int64_t)tiles_n * blocks;
+      } else if (!B_ROWS) {
+        const int nt = min((w.n0 + half * S::kCols) / 128, tiles_n - 1);
+        sb0 += ((int64_t)w.g * tiles_n + nt) * blocks;
+      }
+      int col[4];  // B_ROWS: the columns whose scales this lane fetches for its warp
+#pragma unroll
+      for (int j = 0; j < 4; ++j) col[j] = min(w.n0 + half * S::kCols + lane + j * 32, a.p.n - 1);
+      uint64_t acc[S::kCols / 2];
+#pragma unroll
+      for (int i = 0; i < S::kCols / 2; ++i) acc[i] = 0;
+      float fa = sa[0], fb = sb0[0], fc = SWIGLU ? sb1[0] : 0.0f, fd[4];
+      if (B_ROWS) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) fd[j] = sb0[col[j]];
+      }
+      for (int kb = 0; kb < blocks; ++kb) {
+        const float ra = fa, rb = fb, rc = fc;
+        if (B_ROWS) {  // (the warp's last reads of this half were two blocks ago)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) my_scale[buf * 128 + lane + j * 32] = fd[j];
+          __syncwarp();
+        }
+        if (kb + 1 < blocks) {  // the next block's scales travel while this one is added
+          fa = sa[(int64_t)(kb + 1) * a.p.m];
+          if (B_ROWS) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) fd[j] = sb0[(int64_t)(kb + 1) * a.p.n + col[j]];
+          } else {
+            fb = sb0[kb + 1];
+          }
+          if (SWIGLU) fc = sb1[kb + 1];
+        }
+        ok = __all_sync(~0u, mbar_wait(done + 8 * buf, buf_phase, given_up));  // (and the warp is whole for the loads)
+        if (!ok) break;
+        tc_fence_after();
+        const float s0 = ra * rb, s1 = ra * rc;
+        const uint64_t p0 = B_ROWS ? pair(ra, ra) : pair(s0, s0), p1 = pair(s1, s1);
+        uint32_t v[2][32];
+        tmem_load32(from + buf * BN, v[0]);
+#pragma unroll
+        for (int c = 0; c < S::kCols / 32; ++c) {
+          tmem_wait(v[c & 1]);
+          if (c + 1 < S::kCols / 32) tmem_load32(from + buf * BN + (c + 1) * 32, v[(c + 1) & 1]);
+          if (c + 1 == S::kCols / 32) {  // everything is in registers: the accumulator may be filled again
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(freed + 8 * buf);
+          }
+          uint32_t(&x)[32] = v[c & 1];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            uint64_t s = SWIGLU && c >= 2 ? p1 : p0;
+            if (B_ROWS) {
+              const float2 f = *reinterpret_cast<const float2 *>(my_scale + buf * 128 + c * 32 + i * 2);
+              s = mul2(p0, pair(f.x, f.y));
+            }
+            acc[c * 16 + i] = fma2(pair(x[2 * i], x[2 * i + 1]), s, acc[c * 16 + i]);
+          }
+        }
+        if (++buf == 2) buf = 0, buf_phase ^= 1;
+      }
+      if constexpr (!SWIGLU) {
+        if (!ok) break;
+      } else {
+        if (!ok) *lost = 1;  // told before the barrier that the eight warps share: they leave together
+        // columns 0..63: gate, 64..127: up of the same 64 places
+        float h[64];
+        uint32_t amax = 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          float g[2], u[2];
+          unpair(acc[i], g[0], g[1]);
+          unpair(acc[32 + i], u[0], u[1]);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const float x = g[j] / (1.0f + expf(-g[j])) * u[j];
+            h[2 * i + j] = x;
+            amax = max(amax, abs_bits(x));
+          }
+        }
+        row_amax[half * 128 + row_in] = amax;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (*lost) break;
+        amax = max(amax, row_amax[(half ^ 1) * 128 + row_in]);
+        asm volatile("bar.sync 1, 256;" ::: "memory");  // before the next tile's values
+        const float s = fp8_scale(amax);
+        if (there) {
+          if (half == 0) a.p.hs[(int64_t)(w.n0 / 128) * a.p.m + row] = s;
+          uint8_t *out = (uint8_t *)a.p.out + row * a.p.ldo + w.n0 + half * 64;  // (the pitch covers whole blocks)
+#pragma unroll
+          for (int i = 0; i < 64; i += 16) {
+            uint4 q;
+            q.x = fp8_quad(h[i], h[i + 1], h[i + 2], h[i + 3], s), q.y = fp8_quad(h[i + 4], h[i + 5], h[i + 6], h[i + 7], s);
+            q.z = fp8_quad(h[i + 8], h[i + 9], h[i + 10], h[i + 11], s), q.w = fp8_quad(h[i + 12], h[i + 13], h[i + 14], h[i + 15], s);
+            *reinterpret_cast<uint4 *>(out + i) = q;
+          }
+        }
+      }
+      if constexpr (!SWIGLU) {
+        if (there) {
+          TO *out = (TO *)a.p.out + row * a.p.ldo;
+          const int c0 = w.n0 + half * S::kCols;
+          const bool vec = (((uintptr_t)a.p.out | (uint64_t)a.p.ldo * sizeof(TO)) & 15) == 0;
+#pragma unroll
+          for (int i = 0; i < S::kCols; i += 8) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) unpair(acc[i / 2 + j], v[2 * j], v[2 * j + 1]);
+            if (vec && c0 + i + 8 <= a.p.n) {
+              store_row(out + c0 + i, v);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (c0 + i + j < a.p.n) out[c0 + i + j] = from_f32<TO>(v[j]);
+            }
+          }
+        }
+      }
+      __syncwarp();
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 2) tmem_free(tmem, 2 * BN);
+  if (threadIdx.x == 0 && *given_up) *a.error = 1;
+}
+
+// ---- host ------------------------------------------------------------------------------------
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                 CUtensorMapFloatOOBfill);
+EncodeTiled encoder() {
+  static std::mutex m;
+  static EncodeTiled fn = nullptr;
+  std::lock_guard<std::mutex> lock(m);
+  if (!fn) {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (!note_cuda(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found)) &&
+        found == cudaDriverEntryPointSuccess)
+      fn = (EncodeTiled)p;
+  }
+  return fn;
+}
+
+// An e4m3 operand: k contiguous, then rows, then matrices; boxes of 128 x `box` rows.
+int make_map(CUtensorMap *map, int rank, const void *p, int64_t k, int64_t rows, int64_t matrices, int64_t ld, int box) {
+  EncodeTiled f = encoder();
+  if (!f) return TUNA_ERR_CUDA;
+  const cuuint64_t dims[3] = {(cuuint64_t)k, (cuuint64_t)rows, (cuuint64_t)matrices};
+  const cuuint64_t strides[2] = {(cuuint64_t)ld, (cuuint64_t)(ld * rows)};
+  const cuuint32_t boxes[3] = {128, (cuuint32_t)box, 1}, ones[3] = {1, 1, 1};
+  const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, (cuuint32_t)rank, const_cast<void *>(p), dims, strides, boxes, ones,
+                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? TUNA_OK : note_cuda(cudaErrorInvalidValue);
+}
+
+// Dynamic shared memory above the default needs the kernel's leave, once a device.
+template <typename K>
+int allow_smem(K kernel, size_t bytes, bool (&set)[64]) {
+  static std::mutex m;
+  int dev = 0;
+  if (const int rc = note_cuda(cudaGetDevice(&dev))) return rc;
+  std::lock_guard<std::mutex> lock(m);
+  if (dev >= 0 && dev < 64 && set[dev]) return TUNA_OK;
+  if (const int rc = note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes))) return rc;
+  if (dev >= 0 && dev < 64) set[dev] = true;
+  return TUNA_OK;
+}
+
+template <int BN, bool SWIGLU, bool B_ROWS, typename TO>
+int run_tiles(const ProductArgs &p, cudaStream_t st) {
+  TileArgs a = {};
+  a.p = p;
+  a.blocks = (int)ceil_div(p.k, 128);
+  a.n_tiles = (int)ceil_div(p.n, SWIGLU ? BN / 2 : BN);
+  a.error = error_word();
+  if (!a.error) return TUNA_ERR_CUDA;
+  CUtensorMap ma, mb;
+  if (const int rc = make_map(&ma, 2, p.a, p.k, p.m, 1, p.lda, 128)) return rc;
+  if (const int rc = make_map(&mb, 3, p.b, p.k, p.n, (int64_t)p.groups * (SWIGLU ? 2 : 1), p.ldb, SWIGLU ? 64 : BN)) return rc;
+  static bool set[64] = {};
+  auto kernel = tuna_product_kernel<BN, SWIGLU, B_ROWS, TO>;
+  if (const int rc = allow_smem(kernel, Shape<BN>::kSmem, set)) return rc;
+  const int64_t most = (ceil_div(p.m, 128) + (p.offsets ? p.groups : 0)) * a.n_tiles;
+  return launch(kernel, dim3((unsigned)std::min<int64_t>(most, sm_count())), kGemmThreads, Shape<BN>::kSmem, st, false, ma, mb, a);
+}
+
+size_t dtype_size(int dtype) { return dtype == TUNA_DTYPE_F32 ? 4 : dtype == TUNA_DTYPE_BF16 ? 2 : 0; }
+
+template <int MODE, typename T>
+int run_quantize_tiles(const QuantArgs &a, cudaStream_t st) {
+  static bool set[64] = {};
+  if (const int rc = allow_smem(tuna_quantize_tile_kernel<MODE, T>, kTileSmem, set)) return rc;
+  return launch(tuna_quantize_tile_kernel<MODE, T>, dim3((unsigned)(ceil_div(a.rows, 128) * ceil_div(a.cols, 128))), 256, kTileSmem, st, false, a);
+}
+
+}  // namespace
+
+int launch_product(const ProductArgs &p, cudaStream_t st) {
+  if (p.swiglu) return run_tiles<256, true, false, uint8_t>(p, st);
+  const int64_t wide = (ceil_div(p.m, 128) + (p.offsets ? p.groups - 1 : 0)) * ceil_div(p.n, 256);
+  if (p.b_rows) {
+    if (p.out_f32) return run_tiles<256, false, true, float>(p, st);
+    return run_tiles<256, false, true, __nv_bfloat16>(p, st);
+  }
+  if (wide >= sm_count()) {
+    if (p.out_f32) return run_tiles<256, false, false, float>(p, st);
+    return run_tiles<256, false, false, __nv_bfloat16>(p, st);
+  }
+  if (p.out_f32) return run_tiles<128, false, false, float>(p, st);
+  return run_tiles<128, false, false, __nv_bfloat16>(p, st);
+}
+
+int launch_quantize_rows(const void *x, bool f32, int64_t rows, int cols, int64_t ldx, const int64_t *gather, int64_t in_rows,
+                         void *q, int64_t ldq, float *scale, cudaStream_t st) {
+  QuantArgs a = {};
+  a.x = x, a.rows = rows, a.cols = cols, a.ldx = ldx, a.gather = gather, a.in_rows = in_rows, a.q = (uint8_t *)q, a.ldq = ldq, a.scale = scale;
+  a.vec = aligned(x, 16) && ldx * (f32 ? 4 : 2) % 16 == 0;
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(rows * ceil_div(cols, 512), 8), (int64_t)sm_count() * 32));
+  return f32 ? launch(tuna_quantize_rows_kernel<float>, grid, 256, 0, st, false, a)
+             : launch(tuna_quantize_rows_kernel<__nv_bfloat16>, grid, 256, 0, st, false, a);
+}
+
+}  // namespace tuna_ops
+
+using namespace tuna_ops;
+
+extern "C" {
+
+int tuna_fp8_quantize(const void *x, int dtype, int64_t rows, int cols, int64_t ldx, int layout, void *q, int64_t ldq, float *scale,
+                      void *stream) {
+  const size_t size = dtype_size(dtype);
+  if (!size || rows < 0 || cols < 0 || ldx < cols || layout < TUNA_FP8_ROWS || layout > TUNA_FP8_TILES_T) return TUNA_ERR_INVALID_ARG;
+  const bool turned = layout == TUNA_FP8_COLUMNS || layout == TUNA_FP8_TILES_T;
+  if (ldq < (turned ? rows : cols) || ldq % 16 != 0) return TUNA_ERR_INVALID_ARG;
+  if (cols > kMaxDim || (turned && rows > kMaxDim) || ceil_div(rows, 128) * ceil_div(cols, 128) > INT32_MAX) return TUNA_ERR_RANGE;
+  if (rows == 0 || cols == 0) return TUNA_OK;
+  if (!x || !q || !scale || !aligned(x, size) || !aligned(q, 16) || !aligned(scale, 4)) return TUNA_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (layout == TUNA_FP8_ROWS) return launch_quantize_rows(x, dtype == TUNA_DTYPE_F32, rows, cols, ldx, nullptr, rows, q, ldq, scale, st);
+  QuantArgs a = {};
+  a.x = x, a.rows = rows, a.cols = cols, a.ldx = ldx, a.q = (uint8_t *)q, a.ldq = ldq, a.scale = scale;
+  a.vec = aligned(x, 4 * size) && ldx % 4 == 0;
+  const bool f32 = dtype == TUNA_DTYPE_F32;
+  if (layout == TUNA_FP8_COLUMNS)
+    return f32 ? run_quantize_tiles<kColumns, float>(a, st) : run_quantize_tiles<kColumns, __nv_bfloat16>(a, st);
+  if (layout == TUNA_FP8_TILES) return f32 ? run_quantize_tiles<kTiles, float>(a, st) : run_quantize_tiles<kTiles, __nv_bfloat16>(a, st);
+  return f32 ? run_quantize_tiles<kTilesT, float>(a, st) : run_quantize_tiles<kTilesT, __nv_bfloat16>(a, st);
+}
+
+int tuna_fp8_matmul(const void *a, const float *a_scale, int64_t m, int64_t lda, const void *b, const float *b_scale, int b_layout, int n,
+                    int64_t ldb, int k, int groups, const int64_t *offsets, void *out, int out_dtype, int64_t ldo, void *stream) {
+  const size_t so = dtype_size(out_dtype);
+  if (!so || m < 0 || n < 0 || k < 0 || groups < 1 || lda < k || ldb < k || ldo < n || lda % 16 || ldb % 16) return TUNA_ERR_INVALID_ARG;
+  if (b_layout != TUNA_FP8_TILES && b_layout != TUNA_FP8_ROWS) return TUNA_ERR_INVALID_ARG;
+  if ((groups > 1 && !offsets) || (b_layout == TUNA_FP8_ROWS && offsets)) return TUNA_ERR_INVALID_ARG;
+  if (groups > TUNA_MOE_MAX_EXPERTS || n > kMaxDim || k > kMaxDim || m > INT32_MAX - 256) return TUNA_ERR_RANGE;
+  if ((ceil_div(m, 128) + groups) > INT32_MAX / std::max<int64_t>(1, ceil_div(n, 128))) return TUNA_ERR_RANGE;
+  if (m == 0 || n == 0) return TUNA_OK;
+  if (!out || !aligned(out, so)) return TUNA_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (k == 0) return note_cuda(cudaMemset2DAsync(out, ldo * so, 0, n * so, m, st));  // an empty sum
+  if (!a || !b || !a_scale || !b_scale || !aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 4) || !aligned(b_scale, 4)) return TUNA_ERR_INVALID_ARG;
+  ProductArgs p = {};
+  p.a = a, p.b = b, p.sa = a_scale, p.sb = b_scale, p.m = m, p.n = n, p.k = k, p.lda = lda, p.ldb = ldb, p.ldo = ldo;
+  p.groups = groups, p.offsets = offsets, p.b_rows = b_layout == TUNA_FP8_ROWS, p.out = out, p.out_f32 = out_dtype == TUNA_DTYPE_F32;
+  return launch_product(p, st);
+}
+
+}  // extern "C"

@@ -19,6 +19,7 @@ from . import binding as B
 SOFTMAX, SIGMOID = 0, 1
 SCORING = {"softmax": SOFTMAX, "sigmoid": SIGMOID}
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2}
+LAYOUTS = {"rows": 0, "columns": 1, "tiles": 2, "tiles_t": 3}
 FLOATS = (torch.float32, torch.bfloat16)
 
 
@@ -145,6 +146,75 @@ def combine_backward(dout, y, weights, pos, *, stream=None):
                                              y.shape[1], ldy, weights.data_ptr(), pos.data_ptr(), t, k, dy.data_ptr(), y.shape[1],
                                              dw.data_ptr(), B._stream(stream)), "tuna_moe_combine_backward")
     return dy, dw
+
+
+def _blocks(n):
+    return -(-n // 128)
+
+
+def fp8_quantize(x, layout="rows", *, stream=None):
+    """(q, scale): ``x`` in 8 bits with a scale for each block (``tuna_fp8_quantize``).
+
+    ``q`` of the layouts "columns" and "tiles_t" is that of the transposed matrix."""
+    ld = _matrix(x, "x", FLOATS)
+    if layout not in LAYOUTS:
+        raise ValueError(f"layout: one of {', '.join(LAYOUTS)}, got {layout!r}")
+    rows, cols = x.shape
+    out = (cols, rows) if layout in ("columns", "tiles_t") else (rows, cols)
+    pitch = (out[1] + 15) // 16 * 16
+    q = torch.empty(out[0], pitch, dtype=torch.float8_e4m3fn, device=x.device)
+    tiles = layout in ("tiles", "tiles_t")
+    scale = torch.empty((_blocks(out[0]), _blocks(out[1])) if tiles else (_blocks(out[1]), out[0]), dtype=torch.float32, device=x.device)
+    _check(B.lib().tuna_fp8_quantize(x.data_ptr(), DTYPES[x.dtype], rows, cols, ld, LAYOUTS[layout], q.data_ptr(), max(pitch, 16),
+                                     scale.data_ptr(), B._stream(stream)), "tuna_fp8_quantize")
+    return q[:, :out[1]], scale
+
+
+def _fp8_matrix(q, name):
+    """An e4m3 operand's pitch; copies one whose rows do not start on 16-byte boundaries."""
+    ld = _matrix(q, name, (torch.float8_e4m3fn,))
+    if q.shape[0] <= 1:
+        ld = (q.shape[1] + 15) // 16 * 16   # the pitch of a single row is free
+    if ld % 16 or q.data_ptr() % 16:
+        p = torch.zeros(q.shape[0], (q.shape[1] + 15) // 16 * 16, dtype=torch.uint8, device=q.device)
+        p[:, :q.shape[1]] = q.view(torch.uint8)
+        return p, p.shape[1]
+    return q, ld
+
+
+def fp8_matmul(a, a_scale, b, b_scale, *, offsets=None, b_blocks="tiles", out_dtype=torch.bfloat16, stream=None):
+    """a b^T with a scale for each block of 128 (``tuna_fp8_matmul``).
+
+    ``a`` [m, k] with "rows" scales.  ``b`` [n, k] with "tiles" scales, or "rows" scales
+    (``b_blocks="rows"``); or [groups, n, k] with ``offsets`` (int64 [groups + 1]): rows
+    offsets[g] .. offsets[g + 1] of ``a`` meet ``b[g]``."""
+    k = b.shape[-1]
+    if a.dim() != 2 or a.shape[1] != k:
+        raise ValueError(f"a: shape {tuple(a.shape)}, wanted (any, {k})")
+    m = a.shape[0]
+    a, lda = _fp8_matrix(a, "a")
+    if out_dtype not in FLOATS:
+        raise ValueError(f"out_dtype: one of {FLOATS}")
+    if b_blocks not in ("tiles", "rows"):
+        raise ValueError(f"b_blocks: tiles or rows, got {b_blocks!r}")
+    groups = 1
+    if offsets is not None:
+        if b.dim() != 3 or not b.is_contiguous() or b_blocks != "tiles":
+            raise ValueError("b: contiguous matrices [groups, n, k] with tile scales go with offsets")
+        groups, n = b.shape[:2]
+        _dense(offsets, "offsets", torch.int64, (groups + 1,))
+        flat, ldb = _fp8_matrix(b.view(groups * n, k), "b")
+    else:
+        n = b.shape[0]
+        flat, ldb = _fp8_matrix(b, "b")
+    _dense(a_scale, "a_scale", torch.float32, (_blocks(k), m))
+    tiles = (groups, _blocks(n), _blocks(k)) if offsets is not None else (_blocks(n), _blocks(k))
+    _dense(b_scale, "b_scale", torch.float32, (_blocks(k), n) if b_blocks == "rows" else tiles)
+    out = torch.empty(m, n, dtype=out_dtype, device=a.device)
+    _check(B.lib().tuna_fp8_matmul(a.data_ptr(), a_scale.data_ptr(), m, max(lda, 16), flat.data_ptr(), b_scale.data_ptr(), LAYOUTS[b_blocks], n,
+                                   max(ldb, 16), k, groups, None if offsets is None else offsets.data_ptr(), out.data_ptr(),
+                                   DTYPES[out_dtype], max(n, 1), B._stream(stream)), "tuna_fp8_matmul")
+    return out
 
 
 def device_status() -> int:
