@@ -613,6 +613,56 @@ int tuna_fp8_matmul(const void *a, const float *a_scale, int64_t m, int64_t lda,
                     const float *b_scale, int b_layout, int n, int64_t ldb, int k, int groups,
                     const int64_t *offsets, void *out, int out_dtype, int64_t ldo, void *stream);
 
+/*
+ * tuna_moe_experts - the experts of many tokens, weights and products in 8 bits:
+ *   out[t] = sum over s of weights[t][s] * (h Wd[e]^T),  e = ids[t][s],
+ *   h = silu(x[t] Wg[e]^T) * (x[t] Wu[e]^T), with x and h rounded to 8 bits in blocks of
+ *   1 x 128 (tuna_fp8_quantize) and each expert's row rounded to bf16 before the sum.
+ *   x, out   tokens x hidden, bf16.  ids (int32), weights (f32): tokens x k; ids outside
+ *            [0, experts) add nothing.
+ *   w13      experts x 2 x inter x hidden, e4m3: the gate matrix, then the up matrix;
+ *   s13      experts x 2 x ceil(inter/128) x ceil(hidden/128);
+ *   w2, s2   experts x hidden x inter and experts x ceil(hidden/128) x ceil(inter/128).
+ *   hidden and inter are multiples of 16; weights start on 16-byte boundaries.
+ * tuna_moe_expert_rows - the same for rows that are in expert order already, as a token
+ * dispatch leaves them: rows [offsets[e], offsets[e+1]) of x (DEVICE, experts + 1) meet
+ * expert e, and the row of y (bf16) is its result; other rows of y are not written.
+ * Limits: experts <= TUNA_MOE_MAX_EXPERTS, rows (tokens * k) <= 2^24, hidden, inter <= 2^20.
+ */
+int tuna_moe_expert_rows_workspace_bytes(int64_t rows, int hidden, int inter, size_t *bytes);
+int tuna_moe_expert_rows(const void *x, int64_t ldx, int64_t rows, int experts,
+                         const int64_t *offsets, int hidden, int inter, const void *w13,
+                         const float *s13, const void *w2, const float *s2, void *y, int64_t ldy,
+                         void *workspace, size_t workspace_bytes, void *stream);
+int tuna_moe_experts_workspace_bytes(int64_t tokens, int experts, int k, int hidden, int inter,
+                                     size_t *bytes);
+int tuna_moe_experts(const void *x, int64_t ldx, int64_t tokens, const int32_t *ids,
+                     const float *weights, int k, int experts, int hidden, int inter,
+                     const void *w13, const float *s13, const void *w2, const float *s2, void *out,
+                     int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * tuna_moe_few - a whole layer for a few tokens in one (cooperative) launch: logits
+ * x router^T, the choice as in tuna_moe_route, the experts, the weighted sum.
+ *   x        tokens x hidden, bf16, 16-byte aligned rows (ldx a multiple of 8);
+ *   router   experts x hidden, bf16, contiguous.
+ *   weight_dtype   TUNA_DTYPE_BF16, or TUNA_DTYPE_E4M3 with scales as in tuna_moe_experts
+ *            (then only the weights are in 8 bits: x and h keep at least bf16's precision).
+ *   ids, weights   tokens x k, receive the choice; may be NULL.
+ * The first `zeroed` bytes of the workspace must be zero before its first use; every call
+ * leaves them so (a call that gave up a wait, see tuna_ops_device_status, may not).  The
+ * workspace may serve calls of other sizes if it is large enough.
+ * Limits (TUNA_ERR_RANGE): tokens <= TUNA_MOE_FEW_MAX_TOKENS, hidden, inter <= 8192.
+ */
+#define TUNA_MOE_FEW_MAX_TOKENS 64
+int tuna_moe_few_workspace_bytes(int tokens, int experts, int k, int hidden, int inter,
+                                 size_t *bytes, size_t *zeroed);
+int tuna_moe_few(const void *x, int64_t ldx, int tokens, const void *router, int experts, int k,
+                 int scoring, int renormalize, float scale, int hidden, int inter,
+                 int weight_dtype, const void *w13, const float *s13, const void *w2,
+                 const float *s2, void *out, int64_t ldo, int32_t *ids, float *weights,
+                 void *workspace, size_t workspace_bytes, void *stream);
+
 /* Synchronises the device and reports in *gave_up (host) whether a kernel of these operators
  * abandoned a bounded wait; its outputs are then incomplete.  tuna_ops_cuda_error: the
  * cudaError_t behind this thread's latest TUNA_ERR_CUDA of these operators. */

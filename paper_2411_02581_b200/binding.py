@@ -91,6 +91,14 @@ SIGNATURES = {
                                                  _VP, _VP]),
     "tuna_fp8_quantize": (ctypes.c_int, [_VP, _INT, _I64, _INT, _I64, _INT, _VP, _I64, _VP, _VP]),
     "tuna_fp8_matmul": (ctypes.c_int, [_VP, _VP, _I64, _I64, _VP, _VP, _INT, _INT, _I64, _INT, _INT, _VP, _VP, _INT, _I64, _VP]),
+    "tuna_moe_expert_rows_workspace_bytes": (ctypes.c_int, [_I64, _INT, _INT, _SZP]),
+    "tuna_moe_expert_rows": (ctypes.c_int, [_VP, _I64, _I64, _INT, _VP, _INT, _INT] + [_VP] * 5 + [_I64, _VP, ctypes.c_size_t, _VP]),
+    "tuna_moe_experts_workspace_bytes": (ctypes.c_int, [_I64, _INT, _INT, _INT, _INT, _SZP]),
+    "tuna_moe_experts": (ctypes.c_int, [_VP, _I64, _I64, _VP, _VP, _INT, _INT, _INT, _INT] + [_VP] * 5
+                         + [_I64, _VP, ctypes.c_size_t, _VP]),
+    "tuna_moe_few_workspace_bytes": (ctypes.c_int, [_INT] * 5 + [_SZP, _SZP]),
+    "tuna_moe_few": (ctypes.c_int, [_VP, _I64, _INT, _VP, _INT, _INT, _INT, _INT, ctypes.c_float, _INT, _INT, _INT] + [_VP] * 5
+                     + [_I64, _VP, _VP, _VP, ctypes.c_size_t, _VP]),
     "tuna_ops_device_status": (ctypes.c_int, [_INTP]),
     "tuna_ops_cuda_error": (ctypes.c_int, []),
     "tuna_strerror": (ctypes.c_char_p, [ctypes.c_int]),

@@ -11,8 +11,8 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB_DIR = os.path.join(_HERE, "_lib")
 LIB_PATH = os.path.join(LIB_DIR, "libtuna.so")
 SOURCES = ["tuna_plan.cu", "tuna_api.cu", "tuna_static.cu", "tuna_shard.cu", "tuna_move.cu",
-           "tuna_route.cu", "tuna_fp8.cu"]
-HEADERS = [os.path.join(CSRC, h) for h in ("tuna_internal.h", "tuna_plan.h", "tuna_plan_kernels.cuh", "tuna_ops.cuh", "tuna_fp8.h")] + [
+           "tuna_route.cu", "tuna_fp8.cu", "tuna_moe.cu", "tuna_few.cu"]
+HEADERS = [os.path.join(CSRC, h) for h in ("tuna_internal.h", "tuna_plan.h", "tuna_plan_kernels.cuh", "tuna_ops.cuh", "tuna_fp8.h", "tuna_route.cuh")] + [
     os.path.join(ROOT, "include", "tuna.h")]
 
 

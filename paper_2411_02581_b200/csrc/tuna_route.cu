@@ -7,7 +7,9 @@
 #include <algorithm>
 #include <mutex>
 
+#include "tuna_fp8.h"
 #include "tuna_ops.cuh"
+#include "tuna_route.cuh"
 
 namespace tuna_ops {
 
@@ -47,27 +49,7 @@ int *error_word() {
 
 namespace {
 
-constexpr int kMaxK = 32;
 constexpr int kTopThreads = 256;
-
-// What a router makes of a logit.  A NaN is a masked place, like -inf: never chosen.
-__device__ __forceinline__ float logit_of(float v) { return v != v ? -INFINITY : v; }
-// exp(z - m) where both may be infinite: the places that hold +inf share the weight.
-__device__ __forceinline__ float exp_of(float z, float m) { return z == m ? 1.0f : expf(z - m); }
-__device__ __forceinline__ float sigmoid_of(float z) { return 1.0f / (1.0f + expf(-z)); }
-
-// A token's logits, VPL a lane in a group of LPT lanes: lane l holds experts l*VPL ...
-template <int VPL, typename T>
-__device__ __forceinline__ void load_logits(const T *row, int first, int experts, bool vec, float (&z)[VPL]) {
-  if (vec && first + VPL <= experts) {
-    load_row(row + first, z);
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) z[i] = logit_of(z[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) z[i] = first + i < experts ? logit_of(to_f32(row[first + i])) : -INFINITY;
-  }
-}
 
 struct RouteArgs {
   const void *logits;
@@ -77,53 +59,6 @@ struct RouteArgs {
   int32_t *ids;
   float *weights;
 };
-
-// The choice for one token by its group of LPT lanes; lane s of the group leaves with slot s
-// (k <= LPT).  k rounds of an argmax: within a lane over its VPL values, then across lanes by
-// shuffles; ties go to the lower expert because a later one must be strictly larger.
-template <int LPT, int VPL>
-__device__ __forceinline__ void choose(float (&z)[VPL], int lane, int k, int scoring, int renormalize, float scale, int &id, float &weight) {
-  const int first = lane * VPL;
-  uint32_t taken = 0;
-  float mine = -INFINITY, top = -INFINITY;
-  id = -1;
-  for (int s = 0; s < k; ++s) {
-    float best = -INFINITY;
-    int at = 0;
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-      if (z[i] > best && !((taken >> i) & 1)) best = z[i], at = i;
-    }
-    int e = first + at;
-#pragma unroll
-    for (int d = 1; d < LPT; d <<= 1) {
-      const float ob = __shfl_xor_sync(~0u, best, d);
-      const int oe = __shfl_xor_sync(~0u, e, d);
-      if (ob > best || (ob == best && oe < e)) best = ob, e = oe;
-    }
-    if (s == 0) top = best;
-    if (best != -INFINITY) {  // (no early end: the other groups of the warp go on with the shuffles)
-      if (e >= first && e < first + VPL) taken |= 1u << (e - first);
-      if (s == lane) id = e, mine = best;
-    }
-  }
-  float w = 0.0f;
-  if (scoring == TUNA_MOE_SIGMOID) {
-    if (id >= 0) w = sigmoid_of(mine);
-  } else if (id >= 0) {
-    w = exp_of(mine, top);
-  }
-  float sum = w;
-  if (!renormalize && scoring == TUNA_MOE_SOFTMAX) {
-    sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) sum += z[i] == -INFINITY ? 0.0f : exp_of(z[i], top);
-  }
-#pragma unroll
-  for (int d = 1; d < LPT; d <<= 1) sum += __shfl_xor_sync(~0u, sum, d);
-  if (renormalize || scoring == TUNA_MOE_SOFTMAX) w = sum > 0.0f ? w / sum : 0.0f;
-  weight = id >= 0 ? w * scale : 0.0f;
-}
 
 // ---- the rows' order ---------------------------------------------------------------------
 //

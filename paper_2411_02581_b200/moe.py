@@ -217,6 +217,118 @@ def fp8_matmul(a, a_scale, b, b_scale, *, offsets=None, b_blocks="tiles", out_dt
     return out
 
 
+def _experts_weights(w13, s13, w2, s2, hidden):
+    """Checked shapes of 8-bit expert weights: (experts, inter)."""
+    if w13.dim() != 4 or w13.shape[1] != 2 or w13.shape[3] != hidden:
+        raise ValueError(f"w13: [experts, 2, inter, {hidden}] is wanted, got {tuple(w13.shape)}")
+    e, _, i, d = w13.shape
+    _dense(w13, "w13", torch.float8_e4m3fn, (e, 2, i, d))
+    _dense(s13, "s13", torch.float32, (e, 2, _blocks(i), _blocks(d)))
+    _dense(w2, "w2", torch.float8_e4m3fn, (e, d, i))
+    _dense(s2, "s2", torch.float32, (e, _blocks(d), _blocks(i)))
+    return e, i
+
+
+def _space(need, workspace, device):
+    if workspace is None:
+        return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+    return workspace
+
+
+def expert_rows(x, offsets, w13, s13, w2, s2, *, workspace=None, stream=None):
+    """Rows in expert order through their experts (``tuna_moe_expert_rows``); a row of the result that no expert has is undefined."""
+    ldx = _matrix(x, "x", (torch.bfloat16,))
+    rows, d = x.shape
+    e, i = _experts_weights(w13, s13, w2, s2, d)
+    _dense(offsets, "offsets", torch.int64, (e + 1,))
+    n = ctypes.c_size_t()
+    _check(B.lib().tuna_moe_expert_rows_workspace_bytes(rows, d, i, ctypes.byref(n)), "tuna_moe_expert_rows_workspace_bytes")
+    ws = _space(n.value, workspace, x.device)
+    y = torch.empty(rows, d, dtype=torch.bfloat16, device=x.device)
+    _check(B.lib().tuna_moe_expert_rows(x.data_ptr(), ldx, rows, e, offsets.data_ptr(), d, i, w13.data_ptr(), s13.data_ptr(), w2.data_ptr(),
+                                        s2.data_ptr(), y.data_ptr(), d, ws.data_ptr(), ws.numel(), B._stream(stream)), "tuna_moe_expert_rows")
+    return y
+
+
+def experts(x, ids, weights, w13, s13, w2, s2, *, workspace=None, stream=None):
+    """The experts of many tokens in 8 bits (``tuna_moe_experts``): ids and weights as :func:`route` makes them."""
+    ldx = _matrix(x, "x", (torch.bfloat16,))
+    t, d = x.shape
+    e, i = _experts_weights(w13, s13, w2, s2, d)
+    k = ids.shape[-1]
+    _dense(ids, "ids", torch.int32, (t, k))
+    _dense(weights, "weights", torch.float32, (t, k))
+    n = ctypes.c_size_t()
+    _check(B.lib().tuna_moe_experts_workspace_bytes(t, e, k, d, i, ctypes.byref(n)), "tuna_moe_experts_workspace_bytes")
+    ws = _space(n.value, workspace, x.device)
+    out = torch.empty(t, d, dtype=torch.bfloat16, device=x.device)
+    _check(B.lib().tuna_moe_experts(x.data_ptr(), ldx, t, ids.data_ptr(), weights.data_ptr(), k, e, d, i, w13.data_ptr(), s13.data_ptr(),
+                                    w2.data_ptr(), s2.data_ptr(), out.data_ptr(), d, ws.data_ptr(), ws.numel(), B._stream(stream)),
+           "tuna_moe_experts")
+    return out
+
+
+def few_workspace(tokens, experts, k, hidden, inter, device="cuda"):
+    """A workspace of :func:`few`, ready for use by one stream."""
+    n, z = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(B.lib().tuna_moe_few_workspace_bytes(tokens, experts, k, hidden, inter, ctypes.byref(n), ctypes.byref(z)),
+           "tuna_moe_few_workspace_bytes")
+    ws = torch.empty(max(n.value, 256), dtype=torch.uint8, device=device)
+    ws[:z.value].zero_()
+    return ws
+
+
+_few_spaces = {}  # (device, stream) -> workspaces that few() keeps: the last one serves, older ones may be held by graphs
+
+
+def few(x, router, k, w13, w2, *, s13=None, s2=None, scoring="softmax", renormalize=False, scale=1.0, ids=None, weights=None,
+        workspace=None, stream=None):
+    """A whole layer for at most 64 tokens in one launch (``tuna_moe_few``).
+
+    ``w13`` [experts, 2, inter, hidden] and ``w2`` [experts, hidden, inter] in bf16, or in
+    e4m3 with ``s13`` and ``s2``.  ``ids`` / ``weights``: optional outputs [tokens, k].
+    ``workspace``: from :func:`few_workspace`; without one the module keeps one a stream."""
+    ldx = _matrix(x, "x", (torch.bfloat16,))
+    t, d = x.shape
+    if ldx % 8 or x.data_ptr() % 16:
+        x, ldx = x.clone(memory_format=torch.contiguous_format), d
+    e = router.shape[0]
+    _dense(router, "router", torch.bfloat16, (e, d))
+    if w13.dim() != 4:
+        raise ValueError(f"w13: [experts, 2, inter, hidden] is wanted, got {tuple(w13.shape)}")
+    i = w13.shape[2]
+    if w13.dtype == torch.float8_e4m3fn:
+        if s13 is None or s2 is None:
+            raise ValueError("8-bit weights need s13 and s2")
+        if _experts_weights(w13, s13, w2, s2, d) != (e, i):
+            raise ValueError(f"w13: {e} experts are wanted, got {w13.shape[0]}")
+    else:
+        _dense(w13, "w13", torch.bfloat16, (e, 2, i, d))
+        _dense(w2, "w2", torch.bfloat16, (e, d, i))
+    if ids is not None:
+        _dense(ids, "ids", torch.int32, (t, k))
+    if weights is not None:
+        _dense(weights, "weights", torch.float32, (t, k))
+    s = B._stream(stream)
+    if workspace is None:
+        n, z = ctypes.c_size_t(), ctypes.c_size_t()
+        _check(B.lib().tuna_moe_few_workspace_bytes(t, e, k, d, i, ctypes.byref(n), ctypes.byref(z)), "tuna_moe_few_workspace_bytes")
+        kept = _few_spaces.setdefault((x.device.index, s), [])
+        if not kept or kept[-1].numel() < n.value:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("few: pass a workspace (few_workspace) when the first call of this size is captured")
+            with torch.cuda.stream(torch.cuda.ExternalStream(s, device=x.device)):
+                kept.append(few_workspace(t, e, k, d, i, x.device))
+        workspace = kept[-1]
+    out = torch.empty(t, d, dtype=torch.bfloat16, device=x.device)
+    _check(B.lib().tuna_moe_few(x.data_ptr(), ldx, t, router.data_ptr(), e, k, _scoring(scoring), int(renormalize), scale, d, i,
+                                DTYPES[w13.dtype], w13.data_ptr(), None if s13 is None else s13.data_ptr(), w2.data_ptr(),
+                                None if s2 is None else s2.data_ptr(), out.data_ptr(), d, None if ids is None else ids.data_ptr(),
+                                None if weights is None else weights.data_ptr(), workspace.data_ptr(), workspace.numel(), s),
+           "tuna_moe_few")
+    return out
+
+
 def device_status() -> int:
     """0, or 1 if a kernel of these operators gave up a bounded wait (synchronises the device)."""
     n = ctypes.c_int()
