@@ -22,7 +22,6 @@
 // 8-bit weights are exact in f16, one conversion instruction for two values; x and h then are
 // f16 too, after a division by a power of two of the row's largest magnitude: 11 bits, more
 // than bf16 holds.  Sums, logits and probabilities are in 32 bits.
-#include <mutex>
 #include <type_traits>
 
 #include "tuna_ops.cuh"
@@ -568,18 +567,9 @@ int check_few(int tokens, int experts, int k, int hidden, int inter) {
 
 template <bool FP8, int MAXC, int NT>
 int launch_few(const FewArgs &a, cudaStream_t st) {
-  static std::mutex m;
   static bool set[64] = {};
   auto kernel = tuna_few_kernel<FP8, MAXC, NT>;
-  int dev = 0;
-  if (const int rc = note_cuda(cudaGetDevice(&dev))) return rc;
-  {
-    std::lock_guard<std::mutex> lock(m);
-    if (dev < 0 || dev >= 64 || !set[dev]) {
-      if (const int rc = note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem))) return rc;
-      if (dev >= 0 && dev < 64) set[dev] = true;
-    }
-  }
+  if (const int rc = allow_smem(kernel, kFewSmem, set)) return rc;
   return launch(kernel, dim3((unsigned)sm_count()), kThreads, kFewSmem, st, true, a);
 }
 

@@ -487,19 +487,6 @@ int make_map(CUtensorMap *map, int rank, const void *p, int64_t k, int64_t rows,
   return r == CUDA_SUCCESS ? TUNA_OK : note_cuda(cudaErrorInvalidValue);
 }
 
-// Dynamic shared memory above the default needs the kernel's leave, once a device.
-template <typename K>
-int allow_smem(K kernel, size_t bytes, bool (&set)[64]) {
-  static std::mutex m;
-  int dev = 0;
-  if (const int rc = note_cuda(cudaGetDevice(&dev))) return rc;
-  std::lock_guard<std::mutex> lock(m);
-  if (dev >= 0 && dev < 64 && set[dev]) return TUNA_OK;
-  if (const int rc = note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes))) return rc;
-  if (dev >= 0 && dev < 64) set[dev] = true;
-  return TUNA_OK;
-}
-
 template <int BN, bool SWIGLU, bool B_ROWS, typename TO>
 int run_tiles(const ProductArgs &p, cudaStream_t st) {
   TileArgs a = {};

@@ -48,6 +48,18 @@ inline int launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cud
   return note_cuda(cudaLaunchKernelEx(&cfg, kernel, P(args)...));
 }
 
+// Dynamic shared memory above the default needs the kernel's leave, once a device (`set`: one
+// flag a device and kernel; two threads that both find it clear do the same harmless thing).
+template <typename K>
+inline int allow_smem(K kernel, size_t bytes, bool (&set)[64]) {
+  int dev = 0;
+  if (const int rc = note_cuda(cudaGetDevice(&dev))) return rc;
+  if (dev >= 0 && dev < 64 && __atomic_load_n(&set[dev], __ATOMIC_ACQUIRE)) return TUNA_OK;
+  if (const int rc = note_cuda(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes))) return rc;
+  if (dev >= 0 && dev < 64) __atomic_store_n(&set[dev], true, __ATOMIC_RELEASE);
+  return TUNA_OK;
+}
+
 // Carves a caller's workspace into 256-byte aligned pieces; with base == nullptr it only adds up.
 struct Carve {
   char *base;

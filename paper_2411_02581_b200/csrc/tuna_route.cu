@@ -50,6 +50,7 @@ int *error_word() {
 namespace {
 
 constexpr int kTopThreads = 256;
+constexpr int kSmallTokens = 256;  // up to here one block is done before a second launch would be
 
 struct RouteArgs {
   const void *logits;
@@ -275,6 +276,52 @@ __global__ void __launch_bounds__(kTopThreads) tuna_route_kernel(RouteArgs a, Or
   }
   __syncthreads();
   for (int e = threadIdx.x; e < a.experts; e += kTopThreads) o.hist[(int64_t)blockIdx.x * a.experts + e] = (uint16_t)count[e];
+}
+
+// A few tokens of one rank: choice and order in one block and one launch.
+template <int LPT, int VPL, typename T>
+__global__ void __launch_bounds__(kOrderThreads) tuna_route_small_kernel(RouteArgs a, OrderArgs o) {
+  extern __shared__ __align__(16) char smem[];
+  int64_t *base = (int64_t *)smem;
+  int *count = (int *)(smem + (size_t)a.experts * 8);
+  for (int e = threadIdx.x; e < a.experts; e += kOrderThreads) count[e] = 0;
+  wait_previous();
+  allow_next();
+  __syncthreads();
+  const int lane = threadIdx.x % LPT;
+  for (int64_t tb = 0; tb < a.tokens; tb += kOrderThreads / LPT) {
+    const int64_t t = tb + threadIdx.x / LPT;
+    float z[VPL];
+    if (t < a.tokens) {
+      load_logits(reinterpret_cast<const T *>(a.logits) + t * a.ld, lane * VPL, a.experts, a.vec, z);
+    } else {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) z[i] = -INFINITY;
+    }
+    int id;
+    float w;
+    choose<LPT>(z, lane, a.k, a.scoring, a.renormalize, a.scale, id, w);
+    if (t < a.tokens && lane < a.k) {
+      a.ids[t * a.k + lane] = id;
+      a.weights[t * a.k + lane] = w;
+      if (id >= 0) atomicAdd(count + id, 1);
+    }
+  }
+  __syncthreads();
+  const int e = threadIdx.x;  // (experts <= TUNA_MOE_MAX_EXPERTS < kOrderThreads)
+  const int64_t c = e < a.experts ? count[e] : 0;
+  int64_t sum;
+  const int64_t x = block_scan(c, &sum);
+  if (e < a.experts) {
+    base[e] = x;
+    if (o.counts) o.counts[e] = c;
+    if (o.offsets) {
+      o.offsets[e] = x;
+      if (e == a.experts - 1) o.offsets[a.experts] = sum;
+    }
+  }
+  place_entries(o, smem, 0, 0, a.tokens * a.k);
+  for (int64_t j = sum + threadIdx.x; j < a.tokens * a.k; j += kOrderThreads) o.rows[j] = -1;
 }
 
 // Gradient of the weights with respect to the logits; the probabilities are computed anew
@@ -508,21 +555,9 @@ int zero_order(const OrderArgs &o, int ranks, int experts, cudaStream_t st) {
 }
 
 int launch_order(const OrderArgs &o, cudaStream_t st) {
-  const size_t smem = order_smem(o.experts);
-  static std::mutex m;
   static bool set[64] = {};
-  int dev = 0;
-  if (const int rc = note_cuda(cudaGetDevice(&dev))) return rc;
-  {
-    std::lock_guard<std::mutex> lock(m);
-    if (dev < 0 || dev >= 64 || !set[dev]) {
-      if (const int rc = note_cuda(cudaFuncSetAttribute(tuna_order_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                        (int)order_smem(TUNA_MOE_MAX_EXPERTS))))
-        return rc;
-      if (dev >= 0 && dev < 64) set[dev] = true;
-    }
-  }
-  return launch(tuna_order_kernel, dim3((unsigned)(o.rank_groups * o.ranks)), kOrderThreads, smem, st, false, o);
+  if (const int rc = allow_smem(tuna_order_kernel, order_smem(TUNA_MOE_MAX_EXPERTS), set)) return rc;
+  return launch(tuna_order_kernel, dim3((unsigned)(o.rank_groups * o.ranks)), kOrderThreads, order_smem(o.experts), st, false, o);
 }
 
 // Lanes a token and values a lane: the fewest lanes that hold the experts at 8 values each
@@ -542,6 +577,18 @@ struct RouteLaunch {
   template <int LPT, int VPL>
   int operator()() {
     return launch(tuna_route_kernel<LPT, VPL, T>, dim3((unsigned)(o.rank_chunks * o.ranks)), kTopThreads, (size_t)a.experts * 4, st, false, a, o);
+  }
+};
+template <typename T>
+struct SmallLaunch {
+  const RouteArgs &a;
+  const OrderArgs &o;
+  cudaStream_t st;
+  template <int LPT, int VPL>
+  int operator()() {
+    static bool set[64] = {};
+    if (const int rc = allow_smem(tuna_route_small_kernel<LPT, VPL, T>, order_smem(TUNA_MOE_MAX_EXPERTS), set)) return rc;
+    return launch(tuna_route_small_kernel<LPT, VPL, T>, dim3(1), kOrderThreads, order_smem(a.experts), st, false, a, o);
   }
 };
 template <typename T>
@@ -610,6 +657,8 @@ int tuna_moe_route(const void *logits, int dtype, int64_t tokens, int experts, i
   a.logits = logits, a.tokens = tokens, a.ld = ld, a.experts = experts, a.k = k;
   a.scoring = scoring, a.renormalize = renormalize != 0, a.scale = scale, a.ids = ids, a.weights = weights;
   a.vec = aligned(logits, 16) && ld * dtype_size(dtype) % 16 == 0;
+  if (ranks == 1 && tokens <= kSmallTokens)
+    return dtype == TUNA_DTYPE_F32 ? by_width(experts, k, SmallLaunch<float>{a, o, st}) : by_width(experts, k, SmallLaunch<__nv_bfloat16>{a, o, st});
   const int rc = dtype == TUNA_DTYPE_F32 ? by_width(experts, k, RouteLaunch<float>{a, o, st})
                                          : by_width(experts, k, RouteLaunch<__nv_bfloat16>{a, o, st});
   return rc ? rc : launch_order(o, st);

@@ -10,6 +10,7 @@ the caller's to order, as with any torch operation.
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import NamedTuple
 
 import torch
@@ -33,25 +34,31 @@ class Routing(NamedTuple):
     pos: torch.Tensor      # int64 [tokens, k]
 
 
+def _stream(stream, device):
+    """The raw stream: torch's current one of the tensors' device, or the caller's."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    return B._stream(stream)
+
+
 def _check(rc, what):
     if rc != 0:
         raise B.TunaError(rc, what, B.lib().tuna_ops_cuda_error() if rc == -7 else 0)
 
 
-def _matrix(t, name, dtypes, rows=None, cols=None):
+def _matrix(t, name, dtypes):
     """A CUDA matrix whose rows are contiguous; returns its row pitch."""
     if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype not in dtypes or not t.is_cuda:
         raise ValueError(f"{name}: a CUDA matrix of {', '.join(str(d) for d in dtypes)} is wanted")
-    if rows is not None and t.shape[0] != rows or cols is not None and t.shape[1] != cols:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, wanted ({rows if rows is not None else 'any'}, "
-                         f"{cols if cols is not None else 'any'})")
-    if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+    rows, cols = t.shape
+    ld, step = t.stride()
+    if cols > 1 and step != 1 or rows > 1 and ld < cols:
         raise ValueError(f"{name}: rows must be contiguous and must not overlap (strides {t.stride()})")
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+    return ld if rows > 1 else max(cols, 1)
 
 
 def _dense(t, name, dtype, shape):
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_cuda or not t.is_contiguous():
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous CUDA tensor of {dtype}, shape {tuple(shape)}, is wanted")
     return t
 
@@ -62,15 +69,22 @@ def _scoring(name):
     return SCORING[name]
 
 
-def _order_workspace(tokens, experts, k, ranks, device):
+@functools.lru_cache(maxsize=4096)
+def _bytes(function, *sizes):
+    """A workspace size, asked of the library once for each set of sizes."""
     n = ctypes.c_size_t()
-    _check(B.lib().tuna_moe_order_workspace_bytes(tokens, experts, k, ranks, ctypes.byref(n)), "tuna_moe_order_workspace_bytes")
-    return torch.empty(max(n.value, 256), dtype=torch.uint8, device=device)
+    _check(getattr(B.lib(), function)(*sizes, ctypes.byref(n)), function)
+    return max(n.value, 256)
+
+
+def _order_workspace(tokens, experts, k, ranks, device):
+    return torch.empty(_bytes("tuna_moe_order_workspace_bytes", tokens, experts, k, ranks), dtype=torch.uint8, device=device)
 
 
 def _order_outputs(tokens, experts, k, ranks, device):
-    new = lambda *shape: torch.empty(*shape, dtype=torch.int64, device=device)  # noqa: E731
-    return new(ranks, experts), new(ranks * experts + 1), new(tokens * k), new(tokens, k)
+    new = torch.empty
+    return (new(ranks, experts, dtype=torch.int64, device=device), new(ranks * experts + 1, dtype=torch.int64, device=device),
+            new(tokens * k, dtype=torch.int64, device=device), new(tokens, k, dtype=torch.int64, device=device))
 
 
 def route(logits, k, *, scoring="softmax", renormalize=False, scale=1.0, ranks=1, stream=None) -> Routing:
@@ -79,13 +93,14 @@ def route(logits, k, *, scoring="softmax", renormalize=False, scale=1.0, ranks=1
     t, e = logits.shape
     if ranks < 1 or t % ranks:
         raise ValueError(f"{t} tokens do not divide over {ranks} ranks")
-    ws = _order_workspace(t, e, k, ranks, logits.device)
-    ids = torch.empty(t, k, dtype=torch.int32, device=logits.device)
-    weights = torch.empty(t, k, dtype=torch.float32, device=logits.device)
-    counts, offsets, rows, pos = _order_outputs(t, e, k, ranks, logits.device)
+    device = logits.device
+    ws = _order_workspace(t, e, k, ranks, device)
+    ids = torch.empty(t, k, dtype=torch.int32, device=device)
+    weights = torch.empty(t, k, dtype=torch.float32, device=device)
+    counts, offsets, rows, pos = _order_outputs(t, e, k, ranks, device)
     _check(B.lib().tuna_moe_route(logits.data_ptr(), DTYPES[logits.dtype], t, e, ld, k, ranks, _scoring(scoring), int(renormalize), scale,
                                   ids.data_ptr(), weights.data_ptr(), counts.data_ptr(), offsets.data_ptr(), rows.data_ptr(),
-                                  pos.data_ptr(), ws.data_ptr(), ws.numel(), B._stream(stream)), "tuna_moe_route")
+                                  pos.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream, logits.device)), "tuna_moe_route")
     return Routing(ids, weights, counts, offsets, rows, pos)
 
 
@@ -100,7 +115,7 @@ def order(ids, experts, *, ranks=1, stream=None):
     ws = _order_workspace(t, experts, k, ranks, ids.device)
     out = _order_outputs(t, experts, k, ranks, ids.device)
     _check(B.lib().tuna_moe_order(ids.data_ptr(), t, experts, k, ranks, *[o.data_ptr() for o in out], ws.data_ptr(), ws.numel(),
-                                  B._stream(stream)), "tuna_moe_order")
+                                  _stream(stream, ids.device)), "tuna_moe_order")
     return out
 
 
@@ -113,7 +128,7 @@ def route_backward(logits, ids, dweights, *, scoring="softmax", renormalize=Fals
     _dense(dweights, "dweights", torch.float32, (t, k))
     d = torch.empty(t, e, dtype=logits.dtype, device=logits.device)
     _check(B.lib().tuna_moe_route_backward(logits.data_ptr(), DTYPES[logits.dtype], t, e, ld, k, _scoring(scoring), int(renormalize),
-                                           scale, ids.data_ptr(), dweights.data_ptr(), d.data_ptr(), e, B._stream(stream)),
+                                           scale, ids.data_ptr(), dweights.data_ptr(), d.data_ptr(), e, _stream(stream, logits.device)),
            "tuna_moe_route_backward")
     return d
 
@@ -128,7 +143,7 @@ def combine(y, weights, pos, *, out_dtype=torch.bfloat16, stream=None):
         raise ValueError(f"out_dtype: one of {FLOATS}")
     out = torch.empty(t, y.shape[1], dtype=out_dtype, device=y.device)
     _check(B.lib().tuna_moe_combine(y.data_ptr(), DTYPES[y.dtype], y.shape[0], y.shape[1], ld, weights.data_ptr(), pos.data_ptr(), t, k,
-                                    out.data_ptr(), DTYPES[out_dtype], y.shape[1], B._stream(stream)), "tuna_moe_combine")
+                                    out.data_ptr(), DTYPES[out_dtype], y.shape[1], _stream(stream, y.device)), "tuna_moe_combine")
     return out
 
 
@@ -144,7 +159,7 @@ def combine_backward(dout, y, weights, pos, *, stream=None):
     dw = torch.zeros_like(weights)
     _check(B.lib().tuna_moe_combine_backward(dout.data_ptr(), DTYPES[dout.dtype], ldg, y.data_ptr(), DTYPES[y.dtype], y.shape[0],
                                              y.shape[1], ldy, weights.data_ptr(), pos.data_ptr(), t, k, dy.data_ptr(), y.shape[1],
-                                             dw.data_ptr(), B._stream(stream)), "tuna_moe_combine_backward")
+                                             dw.data_ptr(), _stream(stream, y.device)), "tuna_moe_combine_backward")
     return dy, dw
 
 
@@ -162,12 +177,13 @@ def fp8_quantize(x, layout="rows", *, stream=None):
     rows, cols = x.shape
     out = (cols, rows) if layout in ("columns", "tiles_t") else (rows, cols)
     pitch = (out[1] + 15) // 16 * 16
-    q = torch.empty(out[0], pitch, dtype=torch.float8_e4m3fn, device=x.device)
+    device = x.device
+    q = torch.empty(out[0], pitch, dtype=torch.float8_e4m3fn, device=device)
     tiles = layout in ("tiles", "tiles_t")
-    scale = torch.empty((_blocks(out[0]), _blocks(out[1])) if tiles else (_blocks(out[1]), out[0]), dtype=torch.float32, device=x.device)
+    scale = torch.empty(_blocks(out[0]) if tiles else _blocks(out[1]), _blocks(out[1]) if tiles else out[0], dtype=torch.float32, device=device)
     _check(B.lib().tuna_fp8_quantize(x.data_ptr(), DTYPES[x.dtype], rows, cols, ld, LAYOUTS[layout], q.data_ptr(), max(pitch, 16),
-                                     scale.data_ptr(), B._stream(stream)), "tuna_fp8_quantize")
-    return q[:, :out[1]], scale
+                                     scale.data_ptr(), _stream(stream, x.device)), "tuna_fp8_quantize")
+    return q if pitch == out[1] else q[:, :out[1]], scale
 
 
 def _fp8_matrix(q, name):
@@ -213,7 +229,7 @@ def fp8_matmul(a, a_scale, b, b_scale, *, offsets=None, b_blocks="tiles", out_dt
     out = torch.empty(m, n, dtype=out_dtype, device=a.device)
     _check(B.lib().tuna_fp8_matmul(a.data_ptr(), a_scale.data_ptr(), m, max(lda, 16), flat.data_ptr(), b_scale.data_ptr(), LAYOUTS[b_blocks], n,
                                    max(ldb, 16), k, groups, None if offsets is None else offsets.data_ptr(), out.data_ptr(),
-                                   DTYPES[out_dtype], max(n, 1), B._stream(stream)), "tuna_fp8_matmul")
+                                   DTYPES[out_dtype], max(n, 1), _stream(stream, a.device)), "tuna_fp8_matmul")
     return out
 
 
@@ -231,7 +247,7 @@ def _experts_weights(w13, s13, w2, s2, hidden):
 
 def _space(need, workspace, device):
     if workspace is None:
-        return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+        return torch.empty(need, dtype=torch.uint8, device=device)
     return workspace
 
 
@@ -241,12 +257,10 @@ def expert_rows(x, offsets, w13, s13, w2, s2, *, workspace=None, stream=None):
     rows, d = x.shape
     e, i = _experts_weights(w13, s13, w2, s2, d)
     _dense(offsets, "offsets", torch.int64, (e + 1,))
-    n = ctypes.c_size_t()
-    _check(B.lib().tuna_moe_expert_rows_workspace_bytes(rows, d, i, ctypes.byref(n)), "tuna_moe_expert_rows_workspace_bytes")
-    ws = _space(n.value, workspace, x.device)
+    ws = _space(_bytes("tuna_moe_expert_rows_workspace_bytes", rows, d, i), workspace, x.device)
     y = torch.empty(rows, d, dtype=torch.bfloat16, device=x.device)
     _check(B.lib().tuna_moe_expert_rows(x.data_ptr(), ldx, rows, e, offsets.data_ptr(), d, i, w13.data_ptr(), s13.data_ptr(), w2.data_ptr(),
-                                        s2.data_ptr(), y.data_ptr(), d, ws.data_ptr(), ws.numel(), B._stream(stream)), "tuna_moe_expert_rows")
+                                        s2.data_ptr(), y.data_ptr(), d, ws.data_ptr(), ws.numel(), _stream(stream, x.device)), "tuna_moe_expert_rows")
     return y
 
 
@@ -258,23 +272,26 @@ def experts(x, ids, weights, w13, s13, w2, s2, *, workspace=None, stream=None):
     k = ids.shape[-1]
     _dense(ids, "ids", torch.int32, (t, k))
     _dense(weights, "weights", torch.float32, (t, k))
-    n = ctypes.c_size_t()
-    _check(B.lib().tuna_moe_experts_workspace_bytes(t, e, k, d, i, ctypes.byref(n)), "tuna_moe_experts_workspace_bytes")
-    ws = _space(n.value, workspace, x.device)
+    ws = _space(_bytes("tuna_moe_experts_workspace_bytes", t, e, k, d, i), workspace, x.device)
     out = torch.empty(t, d, dtype=torch.bfloat16, device=x.device)
     _check(B.lib().tuna_moe_experts(x.data_ptr(), ldx, t, ids.data_ptr(), weights.data_ptr(), k, e, d, i, w13.data_ptr(), s13.data_ptr(),
-                                    w2.data_ptr(), s2.data_ptr(), out.data_ptr(), d, ws.data_ptr(), ws.numel(), B._stream(stream)),
+                                    w2.data_ptr(), s2.data_ptr(), out.data_ptr(), d, ws.data_ptr(), ws.numel(), _stream(stream, x.device)),
            "tuna_moe_experts")
     return out
 
 
+@functools.lru_cache(maxsize=4096)
+def _few_bytes(*sizes):
+    n, z = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(B.lib().tuna_moe_few_workspace_bytes(*sizes, ctypes.byref(n), ctypes.byref(z)), "tuna_moe_few_workspace_bytes")
+    return max(n.value, 256), z.value
+
+
 def few_workspace(tokens, experts, k, hidden, inter, device="cuda"):
     """A workspace of :func:`few`, ready for use by one stream."""
-    n, z = ctypes.c_size_t(), ctypes.c_size_t()
-    _check(B.lib().tuna_moe_few_workspace_bytes(tokens, experts, k, hidden, inter, ctypes.byref(n), ctypes.byref(z)),
-           "tuna_moe_few_workspace_bytes")
-    ws = torch.empty(max(n.value, 256), dtype=torch.uint8, device=device)
-    ws[:z.value].zero_()
+    need, zeroed = _few_bytes(tokens, experts, k, hidden, inter)
+    ws = torch.empty(need, dtype=torch.uint8, device=device)
+    ws[:zeroed].zero_()
     return ws
 
 
@@ -309,12 +326,10 @@ def few(x, router, k, w13, w2, *, s13=None, s2=None, scoring="softmax", renormal
         _dense(ids, "ids", torch.int32, (t, k))
     if weights is not None:
         _dense(weights, "weights", torch.float32, (t, k))
-    s = B._stream(stream)
+    s = _stream(stream, x.device)
     if workspace is None:
-        n, z = ctypes.c_size_t(), ctypes.c_size_t()
-        _check(B.lib().tuna_moe_few_workspace_bytes(t, e, k, d, i, ctypes.byref(n), ctypes.byref(z)), "tuna_moe_few_workspace_bytes")
         kept = _few_spaces.setdefault((x.device.index, s), [])
-        if not kept or kept[-1].numel() < n.value:
+        if not kept or kept[-1].numel() < _few_bytes(t, e, k, d, i)[0]:
             if torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("few: pass a workspace (few_workspace) when the first call of this size is captured")
             with torch.cuda.stream(torch.cuda.ExternalStream(s, device=x.device)):
