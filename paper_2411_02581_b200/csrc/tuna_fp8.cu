@@ -176,7 +176,7 @@ struct Shape {
   static constexpr int kCols = BN / 2;  // accumulator columns of a thread
   // stages, then the groups' tile offsets, a copy of the second operand's scales for each of the
   // eight warps and two blocks, the rows' largest magnitudes, barriers and flags
-  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + (kMaxGroups + 4) * 4 + 8 * 2 * 128 * 4 + 256 * 4 + 256;
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + (kMaxGroups + 8) * 4 + 8 * 2 * 128 * 4 + 256 * 4 + 256;
 };
 
 // Tile t of the walk: the group it is in (never walked backwards), its rows and columns.
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   extern __shared__ char smem_raw[];
   char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   int *tile_base = (int *)(smem + (size_t)S::kStages * S::kStageBytes);
-  float *col_scale = (float *)(tile_base + kMaxGroups + 4);  // [8 warps][2][128]
+  float *col_scale = (float *)(tile_base + kMaxGroups + 8);  // [8 warps][2][128]
   uint32_t *row_amax = (uint32_t *)(col_scale + 2048);       // [256]
   uint64_t *bars = (uint64_t *)(((uintptr_t)(row_amax + 256) + 7) & ~(uintptr_t)7);
   volatile int *given_up = (volatile int *)(bars + 2 * S::kStages + 5);
@@ -336,56 +336,72 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       uint64_t acc[S::kCols / 2];
 #pragma unroll
       for (int i = 0; i < S::kCols / 2; ++i) acc[i] = 0;
-      float fa = sa[0], fb = sb0[0], fc = SWIGLU ? sb1[0] : 0.0f, fd[4];
-      if (B_ROWS) {
+      // Scales of the next kAhead blocks travel while these are added: one block ahead, their
+      // latency would set the pace.
+      constexpr int kAhead = B_ROWS ? 2 : 4;
+      float fa[kAhead], fb[kAhead], fc[kAhead], fd[kAhead][4];
+      auto fetch = [&](int kb0) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) fd[j] = sb0[col[j]];
-      }
-      for (int kb = 0; kb < blocks; ++kb) {
-        const float ra = fa, rb = fb, rc = fc;
-        if (B_ROWS) {  // (the warp's last reads of this half were two blocks ago)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) my_scale[buf * 128 + lane + j * 32] = fd[j];
-          __syncwarp();
-        }
-        if (kb + 1 < blocks) {  // the next block's scales travel while this one is added
-          fa = sa[(int64_t)(kb + 1) * a.p.m];
+        for (int j = 0; j < kAhead; ++j) {
+          const int kb = min(kb0 + j, blocks - 1);
+          fa[j] = __ldg(sa + (int64_t)kb * a.p.m);
           if (B_ROWS) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) fd[j] = sb0[(int64_t)(kb + 1) * a.p.n + col[j]];
+            for (int q = 0; q < 4; ++q) fd[j][q] = __ldg(sb0 + (int64_t)kb * a.p.n + col[q]);
           } else {
-            fb = sb0[kb + 1];
+            fb[j] = __ldg(sb0 + kb);
           }
-          if (SWIGLU) fc = sb1[kb + 1];
+          if (SWIGLU) fc[j] = __ldg(sb1 + kb);
         }
-        ok = __all_sync(~0u, mbar_wait(done + 8 * buf, buf_phase, given_up));  // (and the warp is whole for the loads)
-        if (!ok) break;
-        tc_fence_after();
-        const float s0 = ra * rb, s1 = ra * rc;
-        const uint64_t p0 = B_ROWS ? pair(ra, ra) : pair(s0, s0), p1 = pair(s1, s1);
-        uint32_t v[2][32];
-        tmem_load32(from + buf * BN, v[0]);
+      };
+      fetch(0);
+      for (int kb0 = 0; ok && kb0 < blocks; kb0 += kAhead) {
+        float ra[kAhead], rb[kAhead], rc[kAhead], rd[kAhead][4];
 #pragma unroll
-        for (int c = 0; c < S::kCols / 32; ++c) {
-          tmem_wait(v[c & 1]);
-          if (c + 1 < S::kCols / 32) tmem_load32(from + buf * BN + (c + 1) * 32, v[(c + 1) & 1]);
-          if (c + 1 == S::kCols / 32) {  // everything is in registers: the accumulator may be filled again
-            tc_fence_before();
+        for (int j = 0; j < kAhead; ++j) {
+          ra[j] = fa[j], rb[j] = fb[j], rc[j] = fc[j];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) rd[j][q] = fd[j][q];
+        }
+        if (kb0 + kAhead < blocks) fetch(kb0 + kAhead);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          if (kb0 + j >= blocks) break;
+          if (B_ROWS) {  // (the warp's last reads of this half were two blocks ago)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) my_scale[buf * 128 + lane + q * 32] = rd[j][q];
             __syncwarp();
-            if (lane == 0) mbar_arrive(freed + 8 * buf);
           }
-          uint32_t(&x)[32] = v[c & 1];
+          ok = __all_sync(~0u, mbar_wait(done + 8 * buf, buf_phase, given_up));  // (and the warp is whole for the loads)
+          if (!ok) break;
+          tc_fence_after();
+          const float s0 = ra[j] * rb[j], s1 = ra[j] * rc[j];
+          const uint64_t p0 = B_ROWS ? pair(ra[j], ra[j]) : pair(s0, s0), p1 = pair(s1, s1);
+          uint32_t v[2][16];
+          tmem_load16(from + buf * BN, v[0]);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            uint64_t s = SWIGLU && c >= 2 ? p1 : p0;
-            if (B_ROWS) {
-              const float2 f = *reinterpret_cast<const float2 *>(my_scale + buf * 128 + c * 32 + i * 2);
-              s = mul2(p0, pair(f.x, f.y));
+          for (int c = 0; c < S::kCols / 16; ++c) {
+            tmem_wait(v[c & 1]);
+            if (c + 1 < S::kCols / 16) tmem_load16(from + buf * BN + (c + 1) * 16, v[(c + 1) & 1]);
+            if (c + 1 == S::kCols / 16) {  // everything is in registers: the accumulator may be filled again
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(freed + 8 * buf);
             }
-            acc[c * 16 + i] = fma2(pair(x[2 * i], x[2 * i + 1]), s, acc[c * 16 + i]);
+            uint32_t(&x)[16] = v[c & 1];
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+              uint64_t f = SWIGLU && c >= 4 ? p1 : p0, g = f;
+              if (B_ROWS) {
+                const float4 q = *reinterpret_cast<const float4 *>(my_scale + buf * 128 + c * 16 + i * 2);
+                f = mul2(p0, pair(q.x, q.y)), g = mul2(p0, pair(q.z, q.w));
+              }
+              acc[c * 8 + i] = fma2(pair(x[2 * i], x[2 * i + 1]), f, acc[c * 8 + i]);
+              acc[c * 8 + i + 1] = fma2(pair(x[2 * i + 2], x[2 * i + 3]), g, acc[c * 8 + i + 1]);
+            }
           }
+          if (++buf == 2) buf = 0, buf_phase ^= 1;
         }
-        if (++buf == 2) buf = 0, buf_phase ^= 1;
       }
       if constexpr (!SWIGLU) {
         if (!ok) break;
