@@ -56,10 +56,7 @@ __global__ void __launch_bounds__(256) tuna_quantize_rows_kernel(QuantArgs a) {
     for (int d = 1; d < 8; d <<= 1) amax = max(amax, __shfl_xor_sync(~0u, amax, d));
     const float s = fp8_scale(amax);
     if (c < a.cols) {
-      uint4 u;
-      u.x = fp8_quad(v[0], v[1], v[2], v[3], s), u.y = fp8_quad(v[4], v[5], v[6], v[7], s);
-      u.z = fp8_quad(v[8], v[9], v[10], v[11], s), u.w = fp8_quad(v[12], v[13], v[14], v[15], s);
-      *reinterpret_cast<uint4 *>(a.q + r * a.ldq + c) = u;
+      *reinterpret_cast<uint4 *>(a.q + r * a.ldq + c) = fp8_sixteen(v, divisor(s));
       if (lane % 8 == 0) a.scale[(int64_t)(c / 128) * a.rows + r] = s;
     }
   }
@@ -133,16 +130,14 @@ __global__ void __launch_bounds__(256) tuna_quantize_tile_kernel(QuantArgs a) {
     a.scale[MODE == kTiles ? (r0 / 128) * col_tiles + c0 / 128 : (c0 / 128) * ((a.rows + 127) / 128) + r0 / 128] = s;
   }
   if (out_row >= out_rows) return;
+  const Divisor by = divisor(s);
 #pragma unroll
   for (int j = 0; j < 64; j += 16) {
     if (out_col + j >= out_cols) break;
     float v[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) v[e] = turned ? tile[(half * 64 + j + e) * kTilePitch + i] : tile[i * kTilePitch + half * 64 + j + e];
-    uint4 u;
-    u.x = fp8_quad(v[0], v[1], v[2], v[3], s), u.y = fp8_quad(v[4], v[5], v[6], v[7], s);
-    u.z = fp8_quad(v[8], v[9], v[10], v[11], s), u.w = fp8_quad(v[12], v[13], v[14], v[15], s);
-    *reinterpret_cast<uint4 *>(a.q + out_row * a.ldq + out_col + j) = u;
+    *reinterpret_cast<uint4 *>(a.q + out_row * a.ldq + out_col + j) = fp8_sixteen(v, by);
   }
 }
 
@@ -150,13 +145,15 @@ __global__ void __launch_bounds__(256) tuna_quantize_tile_kernel(QuantArgs a) {
 //
 // A persistent block takes tiles of 128 x BN.  One warp copies 128 x 128 blocks of a and BN x
 // 128 blocks of b into a ring of stages; one thread issues the four tensor-core steps of a
-// block into one of two accumulators in tensor memory; eight warps read a finished accumulator
-// back, multiply it by sa * sb and add it to the 32-bit sums they keep in registers (128 a
-// thread at BN = 256), while the tensor cores fill the other one.  At BN = 256 a block keeps
-// the tensor cores busy for 512 cycles and the promotion needs 128 KB of tensor-memory reads
-// and 64 packed multiply-adds a thread, about half of that.
+// block into one of two accumulators in tensor memory; sixteen warps read a finished accumulator
+// back, multiply it by sa * sb and add it to the 32-bit sums they keep in registers (64 a
+// thread at BN = 256), while the tensor cores fill the other one.  The promotion is what bounds
+// the kernel: 256 cycles of packed multiply-adds a block at least, and the tensor-memory loads
+// in front of them.  Eight warps with 128 sums each had no registers left to load ahead (163 us
+// for 8192 x 4096 x 4096).  The scales come through a small ring of asynchronous copies that
+// every thread fills for itself, three blocks ahead: read when needed, their latency set the pace.
 //
-// With `swiglu` the 256 columns are 2 x (64 gate + 64 up) rows of the two matrices, so that the
+// With `swiglu` the 256 columns are 4 x (32 gate + 32 up) rows of the two matrices, so that the
 // thread that holds a gate value holds its up value, and a tile is exactly one 128-block of the
 // result: it leaves as e4m3 with its scale, and the 32-bit product never reaches memory.
 struct TileArgs {
@@ -166,17 +163,22 @@ struct TileArgs {
   int *error;
 };
 
-constexpr int kGemmThreads = 384;
+constexpr int kSumWarps = 16;   // promotion: four quarters of the columns x 128 rows
+constexpr int kGemmThreads = 128 + kSumWarps * 32;
+constexpr int kScaleRing = 4;
+constexpr int kCopyRegs = 32, kSumRegs = 112;  // registers of a thread: copying and issuing warps, promotion
 constexpr int kMaxGroups = TUNA_MOE_MAX_EXPERTS;
 
 template <int BN>
 struct Shape {
   static constexpr int kStages = BN == 256 ? 4 : 6;
   static constexpr int kStageBytes = 128 * 128 + BN * 128;
-  static constexpr int kCols = BN / 2;  // accumulator columns of a thread
-  // stages, then the groups' tile offsets, a copy of the second operand's scales for each of the
-  // eight warps and two blocks, the rows' largest magnitudes, barriers and flags
-  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + (kMaxGroups + 8) * 4 + 8 * 2 * 128 * 4 + 256 * 4 + 256;
+  static constexpr int kCols = BN / 4;  // accumulator columns of a thread
+  // stages, then the rings of row scales (and of column scales: a copy for each warp), the rows'
+  // largest magnitudes, the groups' tile offsets, barriers and flags
+  static constexpr size_t smem(bool b_rows) {
+    return 1024 + (size_t)kStages * kStageBytes + kScaleRing * kSumWarps * (32 + (b_rows ? 64 : 0)) * 4 + 512 * 4 + (kMaxGroups + 8) * 4 + 256;
+  }
 };
 
 // Tile t of the walk: the group it is in (never walked backwards), its rows and columns.
@@ -203,19 +205,20 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   using S = Shape<BN>;
   extern __shared__ char smem_raw[];
   char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-  int *tile_base = (int *)(smem + (size_t)S::kStages * S::kStageBytes);
-  float *col_scale = (float *)(tile_base + kMaxGroups + 8);  // [8 warps][2][128]
-  uint32_t *row_amax = (uint32_t *)(col_scale + 2048);       // [256]
-  uint64_t *bars = (uint64_t *)(((uintptr_t)(row_amax + 256) + 7) & ~(uintptr_t)7);
+  float *row_scale = (float *)(smem + (size_t)S::kStages * S::kStageBytes);       // [ring][16 warps][32]
+  float *col_scale = row_scale + kScaleRing * kSumWarps * 32;                     // [ring][16 warps][64], if B_ROWS
+  uint32_t *row_amax = (uint32_t *)(col_scale + (B_ROWS ? kScaleRing * kSumWarps * 64 : 0));  // [4][128]
+  int *tile_base = (int *)(row_amax + 512);
+  uint64_t *bars = (uint64_t *)(tile_base + kMaxGroups + 8);
   volatile int *given_up = (volatile int *)(bars + 2 * S::kStages + 5);
-  volatile int *lost = given_up + 1;  // an eighth of the promotion gave up
+  volatile int *lost = given_up + 1;  // a warp of the promotion gave up
   uint32_t *tmem_at = (uint32_t *)(given_up + 2);
   const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages, freed = done + 16, drained = freed + 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S::kStages; ++s) mbar_init(full + 8 * s, 1), mbar_init(empty + 8 * s, 1);
-    for (int s = 0; s < 2; ++s) mbar_init(done + 8 * s, 1), mbar_init(freed + 8 * s, 8);
+    for (int s = 0; s < 2; ++s) mbar_init(done + 8 * s, 1), mbar_init(freed + 8 * s, kSumWarps);
     mbar_init(drained, 1);
     *given_up = 0, *lost = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -251,7 +254,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   const int blocks = a.blocks;
 
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCopyRegs));
     if (warp == 0 && lane == 0) {
       // ---- copies
       int stage = 0, phase = 0;
@@ -267,8 +270,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           tma_load_2d(at, &map_a, kb * 128, (int)w.row, bar);
           if (SWIGLU) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-              tma_load_3d(at + 128 * 128 + q * 64 * 128, &map_b, kb * 128, w.n0 + (q >> 1) * 64, w.g * 2 + (q & 1), bar);
+            for (int q = 0; q < 8; ++q)
+              tma_load_3d(at + 128 * 128 + q * 32 * 128, &map_b, kb * 128, w.n0 + (q >> 1) * 32, w.g * 2 + (q & 1), bar);
           } else {
             tma_load_3d(at + 128 * 128, &map_b, kb * 128, w.n0, w.g, bar);
           }
@@ -288,7 +291,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       bool ok = true;
       for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
         for (int kb = 0; kb < blocks; ++kb) {
-          if (!(ok = mbar_wait(freed + 8 * buf, buf_phase ^ 1, given_up) && mbar_wait(full + 8 * stage, phase, given_up))) break;
+          if (!(ok = mbar_wait(full + 8 * stage, phase, given_up) && mbar_wait(freed + 8 * buf, buf_phase ^ 1, given_up))) break;
           tc_fence_after();
           const uint32_t at = smem_u32(smem) + stage * S::kStageBytes;
           const uint64_t da = tc_desc(at), db = tc_desc(at + 128 * 128);
@@ -307,114 +310,146 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
-    // ---- promotion and results: thread = one row, columns [half * kCols, ...) of the tile
-    const int half = (warp - 4) >> 2, row_in = (warp & 3) * 32 + lane;
-    float *my_scale = col_scale + (warp - 4) * 256;
-    const uint32_t from = tmem + ((uint32_t)((warp & 3) * 32) << 16) + half * S::kCols;
-    int buf = 0, buf_phase = 0;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSumRegs));
+    // ---- promotion and results: thread = one row, columns [quarter * kCols, ...) of the tile
+    const int quarter = (warp - 4) >> 2, row_in = (warp & 3) * 32 + lane;
+    const uint32_t from = tmem + ((uint32_t)((warp & 3) * 32) << 16) + quarter * S::kCols;
+    const uint32_t my_row = smem_u32(row_scale + (warp - 4) * 32 + lane), my_col = smem_u32(col_scale + (warp - 4) * 64 + lane);
+    constexpr int kRowStep = kSumWarps * 32 * 4, kColStep = kSumWarps * 64 * 4;
+    const int tiles_n = (a.p.n + 127) / 128;
+    int buf = 0, buf_phase = 0, slot = 0;
     bool ok = true;
+    // where the scales of a tile are: of this thread's row; of its columns, one a block of k, or with
+    // SWIGLU one for each matrix, or with B_ROWS one a column and block
     Walk w;
-    for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+    const float *sa = nullptr, *sb0 = nullptr, *sb1 = nullptr;
+    auto aim = [&](int64_t t) {
       walk_to(w, t, a, tile_base, SWIGLU ? BN / 2 : BN);
+      sa = a.p.sa + min(w.row + row_in, w.end - 1);
+      if (SWIGLU) {
+        sb0 = a.p.sb + ((int64_t)(w.g * 2) * tiles_n + w.n0 / 128) * blocks;
+        sb1 = sb0 + (int64_t)tiles_n * blocks;
+      } else if (B_ROWS) {
+        sb0 = a.p.sb + min(w.n0 + quarter * S::kCols + lane, a.p.n - 1);
+        sb1 = a.p.sb + min(w.n0 + quarter * S::kCols + lane + 32, a.p.n - 1);
+      } else {
+        sb0 = a.p.sb + ((int64_t)w.g * tiles_n + min((w.n0 + quarter * S::kCols) / 128, tiles_n - 1)) * blocks;
+      }
+    };
+    auto feed = [&](int kb, int at) {  // block kb's scales into ring place `at` (or an empty group, which keeps the count)
+      if (kb < blocks) {
+        copy4(my_row + at * kRowStep, sa + (int64_t)kb * a.p.m);
+        if (B_ROWS) {
+          copy4(my_col + at * kColStep, sb0 + (int64_t)kb * a.p.n);
+          if (S::kCols > 32) copy4(my_col + at * kColStep + 128, sb1 + (int64_t)kb * a.p.n);
+        }
+      }
+      copy_commit();
+    };
+    float fb = 0.0f, fc = 0.0f;  // lane i: the columns' scale of block i of the running 32
+    auto fetch = [&](int kb0) {
+      if (!B_ROWS) fb = __ldg(sb0 + min(kb0 + lane, blocks - 1));
+      if (SWIGLU) fc = __ldg(sb1 + min(kb0 + lane, blocks - 1));
+    };
+    auto open = [&](int64_t t) {
+      aim(t);
+      fetch(0);
+#pragma unroll
+      for (int i = 0; i < kScaleRing - 1; ++i) feed(i, (slot + i) % kScaleRing);
+    };
+    if (blockIdx.x < tiles) open(blockIdx.x);
+    for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
       const int64_t row = w.row + row_in;
       const bool there = row < w.end;
-      const float *sa = a.p.sa + (there ? row : w.row);
-      // scales of this thread's columns: one a block of k, or with SWIGLU one for each matrix
-      const int tiles_n = (a.p.n + 127) / 128;
-      const float *sb0 = a.p.sb, *sb1 = a.p.sb;
-      if (SWIGLU) {
-        sb0 += ((int64_t)(w.g * 2) * tiles_n + w.n0 / 128) * blocks;
-        sb1 = sb0 + (int64_t)tiles_n * blocks;
-      } else if (!B_ROWS) {
-        const int nt = min((w.n0 + half * S::kCols) / 128, tiles_n - 1);
-        sb0 += ((int64_t)w.g * tiles_n + nt) * blocks;
-      }
-      int col[4];  // B_ROWS: the columns whose scales this lane fetches for its warp
-#pragma unroll
-      for (int j = 0; j < 4; ++j) col[j] = min(w.n0 + half * S::kCols + lane + j * 32, a.p.n - 1);
+      const int n0 = w.n0;
       uint64_t acc[S::kCols / 2];
 #pragma unroll
       for (int i = 0; i < S::kCols / 2; ++i) acc[i] = 0;
-      // Scales of the next kAhead blocks travel while these are added: one block ahead, their
-      // latency would set the pace.
-      constexpr int kAhead = B_ROWS ? 2 : 4;
-      float fa[kAhead], fb[kAhead], fc[kAhead], fd[kAhead][4];
-      auto fetch = [&](int kb0) {
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-          const int kb = min(kb0 + j, blocks - 1);
-          fa[j] = __ldg(sa + (int64_t)kb * a.p.m);
-          if (B_ROWS) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) fd[j][q] = __ldg(sb0 + (int64_t)kb * a.p.n + col[q]);
-          } else {
-            fb[j] = __ldg(sb0 + kb);
-          }
-          if (SWIGLU) fc[j] = __ldg(sb1 + kb);
-        }
+      // the factors of block kb: read from the ring one block early, behind the first tensor-memory load
+      float s0, s1;
+      int here = 0;  // the ring place of the block at hand
+      auto prepare = [&](int kb) {
+        copy_wait<kScaleRing - 2>();
+        if (B_ROWS) __syncwarp();  // the other lanes' columns too
+        float ra;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ra) : "r"(my_row + slot * kRowStep) : "memory");
+        s0 = B_ROWS ? ra : ra * __shfl_sync(~0u, fb, kb & 31), s1 = SWIGLU ? ra * __shfl_sync(~0u, fc, kb & 31) : s0;
+        if ((kb & 31) == 31 && kb + 1 < blocks) fetch(kb + 1);
+        here = slot;
+        slot = (slot + 1) % kScaleRing;
       };
-      fetch(0);
-      for (int kb0 = 0; ok && kb0 < blocks; kb0 += kAhead) {
-        float ra[kAhead], rb[kAhead], rc[kAhead], rd[kAhead][4];
+      prepare(0);
+      for (int kb = 0; kb < blocks; ++kb) {
+        ok = __all_sync(~0u, mbar_wait(done + 8 * buf, buf_phase, given_up));  // (and the warp is whole for the loads)
+        if (!ok) break;
+        tc_fence_after();
+        const uint64_t p0 = pair(s0, s0), p1 = pair(s1, s1);
+        const float *cs = col_scale + ((size_t)here * kSumWarps + (warp - 4)) * 64;
+        uint32_t v[2][16];
+        tmem_load16(from + buf * BN, v[0]);
+        // (the ring place that is filled here was read two blocks ago, by the whole warp)
+        feed(kb + kScaleRing - 1, (here + kScaleRing - 1) % kScaleRing);
+        if (kb + 1 < blocks) prepare(kb + 1);
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-          ra[j] = fa[j], rb[j] = fb[j], rc[j] = fc[j];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) rd[j][q] = fd[j][q];
-        }
-        if (kb0 + kAhead < blocks) fetch(kb0 + kAhead);
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-          if (kb0 + j >= blocks) break;
-          if (B_ROWS) {  // (the warp's last reads of this half were two blocks ago)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) my_scale[buf * 128 + lane + q * 32] = rd[j][q];
+        for (int c = 0; c < S::kCols / 16; ++c) {
+          tmem_wait(v[c & 1]);
+          if (c + 1 < S::kCols / 16) {
+            tmem_load16(from + buf * BN + (c + 1) * 16, v[(c + 1) & 1]);
+          } else {  // everything is in registers: the accumulator may be filled again
+            tc_fence_before();
             __syncwarp();
+            if (lane == 0) mbar_arrive(freed + 8 * buf);
           }
-          ok = __all_sync(~0u, mbar_wait(done + 8 * buf, buf_phase, given_up));  // (and the warp is whole for the loads)
-          if (!ok) break;
-          tc_fence_after();
-          const float s0 = ra[j] * rb[j], s1 = ra[j] * rc[j];
-          const uint64_t p0 = B_ROWS ? pair(ra[j], ra[j]) : pair(s0, s0), p1 = pair(s1, s1);
-          uint32_t v[2][16];
-          tmem_load16(from + buf * BN, v[0]);
+          uint32_t(&x)[16] = v[c & 1];
 #pragma unroll
-          for (int c = 0; c < S::kCols / 16; ++c) {
-            tmem_wait(v[c & 1]);
-            if (c + 1 < S::kCols / 16) tmem_load16(from + buf * BN + (c + 1) * 16, v[(c + 1) & 1]);
-            if (c + 1 == S::kCols / 16) {  // everything is in registers: the accumulator may be filled again
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(freed + 8 * buf);
+          for (int i = 0; i < 8; i += 2) {
+            uint64_t f = SWIGLU && c >= 2 ? p1 : p0, g = f;
+            if (B_ROWS) {
+              const float4 q = *reinterpret_cast<const float4 *>(cs + c * 16 + i * 2);
+              f = mul2(p0, pair(q.x, q.y)), g = mul2(p0, pair(q.z, q.w));
             }
-            uint32_t(&x)[16] = v[c & 1];
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-              uint64_t f = SWIGLU && c >= 4 ? p1 : p0, g = f;
-              if (B_ROWS) {
-                const float4 q = *reinterpret_cast<const float4 *>(my_scale + buf * 128 + c * 16 + i * 2);
-                f = mul2(p0, pair(q.x, q.y)), g = mul2(p0, pair(q.z, q.w));
-              }
-              acc[c * 8 + i] = fma2(pair(x[2 * i], x[2 * i + 1]), f, acc[c * 8 + i]);
-              acc[c * 8 + i + 1] = fma2(pair(x[2 * i + 2], x[2 * i + 3]), g, acc[c * 8 + i + 1]);
-            }
+            acc[c * 8 + i] = fma2(pair(x[2 * i], x[2 * i + 1]), f, acc[c * 8 + i]);
+            acc[c * 8 + i + 1] = fma2(pair(x[2 * i + 2], x[2 * i + 3]), g, acc[c * 8 + i + 1]);
           }
-          if (++buf == 2) buf = 0, buf_phase ^= 1;
         }
+        if (++buf == 2) buf = 0, buf_phase ^= 1;
       }
+      if (ok && t + gridDim.x < tiles) open(t + gridDim.x);  // the next tile's scales travel during this one's stores
       if constexpr (!SWIGLU) {
         if (!ok) break;
+        if (there) {
+          TO *out = (TO *)a.p.out + row * a.p.ldo;
+          const int c0 = n0 + quarter * S::kCols;
+          // whole 32-byte sectors: as 16-byte stores, the results took a third of the kernel's time
+          constexpr int kRun = 32 / sizeof(TO);
+          const bool vec = (((uintptr_t)a.p.out | (uint64_t)a.p.ldo * sizeof(TO)) & 31) == 0;
+#pragma unroll
+          for (int i = 0; i < S::kCols; i += kRun) {
+            float v[kRun];
+#pragma unroll
+            for (int j = 0; j < kRun / 2; ++j) unpair(acc[i / 2 + j], v[2 * j], v[2 * j + 1]);
+            if (vec && c0 + i + kRun <= a.p.n) {
+              uint32_t u[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) u[j] = sizeof(TO) == 2 ? pack_bf16(v[2 * j % kRun], v[(2 * j + 1) % kRun]) : __float_as_uint(v[j]);
+              store32(out + c0 + i, u);
+            } else {
+#pragma unroll
+              for (int j = 0; j < kRun; ++j)
+                if (c0 + i + j < a.p.n) out[c0 + i + j] = from_f32<TO>(v[j]);
+            }
+          }
+        }
       } else {
-        if (!ok) *lost = 1;  // told before the barrier that the eight warps share: they leave together
-        // columns 0..63: gate, 64..127: up of the same 64 places
-        float h[64];
+        if (!ok) *lost = 1;  // told before the barrier that the sixteen warps share: they leave together
+        // columns 0..31: gate, 32..63: up of the same 32 places
+        float h[32];
         uint32_t amax = 0;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
+        for (int i = 0; i < 16; ++i) {
           float g[2], u[2];
           unpair(acc[i], g[0], g[1]);
-          unpair(acc[32 + i], u[0], u[1]);
+          unpair(acc[16 + i], u[0], u[1]);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const float x = g[j] / (1.0f + expf(-g[j])) * u[j];
@@ -422,46 +457,23 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             amax = max(amax, abs_bits(x));
           }
         }
-        row_amax[half * 128 + row_in] = amax;
-        asm volatile("bar.sync 1, 256;" ::: "memory");
+        row_amax[quarter * 128 + row_in] = amax;
+        asm volatile("bar.sync 1, 512;" ::: "memory");
         if (*lost) break;
-        amax = max(amax, row_amax[(half ^ 1) * 128 + row_in]);
-        asm volatile("bar.sync 1, 256;" ::: "memory");  // before the next tile's values
+#pragma unroll
+        for (int q = 0; q < 4; ++q) amax = max(amax, row_amax[q * 128 + row_in]);
+        asm volatile("bar.sync 1, 512;" ::: "memory");  // before the next tile's values
         const float s = fp8_scale(amax);
         if (there) {
-          if (half == 0) a.p.hs[(int64_t)(w.n0 / 128) * a.p.m + row] = s;
-          uint8_t *out = (uint8_t *)a.p.out + row * a.p.ldo + w.n0 + half * 64;  // (the pitch covers whole blocks)
-#pragma unroll
-          for (int i = 0; i < 64; i += 16) {
-            uint4 q;
-            q.x = fp8_quad(h[i], h[i + 1], h[i + 2], h[i + 3], s), q.y = fp8_quad(h[i + 4], h[i + 5], h[i + 6], h[i + 7], s);
-            q.z = fp8_quad(h[i + 8], h[i + 9], h[i + 10], h[i + 11], s), q.w = fp8_quad(h[i + 12], h[i + 13], h[i + 14], h[i + 15], s);
-            *reinterpret_cast<uint4 *>(out + i) = q;
-          }
-        }
-      }
-      if constexpr (!SWIGLU) {
-        if (there) {
-          TO *out = (TO *)a.p.out + row * a.p.ldo;
-          const int c0 = w.n0 + half * S::kCols;
-          const bool vec = (((uintptr_t)a.p.out | (uint64_t)a.p.ldo * sizeof(TO)) & 15) == 0;
-#pragma unroll
-          for (int i = 0; i < S::kCols; i += 8) {
-            float v[8];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) unpair(acc[i / 2 + j], v[2 * j], v[2 * j + 1]);
-            if (vec && c0 + i + 8 <= a.p.n) {
-              store_row(out + c0 + i, v);
-            } else {
-#pragma unroll
-              for (int j = 0; j < 8; ++j)
-                if (c0 + i + j < a.p.n) out[c0 + i + j] = from_f32<TO>(v[j]);
-            }
-          }
+          if (quarter == 0) a.p.hs[(int64_t)(n0 / 128) * a.p.m + row] = s;
+          const Divisor by = divisor(s);
+          uint4 *out = (uint4 *)((uint8_t *)a.p.out + row * a.p.ldo + n0 + quarter * 32);  // (the pitch covers whole blocks)
+          out[0] = fp8_sixteen(h, by), out[1] = fp8_sixteen(h + 16, by);
         }
       }
       __syncwarp();
     }
+    copy_wait<0>();
   }
   __syncwarp();
   tc_fence_before();
@@ -513,12 +525,19 @@ int run_tiles(const ProductArgs &p, cudaStream_t st) {
   if (!a.error) return TUNA_ERR_CUDA;
   CUtensorMap ma, mb;
   if (const int rc = make_map(&ma, 2, p.a, p.k, p.m, 1, p.lda, 128)) return rc;
-  if (const int rc = make_map(&mb, 3, p.b, p.k, p.n, (int64_t)p.groups * (SWIGLU ? 2 : 1), p.ldb, SWIGLU ? 64 : BN)) return rc;
-  static bool set[64] = {};
+  if (const int rc = make_map(&mb, 3, p.b, p.k, p.n, (int64_t)p.groups * (SWIGLU ? 2 : 1), p.ldb, SWIGLU ? 32 : BN)) return rc;
+  static bool set[64] = {}, fits = false;
   auto kernel = tuna_product_kernel<BN, SWIGLU, B_ROWS, TO>;
-  if (const int rc = allow_smem(kernel, Shape<BN>::kSmem, set)) return rc;
+  if (!__atomic_load_n(&fits, __ATOMIC_ACQUIRE)) {
+    // the warps' shares of registers (setmaxnreg) come out of what the block is launched with
+    cudaFuncAttributes at;
+    if (const int rc = note_cuda(cudaFuncGetAttributes(&at, kernel))) return rc;
+    if ((at.numRegs + 7) / 8 * 8 * kGemmThreads < 128 * kCopyRegs + kSumWarps * 32 * kSumRegs) return TUNA_ERR_INTERNAL;
+    __atomic_store_n(&fits, true, __ATOMIC_RELEASE);
+  }
+  if (const int rc = allow_smem(kernel, Shape<BN>::smem(B_ROWS), set)) return rc;
   const int64_t most = (ceil_div(p.m, 128) + (p.offsets ? p.groups : 0)) * a.n_tiles;
-  return launch(kernel, dim3((unsigned)std::min<int64_t>(most, sm_count())), kGemmThreads, Shape<BN>::kSmem, st, false, ma, mb, a);
+  return launch(kernel, dim3((unsigned)std::min<int64_t>(most, sm_count())), kGemmThreads, Shape<BN>::smem(B_ROWS), st, false, ma, mb, a);
 }
 
 size_t dtype_size(int dtype) { return dtype == TUNA_DTYPE_F32 ? 4 : dtype == TUNA_DTYPE_BF16 ? 2 : 0; }

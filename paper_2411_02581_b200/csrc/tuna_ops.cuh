@@ -130,6 +130,13 @@ __device__ __forceinline__ void store_row(float *p, const float (&v)[N]) {
     reinterpret_cast<float4 *>(p)[i] = make_float4(v[i * 4], v[i * 4 + 1], v[i * 4 + 2], v[i * 4 + 3]);
 }
 
+// 32 bytes to a 32-byte boundary in one instruction: a whole sector for every lane
+__device__ __forceinline__ void store32(void *p, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
+               "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+
 // ---- 8-bit values --------------------------------------------------------------------
 
 // scale = max(amax, 2^-100) / 448 (448 is the largest e4m3 value).  The floor keeps the scale of
@@ -141,15 +148,74 @@ __device__ __forceinline__ float fp8_scale(uint32_t amax_bits) {
   return __fdiv_rn(fmaxf(__uint_as_float(amax_bits), 7.888609052210118e-31f /* 2^-100 */), 448.0f);
 }
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-// e4m3 of a / s and b / s: a true division, because a product with 1 / s would round the many
-// 16-bit inputs that sit halfway between two 8-bit values the other way.
-__device__ __forceinline__ uint32_t fp8_pair(float a, float b, float s) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(__fdiv_rn(b, s)), "f"(__fdiv_rn(a, s)));
+// Division by a block's scale, correctly rounded.  A product with 1 / s alone would round the many
+// 16-bit inputs that sit halfway between two 8-bit values the other way.  Markstein's theorem (IBM
+// J. Res. Dev. 34, 1990): with y = 1 / s correctly rounded and q within one unit of x / s, q + (x - q s) y
+// in fused operations is x / s correctly rounded, unless the fraction of s is all ones.  x y is within
+// 1.5 units, one correction brings it within one, the next one ends it.  x - q s must not underflow, so
+// very small (and very large) scales divide, as NaN ones do.  Five packed operations for two values,
+// against more than eight each for a division (an 8192 x 4096 matrix: 29 us that way).
+struct Divisor {
+  uint64_t y, minus_s;
+  float s;
+  bool plain;
+};
+__device__ __forceinline__ uint64_t pair(uint32_t lo, uint32_t hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
   return r;
 }
-__device__ __forceinline__ uint32_t fp8_quad(float a, float b, float c, float d, float s) {
+__device__ __forceinline__ uint64_t pair(float lo, float hi) { return pair(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ void unpair(uint64_t v, float &lo, float &hi) {
+  uint32_t a, b;
+  asm("mov.b64 {%0, %1}, %2;" : "=r"(a), "=r"(b) : "l"(v));
+  lo = __uint_as_float(a), hi = __uint_as_float(b);
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ Divisor divisor(float s) {
+  Divisor d;
+  const uint32_t bits = __float_as_uint(s);
+  d.plain = !(s >= 8.271806125530277e-25f /* 2^-80 */ && s <= 1.2676506002282294e30f /* 2^100 */) || (bits & 0x7fffff) == 0x7fffff;
+  const float y = __frcp_rn(s);
+  d.s = s, d.y = pair(y, y), d.minus_s = pair(-s, -s);
+  return d;
+}
+__device__ __forceinline__ uint32_t fp8_pair(float a, float b, const Divisor &d) {
+  float qa, qb;
+  if (d.plain) {
+    qa = __fdiv_rn(a, d.s), qb = __fdiv_rn(b, d.s);
+  } else {
+    const uint64_t x = pair(a, b);
+    uint64_t q = mul2(x, d.y);
+    q = fma2(fma2(q, d.minus_s, x), d.y, q);
+    q = fma2(fma2(q, d.minus_s, x), d.y, q);
+    unpair(q, qa, qb);
+    // (the corrections turn -0 into 0)
+    qa = __uint_as_float(__float_as_uint(qa) | (__float_as_uint(a) & 0x80000000u));
+    qb = __uint_as_float(__float_as_uint(qb) | (__float_as_uint(b) & 0x80000000u));
+  }
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(qb), "f"(qa));
+  return r;
+}
+__device__ __forceinline__ uint32_t fp8_quad(float a, float b, float c, float d, const Divisor &s) {
   return fp8_pair(a, b, s) | (fp8_pair(c, d, s) << 16);
+}
+// 16 values in a row
+__device__ __forceinline__ uint4 fp8_sixteen(const float *v, const Divisor &s) {
+  uint4 u;
+  u.x = fp8_quad(v[0], v[1], v[2], v[3], s), u.y = fp8_quad(v[4], v[5], v[6], v[7], s);
+  u.z = fp8_quad(v[8], v[9], v[10], v[11], s), u.w = fp8_quad(v[12], v[13], v[14], v[15], s);
+  return u;
 }
 
 // ---- barriers in shared memory ---------------------------------------------------------
@@ -246,27 +312,13 @@ __device__ __forceinline__ void tmem_wait(uint32_t (&r)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
 }
-__device__ __forceinline__ uint64_t pair(uint32_t lo, uint32_t hi) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
-  return r;
+// Four-byte asynchronous copy to the caller's own shared memory, and its groups.
+__device__ __forceinline__ void copy4(uint32_t dst, const void *src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
-__device__ __forceinline__ uint64_t pair(float lo, float hi) { return pair(__float_as_uint(lo), __float_as_uint(hi)); }
-__device__ __forceinline__ void unpair(uint64_t v, float &lo, float &hi) {
-  uint32_t a, b;
-  asm("mov.b64 {%0, %1}, %2;" : "=r"(a), "=r"(b) : "l"(v));
-  lo = __uint_as_float(a), hi = __uint_as_float(b);
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 #endif  // __CUDACC__
 
 }  // namespace tuna_ops
