@@ -150,8 +150,9 @@ __global__ void __launch_bounds__(256) tuna_quantize_tile_kernel(QuantArgs a) {
 // thread at BN = 256), while the tensor cores fill the other one.  The promotion is what bounds
 // the kernel: 256 cycles of packed multiply-adds a block at least, and the tensor-memory loads
 // in front of them.  Eight warps with 128 sums each had no registers left to load ahead (163 us
-// for 8192 x 4096 x 4096).  The scales come through a small ring of asynchronous copies that
-// every thread fills for itself, three blocks ahead: read when needed, their latency set the pace.
+// for 8192 x 4096 x 4096).  Two more warps fetch the scales, four blocks ahead, multiply them and
+// leave one factor a row and 128 columns beside each accumulator: loads, shuffles or asynchronous
+// copies of their own cost the promotion warps 500 cycles a block.
 //
 // With `swiglu` the 256 columns are 4 x (32 gate + 32 up) rows of the two matrices, so that the
 // thread that holds a gate value holds its up value, and a tile is exactly one 128-block of the
@@ -165,8 +166,7 @@ struct TileArgs {
 
 constexpr int kSumWarps = 16;   // promotion: four quarters of the columns x 128 rows
 constexpr int kGemmThreads = 128 + kSumWarps * 32;
-constexpr int kScaleRing = 4;
-constexpr int kCopyRegs = 32, kSumRegs = 112;  // registers of a thread: copying and issuing warps, promotion
+constexpr int kCopyRegs = 64, kSumRegs = 104;  // registers of a thread: copying and issuing warps, promotion
 constexpr int kMaxGroups = TUNA_MOE_MAX_EXPERTS;
 
 template <int BN>
@@ -174,11 +174,9 @@ struct Shape {
   static constexpr int kStages = BN == 256 ? 4 : 6;
   static constexpr int kStageBytes = 128 * 128 + BN * 128;
   static constexpr int kCols = BN / 4;  // accumulator columns of a thread
-  // stages, then the rings of row scales (and of column scales: a copy for each warp), the rows'
-  // largest magnitudes, the groups' tile offsets, barriers and flags
-  static constexpr size_t smem(bool b_rows) {
-    return 1024 + (size_t)kStages * kStageBytes + kScaleRing * kSumWarps * (32 + (b_rows ? 64 : 0)) * 4 + 512 * 4 + (kMaxGroups + 8) * 4 + 256;
-  }
+  // stages, then the factors beside the two accumulators, the rows' largest magnitudes, the groups'
+  // tile offsets, barriers and flags
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + 2 * 384 * 4 + 512 * 4 + (kMaxGroups + 8) * 4 + 256;
 };
 
 // Tile t of the walk: the group it is in (never walked backwards), its rows and columns.
@@ -205,9 +203,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   using S = Shape<BN>;
   extern __shared__ char smem_raw[];
   char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-  float *row_scale = (float *)(smem + (size_t)S::kStages * S::kStageBytes);       // [ring][16 warps][32]
-  float *col_scale = row_scale + kScaleRing * kSumWarps * 32;                     // [ring][16 warps][64], if B_ROWS
-  uint32_t *row_amax = (uint32_t *)(col_scale + (B_ROWS ? kScaleRing * kSumWarps * 64 : 0));  // [4][128]
+  // beside each accumulator: [2][128] factors of the rows for either half of the columns, or with
+  // B_ROWS [128] scales of the rows, then [256] of the columns
+  float *factors = (float *)(smem + (size_t)S::kStages * S::kStageBytes);
+  uint32_t *row_amax = (uint32_t *)(factors + 2 * 384);  // [4][128]
   int *tile_base = (int *)(row_amax + 512);
   uint64_t *bars = (uint64_t *)(tile_base + kMaxGroups + 8);
   volatile int *given_up = (volatile int *)(bars + 2 * S::kStages + 5);
@@ -218,7 +217,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S::kStages; ++s) mbar_init(full + 8 * s, 1), mbar_init(empty + 8 * s, 1);
-    for (int s = 0; s < 2; ++s) mbar_init(done + 8 * s, 1), mbar_init(freed + 8 * s, kSumWarps);
+    for (int s = 0; s < 2; ++s) mbar_init(done + 8 * s, 3), mbar_init(freed + 8 * s, kSumWarps);  // done: the tensor cores and two scale warps
     mbar_init(drained, 1);
     *given_up = 0, *lost = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -308,94 +307,103 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         tc_commit(drained);
         mbar_wait(drained, 0, &never);
       }
+    } else if (warp >= 2) {
+      // ---- scales: a lane has two rows of the tile, and with B_ROWS four columns
+      constexpr int kAhead = 4, kVals = B_ROWS ? 6 : 4;
+      const int i = threadIdx.x - 64, tiles_n = (a.p.n + 127) / 128;
+      int buf = 0, buf_phase = 0;
+      bool ok = true;
+      Walk w;
+      for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+        walk_to(w, t, a, tile_base, SWIGLU ? BN / 2 : BN);
+        const float *sa0 = a.p.sa + min(w.row + i, w.end - 1), *sa1 = a.p.sa + min(w.row + i + 64, w.end - 1);
+        const float *sb0 = a.p.sb, *sb1 = a.p.sb;
+        if (SWIGLU) {
+          sb0 += ((int64_t)(w.g * 2) * tiles_n + w.n0 / 128) * blocks;
+          sb1 = sb0 + (int64_t)tiles_n * blocks;
+        } else if (!B_ROWS) {
+          sb0 += ((int64_t)w.g * tiles_n + w.n0 / 128) * blocks;
+          sb1 = w.n0 / 128 + 1 < tiles_n ? sb0 + blocks : sb0;
+        }
+        float next[kAhead][kVals];
+        auto fetch = [&](int kb0) {
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j) {
+            const int kb = min(kb0 + j, blocks - 1);
+            next[j][0] = __ldg(sa0 + (int64_t)kb * a.p.m), next[j][1] = __ldg(sa1 + (int64_t)kb * a.p.m);
+            if (B_ROWS) {
+#pragma unroll
+              for (int q = 0; q < 4; ++q) next[j][2 + q] = __ldg(a.p.sb + (int64_t)kb * a.p.n + min(w.n0 + i + q * 64, a.p.n - 1));
+            } else {
+              next[j][2] = __ldg(sb0 + kb), next[j][3] = __ldg(sb1 + kb);
+            }
+          }
+        };
+        fetch(0);
+        for (int kb0 = 0; ok && kb0 < blocks; kb0 += kAhead) {
+          float now[kAhead][kVals];
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+            for (int q = 0; q < kVals; ++q) now[j][q] = next[j][q];
+          if (kb0 + kAhead < blocks) fetch(kb0 + kAhead);
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j) {
+            if (kb0 + j >= blocks) break;
+            ok = __all_sync(~0u, mbar_wait(freed + 8 * buf, buf_phase ^ 1, given_up));
+            if (!ok) break;
+            float *f = factors + buf * 384 + i;
+            if (B_ROWS) {
+              f[0] = now[j][0], f[64] = now[j][1];
+#pragma unroll
+              for (int q = 0; q < 4; ++q) f[128 + q * 64] = now[j][2 + q];
+            } else {
+              f[0] = now[j][0] * now[j][2], f[64] = now[j][1] * now[j][2];
+              f[128] = now[j][0] * now[j][3], f[192] = now[j][1] * now[j][3];
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(done + 8 * buf);
+            if (++buf == 2) buf = 0, buf_phase ^= 1;
+          }
+        }
+      }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSumRegs));
     // ---- promotion and results: thread = one row, columns [quarter * kCols, ...) of the tile
     const int quarter = (warp - 4) >> 2, row_in = (warp & 3) * 32 + lane;
     const uint32_t from = tmem + ((uint32_t)((warp & 3) * 32) << 16) + quarter * S::kCols;
-    const uint32_t my_row = smem_u32(row_scale + (warp - 4) * 32 + lane), my_col = smem_u32(col_scale + (warp - 4) * 64 + lane);
-    constexpr int kRowStep = kSumWarps * 32 * 4, kColStep = kSumWarps * 64 * 4;
-    const int tiles_n = (a.p.n + 127) / 128;
-    int buf = 0, buf_phase = 0, slot = 0;
+    // its factor: of its row and of its half of the columns (SWIGLU: gate, and up 128 places on)
+    const uint32_t factor = smem_u32(factors) + (SWIGLU || B_ROWS ? row_in : (BN == 256 ? quarter >> 1 : 0) * 128 + row_in) * 4;
+    int buf = 0, buf_phase = 0;
     bool ok = true;
-    // where the scales of a tile are: of this thread's row; of its columns, one a block of k, or with
-    // SWIGLU one for each matrix, or with B_ROWS one a column and block
     Walk w;
-    const float *sa = nullptr, *sb0 = nullptr, *sb1 = nullptr;
-    auto aim = [&](int64_t t) {
-      walk_to(w, t, a, tile_base, SWIGLU ? BN / 2 : BN);
-      sa = a.p.sa + min(w.row + row_in, w.end - 1);
-      if (SWIGLU) {
-        sb0 = a.p.sb + ((int64_t)(w.g * 2) * tiles_n + w.n0 / 128) * blocks;
-        sb1 = sb0 + (int64_t)tiles_n * blocks;
-      } else if (B_ROWS) {
-        sb0 = a.p.sb + min(w.n0 + quarter * S::kCols + lane, a.p.n - 1);
-        sb1 = a.p.sb + min(w.n0 + quarter * S::kCols + lane + 32, a.p.n - 1);
-      } else {
-        sb0 = a.p.sb + ((int64_t)w.g * tiles_n + min((w.n0 + quarter * S::kCols) / 128, tiles_n - 1)) * blocks;
-      }
-    };
-    auto feed = [&](int kb, int at) {  // block kb's scales into ring place `at` (or an empty group, which keeps the count)
-      if (kb < blocks) {
-        copy4(my_row + at * kRowStep, sa + (int64_t)kb * a.p.m);
-        if (B_ROWS) {
-          copy4(my_col + at * kColStep, sb0 + (int64_t)kb * a.p.n);
-          if (S::kCols > 32) copy4(my_col + at * kColStep + 128, sb1 + (int64_t)kb * a.p.n);
-        }
-      }
-      copy_commit();
-    };
-    float fb = 0.0f, fc = 0.0f;  // lane i: the columns' scale of block i of the running 32
-    auto fetch = [&](int kb0) {
-      if (!B_ROWS) fb = __ldg(sb0 + min(kb0 + lane, blocks - 1));
-      if (SWIGLU) fc = __ldg(sb1 + min(kb0 + lane, blocks - 1));
-    };
-    auto open = [&](int64_t t) {
-      aim(t);
-      fetch(0);
-#pragma unroll
-      for (int i = 0; i < kScaleRing - 1; ++i) feed(i, (slot + i) % kScaleRing);
-    };
-    if (blockIdx.x < tiles) open(blockIdx.x);
     for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+      walk_to(w, t, a, tile_base, SWIGLU ? BN / 2 : BN);
       const int64_t row = w.row + row_in;
       const bool there = row < w.end;
       const int n0 = w.n0;
       uint64_t acc[S::kCols / 2];
 #pragma unroll
       for (int i = 0; i < S::kCols / 2; ++i) acc[i] = 0;
-      // the factors of block kb: read from the ring one block early, behind the first tensor-memory load
-      float s0, s1;
-      int here = 0;  // the ring place of the block at hand
-      auto prepare = [&](int kb) {
-        copy_wait<kScaleRing - 2>();
-        if (B_ROWS) __syncwarp();  // the other lanes' columns too
-        float ra;
-        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ra) : "r"(my_row + slot * kRowStep) : "memory");
-        s0 = B_ROWS ? ra : ra * __shfl_sync(~0u, fb, kb & 31), s1 = SWIGLU ? ra * __shfl_sync(~0u, fc, kb & 31) : s0;
-        if ((kb & 31) == 31 && kb + 1 < blocks) fetch(kb + 1);
-        here = slot;
-        slot = (slot + 1) % kScaleRing;
-      };
-      prepare(0);
       for (int kb = 0; kb < blocks; ++kb) {
         ok = __all_sync(~0u, mbar_wait(done + 8 * buf, buf_phase, given_up));  // (and the warp is whole for the loads)
         if (!ok) break;
         tc_fence_after();
-        const uint64_t p0 = pair(s0, s0), p1 = pair(s1, s1);
-        const float *cs = col_scale + ((size_t)here * kSumWarps + (warp - 4)) * 64;
         uint32_t v[2][16];
         tmem_load16(from + buf * BN, v[0]);
-        // (the ring place that is filled here was read two blocks ago, by the whole warp)
-        feed(kb + kScaleRing - 1, (here + kScaleRing - 1) % kScaleRing);
-        if (kb + 1 < blocks) prepare(kb + 1);
+        float s0, s1 = 0.0f;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(s0) : "r"(factor + buf * 384 * 4) : "memory");
+        if (SWIGLU) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(s1) : "r"(factor + buf * 384 * 4 + 512) : "memory");
+        const uint64_t p0 = pair(s0, s0), p1 = pair(s1, s1);
+        const float *cs = factors + buf * 384 + 128 + quarter * S::kCols;
 #pragma unroll
         for (int c = 0; c < S::kCols / 16; ++c) {
           tmem_wait(v[c & 1]);
           if (c + 1 < S::kCols / 16) {
             tmem_load16(from + buf * BN + (c + 1) * 16, v[(c + 1) & 1]);
-          } else {  // everything is in registers: the accumulator may be filled again
+          } else if (!B_ROWS) {  // everything is in registers, the factors too: the accumulator may be filled again
+            asm volatile("" ::"f"(s0), "f"(s1));
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(freed + 8 * buf);
@@ -412,9 +420,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             acc[c * 8 + i + 1] = fma2(pair(x[2 * i + 2], x[2 * i + 3]), g, acc[c * 8 + i + 1]);
           }
         }
+        if (B_ROWS) {  // (the column scales have been read only now)
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(freed + 8 * buf);
+        }
         if (++buf == 2) buf = 0, buf_phase ^= 1;
       }
-      if (ok && t + gridDim.x < tiles) open(t + gridDim.x);  // the next tile's scales travel during this one's stores
       if constexpr (!SWIGLU) {
         if (!ok) break;
         if (there) {
@@ -473,7 +485,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       }
       __syncwarp();
     }
-    copy_wait<0>();
   }
   __syncwarp();
   tc_fence_before();
@@ -535,9 +546,9 @@ int run_tiles(const ProductArgs &p, cudaStream_t st) {
     if ((at.numRegs + 7) / 8 * 8 * kGemmThreads < 128 * kCopyRegs + kSumWarps * 32 * kSumRegs) return TUNA_ERR_INTERNAL;
     __atomic_store_n(&fits, true, __ATOMIC_RELEASE);
   }
-  if (const int rc = allow_smem(kernel, Shape<BN>::smem(B_ROWS), set)) return rc;
+  if (const int rc = allow_smem(kernel, Shape<BN>::kSmem, set)) return rc;
   const int64_t most = (ceil_div(p.m, 128) + (p.offsets ? p.groups : 0)) * a.n_tiles;
-  return launch(kernel, dim3((unsigned)std::min<int64_t>(most, sm_count())), kGemmThreads, Shape<BN>::smem(B_ROWS), st, false, ma, mb, a);
+  return launch(kernel, dim3((unsigned)std::min<int64_t>(most, sm_count())), kGemmThreads, Shape<BN>::kSmem, st, false, ma, mb, a);
 }
 
 size_t dtype_size(int dtype) { return dtype == TUNA_DTYPE_F32 ? 4 : dtype == TUNA_DTYPE_BF16 ? 2 : 0; }
