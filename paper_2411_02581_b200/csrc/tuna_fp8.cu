@@ -161,6 +161,7 @@ struct TileArgs {
   ProductArgs p;
   int blocks;   // of k
   int n_tiles;
+  int store_tiles;  // results leave through map_out
   int *error;
 };
 
@@ -171,12 +172,13 @@ constexpr int kMaxGroups = TUNA_MOE_MAX_EXPERTS;
 
 template <int BN>
 struct Shape {
-  static constexpr int kStages = BN == 256 ? 4 : 6;
+  static constexpr int kStages = BN == 256 ? 3 : 6;
   static constexpr int kStageBytes = 128 * 128 + BN * 128;
   static constexpr int kCols = BN / 4;  // accumulator columns of a thread
-  // stages, then the factors beside the two accumulators, the rows' largest magnitudes, the groups'
+  static constexpr int kOutBytes = BN == 256 ? kSumWarps * 4096 : 0;  // each promotion warp's 32 x 64 results, on their way out
+  // stages, results, then the factors beside the two accumulators, the rows' largest magnitudes, the groups'
   // tile offsets, barriers and flags
-  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + 2 * 384 * 4 + 512 * 4 + (kMaxGroups + 8) * 4 + 256;
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kOutBytes + 2 * 384 * 4 + 512 * 4 + (kMaxGroups + 8) * 4 + 256;
 };
 
 // Tile t of the walk: the group it is in (never walked backwards), its rows and columns.
@@ -199,13 +201,14 @@ __device__ __forceinline__ void walk_to(Walk &w, int64_t t, const TileArgs &a, c
 
 template <int BN, bool SWIGLU, bool B_ROWS, typename TO>
 __global__ void __launch_bounds__(kGemmThreads, 1)
-    tuna_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const TileArgs a) {
+    tuna_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                        const __grid_constant__ CUtensorMap map_out, const TileArgs a) {
   using S = Shape<BN>;
   extern __shared__ char smem_raw[];
   char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   // beside each accumulator: [2][128] factors of the rows for either half of the columns, or with
   // B_ROWS [128] scales of the rows, then [256] of the columns
-  float *factors = (float *)(smem + (size_t)S::kStages * S::kStageBytes);
+  float *factors = (float *)(smem + (size_t)S::kStages * S::kStageBytes + S::kOutBytes);
   uint32_t *row_amax = (uint32_t *)(factors + 2 * 384);  // [4][128]
   int *tile_base = (int *)(row_amax + 512);
   uint64_t *bars = (uint64_t *)(tile_base + kMaxGroups + 8);
@@ -429,10 +432,30 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       }
       if constexpr (!SWIGLU) {
         if (!ok) break;
-        if (there) {
+        // 32 whole rows of bf16 go to shared memory and from there by a tensor copy, which runs on
+        // during the next tile: stored from registers, all blocks at once, they cost 3 us a tile.
+        // Rows that a group's end cuts, and results that a tensor copy cannot reach, are stored here.
+        const bool whole = sizeof(TO) == 2 && S::kOutBytes && a.store_tiles && w.row + (warp & 3) * 32 + 31 < w.end;
+        if (whole) {
+          const uint32_t to = smem_u32(smem) + S::kStages * S::kStageBytes + (warp - 4) * 4096;
+          if (lane == 0) tma_store_read();
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < S::kCols / 8; ++i) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) unpair(acc[i * 4 + j], v[2 * j], v[2 * j + 1]);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + lane * 128 + ((i ^ (lane & 7)) * 16)), "r"(pack_bf16(v[0], v[1])),
+                         "r"(pack_bf16(v[2], v[3])), "r"(pack_bf16(v[4], v[5])), "r"(pack_bf16(v[6], v[7]))
+                         : "memory");
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0 && n0 + quarter * S::kCols < a.p.n) tma_store_2d(&map_out, n0 + quarter * S::kCols, (int)(row - lane), to);
+        } else if (there) {
           TO *out = (TO *)a.p.out + row * a.p.ldo;
           const int c0 = n0 + quarter * S::kCols;
-          // whole 32-byte sectors: as 16-byte stores, the results took a third of the kernel's time
+          // whole 32-byte sectors
           constexpr int kRun = 32 / sizeof(TO);
           const bool vec = (((uintptr_t)a.p.out | (uint64_t)a.p.ldo * sizeof(TO)) & 31) == 0;
 #pragma unroll
@@ -485,6 +508,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       }
       __syncwarp();
     }
+    if (S::kOutBytes && lane == 0) tma_store_done();
   }
   __syncwarp();
   tc_fence_before();
@@ -513,14 +537,15 @@ EncodeTiled encoder() {
   return fn;
 }
 
-// An e4m3 operand: k contiguous, then rows, then matrices; boxes of 128 x `box` rows.
-int make_map(CUtensorMap *map, int rank, const void *p, int64_t k, int64_t rows, int64_t matrices, int64_t ld, int box) {
+// An e4m3 operand (or bf16 results): k contiguous, then rows, then matrices; boxes of 128 bytes x `box` rows.
+int make_map(CUtensorMap *map, int rank, const void *p, int64_t k, int64_t rows, int64_t matrices, int64_t ld, int box, bool bf16 = false) {
   EncodeTiled f = encoder();
   if (!f) return TUNA_ERR_CUDA;
   const cuuint64_t dims[3] = {(cuuint64_t)k, (cuuint64_t)rows, (cuuint64_t)matrices};
-  const cuuint64_t strides[2] = {(cuuint64_t)ld, (cuuint64_t)(ld * rows)};
-  const cuuint32_t boxes[3] = {128, (cuuint32_t)box, 1}, ones[3] = {1, 1, 1};
-  const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, (cuuint32_t)rank, const_cast<void *>(p), dims, strides, boxes, ones,
+  const int size = bf16 ? 2 : 1;
+  const cuuint64_t strides[2] = {(cuuint64_t)(ld * size), (cuuint64_t)(ld * size * rows)};
+  const cuuint32_t boxes[3] = {(cuuint32_t)(128 / size), (cuuint32_t)box, 1}, ones[3] = {1, 1, 1};
+  const CUresult r = f(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, (cuuint32_t)rank, const_cast<void *>(p), dims, strides, boxes, ones,
                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? TUNA_OK : note_cuda(cudaErrorInvalidValue);
@@ -534,9 +559,13 @@ int run_tiles(const ProductArgs &p, cudaStream_t st) {
   a.n_tiles = (int)ceil_div(p.n, SWIGLU ? BN / 2 : BN);
   a.error = error_word();
   if (!a.error) return TUNA_ERR_CUDA;
-  CUtensorMap ma, mb;
+  CUtensorMap ma, mb, mo;
   if (const int rc = make_map(&ma, 2, p.a, p.k, p.m, 1, p.lda, 128)) return rc;
   if (const int rc = make_map(&mb, 3, p.b, p.k, p.n, (int64_t)p.groups * (SWIGLU ? 2 : 1), p.ldb, SWIGLU ? 32 : BN)) return rc;
+  mo = ma;
+  a.store_tiles = Shape<BN>::kOutBytes && !SWIGLU && !p.out_f32 && aligned(p.out, 16) && p.ldo % 8 == 0;
+  if (a.store_tiles)
+    if (const int rc = make_map(&mo, 2, p.out, p.n, p.m, 1, p.ldo, 32, true)) return rc;
   static bool set[64] = {}, fits = false;
   auto kernel = tuna_product_kernel<BN, SWIGLU, B_ROWS, TO>;
   if (!__atomic_load_n(&fits, __ATOMIC_ACQUIRE)) {
@@ -548,7 +577,7 @@ int run_tiles(const ProductArgs &p, cudaStream_t st) {
   }
   if (const int rc = allow_smem(kernel, Shape<BN>::kSmem, set)) return rc;
   const int64_t most = (ceil_div(p.m, 128) + (p.offsets ? p.groups : 0)) * a.n_tiles;
-  return launch(kernel, dim3((unsigned)std::min<int64_t>(most, sm_count())), kGemmThreads, Shape<BN>::kSmem, st, false, ma, mb, a);
+  return launch(kernel, dim3((unsigned)std::min<int64_t>(most, sm_count())), kGemmThreads, Shape<BN>::kSmem, st, false, ma, mb, mo, a);
 }
 
 size_t dtype_size(int dtype) { return dtype == TUNA_DTYPE_F32 ? 4 : dtype == TUNA_DTYPE_BF16 ? 2 : 0; }
