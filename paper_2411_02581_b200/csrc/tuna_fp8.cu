@@ -30,114 +30,137 @@ struct QuantArgs {
   uint8_t *q;
   float *scale;
 };
+// A block of threads takes 16 rows x 512 columns, a warp two of the rows, whose loads it has in
+// flight together.
+constexpr int kQuantRows = 16;
 template <typename T>
 __global__ void __launch_bounds__(256) tuna_quantize_rows_kernel(QuantArgs a) {
   wait_previous();
   allow_next();
-  const int parts = (a.cols + 511) / 512;
-  const int lane = threadIdx.x & 31;
-  for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < a.rows * parts; i += (int64_t)gridDim.x * 8) {
-    const int64_t r = i / parts;
-    const int c = (int)(i - r * parts) * 512 + lane * 16;
-    const int64_t from = a.gather ? a.gather[r] : r;
+  const int lane = threadIdx.x & 31, c = (int)blockIdx.y * 512 + lane * 16;
+  const int64_t r0 = (int64_t)blockIdx.x * kQuantRows + (threadIdx.x >> 5) * 2;
+  Eight<T> x[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int64_t r = r0 + i;
+    const int64_t from = r >= a.rows ? -1 : a.gather ? __ldg(a.gather + r) : r;
     const bool there = from >= 0 && from < a.in_rows;
-    const T *x = reinterpret_cast<const T *>(a.x) + (there ? from : 0) * a.ldx + c;
-    float v[16];
-    if (there && a.vec && c + 16 <= a.cols) {
-      load_row(x, v);
-    } else {
+    const T *p = reinterpret_cast<const T *>(a.x) + (there ? from : 0) * a.ldx + c;
+    x[i][0].load(p, a.vec, there ? a.cols - c : 0), x[i][1].load(p + 8, a.vec, there ? a.cols - c - 8 : 0);
+  }
 #pragma unroll
-      for (int j = 0; j < 16; ++j) v[j] = there && c + j < a.cols ? to_f32(x[j]) : 0.0f;
-    }
-    uint32_t amax = 0;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) amax = max(amax, abs_bits(v[j]));
+  for (int i = 0; i < 2; ++i) {
+    const int64_t r = r0 + i;
+    uint32_t amax = Eight<T>::top_bits(x[i][1].top(x[i][0].top(0)));
 #pragma unroll
     for (int d = 1; d < 8; d <<= 1) amax = max(amax, __shfl_xor_sync(~0u, amax, d));
+    if (r >= a.rows || c >= a.cols) continue;
     const float s = fp8_scale(amax);
-    if (c < a.cols) {
-      *reinterpret_cast<uint4 *>(a.q + r * a.ldq + c) = fp8_sixteen(v, divisor(s));
-      if (lane % 8 == 0) a.scale[(int64_t)(c / 128) * a.rows + r] = s;
-    }
+    float v[16];
+    x[i][0].values(v), x[i][1].values(v + 8);
+    *reinterpret_cast<uint4 *>(a.q + r * a.ldq + c) = fp8_sixteen(v, divisor(s));
+    if (lane % 8 == 0) a.scale[(int64_t)(c / 128) * a.rows + r] = s;
   }
 }
 
-// Blocks that span rows: a 128 x 128 tile goes through shared memory.
+// Blocks that span rows: a block of threads takes a 128 x 128 tile, 8 columns of 8 rows a thread.
+// As they are (kTiles), the tile never leaves the registers.  Turned (kColumns, kTilesT), it goes
+// through shared memory in its own type; a thread then has 32 rows of two columns, read as pairs.
 enum { kColumns = 1, kTiles = 2, kTilesT = 3 };
-constexpr int kTilePitch = 129;  // words: columns and rows of the tile are both free of bank conflicts
-constexpr size_t kTileSmem = (size_t)128 * kTilePitch * 4;
+template <typename T>
+struct TileShape {
+  static constexpr int kPitch = 128 + 16 / sizeof(T);  // rows stay on 16-byte boundaries, four banks apart
+  static constexpr size_t kSmem = 128 * kPitch * sizeof(T);
+};
 template <int MODE, typename T>
 __global__ void __launch_bounds__(256) tuna_quantize_tile_kernel(QuantArgs a) {
-  extern __shared__ float tile[];
-  __shared__ uint32_t part[256];
+  extern __shared__ __align__(16) char tile_raw[];
+  T *tile = reinterpret_cast<T *>(tile_raw);
+  constexpr int kPitch = TileShape<T>::kPitch;
+  __shared__ uint32_t part[4][128];
   wait_previous();
   allow_next();
   const int col_tiles = (a.cols + 127) / 128;
   const int64_t r0 = (int64_t)(blockIdx.x / col_tiles) * 128;
   const int c0 = (int)(blockIdx.x % col_tiles) * 128;
-  const int tid = threadIdx.x, lane = tid & 31;
-  uint32_t amax = 0;
-  for (int r = tid >> 5; r < 128; r += 8) {
-    const int c = c0 + lane * 4;
-    const T *x = reinterpret_cast<const T *>(a.x) + (r0 + r) * a.ldx + c;
-    float v[4] = {};
-    if (r0 + r < a.rows) {
-      if (a.vec && c + 4 <= a.cols) {
-        if constexpr (sizeof(T) == 2) {
-          const uint2 u = *reinterpret_cast<const uint2 *>(x);
-          v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xffff0000u);
-          v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xffff0000u);
-        } else {
-          load_row(x, v);
-        }
-      } else {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int mine = tid >> 4, c = (tid & 15) * 8;  // rows mine, mine + 16, ...; columns c .. c + 7
+  Eight<T> x[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (c + j < a.cols) v[j] = to_f32(x[j]);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      tile[r * kTilePitch + lane * 4 + j] = v[j];
-      if (MODE != kColumns) amax = max(amax, abs_bits(v[j]));
-    }
+  for (int i = 0; i < 8; ++i) {
+    const int64_t r = r0 + mine + i * 16;
+    x[i].load(reinterpret_cast<const T *>(a.x) + r * a.ldx + c0 + c, a.vec, r < a.rows ? a.cols - c0 - c : 0);
   }
+  uint32_t amax = 0;
   if (MODE != kColumns) {
 #pragma unroll
+    for (int i = 0; i < 8; ++i) amax = x[i].top(amax);
+    amax = Eight<T>::top_bits(amax);
+#pragma unroll
     for (int d = 1; d < 32; d <<= 1) amax = max(amax, __shfl_xor_sync(~0u, amax, d));
-    if (lane == 0) part[tid >> 5] = amax;
+    if (lane == 0) part[0][warp] = amax;
+  }
+  if (MODE != kTiles) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int q = 0; q < Eight<T>::kWords; ++q) *reinterpret_cast<uint4 *>(tile + (mine + i * 16) * kPitch + c + q * (8 / Eight<T>::kWords)) = x[i].w[q];
   }
   __syncthreads();
-  const int i = tid & 127, half = tid >> 7;  // the output row of this tile, and which 64 values of it
+  if (MODE != kColumns) {
+#pragma unroll
+    for (int w = 0; w < 8; ++w) amax = max(amax, part[0][w]);
+  }
+  if (MODE == kTiles) {
+    const float s = fp8_scale(amax);
+    const Divisor by = divisor(s);
+    if (tid == 0) a.scale[(r0 / 128) * col_tiles + c0 / 128] = s;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t r = r0 + mine + i * 16;
+      float v[8];
+      x[i].values(v);
+      uint32_t w[2];
+      fp8_run<8>(v, by, w);
+      // (rows are written up to the next multiple of 16 columns, with zeros)
+      if (r < a.rows && c0 + c < (a.cols + 15) / 16 * 16) *reinterpret_cast<uint2 *>(a.q + r * a.ldq + c0 + c) = make_uint2(w[0], w[1]);
+    }
+    return;
+  }
+  const int two = (tid & 63) * 2, quarter = tid >> 6;  // columns two, two + 1; rows quarter * 32 ..
+  float t[2][32];
+  uint32_t top[2] = {0, 0};
+#pragma unroll
+  for (int r = 0; r < 32; ++r) {
+    const T *p = tile + (quarter * 32 + r) * kPitch + two;
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t u = *reinterpret_cast<const uint32_t *>(p);
+      t[0][r] = __uint_as_float(u << 16), t[1][r] = __uint_as_float(u & 0xffff0000u);
+    } else {
+      const float2 u = *reinterpret_cast<const float2 *>(p);
+      t[0][r] = u.x, t[1][r] = u.y;
+    }
+    if (MODE == kColumns) top[0] = max(top[0], abs_bits(t[0][r])), top[1] = max(top[1], abs_bits(t[1][r]));
+  }
   if (MODE == kColumns) {
-#pragma unroll 16
-    for (int r = 0; r < 64; ++r) amax = max(amax, abs_bits(tile[(half * 64 + r) * kTilePitch + i]));
-    part[tid] = amax;
+    part[quarter][two] = top[0], part[quarter][two + 1] = top[1];
     __syncthreads();
-    amax = max(part[i], part[i + 128]);
-  } else {
-    amax = 0;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) amax = max(amax, part[w]);
   }
-  const float s = fp8_scale(amax);
-  const bool turned = MODE != kTiles;
-  const int64_t out_row = (turned ? c0 : r0) + i, out_rows = turned ? a.cols : a.rows;
-  const int64_t out_col = (turned ? r0 : c0) + half * 64, out_cols = turned ? a.rows : a.cols;
-  if (MODE == kColumns) {
-    if (half == 0 && out_row < out_rows) a.scale[(r0 / 128) * a.cols + out_row] = s;
-  } else if (tid == 0) {
-    a.scale[MODE == kTiles ? (r0 / 128) * col_tiles + c0 / 128 : (c0 / 128) * ((a.rows + 127) / 128) + r0 / 128] = s;
-  }
-  if (out_row >= out_rows) return;
-  const Divisor by = divisor(s);
 #pragma unroll
-  for (int j = 0; j < 64; j += 16) {
-    if (out_col + j >= out_cols) break;
-    float v[16];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) v[e] = turned ? tile[(half * 64 + j + e) * kTilePitch + i] : tile[i * kTilePitch + half * 64 + j + e];
-    *reinterpret_cast<uint4 *>(a.q + out_row * a.ldq + out_col + j) = fp8_sixteen(v, by);
+  for (int e = 0; e < 2; ++e) {
+    const int64_t out_row = c0 + two + e, out_col = r0 + quarter * 32;
+    if (MODE == kColumns) amax = max(max(part[0][two + e], part[1][two + e]), max(part[2][two + e], part[3][two + e]));
+    const float s = fp8_scale(amax);
+    const Divisor by = divisor(s);
+    if (MODE == kColumns) {
+      if (quarter == 0 && out_row < a.cols) a.scale[(r0 / 128) * a.cols + out_row] = s;
+    } else if (tid == 0 && e == 0) {
+      a.scale[(c0 / 128) * ((a.rows + 127) / 128) + r0 / 128] = s;
+    }
+    if (out_row >= a.cols) continue;
+    uint4 *q = reinterpret_cast<uint4 *>(a.q + out_row * a.ldq + out_col);
+    if (out_col < a.rows) q[0] = fp8_sixteen(t[e], by);
+    if (out_col + 16 < a.rows) q[1] = fp8_sixteen(t[e] + 16, by);
   }
 }
 
@@ -585,8 +608,9 @@ size_t dtype_size(int dtype) { return dtype == TUNA_DTYPE_F32 ? 4 : dtype == TUN
 template <int MODE, typename T>
 int run_quantize_tiles(const QuantArgs &a, cudaStream_t st) {
   static bool set[64] = {};
-  if (const int rc = allow_smem(tuna_quantize_tile_kernel<MODE, T>, kTileSmem, set)) return rc;
-  return launch(tuna_quantize_tile_kernel<MODE, T>, dim3((unsigned)(ceil_div(a.rows, 128) * ceil_div(a.cols, 128))), 256, kTileSmem, st, false, a);
+  const size_t smem = MODE == kTiles ? 0 : TileShape<T>::kSmem;
+  if (const int rc = allow_smem(tuna_quantize_tile_kernel<MODE, T>, smem, set)) return rc;
+  return launch(tuna_quantize_tile_kernel<MODE, T>, dim3((unsigned)(ceil_div(a.rows, 128) * ceil_div(a.cols, 128))), 256, smem, st, false, a);
 }
 
 }  // namespace
@@ -611,7 +635,7 @@ int launch_quantize_rows(const void *x, bool f32, int64_t rows, int cols, int64_
   QuantArgs a = {};
   a.x = x, a.rows = rows, a.cols = cols, a.ldx = ldx, a.gather = gather, a.in_rows = in_rows, a.q = (uint8_t *)q, a.ldq = ldq, a.scale = scale;
   a.vec = aligned(x, 16) && ldx * (f32 ? 4 : 2) % 16 == 0;
-  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(rows * ceil_div(cols, 512), 8), (int64_t)sm_count() * 32));
+  const dim3 grid((unsigned)ceil_div(rows, kQuantRows), (unsigned)ceil_div(cols, 512));
   return f32 ? launch(tuna_quantize_rows_kernel<float>, grid, 256, 0, st, false, a)
              : launch(tuna_quantize_rows_kernel<__nv_bfloat16>, grid, 256, 0, st, false, a);
 }
@@ -635,7 +659,7 @@ int tuna_fp8_quantize(const void *x, int dtype, int64_t rows, int cols, int64_t 
   if (layout == TUNA_FP8_ROWS) return launch_quantize_rows(x, dtype == TUNA_DTYPE_F32, rows, cols, ldx, nullptr, rows, q, ldq, scale, st);
   QuantArgs a = {};
   a.x = x, a.rows = rows, a.cols = cols, a.ldx = ldx, a.q = (uint8_t *)q, a.ldq = ldq, a.scale = scale;
-  a.vec = aligned(x, 4 * size) && ldx % 4 == 0;
+  a.vec = aligned(x, 16) && ldx * size % 16 == 0;
   const bool f32 = dtype == TUNA_DTYPE_F32;
   if (layout == TUNA_FP8_COLUMNS)
     return f32 ? run_quantize_tiles<kColumns, float>(a, st) : run_quantize_tiles<kColumns, __nv_bfloat16>(a, st);

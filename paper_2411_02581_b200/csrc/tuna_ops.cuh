@@ -148,15 +148,16 @@ __device__ __forceinline__ float fp8_scale(uint32_t amax_bits) {
   return __fdiv_rn(fmaxf(__uint_as_float(amax_bits), 7.888609052210118e-31f /* 2^-100 */), 448.0f);
 }
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
-// Division by a block's scale, correctly rounded.  A product with 1 / s alone would round the many
-// 16-bit inputs that sit halfway between two 8-bit values the other way.  Markstein's theorem (IBM
-// J. Res. Dev. 34, 1990): with y = 1 / s correctly rounded and q within one unit of x / s, q + (x - q s) y
-// in fused operations is x / s correctly rounded, unless the fraction of s is all ones.  x y is within
-// 1.5 units, one correction brings it within one, the next one ends it.  x - q s must not underflow, so
-// very small (and very large) scales divide, as NaN ones do.  Five packed operations for two values,
-// against more than eight each for a division (an 8192 x 4096 matrix: 29 us that way).
+// Division by a block's scale, correctly rounded as the definition has it: many 16-bit inputs sit
+// exactly halfway between two 8-bit values, and a product with 1 / s would send them the other way.
+// Markstein's theorem (IBM J. Res. Dev. 34, 1990): with y = 1 / s correctly rounded and q within one
+// unit of x / s, q + (x - q s) y in fused operations is x / s correctly rounded, unless the fraction of
+// s is all ones.  x y is within 1.5 units, one correction brings it within one, the next one ends it:
+// five packed operations for two values.  x - q s must not underflow, so very small (and very large,
+// and NaN) scales divide.  The quotient is kept with its sign turned (y is -1 / s), which carries the
+// sign of a zero through the corrections; the codes' signs are turned back four at a time.
 struct Divisor {
-  uint64_t y, minus_s;
+  uint64_t y, s2;  // -1 / s, s
   float s;
   bool plain;
 };
@@ -185,38 +186,95 @@ __device__ __forceinline__ Divisor divisor(float s) {
   Divisor d;
   const uint32_t bits = __float_as_uint(s);
   d.plain = !(s >= 8.271806125530277e-25f /* 2^-80 */ && s <= 1.2676506002282294e30f /* 2^100 */) || (bits & 0x7fffff) == 0x7fffff;
-  const float y = __frcp_rn(s);
-  d.s = s, d.y = pair(y, y), d.minus_s = pair(-s, -s);
+  const float y = -__frcp_rn(s);
+  d.s = s, d.y = pair(y, y), d.s2 = pair(s, s);
   return d;
 }
-__device__ __forceinline__ uint32_t fp8_pair(float a, float b, const Divisor &d) {
-  float qa, qb;
-  if (d.plain) {
-    qa = __fdiv_rn(a, d.s), qb = __fdiv_rn(b, d.s);
-  } else {
-    const uint64_t x = pair(a, b);
-    uint64_t q = mul2(x, d.y);
-    q = fma2(fma2(q, d.minus_s, x), d.y, q);
-    q = fma2(fma2(q, d.minus_s, x), d.y, q);
-    unpair(q, qa, qb);
-    // (the corrections turn -0 into 0)
-    qa = __uint_as_float(__float_as_uint(qa) | (__float_as_uint(a) & 0x80000000u));
-    qb = __uint_as_float(__float_as_uint(qb) | (__float_as_uint(b) & 0x80000000u));
-  }
+__device__ __forceinline__ uint32_t e4m3_pair(float lo, float hi) {
   uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(qb), "f"(qa));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
-__device__ __forceinline__ uint32_t fp8_quad(float a, float b, float c, float d, const Divisor &s) {
-  return fp8_pair(a, b, s) | (fp8_pair(c, d, s) << 16);
+// N (a multiple of 4) values over the scale, to N / 4 words
+template <int N>
+__device__ __forceinline__ void fp8_run(const float *v, const Divisor &d, uint32_t (&out)[N / 4]) {
+  if (d.plain) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4)
+      out[i / 4] = e4m3_pair(__fdiv_rn(v[i], d.s), __fdiv_rn(v[i + 1], d.s)) | (e4m3_pair(__fdiv_rn(v[i + 2], d.s), __fdiv_rn(v[i + 3], d.s)) << 16);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    uint32_t half[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint64_t x = pair(v[i + 2 * j], v[i + 2 * j + 1]);
+      uint64_t q = mul2(x, d.y);
+      q = fma2(fma2(q, d.s2, x), d.y, q);
+      q = fma2(fma2(q, d.s2, x), d.y, q);
+      float lo, hi;
+      unpair(q, lo, hi);
+      half[j] = e4m3_pair(lo, hi);
+    }
+    out[i / 4] = __byte_perm(half[0], half[1], 0x5410) ^ 0x80808080u;
+  }
 }
-// 16 values in a row
-__device__ __forceinline__ uint4 fp8_sixteen(const float *v, const Divisor &s) {
-  uint4 u;
-  u.x = fp8_quad(v[0], v[1], v[2], v[3], s), u.y = fp8_quad(v[4], v[5], v[6], v[7], s);
-  u.z = fp8_quad(v[8], v[9], v[10], v[11], s), u.w = fp8_quad(v[12], v[13], v[14], v[15], s);
-  return u;
+__device__ __forceinline__ uint4 fp8_sixteen(const float *v, const Divisor &d) {
+  uint32_t w[4];
+  fp8_run<16>(v, d, w);
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
+
+// Eight consecutive values as they are stored, for loads that are all issued before the first use.
+template <typename T>
+struct Eight {
+  static constexpr int kWords = sizeof(T) / 2;
+  uint4 w[kWords];
+  __device__ __forceinline__ void load(const T *p, bool vec, int left) {  // `left`: how many of them there are
+    if (vec && left >= 8) {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+    } else {
+      union {
+        uint4 u[kWords];
+        T t[8];
+      } x;
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) x.u[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < left) x.t[i] = p[i];
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = x.u[i];
+    }
+  }
+  // the largest magnitude's bits, kept as `T` has them (two 16-bit values in a word for bf16)
+  __device__ __forceinline__ uint32_t top(uint32_t so_far) const {
+    constexpr uint32_t mask = sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) so_far = sizeof(T) == 2 ? __vmaxu2(so_far, x[j] & mask) : max(so_far, x[j] & mask);
+    }
+    return so_far;
+  }
+  static __device__ __forceinline__ uint32_t top_bits(uint32_t t) { return sizeof(T) == 2 ? max(t << 16, t & 0xffff0000u) : t; }
+  __device__ __forceinline__ void values(float *v) const {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (sizeof(T) == 2)
+          v[2 * j] = __uint_as_float(x[j] << 16), v[2 * j + 1] = __uint_as_float(x[j] & 0xffff0000u);
+        else
+          v[4 * i + j] = __uint_as_float(x[j]);
+      }
+    }
+  }
+};
 
 // ---- barriers in shared memory ---------------------------------------------------------
 

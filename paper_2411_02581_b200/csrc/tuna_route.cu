@@ -126,7 +126,7 @@ __device__ __forceinline__ void place_entries(const OrderArgs &o, char *smem, in
     if (there) {
       const int64_t at = base[id] + mine[id] + before;
       o.pos[i + lane] = at;
-      o.rows[at] = (i + lane) / o.k;
+      o.rows[at] = (uint32_t)(i + lane) / (uint32_t)o.k;  // (entries of one call stay below 2^31)
     } else if (i + lane < b) {
       o.pos[i + lane] = -1;
     }
@@ -435,11 +435,10 @@ template <typename TY, typename TO>
 __global__ void __launch_bounds__(256) tuna_combine_kernel(CombineArgs a) {
   wait_previous();
   allow_next();
-  const int cols = (a.dim + 7) / 8;
-  const int64_t n = a.tokens * cols;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t t = i / cols;
-    const int c = (int)(i - t * cols) * 8;
+  // a block takes 2048 columns of a token
+  const int c = (int)(blockIdx.y * 256 + threadIdx.x) * 8;
+  if (c >= a.dim) return;
+  for (int64_t t = blockIdx.x; t < a.tokens; t += gridDim.x) {
     float acc[8] = {};
     for (int s = 0; s < a.k; ++s) {
       const int64_t r = a.pos[t * a.k + s];
@@ -699,7 +698,7 @@ int tuna_moe_combine(const void *y, int y_dtype, int64_t rows, int dim, int64_t 
   const size_t sy = dtype_size(y_dtype), so = dtype_size(out_dtype);
   if (!out || !aligned(y, sy) || !aligned(out, so)) return TUNA_ERR_INVALID_ARG;
   a.vec = dim % 8 == 0 && aligned(y, 16) && aligned(out, 16) && ldy * sy % 16 == 0 && ldo * so % 16 == 0;
-  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(tokens * ceil_div(dim, 8), 256), (int64_t)sm_count() * 16));
+  const dim3 grid((unsigned)std::min<int64_t>(tokens, 1 << 20), (unsigned)ceil_div(dim, 2048));
   cudaStream_t st = (cudaStream_t)stream;
   if (y_dtype == TUNA_DTYPE_F32)
     return out_dtype == TUNA_DTYPE_F32 ? launch(tuna_combine_kernel<float, float>, grid, 256, 0, st, false, a)
