@@ -543,37 +543,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 
 // ---- host ------------------------------------------------------------------------------------
 
-using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                 CUtensorMapFloatOOBfill);
-EncodeTiled encoder() {
-  static std::mutex m;
-  static EncodeTiled fn = nullptr;
-  std::lock_guard<std::mutex> lock(m);
-  if (!fn) {
-    void *p = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    if (!note_cuda(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found)) &&
-        found == cudaDriverEntryPointSuccess)
-      fn = (EncodeTiled)p;
-  }
-  return fn;
-}
-
-// An e4m3 operand (or bf16 results): k contiguous, then rows, then matrices; boxes of 128 bytes x `box` rows.
-int make_map(CUtensorMap *map, int rank, const void *p, int64_t k, int64_t rows, int64_t matrices, int64_t ld, int box, bool bf16 = false) {
-  EncodeTiled f = encoder();
-  if (!f) return TUNA_ERR_CUDA;
-  const cuuint64_t dims[3] = {(cuuint64_t)k, (cuuint64_t)rows, (cuuint64_t)matrices};
-  const int size = bf16 ? 2 : 1;
-  const cuuint64_t strides[2] = {(cuuint64_t)(ld * size), (cuuint64_t)(ld * size * rows)};
-  const cuuint32_t boxes[3] = {(cuuint32_t)(128 / size), (cuuint32_t)box, 1}, ones[3] = {1, 1, 1};
-  const CUresult r = f(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, (cuuint32_t)rank, const_cast<void *>(p), dims, strides, boxes, ones,
-                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? TUNA_OK : note_cuda(cudaErrorInvalidValue);
-}
-
 template <int BN, bool SWIGLU, bool B_ROWS, typename TO>
 int run_tiles(const ProductArgs &p, cudaStream_t st) {
   TileArgs a = {};
@@ -614,6 +583,37 @@ int run_quantize_tiles(const QuantArgs &a, cudaStream_t st) {
 }
 
 }  // namespace
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                 CUtensorMapFloatOOBfill);
+static EncodeTiled encoder() {
+  static std::mutex m;
+  static EncodeTiled fn = nullptr;
+  std::lock_guard<std::mutex> lock(m);
+  if (!fn) {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (!note_cuda(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found)) &&
+        found == cudaDriverEntryPointSuccess)
+      fn = (EncodeTiled)p;
+  }
+  return fn;
+}
+
+// An e4m3 operand (or bf16 results): k contiguous, then rows, then matrices; boxes of 128 bytes x `box` rows.
+int make_map(CUtensorMap *map, int rank, const void *p, int64_t k, int64_t rows, int64_t matrices, int64_t ld, int box, bool bf16) {
+  EncodeTiled f = encoder();
+  if (!f) return TUNA_ERR_CUDA;
+  const cuuint64_t dims[3] = {(cuuint64_t)k, (cuuint64_t)rows, (cuuint64_t)matrices};
+  const int size = bf16 ? 2 : 1;
+  const cuuint64_t strides[2] = {(cuuint64_t)(ld * size), (cuuint64_t)(ld * size * rows)};
+  const cuuint32_t boxes[3] = {(cuuint32_t)(128 / size), (cuuint32_t)box, 1}, ones[3] = {1, 1, 1};
+  const CUresult r = f(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, (cuuint32_t)rank, const_cast<void *>(p), dims, strides, boxes, ones,
+                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? TUNA_OK : note_cuda(cudaErrorInvalidValue);
+}
 
 int launch_product(const ProductArgs &p, cudaStream_t st) {
   if (p.swiglu) return run_tiles<256, true, false, uint8_t>(p, st);

@@ -6,6 +6,7 @@
 
 #include <cuda.h>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -59,6 +60,10 @@ inline int allow_smem(K kernel, size_t bytes, bool (&set)[64]) {
   if (dev >= 0 && dev < 64) __atomic_store_n(&set[dev], true, __ATOMIC_RELEASE);
   return TUNA_OK;
 }
+
+// Tensor map of a matrix stack: rows of k values (e4m3 bytes, or bf16), k contiguous with pitch ld, then
+// rows, then `matrices` back to back; boxes of 128 bytes x `box` rows, swizzled (tuna_fp8.cu).
+int make_map(CUtensorMap *map, int rank, const void *p, int64_t k, int64_t rows, int64_t matrices, int64_t ld, int box, bool bf16 = false);
 
 // Carves a caller's workspace into 256-byte aligned pieces; with base == nullptr it only adds up.
 struct Carve {
@@ -344,6 +349,14 @@ __device__ __forceinline__ void tc_mma_fp8(uint32_t d, uint64_t a, uint64_t b, u
   asm volatile(
       "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
       " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+      : "memory");
+}
+// the same for bf16 operands (128 x 16)
+__device__ __forceinline__ void tc_mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
       "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
       : "memory");
 }
