@@ -130,18 +130,29 @@ struct Product {
   int tiles, segments, segment, blocks;  // row tiles; segments; blocks of a segment, of a row
   int unit0, unit1;                      // this block's units, row tiles fastest, then segments, then groups
 };
+// A walk over a block's units.  Every role steps through its own; divisions are done once, at the start.
 struct Unit {
-  int g, s, m, blocks;  // group, segment, row tile; blocks of the segment
+  int left;               // units from here on
+  int g, s, m, blocks;    // group, segment, row tile; blocks of the segment
+  __device__ __forceinline__ Unit(const Product &p) {
+    left = p.unit1 - p.unit0;
+    const int q = p.unit0 / p.tiles;
+    m = p.unit0 - q * p.tiles;
+    g = q / p.segments;
+    s = q - g * p.segments;
+    blocks = min(p.segment, p.blocks - s * p.segment);
+  }
+  __device__ __forceinline__ void turn(const Product &p) {  // to the next segment or group
+    m = 0;
+    if (++s == p.segments) s = 0, ++g;
+    blocks = min(p.segment, p.blocks - s * p.segment);
+  }
+  __device__ __forceinline__ void step(const Product &p) {
+    --left;
+    if (++m == p.tiles) turn(p);
+  }
+  __device__ __forceinline__ bool last(const Product &p) const { return left == 1 || m + 1 == p.tiles; }  // of its group and segment
 };
-__device__ __forceinline__ Unit unit_at(const Product &p, int u) {
-  Unit w;
-  const int q = u / p.tiles;
-  w.m = u - q * p.tiles;
-  w.g = q / p.segments;
-  w.s = q - w.g * p.segments;
-  w.blocks = min(p.segment, p.blocks - w.s * p.segment);
-  return w;
-}
 
 // Position of a 16-byte piece in a swizzled operand of rows of 128 bytes.
 __device__ __forceinline__ uint32_t swizzled(int row, int piece) { return (uint32_t)((row >> 3) * 1024 + (row & 7) * 128 + ((piece ^ (row & 7)) * 16)); }
@@ -317,8 +328,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // -- weights
         if (lane == 0) {
           const CUtensorMap *map = up ? &map13 : &map2;
-          for (int u = p.unit0; ok && u < p.unit1; ++u) {
-            const Unit w = unit_at(p, u);
+          for (Unit w(p); ok && w.left > 0; w.step(p)) {
             const int expert = l.group[w.g].expert;
             for (int b = 0; b < w.blocks; ++b) {
               if (!(ok = mbar_wait(smem_u32(l.empty + stage), stage_phase ^ 1, &l.given_up))) break;
@@ -339,13 +349,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       } else if (warp == 1) {
         // -- tensor cores
         if (lane == 0) {
-          int held = -1;  // the (group, segment) whose operand is at hand
-          for (int u = p.unit0; ok && u < p.unit1; ++u) {
-            const Unit w = unit_at(p, u);
-            if (u / p.tiles != held) {
-              held = u / p.tiles;
-              if (!(ok = mbar_wait(smem_u32(l.laid + op), op_phase, &l.given_up))) break;
-            }
+          bool held = false;  // the group's and segment's operand is at hand
+          for (Unit w(p); ok && w.left > 0; w.step(p)) {
+            if (!held && !(ok = mbar_wait(smem_u32(l.laid + op), op_phase, &l.given_up))) break;
+            held = !w.last(p);
             const int N = FP8 && l.group[w.g].count > 8 ? 32 : 16;
             const uint32_t idesc = (1u << 4) | (FP8 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
             for (int b = 0; b < w.blocks; ++b) {
@@ -369,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (++buf == kBufs) buf = 0, buf_phase ^= 1;
               }
             }
-            if (ok && (u + 1 == p.unit1 || (u + 1) / p.tiles != held)) {
+            if (ok && !held) {
               tc_commit(smem_u32(l.used + op));
               if (++op == 2) op = 0, op_phase ^= 1;
             }
@@ -387,9 +394,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         float *to = up ? a.up : a.y;
         const int block_rows = up ? 2 * ((I + 127) / 128) : (D + 127) / 128;
         // the scales of a unit's blocks for this row
-        auto fetch = [&](int u, float (&ws)[8]) {
-          if (!FP8 || u >= p.unit1) return;
-          const Unit w = unit_at(p, u);
+        auto fetch = [&](const Unit &w, float (&ws)[8]) {
+          if (!FP8 || w.left <= 0) return;
           const int r = min(w.m * 128 + mine, rows - 1);
           const int br = up && r >= I ? (I + 127) / 128 + (r - I) / 128 : r / 128;
           const float *s = (up ? a.s13 : a.s2) + ((int64_t)l.group[w.g].expert * block_rows + br) * p.blocks + w.s * p.segment;
@@ -397,16 +403,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int b = 0; b < 8; ++b) ws[b] = __ldg(s + min(b, w.blocks - 1));
         };
         float next[8];
-        fetch(p.unit0, next);
-        for (int u = p.unit0; ok && u < p.unit1; ++u) {
-          const Unit w = unit_at(p, u);
+        Unit ahead(p);
+        fetch(ahead, next);
+        for (Unit w(p); ok && w.left > 0; w.step(p)) {
           const int first = l.group[w.g].first, count = l.group[w.g].count;
           float ws[8], acc[kTile];
 #pragma unroll
           for (int b = 0; b < 8; ++b) ws[b] = next[b];
 #pragma unroll
           for (int i = 0; i < kTile; ++i) acc[i] = 0.0f;
-          fetch(u + 1, next);
+          ahead.step(p);
+          fetch(ahead, next);
           if constexpr (FP8) {
 #pragma unroll
             for (int b = 0; b < 8; ++b) {
@@ -464,7 +471,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int i = 0; i < kTile; ++i)
               if (i < count) to[((int64_t)w.s * n + l.entry[first + i]) * rows + r] = acc[i];
           }
-          if (u + 1 == p.unit1 || (u + 1) / p.tiles != u / p.tiles) {
+          if (w.last(p)) {
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(l.used + op));
             if (++op == 2) op = 0, op_phase ^= 1;
@@ -473,9 +480,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       } else if (warp >= kWarps - kLoaders && p.unit0 < p.unit1) {
         // -- the tokens' operands, a (group, segment) ahead of the tensor cores
         if (!up) ok = __all_sync(~0u, lane != 0 || grid_wait(a.barrier, l.generation, &l.given_up));  // every block's sums are there
-        const int first_q = p.unit0 / p.tiles, last_q = (p.unit1 - 1) / p.tiles, i0 = tid - (kWarps - kLoaders) * 32;
-        for (int q = first_q; ok && q <= last_q; ++q) {
-          const Unit w = unit_at(p, q * p.tiles);
+        const int i0 = tid - (kWarps - kLoaders) * 32;
+        for (Unit w(p); ok && w.left > 0; w.left -= p.tiles - w.m, w.turn(p)) {
           const int first = l.group[w.g].first, count = l.group[w.g].count, N = FP8 && count > 8 ? 32 : 16;
           ok = __all_sync(~0u, mbar_wait(smem_u32(l.used + op), op_phase ^ 1, &l.given_up));
           if (!ok) break;
@@ -504,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 float u[kValues];
 #pragma unroll
                 for (int j = 0; j < kValues; ++j) u[j] = 0.0f;
-#pragma unroll 2
+#pragma unroll 4
                 for (int s = 0; s < a.segments[0]; ++s) {
                   const float4 *g4 = (const float4 *)(a.up + ((int64_t)s * n + entry) * 2 * I + col), *u4 = (const float4 *)((const float *)g4 + I);
 #pragma unroll
@@ -600,12 +606,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (tid == 0 && *(volatile int *)&l.given_up) *a.error = 1;
 }
 
-// Blocks of a segment: as long as possible (fewer partial sums) while the units still share out
-// evenly, six or more a block.  Every token's experts differ, so there are at least k groups.
+// Blocks of a segment: as long as possible (fewer partial sums) while there is work for all blocks:
+// three units for two of them.  Every token's experts differ, so there are at least k groups.
 void plan_segments(int tokens, int k, int64_t rows, int64_t cols, int block, int &segment, int &segments) {
   const int64_t groups = std::max<int64_t>(k, ceil_div((int64_t)tokens * k, kTile)), tiles = ceil_div(rows, 128), blocks = ceil_div(cols, block);
   int64_t s = 1024 / block;
-  while (s * block > 128 && groups * tiles * ceil_div(blocks, s) < 6 * 148) s /= 2;
+  while (s * block > 128 && 2 * groups * tiles * ceil_div(blocks, s) < 3 * 148) s /= 2;
   segment = (int)s, segments = (int)ceil_div(blocks, s);
 }
 
