@@ -7,9 +7,11 @@
 // For so few tokens the layer is bound by reading the chosen experts' weights once (3 D I
 // values an expert), so everything else has to stay out of that stream's way.  A block a
 // multiprocessor (cooperative launch: the phases are separated by barriers across the grid)
-// brings 128 weight rows x 128 bytes at a time into a ring of nine stages, 144 KB in flight; the
+// brings 128 weight rows x 256 bytes at a time into a ring of four stages, 128 KB in flight; the
 // tensor cores take them from there as the 128-row operand, with the tokens of one expert as the
-// columns of the other one.  The weights are never touched by a thread.  The first form of this
+// columns of the other one.  The weights are never touched by a thread.  (With stages of half the size
+// the thread that issues the steps could not keep up: 840 cycles for 16 KB, and 700 are the memory's
+// pace.)  The first form of this
 // kernel multiplied with m16n8k16 steps out of registers; widening 8-bit weights to 16 bits and
 // adding up the warps' partial sums left it at a quarter of the memory rate (64 tokens: 887 us).
 //
@@ -35,11 +37,11 @@ namespace {
 
 constexpr int kThreads = 512, kWarps = 16;
 constexpr int kMaxTokens = TUNA_MOE_FEW_MAX_TOKENS;
-constexpr int kStages = 9, kStageBytes = 128 * 128;
+constexpr int kStages = 4, kBlockBytes = 128 * 128, kStageBytes = 2 * kBlockBytes;  // a stage: two blocks of 128 rows x 128 bytes
 constexpr int kTile = 16;                 // tokens of a group: more of one expert form another group
-constexpr int kBufs = 8, kBufCols = 32;   // accumulators in tensor memory
+constexpr int kBufs = 4, kBufCols = 64;   // accumulators in tensor memory: two of 32 columns (8-bit), or one
 constexpr int kOperand = 32 * 1024;       // token operand of a segment (two of them)
-constexpr int kSplit = kWarps * 32;       // columns of x that a block takes in the router phase
+constexpr int kSplit = kWarps * 64;       // columns of x that a block takes in the router phase
 constexpr int kMaxDimFew = 8192;
 constexpr int kLoaders = 8;               // warps that lay out the token operands
 
@@ -157,9 +159,6 @@ struct Unit {
 // Position of a 16-byte piece in a swizzled operand of rows of 128 bytes.
 __device__ __forceinline__ uint32_t swizzled(int row, int piece) { return (uint32_t)((row >> 3) * 1024 + (row & 7) * 128 + ((piece ^ (row & 7)) * 16)); }
 
-__device__ __forceinline__ void sts16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
-}
 __device__ __forceinline__ float2 e4m3_values(uint32_t two) {
   uint32_t h;
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
@@ -187,27 +186,31 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   if (warp == 2) tmem_alloc(smem_u32(&l.tmem), kBufs * kBufCols);
 
-  // ---- logits: a block takes 16 experts and 512 columns, a warp 32 of them
+  // ---- logits: a block takes 16 experts and 1024 columns, a warp 64 of them
   {
     const int units = (E + 15) / 16 * splits, nt = (T + 7) / 8;
     float4 *sums = (float4 *)smem;  // [token tile][warp][lane]
     for (int u = blockIdx.x; u < units; u += gridDim.x) {
       const int m = u / splits, split = u - m * splits;
-      const int col = split * kSplit + warp * 32 + quad * 8;
-      uint4 w0 = make_uint4(0, 0, 0, 0), w1 = w0;
-      if (col < D) {
-        const int e0 = m * 16 + row_in, e1 = e0 + 8;
-        if (e0 < E) w0 = __ldg((const uint4 *)(a.router + (int64_t)e0 * D + col));
-        if (e1 < E) w1 = __ldg((const uint4 *)(a.router + (int64_t)e1 * D + col));
+      const int col = split * kSplit + warp * 64 + quad * 8, e0 = m * 16 + row_in, e1 = e0 + 8;
+      const uint4 none = make_uint4(0, 0, 0, 0);
+      uint4 w0[2], w1[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bool in = col + h * 32 < D;
+        w0[h] = in && e0 < E ? __ldg((const uint4 *)(a.router + (int64_t)e0 * D + col + h * 32)) : none;
+        w1[h] = in && e1 < E ? __ldg((const uint4 *)(a.router + (int64_t)e1 * D + col + h * 32)) : none;
       }
 #pragma unroll 4
       for (int j = 0; j < nt; ++j) {
         const int t = j * 8 + row_in;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (col < D && t < T) v = __ldg((const uint4 *)(a.x + t * a.ldx + col));
         float c[4] = {};
-        mma_bf16(c, w0.x, w1.x, w0.y, w1.y, v.x, v.y);
-        mma_bf16(c, w0.z, w1.z, w0.w, w1.w, v.z, v.w);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint4 v = col + h * 32 < D && t < T ? __ldg((const uint4 *)(a.x + t * a.ldx + col + h * 32)) : none;
+          mma_bf16(c, w0[h].x, w1[h].x, w0[h].y, w1[h].y, v.x, v.y);
+          mma_bf16(c, w0[h].z, w1[h].z, w0[h].w, w1[h].w, v.z, v.w);
+        }
         sums[(j * kWarps + warp) * 32 + lane] = make_float4(c[0], c[1], c[2], c[3]);
       }
       __syncthreads();
@@ -231,43 +234,47 @@ __global__ void __launch_bounds__(kThreads, 1)
   bool fine = grid_meet(a.barrier, &l.given_up);
 
   if (fine) {
-    // ---- the choice, by every block for itself: a warp a token
+    // ---- the choice, by every block for itself; the fewer experts, the more tokens a warp takes
     Choice &c = *(Choice *)smem;
-    for (int t = warp; t < T; t += kWarps) {
-      int id;
-      float w;
-      auto take = [&](auto vpl) {
-        constexpr int VPL = decltype(vpl)::value;
+    auto take = [&](auto lanes, auto values) {
+      constexpr int LPT = decltype(lanes)::value, VPL = decltype(values)::value;
+      const int in = lane % LPT;
+      for (int t0 = warp * (32 / LPT); t0 < T; t0 += kWarps * (32 / LPT)) {
+        const int t = t0 + lane / LPT;
         float z[VPL];
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) z[i] = lane * VPL + i < E ? 0.0f : -INFINITY;
-#pragma unroll 4
-        for (int q = 0; q < splits; ++q) {
+        for (int i = 0; i < VPL; ++i) z[i] = t < T && in * VPL + i < E ? 0.0f : -INFINITY;
+        if (t < T) {
+          const float *part = a.part + (int64_t)t * E + in * VPL;
+#pragma unroll 8
+          for (int q = 0; q < splits; ++q) {
 #pragma unroll
-          for (int i = 0; i < VPL; ++i) {
-            const int e = lane * VPL + i;
-            if (e < E) z[i] += __ldcg(a.part + ((int64_t)q * T + t) * E + e);
+            for (int i = 0; i < VPL; ++i)
+              if (in * VPL + i < E) z[i] += __ldcg(part + (int64_t)q * T * E + i);
           }
         }
 #pragma unroll
         for (int i = 0; i < VPL; ++i) z[i] = logit_of(z[i]);
-        choose<32>(z, lane, K, a.scoring, a.renormalize, a.scale, id, w);
-      };
-      if (E <= 64)
-        take(std::integral_constant<int, 2>());
-      else if (E <= 256)
-        take(std::integral_constant<int, 8>());
-      else
-        take(std::integral_constant<int, 16>());
-      if (lane < K) {
-        c.id[t * K + lane] = (int16_t)id;
-        if (blockIdx.x == 0) {
-          a.ids[t * K + lane] = id, a.weights[t * K + lane] = w;
-          if (a.ids_out) a.ids_out[t * K + lane] = id;
-          if (a.weights_out) a.weights_out[t * K + lane] = w;
+        int id;
+        float w;
+        choose<LPT>(z, in, K, a.scoring, a.renormalize, a.scale, id, w);
+        if (t < T && in < K) {
+          c.id[t * K + in] = (int16_t)id;
+          if (blockIdx.x == 0) {
+            a.ids[t * K + in] = id, a.weights[t * K + in] = w;
+            if (a.ids_out) a.ids_out[t * K + in] = id;
+            if (a.weights_out) a.weights_out[t * K + in] = w;
+          }
         }
       }
-    }
+    };
+    using std::integral_constant;
+    if (E <= 64 && K <= 8)
+      take(integral_constant<int, 8>(), integral_constant<int, 8>());
+    else if (E <= 256)
+      take(integral_constant<int, 32>(), integral_constant<int, 8>());
+    else
+      take(integral_constant<int, 32>(), integral_constant<int, 16>());
     for (int e = tid; e < E; e += kThreads) c.count[e] = 0;
     __syncthreads();
     for (int i = tid; i < n; i += kThreads)
@@ -330,11 +337,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           const CUtensorMap *map = up ? &map13 : &map2;
           for (Unit w(p); ok && w.left > 0; w.step(p)) {
             const int expert = l.group[w.g].expert;
-            for (int b = 0; b < w.blocks; ++b) {
+            for (int b = 0; b < w.blocks; b += 2) {
               if (!(ok = mbar_wait(smem_u32(l.empty + stage), stage_phase ^ 1, &l.given_up))) break;
-              const uint32_t bar = smem_u32(l.full + stage);
-              mbar_expect(bar, kStageBytes);
-              tma_load_3d(ring + stage * kStageBytes, map, (w.s * p.segment + b) * kBlock, w.m * 128, expert, bar);
+              const uint32_t bar = smem_u32(l.full + stage), to = ring + stage * kStageBytes;
+              const int col = (w.s * p.segment + b) * kBlock;
+              const bool both = b + 1 < w.blocks;
+              mbar_expect(bar, both ? kStageBytes : kBlockBytes);
+              tma_load_3d(to, map, col, w.m * 128, expert, bar);
+              if (both) tma_load_3d(to + kBlockBytes, map, col + kBlock, w.m * 128, expert, bar);
               if (++stage == kStages) stage = 0, stage_phase ^= 1;
             }
           }
@@ -355,7 +365,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             held = !w.last(p);
             const int N = FP8 && l.group[w.g].count > 8 ? 32 : 16;
             const uint32_t idesc = (1u << 4) | (FP8 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-            for (int b = 0; b < w.blocks; ++b) {
+            for (int b = 0; b < w.blocks; b += 2) {
               if (!(ok = mbar_wait(smem_u32(l.full + stage), stage_phase, &l.given_up))) break;
               if (FP8 || b == 0)
                 if (!(ok = mbar_wait(smem_u32(l.freed + buf), buf_phase ^ 1, &l.given_up))) break;
@@ -363,15 +373,20 @@ __global__ void __launch_bounds__(kThreads, 1)
               const uint64_t da = tc_desc(ring + stage * kStageBytes), db = tc_desc(operands + op * kOperand + b * N * 128);
               const uint32_t d = tmem + buf * kBufCols;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                if (FP8)
-                  tc_mma_fp8(d, da + 2 * i, db + 2 * i, idesc, i > 0);
-                else
-                  tc_mma_bf16(d, da + 2 * i, db + 2 * i, idesc, b > 0 || i > 0);
+              for (int h = 0; h < 2; ++h) {
+                if (h && b + 1 >= w.blocks) break;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const uint64_t ha = da + h * (kBlockBytes >> 4) + 2 * i, hb = db + h * (N * 128 >> 4) + 2 * i;
+                  if (FP8)
+                    tc_mma_fp8(d + h * 32, ha, hb, idesc, i > 0);
+                  else
+                    tc_mma_bf16(d, ha, hb, idesc, b > 0 || h > 0 || i > 0);
+                }
               }
               tc_commit(smem_u32(l.empty + stage));
               if (++stage == kStages) stage = 0, stage_phase ^= 1;
-              if (FP8 || b == w.blocks - 1) {
+              if (FP8 || b + 2 >= w.blocks) {
                 tc_commit(smem_u32(l.done + buf));
                 if (++buf == kBufs) buf = 0, buf_phase ^= 1;
               }
@@ -416,35 +431,47 @@ __global__ void __launch_bounds__(kThreads, 1)
           fetch(ahead, next);
           if constexpr (FP8) {
 #pragma unroll
-            for (int b = 0; b < 8; ++b) {
+            for (int b = 0; b < 8; b += 2) {
               if (b >= w.blocks) break;
               ok = __all_sync(~0u, mbar_wait(smem_u32(l.done + buf), buf_phase, &l.given_up));
               if (!ok) break;
               tc_fence_after();
-              const float4 *xs = (const float4 *)l.piece_scale[op][b];
-              // (below 9 tokens, p and q are 8 columns each, else 16)
-              uint32_t v[32];
+              // below 9 tokens, the pieces p and q of a block are 8 columns each, else 16
+              uint32_t v[2][32];
               if (count > 8) {
-                tmem_load32(from + buf * kBufCols, v);
-                tmem_wait(v);
+                tmem_load32(from + buf * kBufCols, v[0]);
+                tmem_load32(from + buf * kBufCols + 32, v[1]);
               } else {
-                uint32_t x[16];
-                tmem_load16(from + buf * kBufCols, x);
-                tmem_wait(x);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = x[i], v[16 + i] = x[8 + i];
+                tmem_load16(from + buf * kBufCols, reinterpret_cast<uint32_t(&)[16]>(v[0]));
+                tmem_load16(from + buf * kBufCols + 32, reinterpret_cast<uint32_t(&)[16]>(v[1]));
               }
+              tmem_wait(v[0]);
+              tmem_wait(v[1]);
               tc_fence_before();
               __syncwarp();
               if (lane == 0) mbar_arrive(smem_u32(l.freed + buf));
 #pragma unroll
-              for (int i = 0; i < kTile; i += 4) {
-                if (i < count) {
-                  const float4 s = xs[i / 4];
-                  const float f[4] = {s.x, s.y, s.z, s.w};
+              for (int h = 0; h < 2; ++h) {
+                if (b + h >= w.blocks) break;
+                const float4 *xs = (const float4 *)l.piece_scale[op][b + h];
+                if (count > 8) {
 #pragma unroll
-                  for (int j = 0; j < 4; ++j)
-                    acc[i + j] = fmaf(fmaf(__uint_as_float(v[16 + i + j]), 0.0625f, __uint_as_float(v[i + j])), ws[b] * f[j], acc[i + j]);
+                  for (int i = 0; i < 16; i += 4) {
+                    const float4 s = xs[i / 4];
+                    const float f[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                      acc[i + j] = fmaf(fmaf(__uint_as_float(v[h][16 + i + j]), 0.0625f, __uint_as_float(v[h][i + j])), ws[b + h] * f[j], acc[i + j]);
+                  }
+                } else {
+#pragma unroll
+                  for (int i = 0; i < 8; i += 4) {
+                    const float4 s = xs[i / 4];
+                    const float f[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                      acc[i + j] = fmaf(fmaf(__uint_as_float(v[h][8 + i + j]), 0.0625f, __uint_as_float(v[h][i + j])), ws[b + h] * f[j], acc[i + j]);
+                  }
                 }
               }
               if (++buf == kBufs) buf = 0, buf_phase ^= 1;
@@ -485,77 +512,60 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int first = l.group[w.g].first, count = l.group[w.g].count, N = FP8 && count > 8 ? 32 : 16;
           ok = __all_sync(~0u, mbar_wait(smem_u32(l.used + op), op_phase ^ 1, &l.given_up));
           if (!ok) break;
-          const int pieces = count * w.blocks * 8;  // 16 bytes each: 8 of them are one token's block
-          for (int base = 0; base < pieces; base += kLoaders * 32) {
-            const int i = base + i0, piece = i & 7, t = (i >> 3) / w.blocks, b = (i >> 3) - t * w.blocks;
-            const bool there = i < pieces;
-            const int entry = there ? l.entry[first + t] : 0;
-            constexpr int kValues = FP8 ? 16 : 8;
-            const int col = (w.s * p.segment + b) * kBlock + piece * kValues;
-            float v[kValues];
-#pragma unroll
-            for (int j = 0; j < kValues; ++j) v[j] = 0.0f;
-            if (there && col < cols) {  // (cols is a multiple of 16)
+          // a warp takes 128 columns of a token, a lane four of them
+          const int spans = (w.blocks * kBlock + 127) / 128;
+          int t = i0 >> 5, span = 0;
+          while (t >= count && span < spans) t -= count, ++span;
+          for (; span < spans;) {
+            const int entry = l.entry[first + t], col = w.s * p.segment * kBlock + span * 128 + lane * 4;
+            float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (col < cols) {  // (cols is a multiple of 16)
               if (up) {
-                uint4 r[kValues / 8];
-#pragma unroll
-                for (int j = 0; j < kValues / 8; ++j) r[j] = __ldg((const uint4 *)(a.x + (entry / K) * a.ldx + col) + j);
-#pragma unroll
-                for (int j = 0; j < kValues / 8; ++j) {
-                  const uint32_t k4[4] = {r[j].x, r[j].y, r[j].z, r[j].w};
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) v[8 * j + 2 * e] = __uint_as_float(k4[e] << 16), v[8 * j + 2 * e + 1] = __uint_as_float(k4[e] & 0xffff0000u);
-                }
+                const uint2 r = __ldg((const uint2 *)(a.x + (entry / K) * a.ldx + col));
+                v[0] = __uint_as_float(r.x << 16), v[1] = __uint_as_float(r.x & 0xffff0000u);
+                v[2] = __uint_as_float(r.y << 16), v[3] = __uint_as_float(r.y & 0xffff0000u);
               } else {
-                float u[kValues];
-#pragma unroll
-                for (int j = 0; j < kValues; ++j) u[j] = 0.0f;
-#pragma unroll 4
+                float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                const float *g0 = a.up + (int64_t)entry * 2 * I + col;
+#pragma unroll 8
                 for (int s = 0; s < a.segments[0]; ++s) {
-                  const float4 *g4 = (const float4 *)(a.up + ((int64_t)s * n + entry) * 2 * I + col), *u4 = (const float4 *)((const float *)g4 + I);
-#pragma unroll
-                  for (int j = 0; j < kValues / 4; ++j) {
-                    const float4 x = __ldcg(g4 + j), y = __ldcg(u4 + j);
-                    v[4 * j] += x.x, v[4 * j + 1] += x.y, v[4 * j + 2] += x.z, v[4 * j + 3] += x.w;
-                    u[4 * j] += y.x, u[4 * j + 1] += y.y, u[4 * j + 2] += y.z, u[4 * j + 3] += y.w;
-                  }
+                  const float4 x = __ldcg((const float4 *)(g0 + (int64_t)s * n * 2 * I)), y = __ldcg((const float4 *)(g0 + (int64_t)s * n * 2 * I + I));
+                  v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+                  u[0] += y.x, u[1] += y.y, u[2] += y.z, u[3] += y.w;
                 }
 #pragma unroll
-                for (int j = 0; j < kValues; ++j) v[j] = v[j] / (1.0f + expf(-v[j])) * u[j];
+                for (int j = 0; j < 4; ++j) v[j] = v[j] / (1.0f + expf(-v[j])) * u[j];
               }
             }
-            const uint32_t to = operands + op * kOperand + b * N * 128;
             if constexpr (FP8) {
-              uint32_t top = 0;
-#pragma unroll
-              for (int j = 0; j < kValues; ++j) top = max(top, abs_bits(v[j]));
-#pragma unroll
-              for (int d = 1; d < 8; d <<= 1) top = max(top, __shfl_xor_sync(~0u, top, d));
+              uint32_t top = max(max(abs_bits(v[0]), abs_bits(v[1])), max(abs_bits(v[2]), abs_bits(v[3])));
+              top = __reduce_max_sync(~0u, top);
               // s takes the block's largest value to [2^7, 2^8); a block that is not finite is lost to NaN
               const int e = min(max((int)(top >> 23), 27) - 7, 240);
               const float s = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)e << 23);
               const float by = __uint_as_float((uint32_t)(254 - e) << 23);
-              uint32_t hi[4], lo[4];
+              uint32_t h2[2], l2[2];
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                uint32_t h2[2], l2[2];
-#pragma unroll
-                for (int i2 = 0; i2 < 2; ++i2) {
-                  const float x = v[4 * j + 2 * i2] * by, y = v[4 * j + 2 * i2 + 1] * by;
-                  h2[i2] = e4m3_pair(x, y);
-                  const float2 have = e4m3_values(h2[i2]);
-                  l2[i2] = e4m3_pair((x - have.x) * 16.0f, (y - have.y) * 16.0f);
-                }
-                hi[j] = h2[0] | (h2[1] << 16), lo[j] = l2[0] | (l2[1] << 16);
+              for (int j = 0; j < 2; ++j) {
+                const float x = v[2 * j] * by, y = v[2 * j + 1] * by;
+                h2[j] = e4m3_pair(x, y);
+                const float2 have = e4m3_values(h2[j]);
+                l2[j] = e4m3_pair((x - have.x) * 16.0f, (y - have.y) * 16.0f);
               }
-              if (there) {
-                sts16(to + swizzled(t, piece), hi[0], hi[1], hi[2], hi[3]);
-                sts16(to + swizzled(N / 2 + t, piece), lo[0], lo[1], lo[2], lo[3]);
-                if (piece == 0) l.piece_scale[op][b][t] = s;
-              }
-            } else if (there) {
-              sts16(to + swizzled(t, piece), pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+              const uint32_t to = operands + op * kOperand + span * N * 128 + (lane & 3) * 4;
+              asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + swizzled(t, lane >> 2)), "r"(h2[0] | (h2[1] << 16)) : "memory");
+              asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + swizzled(N / 2 + t, lane >> 2)), "r"(l2[0] | (l2[1] << 16)) : "memory");
+              if (lane == 0) l.piece_scale[op][span][t] = s;
+            } else {
+              // (two blocks of 64; the second may lie behind the segment, where its place is unused)
+              const int b = span * 2 + (lane >> 4);
+              if (b < w.blocks)
+                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(operands + op * kOperand + b * N * 128 + swizzled(t, (lane & 15) >> 1) + (lane & 1) * 8),
+                             "r"(pack_bf16(v[0], v[1])), "r"(pack_bf16(v[2], v[3]))
+                             : "memory");
             }
+            t += kLoaders;
+            while (t >= count && span < spans) t -= count, ++span;
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
