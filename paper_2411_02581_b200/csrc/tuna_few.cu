@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   const uint32_t ring = smem_u32(smem), operands = ring + kStages * kStageBytes;
   Lists &l = *(Lists *)(smem + kStages * kStageBytes + 2 * kOperand);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, row_in = lane >> 2, quad = lane & 3;
+  const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid >> 5, 0), lane = tid & 31, row_in = lane >> 2, quad = lane & 3;
   const int T = a.tokens, E = a.experts, K = a.k, D = a.hidden, I = a.inter, n = T * K;
   const int splits = (D + kSplit - 1) / kSplit;
   if (tid == 0) {
@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
     // ---- the two products
     const int groups = l.groups;
-    const uint32_t tmem = l.tmem;
+    const uint32_t tmem = __shfl_sync(~0u, l.tmem, 0);
     constexpr int kBlock = FP8 ? 128 : 64;  // columns of a block
     int stage = 0, stage_phase = 0, buf = 0, buf_phase = 0, op = 0, op_phase = 0;
     bool ok = true;
@@ -357,48 +357,51 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       } else if (warp == 1) {
-        // -- tensor cores
-        if (lane == 0) {
+        // -- tensor cores (the whole warp walks, one lane issues)
+        {
           bool held = false;  // the group's and segment's operand is at hand
           for (Unit w(p); ok && w.left > 0; w.step(p)) {
-            if (!held && !(ok = mbar_wait(smem_u32(l.laid + op), op_phase, &l.given_up))) break;
+            if (!held && !(ok = __all_sync(~0u, mbar_wait(smem_u32(l.laid + op), op_phase, &l.given_up)))) break;
             held = !w.last(p);
             const int N = FP8 && l.group[w.g].count > 8 ? 32 : 16;
             const uint32_t idesc = (1u << 4) | (FP8 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
             for (int b = 0; b < w.blocks; b += 2) {
-              if (!(ok = mbar_wait(smem_u32(l.full + stage), stage_phase, &l.given_up))) break;
+              if (!(ok = __all_sync(~0u, mbar_wait(smem_u32(l.full + stage), stage_phase, &l.given_up)))) break;
               if (FP8 || b == 0)
-                if (!(ok = mbar_wait(smem_u32(l.freed + buf), buf_phase ^ 1, &l.given_up))) break;
+                if (!(ok = __all_sync(~0u, mbar_wait(smem_u32(l.freed + buf), buf_phase ^ 1, &l.given_up)))) break;
               tc_fence_after();
               const uint64_t da = tc_desc(ring + stage * kStageBytes), db = tc_desc(operands + op * kOperand + b * N * 128);
               const uint32_t d = tmem + buf * kBufCols;
+              const bool out = FP8 || b + 2 >= w.blocks;  // the accumulator is complete
+              if (elect_one()) {
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                if (h && b + 1 >= w.blocks) break;
+                for (int h = 0; h < 2; ++h) {
+                  if (h && b + 1 >= w.blocks) break;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const uint64_t ha = da + h * (kBlockBytes >> 4) + 2 * i, hb = db + h * (N * 128 >> 4) + 2 * i;
-                  if (FP8)
-                    tc_mma_fp8(d + h * 32, ha, hb, idesc, i > 0);
-                  else
-                    tc_mma_bf16(d, ha, hb, idesc, b > 0 || h > 0 || i > 0);
+                  for (int i = 0; i < 4; ++i) {
+                    const uint64_t ha = da + h * (kBlockBytes >> 4) + 2 * i, hb = db + h * (N * 128 >> 4) + 2 * i;
+                    if (FP8)
+                      tc_mma_fp8(d + h * 32, ha, hb, idesc, i > 0);
+                    else
+                      tc_mma_bf16(d, ha, hb, idesc, b > 0 || h > 0 || i > 0);
+                  }
                 }
+                tc_commit(smem_u32(l.empty + stage));
+                if (out) tc_commit(smem_u32(l.done + buf));
               }
-              tc_commit(smem_u32(l.empty + stage));
+              __syncwarp();
               if (++stage == kStages) stage = 0, stage_phase ^= 1;
-              if (FP8 || b + 2 >= w.blocks) {
-                tc_commit(smem_u32(l.done + buf));
-                if (++buf == kBufs) buf = 0, buf_phase ^= 1;
-              }
+              if (out && ++buf == kBufs) buf = 0, buf_phase ^= 1;
             }
             if (ok && !held) {
-              tc_commit(smem_u32(l.used + op));
+              if (elect_one()) tc_commit(smem_u32(l.used + op));
+              __syncwarp();
               if (++op == 2) op = 0, op_phase ^= 1;
             }
           }
           if (!ok) {
             int never = 0;
-            tc_commit(smem_u32(&l.drained));
+            if (elect_one()) tc_commit(smem_u32(&l.drained));
             mbar_wait(smem_u32(&l.drained), 0, &never);
           }
         }

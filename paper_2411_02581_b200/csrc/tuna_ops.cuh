@@ -281,6 +281,14 @@ struct Eight {
   }
 };
 
+// True in one lane of a whole warp.  What a warp issues to the tensor cores is issued so: the
+// operands stay in uniform registers, where a branch on the lane would move each of them there.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(r));
+  return r != 0;
+}
+
 // ---- barriers in shared memory ---------------------------------------------------------
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
