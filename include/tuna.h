@@ -546,12 +546,14 @@ int tuna_plan_device_status(tuna_plan_t *plan, int *gave_up);
  * tokens * k <= 2^31, ranks * experts <= 2^20.
  *
  * tuna_moe_order - the same order from ids that another router made (ids below 0 or from
- * `experts` on are left out).  One workspace size for both.
+ * `experts` on are left out).
+ * A few tokens of one rank are routed without a workspace (0 bytes: it may be NULL).
  *
  * tuna_moe_route_backward - dlogits (the logits' type) from dweights (tokens x k, f32):
  * the gradient through scoring, renormalisation and scale; the choice itself is constant.
  */
 int tuna_moe_order_workspace_bytes(int64_t tokens, int experts, int k, int ranks, size_t *bytes);
+int tuna_moe_route_workspace_bytes(int64_t tokens, int experts, int k, int ranks, size_t *bytes);
 int tuna_moe_route(const void *logits, int dtype, int64_t tokens, int experts, int64_t ld, int k,
                    int ranks, int scoring, int renormalize, float scale, int32_t *ids,
                    float *weights, int64_t *counts, int64_t *offsets, int64_t *rows, int64_t *pos,

@@ -81,6 +81,7 @@ SIGNATURES = {
     "tuna_plan_cuda_error": (ctypes.c_int, [_VP]),
     "tuna_plan_device_status": (ctypes.c_int, [_VP, _INTP]),
     "tuna_moe_order_workspace_bytes": (ctypes.c_int, [_I64, _INT, _INT, _INT, _SZP]),
+    "tuna_moe_route_workspace_bytes": (ctypes.c_int, [_I64, _INT, _INT, _INT, _SZP]),
     "tuna_moe_route": (ctypes.c_int, [_VP, _INT, _I64, _INT, _I64] + [_INT] * 4 + [ctypes.c_float] + [_VP] * 7
                        + [ctypes.c_size_t, _VP]),
     "tuna_moe_order": (ctypes.c_int, [_VP, _I64, _INT, _INT, _INT] + [_VP] * 5 + [ctypes.c_size_t, _VP]),

@@ -185,6 +185,7 @@ struct TileArgs {
   int blocks;   // of k
   int n_tiles;
   int store_tiles;  // results leave through map_out
+  int one_copy;     // SWIGLU: map_b brings gate and up rows together
   int *error;
 };
 
@@ -293,7 +294,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           const uint32_t at = smem_u32(smem) + stage * S::kStageBytes, bar = full + 8 * stage;
           mbar_expect(bar, S::kStageBytes);
           tma_load_2d(at, &map_a, kb * 128, (int)w.row, bar);
-          if (SWIGLU) {
+          if (SWIGLU && a.one_copy) {
+            tma_load_5d(at + 128 * 128, &map_b, kb * 128, 0, 0, w.n0 / 32, w.g, bar);
+          } else if (SWIGLU) {
 #pragma unroll
             for (int q = 0; q < 8; ++q)
               tma_load_3d(at + 128 * 128 + q * 32 * 128, &map_b, kb * 128, w.n0 + (q >> 1) * 32, w.g * 2 + (q & 1), bar);
@@ -553,7 +556,15 @@ int run_tiles(const ProductArgs &p, cudaStream_t st) {
   if (!a.error) return TUNA_ERR_CUDA;
   CUtensorMap ma, mb, mo;
   if (const int rc = make_map(&ma, 2, p.a, p.k, p.m, 1, p.lda, 128)) return rc;
-  if (const int rc = make_map(&mb, 3, p.b, p.k, p.n, (int64_t)p.groups * (SWIGLU ? 2 : 1), p.ldb, SWIGLU ? 32 : BN)) return rc;
+  // One copy of 32 KB for a block's gate and up rows, instead of eight of 4 KB that the issuing thread
+  // could not keep up with (64 experts of 4096 x 2048, 16384 rows: 471 us).  Its 32-row steps must not
+  // cross from one matrix into the next.
+  a.one_copy = SWIGLU && p.n % 32 == 0;
+  if (a.one_copy) {
+    if (const int rc = make_gate_up_map(&mb, p.b, p.k, p.n, p.groups, p.ldb)) return rc;
+  } else {
+    if (const int rc = make_map(&mb, 3, p.b, p.k, p.n, (int64_t)p.groups * (SWIGLU ? 2 : 1), p.ldb, SWIGLU ? 32 : BN)) return rc;
+  }
   mo = ma;
   a.store_tiles = Shape<BN>::kOutBytes && !SWIGLU && !p.out_f32 && aligned(p.out, 16) && p.ldo % 8 == 0;
   if (a.store_tiles)
@@ -612,6 +623,17 @@ int make_map(CUtensorMap *map, int rank, const void *p, int64_t k, int64_t rows,
   const CUresult r = f(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, (cuuint32_t)rank, const_cast<void *>(p), dims, strides, boxes, ones,
                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? TUNA_OK : note_cuda(cudaErrorInvalidValue);
+}
+
+int make_gate_up_map(CUtensorMap *map, const void *p, int64_t k, int64_t rows, int64_t groups, int64_t ld) {
+  EncodeTiled f = encoder();
+  if (!f) return TUNA_ERR_CUDA;
+  const cuuint64_t dims[5] = {(cuuint64_t)k, 32, 2, (cuuint64_t)(rows / 32), (cuuint64_t)groups};
+  const cuuint64_t strides[4] = {(cuuint64_t)ld, (cuuint64_t)(ld * rows), (cuuint64_t)(ld * 32), (cuuint64_t)(ld * rows * 2)};
+  const cuuint32_t boxes[5] = {128, 32, 2, 4, 1}, ones[5] = {1, 1, 1, 1, 1};
+  const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, const_cast<void *>(p), dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? TUNA_OK : note_cuda(cudaErrorInvalidValue);
 }
 

@@ -65,6 +65,10 @@ inline int allow_smem(K kernel, size_t bytes, bool (&set)[64]) {
 // rows, then `matrices` back to back; boxes of 128 bytes x `box` rows, swizzled (tuna_fp8.cu).
 int make_map(CUtensorMap *map, int rank, const void *p, int64_t k, int64_t rows, int64_t matrices, int64_t ld, int box, bool bf16 = false);
 
+// The same for gate and up matrices that alternate (groups x 2 x rows x k bytes, rows a multiple of 32):
+// boxes of 128 bytes x 32 rows x gate, up x 4, so that one copy brings the rows that a tile interleaves.
+int make_gate_up_map(CUtensorMap *map, const void *p, int64_t k, int64_t rows, int64_t groups, int64_t ld);
+
 // Carves a caller's workspace into 256-byte aligned pieces; with base == nullptr it only adds up.
 struct Carve {
   char *base;
@@ -332,6 +336,11 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
                "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int u, int v, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(z), "r"(u), "r"(v), "r"(bar)
                : "memory");
 }
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, int x, int y, uint32_t src) {

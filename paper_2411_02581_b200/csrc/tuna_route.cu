@@ -82,24 +82,26 @@ struct OrderArgs {
   int64_t *counts, *offsets, *rows, *pos;
 };
 
-constexpr int kOrderThreads = 1024, kOrderWarps = kOrderThreads / 32;
+// The small router has more threads, for its choice.
+constexpr int kOrderThreads = 256, kSmallThreads = 1024;
 
 // Shared memory of the order step: base[experts] (64 bits), then the warps' tables, then the
 // column sums (64-bit pairs would be wasteful: entries of one call stay below 2^31).
-__host__ __device__ inline size_t order_smem(int experts) {
-  return (size_t)experts * 8 + (size_t)kOrderWarps * experts * 4 + (size_t)experts * 8 + 256;
+__host__ __device__ inline size_t order_smem(int experts, int threads) {
+  return (size_t)experts * 8 + (size_t)(threads / 32) * experts * 4 + (size_t)experts * 8 + 256;
 }
 
-__device__ __forceinline__ void place_entries(const OrderArgs &o, char *smem, int rank, int64_t first_entry, int64_t last_entry) {
+template <int THREADS>
+__device__ __forceinline__ void place_entries(const OrderArgs &o, char *smem, int64_t first_entry, int64_t last_entry) {
   // base[e]: the row of the first of this block's entries that chose e
   int64_t *base = (int64_t *)smem;
   uint32_t *table = (uint32_t *)(smem + (size_t)o.experts * 16);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t n = last_entry - first_entry;
-  const int64_t per = (n + kOrderWarps - 1) / kOrderWarps;
+  const int64_t per = (n + (THREADS / 32) - 1) / (THREADS / 32);
   const int64_t a = first_entry + min(n, warp * per), b = first_entry + min(n, (warp + 1) * per);
   uint32_t *mine = table + (size_t)warp * o.experts;
-  for (int e = threadIdx.x; e < kOrderWarps * o.experts; e += kOrderThreads) table[e] = 0;
+  for (int e = threadIdx.x; e < (THREADS / 32) * o.experts; e += THREADS) table[e] = 0;
   __syncthreads();
   for (int64_t i = a; i < b; i += 32) {
     const int id = i + lane < b ? o.ids[i + lane] : -1;
@@ -109,9 +111,9 @@ __device__ __forceinline__ void place_entries(const OrderArgs &o, char *smem, in
     __syncwarp();
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < o.experts; e += kOrderThreads) {
+  for (int e = threadIdx.x; e < o.experts; e += THREADS) {
     uint32_t sum = 0;
-    for (int w = 0; w < kOrderWarps; ++w) {
+    for (int w = 0; w < (THREADS / 32); ++w) {
       const uint32_t c = table[(size_t)w * o.experts + e];
       table[(size_t)w * o.experts + e] = sum;
       sum += c;
@@ -173,8 +175,8 @@ __global__ void __launch_bounds__(kOrderThreads) tuna_order_kernel(OrderArgs o) 
   wait_previous();
   allow_next();
   const int E = o.experts;
-  const int rank = (int)(blockIdx.x / o.rank_groups);
-  const int64_t group = blockIdx.x % o.rank_groups;
+  const int rank = (int)blockIdx.x / (int)o.rank_groups;
+  const int64_t group = (int)blockIdx.x - rank * (int)o.rank_groups;
   int64_t *base = (int64_t *)smem;
   int *total = (int *)(smem + (size_t)E * 8);  // of this rank, per expert
   int *before = total + E;                     // of this rank's earlier chunks
@@ -182,12 +184,22 @@ __global__ void __launch_bounds__(kOrderThreads) tuna_order_kernel(OrderArgs o) 
   __syncthreads();
   const int64_t chunks = o.rank_chunks, mine = group * o.group;
   // threads take (a row of hist, an expert) with the expert along the lanes
-  const int lanes = E >= kOrderThreads ? kOrderThreads : E;
+  const int lanes = E >= kOrderThreads ? kOrderThreads : E;  // (more experts than threads: several rounds)
   const int stripes = kOrderThreads / lanes;
   const int stripe = threadIdx.x / lanes;
-  int64_t earlier = 0;  // entries of earlier ranks
+  // entries of earlier ranks: all of hist before this rank's part, eight at a time (hist is aligned)
+  int64_t earlier = 0;
+  {
+    const int64_t before = rank * chunks * E;
+    const uint4 *h = reinterpret_cast<const uint4 *>(o.hist);
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < before / 8; i += kOrderThreads) {
+      const uint4 v = h[i];
+      earlier += (v.x & 0xffffu) + (v.x >> 16) + (v.y & 0xffffu) + (v.y >> 16) + (v.z & 0xffffu) + (v.z >> 16) + (v.w & 0xffffu) + (v.w >> 16);
+    }
+    for (int64_t i = before / 8 * 8 + threadIdx.x; i < before; i += kOrderThreads) earlier += o.hist[i];
+  }
   for (int e = threadIdx.x % lanes; e < E && stripe < stripes; e += lanes) {
-    for (int64_t c = stripe; c < rank * chunks; c += stripes) earlier += o.hist[c * E + e];
     int t = 0, p = 0;
     const uint16_t *h = o.hist + rank * chunks * E + e;
 #pragma unroll 8
@@ -222,7 +234,7 @@ __global__ void __launch_bounds__(kOrderThreads) tuna_order_kernel(OrderArgs o) 
   __syncthreads();
   const int64_t t0 = rank * o.rank_tokens + mine * o.chunk;
   const int64_t t1 = min((int64_t)(rank + 1) * o.rank_tokens, t0 + (int64_t)o.group * o.chunk);
-  place_entries(o, smem, rank, t0 * o.k, t1 * o.k);
+  place_entries<kOrderThreads>(o, smem, t0 * o.k, t1 * o.k);
   // rows that no entry fills (masked choices): -1, written by the last rank's blocks, which know the sum
   if (rank == o.ranks - 1)
     for (int64_t j = rows_before + group * kOrderThreads + threadIdx.x; j < o.tokens * o.k; j += o.rank_groups * kOrderThreads) o.rows[j] = -1;
@@ -235,8 +247,8 @@ __global__ void __launch_bounds__(256) tuna_order_hist_kernel(OrderArgs o) {
   allow_next();
   for (int e = threadIdx.x; e < o.experts; e += 256) count[e] = 0;
   __syncthreads();
-  const int64_t rank = blockIdx.x / o.rank_chunks, c = blockIdx.x % o.rank_chunks;
-  const int64_t t0 = rank * o.rank_tokens + c * o.chunk, t1 = min((rank + 1) * o.rank_tokens, t0 + o.chunk);
+  const int rank = (int)blockIdx.x / (int)o.rank_chunks, c = (int)blockIdx.x - rank * (int)o.rank_chunks;
+  const int64_t t0 = rank * o.rank_tokens + (int64_t)c * o.chunk, t1 = min((rank + 1) * o.rank_tokens, t0 + o.chunk);
   for (int64_t i = t0 * o.k + threadIdx.x; i < t1 * o.k; i += 256) {
     const int id = o.ids[i];
     if (id >= 0 && id < o.experts) atomicAdd(count + id, 1);
@@ -249,22 +261,30 @@ __global__ void __launch_bounds__(256) tuna_order_hist_kernel(OrderArgs o) {
 template <int LPT, int VPL, typename T>
 __global__ void __launch_bounds__(kTopThreads) tuna_route_kernel(RouteArgs a, OrderArgs o) {
   extern __shared__ int count[];
+  for (int e = threadIdx.x; e < a.experts; e += kTopThreads) count[e] = 0;
   wait_previous();
   allow_next();
-  for (int e = threadIdx.x; e < a.experts; e += kTopThreads) count[e] = 0;
-  __syncthreads();
-  const int64_t rank = blockIdx.x / o.rank_chunks, c = blockIdx.x % o.rank_chunks;
-  const int64_t t0 = rank * o.rank_tokens + c * o.chunk, t1 = min((rank + 1) * o.rank_tokens, t0 + o.chunk);
+  const int rank = (int)blockIdx.x / (int)o.rank_chunks, c = (int)blockIdx.x - rank * (int)o.rank_chunks;
+  const int64_t t0 = rank * o.rank_tokens + (int64_t)c * o.chunk, t1 = min((rank + 1) * o.rank_tokens, t0 + o.chunk);
   const int lane = threadIdx.x % LPT;
-  for (int64_t tb = t0; tb < t1; tb += kTopThreads / LPT) {  // (uniform: the shuffles need whole warps)
-    const int64_t t = tb + threadIdx.x / LPT;
-    float z[VPL];
+  constexpr int kStep = kTopThreads / LPT;
+  auto fetch = [&](int64_t t, float (&z)[VPL]) {
     if (t < t1) {
       load_logits(reinterpret_cast<const T *>(a.logits) + t * a.ld, lane * VPL, a.experts, a.vec, z);
     } else {
 #pragma unroll
       for (int i = 0; i < VPL; ++i) z[i] = -INFINITY;
     }
+  };
+  float next[VPL];
+  int64_t t = t0 + threadIdx.x / LPT;
+  fetch(t, next);
+  __syncthreads();
+  for (int64_t tb = t0; tb < t1; tb += kStep, t += kStep) {  // (uniform: the shuffles need whole warps)
+    float z[VPL];
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) z[i] = next[i];
+    fetch(t + kStep, next);  // the next token's logits are on their way during this one's choice
     int id;
     float w;
     choose<LPT>(z, lane, a.k, a.scoring, a.renormalize, a.scale, id, w);
@@ -280,16 +300,16 @@ __global__ void __launch_bounds__(kTopThreads) tuna_route_kernel(RouteArgs a, Or
 
 // A few tokens of one rank: choice and order in one block and one launch.
 template <int LPT, int VPL, typename T>
-__global__ void __launch_bounds__(kOrderThreads) tuna_route_small_kernel(RouteArgs a, OrderArgs o) {
+__global__ void __launch_bounds__(kSmallThreads) tuna_route_small_kernel(RouteArgs a, OrderArgs o) {
   extern __shared__ __align__(16) char smem[];
   int64_t *base = (int64_t *)smem;
   int *count = (int *)(smem + (size_t)a.experts * 8);
-  for (int e = threadIdx.x; e < a.experts; e += kOrderThreads) count[e] = 0;
+  for (int e = threadIdx.x; e < a.experts; e += kSmallThreads) count[e] = 0;
   wait_previous();
   allow_next();
   __syncthreads();
   const int lane = threadIdx.x % LPT;
-  for (int64_t tb = 0; tb < a.tokens; tb += kOrderThreads / LPT) {
+  for (int64_t tb = 0; tb < a.tokens; tb += kSmallThreads / LPT) {
     const int64_t t = tb + threadIdx.x / LPT;
     float z[VPL];
     if (t < a.tokens) {
@@ -308,7 +328,7 @@ __global__ void __launch_bounds__(kOrderThreads) tuna_route_small_kernel(RouteAr
     }
   }
   __syncthreads();
-  const int e = threadIdx.x;  // (experts <= TUNA_MOE_MAX_EXPERTS < kOrderThreads)
+  const int e = threadIdx.x;  // (experts <= TUNA_MOE_MAX_EXPERTS < kSmallThreads)
   const int64_t c = e < a.experts ? count[e] : 0;
   int64_t sum;
   const int64_t x = block_scan(c, &sum);
@@ -320,8 +340,8 @@ __global__ void __launch_bounds__(kOrderThreads) tuna_route_small_kernel(RouteAr
       if (e == a.experts - 1) o.offsets[a.experts] = sum;
     }
   }
-  place_entries(o, smem, 0, 0, a.tokens * a.k);
-  for (int64_t j = sum + threadIdx.x; j < a.tokens * a.k; j += kOrderThreads) o.rows[j] = -1;
+  place_entries<kSmallThreads>(o, smem, 0, a.tokens * a.k);
+  for (int64_t j = sum + threadIdx.x; j < a.tokens * a.k; j += kSmallThreads) o.rows[j] = -1;
 }
 
 // Gradient of the weights with respect to the logits; the probabilities are computed anew
@@ -347,47 +367,35 @@ __global__ void __launch_bounds__(kTopThreads) tuna_route_grad_kernel(RouteGradA
   const int64_t t = (int64_t)blockIdx.x * (kTopThreads / LPT) + threadIdx.x / LPT;
   const bool there = t < a.tokens;
   float z[VPL], d[VPL];
+  int id = -1;
+  float g = 0.0f;
+  if (there && lane < a.k) id = __ldg(a.ids + t * a.k + lane), g = __ldg(a.dweights + t * a.k + lane) * a.scale;
   if (there) {
     load_logits(reinterpret_cast<const T *>(a.logits) + t * a.ld, lane * VPL, a.experts, a.vec, z);
   } else {
 #pragma unroll
     for (int i = 0; i < VPL; ++i) z[i] = -INFINITY;
   }
-  int id = -1;
-  float g = 0.0f;
-  if (there && lane < a.k) {
-    id = a.ids[t * a.k + lane];
-    if (id >= a.experts) id = -1;
-    g = id < 0 ? 0.0f : a.dweights[t * a.k + lane] * a.scale;
-  }
-  float top = -INFINITY, mine = -INFINITY;
+  if (id < 0 || id >= a.experts) id = -1, g = 0.0f;
+  // the chosen logit of this lane's slot, anew from memory: it is there already
+  const float mine = id < 0 ? -INFINITY : logit_of(to_f32(__ldg(reinterpret_cast<const T *>(a.logits) + t * a.ld + id)));
+  const bool soft = a.scoring == TUNA_MOE_SOFTMAX;
+  float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < VPL; ++i) top = fmaxf(top, z[i]), d[i] = 0.0f;
 #pragma unroll
   for (int s = 1; s < LPT; s <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, s));
-  // the chosen logits, from the lanes that hold them
-  for (int s = 0; s < a.k; ++s) {
-    const int e = __shfl_sync(~0u, id, s, LPT);
-    const int owner = e < 0 ? 0 : e / VPL;
-    float v = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < VPL; ++i)
-      if (e == lane * VPL + i) v = z[i];
-    v = __shfl_sync(~0u, v, owner, LPT);
-    if (lane == s) mine = e < 0 ? -INFINITY : v;
-  }
-  const bool soft = a.scoring == TUNA_MOE_SOFTMAX;
   float p = mine == -INFINITY ? 0.0f : soft ? exp_of(mine, top) : sigmoid_of(mine);
   float sum = p;
   if (soft && !a.renormalize) {
     sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) sum += z[i] == -INFINITY ? 0.0f : exp_of(z[i], top);
+    for (int i = 0; i < VPL; ++i) d[i] = z[i] == -INFINITY ? 0.0f : exp_of(z[i], top), sum += d[i];
   }
 #pragma unroll
   for (int s = 1; s < LPT; s <<= 1) sum += __shfl_xor_sync(~0u, sum, s);
   const float over = sum > 0.0f ? 1.0f / sum : 0.0f;
-  const float w = soft || a.renormalize ? (sum > 0.0f ? p / sum : 0.0f) : p;
+  const float w = soft || a.renormalize ? p * over : p;
   float gw = g * w;
 #pragma unroll
   for (int s = 1; s < LPT; s <<= 1) gw += __shfl_xor_sync(~0u, gw, s);
@@ -396,16 +404,15 @@ __global__ void __launch_bounds__(kTopThreads) tuna_route_grad_kernel(RouteGradA
     mine_d = a.renormalize ? w * (g - gw) : w * g;
   else
     mine_d = (a.renormalize ? (g - gw) * over : g) * p * (1.0f - p);
-  for (int s = 0; s < a.k; ++s) {
-    const int e = __shfl_sync(~0u, id, s, LPT);
-    const float v = __shfl_sync(~0u, mine_d, s, LPT);
-#pragma unroll
-    for (int i = 0; i < VPL; ++i)
-      if (e == lane * VPL + i) d[i] += v;
-  }
   if (soft && !a.renormalize) {
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) d[i] -= z[i] == -INFINITY ? 0.0f : (sum > 0.0f ? exp_of(z[i], top) / sum : 0.0f) * gw;
+    for (int i = 0; i < VPL; ++i) d[i] *= -over * gw;
+  }
+  for (int s = 0; s < a.k; ++s) {
+    const int at = __shfl_sync(~0u, id, s, LPT) - lane * VPL;
+    const float v = __shfl_sync(~0u, mine_d, s, LPT);
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) d[i] += at == i ? v : 0.0f;
   }
   if (!there) return;
   T *out = reinterpret_cast<T *>(a.dlogits) + t * a.ldd + lane * VPL;
@@ -440,20 +447,27 @@ __global__ void __launch_bounds__(256) tuna_combine_kernel(CombineArgs a) {
   if (c >= a.dim) return;
   for (int64_t t = blockIdx.x; t < a.tokens; t += gridDim.x) {
     float acc[8] = {};
-    for (int s = 0; s < a.k; ++s) {
-      const int64_t r = a.pos[t * a.k + s];
-      if (r < 0 || r >= a.rows) continue;
-      const float w = a.weights[t * a.k + s];
-      const TY *y = reinterpret_cast<const TY *>(a.y) + r * a.ldy + c;
-      float v[8];
-      if (a.vec) {
-        load_row(y, v);
-      } else {
+    for (int s = 0; s < a.k; s += 2) {  // two rows in flight
+      Eight<TY> y[2];
+      float w[2];
+      bool there[2];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c + j < a.dim ? to_f32(y[j]) : 0.0f;
+      for (int i = 0; i < 2; ++i) {
+        const int64_t r = s + i < a.k ? __ldg(a.pos + t * a.k + s + i) : -1;
+        there[i] = r >= 0 && r < a.rows;
+        if (there[i]) {
+          w[i] = __ldg(a.weights + t * a.k + s + i);
+          y[i].load(reinterpret_cast<const TY *>(a.y) + r * a.ldy + c, a.vec, a.dim - c);
+        }
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] = fmaf(w, v[j], acc[j]);
+      for (int i = 0; i < 2; ++i) {
+        if (!there[i]) continue;
+        float v[8];
+        y[i].values(v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = fmaf(w[i], v[j], acc[j]);
+      }
     }
     TO *out = reinterpret_cast<TO *>(a.out) + t * a.ldo + c;
     if (a.vec) {
@@ -555,8 +569,8 @@ int zero_order(const OrderArgs &o, int ranks, int experts, cudaStream_t st) {
 
 int launch_order(const OrderArgs &o, cudaStream_t st) {
   static bool set[64] = {};
-  if (const int rc = allow_smem(tuna_order_kernel, order_smem(TUNA_MOE_MAX_EXPERTS), set)) return rc;
-  return launch(tuna_order_kernel, dim3((unsigned)(o.rank_groups * o.ranks)), kOrderThreads, order_smem(o.experts), st, false, o);
+  if (const int rc = allow_smem(tuna_order_kernel, order_smem(TUNA_MOE_MAX_EXPERTS, kOrderThreads), set)) return rc;
+  return launch(tuna_order_kernel, dim3((unsigned)(o.rank_groups * o.ranks)), kOrderThreads, order_smem(o.experts, kOrderThreads), st, false, o);
 }
 
 // Lanes a token and values a lane: the fewest lanes that hold the experts at 8 values each
@@ -586,8 +600,8 @@ struct SmallLaunch {
   template <int LPT, int VPL>
   int operator()() {
     static bool set[64] = {};
-    if (const int rc = allow_smem(tuna_route_small_kernel<LPT, VPL, T>, order_smem(TUNA_MOE_MAX_EXPERTS), set)) return rc;
-    return launch(tuna_route_small_kernel<LPT, VPL, T>, dim3(1), kOrderThreads, order_smem(a.experts), st, false, a, o);
+    if (const int rc = allow_smem(tuna_route_small_kernel<LPT, VPL, T>, order_smem(TUNA_MOE_MAX_EXPERTS, kSmallThreads), set)) return rc;
+    return launch(tuna_route_small_kernel<LPT, VPL, T>, dim3(1), kSmallThreads, order_smem(a.experts, kSmallThreads), st, false, a, o);
   }
 };
 template <typename T>
@@ -624,6 +638,12 @@ int tuna_moe_order_workspace_bytes(int64_t tokens, int experts, int k, int ranks
   return TUNA_OK;
 }
 
+int tuna_moe_route_workspace_bytes(int64_t tokens, int experts, int k, int ranks, size_t *bytes) {
+  if (const int rc = tuna_moe_order_workspace_bytes(tokens, experts, k, ranks, bytes)) return rc;
+  if (ranks == 1 && tokens <= kSmallTokens) *bytes = 0;
+  return TUNA_OK;
+}
+
 int tuna_moe_order(const int32_t *ids, int64_t tokens, int experts, int k, int ranks, int64_t *counts, int64_t *offsets,
                    int64_t *rows, int64_t *pos, void *workspace, size_t workspace_bytes, void *stream) {
   if (const int rc = check_order(tokens, experts, k, ranks)) return rc;
@@ -650,13 +670,14 @@ int tuna_moe_route(const void *logits, int dtype, int64_t tokens, int experts, i
   if (tokens == 0) return zero_order(o, ranks, experts, st);
   if (!logits || !ids || !weights || !rows || !pos || !aligned(logits, dtype_size(dtype))) return TUNA_ERR_INVALID_ARG;
   plan_order(o, tokens, experts, k, ranks);
-  if (!workspace || !aligned(workspace, 256) || workspace_bytes < order_bytes(tokens, experts, k, ranks)) return TUNA_ERR_WORKSPACE;
+  const bool small = ranks == 1 && tokens <= kSmallTokens;
+  if (!small && (!workspace || !aligned(workspace, 256) || workspace_bytes < order_bytes(tokens, experts, k, ranks))) return TUNA_ERR_WORKSPACE;
   o.hist = (uint16_t *)workspace;
   RouteArgs a = {};
   a.logits = logits, a.tokens = tokens, a.ld = ld, a.experts = experts, a.k = k;
   a.scoring = scoring, a.renormalize = renormalize != 0, a.scale = scale, a.ids = ids, a.weights = weights;
   a.vec = aligned(logits, 16) && ld * dtype_size(dtype) % 16 == 0;
-  if (ranks == 1 && tokens <= kSmallTokens)
+  if (small)
     return dtype == TUNA_DTYPE_F32 ? by_width(experts, k, SmallLaunch<float>{a, o, st}) : by_width(experts, k, SmallLaunch<__nv_bfloat16>{a, o, st});
   const int rc = dtype == TUNA_DTYPE_F32 ? by_width(experts, k, RouteLaunch<float>{a, o, st})
                                          : by_width(experts, k, RouteLaunch<__nv_bfloat16>{a, o, st});

@@ -74,11 +74,11 @@ def _bytes(function, *sizes):
     """A workspace size, asked of the library once for each set of sizes."""
     n = ctypes.c_size_t()
     _check(getattr(B.lib(), function)(*sizes, ctypes.byref(n)), function)
-    return max(n.value, 256)
+    return n.value
 
 
 def _order_workspace(tokens, experts, k, ranks, device):
-    return torch.empty(_bytes("tuna_moe_order_workspace_bytes", tokens, experts, k, ranks), dtype=torch.uint8, device=device)
+    return torch.empty(max(_bytes("tuna_moe_order_workspace_bytes", tokens, experts, k, ranks), 256), dtype=torch.uint8, device=device)
 
 
 def _order_outputs(tokens, experts, k, ranks, device):
@@ -93,14 +93,20 @@ def route(logits, k, *, scoring="softmax", renormalize=False, scale=1.0, ranks=1
     t, e = logits.shape
     if ranks < 1 or t % ranks:
         raise ValueError(f"{t} tokens do not divide over {ranks} ranks")
-    device = logits.device
-    ws = _order_workspace(t, e, k, ranks, device)
-    ids = torch.empty(t, k, dtype=torch.int32, device=device)
-    weights = torch.empty(t, k, dtype=torch.float32, device=device)
-    counts, offsets, rows, pos = _order_outputs(t, e, k, ranks, device)
-    _check(B.lib().tuna_moe_route(logits.data_ptr(), DTYPES[logits.dtype], t, e, ld, k, ranks, _scoring(scoring), int(renormalize), scale,
-                                  ids.data_ptr(), weights.data_ptr(), counts.data_ptr(), offsets.data_ptr(), rows.data_ptr(),
-                                  pos.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream, logits.device)), "tuna_moe_route")
+    device, empty, long = logits.device, torch.empty, torch.int64
+    need = _bytes("tuna_moe_route_workspace_bytes", t, e, k, ranks)
+    ws = empty(need, dtype=torch.uint8, device=device) if need else None
+    ids = empty(t, k, dtype=torch.int32, device=device)
+    weights = empty(t, k, dtype=torch.float32, device=device)
+    counts = empty(ranks, e, dtype=long, device=device)
+    offsets = empty(ranks * e + 1, dtype=long, device=device)
+    rows = empty(t * k, dtype=long, device=device)
+    pos = empty(t, k, dtype=long, device=device)
+    rc = B.lib().tuna_moe_route(logits.data_ptr(), DTYPES[logits.dtype], t, e, ld, k, ranks, _scoring(scoring), renormalize, scale,
+                                ids.data_ptr(), weights.data_ptr(), counts.data_ptr(), offsets.data_ptr(), rows.data_ptr(),
+                                pos.data_ptr(), ws.data_ptr() if need else None, need, _stream(stream, device))
+    if rc:
+        _check(rc, "tuna_moe_route")
     return Routing(ids, weights, counts, offsets, rows, pos)
 
 
@@ -172,30 +178,37 @@ def fp8_quantize(x, layout="rows", *, stream=None):
 
     ``q`` of the layouts "columns" and "tiles_t" is that of the transposed matrix."""
     ld = _matrix(x, "x", FLOATS)
-    if layout not in LAYOUTS:
+    which = LAYOUTS.get(layout)
+    if which is None:
         raise ValueError(f"layout: one of {', '.join(LAYOUTS)}, got {layout!r}")
     rows, cols = x.shape
-    out = (cols, rows) if layout in ("columns", "tiles_t") else (rows, cols)
-    pitch = (out[1] + 15) // 16 * 16
+    out_rows, out_cols = (cols, rows) if which & 1 else (rows, cols)
+    pitch = (out_cols + 15) & ~15
     device = x.device
-    q = torch.empty(out[0], pitch, dtype=torch.float8_e4m3fn, device=device)
-    tiles = layout in ("tiles", "tiles_t")
-    scale = torch.empty(_blocks(out[0]) if tiles else _blocks(out[1]), _blocks(out[1]) if tiles else out[0], dtype=torch.float32, device=device)
-    _check(B.lib().tuna_fp8_quantize(x.data_ptr(), DTYPES[x.dtype], rows, cols, ld, LAYOUTS[layout], q.data_ptr(), max(pitch, 16),
-                                     scale.data_ptr(), _stream(stream, x.device)), "tuna_fp8_quantize")
-    return q if pitch == out[1] else q[:, :out[1]], scale
+    q = torch.empty(out_rows, pitch, dtype=torch.float8_e4m3fn, device=device)
+    blocks = (out_cols + 127) >> 7
+    if which < 2:
+        scale = torch.empty(blocks, out_rows, dtype=torch.float32, device=device)
+    else:
+        scale = torch.empty((out_rows + 127) >> 7, blocks, dtype=torch.float32, device=device)
+    rc = B.lib().tuna_fp8_quantize(x.data_ptr(), DTYPES[x.dtype], rows, cols, ld, which, q.data_ptr(), pitch or 16, scale.data_ptr(),
+                                   _stream(stream, device))
+    if rc:
+        _check(rc, "tuna_fp8_quantize")
+    return q if pitch == out_cols else q[:, :out_cols], scale
 
 
 def _fp8_matrix(q, name):
-    """An e4m3 operand's pitch; copies one whose rows do not start on 16-byte boundaries."""
+    """(operand, pitch, rows, columns) of an e4m3 matrix; copies one whose rows do not start on 16-byte boundaries."""
     ld = _matrix(q, name, (torch.float8_e4m3fn,))
-    if q.shape[0] <= 1:
-        ld = (q.shape[1] + 15) // 16 * 16   # the pitch of a single row is free
-    if ld % 16 or q.data_ptr() % 16:
-        p = torch.zeros(q.shape[0], (q.shape[1] + 15) // 16 * 16, dtype=torch.uint8, device=q.device)
-        p[:, :q.shape[1]] = q.view(torch.uint8)
-        return p, p.shape[1]
-    return q, ld
+    rows, cols = q.shape
+    if rows <= 1:
+        ld = (cols + 15) & ~15   # the pitch of a single row is free
+    if ld & 15 or q.data_ptr() & 15:
+        p = torch.zeros(rows, (cols + 15) & ~15, dtype=torch.uint8, device=q.device)
+        p[:, :cols] = q.view(torch.uint8)
+        q, ld = p, p.shape[1]
+    return q, ld or 16, rows, cols
 
 
 def fp8_matmul(a, a_scale, b, b_scale, *, offsets=None, b_blocks="tiles", out_dtype=torch.bfloat16, stream=None):
@@ -204,32 +217,35 @@ def fp8_matmul(a, a_scale, b, b_scale, *, offsets=None, b_blocks="tiles", out_dt
     ``a`` [m, k] with "rows" scales.  ``b`` [n, k] with "tiles" scales, or "rows" scales
     (``b_blocks="rows"``); or [groups, n, k] with ``offsets`` (int64 [groups + 1]): rows
     offsets[g] .. offsets[g + 1] of ``a`` meet ``b[g]``."""
-    k = b.shape[-1]
-    if a.dim() != 2 or a.shape[1] != k:
-        raise ValueError(f"a: shape {tuple(a.shape)}, wanted (any, {k})")
-    m = a.shape[0]
-    a, lda = _fp8_matrix(a, "a")
+    a, lda, m, k = _fp8_matrix(a, "a")
     if out_dtype not in FLOATS:
         raise ValueError(f"out_dtype: one of {FLOATS}")
-    if b_blocks not in ("tiles", "rows"):
-        raise ValueError(f"b_blocks: tiles or rows, got {b_blocks!r}")
-    groups = 1
+    blocks = (k + 127) >> 7
+    groups, at = 1, None
     if offsets is not None:
         if b.dim() != 3 or not b.is_contiguous() or b_blocks != "tiles":
             raise ValueError("b: contiguous matrices [groups, n, k] with tile scales go with offsets")
-        groups, n = b.shape[:2]
-        _dense(offsets, "offsets", torch.int64, (groups + 1,))
-        flat, ldb = _fp8_matrix(b.view(groups * n, k), "b")
+        groups, n, kb = b.shape
+        at = _dense(offsets, "offsets", torch.int64, (groups + 1,)).data_ptr()
+        b, ldb, _, _ = _fp8_matrix(b.view(groups * n, kb), "b")
+        _dense(b_scale, "b_scale", torch.float32, (groups, (n + 127) >> 7, blocks))
     else:
-        n = b.shape[0]
-        flat, ldb = _fp8_matrix(b, "b")
-    _dense(a_scale, "a_scale", torch.float32, (_blocks(k), m))
-    tiles = (groups, _blocks(n), _blocks(k)) if offsets is not None else (_blocks(n), _blocks(k))
-    _dense(b_scale, "b_scale", torch.float32, (_blocks(k), n) if b_blocks == "rows" else tiles)
-    out = torch.empty(m, n, dtype=out_dtype, device=a.device)
-    _check(B.lib().tuna_fp8_matmul(a.data_ptr(), a_scale.data_ptr(), m, max(lda, 16), flat.data_ptr(), b_scale.data_ptr(), LAYOUTS[b_blocks], n,
-                                   max(ldb, 16), k, groups, None if offsets is None else offsets.data_ptr(), out.data_ptr(),
-                                   DTYPES[out_dtype], max(n, 1), _stream(stream, a.device)), "tuna_fp8_matmul")
+        b, ldb, n, kb = _fp8_matrix(b, "b")
+        if b_blocks == "tiles":
+            _dense(b_scale, "b_scale", torch.float32, ((n + 127) >> 7, blocks))
+        elif b_blocks == "rows":
+            _dense(b_scale, "b_scale", torch.float32, (blocks, n))
+        else:
+            raise ValueError(f"b_blocks: tiles or rows, got {b_blocks!r}")
+    if kb != k:
+        raise ValueError(f"a has {k} columns, b {kb}")
+    _dense(a_scale, "a_scale", torch.float32, (blocks, m))
+    device = a.device
+    out = torch.empty(m, n, dtype=out_dtype, device=device)
+    rc = B.lib().tuna_fp8_matmul(a.data_ptr(), a_scale.data_ptr(), m, lda, b.data_ptr(), b_scale.data_ptr(), LAYOUTS[b_blocks], n, ldb, k,
+                                 groups, at, out.data_ptr(), DTYPES[out_dtype], n or 1, _stream(stream, device))
+    if rc:
+        _check(rc, "tuna_fp8_matmul")
     return out
 
 
@@ -247,7 +263,7 @@ def _experts_weights(w13, s13, w2, s2, hidden):
 
 def _space(need, workspace, device):
     if workspace is None:
-        return torch.empty(need, dtype=torch.uint8, device=device)
+        return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
     return workspace
 
 

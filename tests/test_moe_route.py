@@ -249,7 +249,9 @@ def test_route_refusals():
     def route(p=256, dtype=0, t=64, e=64, ld=64, k=2, ranks=1, scoring=0, ws=256, ws_bytes=1 << 30):
         return L.tuna_moe_route(p, dtype, t, e, ld, k, ranks, scoring, 0, 1.0, p, p, p, p, p, p, ws, ws_bytes, None)
     assert route(p=None) == -1 and route(dtype=2) == -1 and route(ld=63) == -1 and route(scoring=7) == -1
-    assert route(ws=None) == -6 and route(ws=257) == -6 and route(ws_bytes=8) == -6
+    assert route(ws=None, ranks=2) == -6 and route(ws=257, ranks=2) == -6 and route(ws_bytes=8, ranks=2) == -6
+    need = lambda *a: (L.tuna_moe_route_workspace_bytes(*a, B.ctypes.byref(n)), n.value)  # noqa: E731
+    assert need(64, 64, 2, 1) == (0, 0) and need(64, 64, 2, 2)[1] > 0 and need(5000, 64, 2, 1)[1] > 0   # a few tokens need none
     assert route(p=257) == -1                                              # logits off their own alignment
     assert L.tuna_moe_order(None, 64, 64, 2, 1, None, None, None, None, None, 0, None) == -1
     assert L.tuna_moe_route_backward(None, 0, 64, 64, 64, 2, 0, 0, 1.0, None, None, None, 64, None) == -1
