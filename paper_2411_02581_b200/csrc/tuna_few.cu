@@ -515,33 +515,50 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int first = l.group[w.g].first, count = l.group[w.g].count, N = FP8 && count > 8 ? 32 : 16;
           ok = __all_sync(~0u, mbar_wait(smem_u32(l.used + op), op_phase ^ 1, &l.given_up));
           if (!ok) break;
-          // a warp takes 128 columns of a token, a lane four of them
-          const int spans = (w.blocks * kBlock + 127) / 128;
-          int t = i0 >> 5, span = 0;
-          while (t >= count && span < spans) t -= count, ++span;
-          for (; span < spans;) {
-            const int entry = l.entry[first + t], col = w.s * p.segment * kBlock + span * 128 + lane * 4;
-            float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (col < cols) {  // (cols is a multiple of 16)
-              if (up) {
-                const uint2 r = __ldg((const uint2 *)(a.x + (entry / K) * a.ldx + col));
-                v[0] = __uint_as_float(r.x << 16), v[1] = __uint_as_float(r.x & 0xffff0000u);
-                v[2] = __uint_as_float(r.y << 16), v[3] = __uint_as_float(r.y & 0xffff0000u);
-              } else {
-                float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                const float *g0 = a.up + (int64_t)entry * 2 * I + col;
-#pragma unroll 8
-                for (int s = 0; s < a.segments[0]; ++s) {
-                  const float4 x = __ldcg((const float4 *)(g0 + (int64_t)s * n * 2 * I)), y = __ldcg((const float4 *)(g0 + (int64_t)s * n * 2 * I + I));
-                  v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
-                  u[0] += y.x, u[1] += y.y, u[2] += y.z, u[3] += y.w;
+          // A warp takes 128 columns of a token at a time, a lane four of them, two such pieces in flight.
+          // The loads of a piece are issued together: one after the other, the four segments' sums of a
+          // nine-token group took 80000 cycles to lay out, and the grid waited for that block.
+          const int spans = (w.blocks * kBlock + 127) / 128, pieces = spans * count;
+          struct Piece {
+            int t, span;
+            float v[4];
+          };
+          auto load = [&](Piece &x, int i) {
+            x.span = i / count, x.t = i - x.span * count;
+            const int entry = l.entry[first + x.t], col = w.s * p.segment * kBlock + x.span * 128 + lane * 4;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x.v[j] = 0.0f;
+            if (i >= pieces || col >= cols) return;  // (cols is a multiple of 16)
+            if (up) {
+              const uint2 r = __ldg((const uint2 *)(a.x + (entry / K) * a.ldx + col));
+              x.v[0] = __uint_as_float(r.x << 16), x.v[1] = __uint_as_float(r.x & 0xffff0000u);
+              x.v[2] = __uint_as_float(r.y << 16), x.v[3] = __uint_as_float(r.y & 0xffff0000u);
+            } else {
+              float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+              const float *g0 = a.up + (int64_t)entry * 2 * I + col;
+              const int64_t step = (int64_t)n * 2 * I;
+              const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+              for (int s0 = 0; s0 < a.segments[0]; s0 += 4) {
+                float4 gs[4], us[4];
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                  const bool there = s0 + s < a.segments[0];
+                  gs[s] = there ? __ldcg((const float4 *)(g0 + (s0 + s) * step)) : zero;
+                  us[s] = there ? __ldcg((const float4 *)(g0 + (s0 + s) * step + I)) : zero;
                 }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = v[j] / (1.0f + expf(-v[j])) * u[j];
+                for (int s = 0; s < 4; ++s) {
+                  x.v[0] += gs[s].x, x.v[1] += gs[s].y, x.v[2] += gs[s].z, x.v[3] += gs[s].w;
+                  u[0] += us[s].x, u[1] += us[s].y, u[2] += us[s].z, u[3] += us[s].w;
+                }
               }
+#pragma unroll
+              for (int j = 0; j < 4; ++j) x.v[j] = x.v[j] / (1.0f + expf(-x.v[j])) * u[j];
             }
+          };
+          auto lay = [&](const Piece &x) {
             if constexpr (FP8) {
-              uint32_t top = max(max(abs_bits(v[0]), abs_bits(v[1])), max(abs_bits(v[2]), abs_bits(v[3])));
+              uint32_t top = max(max(abs_bits(x.v[0]), abs_bits(x.v[1])), max(abs_bits(x.v[2]), abs_bits(x.v[3])));
               top = __reduce_max_sync(~0u, top);
               // s takes the block's largest value to [2^7, 2^8); a block that is not finite is lost to NaN
               const int e = min(max((int)(top >> 23), 27) - 7, 240);
@@ -550,25 +567,30 @@ __global__ void __launch_bounds__(kThreads, 1)
               uint32_t h2[2], l2[2];
 #pragma unroll
               for (int j = 0; j < 2; ++j) {
-                const float x = v[2 * j] * by, y = v[2 * j + 1] * by;
-                h2[j] = e4m3_pair(x, y);
+                const float f = x.v[2 * j] * by, g = x.v[2 * j + 1] * by;
+                h2[j] = e4m3_pair(f, g);
                 const float2 have = e4m3_values(h2[j]);
-                l2[j] = e4m3_pair((x - have.x) * 16.0f, (y - have.y) * 16.0f);
+                l2[j] = e4m3_pair((f - have.x) * 16.0f, (g - have.y) * 16.0f);
               }
-              const uint32_t to = operands + op * kOperand + span * N * 128 + (lane & 3) * 4;
-              asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + swizzled(t, lane >> 2)), "r"(h2[0] | (h2[1] << 16)) : "memory");
-              asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + swizzled(N / 2 + t, lane >> 2)), "r"(l2[0] | (l2[1] << 16)) : "memory");
-              if (lane == 0) l.piece_scale[op][span][t] = s;
+              const uint32_t to = operands + op * kOperand + x.span * N * 128 + (lane & 3) * 4;
+              asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + swizzled(x.t, lane >> 2)), "r"(h2[0] | (h2[1] << 16)) : "memory");
+              asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + swizzled(N / 2 + x.t, lane >> 2)), "r"(l2[0] | (l2[1] << 16)) : "memory");
+              if (lane == 0) l.piece_scale[op][x.span][x.t] = s;
             } else {
               // (two blocks of 64; the second may lie behind the segment, where its place is unused)
-              const int b = span * 2 + (lane >> 4);
+              const int b = x.span * 2 + (lane >> 4);
               if (b < w.blocks)
-                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(operands + op * kOperand + b * N * 128 + swizzled(t, (lane & 15) >> 1) + (lane & 1) * 8),
-                             "r"(pack_bf16(v[0], v[1])), "r"(pack_bf16(v[2], v[3]))
+                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(operands + op * kOperand + b * N * 128 + swizzled(x.t, (lane & 15) >> 1) + (lane & 1) * 8),
+                             "r"(pack_bf16(x.v[0], x.v[1])), "r"(pack_bf16(x.v[2], x.v[3]))
                              : "memory");
             }
-            t += kLoaders;
-            while (t >= count && span < spans) t -= count, ++span;
+          };
+          for (int i = i0 >> 5; i < pieces; i += 2 * kLoaders) {
+            Piece x, y;
+            load(x, i);
+            load(y, i + kLoaders < pieces ? i + kLoaders : i);
+            lay(x);
+            if (i + kLoaders < pieces) lay(y);
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
