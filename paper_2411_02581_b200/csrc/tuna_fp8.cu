@@ -194,12 +194,13 @@ constexpr int kGemmThreads = 128 + kSumWarps * 32;
 constexpr int kCopyRegs = 64, kSumRegs = 104;  // registers of a thread: copying and issuing warps, promotion
 constexpr int kMaxGroups = TUNA_MOE_MAX_EXPERTS;
 
-template <int BN>
+// STORES: bf16 results, which leave by tensor copies
+template <int BN, bool STORES>
 struct Shape {
-  static constexpr int kStages = BN == 256 ? 3 : 6;
+  static constexpr int kStages = BN == 256 ? (STORES ? 3 : 4) : 6;
   static constexpr int kStageBytes = 128 * 128 + BN * 128;
   static constexpr int kCols = BN / 4;  // accumulator columns of a thread
-  static constexpr int kOutBytes = BN == 256 ? kSumWarps * 4096 : 0;  // each promotion warp's 32 x 64 results, on their way out
+  static constexpr int kOutBytes = BN == 256 && STORES ? kSumWarps * 4096 : 0;  // each promotion warp's 32 x 64 results, on their way out
   // stages, results, then the factors beside the two accumulators, the rows' largest magnitudes, the groups'
   // tile offsets, barriers and flags
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kOutBytes + 2 * 384 * 4 + 512 * 4 + (kMaxGroups + 8) * 4 + 256;
@@ -227,7 +228,7 @@ template <int BN, bool SWIGLU, bool B_ROWS, typename TO>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     tuna_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                         const __grid_constant__ CUtensorMap map_out, const TileArgs a) {
-  using S = Shape<BN>;
+  using S = Shape<BN, !SWIGLU && sizeof(TO) == 2>;
   extern __shared__ char smem_raw[];
   char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   // beside each accumulator: [2][128] factors of the rows for either half of the columns, or with
@@ -343,39 +344,47 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       int buf = 0, buf_phase = 0;
       bool ok = true;
       Walk w;
-      for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
-        walk_to(w, t, a, tile_base, SWIGLU ? BN / 2 : BN);
-        const float *sa0 = a.p.sa + min(w.row + i, w.end - 1), *sa1 = a.p.sa + min(w.row + i + 64, w.end - 1);
-        const float *sb0 = a.p.sb, *sb1 = a.p.sb;
-        if (SWIGLU) {
-          sb0 += ((int64_t)(w.g * 2) * tiles_n + w.n0 / 128) * blocks;
-          sb1 = sb0 + (int64_t)tiles_n * blocks;
-        } else if (!B_ROWS) {
-          sb0 += ((int64_t)w.g * tiles_n + w.n0 / 128) * blocks;
-          sb1 = w.n0 / 128 + 1 < tiles_n ? sb0 + blocks : sb0;
-        }
-        float next[kAhead][kVals];
-        auto fetch = [&](int kb0) {
-#pragma unroll
-          for (int j = 0; j < kAhead; ++j) {
-            const int kb = min(kb0 + j, blocks - 1);
-            next[j][0] = __ldg(sa0 + (int64_t)kb * a.p.m), next[j][1] = __ldg(sa1 + (int64_t)kb * a.p.m);
-            if (B_ROWS) {
-#pragma unroll
-              for (int q = 0; q < 4; ++q) next[j][2 + q] = __ldg(a.p.sb + (int64_t)kb * a.p.n + min(w.n0 + i + q * 64, a.p.n - 1));
-            } else {
-              next[j][2] = __ldg(sb0 + kb), next[j][3] = __ldg(sb1 + kb);
-            }
+      const float *sa0 = nullptr, *sa1 = nullptr, *sb0 = nullptr, *sb1 = nullptr;
+      // the blocks that are fetched next: one run of kAhead ahead of those handed out, across tiles too
+      int64_t ahead_t = blockIdx.x;
+      int ahead_kb = 0;
+      float next[kAhead][kVals];
+      auto fetch = [&]() {
+        if (ahead_t >= tiles) return;
+        if (ahead_kb == 0) {
+          walk_to(w, ahead_t, a, tile_base, SWIGLU ? BN / 2 : BN);
+          sa0 = a.p.sa + min(w.row + i, w.end - 1), sa1 = a.p.sa + min(w.row + i + 64, w.end - 1);
+          if (SWIGLU) {
+            sb0 = a.p.sb + ((int64_t)(w.g * 2) * tiles_n + w.n0 / 128) * blocks;
+            sb1 = sb0 + (int64_t)tiles_n * blocks;
+          } else if (!B_ROWS) {
+            sb0 = a.p.sb + ((int64_t)w.g * tiles_n + w.n0 / 128) * blocks;
+            sb1 = w.n0 / 128 + 1 < tiles_n ? sb0 + blocks : sb0;
           }
-        };
-        fetch(0);
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          const int kb = min(ahead_kb + j, blocks - 1);
+          next[j][0] = __ldg(sa0 + (int64_t)kb * a.p.m), next[j][1] = __ldg(sa1 + (int64_t)kb * a.p.m);
+          if (B_ROWS) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) next[j][2 + q] = __ldg(a.p.sb + (int64_t)kb * a.p.n + min(w.n0 + i + q * 64, a.p.n - 1));
+          } else {
+            next[j][2] = __ldg(sb0 + kb), next[j][3] = __ldg(sb1 + kb);
+          }
+        }
+        ahead_kb += kAhead;
+        if (ahead_kb >= blocks) ahead_kb = 0, ahead_t += gridDim.x;
+      };
+      fetch();
+      for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
         for (int kb0 = 0; ok && kb0 < blocks; kb0 += kAhead) {
           float now[kAhead][kVals];
 #pragma unroll
           for (int j = 0; j < kAhead; ++j)
 #pragma unroll
             for (int q = 0; q < kVals; ++q) now[j][q] = next[j][q];
-          if (kb0 + kAhead < blocks) fetch(kb0 + kAhead);
+          fetch();
 #pragma unroll
           for (int j = 0; j < kAhead; ++j) {
             if (kb0 + j >= blocks) break;
@@ -513,7 +522,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           unpair(acc[16 + i], u[0], u[1]);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const float x = g[j] / (1.0f + expf(-g[j])) * u[j];
+            const float x = __fdividef(g[j], 1.0f + __expf(-g[j])) * u[j];  // (2^-20: 8 bits are kept)
             h[2 * i + j] = x;
             amax = max(amax, abs_bits(x));
           }
@@ -548,6 +557,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 
 template <int BN, bool SWIGLU, bool B_ROWS, typename TO>
 int run_tiles(const ProductArgs &p, cudaStream_t st) {
+  using S = Shape<BN, !SWIGLU && sizeof(TO) == 2>;
   TileArgs a = {};
   a.p = p;
   a.blocks = (int)ceil_div(p.k, 128);
@@ -566,7 +576,7 @@ int run_tiles(const ProductArgs &p, cudaStream_t st) {
     if (const int rc = make_map(&mb, 3, p.b, p.k, p.n, (int64_t)p.groups * (SWIGLU ? 2 : 1), p.ldb, SWIGLU ? 32 : BN)) return rc;
   }
   mo = ma;
-  a.store_tiles = Shape<BN>::kOutBytes && !SWIGLU && !p.out_f32 && aligned(p.out, 16) && p.ldo % 8 == 0;
+  a.store_tiles = S::kOutBytes && !SWIGLU && !p.out_f32 && aligned(p.out, 16) && p.ldo % 8 == 0;
   if (a.store_tiles)
     if (const int rc = make_map(&mo, 2, p.out, p.n, p.m, 1, p.ldo, 32, true)) return rc;
   static bool set[64] = {}, fits = false;
@@ -578,9 +588,9 @@ int run_tiles(const ProductArgs &p, cudaStream_t st) {
     if ((at.numRegs + 7) / 8 * 8 * kGemmThreads < 128 * kCopyRegs + kSumWarps * 32 * kSumRegs) return TUNA_ERR_INTERNAL;
     __atomic_store_n(&fits, true, __ATOMIC_RELEASE);
   }
-  if (const int rc = allow_smem(kernel, Shape<BN>::kSmem, set)) return rc;
+  if (const int rc = allow_smem(kernel, S::kSmem, set)) return rc;
   const int64_t most = (ceil_div(p.m, 128) + (p.offsets ? p.groups : 0)) * a.n_tiles;
-  return launch(kernel, dim3((unsigned)std::min<int64_t>(most, sm_count())), kGemmThreads, Shape<BN>::kSmem, st, false, ma, mb, mo, a);
+  return launch(kernel, dim3((unsigned)std::min<int64_t>(most, sm_count())), kGemmThreads, S::kSmem, st, false, ma, mb, mo, a);
 }
 
 size_t dtype_size(int dtype) { return dtype == TUNA_DTYPE_F32 ? 4 : dtype == TUNA_DTYPE_BF16 ? 2 : 0; }
