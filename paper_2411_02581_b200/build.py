@@ -10,6 +10,8 @@ ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB_DIR = os.path.join(_HERE, "_lib")
 LIB_PATH = os.path.join(LIB_DIR, "libtuna.so")
+TORCH_PATH = os.path.join(LIB_DIR, "tuna_torch.so")   # the operator calls' torch marshalling (tuna_torch.cpp)
+TORCH_SOURCE = os.path.join(CSRC, "tuna_torch.cpp")
 SOURCES = ["tuna_plan.cu", "tuna_api.cu", "tuna_static.cu", "tuna_shard.cu", "tuna_move.cu",
            "tuna_route.cu", "tuna_fp8.cu", "tuna_moe.cu", "tuna_few.cu"]
 HEADERS = [os.path.join(CSRC, h) for h in ("tuna_internal.h", "tuna_plan.h", "tuna_plan_kernels.cuh", "tuna_ops.cuh", "tuna_fp8.h", "tuna_route.cuh")] + [
@@ -31,8 +33,30 @@ def needs_build() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def build_torch(force: bool = False) -> str:
+    """Compile the torch marshalling of the operator calls (host code only)."""
+    deps = [TORCH_SOURCE, os.path.join(ROOT, "include", "tuna.h")]
+    if not force and os.path.exists(TORCH_PATH) and all(os.path.getmtime(d) <= os.path.getmtime(TORCH_PATH) for d in deps):
+        return TORCH_PATH
+    import sysconfig
+
+    import torch
+    base = os.path.dirname(torch.__file__)
+    os.makedirs(LIB_DIR, exist_ok=True)
+    tmp = TORCH_PATH + ".tmp.%d" % os.getpid()
+    subprocess.check_call(
+        ["g++", "-O2", "-std=c++20", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+         "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(base, "include"),
+         "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
+         "-isystem", sysconfig.get_paths()["include"], "-isystem", "/usr/local/cuda/include", TORCH_SOURCE, "-o", tmp,
+         "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cuda", "-ltorch_cpu", "-lc10_cuda", "-lc10", "-ldl"])
+    os.replace(tmp, TORCH_PATH)
+    return TORCH_PATH
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu file for sm_100a and link the shared library."""
+    """Compile every .cu file for sm_100a and link the shared library; then the torch marshalling."""
+    build_torch(force)
     if not force and not needs_build():
         return LIB_PATH
     os.makedirs(LIB_DIR, exist_ok=True)

@@ -3,7 +3,9 @@ experts, few-token layer.
 
 A thin layer over the C ABI in ``include/tuna.h``, like :mod:`binding`: arguments are
 checked and marshalled, outputs and workspaces come from torch's allocator, every
-computation runs in the CUDA library (there is no CPU fallback).  Work is enqueued on
+computation runs in the CUDA library (there is no CPU fallback).  The calls of a decode
+step are marshalled in C++ (``csrc/tuna_torch.cpp``), where ctypes and the interpreter
+would take longer than their kernels.  Work is enqueued on
 ``stream`` (default: torch's current one).  A tensor that was made on another stream is
 the caller's to order, as with any torch operation.
 """
@@ -11,11 +13,14 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import importlib.util
+import os
 from typing import NamedTuple
 
 import torch
 
 from . import binding as B
+from . import build as _build
 
 SOFTMAX, SIGMOID = 0, 1
 SCORING = {"softmax": SOFTMAX, "sigmoid": SIGMOID}
@@ -46,6 +51,23 @@ def _check(rc, what):
         raise B.TunaError(rc, what, B.lib().tuna_ops_cuda_error() if rc == -7 else 0)
 
 
+_marshal = None
+
+
+def _fast():
+    """The C++ marshalling, bound to the loaded library; raises if it has not been built."""
+    global _marshal
+    if _marshal is None:
+        if not os.path.exists(_build.TORCH_PATH):
+            raise RuntimeError(f"{_build.TORCH_PATH} is missing: build it with `python -m paper_2411_02581_b200.build`")
+        spec = importlib.util.spec_from_file_location("tuna_torch", _build.TORCH_PATH)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.bind(B.lib()._handle, _check)
+        _marshal = module
+    return _marshal
+
+
 def _matrix(t, name, dtypes):
     """A CUDA matrix whose rows are contiguous; returns its row pitch."""
     if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype not in dtypes or not t.is_cuda:
@@ -64,9 +86,10 @@ def _dense(t, name, dtype, shape):
 
 
 def _scoring(name):
-    if name not in SCORING:
+    which = SCORING.get(name)
+    if which is None:
         raise ValueError(f"scoring: one of {', '.join(SCORING)}, got {name!r}")
-    return SCORING[name]
+    return which
 
 
 @functools.lru_cache(maxsize=4096)
@@ -89,25 +112,7 @@ def _order_outputs(tokens, experts, k, ranks, device):
 
 def route(logits, k, *, scoring="softmax", renormalize=False, scale=1.0, ranks=1, stream=None) -> Routing:
     """The ``k`` best experts of every token, their weights and the rows' order (``tuna_moe_route``)."""
-    ld = _matrix(logits, "logits", FLOATS)
-    t, e = logits.shape
-    if ranks < 1 or t % ranks:
-        raise ValueError(f"{t} tokens do not divide over {ranks} ranks")
-    device, empty, long = logits.device, torch.empty, torch.int64
-    need = _bytes("tuna_moe_route_workspace_bytes", t, e, k, ranks)
-    ws = empty(need, dtype=torch.uint8, device=device) if need else None
-    ids = empty(t, k, dtype=torch.int32, device=device)
-    weights = empty(t, k, dtype=torch.float32, device=device)
-    counts = empty(ranks, e, dtype=long, device=device)
-    offsets = empty(ranks * e + 1, dtype=long, device=device)
-    rows = empty(t * k, dtype=long, device=device)
-    pos = empty(t, k, dtype=long, device=device)
-    rc = B.lib().tuna_moe_route(logits.data_ptr(), DTYPES[logits.dtype], t, e, ld, k, ranks, _scoring(scoring), renormalize, scale,
-                                ids.data_ptr(), weights.data_ptr(), counts.data_ptr(), offsets.data_ptr(), rows.data_ptr(),
-                                pos.data_ptr(), ws.data_ptr() if need else None, need, _stream(stream, device))
-    if rc:
-        _check(rc, "tuna_moe_route")
-    return Routing(ids, weights, counts, offsets, rows, pos)
+    return Routing(*(_marshal or _fast()).route(logits, k, _scoring(scoring), renormalize, scale, ranks, stream))
 
 
 def order(ids, experts, *, ranks=1, stream=None):
@@ -127,16 +132,7 @@ def order(ids, experts, *, ranks=1, stream=None):
 
 def route_backward(logits, ids, dweights, *, scoring="softmax", renormalize=False, scale=1.0, stream=None):
     """Gradient of :func:`route`'s weights with respect to the logits (``tuna_moe_route_backward``)."""
-    ld = _matrix(logits, "logits", FLOATS)
-    t, e = logits.shape
-    k = ids.shape[1]
-    _dense(ids, "ids", torch.int32, (t, k))
-    _dense(dweights, "dweights", torch.float32, (t, k))
-    d = torch.empty(t, e, dtype=logits.dtype, device=logits.device)
-    _check(B.lib().tuna_moe_route_backward(logits.data_ptr(), DTYPES[logits.dtype], t, e, ld, k, _scoring(scoring), int(renormalize),
-                                           scale, ids.data_ptr(), dweights.data_ptr(), d.data_ptr(), e, _stream(stream, logits.device)),
-           "tuna_moe_route_backward")
-    return d
+    return (_marshal or _fast()).route_backward(logits, ids, dweights, _scoring(scoring), renormalize, scale, stream)
 
 
 def combine(y, weights, pos, *, out_dtype=torch.bfloat16, stream=None):
@@ -177,38 +173,10 @@ def fp8_quantize(x, layout="rows", *, stream=None):
     """(q, scale): ``x`` in 8 bits with a scale for each block (``tuna_fp8_quantize``).
 
     ``q`` of the layouts "columns" and "tiles_t" is that of the transposed matrix."""
-    ld = _matrix(x, "x", FLOATS)
     which = LAYOUTS.get(layout)
     if which is None:
         raise ValueError(f"layout: one of {', '.join(LAYOUTS)}, got {layout!r}")
-    rows, cols = x.shape
-    out_rows, out_cols = (cols, rows) if which & 1 else (rows, cols)
-    pitch = (out_cols + 15) & ~15
-    device = x.device
-    q = torch.empty(out_rows, pitch, dtype=torch.float8_e4m3fn, device=device)
-    blocks = (out_cols + 127) >> 7
-    if which < 2:
-        scale = torch.empty(blocks, out_rows, dtype=torch.float32, device=device)
-    else:
-        scale = torch.empty((out_rows + 127) >> 7, blocks, dtype=torch.float32, device=device)
-    rc = B.lib().tuna_fp8_quantize(x.data_ptr(), DTYPES[x.dtype], rows, cols, ld, which, q.data_ptr(), pitch or 16, scale.data_ptr(),
-                                   _stream(stream, device))
-    if rc:
-        _check(rc, "tuna_fp8_quantize")
-    return q if pitch == out_cols else q[:, :out_cols], scale
-
-
-def _fp8_matrix(q, name):
-    """(operand, pitch, rows, columns) of an e4m3 matrix; copies one whose rows do not start on 16-byte boundaries."""
-    ld = _matrix(q, name, (torch.float8_e4m3fn,))
-    rows, cols = q.shape
-    if rows <= 1:
-        ld = (cols + 15) & ~15   # the pitch of a single row is free
-    if ld & 15 or q.data_ptr() & 15:
-        p = torch.zeros(rows, (cols + 15) & ~15, dtype=torch.uint8, device=q.device)
-        p[:, :cols] = q.view(torch.uint8)
-        q, ld = p, p.shape[1]
-    return q, ld or 16, rows, cols
+    return (_marshal or _fast()).fp8_quantize(x, which, stream)
 
 
 def fp8_matmul(a, a_scale, b, b_scale, *, offsets=None, b_blocks="tiles", out_dtype=torch.bfloat16, stream=None):
@@ -217,36 +185,11 @@ def fp8_matmul(a, a_scale, b, b_scale, *, offsets=None, b_blocks="tiles", out_dt
     ``a`` [m, k] with "rows" scales.  ``b`` [n, k] with "tiles" scales, or "rows" scales
     (``b_blocks="rows"``); or [groups, n, k] with ``offsets`` (int64 [groups + 1]): rows
     offsets[g] .. offsets[g + 1] of ``a`` meet ``b[g]``."""
-    a, lda, m, k = _fp8_matrix(a, "a")
+    if b_blocks != "tiles" and b_blocks != "rows":
+        raise ValueError(f"b_blocks: tiles or rows, got {b_blocks!r}")
     if out_dtype not in FLOATS:
         raise ValueError(f"out_dtype: one of {FLOATS}")
-    blocks = (k + 127) >> 7
-    groups, at = 1, None
-    if offsets is not None:
-        if b.dim() != 3 or not b.is_contiguous() or b_blocks != "tiles":
-            raise ValueError("b: contiguous matrices [groups, n, k] with tile scales go with offsets")
-        groups, n, kb = b.shape
-        at = _dense(offsets, "offsets", torch.int64, (groups + 1,)).data_ptr()
-        b, ldb, _, _ = _fp8_matrix(b.view(groups * n, kb), "b")
-        _dense(b_scale, "b_scale", torch.float32, (groups, (n + 127) >> 7, blocks))
-    else:
-        b, ldb, n, kb = _fp8_matrix(b, "b")
-        if b_blocks == "tiles":
-            _dense(b_scale, "b_scale", torch.float32, ((n + 127) >> 7, blocks))
-        elif b_blocks == "rows":
-            _dense(b_scale, "b_scale", torch.float32, (blocks, n))
-        else:
-            raise ValueError(f"b_blocks: tiles or rows, got {b_blocks!r}")
-    if kb != k:
-        raise ValueError(f"a has {k} columns, b {kb}")
-    _dense(a_scale, "a_scale", torch.float32, (blocks, m))
-    device = a.device
-    out = torch.empty(m, n, dtype=out_dtype, device=device)
-    rc = B.lib().tuna_fp8_matmul(a.data_ptr(), a_scale.data_ptr(), m, lda, b.data_ptr(), b_scale.data_ptr(), LAYOUTS[b_blocks], n, ldb, k,
-                                 groups, at, out.data_ptr(), DTYPES[out_dtype], n or 1, _stream(stream, device))
-    if rc:
-        _check(rc, "tuna_fp8_matmul")
-    return out
+    return (_marshal or _fast()).fp8_matmul(a, a_scale, b, b_scale, offsets, LAYOUTS[b_blocks], DTYPES[out_dtype], stream)
 
 
 def _experts_weights(w13, s13, w2, s2, hidden):
@@ -321,43 +264,18 @@ def few(x, router, k, w13, w2, *, s13=None, s2=None, scoring="softmax", renormal
     ``w13`` [experts, 2, inter, hidden] and ``w2`` [experts, hidden, inter] in bf16, or in
     e4m3 with ``s13`` and ``s2``.  ``ids`` / ``weights``: optional outputs [tokens, k].
     ``workspace``: from :func:`few_workspace`; without one the module keeps one a stream."""
-    ldx = _matrix(x, "x", (torch.bfloat16,))
-    t, d = x.shape
-    if ldx % 8 or x.data_ptr() % 16:
-        x, ldx = x.clone(memory_format=torch.contiguous_format), d
-    e = router.shape[0]
-    _dense(router, "router", torch.bfloat16, (e, d))
-    if w13.dim() != 4:
-        raise ValueError(f"w13: [experts, 2, inter, hidden] is wanted, got {tuple(w13.shape)}")
-    i = w13.shape[2]
-    if w13.dtype == torch.float8_e4m3fn:
-        if s13 is None or s2 is None:
-            raise ValueError("8-bit weights need s13 and s2")
-        if _experts_weights(w13, s13, w2, s2, d) != (e, i):
-            raise ValueError(f"w13: {e} experts are wanted, got {w13.shape[0]}")
-    else:
-        _dense(w13, "w13", torch.bfloat16, (e, 2, i, d))
-        _dense(w2, "w2", torch.bfloat16, (e, d, i))
-    if ids is not None:
-        _dense(ids, "ids", torch.int32, (t, k))
-    if weights is not None:
-        _dense(weights, "weights", torch.float32, (t, k))
-    s = _stream(stream, x.device)
     if workspace is None:
-        kept = _few_spaces.setdefault((x.device.index, s), [])
+        t, d = x.shape
+        e, i = router.shape[0], w13.shape[2]
+        at = _stream(stream, x.device)
+        kept = _few_spaces.setdefault((x.device.index, at), [])
         if not kept or kept[-1].numel() < _few_bytes(t, e, k, d, i)[0]:
             if torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("few: pass a workspace (few_workspace) when the first call of this size is captured")
-            with torch.cuda.stream(torch.cuda.ExternalStream(s, device=x.device)):
+            with torch.cuda.stream(torch.cuda.ExternalStream(at, device=x.device)):
                 kept.append(few_workspace(t, e, k, d, i, x.device))
         workspace = kept[-1]
-    out = torch.empty(t, d, dtype=torch.bfloat16, device=x.device)
-    _check(B.lib().tuna_moe_few(x.data_ptr(), ldx, t, router.data_ptr(), e, k, _scoring(scoring), int(renormalize), scale, d, i,
-                                DTYPES[w13.dtype], w13.data_ptr(), None if s13 is None else s13.data_ptr(), w2.data_ptr(),
-                                None if s2 is None else s2.data_ptr(), out.data_ptr(), d, None if ids is None else ids.data_ptr(),
-                                None if weights is None else weights.data_ptr(), workspace.data_ptr(), workspace.numel(), s),
-           "tuna_moe_few")
-    return out
+    return (_marshal or _fast()).few(x, router, k, w13, w2, s13, s2, _scoring(scoring), renormalize, scale, ids, weights, workspace, stream)
 
 
 def device_status() -> int:

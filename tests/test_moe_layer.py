@@ -232,3 +232,25 @@ def test_layer_refusals():
     assert rows(256, 64, 4, 8, None, 64, 64, 256, 256, 256, 256, 256, 64, 256, 1 << 20, None) == -1     # no offsets
     assert rows(256, 64, 4, 8, 256, 64, 64, 256, 256, 256, 256, 256, 64, 256, 8, None) == -6
     assert rows(None, 64, 0, 8, None, 64, 64, None, None, None, None, None, 64, None, 0, None) == 0
+
+
+def test_marshalling_is_built_and_refuses_on_the_host():
+    """The C++ marshalling loads, binds to the library and raises the Python errors (no GPU needed)."""
+    import subprocess
+    import sys
+    from paper_2411_02581_b200 import moe
+    build_mod.build()
+    fast = moe._fast()
+    with pytest.raises(ValueError, match="CUDA tensor"):
+        moe.fp8_quantize(torch.zeros(4, 4))
+    with pytest.raises(ValueError, match="layout"):
+        moe.fp8_quantize(torch.zeros(4, 4), "diagonal")
+    with pytest.raises(ValueError, match="a tensor is wanted"):
+        moe.fp8_matmul(None, None, None, None)
+    with pytest.raises(ValueError, match="b_blocks"):
+        moe.fp8_matmul(None, None, None, None, b_blocks="columns")
+    with pytest.raises(TypeError, match="7 arguments"):
+        fast.route(1)
+    missing = "import os; from paper_2411_02581_b200 import build, moe; build.TORCH_PATH = os.devnull + '/none'; moe._fast()"
+    r = subprocess.run([sys.executable, "-c", missing], capture_output=True, text=True, cwd=build_mod.ROOT)
+    assert r.returncode != 0 and "is missing: build it" in r.stderr
