@@ -102,17 +102,33 @@ __device__ __forceinline__ void place_entries(const OrderArgs &o, char *smem, in
   const int64_t a = first_entry + min(n, warp * per), b = first_entry + min(n, (warp + 1) * per);
   uint32_t *mine = table + (size_t)warp * o.experts;
   for (int e = threadIdx.x; e < (THREADS / 32) * o.experts; e += THREADS) table[e] = 0;
+  // A warp's entries, kHeld rounds of 32 at a time: loaded together, and once where they are no more.
+  constexpr int kHeld = 8;
+  int held[kHeld];
+  auto fetch = [&](int64_t from) {
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r) {
+      const int64_t i = from + r * 32 + lane;
+      const int id = i < b ? o.ids[i] : -1;
+      held[r] = id >= 0 && id < o.experts ? id : -1;
+    }
+  };
+  fetch(a);
   __syncthreads();
-  for (int64_t i = a; i < b; i += 32) {
-    const int id = i + lane < b ? o.ids[i + lane] : -1;
-    const bool there = id >= 0 && id < o.experts;
-    const uint32_t peers = __match_any_sync(~0u, there ? id : -1);
-    if (there && lane == __ffs(peers) - 1) mine[id] += __popc(peers);
-    __syncwarp();
+  for (int64_t i = a; i < b; i += kHeld * 32) {
+    if (i > a) fetch(i);
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r) {
+      if (i + r * 32 >= b) break;
+      const uint32_t peers = __match_any_sync(~0u, held[r]);
+      if (held[r] >= 0 && lane == __ffs(peers) - 1) mine[held[r]] += __popc(peers);
+      __syncwarp();
+    }
   }
   __syncthreads();
   for (int e = threadIdx.x; e < o.experts; e += THREADS) {
     uint32_t sum = 0;
+#pragma unroll 8
     for (int w = 0; w < (THREADS / 32); ++w) {
       const uint32_t c = table[(size_t)w * o.experts + e];
       table[(size_t)w * o.experts + e] = sum;
@@ -120,21 +136,26 @@ __device__ __forceinline__ void place_entries(const OrderArgs &o, char *smem, in
     }
   }
   __syncthreads();
-  for (int64_t i = a; i < b; i += 32) {
-    const int id = i + lane < b ? o.ids[i + lane] : -1;
-    const bool there = id >= 0 && id < o.experts;
-    const uint32_t peers = __match_any_sync(~0u, there ? id : -1);
-    const int before = __popc(peers & ((1u << lane) - 1));
-    if (there) {
-      const int64_t at = base[id] + mine[id] + before;
-      o.pos[i + lane] = at;
-      o.rows[at] = (uint32_t)(i + lane) / (uint32_t)o.k;  // (entries of one call stay below 2^31)
-    } else if (i + lane < b) {
-      o.pos[i + lane] = -1;
+  if (b - a > kHeld * 32) fetch(a);
+  for (int64_t i = a; i < b; i += kHeld * 32) {
+    if (i > a) fetch(i);
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r) {
+      const int64_t entry = i + r * 32 + lane;
+      if (i + r * 32 >= b) break;
+      const int id = held[r];
+      const uint32_t peers = __match_any_sync(~0u, id);
+      if (id >= 0) {
+        const int64_t at = base[id] + mine[id] + __popc(peers & ((1u << lane) - 1));
+        o.pos[entry] = at;
+        o.rows[at] = (uint32_t)entry / (uint32_t)o.k;  // (entries of one call stay below 2^31)
+      } else if (entry < b) {
+        o.pos[entry] = -1;
+      }
+      __syncwarp();
+      if (id >= 0 && lane == __ffs(peers) - 1) mine[id] += __popc(peers);
+      __syncwarp();
     }
-    __syncwarp();
-    if (there && lane == __ffs(peers) - 1) mine[id] += __popc(peers);
-    __syncwarp();
   }
 }
 
@@ -192,7 +213,7 @@ __global__ void __launch_bounds__(kOrderThreads) tuna_order_kernel(OrderArgs o) 
   {
     const int64_t before = rank * chunks * E;
     const uint4 *h = reinterpret_cast<const uint4 *>(o.hist);
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t i = threadIdx.x; i < before / 8; i += kOrderThreads) {
       const uint4 v = h[i];
       earlier += (v.x & 0xffffu) + (v.x >> 16) + (v.y & 0xffffu) + (v.y >> 16) + (v.z & 0xffffu) + (v.z >> 16) + (v.w & 0xffffu) + (v.w >> 16);
