@@ -191,6 +191,7 @@ struct TileArgs {
 
 constexpr int kSumWarps = 16;   // promotion: four quarters of the columns x 128 rows
 constexpr int kGemmThreads = 128 + kSumWarps * 32;
+constexpr int kSumPitch = 132;  // floats: rows of sums that a cluster joins, on 16-byte boundaries and four banks apart
 constexpr int kCopyRegs = 64, kSumRegs = 104;  // registers of a thread: copying and issuing warps, promotion
 constexpr int kMaxGroups = TUNA_MOE_MAX_EXPERTS;
 
@@ -224,7 +225,11 @@ __device__ __forceinline__ void walk_to(Walk &w, int64_t t, const TileArgs &a, c
   w.n0 = n * bn;
 }
 
-template <int BN, bool SWIGLU, bool B_ROWS, typename TO>
+//
+// With SPLIT a cluster of 2, 4 or 8 blocks shares one tile: each adds up a part of k, leaves its sums in
+// its shared memory, and adds up the parts of some of the rows from all of them, in order of k.  For few
+// rows there are fewer tiles than multiprocessors otherwise.
+template <int BN, bool SWIGLU, bool B_ROWS, bool SPLIT, typename TO>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     tuna_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                         const __grid_constant__ CUtensorMap map_out, const TileArgs a) {
@@ -278,7 +283,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_at;
   const int64_t tiles = (int64_t)tile_base[a.p.groups] * a.n_tiles;
-  const int blocks = a.blocks;
+  const int parts = SPLIT ? (int)cluster_size() : 1, part = SPLIT ? (int)cluster_rank() : 0;
+  auto first = [&] { return (int64_t)(SPLIT ? blockIdx.x / parts : blockIdx.x); };
+  auto step = [&] { return SPLIT ? gridDim.x / parts : gridDim.x; };
+  // this block's part of k
+  const int kb_first = SPLIT ? (int)((int64_t)a.blocks * part / parts) : 0, blocks = SPLIT ? (int)((int64_t)a.blocks * (part + 1) / parts) - kb_first : a.blocks;
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCopyRegs));
@@ -288,21 +297,22 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       int64_t issued = 0;
       Walk w;
       bool ok = true;
-      for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+      for (int64_t t = first(); ok && t < tiles; t += step()) {
         walk_to(w, t, a, tile_base, SWIGLU ? BN / 2 : BN);
         for (int kb = 0; kb < blocks; ++kb) {
           if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, given_up))) break;
           const uint32_t at = smem_u32(smem) + stage * S::kStageBytes, bar = full + 8 * stage;
           mbar_expect(bar, S::kStageBytes);
-          tma_load_2d(at, &map_a, kb * 128, (int)w.row, bar);
+          const int col = (kb_first + kb) * 128;
+          tma_load_2d(at, &map_a, col, (int)w.row, bar);
           if (SWIGLU && a.one_copy) {
-            tma_load_5d(at + 128 * 128, &map_b, kb * 128, 0, 0, w.n0 / 32, w.g, bar);
+            tma_load_5d(at + 128 * 128, &map_b, col, 0, 0, w.n0 / 32, w.g, bar);
           } else if (SWIGLU) {
 #pragma unroll
             for (int q = 0; q < 8; ++q)
-              tma_load_3d(at + 128 * 128 + q * 32 * 128, &map_b, kb * 128, w.n0 + (q >> 1) * 32, w.g * 2 + (q & 1), bar);
+              tma_load_3d(at + 128 * 128 + q * 32 * 128, &map_b, col, w.n0 + (q >> 1) * 32, w.g * 2 + (q & 1), bar);
           } else {
-            tma_load_3d(at + 128 * 128, &map_b, kb * 128, w.n0, w.g, bar);
+            tma_load_3d(at + 128 * 128, &map_b, col, w.n0, w.g, bar);
           }
           ++issued;
           if (++stage == S::kStages) stage = 0, phase ^= 1;
@@ -318,7 +328,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);  // f32 sums of e4m3 products
       int stage = 0, phase = 0, buf = 0, buf_phase = 0;
       bool ok = true;
-      for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+      for (int64_t t = first(); ok && t < tiles; t += step()) {
         for (int kb = 0; kb < blocks; ++kb) {
           if (!(ok = mbar_wait(full + 8 * stage, phase, given_up) && mbar_wait(freed + 8 * buf, buf_phase ^ 1, given_up))) break;
           tc_fence_after();
@@ -346,7 +356,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       Walk w;
       const float *sa0 = nullptr, *sa1 = nullptr, *sb0 = nullptr, *sb1 = nullptr;
       // the blocks that are fetched next: one run of kAhead ahead of those handed out, across tiles too
-      int64_t ahead_t = blockIdx.x;
+      int64_t ahead_t = first();
       int ahead_kb = 0;
       float next[kAhead][kVals];
       auto fetch = [&]() {
@@ -355,16 +365,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           walk_to(w, ahead_t, a, tile_base, SWIGLU ? BN / 2 : BN);
           sa0 = a.p.sa + min(w.row + i, w.end - 1), sa1 = a.p.sa + min(w.row + i + 64, w.end - 1);
           if (SWIGLU) {
-            sb0 = a.p.sb + ((int64_t)(w.g * 2) * tiles_n + w.n0 / 128) * blocks;
-            sb1 = sb0 + (int64_t)tiles_n * blocks;
+            sb0 = a.p.sb + ((int64_t)(w.g * 2) * tiles_n + w.n0 / 128) * a.blocks;
+            sb1 = sb0 + (int64_t)tiles_n * a.blocks;
           } else if (!B_ROWS) {
-            sb0 = a.p.sb + ((int64_t)w.g * tiles_n + w.n0 / 128) * blocks;
-            sb1 = w.n0 / 128 + 1 < tiles_n ? sb0 + blocks : sb0;
+            sb0 = a.p.sb + ((int64_t)w.g * tiles_n + w.n0 / 128) * a.blocks;
+            sb1 = w.n0 / 128 + 1 < tiles_n ? sb0 + a.blocks : sb0;
           }
         }
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-          const int kb = min(ahead_kb + j, blocks - 1);
+          const int kb = kb_first + min(ahead_kb + j, blocks - 1);
           next[j][0] = __ldg(sa0 + (int64_t)kb * a.p.m), next[j][1] = __ldg(sa1 + (int64_t)kb * a.p.m);
           if (B_ROWS) {
 #pragma unroll
@@ -374,10 +384,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           }
         }
         ahead_kb += kAhead;
-        if (ahead_kb >= blocks) ahead_kb = 0, ahead_t += gridDim.x;
+        if (ahead_kb >= blocks) ahead_kb = 0, ahead_t += step();
       };
       fetch();
-      for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+      for (int64_t t = first(); ok && t < tiles; t += step()) {
         for (int kb0 = 0; ok && kb0 < blocks; kb0 += kAhead) {
           float now[kAhead][kVals];
 #pragma unroll
@@ -416,7 +426,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     int buf = 0, buf_phase = 0;
     bool ok = true;
     Walk w;
-    for (int64_t t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+    for (int64_t t = first(); ok && t < tiles; t += step()) {
       walk_to(w, t, a, tile_base, SWIGLU ? BN / 2 : BN);
       const int64_t row = w.row + row_in;
       const bool there = row < w.end;
@@ -465,7 +475,18 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         }
         if (++buf == 2) buf = 0, buf_phase ^= 1;
       }
-      if constexpr (!SWIGLU) {
+      if constexpr (SPLIT) {
+        // the sums to shared memory, where the stages were: every step that read them is done
+        float *red = (float *)smem + row_in * kSumPitch + quarter * S::kCols;
+        if (ok && there) {
+#pragma unroll
+          for (int i = 0; i < S::kCols; i += 4) {
+            float4 v;
+            unpair(acc[i / 2], v.x, v.y), unpair(acc[i / 2 + 1], v.z, v.w);
+            *reinterpret_cast<float4 *>(red + i) = v;
+          }
+        }
+      } else if constexpr (!SWIGLU) {
         if (!ok) break;
         // 32 whole rows of bf16 go to shared memory and from there by a tensor copy, which runs on
         // during the next tile: stored from registers, all blocks at once, they cost 3 us a tile.
@@ -546,6 +567,27 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     if (S::kOutBytes && lane == 0) tma_store_done();
   }
   __syncwarp();
+  if constexpr (SPLIT) {
+    cluster_meet();
+    if (first() < tiles && !*given_up) {
+      Walk w;
+      walk_to(w, first(), a, tile_base, BN);
+      const int rows = (int)min((int64_t)128, w.end - w.row);
+      for (int i = threadIdx.x; i < (rows - part + parts - 1) / parts * (BN / 4); i += kGemmThreads) {
+        const int r = part + i / (BN / 4) * parts, c = i % (BN / 4) * 4;
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int q = 0; q < parts; ++q) {
+          const float4 x = load_from_block(smem_u32(smem) + (r * kSumPitch + c) * 4, q);
+          v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+        }
+        TO *out = (TO *)a.p.out + (w.row + r) * a.p.ldo + w.n0 + c;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (w.n0 + c + j < a.p.n) out[j] = from_f32<TO>(v[j]);
+      }
+    }
+    cluster_meet();  // no block leaves while its sums are read
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -555,8 +597,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 
 // ---- host ------------------------------------------------------------------------------------
 
-template <int BN, bool SWIGLU, bool B_ROWS, typename TO>
-int run_tiles(const ProductArgs &p, cudaStream_t st) {
+template <int BN, bool SWIGLU, bool B_ROWS, typename TO, bool SPLIT = false>
+int run_tiles(const ProductArgs &p, cudaStream_t st, int parts = 1) {
   using S = Shape<BN, !SWIGLU && sizeof(TO) == 2>;
   TileArgs a = {};
   a.p = p;
@@ -580,7 +622,7 @@ int run_tiles(const ProductArgs &p, cudaStream_t st) {
   if (a.store_tiles)
     if (const int rc = make_map(&mo, 2, p.out, p.n, p.m, 1, p.ldo, 32, true)) return rc;
   static bool set[64] = {}, fits = false;
-  auto kernel = tuna_product_kernel<BN, SWIGLU, B_ROWS, TO>;
+  auto kernel = tuna_product_kernel<BN, SWIGLU, B_ROWS, SPLIT, TO>;
   if (!__atomic_load_n(&fits, __ATOMIC_ACQUIRE)) {
     // the warps' shares of registers (setmaxnreg) come out of what the block is launched with
     cudaFuncAttributes at;
@@ -590,6 +632,7 @@ int run_tiles(const ProductArgs &p, cudaStream_t st) {
   }
   if (const int rc = allow_smem(kernel, S::kSmem, set)) return rc;
   const int64_t most = (ceil_div(p.m, 128) + (p.offsets ? p.groups : 0)) * a.n_tiles;
+  if (SPLIT) return launch_cluster(kernel, dim3((unsigned)(most * parts)), parts, kGemmThreads, S::kSmem, st, false, ma, mb, mo, a);
   return launch(kernel, dim3((unsigned)std::min<int64_t>(most, sm_count())), kGemmThreads, S::kSmem, st, false, ma, mb, mo, a);
 }
 
@@ -657,6 +700,17 @@ int launch_product(const ProductArgs &p, cudaStream_t st) {
   if (wide >= sm_count()) {
     if (p.out_f32) return run_tiles<256, false, false, float>(p, st);
     return run_tiles<256, false, false, __nv_bfloat16>(p, st);
+  }
+  if (!p.offsets) {
+    // few tiles: a cluster shares each, as long as every block keeps two blocks of k or more.  (128 blocks
+    // at most: more clusters of 8 are not resident together.)  One row of 4096 x 4096: 15.3 us without.
+    const int64_t tiles = ceil_div(p.m, 128) * ceil_div(p.n, 128);
+    int parts = 8;
+    while (parts > 1 && (tiles * parts > 128 || ceil_div(p.k, 128) < 2 * parts)) parts /= 2;
+    if (parts > 1) {
+      if (p.out_f32) return run_tiles<128, false, false, float, true>(p, st, parts);
+      return run_tiles<128, false, false, __nv_bfloat16, true>(p, st, parts);
+    }
   }
   if (p.out_f32) return run_tiles<128, false, false, float>(p, st);
   return run_tiles<128, false, false, __nv_bfloat16>(p, st);

@@ -28,15 +28,15 @@ int sm_count();
 int *error_word();  // device address of the flag that a bounded wait raises (nullptr: no device)
 
 // Launches `kernel` so that it may be scheduled while the stream's previous kernel drains:
-// every kernel of these operators begins with wait_previous().
+// every kernel of these operators begins with wait_previous().  `cluster`: blocks of a cluster.
 template <typename... P, typename... A>
-inline int launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, bool cooperative, A... args) {
+inline int launch_cluster(void (*kernel)(P...), dim3 grid, int cluster, int threads, size_t smem, cudaStream_t st, bool cooperative, A... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute at[1];
+  cudaLaunchAttribute at[2];
   if (cooperative) {
     at[0].id = cudaLaunchAttributeCooperative;
     at[0].val.cooperative = 1;
@@ -44,9 +44,15 @@ inline int launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cud
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
   }
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return note_cuda(cudaLaunchKernelEx(&cfg, kernel, P(args)...));
+}
+template <typename... P, typename... A>
+inline int launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, bool cooperative, A... args) {
+  return launch_cluster(kernel, grid, 1, threads, smem, st, cooperative, args...);
 }
 
 // Dynamic shared memory above the default needs the kernel's leave, once a device (`set`: one
@@ -291,6 +297,29 @@ __device__ __forceinline__ bool elect_one() {
   uint32_t r;
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(r));
   return r != 0;
+}
+
+// ---- clusters ---------------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+// All threads of the cluster's blocks meet (every thread comes here, whatever it gave up before).
+__device__ __forceinline__ void cluster_meet() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float4 load_from_block(uint32_t addr, uint32_t rank) {
+  float4 v;
+  asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %4, %5;\n ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n}"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr), "r"(rank) : "memory");
+  return v;
 }
 
 // ---- barriers in shared memory ---------------------------------------------------------
