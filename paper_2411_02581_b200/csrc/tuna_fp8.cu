@@ -195,13 +195,14 @@ constexpr int kSumPitch = 132;  // floats: rows of sums that a cluster joins, on
 constexpr int kCopyRegs = 64, kSumRegs = 104;  // registers of a thread: copying and issuing warps, promotion
 constexpr int kMaxGroups = TUNA_MOE_MAX_EXPERTS;
 
-// STORES: bf16 results, which leave by tensor copies
+// STORES: bf16 results, which leave through shared memory
 template <int BN, bool STORES>
 struct Shape {
-  static constexpr int kStages = BN == 256 ? (STORES ? 3 : 4) : 6;
+  static constexpr int kStages = BN == 256 ? (STORES ? 3 : 4) : (STORES ? 5 : 6);
   static constexpr int kStageBytes = 128 * 128 + BN * 128;
   static constexpr int kCols = BN / 4;  // accumulator columns of a thread
-  static constexpr int kOutBytes = BN == 256 && STORES ? kSumWarps * 4096 : 0;  // each promotion warp's 32 x 64 results, on their way out
+  static constexpr int kRowBytes = BN / 2;  // of bf16 results: a promotion warp's columns
+  static constexpr int kOutBytes = STORES ? kSumWarps * 32 * kRowBytes : 0;  // each promotion warp's 32 rows of them, on their way out
   // stages, results, then the factors beside the two accumulators, the rows' largest magnitudes, the groups'
   // tile offsets, barriers and flags
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kOutBytes + 2 * 384 * 4 + 512 * 4 + (kMaxGroups + 8) * 4 + 256;
@@ -233,7 +234,7 @@ template <int BN, bool SWIGLU, bool B_ROWS, bool SPLIT, typename TO>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     tuna_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                         const __grid_constant__ CUtensorMap map_out, const TileArgs a) {
-  using S = Shape<BN, !SWIGLU && sizeof(TO) == 2>;
+  using S = Shape<BN, !SWIGLU && !SPLIT && sizeof(TO) == 2>;
   extern __shared__ char smem_raw[];
   char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   // beside each accumulator: [2][128] factors of the rows for either half of the columns, or with
@@ -431,6 +432,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       const int64_t row = w.row + row_in;
       const bool there = row < w.end;
       const int n0 = w.n0;
+      const int64_t end = w.end;
       uint64_t acc[S::kCols / 2];
 #pragma unroll
       for (int i = 0; i < S::kCols / 2; ++i) acc[i] = 0;
@@ -488,26 +490,52 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         }
       } else if constexpr (!SWIGLU) {
         if (!ok) break;
-        // 32 whole rows of bf16 go to shared memory and from there by a tensor copy, which runs on
-        // during the next tile: stored from registers, all blocks at once, they cost 3 us a tile.
-        // Rows that a group's end cuts, and results that a tensor copy cannot reach, are stored here.
-        const bool whole = sizeof(TO) == 2 && S::kOutBytes && a.store_tiles && w.row + (warp & 3) * 32 + 31 < w.end;
-        if (whole) {
-          const uint32_t to = smem_u32(smem) + S::kStages * S::kStageBytes + (warp - 4) * 4096;
+        if constexpr (S::kOutBytes != 0) {
+          // bf16 results go to shared memory, in 16-byte pieces swizzled by row.  32 whole rows leave from
+          // there by a tensor copy, which runs on during the next tile (stored from registers, all blocks
+          // at once, they cost 3 us a tile); rows that a group's end cuts, or that a tensor copy cannot
+          // reach (a pitch that is no multiple of 16 bytes), leave in whole rows as the warp reads them back.
+          constexpr int kPieces = S::kRowBytes / 16;
+          auto place = [](int r, int piece) { return (uint32_t)(r * S::kRowBytes + (kPieces == 8 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3)) * 16); };
+          const uint32_t to = smem_u32(smem) + S::kStages * S::kStageBytes + (warp - 4) * 32 * S::kRowBytes;
+          const int64_t row0 = row - lane;
+          const int valid = (int)max((int64_t)0, min((int64_t)32, end - row0)), c0 = n0 + quarter * S::kCols;
           if (lane == 0) tma_store_read();
           __syncwarp();
 #pragma unroll
-          for (int i = 0; i < S::kCols / 8; ++i) {
+          for (int i = 0; i < kPieces; ++i) {
             float v[8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) unpair(acc[i * 4 + j], v[2 * j], v[2 * j + 1]);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + lane * 128 + ((i ^ (lane & 7)) * 16)), "r"(pack_bf16(v[0], v[1])),
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + place(lane, i)), "r"(pack_bf16(v[0], v[1])),
                          "r"(pack_bf16(v[2], v[3])), "r"(pack_bf16(v[4], v[5])), "r"(pack_bf16(v[6], v[7]))
                          : "memory");
           }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          if (a.store_tiles && valid == 32) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0 && c0 < a.p.n) tma_store_2d(&map_out, c0, (int)row0, to);
+          } else {
+            __syncwarp();
+            __nv_bfloat16 *out = (__nv_bfloat16 *)a.p.out + row0 * a.p.ldo + c0;
+            if (a.store_tiles && c0 + S::kCols <= a.p.n) {
+              for (int i = lane; i < valid * kPieces; i += 32) {
+                const int r = i / kPieces, piece = i % kPieces;
+                uint4 u;
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(to + place(r, piece)) : "memory");
+                *reinterpret_cast<uint4 *>(out + r * a.p.ldo + piece * 8) = u;
+              }
+            } else {
+              const int cols = min(S::kCols, a.p.n - c0);
+              for (int r = 0; r < valid; ++r)
+                for (int c = lane; c < cols; c += 32) {
+                  uint16_t u;
+                  asm volatile("ld.shared.b16 %0, [%1];" : "=h"(u) : "r"(to + place(r, c >> 3) + (c & 7) * 2) : "memory");
+                  reinterpret_cast<uint16_t *>(out)[r * a.p.ldo + c] = u;
+                }
+            }
+          }
           __syncwarp();
-          if (lane == 0 && n0 + quarter * S::kCols < a.p.n) tma_store_2d(&map_out, n0 + quarter * S::kCols, (int)(row - lane), to);
         } else if (there) {
           TO *out = (TO *)a.p.out + row * a.p.ldo;
           const int c0 = n0 + quarter * S::kCols;
@@ -597,9 +625,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 
 // ---- host ------------------------------------------------------------------------------------
 
+}  // namespace
+static int make_out_map(CUtensorMap *map, void *p, int64_t cols, int64_t rows, int64_t ld, int row_bytes);
+namespace {
+
 template <int BN, bool SWIGLU, bool B_ROWS, typename TO, bool SPLIT = false>
 int run_tiles(const ProductArgs &p, cudaStream_t st, int parts = 1) {
-  using S = Shape<BN, !SWIGLU && sizeof(TO) == 2>;
+  using S = Shape<BN, !SWIGLU && !SPLIT && sizeof(TO) == 2>;
   TileArgs a = {};
   a.p = p;
   a.blocks = (int)ceil_div(p.k, 128);
@@ -620,7 +652,7 @@ int run_tiles(const ProductArgs &p, cudaStream_t st, int parts = 1) {
   mo = ma;
   a.store_tiles = S::kOutBytes && !SWIGLU && !p.out_f32 && aligned(p.out, 16) && p.ldo % 8 == 0;
   if (a.store_tiles)
-    if (const int rc = make_map(&mo, 2, p.out, p.n, p.m, 1, p.ldo, 32, true)) return rc;
+    if (const int rc = make_out_map(&mo, p.out, p.n, p.m, p.ldo, S::kRowBytes)) return rc;
   static bool set[64] = {}, fits = false;
   auto kernel = tuna_product_kernel<BN, SWIGLU, B_ROWS, SPLIT, TO>;
   if (!__atomic_load_n(&fits, __ATOMIC_ACQUIRE)) {
@@ -675,6 +707,19 @@ int make_map(CUtensorMap *map, int rank, const void *p, int64_t k, int64_t rows,
   const cuuint32_t boxes[3] = {(cuuint32_t)(128 / size), (cuuint32_t)box, 1}, ones[3] = {1, 1, 1};
   const CUresult r = f(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, (cuuint32_t)rank, const_cast<void *>(p), dims, strides, boxes, ones,
                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? TUNA_OK : note_cuda(cudaErrorInvalidValue);
+}
+
+// bf16 results: boxes of `row_bytes` (128 or 64, swizzled alike) x 32 rows.
+static int make_out_map(CUtensorMap *map, void *p, int64_t cols, int64_t rows, int64_t ld, int row_bytes) {
+  EncodeTiled f = encoder();
+  if (!f) return TUNA_ERR_CUDA;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)(ld * 2)};
+  const cuuint32_t boxes[2] = {(cuuint32_t)(row_bytes / 2), 32}, ones[2] = {1, 1};
+  const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p, dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                       row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? TUNA_OK : note_cuda(cudaErrorInvalidValue);
 }

@@ -97,7 +97,7 @@ def test_quantize_keeps_what_is_not_finite():
 
 
 PRODUCTS = [(1, 1, 1), (1, 128, 128), (1, 4096, 512), (2, 100, 300), (17, 640, 2064), (64, 256, 128), (65, 1000, 1040), (128, 256, 4096),
-            (129, 257, 130), (300, 2000, 272), (1000, 96, 1024), (2500, 2304, 256), (0, 64, 64), (5, 7, 0)]
+            (129, 257, 130), (300, 2000, 272), (1000, 96, 1024), (2500, 2304, 256), (20000, 517, 144), (0, 64, 64), (5, 7, 0)]
 
 
 @pytest.mark.gpu
