@@ -443,11 +443,11 @@ __global__ void __launch_bounds__(kThreads, 1)
               // below 9 tokens, the pieces p and q of a block are 8 columns each, else 16
               uint32_t v[2][32];
               if (count > 8) {
-                tmem_load32(from + buf * kBufCols, v[0]);
-                tmem_load32(from + buf * kBufCols + 32, v[1]);
+                tmem_load(from + buf * kBufCols, v[0]);
+                tmem_load(from + buf * kBufCols + 32, v[1]);
               } else {
-                tmem_load16(from + buf * kBufCols, reinterpret_cast<uint32_t(&)[16]>(v[0]));
-                tmem_load16(from + buf * kBufCols + 32, reinterpret_cast<uint32_t(&)[16]>(v[1]));
+                tmem_load(from + buf * kBufCols, reinterpret_cast<uint32_t(&)[16]>(v[0]));
+                tmem_load(from + buf * kBufCols + 32, reinterpret_cast<uint32_t(&)[16]>(v[1]));
               }
               tmem_wait(v[0]);
               tmem_wait(v[1]);
@@ -485,7 +485,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (ok) {
               tc_fence_after();
               uint32_t v[16];
-              tmem_load16(from + buf * kBufCols, v);
+              tmem_load(from + buf * kBufCols, v);
               tmem_wait(v);
               tc_fence_before();
               __syncwarp();

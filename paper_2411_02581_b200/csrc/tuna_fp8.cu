@@ -440,34 +440,35 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         ok = __all_sync(~0u, mbar_wait(done + 8 * buf, buf_phase, given_up));  // (and the warp is whole for the loads)
         if (!ok) break;
         tc_fence_after();
-        uint32_t v[2][16];
-        tmem_load16(from + buf * BN, v[0]);
+        constexpr int kRun = B_ROWS ? 8 : 16;  // columns at a time: with B_ROWS the factors need registers too
+        uint32_t v[2][kRun];
+        tmem_load(from + buf * BN, v[0]);
         float s0, s1 = 0.0f;
         asm volatile("ld.shared.f32 %0, [%1];" : "=f"(s0) : "r"(factor + buf * 384 * 4) : "memory");
         if (SWIGLU) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(s1) : "r"(factor + buf * 384 * 4 + 512) : "memory");
         const uint64_t p0 = pair(s0, s0), p1 = pair(s1, s1);
         const float *cs = factors + buf * 384 + 128 + quarter * S::kCols;
 #pragma unroll
-        for (int c = 0; c < S::kCols / 16; ++c) {
+        for (int c = 0; c < S::kCols / kRun; ++c) {
           tmem_wait(v[c & 1]);
-          if (c + 1 < S::kCols / 16) {
-            tmem_load16(from + buf * BN + (c + 1) * 16, v[(c + 1) & 1]);
+          if (c + 1 < S::kCols / kRun) {
+            tmem_load(from + buf * BN + (c + 1) * kRun, v[(c + 1) & 1]);
           } else if (!B_ROWS) {  // everything is in registers, the factors too: the accumulator may be filled again
             asm volatile("" ::"f"(s0), "f"(s1));
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(freed + 8 * buf);
           }
-          uint32_t(&x)[16] = v[c & 1];
+          uint32_t(&x)[kRun] = v[c & 1];
 #pragma unroll
-          for (int i = 0; i < 8; i += 2) {
-            uint64_t f = SWIGLU && c >= 2 ? p1 : p0, g = f;
+          for (int i = 0; i < kRun / 2; i += 2) {
+            uint64_t f = SWIGLU && c * kRun >= 32 ? p1 : p0, g = f;
             if (B_ROWS) {
-              const float4 q = *reinterpret_cast<const float4 *>(cs + c * 16 + i * 2);
+              const float4 q = *reinterpret_cast<const float4 *>(cs + c * kRun + i * 2);
               f = mul2(p0, pair(q.x, q.y)), g = mul2(p0, pair(q.z, q.w));
             }
-            acc[c * 8 + i] = fma2(pair(x[2 * i], x[2 * i + 1]), f, acc[c * 8 + i]);
-            acc[c * 8 + i + 1] = fma2(pair(x[2 * i + 2], x[2 * i + 3]), g, acc[c * 8 + i + 1]);
+            acc[c * (kRun / 2) + i] = fma2(pair(x[2 * i], x[2 * i + 1]), f, acc[c * (kRun / 2) + i]);
+            acc[c * (kRun / 2) + i + 1] = fma2(pair(x[2 * i + 2], x[2 * i + 3]), g, acc[c * (kRun / 2) + i + 1]);
           }
         }
         if (B_ROWS) {  // (the column scales have been read only now)
