@@ -330,7 +330,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int cols = up ? D : I, rows = up ? 2 * I : D;
       Product p;
       p.tiles = (rows + 127) / 128, p.blocks = (cols + kBlock - 1) / kBlock, p.segment = a.segment[phase], p.segments = a.segments[phase];
-      const int64_t units = (int64_t)groups * p.segments * p.tiles;
+      // (at most 640 groups x 8 segments x 128 tiles: the products below fit 32 bits)
+      const uint32_t units = (uint32_t)groups * p.segments * p.tiles;
       p.unit0 = (int)(units * blockIdx.x / gridDim.x), p.unit1 = (int)(units * (blockIdx.x + 1) / gridDim.x);
       if (warp == 0) {
         // -- weights
@@ -516,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int first = l.group[w.g].first, count = l.group[w.g].count, N = FP8 && count > 8 ? 32 : 16;
           ok = __all_sync(~0u, mbar_wait(smem_u32(l.used + op), op_phase ^ 1, &l.given_up));
           if (!ok) break;
-          // A warp takes 128 columns of a token at a time, a lane four of them, two such pieces in flight.
+          // A warp takes 128 columns of a token at a time, a lane four of them, several such pieces in flight.
           // The loads of a piece are issued together: one after the other, the four segments' sums of a
           // nine-token group took 80000 cycles to lay out, and the grid waited for that block.
           const int spans = (w.blocks * kBlock + 127) / 128, pieces = spans * count;
@@ -524,38 +525,41 @@ __global__ void __launch_bounds__(kThreads, 1)
             int t, span;
             float v[4];
           };
-          auto load = [&](Piece &x, int i) {
+          auto aim = [&](Piece &x, int i) {  // the piece's place; its columns (cols is a multiple of 16: all four or none)
             x.span = i / count, x.t = i - x.span * count;
-            const int entry = l.entry[first + x.t], col = w.s * p.segment * kBlock + x.span * 128 + lane * 4;
+            return w.s * p.segment * kBlock + x.span * 128 + lane * 4;
+          };
+          auto load_x = [&](int i) {
+            Piece x;
+            const int col = aim(x, i);
+            if (i >= pieces || col >= cols) return make_uint2(0, 0);
+            return __ldg((const uint2 *)(a.x + (l.entry[first + x.t] / K) * a.ldx + col));
+          };
+          auto load_h = [&](Piece &x, int i) {
+            const int col = aim(x, i);
 #pragma unroll
             for (int j = 0; j < 4; ++j) x.v[j] = 0.0f;
-            if (i >= pieces || col >= cols) return;  // (cols is a multiple of 16)
-            if (up) {
-              const uint2 r = __ldg((const uint2 *)(a.x + (entry / K) * a.ldx + col));
-              x.v[0] = __uint_as_float(r.x << 16), x.v[1] = __uint_as_float(r.x & 0xffff0000u);
-              x.v[2] = __uint_as_float(r.y << 16), x.v[3] = __uint_as_float(r.y & 0xffff0000u);
-            } else {
-              float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-              const float *g0 = a.up + (int64_t)entry * 2 * I + col;
-              const int64_t step = (int64_t)n * 2 * I;
-              const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-              for (int s0 = 0; s0 < a.segments[0]; s0 += 4) {
-                float4 gs[4], us[4];
+            if (i >= pieces || col >= cols) return;
+            float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            const float *g0 = a.up + (int64_t)l.entry[first + x.t] * 2 * I + col;
+            const int64_t step = (int64_t)n * 2 * I;
+            const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int s0 = 0; s0 < a.segments[0]; s0 += 4) {
+              float4 gs[4], us[4];
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                  const bool there = s0 + s < a.segments[0];
-                  gs[s] = there ? __ldcg((const float4 *)(g0 + (s0 + s) * step)) : zero;
-                  us[s] = there ? __ldcg((const float4 *)(g0 + (s0 + s) * step + I)) : zero;
-                }
-#pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                  x.v[0] += gs[s].x, x.v[1] += gs[s].y, x.v[2] += gs[s].z, x.v[3] += gs[s].w;
-                  u[0] += us[s].x, u[1] += us[s].y, u[2] += us[s].z, u[3] += us[s].w;
-                }
+              for (int s = 0; s < 4; ++s) {
+                const bool there = s0 + s < a.segments[0];
+                gs[s] = there ? __ldcg((const float4 *)(g0 + (s0 + s) * step)) : zero;
+                us[s] = there ? __ldcg((const float4 *)(g0 + (s0 + s) * step + I)) : zero;
               }
 #pragma unroll
-              for (int j = 0; j < 4; ++j) x.v[j] = __fdividef(x.v[j], 1.0f + __expf(-x.v[j])) * u[j];  // (2^-21: h keeps 8 bits)
+              for (int s = 0; s < 4; ++s) {
+                x.v[0] += gs[s].x, x.v[1] += gs[s].y, x.v[2] += gs[s].z, x.v[3] += gs[s].w;
+                u[0] += us[s].x, u[1] += us[s].y, u[2] += us[s].z, u[3] += us[s].w;
+              }
             }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x.v[j] = __fdividef(x.v[j], 1.0f + __expf(-x.v[j])) * u[j];  // (2^-21: h keeps 8 bits)
           };
           auto lay = [&](const Piece &x) {
             if constexpr (FP8) {
@@ -586,12 +590,30 @@ __global__ void __launch_bounds__(kThreads, 1)
                              : "memory");
             }
           };
-          for (int i = i0 >> 5; i < pieces; i += 2 * kLoaders) {
-            Piece x, y;
-            load(x, i);
-            if (i + kLoaders < pieces) load(y, i + kLoaders);
-            lay(x);
-            if (i + kLoaders < pieces) lay(y);
+          if (up) {
+            constexpr int kFlight = 6;
+            for (int i = i0 >> 5; i < pieces; i += kFlight * kLoaders) {
+              uint2 r[kFlight];
+#pragma unroll
+              for (int f = 0; f < kFlight; ++f) r[f] = load_x(i + f * kLoaders);
+#pragma unroll
+              for (int f = 0; f < kFlight; ++f) {
+                if (i + f * kLoaders >= pieces) break;
+                Piece x;
+                aim(x, i + f * kLoaders);
+                x.v[0] = __uint_as_float(r[f].x << 16), x.v[1] = __uint_as_float(r[f].x & 0xffff0000u);
+                x.v[2] = __uint_as_float(r[f].y << 16), x.v[3] = __uint_as_float(r[f].y & 0xffff0000u);
+                lay(x);
+              }
+            }
+          } else {
+            for (int i = i0 >> 5; i < pieces; i += 2 * kLoaders) {
+              Piece x, y;
+              load_h(x, i);
+              load_h(y, i + kLoaders);
+              lay(x);
+              if (i + kLoaders < pieces) lay(y);
+            }
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
