@@ -522,6 +522,7 @@ int tuna_plan_device_status(tuna_plan_t *plan, int *gave_up);
 #define TUNA_MOE_SIGMOID 1
 #define TUNA_MOE_MAX_EXPERTS 512
 #define TUNA_MOE_MAX_K 32
+#define TUNA_MOE_MAX_RANKS 4096
 
 /*
  * tuna_moe_route - the k experts of every token, their weights, and the rows' order.
@@ -543,7 +544,7 @@ int tuna_plan_device_status(tuna_plan_t *plan, int *gave_up);
  *            experts == ranks); may be NULL.
  *   offsets  ranks * experts + 1: the first row of each (rank, expert); may be NULL.
  * Limits (TUNA_ERR_RANGE): experts <= TUNA_MOE_MAX_EXPERTS, k <= TUNA_MOE_MAX_K,
- * tokens * k <= 2^31, ranks * experts <= 2^20.
+ * tokens * k <= 2^31, ranks <= TUNA_MOE_MAX_RANKS.
  *
  * tuna_moe_order - the same order from ids that another router made (ids below 0 or from
  * `experts` on are left out).
@@ -591,7 +592,8 @@ int tuna_moe_combine_backward(const void *dout, int out_dtype, int64_t lddo, con
  *   TUNA_FP8_TILES   128 x 128         rows x cols                [ceil(rows/128)][ceil(cols/128)]
  *   TUNA_FP8_TILES_T 128 x 128         x^T: cols x rows           [ceil(cols/128)][ceil(rows/128)]
  *   q is 16-byte aligned, its pitch ldq a multiple of 16; rows are written up to the
- *   next multiple of 16 (with zeros).  Blocks at the edges are smaller.
+ *   next multiple of 16 (with zeros).  Blocks at the edges are smaller.  rows < 2^31,
+ *   cols (and rows, of the transposed layouts) <= 2^24.
  *
  * tuna_fp8_matmul - out[m][n] = sum over blocks of a_scale * b_scale * (a . b), f32 or bf16.
  *   a        m x k, e4m3, TUNA_FP8_ROWS scales; b: n x k with TUNA_FP8_TILES scales, or
@@ -651,9 +653,10 @@ int tuna_moe_experts(const void *x, int64_t ldx, int64_t tokens, const int32_t *
  *   weight_dtype   TUNA_DTYPE_BF16, or TUNA_DTYPE_E4M3 with scales as in tuna_moe_experts
  *            (then only the weights are in 8 bits: x and h keep at least bf16's precision).
  *   ids, weights   tokens x k, receive the choice; may be NULL.
- * The first `zeroed` bytes of the workspace must be zero before its first use; every call
- * leaves them so (a call that gave up a wait, see tuna_ops_device_status, may not).  The
- * workspace may serve calls of other sizes if it is large enough.
+ * The first `zeroed` bytes of the workspace must be zero before its first use and belong
+ * to the calls from then on (after a call that gave up a wait, see tuna_ops_device_status,
+ * they must be zeroed again).  A workspace may serve calls of other sizes if it is large
+ * enough, one call at a time.
  * Limits (TUNA_ERR_RANGE): tokens <= TUNA_MOE_FEW_MAX_TOKENS, hidden, inter <= 8192.
  */
 #define TUNA_MOE_FEW_MAX_TOKENS 64

@@ -57,7 +57,7 @@ struct FewArgs {
   float scale;
   int segment[2], segments[2];  // of either product: 128-byte blocks of a row, and how many segments
   // workspace
-  unsigned *barrier;   // count, generation: zero before the first call, left so
+  unsigned long long *barrier;  // arrivals of all calls: zero before the first one
   float *part;         // [splits][tokens][experts] logits of a split
   int32_t *ids;        // [tokens * k]
   float *weights;      // [tokens * k]
@@ -79,7 +79,6 @@ struct Lists {
   int16_t entry[kMaxEntries];         // token * k + slot, by expert
   Group group[kMaxGroups];
   int groups, given_up;
-  unsigned generation;
   uint32_t tmem;
 };
 // What is needed only until the lists are made: lies where the stages are later.
@@ -98,32 +97,34 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// All blocks of the grid meet: one thread arrives for its block (after a barrier of the block),
-// any thread may wait.  `bar`: arrivals, generation.
-__device__ unsigned grid_arrive(unsigned *bar) {
-  const unsigned g = *(volatile unsigned *)(bar + 1);
-  __threadfence();
-  if (atomicAdd(bar, 1u) == gridDim.x - 1) {
-    bar[0] = 0;
-    __threadfence();
-    atomicAdd(bar + 1, 1u);
-  }
-  return g;
+// All blocks of the grid meet: one thread arrives for its block (after a barrier of the block), any
+// thread may wait.  The counter only grows, by the grid's size at each meeting, so that an arrival is one
+// addition and a wait one load (with a generation word that the last block advances, one token took 34 us
+// instead of 30).  64 bits never wrap.
+__device__ __forceinline__ unsigned long long meeting_base(const unsigned long long *bar) {
+  // read before this block's first arrival: the count is then short of the next multiple
+  unsigned long long v;
+  asm volatile("ld.relaxed.gpu.global.u64 %0, [%1];" : "=l"(v) : "l"(bar) : "memory");
+  return v - v % gridDim.x;
 }
-__device__ bool grid_wait(unsigned *bar, unsigned g, volatile int *given_up) {
+__device__ __forceinline__ void grid_arrive(unsigned long long *bar) {
+  asm volatile("red.release.gpu.global.add.u64 [%0], 1;" ::"l"(bar) : "memory");
+}
+__device__ bool grid_wait(const unsigned long long *bar, unsigned long long target, volatile int *given_up) {
   const long long t0 = clock64();
-  while (*(volatile unsigned *)(bar + 1) == g) {
+  for (;;) {
+    unsigned long long v;
+    asm volatile("ld.acquire.gpu.global.u64 %0, [%1];" : "=l"(v) : "l"(bar) : "memory");
+    if (v >= target) return true;
     if (*given_up || clock64() - t0 > kWaitCycles) {
       *given_up = 1;
       return false;
     }
   }
-  __threadfence();
-  return true;
 }
-__device__ bool grid_meet(unsigned *bar, int *given_up) {
+__device__ bool grid_meet(unsigned long long *bar, unsigned long long target, int *given_up) {
   __syncthreads();
-  if (threadIdx.x == 0) grid_wait(bar, grid_arrive(bar), given_up);
+  if (threadIdx.x == 0) grid_arrive(bar), grid_wait(bar, target, given_up);
   __syncthreads();
   return !*(volatile int *)given_up;
 }
@@ -186,6 +187,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 2) tmem_alloc(smem_u32(&l.tmem), kBufs * kBufCols);
+  const unsigned long long base = meeting_base(a.barrier);
 
   // ---- logits: a block takes 16 experts and 1024 columns, a warp 64 of them
   {
@@ -232,7 +234,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncthreads();
     }
   }
-  bool fine = grid_meet(a.barrier, &l.given_up);
+  bool fine = grid_meet(a.barrier, base + gridDim.x, &l.given_up);
 
   if (fine) {
     // ---- the choice, by every block for itself; the fewer experts, the more tokens a warp takes
@@ -511,7 +513,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       } else if (warp >= kWarps - kLoaders && p.unit0 < p.unit1) {
         // -- the tokens' operands, a (group, segment) ahead of the tensor cores
-        if (!up) ok = __all_sync(~0u, lane != 0 || grid_wait(a.barrier, l.generation, &l.given_up));  // every block's sums are there
+        if (!up) ok = __all_sync(~0u, lane != 0 || grid_wait(a.barrier, base + 2ull * gridDim.x, &l.given_up));  // every block's sums are there
         const int i0 = tid - (kWarps - kLoaders) * 32;
         for (Unit w(p); ok && w.left > 0; w.left -= p.tiles - w.m, w.turn(p)) {
           const int first = l.group[w.g].first, count = l.group[w.g].count, N = FP8 && count > 8 ? 32 : 16;
@@ -626,14 +628,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (*(volatile int *)&l.given_up) break;
       if (up) {
         // the next product's weights are on their way while the blocks' sums meet
-        if (tid == 0) l.generation = grid_arrive(a.barrier);
-        __syncthreads();
+        if (tid == 0) grid_arrive(a.barrier);
       }
     }
-    // (a block without units has not waited for the barrier between the products yet)
-    if (tid == 0 && !l.given_up) grid_wait(a.barrier, l.generation, &l.given_up);
+    // (a block without units has not waited for the second meeting: it must not arrive at the third before)
+    if (tid == 0 && !l.given_up) grid_wait(a.barrier, base + 2ull * gridDim.x, &l.given_up);
     __syncthreads();
-    fine = !*(volatile int *)&l.given_up && grid_meet(a.barrier, &l.given_up);
+    fine = !*(volatile int *)&l.given_up && grid_meet(a.barrier, base + 3ull * gridDim.x, &l.given_up);
   }
 
   // ---- the weighted sum, slots and segments in order
@@ -681,7 +682,7 @@ size_t carve_few(Carve &c, FewArgs &a, int tokens, int experts, int k, int hidde
   const int64_t n = (int64_t)tokens * k, splits = ceil_div(hidden, kSplit);
   plan_segments(tokens, k, experts, 2 * (int64_t)inter, hidden, fp8 ? 128 : 64, a.segment[0], a.segments[0]);
   plan_segments(tokens, k, experts, hidden, inter, fp8 ? 128 : 64, a.segment[1], a.segments[1]);
-  a.barrier = c.take<unsigned>(2);
+  a.barrier = c.take<unsigned long long>(1);
   const size_t zeroed = c.used;
   a.part = c.take<float>(splits * tokens * experts);
   a.ids = c.take<int32_t>(n);

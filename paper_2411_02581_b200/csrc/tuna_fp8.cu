@@ -784,7 +784,7 @@ int tuna_fp8_quantize(const void *x, int dtype, int64_t rows, int cols, int64_t 
   if (!size || rows < 0 || cols < 0 || ldx < cols || layout < TUNA_FP8_ROWS || layout > TUNA_FP8_TILES_T) return TUNA_ERR_INVALID_ARG;
   const bool turned = layout == TUNA_FP8_COLUMNS || layout == TUNA_FP8_TILES_T;
   if (ldq < (turned ? rows : cols) || ldq % 16 != 0) return TUNA_ERR_INVALID_ARG;
-  if (cols > kMaxDim || (turned && rows > kMaxDim) || ceil_div(rows, 128) * ceil_div(cols, 128) > INT32_MAX) return TUNA_ERR_RANGE;
+  if (cols > kMaxDim || (turned && rows > kMaxDim) || rows > INT32_MAX || ceil_div(rows, 128) * ceil_div(cols, 128) > INT32_MAX) return TUNA_ERR_RANGE;
   if (rows == 0 || cols == 0) return TUNA_OK;
   if (!x || !q || !scale || !aligned(x, size) || !aligned(q, 16) || !aligned(scale, 4)) return TUNA_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;

@@ -574,7 +574,7 @@ void plan_order(OrderArgs &o, int64_t tokens, int experts, int k, int ranks) {
 
 int check_order(int64_t tokens, int experts, int k, int ranks) {
   if (tokens < 0 || experts < 1 || k < 1 || ranks < 1 || tokens % ranks != 0 || k > experts) return TUNA_ERR_INVALID_ARG;
-  if (experts > TUNA_MOE_MAX_EXPERTS || k > kMaxK || tokens > ((int64_t)1 << 31) / k || (int64_t)ranks > (1 << 20) / experts) return TUNA_ERR_RANGE;
+  if (experts > TUNA_MOE_MAX_EXPERTS || k > kMaxK || tokens > ((int64_t)1 << 31) / k || ranks > TUNA_MOE_MAX_RANKS) return TUNA_ERR_RANGE;
   return TUNA_OK;
 }
 

@@ -199,6 +199,26 @@ def test_operands_off_16_bytes_and_other_streams():
 
 
 @pytest.mark.gpu
+def test_more_values_than_32_bits_count():
+    """2^31 + values: the last rows of the operand and of the result are where they should be."""
+    from paper_2411_02581_b200 import moe
+    m, k, n = 66000, 32768, 40
+    x = torch.empty(m, k, dtype=torch.bfloat16, device="cuda")
+    x.view(torch.int16).copy_(torch.arange(k, device="cuda").remainder(251).to(torch.int16)[None, :] + 0x3f00)
+    tail = activations(5, k, 1).cuda()
+    x[-5:] = tail
+    q, s = moe.fp8_quantize(x)
+    wq, ws = plain_quantize(tail.cpu(), "rows")
+    assert torch.equal(s[:, -5:].cpu(), ws) and torch.equal(q[-5:].cpu().view(torch.uint8), wq.view(torch.uint8))
+    v, t = moe.fp8_quantize(activations(n, k, 2).cuda(), "tiles")
+    y = moe.fp8_matmul(q, s, v, t)
+    assert close(y[-5:], value(wq, ws, "rows"), value(v, t, "tiles"), True)
+    assert torch.equal(y[0], y[m - 6])            # equal rows give equal results wherever they are
+    del x, q, y
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
 def test_one_answer_however_often():
     from paper_2411_02581_b200 import moe
     q, s = moe.fp8_quantize(activations(7, 4096, 1).cuda())

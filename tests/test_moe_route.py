@@ -72,7 +72,7 @@ def make_logits(t, e, dtype, seed, kind):
 
 
 SHAPES = [(1, 1, 1, 1), (1, 64, 2, 1), (7, 5, 3, 1), (64, 64, 8, 1), (129, 60, 2, 1), (1000, 256, 8, 4), (96, 100, 9, 8),
-          (333, 512, 32, 3), (5000, 8, 1, 1), (40000, 64, 2, 64), (2050, 130, 17, 1)]
+          (333, 512, 32, 3), (5000, 8, 1, 1), (40000, 64, 2, 64), (4096, 3, 2, 4096), (9000, 512, 4, 300), (2050, 130, 17, 1)]
 
 
 @pytest.mark.gpu
@@ -244,7 +244,7 @@ def test_route_refusals():
     assert size(-1, 64, 2, 1) == -1 and size(64, 0, 2, 1) == -1 and size(64, 64, 0, 1) == -1
     assert size(64, 64, 2, 0) == -1 and size(64, 64, 2, 3) == -1          # 3 ranks do not divide 64 tokens
     assert size(64, 8, 9, 1) == -1                                         # more slots than experts
-    assert size(64, 513, 2, 1) == -9 and size(64, 64, 33, 1) == -9 and size(1 << 31, 64, 2, 1) == -9
+    assert size(8192, 64, 2, 8192) == -9 and size(64, 513, 2, 1) == -9 and size(64, 64, 33, 1) == -9 and size(1 << 31, 64, 2, 1) == -9
 
     def route(p=256, dtype=0, t=64, e=64, ld=64, k=2, ranks=1, scoring=0, ws=256, ws_bytes=1 << 30):
         return L.tuna_moe_route(p, dtype, t, e, ld, k, ranks, scoring, 0, 1.0, p, p, p, p, p, p, ws, ws_bytes, None)
