@@ -605,7 +605,8 @@ int tuna_moe_combine_backward(const void *dout, int out_dtype, int64_t lddo, con
  *            rows [offsets[g], offsets[g+1]) of a meet matrix g (offsets: DEVICE, groups + 1,
  *            not falling, inside [0, m]).  Rows outside every group are not written.
  *            offsets NULL: one group of all rows.
- * Limits (TUNA_ERR_RANGE): groups <= TUNA_MOE_MAX_EXPERTS, n, k <= 2^24, m < 2^31 - 256.
+ * Limits (TUNA_ERR_RANGE): groups <= TUNA_MOE_MAX_EXPERTS, n, k <= 2^24, m < 2^31 - 256,
+ *   groups x (m / 128 + 1) x n / 128 < 2^31.
  */
 #define TUNA_FP8_ROWS 0
 #define TUNA_FP8_COLUMNS 1

@@ -193,7 +193,11 @@ constexpr int kSumWarps = 16;   // promotion: four quarters of the columns x 128
 constexpr int kGemmThreads = 128 + kSumWarps * 32;
 constexpr int kSumPitch = 132;  // floats: rows of sums that a cluster joins, on 16-byte boundaries and four banks apart
 constexpr int kCopyRegs = 64, kSumRegs = 104;  // registers of a thread: copying and issuing warps, promotion
+// columns that a promotion thread reads at a time, twice: with 16 the sums, both reads and the loop's own values do not fit
+// the registers (8192 x 4096 x 4096: 126.8 us, 121.6 with 8; the experts of 8192 tokens x 2: 648 and 633 us)
+constexpr int kRun = 8;
 constexpr int kMaxGroups = TUNA_MOE_MAX_EXPERTS;
+constexpr int kPlaces = 8;  // the scale warps are four tiles ahead of the slowest promotion warp at most
 
 // STORES: bf16 results, which leave through shared memory
 template <int BN, bool STORES>
@@ -205,24 +209,23 @@ struct Shape {
   static constexpr int kOutBytes = STORES ? kSumWarps * 32 * kRowBytes : 0;  // each promotion warp's 32 rows of them, on their way out
   // stages, results, then the factors beside the two accumulators, the rows' largest magnitudes, the groups'
   // tile offsets, barriers and flags
-  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kOutBytes + 2 * 384 * 4 + 512 * 4 + (kMaxGroups + 8) * 4 + 256;
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kOutBytes + 2 * 384 * 4 + 512 * 4 + (kMaxGroups + 8) * 4 + kPlaces * 16 + 256;
 };
 
 // Tile t of the walk: the group it is in (never walked backwards), its rows and columns.
+// (32 bits: there are fewer rows than 2^31, and a result of 2^31 tiles does not fit the memory.)
 struct Walk {
   int g = 0;
-  int64_t row, end;  // first row, end of the group's rows
+  int row, end;  // first row, end of the group's rows
   int n0;
 };
-__device__ __forceinline__ void walk_to(Walk &w, int64_t t, const TileArgs &a, const int *tile_base, int bn) {
-  while (t >= (int64_t)tile_base[w.g + 1] * a.n_tiles) ++w.g;
-  const int mt = tile_base[w.g + 1] - tile_base[w.g];
-  const int64_t local = t - (int64_t)tile_base[w.g] * a.n_tiles;
-  const int n = (int)(local / mt), m = (int)(local - (int64_t)n * mt);  // rows fastest: blocks that run together share b
-  int64_t begin = 0;
-  w.end = a.p.m;
-  if (a.p.offsets) begin = max(a.p.offsets[w.g], (int64_t)0), w.end = min(a.p.offsets[w.g + 1], a.p.m);
-  w.row = begin + (int64_t)m * 128;
+__device__ __forceinline__ void walk_to(Walk &w, int t, const TileArgs &a, const int *tile_base, int bn) {
+  while (t >= tile_base[w.g + 1] * a.n_tiles) ++w.g;
+  const uint32_t mt = tile_base[w.g + 1] - tile_base[w.g], local = t - tile_base[w.g] * a.n_tiles;
+  const uint32_t n = local / mt, m = local - n * mt;  // rows fastest: blocks that run together share b
+  int64_t begin = 0, end = a.p.m;
+  if (a.p.offsets) begin = max(a.p.offsets[w.g], (int64_t)0), end = min(a.p.offsets[w.g + 1], a.p.m);
+  w.row = (int)begin + (int)m * 128, w.end = (int)end;
   w.n0 = n * bn;
 }
 
@@ -243,11 +246,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   uint32_t *row_amax = (uint32_t *)(factors + 2 * 384);  // [4][128]
   int *tile_base = (int *)(row_amax + 512);
   uint64_t *bars = (uint64_t *)(tile_base + kMaxGroups + 8);
-  volatile int *given_up = (volatile int *)(bars + 2 * S::kStages + 5);
+  int4 *places = (int4 *)(bars + 2 * S::kStages + 6 - (2 * S::kStages & 1));  // of the tiles: row, end, first column
+  volatile int *given_up = (volatile int *)(places + kPlaces);
   volatile int *lost = given_up + 1;  // a warp of the promotion gave up
   uint32_t *tmem_at = (uint32_t *)(given_up + 2);
   const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages, freed = done + 16, drained = freed + 16;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // (the same in all lanes, which the compiler then knows)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S::kStages; ++s) mbar_init(full + 8 * s, 1), mbar_init(empty + 8 * s, 1);
@@ -282,11 +286,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_at;
-  const int64_t tiles = (int64_t)tile_base[a.p.groups] * a.n_tiles;
+  const uint32_t tmem = __shfl_sync(~0u, *tmem_at, 0);
+  const int tiles = tile_base[a.p.groups] * a.n_tiles;
   const int parts = SPLIT ? (int)cluster_size() : 1, part = SPLIT ? (int)cluster_rank() : 0;
-  auto first = [&] { return (int64_t)(SPLIT ? blockIdx.x / parts : blockIdx.x); };
-  auto step = [&] { return SPLIT ? gridDim.x / parts : gridDim.x; };
+  auto first = [&] { return (int)(SPLIT ? blockIdx.x / parts : blockIdx.x); };
+  auto step = [&] { return (int)(SPLIT ? gridDim.x / parts : gridDim.x); };
   // this block's part of k
   const int kb_first = SPLIT ? (int)((int64_t)a.blocks * part / parts) : 0, blocks = SPLIT ? (int)((int64_t)a.blocks * (part + 1) / parts) - kb_first : a.blocks;
 
@@ -298,14 +302,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       int64_t issued = 0;
       Walk w;
       bool ok = true;
-      for (int64_t t = first(); ok && t < tiles; t += step()) {
+      for (int t = first(); ok && t < tiles; t += step()) {
         walk_to(w, t, a, tile_base, SWIGLU ? BN / 2 : BN);
         for (int kb = 0; kb < blocks; ++kb) {
           if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, given_up))) break;
           const uint32_t at = smem_u32(smem) + stage * S::kStageBytes, bar = full + 8 * stage;
           mbar_expect(bar, S::kStageBytes);
           const int col = (kb_first + kb) * 128;
-          tma_load_2d(at, &map_a, col, (int)w.row, bar);
+          tma_load_2d(at, &map_a, col, w.row, bar);
           if (SWIGLU && a.one_copy) {
             tma_load_5d(at + 128 * 128, &map_b, col, 0, 0, w.n0 / 32, w.g, bar);
           } else if (SWIGLU) {
@@ -324,46 +328,51 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         for (int64_t i = max((int64_t)0, issued - S::kStages); i < issued; ++i)
           mbar_wait(full + 8 * (int)(i % S::kStages), (uint32_t)((i / S::kStages) & 1), &never);
       }
-    } else if (warp == 1 && lane == 0) {
-      // ---- tensor cores
+    } else if (warp == 1) {
+      // ---- tensor cores: the whole warp goes along, one lane issues
       constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);  // f32 sums of e4m3 products
       int stage = 0, phase = 0, buf = 0, buf_phase = 0;
       bool ok = true;
-      for (int64_t t = first(); ok && t < tiles; t += step()) {
+      for (int t = first(); ok && t < tiles; t += step()) {
         for (int kb = 0; kb < blocks; ++kb) {
-          if (!(ok = mbar_wait(full + 8 * stage, phase, given_up) && mbar_wait(freed + 8 * buf, buf_phase ^ 1, given_up))) break;
+          if (!(ok = __all_sync(~0u, mbar_wait(full + 8 * stage, phase, given_up) && mbar_wait(freed + 8 * buf, buf_phase ^ 1, given_up)))) break;
           tc_fence_after();
           const uint32_t at = smem_u32(smem) + stage * S::kStageBytes;
           const uint64_t da = tc_desc(at), db = tc_desc(at + 128 * 128);
+          if (elect_one()) {
 #pragma unroll
-          for (int s = 0; s < 4; ++s) tc_mma_fp8(tmem + buf * BN, da + 2 * s, db + 2 * s, idesc, s > 0);  // 32 bytes along k
-          tc_commit(empty + 8 * stage);
-          tc_commit(done + 8 * buf);
+            for (int s = 0; s < 4; ++s) tc_mma_fp8(tmem + buf * BN, da + 2 * s, db + 2 * s, idesc, s > 0);  // 32 bytes along k
+            tc_commit(empty + 8 * stage);
+            tc_commit(done + 8 * buf);
+          }
+          __syncwarp();
           if (++stage == S::kStages) stage = 0, phase ^= 1;
           if (++buf == 2) buf = 0, buf_phase ^= 1;
         }
       }
       if (!ok) {
         int never = 0;
-        tc_commit(drained);
+        if (elect_one()) tc_commit(drained);
+        __syncwarp();
         mbar_wait(drained, 0, &never);
       }
     } else if (warp >= 2) {
       // ---- scales: a lane has two rows of the tile, and with B_ROWS four columns
-      constexpr int kAhead = 4, kVals = B_ROWS ? 6 : 4;
+      constexpr int kAhead = 2, kVals = B_ROWS ? 6 : 4;
       const int i = threadIdx.x - 64, tiles_n = (a.p.n + 127) / 128;
       int buf = 0, buf_phase = 0;
       bool ok = true;
       Walk w;
       const float *sa0 = nullptr, *sa1 = nullptr, *sb0 = nullptr, *sb1 = nullptr;
       // the blocks that are fetched next: one run of kAhead ahead of those handed out, across tiles too
-      int64_t ahead_t = first();
-      int ahead_kb = 0;
+      int ahead_t = first(), ahead_kb = 0, ahead_place = 0;
       float next[kAhead][kVals];
       auto fetch = [&]() {
         if (ahead_t >= tiles) return;
         if (ahead_kb == 0) {
           walk_to(w, ahead_t, a, tile_base, SWIGLU ? BN / 2 : BN);
+          // also for the warps that promote, which have no registers for it: `done` tells them
+          if (threadIdx.x == 64) places[ahead_place++ % kPlaces] = make_int4(w.row, w.end, w.n0, 0);
           sa0 = a.p.sa + min(w.row + i, w.end - 1), sa1 = a.p.sa + min(w.row + i + 64, w.end - 1);
           if (SWIGLU) {
             sb0 = a.p.sb + ((int64_t)(w.g * 2) * tiles_n + w.n0 / 128) * a.blocks;
@@ -388,7 +397,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         if (ahead_kb >= blocks) ahead_kb = 0, ahead_t += step();
       };
       fetch();
-      for (int64_t t = first(); ok && t < tiles; t += step()) {
+      for (int t = first(); ok && t < tiles; t += step()) {
         for (int kb0 = 0; ok && kb0 < blocks; kb0 += kAhead) {
           float now[kAhead][kVals];
 #pragma unroll
@@ -426,13 +435,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     const uint32_t factor = smem_u32(factors) + (SWIGLU || B_ROWS ? row_in : (BN == 256 ? quarter >> 1 : 0) * 128 + row_in) * 4;
     int buf = 0, buf_phase = 0;
     bool ok = true;
-    Walk w;
-    for (int64_t t = first(); ok && t < tiles; t += step()) {
-      walk_to(w, t, a, tile_base, SWIGLU ? BN / 2 : BN);
-      const int64_t row = w.row + row_in;
-      const bool there = row < w.end;
-      const int n0 = w.n0;
-      const int64_t end = w.end;
+    int place = 0;
+    for (int t = first(); ok && t < tiles; t += step(), ++place) {
       uint64_t acc[S::kCols / 2];
 #pragma unroll
       for (int i = 0; i < S::kCols / 2; ++i) acc[i] = 0;
@@ -440,7 +444,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         ok = __all_sync(~0u, mbar_wait(done + 8 * buf, buf_phase, given_up));  // (and the warp is whole for the loads)
         if (!ok) break;
         tc_fence_after();
-        constexpr int kRun = B_ROWS ? 8 : 16;  // columns at a time: with B_ROWS the factors need registers too
         uint32_t v[2][kRun];
         tmem_load(from + buf * BN, v[0]);
         float s0, s1 = 0.0f;
@@ -478,6 +481,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         }
         if (++buf == 2) buf = 0, buf_phase ^= 1;
       }
+      const int4 at = places[place % kPlaces];
+      const int row = at.x + row_in, end = at.y, n0 = at.z;
+      const bool there = row < end;
       if constexpr (SPLIT) {
         // the sums to shared memory, where the stages were: every step that read them is done
         float *red = (float *)smem + row_in * kSumPitch + quarter * S::kCols;
@@ -499,8 +505,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           constexpr int kPieces = S::kRowBytes / 16;
           auto place = [](int r, int piece) { return (uint32_t)(r * S::kRowBytes + (kPieces == 8 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3)) * 16); };
           const uint32_t to = smem_u32(smem) + S::kStages * S::kStageBytes + (warp - 4) * 32 * S::kRowBytes;
-          const int64_t row0 = row - lane;
-          const int valid = (int)max((int64_t)0, min((int64_t)32, end - row0)), c0 = n0 + quarter * S::kCols;
+          const int row0 = row - lane;
+          const int valid = max(0, min(32, end - row0)), c0 = n0 + quarter * S::kCols;
           if (lane == 0) tma_store_read();
           __syncwarp();
 #pragma unroll
@@ -515,10 +521,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           if (a.store_tiles && valid == 32) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0 && c0 < a.p.n) tma_store_2d(&map_out, c0, (int)row0, to);
+            if (lane == 0 && c0 < a.p.n) tma_store_2d(&map_out, c0, row0, to);
           } else {
             __syncwarp();
-            __nv_bfloat16 *out = (__nv_bfloat16 *)a.p.out + row0 * a.p.ldo + c0;
+            __nv_bfloat16 *out = (__nv_bfloat16 *)a.p.out + (int64_t)row0 * a.p.ldo + c0;
             if (a.store_tiles && c0 + S::kCols <= a.p.n) {
               for (int i = lane; i < valid * kPieces; i += 32) {
                 const int r = i / kPieces, piece = i % kPieces;
@@ -538,25 +544,25 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           }
           __syncwarp();
         } else if (there) {
-          TO *out = (TO *)a.p.out + row * a.p.ldo;
+          // 32-bit results, in whole 32-byte sectors
+          static_assert(sizeof(TO) == 4);
+          float *out = (float *)a.p.out + (int64_t)row * a.p.ldo;
           const int c0 = n0 + quarter * S::kCols;
-          // whole 32-byte sectors
-          constexpr int kRun = 32 / sizeof(TO);
-          const bool vec = (((uintptr_t)a.p.out | (uint64_t)a.p.ldo * sizeof(TO)) & 31) == 0;
+          const bool vec = (((uintptr_t)a.p.out | (uint64_t)a.p.ldo * 4) & 31) == 0;
 #pragma unroll
-          for (int i = 0; i < S::kCols; i += kRun) {
-            float v[kRun];
+          for (int i = 0; i < S::kCols; i += 8) {
+            float v[8];
 #pragma unroll
-            for (int j = 0; j < kRun / 2; ++j) unpair(acc[i / 2 + j], v[2 * j], v[2 * j + 1]);
-            if (vec && c0 + i + kRun <= a.p.n) {
+            for (int j = 0; j < 4; ++j) unpair(acc[i / 2 + j], v[2 * j], v[2 * j + 1]);
+            if (vec && c0 + i + 8 <= a.p.n) {
               uint32_t u[8];
 #pragma unroll
-              for (int j = 0; j < 8; ++j) u[j] = sizeof(TO) == 2 ? pack_bf16(v[2 * j % kRun], v[(2 * j + 1) % kRun]) : __float_as_uint(v[j]);
+              for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(v[j]);
               store32(out + c0 + i, u);
             } else {
 #pragma unroll
-              for (int j = 0; j < kRun; ++j)
-                if (c0 + i + j < a.p.n) out[c0 + i + j] = from_f32<TO>(v[j]);
+              for (int j = 0; j < 8; ++j)
+                if (c0 + i + j < a.p.n) out[c0 + i + j] = v[j];
             }
           }
         }
@@ -587,7 +593,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         if (there) {
           if (quarter == 0) a.p.hs[(int64_t)(n0 / 128) * a.p.m + row] = s;
           const Divisor by = divisor(s);
-          uint4 *out = (uint4 *)((uint8_t *)a.p.out + row * a.p.ldo + n0 + quarter * 32);  // (the pitch covers whole blocks)
+          uint4 *out = (uint4 *)((uint8_t *)a.p.out + (int64_t)row * a.p.ldo + n0 + quarter * 32);  // (the pitch covers whole blocks)
           out[0] = fp8_sixteen(h, by), out[1] = fp8_sixteen(h + 16, by);
         }
       }
@@ -601,7 +607,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     if (first() < tiles && !*given_up) {
       Walk w;
       walk_to(w, first(), a, tile_base, BN);
-      const int rows = (int)min((int64_t)128, w.end - w.row);
+      const int rows = min(128, w.end - w.row);
       for (int i = threadIdx.x; i < (rows - part + parts - 1) / parts * (BN / 4); i += kGemmThreads) {
         const int r = part + i / (BN / 4) * parts, c = i % (BN / 4) * 4;
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -609,7 +615,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           const float4 x = load_from_block(smem_u32(smem) + (r * kSumPitch + c) * 4, q);
           v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
         }
-        TO *out = (TO *)a.p.out + (w.row + r) * a.p.ldo + w.n0 + c;
+        TO *out = (TO *)a.p.out + (int64_t)(w.row + r) * a.p.ldo + w.n0 + c;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           if (w.n0 + c + j < a.p.n) out[j] = from_f32<TO>(v[j]);
@@ -806,7 +812,7 @@ int tuna_fp8_matmul(const void *a, const float *a_scale, int64_t m, int64_t lda,
   if (b_layout != TUNA_FP8_TILES && b_layout != TUNA_FP8_ROWS) return TUNA_ERR_INVALID_ARG;
   if ((groups > 1 && !offsets) || (b_layout == TUNA_FP8_ROWS && offsets)) return TUNA_ERR_INVALID_ARG;
   if (groups > TUNA_MOE_MAX_EXPERTS || n > kMaxDim || k > kMaxDim || m > INT32_MAX - 256) return TUNA_ERR_RANGE;
-  if ((ceil_div(m, 128) + groups) > INT32_MAX / std::max<int64_t>(1, ceil_div(n, 128))) return TUNA_ERR_RANGE;
+  if (groups * (ceil_div(m, 128) + 1) * ceil_div(n, 128) > INT32_MAX) return TUNA_ERR_RANGE;  // tiles, whatever the offsets hold
   if (m == 0 || n == 0) return TUNA_OK;
   if (!out || !aligned(out, so)) return TUNA_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
