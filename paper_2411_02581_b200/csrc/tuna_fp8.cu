@@ -230,7 +230,7 @@ __device__ __forceinline__ void walk_to(Walk &w, int t, const TileArgs &a, const
 }
 
 //
-// With SPLIT a cluster of 2, 4 or 8 blocks shares one tile: each adds up a part of k, leaves its sums in
+// With SPLIT a cluster of 2 or 4 blocks shares one tile: each adds up a part of k, leaves its sums in
 // its shared memory, and adds up the parts of some of the rows from all of them, in order of k.  For few
 // rows there are fewer tiles than multiprocessors otherwise.
 template <int BN, bool SWIGLU, bool B_ROWS, bool SPLIT, typename TO>
@@ -749,16 +749,23 @@ int launch_product(const ProductArgs &p, cudaStream_t st) {
     if (p.out_f32) return run_tiles<256, false, true, float>(p, st);
     return run_tiles<256, false, true, __nv_bfloat16>(p, st);
   }
-  if (wide >= sm_count()) {
+  // A round of tiles of 256 columns takes 6 / 5 of the time of one of 128 (the promotion is shared by as
+  // many warps), so the rounds decide.  (k = 4096: 1024 x 4096 is 1 round or 2: 20.0 us against 28.2; 512 x
+  // 4096 one of either: 18.9 against 16.5; 1024 x 4736 two of either: 32.4 against 28.4; 1280 x 4096 two or three: 32.6 against 37.9.)
+  const int64_t narrow = (ceil_div(p.m, 128) + (p.offsets ? p.groups - 1 : 0)) * ceil_div(p.n, 128);
+  if (6 * ceil_div(wide, sm_count()) < 5 * ceil_div(narrow, sm_count())) {
     if (p.out_f32) return run_tiles<256, false, false, float>(p, st);
     return run_tiles<256, false, false, __nv_bfloat16>(p, st);
   }
   if (!p.offsets) {
-    // few tiles: a cluster shares each, as long as every block keeps two blocks of k or more.  (128 blocks
-    // at most: more clusters of 8 are not resident together.)  One row of 4096 x 4096: 15.3 us without.
-    const int64_t tiles = ceil_div(p.m, 128) * ceil_div(p.n, 128);
-    int parts = 8;
-    while (parts > 1 && (tiles * parts > 128 || ceil_div(p.k, 128) < 2 * parts)) parts /= 2;
+    // Few tiles: a cluster shares each, while its blocks find room at once and every one is spared 12 blocks
+    // of k, which pay for the meeting.  (Rows 1 to 128, k = 4096: 10.1 us in fours, 12.1 in twos, 14.3 alone,
+    // for 1024 to 4096 columns; clusters of 8 are no faster, and 16 of them are not resident together: 17.8 us.
+    // 128 x 2048 x 2048: 8.6 in fours, 9.5 in twos, 9.0 alone.  128 x 4096 x 1024: 8.3 in fours, 6.7 alone.
+    // 256 x 4096: 12.9 in twos and 15.5 alone at k = 4096, 9.9 and 9.3 at 2048.)
+    const int64_t tiles = ceil_div(p.m, 128) * ceil_div(p.n, 128), blocks = ceil_div(p.k, 128);
+    int parts = 4;
+    while (parts > 1 && (tiles * parts > 128 || blocks - blocks / parts < 12)) parts /= 2;
     if (parts > 1) {
       if (p.out_f32) return run_tiles<128, false, false, float, true>(p, st, parts);
       return run_tiles<128, false, false, __nv_bfloat16, true>(p, st, parts);

@@ -50,7 +50,6 @@ int *error_word() {
 namespace {
 
 constexpr int kTopThreads = 256;
-constexpr int kSmallTokens = 256;  // up to here one block is done before a second launch would be
 
 struct RouteArgs {
   const void *logits;
@@ -557,14 +556,16 @@ __global__ void __launch_bounds__(256) tuna_combine_grad_kernel(CombineArgs a) {
 
 // ---- host --------------------------------------------------------------------------------
 
-// Chunks of at most 128 tokens, fewer where that fills the GPU better; the blocks of the order
+// Chunks of 32 to 128 tokens (more where there were thousands of them), the smallest that leave two
+// blocks a multiprocessor or fewer: a warp chooses for its tokens one after the other (1024 tokens, 256
+// experts, 8 slots: 56.4 us in chunks of 128, 16.6 in chunks of 32).  The blocks of the order
 // kernel take as many chunks as keep their number near one a multiprocessor, since each of them
 // reads the whole table of counts.
 void plan_order(OrderArgs &o, int64_t tokens, int experts, int k, int ranks) {
   o.tokens = tokens, o.experts = experts, o.k = k, o.ranks = ranks;
   o.rank_tokens = tokens / ranks;
-  int64_t chunk = 128;
-  while (ceil_div(tokens, chunk) > 2048) chunk *= 2;
+  int64_t chunk = 32;
+  while (ceil_div(tokens, chunk) > (chunk < 128 ? 296 : 2048)) chunk *= 2;
   while (chunk * k > 65535) chunk /= 2;  // 16 bits hold a chunk's count of one expert
   o.chunk = (int)chunk;
   o.rank_chunks = ceil_div(o.rank_tokens, chunk);
@@ -595,7 +596,8 @@ int launch_order(const OrderArgs &o, cudaStream_t st) {
 }
 
 // Lanes a token and values a lane: the fewest lanes that hold the experts at 8 values each
-// (one 16-byte load of bf16) and the slots at one a lane.
+// (one 16-byte load of bf16) and the slots at one a lane.  (With twice the lanes the choice among 64
+// experts for 65536 tokens, 2 slots, took 48.7 us instead of 30.2 with its order, among 128, 8 slots, 186 instead of 107.)
 template <typename F>
 int by_width(int experts, int k, F f) {
   if (experts <= 64 && k <= 8) return f.template operator()<8, 8>();
@@ -635,6 +637,15 @@ struct GradLaunch {
   }
 };
 
+// Tokens that one block chooses for and orders in two rounds; it is then done before a second launch
+// would be.  Three rounds are not.  (64 experts, 2 slots: 256 tokens 10.2 us against 15.0, 512 tokens
+// 15.4 against 14.9; 256 experts, 8 slots: 64 tokens 14.2 against 16.5, 128 tokens 24.4 against 16.6.)
+struct Lanes {
+  template <int LPT, int VPL>
+  int operator()() { return LPT; }
+};
+int64_t small_tokens(int experts, int k) { return 2 * kSmallThreads / by_width(experts, k, Lanes{}); }
+
 size_t dtype_size(int dtype) { return dtype == TUNA_DTYPE_F32 ? 4 : dtype == TUNA_DTYPE_BF16 ? 2 : 0; }
 
 }  // namespace
@@ -661,7 +672,7 @@ int tuna_moe_order_workspace_bytes(int64_t tokens, int experts, int k, int ranks
 
 int tuna_moe_route_workspace_bytes(int64_t tokens, int experts, int k, int ranks, size_t *bytes) {
   if (const int rc = tuna_moe_order_workspace_bytes(tokens, experts, k, ranks, bytes)) return rc;
-  if (ranks == 1 && tokens <= kSmallTokens) *bytes = 0;
+  if (ranks == 1 && tokens <= small_tokens(experts, k)) *bytes = 0;
   return TUNA_OK;
 }
 
@@ -691,7 +702,7 @@ int tuna_moe_route(const void *logits, int dtype, int64_t tokens, int experts, i
   if (tokens == 0) return zero_order(o, ranks, experts, st);
   if (!logits || !ids || !weights || !rows || !pos || !aligned(logits, dtype_size(dtype))) return TUNA_ERR_INVALID_ARG;
   plan_order(o, tokens, experts, k, ranks);
-  const bool small = ranks == 1 && tokens <= kSmallTokens;
+  const bool small = ranks == 1 && tokens <= small_tokens(experts, k);
   if (!small && (!workspace || !aligned(workspace, 256) || workspace_bytes < order_bytes(tokens, experts, k, ranks))) return TUNA_ERR_WORKSPACE;
   o.hist = (uint16_t *)workspace;
   RouteArgs a = {};

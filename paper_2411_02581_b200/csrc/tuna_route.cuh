@@ -28,8 +28,10 @@ __device__ __forceinline__ void load_logits(const T *row, int first, int experts
 }
 
 // The choice for one token by its group of LPT lanes; lane s of the group leaves with slot s
-// (k <= LPT).  k rounds of an argmax: within a lane over its VPL values, then across lanes by
-// shuffles; ties go to the lower expert because a later one must be strictly larger.
+// (k <= LPT).  k rounds of an argmax: within a lane over its VPL values, then the group's largest
+// value, by shuffles or, where the group is the warp, in one instruction; the first lane that holds
+// it tells its expert.  Ties go to the lower expert: within a lane a later one must be strictly
+// larger, and lanes hold experts in order.
 template <int LPT, int VPL>
 __device__ __forceinline__ void choose(float (&z)[VPL], int lane, int k, int scoring, int renormalize, float scale, int &id, float &weight) {
   const int first = lane * VPL;
@@ -44,12 +46,15 @@ __device__ __forceinline__ void choose(float (&z)[VPL], int lane, int k, int sco
       if (z[i] > best && !((taken >> i) & 1)) best = z[i], at = i;
     }
     int e = first + at;
+    const float own = best;
+    if constexpr (LPT == 32) {
+      asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(best) : "f"(own));
+    } else {
 #pragma unroll
-    for (int d = 1; d < LPT; d <<= 1) {
-      const float ob = __shfl_xor_sync(~0u, best, d);
-      const int oe = __shfl_xor_sync(~0u, e, d);
-      if (ob > best || (ob == best && oe < e)) best = ob, e = oe;
+      for (int d = 1; d < LPT; d <<= 1) best = fmaxf(best, __shfl_xor_sync(~0u, best, d));
     }
+    const uint32_t holders = __ballot_sync(~0u, own == best) >> (threadIdx.x & (32 - LPT));
+    e = __shfl_sync(~0u, e, __ffs(holders) - 1, LPT);
     if (s == 0) top = best;
     if (best != -INFINITY) {  // (no early end: the other groups of the warp go on with the shuffles)
       if (e >= first && e < first + VPL) taken |= 1u << (e - first);
