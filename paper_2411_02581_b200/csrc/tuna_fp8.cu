@@ -167,15 +167,20 @@ __global__ void __launch_bounds__(256) tuna_quantize_tile_kernel(QuantArgs a) {
 // ---- the product -----------------------------------------------------------------------------
 //
 // A persistent block takes tiles of 128 x BN.  One warp copies 128 x 128 blocks of a and BN x
-// 128 blocks of b into a ring of stages; one thread issues the four tensor-core steps of a
+// 128 blocks of b into a ring of stages; one elected lane issues the four tensor-core steps of a
 // block into one of two accumulators in tensor memory; sixteen warps read a finished accumulator
 // back, multiply it by sa * sb and add it to the 32-bit sums they keep in registers (64 a
-// thread at BN = 256), while the tensor cores fill the other one.  The promotion is what bounds
-// the kernel: 256 cycles of packed multiply-adds a block at least, and the tensor-memory loads
-// in front of them.  Eight warps with 128 sums each had no registers left to load ahead (163 us
-// for 8192 x 4096 x 4096).  Two more warps fetch the scales, four blocks ahead, multiply them and
-// leave one factor a row and 128 columns beside each accumulator: loads, shuffles or asynchronous
-// copies of their own cost the promotion warps 500 cycles a block.
+// thread at BN = 256), while the tensor cores fill the other one.  Two more warps fetch the scales,
+// two blocks ahead, multiply them and leave one factor a row and 128 columns beside each
+// accumulator, and a tile's place with its first one: the promotion warps have no registers for either.
+//
+// What bounds it is the round of an accumulator: steps and commit 940 cycles, promotion 500 (256 of
+// packed multiply-adds at least), 200 back to the issuing lane; two accumulators fill the tensor
+// memory, so a block of k takes some 800 cycles, its four steps alone 542 at the nominal rate.
+// 8192 x 4096 x 4096: 121 us, 2270 TFLOP/s, in a burst; weight gradients (B_ROWS: a factor for
+// every column too) 152.  Eight warps of 128 sums had no registers left to load ahead (30 us more); a
+// lane that a branch picks moves every operand to uniform registers (6 us, with B_ROWS 20); scales
+// four blocks ahead and 16 columns a read spill (8 us).
 //
 // With `swiglu` the 256 columns are 4 x (32 gate + 32 up) rows of the two matrices, so that the
 // thread that holds a gate value holds its up value, and a tile is exactly one 128-block of the
