@@ -652,9 +652,9 @@ int run_tiles(const ProductArgs &p, cudaStream_t st, int parts = 1) {
   if (!a.error) return TUNA_ERR_CUDA;
   CUtensorMap ma, mb, mo;
   if (const int rc = make_map(&ma, 2, p.a, p.k, p.m, 1, p.lda, 128)) return rc;
-  // One copy of 32 KB for a block's gate and up rows, instead of eight of 4 KB that the issuing thread
-  // could not keep up with (64 experts of 4096 x 2048, 16384 rows: 471 us).  Its 32-row steps must not
-  // cross from one matrix into the next.
+  // One copy of 32 KB for a block's gate and up rows, instead of eight of 4 KB (64 experts of 4096 x 2048,
+  // 16384 rows, both products and what is around them: 649 us and 658, means of five).  Its 32-row steps
+  // must not cross from one matrix into the next.
   a.one_copy = SWIGLU && p.n % 32 == 0;
   if (a.one_copy) {
     if (const int rc = make_gate_up_map(&mb, p.b, p.k, p.n, p.groups, p.ldb)) return rc;

@@ -559,7 +559,7 @@ __global__ void __launch_bounds__(256) tuna_combine_grad_kernel(CombineArgs a) {
 // Chunks of 32 to 128 tokens (more where there were thousands of them), the smallest that leave two
 // blocks a multiprocessor or fewer: a warp chooses for its tokens one after the other (1024 tokens, 256
 // experts, 8 slots: 56.4 us in chunks of 128, 16.6 in chunks of 32).  The blocks of the order
-// kernel take as many chunks as keep their number near one a multiprocessor, since each of them
+// kernel take as many chunks as keep their number near one a multiprocessor, or four, since each of them
 // reads the whole table of counts.
 void plan_order(OrderArgs &o, int64_t tokens, int experts, int k, int ranks) {
   o.tokens = tokens, o.experts = experts, o.k = k, o.ranks = ranks;
@@ -569,7 +569,11 @@ void plan_order(OrderArgs &o, int64_t tokens, int experts, int k, int ranks) {
   while (chunk * k > 65535) chunk /= 2;  // 16 bits hold a chunk's count of one expert
   o.chunk = (int)chunk;
   o.rank_chunks = ceil_div(o.rank_tokens, chunk);
-  o.group = (int)ceil_div(o.rank_chunks * ranks, 148);
+  // Smaller groups where a rank's table of counts, which every block sums, is little beside a chunk's entries.
+  // (Blocks for 592 and for 148: 65536 tokens, 64 experts, 2 slots, 8 ranks 22.8 and 26.9 us; 128 experts, 8
+  // slots 63 and 87.  One rank, 16384 tokens, 64 experts, 2 slots 19.5 and 18.4; 256 experts, 8 slots 73 and 66.)
+  const bool little = o.rank_chunks * experts <= 64 * chunk * k;
+  o.group = (int)ceil_div(o.rank_chunks * ranks, little ? 592 : 148);
   o.rank_groups = ceil_div(o.rank_chunks, o.group);
 }
 
