@@ -5,12 +5,14 @@
 #include <Python.h>
 
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <dlfcn.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
+#include <optional>
 
 #include "tuna.h"
 
@@ -76,16 +78,39 @@ Tensor make(at::IntArrayRef shape, at::ScalarType type, const Tensor &like) {
   return at::detail::empty_cuda(shape, type, like.device(), std::nullopt);
 }
 
-void *stream_of(PyObject *o, const Tensor &t) {
-  if (o == Py_None) return c10::cuda::getCurrentCUDAStream(t.device().index()).stream();
-  if (PyLong_Check(o)) return PyLong_AsVoidPtr(o);
-  PyObject *s = PyObject_GetAttrString(o, "cuda_stream");
-  if (!s) throw Refused();
-  void *p = PyLong_AsVoidPtr(s);
-  Py_DECREF(s);
-  if (PyErr_Occurred()) throw Refused();
-  return p;
-}
+// Where a call runs: on the device of its tensors and on torch's current stream, or on the stream that was given,
+// which is torch's current one until the call returns.  Workspaces, copies and outputs then belong to the stream that
+// the kernels run on: what is freed at the end is taken again behind them, and no copy runs beside them.
+class Place {
+ public:
+  Place(PyObject *o, const Tensor &t) : device_(t.device()), before_(c10::cuda::getCurrentCUDAStream(t.device().index())), at_(before_) {
+    if (o == Py_None) return;
+    cudaStream_t raw = (cudaStream_t)handle(o);
+    if (raw == cudaStreamLegacy) raw = nullptr;  // torch's name of the same stream
+    if (raw == before_.stream()) return;
+    at_ = c10::cuda::getStreamFromExternal(raw, t.device().index());
+    guard_.emplace(at_);
+  }
+  void *stream() const { return at_.stream(); }
+  // An output on its way to the caller, who may use and free it on the stream that was current before.
+  const Tensor &out(const Tensor &t) const {
+    if (guard_) c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), before_);
+    return t;
+  }
+
+ private:
+  static void *handle(PyObject *o) {
+    PyObject *s = PyLong_Check(o) ? Py_NewRef(o) : PyObject_GetAttrString(o, "cuda_stream");
+    if (!s) throw Refused();
+    void *p = PyLong_AsVoidPtr(s);
+    Py_DECREF(s);
+    if (PyErr_Occurred()) throw Refused();
+    return p;
+  }
+  c10::cuda::CUDAGuard device_;
+  c10::cuda::CUDAStream before_, at_;
+  std::optional<c10::cuda::CUDAStreamGuard> guard_;
+};
 
 int64_t integer(PyObject *o) {
   const int64_t v = PyLong_AsLongLong(o);
@@ -153,7 +178,7 @@ PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const int64_t ld = matrix(z, "logits", true, true, false), t = z.size(0), e = z.size(1), k = integer(a[1]), ranks = integer(a[5]);
     if (ranks < 1 || t % ranks) refuse("%lld tokens do not divide over %lld ranks", (long long)t, (long long)ranks);
     size_t need = 0;
-    const c10::cuda::CUDAGuard device(z.device());
+    const Place place(a[6], z);
     check(p_tuna_moe_route_workspace_bytes(t, clip(e), clip(k), clip(ranks), &need), "tuna_moe_route_workspace_bytes");
     Tensor ws;
     if (need) ws = make({(int64_t)need}, at::kByte, z);
@@ -161,9 +186,9 @@ PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n) {
                  offsets = make({ranks * e + 1}, at::kLong, z), rows = make({t * k}, at::kLong, z), pos = make({t, k}, at::kLong, z);
     check(p_tuna_moe_route(at_of(z), dtype_of(z), t, clip(e), ld, clip(k), clip(ranks), small(a[2]), truth(a[3]), (float)number(a[4]),
                            (int32_t *)at_of(ids), (float *)at_of(weights), (int64_t *)at_of(counts), (int64_t *)at_of(offsets),
-                           (int64_t *)at_of(rows), (int64_t *)at_of(pos), need ? at_of(ws) : nullptr, need, stream_of(a[6], z)),
+                           (int64_t *)at_of(rows), (int64_t *)at_of(pos), need ? at_of(ws) : nullptr, need, place.stream()),
           "tuna_moe_route");
-    return pack(ids, weights, counts, offsets, rows, pos);
+    return pack(place.out(ids), place.out(weights), place.out(counts), place.out(offsets), place.out(rows), place.out(pos));
   });
 }
 
@@ -176,12 +201,12 @@ PyObject *route_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const int64_t k = ids.size(1);
     dense(ids, "ids", at::kInt, {t, k}, z);
     dense(dw, "dweights", at::kFloat, {t, k}, z);
-    const c10::cuda::CUDAGuard device(z.device());
+    const Place place(a[6], z);
     const Tensor d = make({t, e}, z.scalar_type(), z);
     check(p_tuna_moe_route_backward(at_of(z), dtype_of(z), t, clip(e), ld, clip(k), small(a[3]), truth(a[4]), (float)number(a[5]),
-                                    (const int32_t *)at_of(ids), (const float *)at_of(dw), at_of(d), e, stream_of(a[6], z)),
+                                    (const int32_t *)at_of(ids), (const float *)at_of(dw), at_of(d), e, place.stream()),
           "tuna_moe_route_backward");
-    return THPVariable_Wrap(d);
+    return THPVariable_Wrap(place.out(d));
   });
 }
 
@@ -194,12 +219,13 @@ PyObject *fp8_quantize(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const bool turned = layout == TUNA_FP8_COLUMNS || layout == TUNA_FP8_TILES_T, tiles = layout >= TUNA_FP8_TILES;
     const int64_t out_rows = turned ? cols : rows, out_cols = turned ? rows : cols, pitch = (out_cols + 15) / 16 * 16;
     const int64_t blocks = (out_cols + 127) / 128;
-    const c10::cuda::CUDAGuard device(x.device());
+    const Place place(a[2], x);
     Tensor q = make({out_rows, pitch}, at::kFloat8_e4m3fn, x);
     const Tensor scale = tiles ? make({(out_rows + 127) / 128, blocks}, at::kFloat, x) : make({blocks, out_rows}, at::kFloat, x);
     check(p_tuna_fp8_quantize(at_of(x), dtype_of(x), rows, clip(cols), ld, layout, at_of(q), std::max<int64_t>(pitch, 16),
-                              (float *)at_of(scale), stream_of(a[2], x)),
+                              (float *)at_of(scale), place.stream()),
           "tuna_fp8_quantize");
+    place.out(q), place.out(scale);
     return pack(pitch == out_cols ? q : q.narrow(1, 0, out_cols), scale);
   });
 }
@@ -222,7 +248,7 @@ Tensor operand(const Tensor &q, const char *name, int64_t &ld) {
 PyObject *fp8_matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return guarded(n, 8, [&] {
     const Tensor &left = tensor(a[0], "a"), &sa = tensor(a[1], "a_scale"), &right = tensor(a[2], "b"), &sb = tensor(a[3], "b_scale");
-    const c10::cuda::CUDAGuard device(left.device());
+    const Place place(a[7], left);
     int64_t lda = 0, ldb = 0, groups = 1, cols, kb;
     const Tensor x = operand(left, "a", lda);
     const int64_t m = left.size(0), k = left.size(1), blocks = (k + 127) / 128;
@@ -252,9 +278,9 @@ PyObject *fp8_matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (right.device() != left.device()) refuse("b: on another device than its fellow");
     const Tensor y = make({m, cols}, out == TUNA_DTYPE_F32 ? at::kFloat : at::kBFloat16, left);
     check(p_tuna_fp8_matmul(at_of(x), (const float *)at_of(sa), m, lda, at_of(w), (const float *)at_of(sb), layout, clip(cols), ldb, clip(k),
-                            clip(groups), offsets, at_of(y), out, std::max<int64_t>(cols, 1), stream_of(a[7], left)),
+                            clip(groups), offsets, at_of(y), out, std::max<int64_t>(cols, 1), place.stream()),
           "tuna_fp8_matmul");
-    return THPVariable_Wrap(y);
+    return THPVariable_Wrap(place.out(y));
   });
 }
 
@@ -295,15 +321,15 @@ PyObject *few(PyObject *, PyObject *const *a, Py_ssize_t n) {
     }
     const Tensor &ws = tensor(a[12], "workspace");
     if (!ws.is_contiguous()) refuse("workspace: a contiguous tensor is wanted");
-    const c10::cuda::CUDAGuard device(given.device());
+    const Place place(a[13], given);
     Tensor x = given;
     if (ld % 8 || (uintptr_t)given.data_ptr() % 16) x = given.clone(at::MemoryFormat::Contiguous), ld = d;
     const Tensor out = make({t, d}, at::kBFloat16, given);
     check(p_tuna_moe_few(at_of(x), ld, clip(t), at_of(router), clip(e), clip(k), small(a[7]), truth(a[8]), (float)number(a[9]), clip(d), clip(i),
                          fp8 ? TUNA_DTYPE_E4M3 : TUNA_DTYPE_BF16, at_of(w13), s13, at_of(w2), s2, at_of(out), std::max<int64_t>(d, 1), ids, weights,
-                         at_of(ws), (size_t)ws.nbytes(), stream_of(a[13], given)),
+                         at_of(ws), (size_t)ws.nbytes(), place.stream()),
           "tuna_moe_few");
-    return THPVariable_Wrap(out);
+    return THPVariable_Wrap(place.out(out));
   });
 }
 

@@ -5,12 +5,14 @@ A thin layer over the C ABI in ``include/tuna.h``, like :mod:`binding`: argument
 checked and marshalled, outputs and workspaces come from torch's allocator, every
 computation runs in the CUDA library (there is no CPU fallback).  The calls of a decode
 step are marshalled in C++ (``csrc/tuna_torch.cpp``), where ctypes and the interpreter
-would take longer than their kernels.  Work is enqueued on
-``stream`` (default: torch's current one).  A tensor that was made on another stream is
-the caller's to order, as with any torch operation.
+would take longer than their kernels.  Work is enqueued on ``stream`` (default: torch's
+current one), which is torch's current stream until the call returns: outputs, workspaces
+and copies are its own.  An input that was made on another stream is the caller's to
+order, as with any torch operation, and so is an output before another stream reads it.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import importlib.util
@@ -39,11 +41,29 @@ class Routing(NamedTuple):
     pos: torch.Tensor      # int64 [tokens, k]
 
 
-def _stream(stream, device):
-    """The raw stream: torch's current one of the tensors' device, or the caller's."""
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(device.index)
-    return B._stream(stream)
+def _same(*tensors):
+    return tensors if len(tensors) > 1 else tensors[0]
+
+
+@contextlib.contextmanager
+def _on(stream, device):
+    """Makes ``stream`` torch's current one for a whole call, so that what is allocated and filled on
+    the way belongs to it.  Yields the raw stream and what outputs leave through: the caller may use
+    and free them on the stream that was current before."""
+    before = torch._C._cuda_getCurrentRawStream(device.index)
+    at = before if stream is None else B._stream(stream)
+    at = 0 if at == 1 else at  # cudaStreamLegacy: torch's name of the same stream is 0
+    if at == before:
+        yield at, _same
+        return
+    was = torch.cuda.current_stream(device)
+
+    def out(*tensors):
+        for t in tensors:
+            t.record_stream(was)
+        return _same(*tensors)
+    with torch.cuda.stream(torch.cuda.ExternalStream(at, device=device)):
+        yield at, out
 
 
 def _check(rc, what):
@@ -123,11 +143,12 @@ def order(ids, experts, *, ranks=1, stream=None):
     _dense(ids, "ids", torch.int32, (t, k))
     if ranks < 1 or t % ranks:
         raise ValueError(f"{t} tokens do not divide over {ranks} ranks")
-    ws = _order_workspace(t, experts, k, ranks, ids.device)
-    out = _order_outputs(t, experts, k, ranks, ids.device)
-    _check(B.lib().tuna_moe_order(ids.data_ptr(), t, experts, k, ranks, *[o.data_ptr() for o in out], ws.data_ptr(), ws.numel(),
-                                  _stream(stream, ids.device)), "tuna_moe_order")
-    return out
+    with _on(stream, ids.device) as (at, out):
+        ws = _order_workspace(t, experts, k, ranks, ids.device)
+        made = _order_outputs(t, experts, k, ranks, ids.device)
+        _check(B.lib().tuna_moe_order(ids.data_ptr(), t, experts, k, ranks, *[o.data_ptr() for o in made], ws.data_ptr(), ws.numel(), at),
+               "tuna_moe_order")
+        return out(*made)
 
 
 def route_backward(logits, ids, dweights, *, scoring="softmax", renormalize=False, scale=1.0, stream=None):
@@ -143,10 +164,11 @@ def combine(y, weights, pos, *, out_dtype=torch.bfloat16, stream=None):
     _dense(pos, "pos", torch.int64, (t, k))
     if out_dtype not in FLOATS:
         raise ValueError(f"out_dtype: one of {FLOATS}")
-    out = torch.empty(t, y.shape[1], dtype=out_dtype, device=y.device)
-    _check(B.lib().tuna_moe_combine(y.data_ptr(), DTYPES[y.dtype], y.shape[0], y.shape[1], ld, weights.data_ptr(), pos.data_ptr(), t, k,
-                                    out.data_ptr(), DTYPES[out_dtype], y.shape[1], _stream(stream, y.device)), "tuna_moe_combine")
-    return out
+    with _on(stream, y.device) as (at, out):
+        o = torch.empty(t, y.shape[1], dtype=out_dtype, device=y.device)
+        _check(B.lib().tuna_moe_combine(y.data_ptr(), DTYPES[y.dtype], y.shape[0], y.shape[1], ld, weights.data_ptr(), pos.data_ptr(), t, k,
+                                        o.data_ptr(), DTYPES[out_dtype], y.shape[1], at), "tuna_moe_combine")
+        return out(o)
 
 
 def combine_backward(dout, y, weights, pos, *, stream=None):
@@ -157,12 +179,13 @@ def combine_backward(dout, y, weights, pos, *, stream=None):
     _dense(pos, "pos", torch.int64, (t, k))
     if tuple(dout.shape) != (t, y.shape[1]):
         raise ValueError(f"dout: shape {tuple(dout.shape)}, wanted {(t, y.shape[1])}")
-    dy = torch.zeros(y.shape, dtype=y.dtype, device=y.device)
-    dw = torch.zeros_like(weights)
-    _check(B.lib().tuna_moe_combine_backward(dout.data_ptr(), DTYPES[dout.dtype], ldg, y.data_ptr(), DTYPES[y.dtype], y.shape[0],
-                                             y.shape[1], ldy, weights.data_ptr(), pos.data_ptr(), t, k, dy.data_ptr(), y.shape[1],
-                                             dw.data_ptr(), _stream(stream, y.device)), "tuna_moe_combine_backward")
-    return dy, dw
+    with _on(stream, y.device) as (at, out):
+        dy = torch.zeros(y.shape, dtype=y.dtype, device=y.device)
+        dw = torch.zeros_like(weights)
+        _check(B.lib().tuna_moe_combine_backward(dout.data_ptr(), DTYPES[dout.dtype], ldg, y.data_ptr(), DTYPES[y.dtype], y.shape[0],
+                                                 y.shape[1], ldy, weights.data_ptr(), pos.data_ptr(), t, k, dy.data_ptr(), y.shape[1],
+                                                 dw.data_ptr(), at), "tuna_moe_combine_backward")
+        return out(dy, dw)
 
 
 def _blocks(n):
@@ -216,11 +239,12 @@ def expert_rows(x, offsets, w13, s13, w2, s2, *, workspace=None, stream=None):
     rows, d = x.shape
     e, i = _experts_weights(w13, s13, w2, s2, d)
     _dense(offsets, "offsets", torch.int64, (e + 1,))
-    ws = _space(_bytes("tuna_moe_expert_rows_workspace_bytes", rows, d, i), workspace, x.device)
-    y = torch.empty(rows, d, dtype=torch.bfloat16, device=x.device)
-    _check(B.lib().tuna_moe_expert_rows(x.data_ptr(), ldx, rows, e, offsets.data_ptr(), d, i, w13.data_ptr(), s13.data_ptr(), w2.data_ptr(),
-                                        s2.data_ptr(), y.data_ptr(), d, ws.data_ptr(), ws.numel(), _stream(stream, x.device)), "tuna_moe_expert_rows")
-    return y
+    with _on(stream, x.device) as (at, out):
+        ws = _space(_bytes("tuna_moe_expert_rows_workspace_bytes", rows, d, i), workspace, x.device)
+        y = torch.empty(rows, d, dtype=torch.bfloat16, device=x.device)
+        _check(B.lib().tuna_moe_expert_rows(x.data_ptr(), ldx, rows, e, offsets.data_ptr(), d, i, w13.data_ptr(), s13.data_ptr(), w2.data_ptr(),
+                                            s2.data_ptr(), y.data_ptr(), d, ws.data_ptr(), ws.numel(), at), "tuna_moe_expert_rows")
+        return out(y)
 
 
 def experts(x, ids, weights, w13, s13, w2, s2, *, workspace=None, stream=None):
@@ -231,12 +255,12 @@ def experts(x, ids, weights, w13, s13, w2, s2, *, workspace=None, stream=None):
     k = ids.shape[-1]
     _dense(ids, "ids", torch.int32, (t, k))
     _dense(weights, "weights", torch.float32, (t, k))
-    ws = _space(_bytes("tuna_moe_experts_workspace_bytes", t, e, k, d, i), workspace, x.device)
-    out = torch.empty(t, d, dtype=torch.bfloat16, device=x.device)
-    _check(B.lib().tuna_moe_experts(x.data_ptr(), ldx, t, ids.data_ptr(), weights.data_ptr(), k, e, d, i, w13.data_ptr(), s13.data_ptr(),
-                                    w2.data_ptr(), s2.data_ptr(), out.data_ptr(), d, ws.data_ptr(), ws.numel(), _stream(stream, x.device)),
-           "tuna_moe_experts")
-    return out
+    with _on(stream, x.device) as (at, out):
+        ws = _space(_bytes("tuna_moe_experts_workspace_bytes", t, e, k, d, i), workspace, x.device)
+        o = torch.empty(t, d, dtype=torch.bfloat16, device=x.device)
+        _check(B.lib().tuna_moe_experts(x.data_ptr(), ldx, t, ids.data_ptr(), weights.data_ptr(), k, e, d, i, w13.data_ptr(), s13.data_ptr(),
+                                        w2.data_ptr(), s2.data_ptr(), o.data_ptr(), d, ws.data_ptr(), ws.numel(), at), "tuna_moe_experts")
+        return out(o)
 
 
 @functools.lru_cache(maxsize=4096)
@@ -267,14 +291,13 @@ def few(x, router, k, w13, w2, *, s13=None, s2=None, scoring="softmax", renormal
     if workspace is None:
         t, d = x.shape
         e, i = router.shape[0], w13.shape[2]
-        at = _stream(stream, x.device)
-        kept = _few_spaces.setdefault((x.device.index, at), [])
-        if not kept or kept[-1].numel() < _few_bytes(t, e, k, d, i)[0]:
-            if torch.cuda.is_current_stream_capturing():
-                raise RuntimeError("few: pass a workspace (few_workspace) when the first call of this size is captured")
-            with torch.cuda.stream(torch.cuda.ExternalStream(at, device=x.device)):
+        with _on(stream, x.device) as (at, _):
+            kept = _few_spaces.setdefault((x.device.index, at), [])
+            if not kept or kept[-1].numel() < _few_bytes(t, e, k, d, i)[0]:
+                if torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("few: pass a workspace (few_workspace) when the first call of this size is captured")
                 kept.append(few_workspace(t, e, k, d, i, x.device))
-        workspace = kept[-1]
+            workspace = kept[-1]
     return (_marshal or _fast()).few(x, router, k, w13, w2, s13, s2, _scoring(scoring), renormalize, scale, ids, weights, workspace, stream)
 
 
