@@ -278,7 +278,21 @@ def few_workspace(tokens, experts, k, hidden, inter, device="cuda"):
     return ws
 
 
-_few_spaces = {}  # (device, stream) -> workspaces that few() keeps: the last one serves, older ones may be held by graphs
+_few_spaces = {}  # (device, stream) -> the workspace that eager calls of few() share there, one after the other
+
+
+def _few_space(x, router, k, w13, at):
+    """The workspace of a call on the stream ``at``, which is torch's current one.  A captured call gets one
+    of its own out of the graph's memory, zeroed at each replay: a graph may be replayed on any stream, beside
+    other graphs and eager calls."""
+    t, d = x.shape
+    sizes = t, router.shape[0], k, d, w13.shape[2]
+    if torch.cuda.is_current_stream_capturing():
+        return few_workspace(*sizes, x.device)
+    kept = _few_spaces.get((x.device.index, at))
+    if kept is None or kept.numel() < _few_bytes(*sizes)[0]:
+        kept = _few_spaces[x.device.index, at] = few_workspace(*sizes, x.device)
+    return kept
 
 
 def few(x, router, k, w13, w2, *, s13=None, s2=None, scoring="softmax", renormalize=False, scale=1.0, ids=None, weights=None,
@@ -287,17 +301,12 @@ def few(x, router, k, w13, w2, *, s13=None, s2=None, scoring="softmax", renormal
 
     ``w13`` [experts, 2, inter, hidden] and ``w2`` [experts, hidden, inter] in bf16, or in
     e4m3 with ``s13`` and ``s2``.  ``ids`` / ``weights``: optional outputs [tokens, k].
-    ``workspace``: from :func:`few_workspace`; without one the module keeps one a stream."""
+    ``workspace``: from :func:`few_workspace`, of one call at a time.  Without one, the calls on a stream
+    share one that the module keeps, as large as the largest of them needed, and each call that
+    ``torch.cuda.graph`` captures has its own; who captures by other means passes one."""
     if workspace is None:
-        t, d = x.shape
-        e, i = router.shape[0], w13.shape[2]
         with _on(stream, x.device) as (at, _):
-            kept = _few_spaces.setdefault((x.device.index, at), [])
-            if not kept or kept[-1].numel() < _few_bytes(t, e, k, d, i)[0]:
-                if torch.cuda.is_current_stream_capturing():
-                    raise RuntimeError("few: pass a workspace (few_workspace) when the first call of this size is captured")
-                kept.append(few_workspace(t, e, k, d, i, x.device))
-            workspace = kept[-1]
+            workspace = _few_space(x, router, k, w13, at)
     return (_marshal or _fast()).few(x, router, k, w13, w2, s13, s2, _scoring(scoring), renormalize, scale, ids, weights, workspace, stream)
 
 

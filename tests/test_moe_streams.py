@@ -118,3 +118,55 @@ def test_stream_arguments_that_are_none():
         for a, b in zip(want, moe.route(z, 2, stream=stream)):
             assert torch.equal(a, b)
         assert torch.equal(moe.combine(z, want.weights, want.pos.clamp(max=299), stream=stream), moe.combine(z, want.weights, want.pos.clamp(max=299)))
+
+
+@pytest.mark.parametrize("how", ["current", "given"])
+def test_captured_few_has_a_workspace_of_its_own(how):
+    """A graph may be replayed on any stream, so it must not count on the workspace that eager calls on the stream
+    of its capture share: its replays leave that one alone, whether the capturing stream is the current or a given one."""
+    from paper_2411_02581_b200 import moe
+    e, k, d, i = 16, 2, 256, 128
+    router, w13, w2 = bf16_weights(1, e, d, 6)[0], bf16_weights(2 * e, i, d, 7).view(e, 2, i, d), bf16_weights(e, d, i, 8)
+    xs = [activations(t, d, t).cuda() for t in (5, 40)]
+    want = [moe.few(x, router, k, w13, w2) for x in xs]
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    moe.few(xs[1], router, k, w13, w2, stream=side)               # an eager call on the stream that will capture
+    kept = moe._few_spaces[torch.cuda.current_device(), side.cuda_stream]
+    torch.cuda.synchronize()
+    graphs, outs = [torch.cuda.CUDAGraph() for _ in xs], []
+    for graph, x in zip(graphs, xs):
+        with torch.cuda.graph(graph, stream=side):
+            if how == "current":
+                outs.append(moe.few(x, router, k, w13, w2))
+            else:
+                with torch.cuda.stream(other):
+                    outs.append(moe.few(x, router, k, w13, w2, stream=side))
+    was = kept.clone()
+    for out in outs:
+        out.zero_()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for graph, on in zip(graphs, (side, other)):
+            with torch.cuda.stream(on):
+                graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(kept, was)
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    again = moe.few(xs[0], router, k, w13, w2, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(again, want[0])
+    assert moe.device_status() == 0
+
+
+def test_few_keeps_one_workspace_a_stream():
+    from paper_2411_02581_b200 import moe
+    e, k, d, i = 16, 2, 256, 128
+    router, w13, w2 = bf16_weights(1, e, d, 6)[0], bf16_weights(2 * e, i, d, 7).view(e, 2, i, d), bf16_weights(e, d, i, 8)
+    want = moe.few(activations(1, d, 1).cuda(), router, k, w13, w2)
+    sizes = []
+    for t in (64, 3, 64, 1):
+        x = activations(t, d, t).cuda()
+        got = moe.few(x, router, k, w13, w2)
+        sizes.append(moe._few_spaces[torch.cuda.current_device(), torch.cuda.current_stream().cuda_stream])
+    assert all(s is sizes[0] for s in sizes) and torch.equal(got, want)
