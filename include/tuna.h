@@ -655,9 +655,8 @@ int tuna_moe_experts(const void *x, int64_t ldx, int64_t tokens, const int32_t *
  *            (then only the weights are in 8 bits: x and h keep at least bf16's precision).
  *   ids, weights   tokens x k, receive the choice; may be NULL.
  * The first `zeroed` bytes of the workspace must be zero before its first use and belong
- * to the calls from then on (after a call that gave up a wait, see tuna_ops_device_status,
- * they must be zeroed again).  A workspace may serve calls of other sizes if it is large
- * enough, one call at a time.
+ * to the calls from then on, also behind one that gave up a wait (tuna_ops_device_status).
+ * A workspace may serve calls of other sizes if it is large enough, one call at a time.
  * Limits (TUNA_ERR_RANGE): tokens <= TUNA_MOE_FEW_MAX_TOKENS, hidden, inter <= 8192.
  */
 #define TUNA_MOE_FEW_MAX_TOKENS 64

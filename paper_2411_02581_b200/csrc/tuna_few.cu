@@ -100,15 +100,17 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
 // All blocks of the grid meet: one thread arrives for its block (after a barrier of the block), any
 // thread may wait.  The counter only grows, by the grid's size at each meeting, so that an arrival is one
 // addition and a wait one load (with a generation word that the last block advances, one token took 34 us
-// instead of 30).  64 bits never wrap.
+// instead of 30).  64 bits never wrap.  A block adds kMeetings to it in every call, also one that gave up a wait:
+// the count is then a multiple of the grid's size after every call, and the next one finds its base.
+constexpr int kMeetings = 3;
 __device__ __forceinline__ unsigned long long meeting_base(const unsigned long long *bar) {
   // read before this block's first arrival: the count is then short of the next multiple
   unsigned long long v;
   asm volatile("ld.relaxed.gpu.global.u64 %0, [%1];" : "=l"(v) : "l"(bar) : "memory");
   return v - v % gridDim.x;
 }
-__device__ __forceinline__ void grid_arrive(unsigned long long *bar) {
-  asm volatile("red.release.gpu.global.add.u64 [%0], 1;" ::"l"(bar) : "memory");
+__device__ __forceinline__ void grid_arrive(unsigned long long *bar, unsigned long long times = 1) {
+  asm volatile("red.release.gpu.global.add.u64 [%0], %1;" ::"l"(bar), "l"(times) : "memory");
 }
 __device__ bool grid_wait(const unsigned long long *bar, unsigned long long target, volatile int *given_up) {
   const long long t0 = clock64();
@@ -235,6 +237,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
   bool fine = grid_meet(a.barrier, base + gridDim.x, &l.given_up);
+  int met = 1;  // meetings that this block has arrived at
 
   if (fine) {
     // ---- the choice, by every block for itself; the fewer experts, the more tokens a warp takes
@@ -629,12 +632,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (up) {
         // the next product's weights are on their way while the blocks' sums meet
         if (tid == 0) grid_arrive(a.barrier);
+        met = 2;
       }
     }
     // (a block without units has not waited for the second meeting: it must not arrive at the third before)
     if (tid == 0 && !l.given_up) grid_wait(a.barrier, base + 2ull * gridDim.x, &l.given_up);
     __syncthreads();
-    fine = !*(volatile int *)&l.given_up && grid_meet(a.barrier, base + 3ull * gridDim.x, &l.given_up);
+    fine = !*(volatile int *)&l.given_up;
+    if (fine) fine = grid_meet(a.barrier, base + 3ull * gridDim.x, &l.given_up), met = kMeetings;
   }
 
   // ---- the weighted sum, slots and segments in order
@@ -662,7 +667,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   __syncthreads();
   if (warp == 2) tmem_free(l.tmem, kBufs * kBufCols);
-  if (tid == 0 && *(volatile int *)&l.given_up) *a.error = 1;
+  if (tid == 0) {
+    if (*(volatile int *)&l.given_up) *a.error = 1;
+    if (met < kMeetings) grid_arrive(a.barrier, kMeetings - met);
+  }
 }
 
 // Blocks of a segment: as long as possible (fewer partial sums), while some five units a block are
