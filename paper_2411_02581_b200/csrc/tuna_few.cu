@@ -78,7 +78,7 @@ struct Lists {
   alignas(16) float piece_scale[2][8][kTile];  // s of the token operand: operand, block, token
   int16_t entry[kMaxEntries];         // token * k + slot, by expert
   Group group[kMaxGroups];
-  int groups, given_up;
+  int groups, given_up, met;  // met: meetings that the block has arrived at
   uint32_t tmem;
 };
 // What is needed only until the lists are made: lies where the stages are later.
@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int T = a.tokens, E = a.experts, K = a.k, D = a.hidden, I = a.inter, n = T * K;
   const int splits = (D + kSplit - 1) / kSplit;
   if (tid == 0) {
-    l.given_up = 0;
+    l.given_up = 0, l.met = 1;
     for (int i = 0; i < kStages; ++i) mbar_init(smem_u32(l.full + i), 1), mbar_init(smem_u32(l.empty + i), 1);
     for (int i = 0; i < kBufs; ++i) mbar_init(smem_u32(l.done + i), 1), mbar_init(smem_u32(l.freed + i), 4);
     for (int i = 0; i < 2; ++i) mbar_init(smem_u32(l.laid + i), kLoaders), mbar_init(smem_u32(l.used + i), 5);
@@ -237,7 +237,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
   bool fine = grid_meet(a.barrier, base + gridDim.x, &l.given_up);
-  int met = 1;  // meetings that this block has arrived at
 
   if (fine) {
     // ---- the choice, by every block for itself; the fewer experts, the more tokens a warp takes
@@ -355,13 +354,6 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (++stage == kStages) stage = 0, stage_phase ^= 1;
             }
           }
-          if (!ok) {  // given up: nothing may land in shared memory after the block has gone
-            int never = 0;
-            for (int i = 0; i < kStages; ++i) {  // the stages before the one that was waited for, oldest first
-              const int at = (stage + i) % kStages, of = stage_phase ^ (stage + i < kStages ? 1 : 0);
-              mbar_wait(smem_u32(l.full + at), of, &never);
-            }
-          }
         }
       } else if (warp == 1) {
         // -- tensor cores (the whole warp walks, one lane issues)
@@ -405,11 +397,6 @@ __global__ void __launch_bounds__(kThreads, 1)
               __syncwarp();
               if (++op == 2) op = 0, op_phase ^= 1;
             }
-          }
-          if (!ok) {
-            int never = 0;
-            if (elect_one()) tc_commit(smem_u32(&l.drained));
-            mbar_wait(smem_u32(&l.drained), 0, &never);
           }
         }
       } else if (warp >= 4 && warp < 8) {
@@ -628,18 +615,30 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       __syncwarp();
       __syncthreads();
-      if (*(volatile int *)&l.given_up) break;
+      if (*(volatile int *)&l.given_up) {
+        // Whichever warp it was: nothing may land in shared memory after the block has gone, so the last copies are
+        // waited for (oldest first), and no step may be under way when tensor memory is freed.
+        int never = 0;
+        if (tid == 0) {
+          for (int i = 0; i < kStages; ++i)
+            mbar_wait(smem_u32(l.full + (stage + i) % kStages), stage_phase ^ (stage + i < kStages ? 1 : 0), &never);
+        } else if (warp == 1) {
+          if (elect_one()) tc_commit(smem_u32(&l.drained));
+          __syncwarp();
+          mbar_wait(smem_u32(&l.drained), 0, &never);
+        }
+        break;
+      }
       if (up) {
         // the next product's weights are on their way while the blocks' sums meet
-        if (tid == 0) grid_arrive(a.barrier);
-        met = 2;
+        if (tid == 0) grid_arrive(a.barrier), l.met = 2;
       }
     }
     // (a block without units has not waited for the second meeting: it must not arrive at the third before)
     if (tid == 0 && !l.given_up) grid_wait(a.barrier, base + 2ull * gridDim.x, &l.given_up);
     __syncthreads();
-    fine = !*(volatile int *)&l.given_up;
-    if (fine) fine = grid_meet(a.barrier, base + 3ull * gridDim.x, &l.given_up), met = kMeetings;
+    if (tid == 0 && !l.given_up) l.met = kMeetings;
+    fine = !*(volatile int *)&l.given_up && grid_meet(a.barrier, base + 3ull * gridDim.x, &l.given_up);
   }
 
   // ---- the weighted sum, slots and segments in order
@@ -669,7 +668,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 2) tmem_free(l.tmem, kBufs * kBufCols);
   if (tid == 0) {
     if (*(volatile int *)&l.given_up) *a.error = 1;
-    if (met < kMeetings) grid_arrive(a.barrier, kMeetings - met);
+    if (l.met < kMeetings) grid_arrive(a.barrier, kMeetings - l.met);
   }
 }
 

@@ -328,11 +328,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           if (++stage == S::kStages) stage = 0, phase ^= 1;
         }
       }
-      if (!ok) {  // given up: nothing may land in shared memory after the block has gone
-        int never = 0;
-        for (int64_t i = max((int64_t)0, issued - S::kStages); i < issued; ++i)
-          mbar_wait(full + 8 * (int)(i % S::kStages), (uint32_t)((i / S::kStages) & 1), &never);
-      }
+      // nothing may land in shared memory after the block has gone, whichever warp gives up: the last copies are waited for
+      int never = 0;
+      for (int64_t i = max((int64_t)0, issued - S::kStages); i < issued; ++i)
+        mbar_wait(full + 8 * (int)(i % S::kStages), (uint32_t)((i / S::kStages) & 1), &never);
     } else if (warp == 1) {
       // ---- tensor cores: the whole warp goes along, one lane issues
       constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);  // f32 sums of e4m3 products
@@ -355,12 +354,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           if (++buf == 2) buf = 0, buf_phase ^= 1;
         }
       }
-      if (!ok) {
-        int never = 0;
-        if (elect_one()) tc_commit(drained);
-        __syncwarp();
-        mbar_wait(drained, 0, &never);
-      }
+      // and no step may be under way when tensor memory is freed
+      int never = 0;
+      if (elect_one()) tc_commit(drained);
+      __syncwarp();
+      mbar_wait(drained, 0, &never);
     } else if (warp >= 2) {
       // ---- scales: a lane has two rows of the tile, and with B_ROWS four columns
       constexpr int kAhead = 2, kVals = B_ROWS ? 6 : 4;
