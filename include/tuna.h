@@ -669,7 +669,8 @@ int tuna_moe_few(const void *x, int64_t ldx, int tokens, const void *router, int
                  void *workspace, size_t workspace_bytes, void *stream);
 
 /* Synchronises the device and reports in *gave_up (host) whether a kernel of these operators
- * abandoned a bounded wait; its outputs are then incomplete.  tuna_ops_cuda_error: the
+ * abandoned a bounded wait since the last such report; the outputs of calls in between are
+ * then incomplete, later calls are not affected.  tuna_ops_cuda_error: the
  * cudaError_t behind this thread's latest TUNA_ERR_CUDA of these operators. */
 int tuna_ops_device_status(int *gave_up);
 int tuna_ops_cuda_error(void);

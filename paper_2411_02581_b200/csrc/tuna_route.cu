@@ -790,7 +790,8 @@ int tuna_ops_device_status(int *gave_up) {
   int *word = error_word();
   if (!word) return TUNA_ERR_CUDA;
   if (const int rc = note_cuda(cudaDeviceSynchronize())) return rc;
-  return note_cuda(cudaMemcpy(gave_up, word, sizeof(int), cudaMemcpyDeviceToHost));
+  if (const int rc = note_cuda(cudaMemcpy(gave_up, word, sizeof(int), cudaMemcpyDeviceToHost))) return rc;
+  return *gave_up ? note_cuda(cudaMemset(word, 0, sizeof(int))) : TUNA_OK;  // the next report is of later calls
 }
 
 int tuna_ops_cuda_error(void) { return t_cuda_error; }

@@ -311,7 +311,8 @@ def few(x, router, k, w13, w2, *, s13=None, s2=None, scoring="softmax", renormal
 
 
 def device_status() -> int:
-    """0, or 1 if a kernel of these operators gave up a bounded wait (synchronises the device)."""
+    """0, or 1 if a kernel of these operators gave up a bounded wait since the last such call: what it made is
+    incomplete, what comes later is not affected (synchronises the device)."""
     n = ctypes.c_int()
     _check(B.lib().tuna_ops_device_status(ctypes.byref(n)), "tuna_ops_device_status")
     return n.value
