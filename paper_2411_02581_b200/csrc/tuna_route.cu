@@ -560,7 +560,7 @@ __global__ void __launch_bounds__(256) tuna_combine_grad_kernel(CombineArgs a) {
 // blocks a multiprocessor or fewer: a warp chooses for its tokens one after the other (1024 tokens, 256
 // experts, 8 slots: 56.4 us in chunks of 128, 16.6 in chunks of 32).  The blocks of the order
 // kernel take as many chunks as keep their number near one a multiprocessor, or four, since each of them
-// reads the whole table of counts.
+// reads the whole table of counts.  (tokens > 0: there is nothing to cut otherwise.)
 void plan_order(OrderArgs &o, int64_t tokens, int experts, int k, int ranks) {
   o.tokens = tokens, o.experts = experts, o.k = k, o.ranks = ranks;
   o.rank_tokens = tokens / ranks;
@@ -654,8 +654,9 @@ size_t dtype_size(int dtype) { return dtype == TUNA_DTYPE_F32 ? 4 : dtype == TUN
 
 }  // namespace
 
-// The order from ids in memory, for the operators that have them (tuna_moe.cu).
-size_t order_bytes(int64_t tokens, int experts, int k, int ranks) {
+// The table of counts.
+static size_t order_bytes(int64_t tokens, int experts, int k, int ranks) {
+  if (tokens == 0) return 0;
   OrderArgs o = {};
   plan_order(o, tokens, experts, k, ranks);
   return (size_t)o.rank_chunks * ranks * experts * 2;
