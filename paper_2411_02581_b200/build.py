@@ -65,9 +65,9 @@ def build_torch(force: bool = False) -> str:
         if os.path.exists(TORCH_PATH):
             os.remove(TORCH_PATH)  # no old one is left for a load that would rather say that it is missing
         raise
+    os.replace(tmp, TORCH_PATH)
     with open(note, "w") as f:
         f.write(made_for)
-    os.replace(tmp, TORCH_PATH)
     return TORCH_PATH
 
 
