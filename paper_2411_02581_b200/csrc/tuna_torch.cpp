@@ -248,6 +248,7 @@ Tensor operand(const Tensor &q, const char *name, int64_t &ld) {
 PyObject *fp8_matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return guarded(n, 8, [&] {
     const Tensor &left = tensor(a[0], "a"), &sa = tensor(a[1], "a_scale"), &right = tensor(a[2], "b"), &sb = tensor(a[3], "b_scale");
+    if (right.device() != left.device()) refuse("b: on another device than its fellow");
     const Place place(a[7], left);
     int64_t lda = 0, ldb = 0, groups = 1, cols, kb;
     const Tensor x = operand(left, "a", lda);
@@ -275,7 +276,6 @@ PyObject *fp8_matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {
         dense(sb, "b_scale", at::kFloat, {blocks, cols}, left);
     }
     dense(sa, "a_scale", at::kFloat, {blocks, m}, left);
-    if (right.device() != left.device()) refuse("b: on another device than its fellow");
     const Tensor y = make({m, cols}, out == TUNA_DTYPE_F32 ? at::kFloat : at::kBFloat16, left);
     check(p_tuna_fp8_matmul(at_of(x), (const float *)at_of(sa), m, lda, at_of(w), (const float *)at_of(sb), layout, clip(cols), ldb, clip(k),
                             clip(groups), offsets, at_of(y), out, std::max<int64_t>(cols, 1), place.stream()),
@@ -321,6 +321,7 @@ PyObject *few(PyObject *, PyObject *const *a, Py_ssize_t n) {
     }
     const Tensor &ws = tensor(a[12], "workspace");
     if (!ws.is_contiguous()) refuse("workspace: a contiguous tensor is wanted");
+    if (ws.device() != given.device()) refuse("workspace: on another device than its fellow");
     const Place place(a[13], given);
     Tensor x = given;
     if (ld % 8 || (uintptr_t)given.data_ptr() % 16) x = given.clone(at::MemoryFormat::Contiguous), ld = d;

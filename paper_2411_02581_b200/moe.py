@@ -45,25 +45,32 @@ def _same(*tensors):
     return tensors if len(tensors) > 1 else tensors[0]
 
 
-@contextlib.contextmanager
 def _on(stream, device):
-    """Makes ``stream`` torch's current one for a whole call, so that what is allocated and filled on
-    the way belongs to it.  Yields the raw stream and what outputs leave through: the caller may use
-    and free them on the stream that was current before."""
-    before = torch._C._cuda_getCurrentRawStream(device.index)
-    at = before if stream is None else B._stream(stream)
-    at = 0 if at == 1 else at  # cudaStreamLegacy: torch's name of the same stream is 0
-    if at == before:
-        yield at, _same
-        return
-    was = torch.cuda.current_stream(device)
+    """Makes ``device`` the current one and ``stream`` torch's current stream for a whole call, so that
+    what is allocated and filled on the way belongs to it.  Yields the raw stream and what outputs leave
+    through: the caller may use and free them on the stream that was current before."""
+    if stream is None and device.index == torch.cuda.current_device():
+        return contextlib.nullcontext((torch._C._cuda_getCurrentRawStream(device.index), _same))
+    return _on_another(stream, device)
 
-    def out(*tensors):
-        for t in tensors:
-            t.record_stream(was)
-        return _same(*tensors)
-    with torch.cuda.stream(torch.cuda.ExternalStream(at, device=device)):
-        yield at, out
+
+@contextlib.contextmanager
+def _on_another(stream, device):
+    with torch.cuda.device(device.index):
+        before = torch._C._cuda_getCurrentRawStream(device.index)
+        at = before if stream is None else B._stream(stream)
+        at = 0 if at == 1 else at  # cudaStreamLegacy: torch's name of the same stream is 0
+        if at == before:
+            yield at, _same
+            return
+        was = torch.cuda.current_stream(device)
+
+        def out(*tensors):
+            for t in tensors:
+                t.record_stream(was)
+            return _same(*tensors)
+        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(at, device=device)):
+            yield at, out
 
 
 def _check(rc, what):
@@ -88,20 +95,27 @@ def _fast():
     return _marshal
 
 
-def _matrix(t, name, dtypes):
-    """A CUDA matrix whose rows are contiguous; returns its row pitch."""
+def _beside(t, name, device):
+    if t.device != device:
+        raise ValueError(f"{name}: on {t.device}, its fellows are on {device}")
+
+
+def _matrix(t, name, dtypes, device=None):
+    """A CUDA matrix whose rows are contiguous, on ``device``; returns its row pitch."""
     if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype not in dtypes or not t.is_cuda:
         raise ValueError(f"{name}: a CUDA matrix of {', '.join(str(d) for d in dtypes)} is wanted")
     rows, cols = t.shape
     ld, step = t.stride()
     if cols > 1 and step != 1 or rows > 1 and ld < cols:
         raise ValueError(f"{name}: rows must be contiguous and must not overlap (strides {t.stride()})")
+    _beside(t, name, device or t.device)
     return ld if rows > 1 else max(cols, 1)
 
 
-def _dense(t, name, dtype, shape):
+def _dense(t, name, dtype, shape, device=None):
     if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous CUDA tensor of {dtype}, shape {tuple(shape)}, is wanted")
+    _beside(t, name, device or t.device)
     return t
 
 
@@ -160,8 +174,8 @@ def combine(y, weights, pos, *, out_dtype=torch.bfloat16, stream=None):
     """out[t] = sum over s of weights[t, s] * y[pos[t, s]] (``tuna_moe_combine``)."""
     ld = _matrix(y, "y", FLOATS)
     t, k = weights.shape
-    _dense(weights, "weights", torch.float32, (t, k))
-    _dense(pos, "pos", torch.int64, (t, k))
+    _dense(weights, "weights", torch.float32, (t, k), y.device)
+    _dense(pos, "pos", torch.int64, (t, k), y.device)
     if out_dtype not in FLOATS:
         raise ValueError(f"out_dtype: one of {FLOATS}")
     with _on(stream, y.device) as (at, out):
@@ -173,10 +187,10 @@ def combine(y, weights, pos, *, out_dtype=torch.bfloat16, stream=None):
 
 def combine_backward(dout, y, weights, pos, *, stream=None):
     """(dy, dweights) of :func:`combine`; rows of y that no slot names get a zero gradient."""
-    ldg, ldy = _matrix(dout, "dout", FLOATS), _matrix(y, "y", FLOATS)
+    ldg, ldy = _matrix(dout, "dout", FLOATS), _matrix(y, "y", FLOATS, dout.device)
     t, k = weights.shape
-    _dense(weights, "weights", torch.float32, (t, k))
-    _dense(pos, "pos", torch.int64, (t, k))
+    _dense(weights, "weights", torch.float32, (t, k), y.device)
+    _dense(pos, "pos", torch.int64, (t, k), y.device)
     if tuple(dout.shape) != (t, y.shape[1]):
         raise ValueError(f"dout: shape {tuple(dout.shape)}, wanted {(t, y.shape[1])}")
     with _on(stream, y.device) as (at, out):
@@ -215,35 +229,43 @@ def fp8_matmul(a, a_scale, b, b_scale, *, offsets=None, b_blocks="tiles", out_dt
     return (_marshal or _fast()).fp8_matmul(a, a_scale, b, b_scale, offsets, LAYOUTS[b_blocks], DTYPES[out_dtype], stream)
 
 
-def _experts_weights(w13, s13, w2, s2, hidden):
+def _experts_weights(w13, s13, w2, s2, hidden, device):
     """Checked shapes of 8-bit expert weights: (experts, inter)."""
     if w13.dim() != 4 or w13.shape[1] != 2 or w13.shape[3] != hidden:
         raise ValueError(f"w13: [experts, 2, inter, {hidden}] is wanted, got {tuple(w13.shape)}")
     e, _, i, d = w13.shape
-    _dense(w13, "w13", torch.float8_e4m3fn, (e, 2, i, d))
-    _dense(s13, "s13", torch.float32, (e, 2, _blocks(i), _blocks(d)))
-    _dense(w2, "w2", torch.float8_e4m3fn, (e, d, i))
-    _dense(s2, "s2", torch.float32, (e, _blocks(d), _blocks(i)))
+    _dense(w13, "w13", torch.float8_e4m3fn, (e, 2, i, d), device)
+    _dense(s13, "s13", torch.float32, (e, 2, _blocks(i), _blocks(d)), device)
+    _dense(w2, "w2", torch.float8_e4m3fn, (e, d, i), device)
+    _dense(s2, "s2", torch.float32, (e, _blocks(d), _blocks(i)), device)
     return e, i
 
 
-def _space(need, workspace, device):
+def _own_space(workspace, device):
+    """Checks a workspace that the caller brought."""
     if workspace is None:
-        return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
-    return workspace
+        return
+    if not isinstance(workspace, torch.Tensor) or not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace: a contiguous CUDA tensor is wanted")
+    _beside(workspace, "workspace", device)
+
+
+def _space(need, workspace, device):
+    return torch.empty(max(need, 256), dtype=torch.uint8, device=device) if workspace is None else workspace
 
 
 def expert_rows(x, offsets, w13, s13, w2, s2, *, workspace=None, stream=None):
     """Rows in expert order through their experts (``tuna_moe_expert_rows``); a row of the result that no expert has is undefined."""
     ldx = _matrix(x, "x", (torch.bfloat16,))
     rows, d = x.shape
-    e, i = _experts_weights(w13, s13, w2, s2, d)
-    _dense(offsets, "offsets", torch.int64, (e + 1,))
+    e, i = _experts_weights(w13, s13, w2, s2, d, x.device)
+    _dense(offsets, "offsets", torch.int64, (e + 1,), x.device)
+    _own_space(workspace, x.device)
     with _on(stream, x.device) as (at, out):
         ws = _space(_bytes("tuna_moe_expert_rows_workspace_bytes", rows, d, i), workspace, x.device)
         y = torch.empty(rows, d, dtype=torch.bfloat16, device=x.device)
         _check(B.lib().tuna_moe_expert_rows(x.data_ptr(), ldx, rows, e, offsets.data_ptr(), d, i, w13.data_ptr(), s13.data_ptr(), w2.data_ptr(),
-                                            s2.data_ptr(), y.data_ptr(), d, ws.data_ptr(), ws.numel(), at), "tuna_moe_expert_rows")
+                                            s2.data_ptr(), y.data_ptr(), d, ws.data_ptr(), ws.nbytes, at), "tuna_moe_expert_rows")
         return out(y)
 
 
@@ -251,15 +273,16 @@ def experts(x, ids, weights, w13, s13, w2, s2, *, workspace=None, stream=None):
     """The experts of many tokens in 8 bits (``tuna_moe_experts``): ids and weights as :func:`route` makes them."""
     ldx = _matrix(x, "x", (torch.bfloat16,))
     t, d = x.shape
-    e, i = _experts_weights(w13, s13, w2, s2, d)
+    e, i = _experts_weights(w13, s13, w2, s2, d, x.device)
     k = ids.shape[-1]
-    _dense(ids, "ids", torch.int32, (t, k))
-    _dense(weights, "weights", torch.float32, (t, k))
+    _dense(ids, "ids", torch.int32, (t, k), x.device)
+    _dense(weights, "weights", torch.float32, (t, k), x.device)
+    _own_space(workspace, x.device)
     with _on(stream, x.device) as (at, out):
         ws = _space(_bytes("tuna_moe_experts_workspace_bytes", t, e, k, d, i), workspace, x.device)
         o = torch.empty(t, d, dtype=torch.bfloat16, device=x.device)
         _check(B.lib().tuna_moe_experts(x.data_ptr(), ldx, t, ids.data_ptr(), weights.data_ptr(), k, e, d, i, w13.data_ptr(), s13.data_ptr(),
-                                        w2.data_ptr(), s2.data_ptr(), o.data_ptr(), d, ws.data_ptr(), ws.numel(), at), "tuna_moe_experts")
+                                        w2.data_ptr(), s2.data_ptr(), o.data_ptr(), d, ws.data_ptr(), ws.nbytes, at), "tuna_moe_experts")
         return out(o)
 
 
@@ -289,9 +312,10 @@ def _few_space(x, router, k, w13, at):
     sizes = t, router.shape[0], k, d, w13.shape[2]
     if torch.cuda.is_current_stream_capturing():
         return few_workspace(*sizes, x.device)
-    kept = _few_spaces.get((x.device.index, at))
+    place = x.get_device(), at
+    kept = _few_spaces.get(place)
     if kept is None or kept.numel() < _few_bytes(*sizes)[0]:
-        kept = _few_spaces[x.device.index, at] = few_workspace(*sizes, x.device)
+        kept = _few_spaces[place] = few_workspace(*sizes, x.device)
     return kept
 
 
@@ -305,8 +329,13 @@ def few(x, router, k, w13, w2, *, s13=None, s2=None, scoring="softmax", renormal
     share one that the module keeps, as large as the largest of them needed, and each call that
     ``torch.cuda.graph`` captures has its own; who captures by other means passes one."""
     if workspace is None:
-        with _on(stream, x.device) as (at, _):
-            workspace = _few_space(x, router, k, w13, at)
+        if not x.is_cuda:
+            raise ValueError("x: a CUDA matrix of torch.bfloat16 is wanted")
+        if stream is None and x.get_device() == torch.cuda.current_device():  # (a decode step's call: no context to enter)
+            workspace = _few_space(x, router, k, w13, torch._C._cuda_getCurrentRawStream(x.get_device()))
+        else:
+            with _on(stream, x.device) as (at, _):
+                workspace = _few_space(x, router, k, w13, at)
     return (_marshal or _fast()).few(x, router, k, w13, w2, s13, s2, _scoring(scoring), renormalize, scale, ids, weights, workspace, stream)
 
 
