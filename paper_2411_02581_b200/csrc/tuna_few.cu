@@ -557,8 +557,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             if constexpr (FP8) {
               uint32_t top = max(max(abs_bits(x.v[0]), abs_bits(x.v[1])), max(abs_bits(x.v[2]), abs_bits(x.v[3])));
               top = __reduce_max_sync(~0u, top);
-              // s takes the block's largest value to [2^7, 2^8); a block that is not finite is lost to NaN
-              const int e = min(max((int)(top >> 23), 27) - 7, 240);
+              // s takes the block's largest value to [2^7, 2^8), whatever it is (exponents 1 to 254 leave e in 20 to 247);
+              // a block that is not finite is lost to NaN
+              const int e = min(max((int)(top >> 23), 27) - 7, 247);
               const float s = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)e << 23);
               const float by = __uint_as_float((uint32_t)(254 - e) << 23);
               uint32_t h2[2], l2[2];

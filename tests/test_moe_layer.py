@@ -152,6 +152,27 @@ def test_few_values_that_are_large_small_or_not_finite(kind):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("power", [118, 121, 122, 126, 127])
+def test_few_values_up_to_the_largest_finite_one(power):
+    """8-bit weights so small that products with x near the end of its range are ordinary numbers: x is held in two pieces
+    whose scale has to follow it to the end."""
+    from paper_2411_02581_b200 import moe
+    e, k, d, i = 2, 2, 256, 64
+    w13, s13 = fp8_weights(2 * e, i, d, 1)
+    w2, s2 = fp8_weights(e, d, i, 2)
+    s13 = (s13 * 2.0 ** -power).view(e, 2, *s13.shape[1:])
+    x = activations(4, d, 5, torch.float32)
+    x = (x / x.abs().amax() * 1.99 * 2.0 ** power).to(torch.bfloat16)      # (1.99 rounds to 1.992 in 8 bits: finite at 2^127)
+    x[3] *= 2.0 ** -20
+    router = torch.zeros(e, d, dtype=torch.bfloat16, device="cuda")
+    ids, w = torch.empty(4, k, dtype=torch.int32, device="cuda"), torch.empty(4, k, device="cuda")
+    got = moe.few(x.cuda(), router, k, w13.view(e, 2, i, d), w2, s13=s13, s2=s2, renormalize=True, ids=ids, weights=w)
+    want = plain_layer(x, ids, w, w13.view(e, 2, i, d), s13, w2, s2, False)
+    for r in range(4):
+        assert bool(torch.isfinite(got[r]).all()) and near(got[r:r + 1], want[r:r + 1]), r
+
+
+@pytest.mark.gpu
 def test_few_again_and_again_on_one_workspace():
     """Counters return to zero, sums do not depend on the blocks' order, and sizes may change."""
     from paper_2411_02581_b200 import moe
