@@ -652,7 +652,9 @@ int tuna_moe_experts(const void *x, int64_t ldx, int64_t tokens, const int32_t *
  *   x        tokens x hidden, bf16, 16-byte aligned rows (ldx a multiple of 8);
  *   router   experts x hidden, bf16, contiguous.
  *   weight_dtype   TUNA_DTYPE_BF16, or TUNA_DTYPE_E4M3 with scales as in tuna_moe_experts
- *            (then only the weights are in 8 bits: x and h keep at least bf16's precision).
+ *            (then only the weights are in 8 bits: of x and h, 8 significant bits are kept down to 2^-13
+ *            of the largest magnitude of their block of 128 columns, and 2^-21 of that one below).
+ *            With bf16 weights h is rounded to bf16 before the second product.
  *   ids, weights   tokens x k, receive the choice; may be NULL.
  * The first `zeroed` bytes of the workspace must be zero before its first use and belong
  * to the calls from then on, also behind one that gave up a wait (tuna_ops_device_status).

@@ -21,10 +21,12 @@
 // y, which the last phase adds up with the tokens' weights.  Nothing is summed in an order that
 // depends on timing.
 //
-// bf16 weights meet x and h in bf16 (h rounded once, as a two-kernel layer would store it).
+// bf16 weights meet x and h in bf16.  h is rounded to it once (2^-9 of each value, as a two-kernel layer would
+// store it), because the tensor cores multiply both operands in one type and in 32 bits at half the rate or less.
 // 8-bit weights meet two 8-bit pieces of each token value, x = s (p + q / 16) with s a power of
-// two for each 128 values: 8 significant bits, all that x has (within 2^14 of its block's largest
-// value; below, 2^-21 of that), and what bf16 would keep of h.  The pieces are columns of their
+// two for each 128 values, the largest of which lies in [2^7, 2^8) s.  p keeps 4 significant bits and q the
+// next 4 while the value is at least 2^-6 s: 8 bits, all that x has and what bf16 would keep of h, down to 2^-13 of
+// the block's largest value.  Below, the step of q is fixed, and the error at most 2^-14 s, 2^-21 of the largest.  The pieces are columns of their
 // own; a block of 128 is one accumulation, which four warps multiply by the weights' scale.
 #include <algorithm>
 #include <cmath>
@@ -673,9 +675,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-// Blocks of a segment: as long as possible (fewer partial sums), while some five units a block are
-// expected, which share out evenly enough; and at most four segments, since what lays out h adds
-// them all up.  Measured in us, shorter and longer: one token of 64 experts, 8-bit, 39 and 35;
+// Blocks of a segment: as long as possible (fewer partial sums; 1024 columns fill the operand's memory), while
+// some five units a block are expected, which share out evenly enough; and cut for that to four segments at
+// most, since what lays out h adds them all up.  (8192 columns are eight segments of the longest.)  Measured in us, shorter and longer: one token of 64 experts, 8-bit, 39 and 35;
 // 33 tokens x 6 of 16 narrow experts 65 and 70; 64 tokens x 2 of 64 experts 260 and 248.
 void plan_segments(int tokens, int k, int experts, int64_t rows, int64_t cols, int block, int &segment, int &segments) {
   const double chosen = experts * (1.0 - std::pow(1.0 - 1.0 / experts, (double)tokens * k));  // by evenly spread choices

@@ -581,7 +581,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           unpair(acc[16 + i], u[0], u[1]);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const float x = __fdividef(g[j], 1.0f + __expf(-g[j])) * u[j];  // (2^-20: 8 bits are kept)
+            // (2^-20 of the value; it is rounded to 4 significant bits next, and the exact functions take longer)
+            const float x = __fdividef(g[j], 1.0f + __expf(-g[j])) * u[j];
             h[2 * i + j] = x;
             amax = max(amax, abs_bits(x));
           }

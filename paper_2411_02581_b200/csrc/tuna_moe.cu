@@ -6,6 +6,11 @@
 //
 // The widest intermediate, two products of `inter` columns a row, is never written: the
 // first product's epilogue turns it into 8-bit rows (tuna_fp8.cu).
+//
+// An expert's row is rounded to bf16 (2^-9 of each value) before the weighted sum, which adds in 32 bits.  It is the
+// row that tuna_moe_expert_rows hands to the return of a token dispatch, so that a layer gives the same bits with its
+// experts in place and behind an exchange; and in 32 bits it would be written and read at twice the bytes
+// (268 MB more for 8192 tokens x 2 slots of 4096 columns, 41 us at 6552 GB/s).
 #include "tuna_fp8.h"
 #include "tuna_ops.cuh"
 

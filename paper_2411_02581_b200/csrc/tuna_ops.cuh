@@ -27,8 +27,9 @@ int note_cuda(cudaError_t e);
 int sm_count();
 int *error_word();  // device address of the flag that a bounded wait raises (nullptr: no device)
 
-// Launches `kernel` so that it may be scheduled while the stream's previous kernel drains:
-// every kernel of these operators begins with wait_previous().  `cluster`: blocks of a cluster.
+// Launches `kernel` so that it may be scheduled while the stream's previous kernel drains: it
+// begins with wait_previous().  A cooperative one is launched behind the previous kernel's end, and need not.
+// `cluster`: blocks of a cluster.
 template <typename... P, typename... A>
 inline int launch_cluster(void (*kernel)(P...), dim3 grid, int cluster, int threads, size_t smem, cudaStream_t st, bool cooperative, A... args) {
   cudaLaunchConfig_t cfg = {};

@@ -173,6 +173,47 @@ def test_few_values_up_to_the_largest_finite_one(power):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("small", [2.0 ** -10, 2.0 ** -13, 2.0 ** -16, 2.0 ** -20])
+def test_few_small_values_beside_a_large_one(small):
+    """8-bit weights: a value of x or h is held to 2^-9 of itself or to 2^-21 of the largest one of its 128, whichever
+    is more (x, of bf16, exactly where the first is more).  The large channels have no weight of their own, so the
+    result is made of the small ones.
+
+    The bound of an output follows: gate and up sums move by G = sum_k 2^-21 max |x of the block| |w| (and 2^-20 of
+    sum |x w| for the 32-bit sums), h by 1.1 G |u| + |silu(g)| U + 1.1 G U (silu rises by 1.1 at most) and by its own
+    rounding, y and the weighted sum linearly with them; the result is rounded to bf16 (2^-9)."""
+    from paper_2411_02581_b200 import moe
+    e, k, d, i, t = 2, 2, 256, 144, 5
+    g = torch.Generator().manual_seed(4)
+    x = torch.randn(t, d, generator=g) * small
+    loud = [3, 200]                                               # one in each block of 128
+    x[:, loud] = torch.tensor([1.9, -1.5])
+    x = x.to(torch.bfloat16)
+    w13, s13 = fp8_weights(2 * e, i, d, 1)
+    w13.view(torch.uint8)[:, :, loud] = 0
+    w2, s2 = fp8_weights(e, d, i, 2)
+    s13 = s13 / small                                             # so that g and u are about one
+    w13, s13 = w13.view(e, 2, i, d), s13.view(e, 2, *s13.shape[1:])
+    router = torch.zeros(e, d, dtype=torch.bfloat16, device="cuda")
+    ids, w = torch.empty(t, k, dtype=torch.int32, device="cuda"), torch.empty(t, k, device="cuda")
+    got = moe.few(x.cuda(), router, k, w13, w2, s13=s13, s2=s2, renormalize=True, ids=ids, weights=w).cpu().double()
+    X = x.double()
+    top = lambda v: torch.nn.functional.pad(v.abs(), (0, -v.shape[1] % 128)).unflatten(1, (-1, 128)).amax(2).repeat_interleave(128, 1)[:, :v.shape[1]]  # noqa: E731
+    out, bound = torch.zeros(t, d, dtype=torch.float64), torch.zeros(t, d, dtype=torch.float64)
+    for j in range(e):
+        wg, wu, wd = value(w13[j, 0], s13[j, 0], "tiles"), value(w13[j, 1], s13[j, 1], "tiles"), value(w2[j], s2[j], "tiles")
+        a, b = X @ wg.t(), X @ wu.t()
+        A, Bd = [(2.0 ** -21 * top(X) + 2.0 ** -20 * X.abs()) @ m.abs().t() for m in (wg, wu)]
+        silu = torch.nn.functional.silu(a)
+        h = silu * b
+        H = 1.1 * A * b.abs() + silu.abs() * Bd + 1.1 * A * Bd + 2.0 ** -20 * h.abs()
+        H = H + torch.maximum(2.0 ** -9 * (h.abs() + H), 2.0 ** -21 * top(h.abs() + H))
+        out += 0.5 * (h @ wd.t())
+        bound += 0.5 * ((H + 2.0 ** -20 * h.abs()) @ wd.abs().t())
+    assert bool(((got - out).abs() <= bound + 2.0 ** -9 * (out.abs() + bound)).all())
+
+
+@pytest.mark.gpu
 def test_few_again_and_again_on_one_workspace():
     """Counters return to zero, sums do not depend on the blocks' order, and sizes may change."""
     from paper_2411_02581_b200 import moe
