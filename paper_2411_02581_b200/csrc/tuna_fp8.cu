@@ -581,7 +581,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
           unpair(acc[16 + i], u[0], u[1]);
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            // (2^-20 of the value; it is rounded to 4 significant bits next, and the exact functions take longer)
+            // (2^-20 of the value, which is rounded to 4 significant bits next; with the exact functions 501 tokens
+            // x 2 of 64 experts of 2048 x 1408 take 127.8 us in place of 118.2)
             const float x = __fdividef(g[j], 1.0f + __expf(-g[j])) * u[j];
             h[2 * i + j] = x;
             amax = max(amax, abs_bits(x));
