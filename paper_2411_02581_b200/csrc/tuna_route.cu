@@ -773,7 +773,8 @@ int tuna_moe_combine_backward(const void *dout, int out_dtype, int64_t lddo, con
   a.rows = rows, a.tokens = tokens, a.ldy = ldy, a.ldo = lddo, a.lddy = lddy, a.dim = dim, a.k = k;
   if (lddy < dim) return TUNA_ERR_INVALID_ARG;
   if (const int rc = check_combine(a, y_dtype, out_dtype)) return rc;
-  if (tokens == 0 || dim == 0) return TUNA_OK;
+  if (tokens == 0) return TUNA_OK;
+  if (dim == 0) return dweights ? note_cuda(cudaMemsetAsync(dweights, 0, (size_t)tokens * k * 4, (cudaStream_t)stream)) : TUNA_ERR_INVALID_ARG;  // empty sums
   const size_t sy = dtype_size(y_dtype), so = dtype_size(out_dtype);
   if (!dout || !dweights || (rows > 0 && !dy) || !aligned(y, sy) || !aligned(dy, sy) || !aligned(dout, so)) return TUNA_ERR_INVALID_ARG;
   a.vec = dim % 8 == 0 && aligned(y, 16) && aligned(dy, 16) && aligned(dout, 16) && ldy * sy % 16 == 0 && lddy * sy % 16 == 0 && lddo * so % 16 == 0;

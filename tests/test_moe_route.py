@@ -206,6 +206,20 @@ def test_combine_and_its_gradient(t, k, d, y_dtype, out_dtype):
 
 
 @pytest.mark.gpu
+def test_combine_gradient_of_rows_without_columns():
+    """<dout, y> of empty rows is zero, and written."""
+    from paper_2411_02581_b200 import moe
+    L = B.lib()
+    w, pos, dw = torch.ones(5, 3, device="cuda"), torch.arange(15, device="cuda"), torch.full((5, 3), 7.0, device="cuda")
+    assert L.tuna_moe_combine_backward(None, 0, 0, None, 0, 15, 0, 0, w.data_ptr(), pos.data_ptr(), 5, 3, None, 0, dw.data_ptr(), None) == 0
+    torch.cuda.synchronize()
+    assert int(torch.count_nonzero(dw)) == 0
+    assert L.tuna_moe_combine_backward(None, 0, 0, None, 0, 15, 0, 0, w.data_ptr(), pos.data_ptr(), 5, 3, None, 0, None, None) == -1
+    dy, dw = moe.combine_backward(torch.empty(5, 0, device="cuda"), torch.empty(15, 0, device="cuda"), w, pos.view(5, 3))
+    assert dy.shape == (15, 0) and int(torch.count_nonzero(dw)) == 0
+
+
+@pytest.mark.gpu
 def test_no_tokens():
     from paper_2411_02581_b200 import moe
     r = moe.route(torch.empty(0, 64, device="cuda"), 2)
