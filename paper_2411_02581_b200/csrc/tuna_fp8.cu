@@ -191,6 +191,7 @@ struct TileArgs {
   int n_tiles;
   int store_tiles;  // results leave through map_out
   int one_copy;     // SWIGLU: map_b brings gate and up rows together
+  uint32_t most_rows;  // row tiles, at most: their number times n_tiles, and a step beyond, fits 31 bits
   int *error;
 };
 
@@ -269,24 +270,26 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   if (warp == 2) tmem_alloc(smem_u32(tmem_at), 2 * BN);
   wait_previous();
   allow_next();
-  // tiles of rows before each group
+  // Tiles of rows before each group.  Groups that lie apart never come near most_rows (their results would not fit the
+  // memory); offsets that make them overlap may, and are cut there.
   if (warp == 1) {
-    int sum = 0;
+    uint32_t sum = 0;
     for (int g0 = 0; g0 < a.p.groups; g0 += 32) {
       const int g = g0 + lane;
       int64_t rows = 0;
-      if (g < a.p.groups) rows = a.p.offsets ? min(a.p.offsets[g + 1], a.p.m) - max(a.p.offsets[g], (int64_t)0) : a.p.m;
-      const int mt = rows > 0 ? (int)((rows + 127) / 128) : 0;
-      int x = mt;
+      auto cut = [&](int64_t row) { return min(max(row, (int64_t)0), a.p.m); };
+      if (g < a.p.groups) rows = a.p.offsets ? cut(a.p.offsets[g + 1]) - cut(a.p.offsets[g]) : a.p.m;
+      const uint32_t mt = rows > 0 ? (uint32_t)((rows + 127) / 128) : 0;  // (2^24 at most: 32 of them and most_rows fit 32 bits)
+      uint32_t x = mt;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
-        const int y = __shfl_up_sync(~0u, x, d);
+        const uint32_t y = __shfl_up_sync(~0u, x, d);
         if (lane >= d) x += y;
       }
-      if (g < a.p.groups) tile_base[g] = sum + x - mt;
-      sum += __shfl_sync(~0u, x, 31);
+      if (g < a.p.groups) tile_base[g] = (int)min(sum + x - mt, a.most_rows);
+      sum = min(sum + __shfl_sync(~0u, x, 31), a.most_rows);
     }
-    if (lane == 0) tile_base[a.p.groups] = sum;
+    if (lane == 0) tile_base[a.p.groups] = (int)sum;
   }
   tc_fence_before();
   __syncthreads();
@@ -648,6 +651,7 @@ int run_tiles(const ProductArgs &p, cudaStream_t st, int parts = 1) {
   a.p = p;
   a.blocks = (int)ceil_div(p.k, 128);
   a.n_tiles = (int)ceil_div(p.n, SWIGLU ? BN / 2 : BN);
+  a.most_rows = (INT32_MAX - (1 << 20)) / a.n_tiles;
   a.error = error_word();
   if (!a.error) return TUNA_ERR_CUDA;
   CUtensorMap ma, mb, mo;

@@ -153,6 +153,34 @@ def test_rows_outside_the_groups_are_left_alone():
 
 
 @pytest.mark.gpu
+def test_offsets_that_are_no_offsets_are_cut_to_the_operand():
+    """Falling, negative and too large ones: no row outside the operand is read or written, and the call ends."""
+    from paper_2411_02581_b200 import moe
+    m, n, k = 100, 72, 144
+    a, w = activations(m, k, 1), activations(5 * n, k, 2)
+    qa, sa = moe.fp8_quantize(a.cuda())
+    tiles = [moe.fp8_quantize(w[i * n:(i + 1) * n].cuda(), "tiles") for i in range(5)]
+    qw, sw = torch.stack([q.view(torch.uint8) for q, _ in tiles]).view(FP8), torch.stack([s for _, s in tiles])
+    for offsets, alone in (([50, 20, -5, 1 << 40, 10, 0], 2), ([-(1 << 63), (1 << 63) - 1, 0, -(1 << 63), 0, 0], 0), ([7, 7, 7, 7, 7, 7], None)):
+        space = torch.full((m + 64, n), 7.0, dtype=torch.bfloat16, device="cuda")     # canaries on both sides
+        assert B.lib().tuna_fp8_matmul(qa.data_ptr(), sa.data_ptr(), m, k, qw.data_ptr(), sw.data_ptr(), 2, n, k, k, 5,
+                                       torch.tensor(offsets, device="cuda").data_ptr(), space[32:].data_ptr(), 1, n, None) == 0
+        torch.cuda.synchronize()
+        assert bool((space[:32] == 7).all()) and bool((space[32 + m:] == 7).all())
+        out = space[32:32 + m]
+        if alone is None:
+            assert bool((out == 7).all())
+        else:
+            assert close(out, value(qa, sa, "rows"), value(qw[alone], sw[alone], "tiles"), True)
+    # all rows in each of the groups: many more tiles than rows, the same results from equal matrices
+    same = torch.stack([qw[0].view(torch.uint8)] * 5).view(FP8)
+    overlapping = torch.tensor([0, m, 0, m, 0, m], device="cuda")
+    got = moe.fp8_matmul(qa, sa, same, torch.stack([sw[0]] * 5), offsets=overlapping)
+    assert close(got, value(qa, sa, "rows"), value(qw[0], sw[0], "tiles"), True)
+    assert moe.device_status() == 0
+
+
+@pytest.mark.gpu
 def test_layer_gradients_against_the_formula_and_differences():
     """dx and dw of y = x w^T: the formula on the quantised operands, and the change of <y, dy>."""
     from paper_2411_02581_b200 import moe
