@@ -9,6 +9,12 @@ would take longer than their kernels.  Work is enqueued on ``stream`` (default: 
 current one), which is torch's current stream until the call returns: outputs, workspaces
 and copies are its own.  An input that was made on another stream is the caller's to
 order, as with any torch operation, and so is an output before another stream reads it.
+
+Nothing here is recorded by autograd: outputs carry no gradient, whatever the inputs require.
+Gradients are calls of their own (:func:`route_backward`, :func:`combine_backward`, and
+:func:`fp8_matmul` on operands quantised along the other axis), which a
+``torch.autograd.Function`` of the caller's may make; :func:`experts`, :func:`expert_rows`
+and :func:`few` have none.
 """
 from __future__ import annotations
 
