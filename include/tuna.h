@@ -567,6 +567,40 @@ int tuna_moe_route_backward(const void *logits, int dtype, int64_t tokens, int e
                             const float *dweights, void *dlogits, int64_t ldd, void *stream);
 
 /*
+ * tuna_moe_balance - the balance loss of a router: for each segment g of the tokens (a sequence of a
+ * packed batch, or all of it), over its n live tokens, those with a logit that is neither -inf nor NaN,
+ *   loss[g] = experts / (k n^2) * sum over e of counts[g][e] * mass[g][e],
+ *   z[g]    = (1 / n) * sum over t of (log of the sum over e of exp(logit))^2,
+ *   counts[g][e] = how often ids names e in the segment (ids outside [0, experts) are left out),
+ *   mass[g][e]   = sum over t of the probability of e: TUNA_MOE_SOFTMAX the softmax over the experts,
+ *                  TUNA_MOE_SIGMOID 1/(1+exp(-logit)) divided by the token's sum of them,
+ *   live[g] = n.  An even choice has a loss of 1; a segment without live tokens one of 0.
+ *   logits   tokens x experts, f32 or bf16, pitch ld; masked logits (-inf, NaN) have probability 0,
+ *            logits of +inf share the softmax (z is then +inf).  ids: tokens x k (int32), as
+ *            tuna_moe_route makes them.
+ *   offsets  segments + 1 (DEVICE, not falling, cut to [0, tokens]): tokens [offsets[g], offsets[g+1])
+ *            are segment g's, the others nobody's; NULL: one segment of all tokens.
+ *   loss, z (NULL: not wanted), live: segments; counts (int64), mass: segments x experts.
+ * The loss of a batch that is spread over GPUs: add up counts, mass and live, and apply the formula.
+ * A few tokens need no workspace (0 bytes: it may be NULL).
+ * tuna_moe_balance_backward - dlogits (the logits' type, pitch ldd) of sum over g of dloss[g] * loss[g] +
+ * dz[g] * z[g] (dz NULL: no such part); counts, the choice itself, are constant.  counts and live are those
+ * of the loss (of all GPUs, where they were added up).  Masked logits, rows without live logits and tokens
+ * of no segment get zeros.
+ * Limits (TUNA_ERR_RANGE): those of tuna_moe_route, segments <= TUNA_MOE_MAX_SEGMENTS.
+ */
+#define TUNA_MOE_MAX_SEGMENTS 65536
+int tuna_moe_balance_workspace_bytes(int64_t tokens, int experts, int segments, size_t *bytes);
+int tuna_moe_balance(const void *logits, int dtype, int64_t tokens, int experts, int64_t ld,
+                     const int32_t *ids, int k, int scoring, int segments, const int64_t *offsets,
+                     float *loss, float *z, int64_t *counts, float *mass, int64_t *live,
+                     void *workspace, size_t workspace_bytes, void *stream);
+int tuna_moe_balance_backward(const void *logits, int dtype, int64_t tokens, int experts, int64_t ld,
+                              int k, int scoring, int segments, const int64_t *offsets,
+                              const int64_t *counts, const int64_t *live, const float *dloss,
+                              const float *dz, void *dlogits, int64_t ldd, void *stream);
+
+/*
  * tuna_moe_combine - out[t] = sum over s of weights[t][s] * y[pos[t][s]], in slot order and
  * in 32 bits; slots whose pos is outside [0, rows) add nothing.  y: rows x dim, out:
  * tokens x dim, each f32 or bf16.
@@ -619,6 +653,52 @@ int tuna_fp8_matmul(const void *a, const float *a_scale, int64_t m, int64_t lda,
                     const int64_t *offsets, void *out, int out_dtype, int64_t ldo, void *stream);
 
 /*
+ * tuna_fp4_quantize - a matrix to 4 bits with a power of two for every 32 values (microscaling: values
+ * e2m1, that is 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; scales e8m0, a byte b for 2^(b - 127),
+ * 255 for NaN).
+ *   scale = 2^(floor(log2 of the block's largest |x|) - 2), at least 2^-127, and q = e2m1(x / scale), halves
+ *   to even, magnitudes over 6 to 6; a block that holds a NaN or an infinity gets the scale NaN.
+ *   x: rows x cols, f32 or bf16, pitch ldx.
+ *   layout           blocks    q (two values a byte, the first in the low half)
+ *   TUNA_FP4_ROWS    1 x 32    rows x cols, pitch ldq bytes
+ *   TUNA_FP4_COLUMNS 32 x 1    x^T: cols x rows, pitch ldq bytes
+ *   q is 16-byte aligned, ldq a multiple of 16; rows are written up to the next multiple of 32 values.
+ *   scale    [row tiles][runs][512] bytes, 16-byte aligned: a tile has 128 rows of q, a run 128 of its columns; the byte
+ *            of row r and block j of a tile's run is at (r % 32) * 16 + (r / 32) * 4 + j.  Blocks behind the last
+ *            column of a run have 0 or anything that is not NaN; rows behind the last anything.
+ *   groups, offsets   0 and NULL: row tile i has rows [128 i, 128 i + 128).  Otherwise (TUNA_FP4_ROWS) rows
+ *            [offsets[g], offsets[g+1]) are those of group g (offsets: DEVICE, groups + 1, not falling, cut to
+ *            [0, rows]) and its row tiles, of its own rows only, begin at offsets[g] / 128 + g.  Rows outside
+ *            every group are not written.
+ * tuna_fp4_scale_tiles - row tiles of such scales: ceil(rows / 128), or rows / 128 + groups.
+ *
+ * tuna_fp4_dequantize - the values that rows x cols of q (pitch ldq bytes, any alignment) stand for, f32 or bf16;
+ * rows outside every group are not written.
+ *
+ * tuna_fp4_matmul - out[m][n] = sum over k of a[m][k] * b[n][k], in 32 bits, to f32 or bf16; a: m x k, b: n x k, k even,
+ * both quantised along k, pitches in bytes, multiples of 16.  A layer y = x w^T and its gradients are the same
+ * product on operands quantised along the contracted axis:  y = (x ROWS) (w ROWS);  dx = (dy ROWS) (w COLUMNS);
+ * dw = (dy COLUMNS) (x COLUMNS).
+ *   groups, offsets   0 and NULL, or: b holds `groups` matrices (n * ldb bytes apart, each with ceil(n / 128) row tiles
+ *            of scales, back to back); rows [offsets[g], offsets[g+1]) of a, quantised with these offsets, meet
+ *            matrix g.  Rows outside every group are not written.
+ * Limits (TUNA_ERR_RANGE): groups <= TUNA_MOE_MAX_EXPERTS, cols, n, k (and rows of TUNA_FP4_COLUMNS) <= 2^24, rows, m <
+ *   2^31 - 256, groups x (m / 128 + 1) x n / 128 < 2^31.
+ */
+#define TUNA_FP4_ROWS 0
+#define TUNA_FP4_COLUMNS 1
+int tuna_fp4_scale_tiles(int64_t rows, int groups, int64_t *tiles);
+int tuna_fp4_quantize(const void *x, int dtype, int64_t rows, int cols, int64_t ldx, int layout,
+                      int groups, const int64_t *offsets, void *q, int64_t ldq, void *scale,
+                      void *stream);
+int tuna_fp4_dequantize(const void *q, int64_t ldq, const void *scale, int64_t rows, int cols,
+                        int groups, const int64_t *offsets, void *out, int out_dtype, int64_t ldo,
+                        void *stream);
+int tuna_fp4_matmul(const void *a, const void *a_scale, int64_t m, int64_t lda, const void *b,
+                    const void *b_scale, int n, int64_t ldb, int k, int groups,
+                    const int64_t *offsets, void *out, int out_dtype, int64_t ldo, void *stream);
+
+/*
  * tuna_moe_experts - the experts of many tokens, weights and products in 8 bits:
  *   out[t] = sum over s of weights[t][s] * (h Wd[e]^T),  e = ids[t][s],
  *   h = silu(x[t] Wg[e]^T) * (x[t] Wu[e]^T), with x and h rounded to 8 bits in blocks of
@@ -644,6 +724,25 @@ int tuna_moe_experts_workspace_bytes(int64_t tokens, int experts, int k, int hid
 int tuna_moe_experts(const void *x, int64_t ldx, int64_t tokens, const int32_t *ids,
                      const float *weights, int k, int experts, int hidden, int inter,
                      const void *w13, const float *s13, const void *w2, const float *s2, void *out,
+                     int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * tuna_fp4_experts, tuna_fp4_expert_rows - the same with weights, x and h in 4 bits (tuna_fp4_quantize):
+ *   w13      experts x 2 x inter x hidden / 2 bytes; s13: experts x 2 x ceil(inter/128) x ceil(hidden/128) x 512;
+ *   w2, s2   experts x hidden x inter / 2 and experts x ceil(hidden/128) x ceil(inter/128) x 512.
+ *   hidden and inter are multiples of 32; weights and scales start on 16-byte boundaries.  Limits as above.
+ */
+int tuna_fp4_expert_rows_workspace_bytes(int64_t rows, int experts, int hidden, int inter,
+                                         size_t *bytes);
+int tuna_fp4_expert_rows(const void *x, int64_t ldx, int64_t rows, int experts,
+                         const int64_t *offsets, int hidden, int inter, const void *w13,
+                         const void *s13, const void *w2, const void *s2, void *y, int64_t ldy,
+                         void *workspace, size_t workspace_bytes, void *stream);
+int tuna_fp4_experts_workspace_bytes(int64_t tokens, int experts, int k, int hidden, int inter,
+                                     size_t *bytes);
+int tuna_fp4_experts(const void *x, int64_t ldx, int64_t tokens, const int32_t *ids,
+                     const float *weights, int k, int experts, int hidden, int inter,
+                     const void *w13, const void *s13, const void *w2, const void *s2, void *out,
                      int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
 
 /*

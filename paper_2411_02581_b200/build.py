@@ -15,8 +15,8 @@ LIB_PATH = os.path.join(LIB_DIR, "libtuna.so")
 TORCH_PATH = os.path.join(LIB_DIR, "tuna_torch.so")   # the operator calls' torch marshalling (tuna_torch.cpp)
 TORCH_SOURCE = os.path.join(CSRC, "tuna_torch.cpp")
 SOURCES = ["tuna_plan.cu", "tuna_api.cu", "tuna_static.cu", "tuna_shard.cu", "tuna_move.cu",
-           "tuna_route.cu", "tuna_fp8.cu", "tuna_moe.cu", "tuna_few.cu"]
-HEADERS = [os.path.join(CSRC, h) for h in ("tuna_internal.h", "tuna_plan.h", "tuna_plan_kernels.cuh", "tuna_ops.cuh", "tuna_fp8.h", "tuna_route.cuh")] + [
+           "tuna_route.cu", "tuna_balance.cu", "tuna_fp8.cu", "tuna_fp4.cu", "tuna_moe.cu", "tuna_few.cu"]
+HEADERS = [os.path.join(CSRC, h) for h in ("tuna_internal.h", "tuna_plan.h", "tuna_plan_kernels.cuh", "tuna_ops.cuh", "tuna_fp8.h", "tuna_fp4.h", "tuna_route.cuh")] + [
     os.path.join(ROOT, "include", "tuna.h")]
 
 

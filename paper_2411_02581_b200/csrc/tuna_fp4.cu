@@ -1,0 +1,757 @@
+// Matrices in 4-bit floating point with a power of two for every 32 values along the contracted axis (microscaling: e2m1
+// values, e8m0 scales), and their products, dense and grouped by expert.
+//
+//   y[m,n] = sum_b 2^(ea[m,b] + eb[n,b]) sum_{k in block b} a[m,k] b[n,k]
+//
+// The tensor cores apply the scales themselves, so a product accumulates in tensor memory from the first step to the last.
+#include <algorithm>
+#include <mutex>
+
+#include "tuna_fp4.h"
+#include "tuna_ops.cuh"
+
+namespace tuna_ops {
+namespace {
+
+// ---- values --------------------------------------------------------------------------------
+
+// The scale's byte: the exponent of the block's largest magnitude less that of the largest 4-bit value (6 = 1.5 * 2^2), 2^-127
+// at least; 255, which stands for NaN, where the block holds a NaN or an infinity.
+__device__ __forceinline__ uint32_t fp4_scale(uint32_t amax_bits) {
+  const int e = amax_bits >> 23;
+  return e == 255 ? 255u : (uint32_t)max(e - 2, 0);
+}
+__device__ __forceinline__ float fp4_power(uint32_t byte) {  // 2^(byte - 127)
+  return __uint_as_float(byte == 255 ? 0x7fc00000u : byte ? byte << 23 : 0x00400000u);
+}
+__device__ __forceinline__ float fp4_inverse(uint32_t byte) { return __uint_as_float((254u - min(byte, 253u)) << 23); }  // 2^(127 - byte)
+// Eight values, already over their scale, to 4 bits each, the first lowest; halves to even, at most 6.
+__device__ __forceinline__ uint32_t fp4_eight(const float *v) {
+  uint32_t r;
+  asm("{\n .reg .b8 a, b, c, d;\n"
+      " cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+      " cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n"
+      " mov.b32 %0, {a, b, c, d};\n}"
+      : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+  return r;
+}
+__device__ __forceinline__ void fp4_values(uint32_t q, float (&v)[8]) {
+  uint32_t h[4];
+  asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n"
+      " cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(q));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[i]));
+    v[2 * i] = f.x, v[2 * i + 1] = f.y;
+  }
+}
+
+// ---- quantisation --------------------------------------------------------------------------
+//
+// Bound by memory: two bytes (bf16) read and 17/32 written a value.  A warp takes 256 columns of four rows that are 32
+// apart, 8 columns a lane, so that a lane loads 16 bytes of bf16, a block's largest magnitude costs two shuffles, and
+// the four rows' scales of four blocks are 16 bytes in a row.
+struct Quant4Args {
+  const void *x;
+  int64_t rows, ldx, ldq, in_rows;
+  int cols, vec, runs;
+  const int64_t *gather;
+  const int64_t *offsets;  // of groups; nullptr: none
+  int groups;
+  uint8_t *q, *scale;
+};
+
+// The rows of tile slot `slot`: [row, end), none if row >= end.  Every lane of a warp comes here.
+__device__ __forceinline__ void slot_rows(const int64_t *offsets, int groups, int64_t rows, int64_t slot, int64_t &row, int64_t &end) {
+  if (!offsets) {
+    row = slot * 128, end = min(row + 128, rows);
+    return;
+  }
+  const int lane = threadIdx.x & 31;
+  auto cut = [&](int g) { return min(max(offsets[g], (int64_t)0), rows); };
+  // the last group whose tiles begin at the slot or before it: among every 32nd group (there are 1024 at most), then among 32
+  int g = lane * 32;
+  const uint32_t coarse = __ballot_sync(~0u, g < groups && cut(min(g, groups - 1)) / 128 + g <= slot);
+  row = 0, end = 0;
+  if (!(coarse & 1)) return;
+  const int base = (31 - __clz(coarse)) * 32;
+  g = base + lane;
+  const uint32_t fine = __ballot_sync(~0u, g < groups && cut(min(g, groups - 1)) / 128 + g <= slot);
+  if (!(fine & 1)) return;
+  g = base + 31 - __clz(fine);
+  const int64_t begin = cut(g);
+  row = begin + (slot - begin / 128 - g) * 128, end = min(row + 128, cut(g + 1));
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) tuna_quantize4_rows_kernel(Quant4Args a) {
+  wait_previous();
+  allow_next();
+  const int lane = threadIdx.x & 31, c = (int)blockIdx.y * 256 + lane * 8, run = (int)blockIdx.y * 2 + (lane >> 4);
+  const int64_t slot = blockIdx.x;
+  int64_t row0, end;
+  slot_rows(a.offsets, a.groups, a.rows, slot, row0, end);
+  for (int l = threadIdx.x >> 5; l < 32 && row0 + l < end; l += 8) {
+    Eight<T> x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t r = row0 + l + 32 * i;
+      const int64_t from = r >= end ? -1 : a.gather ? __ldg(a.gather + r) : r;
+      const bool there = from >= 0 && from < a.in_rows;
+      x[i].load(reinterpret_cast<const T *>(a.x) + (there ? from : 0) * a.ldx + c, a.vec, there ? a.cols - c : 0);
+    }
+    uint32_t words[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t r = row0 + l + 32 * i;
+      uint32_t amax = Eight<T>::top_bits(x[i].top(0));
+      amax = max(amax, __shfl_xor_sync(~0u, amax, 1));
+      amax = max(amax, __shfl_xor_sync(~0u, amax, 2));
+      const uint32_t byte = fp4_scale(amax);
+      const float by = fp4_inverse(byte);
+      float v[8];
+      x[i].values(v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] *= by;
+      if (r < end && c < (a.cols + 31) / 32 * 32) *reinterpret_cast<uint32_t *>(a.q + r * a.ldq + c / 2) = fp4_eight(v);
+      words[i] = byte << (lane & 12) * 2;
+      words[i] |= __shfl_xor_sync(~0u, words[i], 4);
+      words[i] |= __shfl_xor_sync(~0u, words[i], 8);
+    }
+    if ((lane & 15) == 0 && run < a.runs)
+      *reinterpret_cast<uint4 *>(a.scale + (slot * a.runs + run) * kScaleTile + l * 16) = make_uint4(words[0], words[1], words[2], words[3]);
+  }
+}
+
+// Blocks along the columns, for the turned matrix: a block of threads takes a 128 x 128 tile through shared memory in its
+// own type; a thread then has 32 rows, one scale block, of two columns, read as pairs.  The tile's scales are one tile of them.
+template <typename T>
+struct Turn {
+  static constexpr int kPitch = 128 + 16 / sizeof(T);  // rows stay on 16-byte boundaries, four banks apart
+  static constexpr size_t kSmem = 128 * kPitch * sizeof(T);
+};
+template <typename T>
+__global__ void __launch_bounds__(256) tuna_quantize4_columns_kernel(Quant4Args a) {
+  extern __shared__ __align__(16) char tile_raw[];
+  T *tile = reinterpret_cast<T *>(tile_raw);
+  constexpr int kPitch = Turn<T>::kPitch;
+  __shared__ __align__(16) uint8_t scales[kScaleTile];
+  wait_previous();
+  allow_next();
+  const int col_tiles = (a.cols + 127) / 128, col_tile = blockIdx.x % col_tiles, run = blockIdx.x / col_tiles;
+  const int64_t r0 = (int64_t)run * 128;
+  const int c0 = col_tile * 128, tid = threadIdx.x;
+  const int mine = tid >> 4, c = (tid & 15) * 8;  // rows mine, mine + 16, ...; columns c .. c + 7
+  Eight<T> x[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t r = r0 + mine + i * 16;
+    x[i].load(reinterpret_cast<const T *>(a.x) + r * a.ldx + c0 + c, a.vec, r < a.rows ? a.cols - c0 - c : 0);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int q = 0; q < Eight<T>::kWords; ++q) *reinterpret_cast<uint4 *>(tile + (mine + i * 16) * kPitch + c + q * (8 / Eight<T>::kWords)) = x[i].w[q];
+  __syncthreads();
+  const int two = (tid & 63) * 2, quarter = tid >> 6;  // columns two, two + 1; rows quarter * 32 ..
+  float t[2][32];
+  uint32_t top[2] = {0, 0};
+#pragma unroll
+  for (int r = 0; r < 32; ++r) {
+    const T *p = tile + (quarter * 32 + r) * kPitch + two;
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t u = *reinterpret_cast<const uint32_t *>(p);
+      t[0][r] = __uint_as_float(u << 16), t[1][r] = __uint_as_float(u & 0xffff0000u);
+    } else {
+      const float2 u = *reinterpret_cast<const float2 *>(p);
+      t[0][r] = u.x, t[1][r] = u.y;
+    }
+    top[0] = max(top[0], abs_bits(t[0][r])), top[1] = max(top[1], abs_bits(t[1][r]));
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const uint32_t byte = fp4_scale(top[e]);
+    const float by = fp4_inverse(byte);
+    const int col = two + e;
+    scales[(col & 31) * 16 + (col >> 5) * 4 + quarter] = (uint8_t)byte;
+#pragma unroll
+    for (int r = 0; r < 32; ++r) t[e][r] *= by;
+    if (c0 + col < a.cols && r0 + quarter * 32 < a.rows)
+      *reinterpret_cast<uint4 *>(a.q + (int64_t)(c0 + col) * a.ldq + (r0 + quarter * 32) / 2) =
+          make_uint4(fp4_eight(t[e]), fp4_eight(t[e] + 8), fp4_eight(t[e] + 16), fp4_eight(t[e] + 24));
+  }
+  __syncthreads();
+  if (tid < 32) reinterpret_cast<uint4 *>(a.scale + ((int64_t)col_tile * a.runs + run) * kScaleTile)[tid] = reinterpret_cast<const uint4 *>(scales)[tid];
+}
+
+// The values that 4-bit rows stand for, in the quantisation's arrangement.
+template <typename T>
+__global__ void __launch_bounds__(256) tuna_dequantize4_kernel(Quant4Args a, T *out, int64_t ldo) {
+  wait_previous();
+  allow_next();
+  const int lane = threadIdx.x & 31, c = (int)blockIdx.y * 256 + lane * 8, run = (int)blockIdx.y * 2 + (lane >> 4);
+  const int64_t slot = blockIdx.x;
+  int64_t row0, end;
+  slot_rows(a.offsets, a.groups, a.rows, slot, row0, end);
+  if (c >= a.cols) return;
+  const bool whole = c + 8 <= a.cols;
+  for (int l = threadIdx.x >> 5; l < 32 && row0 + l < end; l += 8) {
+    const uint4 s = *reinterpret_cast<const uint4 *>(a.scale + (slot * a.runs + run) * kScaleTile + l * 16);
+    const uint32_t words[4] = {s.x, s.y, s.z, s.w};
+    uint32_t q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t r = row0 + l + 32 * i;
+      const uint8_t *p = a.q + r * a.ldq + c / 2;
+      q[i] = 0;
+      if (r >= end) continue;
+      if (whole && a.vec) {
+        q[i] = __ldg(reinterpret_cast<const uint32_t *>(p));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (c + 2 * j < a.cols) q[i] |= (uint32_t)p[j] << (8 * j);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t r = row0 + l + 32 * i;
+      if (r >= end) continue;
+      const float by = fp4_power((words[i] >> (lane & 12) * 2) & 255);
+      float v[8];
+      fp4_values(q[i], v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] *= by;
+      T *o = out + r * ldo + c;
+      if (whole && a.vec) {
+        store_row(o, v);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (c + j < a.cols) o[j] = from_f32<T>(v[j]);
+      }
+    }
+  }
+}
+
+// ---- the product -----------------------------------------------------------------------------
+//
+// A persistent block takes tiles of 128 x BN.  One lane copies 128 x 256 values of a, BN x 256 of b and the scales of both
+// into a ring of stages; one elected lane moves a stage's scales into tensor memory, to columns that belong to the stage,
+// and issues its four tensor-core steps; eight warps read a finished accumulator back and store it.
+//
+// With `swiglu` the 256 columns are 128 rows of the gate matrix and the same 128 of the up matrix, so that a thread reads
+// both values of a place from its own row of the accumulator, and 32 of them are one block of the 4-bit result.
+struct Tile4Args {
+  Product4Args p;
+  int stages;   // of k: 256 values each
+  int n_tiles;
+  int store_tiles;     // bf16 results leave through map_out
+  uint32_t most_rows;  // row tiles, at most: their number times n_tiles, and a step beyond, fits 31 bits
+  int *error;
+};
+
+constexpr int kOutWarps = 8;
+constexpr int kThreads4 = 128 + kOutWarps * 32;
+constexpr int kSumPitch4 = 132;  // floats: rows of sums that a cluster joins, on 16-byte boundaries and four banks apart
+constexpr int kMaxGroups4 = TUNA_MOE_MAX_EXPERTS;
+
+template <int BN, bool STORES>
+struct Shape4 {
+  static constexpr int kStages = BN == 256 ? 3 : 5;
+  static constexpr int kScaleBytes = 1024 + BN / 128 * 1024;
+  static constexpr int kStageBytes = (128 + BN) * 128 + kScaleBytes;
+  static constexpr int kAccs = BN == 256 ? 1 : 2;              // accumulators
+  static constexpr int kScaleCols = 8 + BN / 128 * 8;          // tensor-memory columns of a stage's scales
+  static constexpr int kCols = BN / 2;                         // accumulator columns of a warp of the results
+  static constexpr int kOutBytes = STORES ? kOutWarps * 4096 : 0;  // 32 rows of 64 bf16 results a warp, on their way out
+  static_assert(kAccs * BN + kStages * kScaleCols <= 512);
+  static_assert(kStageBytes % 1024 == 0);
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kOutBytes + (kMaxGroups4 + 8) * 4 + 256;
+};
+
+__device__ __forceinline__ void tma_load_scales(uint32_t dst, const CUtensorMap *map, int run, int tile, uint32_t bar) { tma_load_3d(dst, map, 0, run, tile, bar); }
+// 512 bytes of scales to 4 columns of tensor memory, once for each quarter of the lanes
+__device__ __forceinline__ void tc_copy_scales(uint32_t to, uint32_t smem) {
+  // rows of 16 bytes, 8 of them 128 bytes apart, no swizzle
+  const uint64_t desc = (uint64_t)((smem & 0x3ffff) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(desc) : "memory");
+}
+// d[tmem] (+)= A (128 x 64) * B^T (N x 64), 4-bit values with a scale for each 32 of them
+__device__ __forceinline__ void tc_mma_fp4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, bool accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%5], [%6], p;\n}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate), "r"(sa), "r"(sb)
+      : "memory");
+}
+// Instruction descriptor: e2m1 operands, e8m0 scales, n columns, m rows; `half`: which two of a word's four scales
+__host__ __device__ constexpr uint32_t fp4_idesc(int m, int n, int half) {
+  return (1u << 7) | (1u << 10) | (1u << 23) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24) | ((uint32_t)(half * 2) << 29) | ((uint32_t)(half * 2) << 4);
+}
+
+// Tile t of the walk: the group it is in (never walked backwards), its rows and columns.
+struct Walk4 {
+  int g = 0;
+  int row, end;  // first row, end of the group's rows
+  int slot;      // tile of the rows' scales
+  int n0;
+};
+__device__ __forceinline__ void walk_to(Walk4 &w, int t, const Tile4Args &a, const int *tile_base, int bn) {
+  while (t >= tile_base[w.g + 1] * a.n_tiles) ++w.g;
+  const uint32_t mt = tile_base[w.g + 1] - tile_base[w.g], local = t - tile_base[w.g] * a.n_tiles;
+  const uint32_t n = local / mt, m = local - n * mt;  // rows fastest: blocks that run together share b
+  int64_t begin = 0, end = a.p.m;
+  if (a.p.offsets) begin = max(a.p.offsets[w.g], (int64_t)0), end = min(a.p.offsets[w.g + 1], a.p.m);
+  w.row = (int)begin + (int)m * 128, w.end = (int)end;
+  w.slot = (int)begin / 128 + w.g + (int)m;
+  w.n0 = n * bn;
+}
+
+// With SPLIT a cluster of 2 or 4 blocks shares one tile: each adds up a part of k, leaves its sums in its shared memory,
+// and adds up the parts of some of the rows from all of them, in order of k.
+template <int BN, bool SWIGLU, bool SPLIT, typename TO>
+__global__ void __launch_bounds__(kThreads4, 1)
+    tuna_product4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_sa,
+                         const __grid_constant__ CUtensorMap map_sb, const __grid_constant__ CUtensorMap map_out, const Tile4Args a) {
+  using S = Shape4<BN, !SWIGLU && !SPLIT && sizeof(TO) == 2>;
+  extern __shared__ char smem_raw[];
+  char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+  int *tile_base = (int *)(smem + (size_t)S::kStages * S::kStageBytes + S::kOutBytes);
+  uint64_t *bars = (uint64_t *)(tile_base + kMaxGroups4 + 8);
+  volatile int *given_up = (volatile int *)(bars + 2 * S::kStages + 2 * S::kAccs + 1);
+  uint32_t *tmem_at = (uint32_t *)(given_up + 1);
+  const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages, freed = done + 8 * S::kAccs, drained = freed + 8 * S::kAccs;
+  const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S::kStages; ++s) mbar_init(full + 8 * s, 1), mbar_init(empty + 8 * s, 1);
+    for (int s = 0; s < S::kAccs; ++s) mbar_init(done + 8 * s, 1), mbar_init(freed + 8 * s, kOutWarps);
+    mbar_init(drained, 1);
+    *given_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 2) tmem_alloc(smem_u32(tmem_at), 512);
+  wait_previous();
+  allow_next();
+  // Tiles of rows before each group, cut at most_rows, which groups that lie apart never come near.
+  if (warp == 1) {
+    uint32_t sum = 0;
+    for (int g0 = 0; g0 < a.p.groups; g0 += 32) {
+      const int g = g0 + lane;
+      int64_t rows = 0;
+      auto cut = [&](int64_t row) { return min(max(row, (int64_t)0), a.p.m); };
+      if (g < a.p.groups) rows = a.p.offsets ? cut(a.p.offsets[g + 1]) - cut(a.p.offsets[g]) : a.p.m;
+      const uint32_t mt = rows > 0 ? (uint32_t)((rows + 127) / 128) : 0;  // (2^24 at most: 32 of them and most_rows fit 32 bits)
+      uint32_t x = mt;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t y = __shfl_up_sync(~0u, x, d);
+        if (lane >= d) x += y;
+      }
+      if (g < a.p.groups) tile_base[g] = (int)min(sum + x - mt, a.most_rows);
+      sum = min(sum + __shfl_sync(~0u, x, 31), a.most_rows);
+    }
+    if (lane == 0) tile_base[a.p.groups] = (int)sum;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = __shfl_sync(~0u, *tmem_at, 0);
+  const int tiles = tile_base[a.p.groups] * a.n_tiles;
+  const int parts = SPLIT ? (int)cluster_size() : 1, part = SPLIT ? (int)cluster_rank() : 0;
+  const int first = (int)(SPLIT ? blockIdx.x / parts : blockIdx.x), step = (int)(SPLIT ? gridDim.x / parts : gridDim.x);
+  // this block's part of k
+  const int s_first = SPLIT ? (int)((int64_t)a.stages * part / parts) : 0, stages = SPLIT ? (int)((int64_t)a.stages * (part + 1) / parts) - s_first : a.stages;
+  constexpr int kTileN = SWIGLU ? BN / 2 : BN;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      // ---- copies
+      int stage = 0, phase = 0;
+      int64_t issued = 0;
+      const int tiles_n = (a.p.n + 127) / 128;
+      Walk4 w;
+      bool ok = true;
+      for (int t = first; ok && t < tiles; t += step) {
+        walk_to(w, t, a, tile_base, kTileN);
+        for (int s = 0; s < stages; ++s) {
+          if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, given_up))) break;
+          const uint32_t at = smem_u32(smem) + stage * S::kStageBytes, bar = full + 8 * stage, scales = at + (128 + BN) * 128;
+          mbar_expect(bar, S::kStageBytes);
+          const int col = (s_first + s) * 128, run = (s_first + s) * 2;
+          tma_load_2d(at, &map_a, col, w.row, bar);
+          tma_load_scales(scales, &map_sa, run, w.slot, bar);
+          if (SWIGLU) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              tma_load_3d(at + 128 * 128 + q * 128 * 128, &map_b, col, w.n0, w.g * 2 + q, bar);
+              tma_load_scales(scales + 1024 + q * 1024, &map_sb, run, (w.g * 2 + q) * tiles_n + w.n0 / 128, bar);
+            }
+          } else {
+            tma_load_3d(at + 128 * 128, &map_b, col, w.n0, w.g, bar);
+            tma_load_scales(scales + 1024, &map_sb, run, w.g * tiles_n + w.n0 / 128, bar);
+          }
+          ++issued;
+          if (++stage == S::kStages) stage = 0, phase ^= 1;
+        }
+      }
+      // nothing may land in shared memory after the block has gone, whichever warp gives up: the last copies are waited for
+      int never = 0;
+      for (int64_t i = max((int64_t)0, issued - S::kStages); i < issued; ++i)
+        mbar_wait(full + 8 * (int)(i % S::kStages), (uint32_t)((i / S::kStages) & 1), &never);
+    }
+  } else if (warp == 1) {
+    // ---- tensor cores: the whole warp goes along, one lane issues
+    int stage = 0, phase = 0, acc = 0, acc_phase = 0;
+    bool ok = true;
+    for (int t = first; ok && t < tiles; t += step) {
+      ok = __all_sync(~0u, mbar_wait(freed + 8 * acc, acc_phase ^ 1, given_up));
+      for (int s = 0; ok && s < stages; ++s) {
+        if (!(ok = __all_sync(~0u, mbar_wait(full + 8 * stage, phase, given_up)))) break;
+        tc_fence_after();
+        const uint32_t at = smem_u32(smem) + stage * S::kStageBytes, scales = at + (128 + BN) * 128;
+        const uint64_t da = tc_desc(at), db = tc_desc(at + 128 * 128);
+        const uint32_t ta = tmem + S::kAccs * BN + stage * S::kScaleCols, tb = ta + 8;
+        if (elect_one()) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {  // runs of 128 along k
+            tc_copy_scales(ta + r * 4, scales + r * 512);
+#pragma unroll
+            for (int q = 0; q < BN / 128; ++q) tc_copy_scales(tb + r * (BN / 32) + q * 4, scales + 1024 + q * 1024 + r * 512);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)  // 32 bytes along k
+            tc_mma_fp4(tmem + acc * BN, da + 2 * i, db + 2 * i, fp4_idesc(128, BN, i & 1), ta + (i >> 1) * 4, tb + (i >> 1) * (BN / 32), s > 0 || i > 0);
+          tc_commit(empty + 8 * stage);
+          if (s == stages - 1) tc_commit(done + 8 * acc);
+        }
+        __syncwarp();
+        if (++stage == S::kStages) stage = 0, phase ^= 1;
+      }
+      if (++acc == S::kAccs) acc = 0, acc_phase ^= 1;
+    }
+    // and no step may be under way when tensor memory is freed
+    int never = 0;
+    if (elect_one()) tc_commit(drained);
+    __syncwarp();
+    mbar_wait(drained, 0, &never);
+  } else if (warp >= 4) {
+    // ---- results: thread = one row, columns [half * kCols, ...) of the tile
+    const int half = (warp - 4) >> 2, row_in = (warp & 3) * 32 + lane;
+    const uint32_t from = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    int acc = 0, acc_phase = 0;
+    Walk4 w;
+    for (int t = first; t < tiles; t += step) {
+      walk_to(w, t, a, tile_base, kTileN);
+      if (!__all_sync(~0u, mbar_wait(done + 8 * acc, acc_phase, given_up))) break;  // (and the warp is whole for the loads)
+      tc_fence_after();
+      const uint32_t at = from + acc * BN;
+      auto release = [&] {  // everything is in registers: the accumulator may be filled again
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(freed + 8 * acc);
+      };
+      const int row = w.row + row_in;
+      const bool there = row < w.end;
+      if constexpr (SPLIT) {
+        // the sums to shared memory, where the stages were: every step that read them is done
+        float *red = (float *)smem + row_in * kSumPitch4 + half * S::kCols;
+#pragma unroll
+        for (int c = 0; c < S::kCols; c += 32) {
+          uint32_t v[32];
+          tmem_load(at + half * S::kCols + c, v);
+          tmem_wait(v);
+          if (there) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4 *>(red + c + i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+          }
+        }
+        release();
+      } else if constexpr (SWIGLU) {
+        const int c0 = half * 64;
+        uint32_t packed[2][4], bytes = 0;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          uint32_t g[32], u[32];
+          tmem_load(at + c0 + b * 32, g);
+          tmem_load(at + 128 + c0 + b * 32, u);
+          tmem_wait(g), tmem_wait(u);
+          if (b == 1) release();
+          float h[32];
+          uint32_t amax = 0;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const float x = __uint_as_float(g[i]);
+            h[i] = x / (1.0f + expf(-x)) * __uint_as_float(u[i]);
+            amax = max(amax, abs_bits(h[i]));
+          }
+          const uint32_t byte = fp4_scale(amax);
+          const float by = fp4_inverse(byte);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) h[i] *= by;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) packed[b][i] = fp4_eight(h + i * 8);
+          bytes |= byte << (8 * b);
+        }
+        if (there) {
+          uint8_t *out = (uint8_t *)a.p.out + (int64_t)row * a.p.ldo + (w.n0 + c0) / 2;  // (the pitch covers whole tiles)
+          *reinterpret_cast<uint4 *>(out) = make_uint4(packed[0][0], packed[0][1], packed[0][2], packed[0][3]);
+          *reinterpret_cast<uint4 *>(out + 16) = make_uint4(packed[1][0], packed[1][1], packed[1][2], packed[1][3]);
+          *reinterpret_cast<uint16_t *>(a.p.hs + ((int64_t)w.slot * a.n_tiles + w.n0 / 128) * kScaleTile + lane * 16 + (warp & 3) * 4 + half * 2) = (uint16_t)bytes;
+        }
+      } else if constexpr (sizeof(TO) == 2) {
+        uint32_t packed[S::kCols / 2];
+#pragma unroll
+        for (int c = 0; c < S::kCols; c += 32) {
+          uint32_t v[32];
+          tmem_load(at + half * S::kCols + c, v);
+          tmem_wait(v);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) packed[c / 2 + i] = pack_bf16(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+        }
+        release();
+        // 64 columns at a time to shared memory, in 16-byte pieces swizzled by row.  32 whole rows leave from there by a tensor
+        // copy; rows that a group's end cuts, or that a tensor copy cannot reach (a pitch that is no multiple of 16 bytes),
+        // leave in whole rows as the warp reads them back.
+        const uint32_t to = smem_u32(smem) + S::kStages * S::kStageBytes + (warp - 4) * 4096;
+        const int row0 = row - lane, valid = max(0, min(32, w.end - row0));
+#pragma unroll
+        for (int c = 0; c < S::kCols; c += 64) {
+          const int c0 = w.n0 + half * S::kCols + c;
+          if (lane == 0) tma_store_read();
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + lane * 128 + (i ^ (lane & 7)) * 16), "r"(packed[c / 2 + i * 4]),
+                         "r"(packed[c / 2 + i * 4 + 1]), "r"(packed[c / 2 + i * 4 + 2]), "r"(packed[c / 2 + i * 4 + 3])
+                         : "memory");
+          if (a.store_tiles && valid == 32) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0 && c0 < a.p.n) tma_store_2d(&map_out, c0, row0, to);
+          } else {
+            __syncwarp();
+            __nv_bfloat16 *out = (__nv_bfloat16 *)a.p.out + (int64_t)row0 * a.p.ldo + c0;
+            if (a.store_tiles && c0 + 64 <= a.p.n) {
+              for (int i = lane; i < valid * 8; i += 32) {
+                const int r = i / 8, piece = i % 8;
+                uint4 u;
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(to + r * 128 + (piece ^ (r & 7)) * 16) : "memory");
+                *reinterpret_cast<uint4 *>(out + r * a.p.ldo + piece * 8) = u;
+              }
+            } else {
+              const int cols = min(64, a.p.n - c0);
+              for (int r = 0; r < valid; ++r)
+                for (int j = lane; j < cols; j += 32) {
+                  uint16_t u;
+                  asm volatile("ld.shared.b16 %0, [%1];" : "=h"(u) : "r"(to + r * 128 + ((j >> 3) ^ (r & 7)) * 16 + (j & 7) * 2) : "memory");
+                  reinterpret_cast<uint16_t *>(out)[r * a.p.ldo + j] = u;
+                }
+            }
+          }
+          __syncwarp();
+        }
+      } else {
+        // 32-bit results, in whole 32-byte sectors
+        float *out = (float *)a.p.out + (int64_t)row * a.p.ldo;
+        const bool vec = (((uintptr_t)a.p.out | (uint64_t)a.p.ldo * 4) & 31) == 0;
+#pragma unroll
+        for (int c = 0; c < S::kCols; c += 32) {
+          uint32_t v[32];
+          tmem_load(at + half * S::kCols + c, v);
+          tmem_wait(v);
+          if (c + 32 == S::kCols) release();
+          const int c0 = w.n0 + half * S::kCols + c;
+          if (!there) continue;
+#pragma unroll
+          for (int i = 0; i < 32; i += 8) {
+            if (vec && c0 + i + 8 <= a.p.n) {
+              const uint32_t u[8] = {v[i], v[i + 1], v[i + 2], v[i + 3], v[i + 4], v[i + 5], v[i + 6], v[i + 7]};
+              store32(out + c0 + i, u);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (c0 + i + j < a.p.n) out[c0 + i + j] = __uint_as_float(v[i + j]);
+            }
+          }
+        }
+      }
+      __syncwarp();
+      if (++acc == S::kAccs) acc = 0, acc_phase ^= 1;
+    }
+    if (S::kOutBytes && lane == 0) tma_store_done();
+  }
+  __syncwarp();
+  if constexpr (SPLIT) {
+    cluster_meet();
+    if (first < tiles && !*given_up) {
+      Walk4 w;
+      walk_to(w, first, a, tile_base, BN);
+      const int rows = min(128, w.end - w.row);
+      for (int i = threadIdx.x; i < (rows - part + parts - 1) / parts * (BN / 4); i += kThreads4) {
+        const int r = part + i / (BN / 4) * parts, c = i % (BN / 4) * 4;
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int q = 0; q < parts; ++q) {
+          const float4 x = load_from_block(smem_u32(smem) + (r * kSumPitch4 + c) * 4, q);
+          v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+        }
+        TO *out = (TO *)a.p.out + (int64_t)(w.row + r) * a.p.ldo + w.n0 + c;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (w.n0 + c + j < a.p.n) out[j] = from_f32<TO>(v[j]);
+      }
+    }
+    cluster_meet();  // no block leaves while its sums are read
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 2) tmem_free(tmem, 512);
+  if (threadIdx.x == 0 && *given_up) *a.error = 1;
+}
+
+// ---- host ------------------------------------------------------------------------------------
+
+template <int BN, bool SWIGLU, typename TO, bool SPLIT = false>
+int run_tiles4(const Product4Args &p, cudaStream_t st, int parts = 1) {
+  using S = Shape4<BN, !SWIGLU && !SPLIT && sizeof(TO) == 2>;
+  Tile4Args a = {};
+  a.p = p;
+  const int64_t bytes = ceil_div(p.k, 2), runs = ceil_div(p.k, 128), tiles_n = ceil_div(p.n, 128), matrices = (int64_t)p.groups * (SWIGLU ? 2 : 1);
+  a.stages = (int)ceil_div(p.k, 256);
+  a.n_tiles = (int)ceil_div(p.n, SWIGLU ? BN / 2 : BN);
+  a.most_rows = (INT32_MAX - (1 << 20)) / a.n_tiles;
+  a.error = error_word();
+  if (!a.error) return TUNA_ERR_CUDA;
+  CUtensorMap ma, mb, msa, msb, mo;
+  if (const int rc = make_map(&ma, 2, p.a, bytes, p.m, 1, p.lda, 128)) return rc;
+  if (const int rc = make_map(&mb, 3, p.b, bytes, p.n, matrices, p.ldb, SWIGLU ? 128 : BN)) return rc;
+  if (const int rc = make_scale_map(&msa, p.sa, runs, fp4_slots(p.m, p.offsets ? p.groups : 0), 1)) return rc;
+  if (const int rc = make_scale_map(&msb, p.sb, runs, matrices * tiles_n, SWIGLU ? 1 : BN / 128)) return rc;
+  mo = ma;
+  a.store_tiles = S::kOutBytes && aligned(p.out, 16) && p.ldo % 8 == 0 && p.n % 8 == 0;  // (a tensor copy's rows end on 16 bytes)
+  if (a.store_tiles)
+    if (const int rc = make_out_map(&mo, p.out, p.n, p.m, p.ldo, 128)) return rc;
+  static bool set[64] = {};
+  auto kernel = tuna_product4_kernel<BN, SWIGLU, SPLIT, TO>;
+  if (const int rc = allow_smem(kernel, S::kSmem, set)) return rc;
+  const int64_t most = (ceil_div(p.m, 128) + (p.offsets ? p.groups : 0)) * a.n_tiles;
+  if (SPLIT) return launch_cluster(kernel, dim3((unsigned)(most * parts)), parts, kThreads4, S::kSmem, st, false, ma, mb, msa, msb, mo, a);
+  return launch(kernel, dim3((unsigned)std::min<int64_t>(most, sm_count())), kThreads4, S::kSmem, st, false, ma, mb, msa, msb, mo, a);
+}
+
+size_t dtype_size(int dtype) { return dtype == TUNA_DTYPE_F32 ? 4 : dtype == TUNA_DTYPE_BF16 ? 2 : 0; }
+
+}  // namespace
+
+int launch_product4(const Product4Args &p, cudaStream_t st) {
+  if (p.swiglu) return run_tiles4<256, true, uint8_t>(p, st);
+  const int64_t rows = ceil_div(p.m, 128) + (p.offsets ? p.groups - 1 : 0);
+  const int64_t wide = rows * ceil_div(p.n, 256), narrow = rows * ceil_div(p.n, 128);
+  if (6 * ceil_div(wide, sm_count()) < 5 * ceil_div(narrow, sm_count()))
+    return p.out_f32 ? run_tiles4<256, false, float>(p, st) : run_tiles4<256, false, __nv_bfloat16>(p, st);
+  if (!p.offsets) {
+    const int64_t stages = ceil_div(p.k, 256);
+    int parts = 4;
+    while (parts > 1 && (narrow * parts > 128 || stages - stages / parts < 6)) parts /= 2;
+    if (parts > 1) return p.out_f32 ? run_tiles4<128, false, float, true>(p, st, parts) : run_tiles4<128, false, __nv_bfloat16, true>(p, st, parts);
+  }
+  return p.out_f32 ? run_tiles4<128, false, float>(p, st) : run_tiles4<128, false, __nv_bfloat16>(p, st);
+}
+
+int launch_quantize4_rows(const void *x, bool f32, int64_t rows, int cols, int64_t ldx, const int64_t *gather, int64_t in_rows, int groups,
+                          const int64_t *offsets, void *q, int64_t ldq, uint8_t *scale, cudaStream_t st) {
+  Quant4Args a = {};
+  a.x = x, a.rows = rows, a.cols = cols, a.ldx = ldx, a.gather = gather, a.in_rows = in_rows, a.groups = groups, a.offsets = offsets;
+  a.q = (uint8_t *)q, a.ldq = ldq, a.scale = scale, a.runs = (int)ceil_div(cols, 128);
+  a.vec = aligned(x, 16) && ldx * (f32 ? 4 : 2) % 16 == 0;
+  const dim3 grid((unsigned)fp4_slots(rows, offsets ? groups : 0), (unsigned)ceil_div(cols, 256));
+  return f32 ? launch(tuna_quantize4_rows_kernel<float>, grid, 256, 0, st, false, a)
+             : launch(tuna_quantize4_rows_kernel<__nv_bfloat16>, grid, 256, 0, st, false, a);
+}
+
+}  // namespace tuna_ops
+
+using namespace tuna_ops;
+
+static int check_groups4(int64_t rows, int cols, int groups, const int64_t *offsets) {
+  if (groups < 0 || (groups > 0) != (offsets != nullptr)) return TUNA_ERR_INVALID_ARG;
+  if (groups > TUNA_MOE_MAX_EXPERTS || cols > kMaxDim || rows > INT32_MAX - 256) return TUNA_ERR_RANGE;
+  return TUNA_OK;
+}
+
+extern "C" {
+
+int tuna_fp4_scale_tiles(int64_t rows, int groups, int64_t *tiles) {
+  if (!tiles || rows < 0 || groups < 0) return TUNA_ERR_INVALID_ARG;
+  *tiles = fp4_slots(rows, groups);
+  return TUNA_OK;
+}
+
+int tuna_fp4_quantize(const void *x, int dtype, int64_t rows, int cols, int64_t ldx, int layout, int groups, const int64_t *offsets, void *q,
+                      int64_t ldq, void *scale, void *stream) {
+  const size_t size = dtype_size(dtype);
+  if (!size || rows < 0 || cols < 0 || ldx < cols || (layout != TUNA_FP4_ROWS && layout != TUNA_FP4_COLUMNS)) return TUNA_ERR_INVALID_ARG;
+  if (layout == TUNA_FP4_COLUMNS && offsets) return TUNA_ERR_INVALID_ARG;
+  if (const int rc = check_groups4(rows, cols, groups, offsets)) return rc;
+  if (ldq % 16 != 0 || ldq < ceil_div(layout == TUNA_FP4_COLUMNS ? rows : cols, 2)) return TUNA_ERR_INVALID_ARG;
+  if (layout == TUNA_FP4_COLUMNS && (rows > kMaxDim || ceil_div(rows, 128) * ceil_div(cols, 128) > INT32_MAX)) return TUNA_ERR_RANGE;
+  if (rows == 0 || cols == 0) return TUNA_OK;
+  if (!x || !q || !scale || !aligned(x, size) || !aligned(q, 16) || !aligned(scale, 16) || !aligned(offsets, 8)) return TUNA_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  const bool f32 = dtype == TUNA_DTYPE_F32;
+  if (layout == TUNA_FP4_ROWS) return launch_quantize4_rows(x, f32, rows, cols, ldx, nullptr, rows, groups, offsets, q, ldq, (uint8_t *)scale, st);
+  Quant4Args a = {};
+  a.x = x, a.rows = rows, a.cols = cols, a.ldx = ldx, a.q = (uint8_t *)q, a.ldq = ldq, a.scale = (uint8_t *)scale, a.runs = (int)ceil_div(rows, 128);
+  a.vec = aligned(x, 16) && ldx * size % 16 == 0;
+  const dim3 grid((unsigned)(ceil_div(rows, 128) * ceil_div(cols, 128)));
+  static bool set[2][64] = {};
+  if (f32) {
+    if (const int rc = allow_smem(tuna_quantize4_columns_kernel<float>, Turn<float>::kSmem, set[0])) return rc;
+    return launch(tuna_quantize4_columns_kernel<float>, grid, 256, Turn<float>::kSmem, st, false, a);
+  }
+  if (const int rc = allow_smem(tuna_quantize4_columns_kernel<__nv_bfloat16>, Turn<__nv_bfloat16>::kSmem, set[1])) return rc;
+  return launch(tuna_quantize4_columns_kernel<__nv_bfloat16>, grid, 256, Turn<__nv_bfloat16>::kSmem, st, false, a);
+}
+
+int tuna_fp4_dequantize(const void *q, int64_t ldq, const void *scale, int64_t rows, int cols, int groups, const int64_t *offsets, void *out,
+                        int out_dtype, int64_t ldo, void *stream) {
+  const size_t size = dtype_size(out_dtype);
+  if (!size || rows < 0 || cols < 0 || ldq < ceil_div(cols, 2) || ldo < cols) return TUNA_ERR_INVALID_ARG;
+  if (const int rc = check_groups4(rows, cols, groups, offsets)) return rc;
+  if (rows == 0 || cols == 0) return TUNA_OK;
+  if (!q || !scale || !out || !aligned(scale, 16) || !aligned(out, size) || !aligned(offsets, 8)) return TUNA_ERR_INVALID_ARG;
+  Quant4Args a = {};
+  a.rows = rows, a.cols = cols, a.groups = groups, a.offsets = offsets, a.q = (uint8_t *)q, a.ldq = ldq, a.scale = (uint8_t *)scale;
+  a.runs = (int)ceil_div(cols, 128);
+  a.vec = aligned(q, 4) && ldq % 4 == 0 && aligned(out, 16) && ldo * size % 16 == 0;
+  const dim3 grid((unsigned)fp4_slots(rows, groups), (unsigned)ceil_div(cols, 256));
+  cudaStream_t st = (cudaStream_t)stream;
+  return out_dtype == TUNA_DTYPE_F32 ? launch(tuna_dequantize4_kernel<float>, grid, 256, 0, st, false, a, (float *)out, ldo)
+                                     : launch(tuna_dequantize4_kernel<__nv_bfloat16>, grid, 256, 0, st, false, a, (__nv_bfloat16 *)out, ldo);
+}
+
+int tuna_fp4_matmul(const void *a, const void *a_scale, int64_t m, int64_t lda, const void *b, const void *b_scale, int n, int64_t ldb, int k, int groups,
+                    const int64_t *offsets, void *out, int out_dtype, int64_t ldo, void *stream) {
+  const size_t so = dtype_size(out_dtype);
+  if (!so || m < 0 || n < 0 || k < 0 || k % 2 || lda < k / 2 || ldb < k / 2 || ldo < n || lda % 16 || ldb % 16) return TUNA_ERR_INVALID_ARG;
+  if (const int rc = check_groups4(m, n, groups, offsets)) return rc;
+  if (k > kMaxDim) return TUNA_ERR_RANGE;
+  const int matrices = std::max(groups, 1);
+  if (matrices * (ceil_div(m, 128) + 1) * ceil_div(n, 128) > INT32_MAX) return TUNA_ERR_RANGE;  // tiles, whatever the offsets hold
+  if (m == 0 || n == 0) return TUNA_OK;
+  if (!out || !aligned(out, so)) return TUNA_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (k == 0) return note_cuda(cudaMemset2DAsync(out, ldo * so, 0, n * so, m, st));  // an empty sum
+  if (!a || !b || !a_scale || !b_scale || !aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 16) || !aligned(b_scale, 16) || !aligned(offsets, 8))
+    return TUNA_ERR_INVALID_ARG;
+  Product4Args p = {};
+  p.a = a, p.b = b, p.sa = (const uint8_t *)a_scale, p.sb = (const uint8_t *)b_scale, p.m = m, p.n = n, p.k = k, p.lda = lda, p.ldb = ldb, p.ldo = ldo;
+  p.groups = matrices, p.offsets = offsets, p.out = out, p.out_f32 = out_dtype == TUNA_DTYPE_F32;
+  return launch_product4(p, st);
+}
+
+}  // extern "C"

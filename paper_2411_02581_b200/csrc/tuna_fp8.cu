@@ -640,10 +640,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 
 // ---- host ------------------------------------------------------------------------------------
 
-}  // namespace
-static int make_out_map(CUtensorMap *map, void *p, int64_t cols, int64_t rows, int64_t ld, int row_bytes);
-namespace {
-
 template <int BN, bool SWIGLU, bool B_ROWS, typename TO, bool SPLIT = false>
 int run_tiles(const ProductArgs &p, cudaStream_t st, int parts = 1) {
   using S = Shape<BN, !SWIGLU && !SPLIT && sizeof(TO) == 2>;
@@ -727,8 +723,7 @@ int make_map(CUtensorMap *map, int rank, const void *p, int64_t k, int64_t rows,
   return r == CUDA_SUCCESS ? TUNA_OK : note_cuda(cudaErrorInvalidValue);
 }
 
-// bf16 results: boxes of `row_bytes` (128 or 64, swizzled alike) x 32 rows.
-static int make_out_map(CUtensorMap *map, void *p, int64_t cols, int64_t rows, int64_t ld, int row_bytes) {
+int make_out_map(CUtensorMap *map, void *p, int64_t cols, int64_t rows, int64_t ld, int row_bytes) {
   EncodeTiled f = encoder();
   if (!f) return TUNA_ERR_CUDA;
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
@@ -737,6 +732,17 @@ static int make_out_map(CUtensorMap *map, void *p, int64_t cols, int64_t rows, i
   const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p, dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                        row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? TUNA_OK : note_cuda(cudaErrorInvalidValue);
+}
+
+int make_scale_map(CUtensorMap *map, const void *p, int64_t runs, int64_t tiles, int box) {
+  EncodeTiled f = encoder();
+  if (!f) return TUNA_ERR_CUDA;
+  const cuuint64_t dims[3] = {128, (cuuint64_t)runs, (cuuint64_t)tiles};
+  const cuuint64_t strides[2] = {512, (cuuint64_t)(512 * runs)};
+  const cuuint32_t boxes[3] = {128, 2, (cuuint32_t)box}, ones[3] = {1, 1, 1};
+  const CUresult r = f(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void *>(p), dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                       CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? TUNA_OK : note_cuda(cudaErrorInvalidValue);
 }
 

@@ -1,4 +1,4 @@
-// Shared by the mixture-of-experts operators (tuna_route.cu, tuna_fp8.cu, tuna_moe.cu):
+// Shared by the mixture-of-experts operators (tuna_route.cu, tuna_balance.cu, tuna_fp8.cu, tuna_fp4.cu, tuna_moe.cu):
 // launch helper, argument checks, small device helpers, and the PTX of barriers,
 // tensor copies and the fifth-generation tensor cores.
 #ifndef TUNA_OPS_CUH
@@ -75,6 +75,12 @@ int make_map(CUtensorMap *map, int rank, const void *p, int64_t k, int64_t rows,
 // The same for gate and up matrices that alternate (groups x 2 x rows x k bytes, rows a multiple of 32):
 // boxes of 128 bytes x 32 rows x gate, up x 4, so that one copy brings the rows that a tile interleaves.
 int make_gate_up_map(CUtensorMap *map, const void *p, int64_t k, int64_t rows, int64_t groups, int64_t ld);
+
+// bf16 results: boxes of `row_bytes` (128 or 64, swizzled alike) x 32 rows.
+int make_out_map(CUtensorMap *map, void *p, int64_t cols, int64_t rows, int64_t ld, int row_bytes);
+
+// Scales of 4-bit operands: tiles x runs x 512 bytes; boxes of 512 bytes x 2 runs x `box` tiles (tuna_fp4.cu).
+int make_scale_map(CUtensorMap *map, const void *p, int64_t runs, int64_t tiles, int box);
 
 // Carves a caller's workspace into 256-byte aligned pieces; with base == nullptr it only adds up.
 struct Carve {

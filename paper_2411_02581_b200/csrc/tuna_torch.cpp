@@ -13,6 +13,7 @@
 
 #include <algorithm>
 #include <optional>
+#include <utility>
 
 #include "tuna.h"
 
@@ -20,7 +21,9 @@ namespace {
 
 #define TUNA_CALLS(X)                                                                                       \
   X(tuna_moe_route_workspace_bytes) X(tuna_moe_route) X(tuna_moe_route_backward) X(tuna_fp8_quantize) \
-  X(tuna_fp8_matmul) X(tuna_moe_few)
+  X(tuna_fp8_matmul) X(tuna_moe_few) X(tuna_moe_balance_workspace_bytes) X(tuna_moe_balance) X(tuna_moe_balance_backward)  \
+  X(tuna_fp4_quantize) X(tuna_fp4_dequantize) X(tuna_fp4_matmul) X(tuna_fp4_expert_rows_workspace_bytes) X(tuna_fp4_expert_rows) \
+  X(tuna_fp4_experts_workspace_bytes) X(tuna_fp4_experts)
 #define X(f) decltype(&f) p_##f = nullptr;
 TUNA_CALLS(X)
 #undef X
@@ -334,6 +337,237 @@ PyObject *few(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// The segments' bounds: int64 [segments + 1], or None for one segment.
+const int64_t *segments_of(PyObject *o, const Tensor &with, int64_t &segments) {
+  segments = 1;
+  if (o == Py_None) return nullptr;
+  const Tensor &t = tensor(o, "offsets");
+  if (t.dim() != 1 || t.size(0) < 2) refuse("offsets: [segments + 1] is wanted");
+  segments = t.size(0) - 1;
+  dense(t, "offsets", at::kLong, {segments + 1}, with);
+  return (const int64_t *)at_of(t);
+}
+
+// balance(logits, ids, scoring, offsets, stream)
+PyObject *balance(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 5, [&] {
+    const Tensor &z = tensor(a[0], "logits"), &ids = tensor(a[1], "ids");
+    const int64_t ld = matrix(z, "logits", true, true, false), t = z.size(0), e = z.size(1);
+    if (ids.dim() != 2) refuse("ids: [tokens, k] is wanted");
+    const int64_t k = ids.size(1);
+    dense(ids, "ids", at::kInt, {t, k}, z);
+    int64_t segments;
+    const int64_t *offsets = segments_of(a[3], z, segments);
+    const Place place(a[4], z);
+    size_t need = 0;
+    check(p_tuna_moe_balance_workspace_bytes(t, clip(e), clip(segments), &need), "tuna_moe_balance_workspace_bytes");
+    Tensor ws;
+    if (need) ws = make({(int64_t)need}, at::kByte, z);
+    const Tensor loss = make({segments}, at::kFloat, z), squares = make({segments}, at::kFloat, z), counts = make({segments, e}, at::kLong, z),
+                 mass = make({segments, e}, at::kFloat, z), live = make({segments}, at::kLong, z);
+    check(p_tuna_moe_balance(at_of(z), dtype_of(z), t, clip(e), ld, (const int32_t *)at_of(ids), clip(k), small(a[2]), clip(segments), offsets,
+                             (float *)at_of(loss), (float *)at_of(squares), (int64_t *)at_of(counts), (float *)at_of(mass), (int64_t *)at_of(live),
+                             need ? at_of(ws) : nullptr, need, place.stream()),
+          "tuna_moe_balance");
+    return pack(place.out(loss), place.out(squares), place.out(counts), place.out(mass), place.out(live));
+  });
+}
+
+// balance_backward(logits, counts, tokens, k, dloss, dz, scoring, offsets, stream)
+PyObject *balance_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 9, [&] {
+    const Tensor &z = tensor(a[0], "logits"), &counts = tensor(a[1], "counts"), &live = tensor(a[2], "tokens"), &dloss = tensor(a[4], "dloss");
+    const int64_t ld = matrix(z, "logits", true, true, false), t = z.size(0), e = z.size(1), k = integer(a[3]);
+    int64_t segments;
+    const int64_t *offsets = segments_of(a[7], z, segments);
+    dense(counts, "counts", at::kLong, {segments, e}, z);
+    dense(live, "tokens", at::kLong, {segments}, z);
+    dense(dloss, "dloss", at::kFloat, {segments}, z);
+    const float *dz = nullptr;
+    if (a[5] != Py_None) {
+      const Tensor &o = tensor(a[5], "dz");
+      dense(o, "dz", at::kFloat, {segments}, z);
+      dz = (const float *)at_of(o);
+    }
+    const Place place(a[8], z);
+    const Tensor d = make({t, e}, z.scalar_type(), z);
+    check(p_tuna_moe_balance_backward(at_of(z), dtype_of(z), t, clip(e), ld, clip(k), small(a[6]), clip(segments), offsets, (const int64_t *)at_of(counts),
+                                      (const int64_t *)at_of(live), (const float *)at_of(dloss), dz, at_of(d), std::max<int64_t>(e, 1), place.stream()),
+          "tuna_moe_balance_backward");
+    return THPVariable_Wrap(place.out(d));
+  });
+}
+
+constexpr at::ScalarType kFp4 = at::ScalarType::Float4_e2m1fn_x2, kPower = at::ScalarType::Float8_e8m0fnu;
+
+// The groups' bounds: int64 [groups + 1], or None (0 groups).
+const int64_t *groups_of(PyObject *o, const Tensor &with, int64_t &groups) {
+  groups = 0;
+  if (o == Py_None) return nullptr;
+  const Tensor &t = tensor(o, "offsets");
+  if (t.dim() != 1 || t.size(0) < 2) refuse("offsets: [groups + 1] is wanted");
+  groups = t.size(0) - 1;
+  dense(t, "offsets", at::kLong, {groups + 1}, with);
+  return (const int64_t *)at_of(t);
+}
+int64_t scale_tiles(int64_t rows, int64_t groups) { return groups ? rows / 128 + groups : (rows + 127) / 128; }
+
+// A matrix of 4-bit values, two a byte; its pitch in bytes.
+int64_t matrix4(const Tensor &t, const char *name) {
+  if (t.dim() != 2 || t.scalar_type() != kFp4) refuse("%s: a CUDA matrix of float4_e2m1fn_x2 is wanted", name);
+  const int64_t rows = t.size(0), cols = t.size(1);
+  if ((cols > 1 && t.stride(1) != 1) || (rows > 1 && t.stride(0) < cols))
+    refuse("%s: rows must be contiguous and must not overlap (strides %lld, %lld)", name, (long long)t.stride(0), (long long)t.stride(1));
+  return rows > 1 ? t.stride(0) : std::max<int64_t>(cols, 1);
+}
+// The same for a product: rows on 16-byte boundaries, the tensor itself or a copy.
+Tensor operand4(const Tensor &q, const char *name, int64_t &ld) {
+  ld = matrix4(q, name);
+  if (q.size(0) <= 1) ld = (q.size(1) + 15) / 16 * 16;  // the pitch of a single row is free
+  if (ld % 16 == 0 && (uintptr_t)q.data_ptr() % 16 == 0) {
+    ld = std::max<int64_t>(ld, 16);
+    return q;
+  }
+  ld = std::max<int64_t>((q.size(1) + 15) / 16 * 16, 16);
+  Tensor p = make({q.size(0), ld}, at::kByte, q).zero_();
+  p.narrow(1, 0, q.size(1)).copy_(q.view(at::kByte));
+  return p;
+}
+
+// fp4_quantize(x, layout, offsets, stream)
+PyObject *fp4_quantize(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 4, [&] {
+    const Tensor &x = tensor(a[0], "x");
+    const int64_t ld = matrix(x, "x", true, true, false), rows = x.size(0), cols = x.size(1);
+    const int layout = small(a[1]);
+    const bool turned = layout == TUNA_FP4_COLUMNS;
+    if (turned && a[2] != Py_None) refuse("offsets go with the layout rows");
+    int64_t groups;
+    const int64_t *offsets = groups_of(a[2], x, groups);
+    const int64_t out_rows = turned ? cols : rows, out_cols = turned ? rows : cols, bytes = (out_cols + 1) / 2, pitch = (bytes + 15) / 16 * 16;
+    const Place place(a[3], x);
+    const Tensor q = make({out_rows, pitch}, kFp4, x), scale = make({scale_tiles(out_rows, groups), (out_cols + 127) / 128, 32, 4, 4}, kPower, x);
+    check(p_tuna_fp4_quantize(at_of(x), dtype_of(x), rows, clip(cols), ld, layout, clip(groups), offsets, at_of(q), pitch, at_of(scale),
+                              place.stream()),
+          "tuna_fp4_quantize");
+    place.out(q), place.out(scale);
+    return pack(pitch == bytes ? q : q.narrow(1, 0, bytes), scale);
+  });
+}
+
+// fp4_dequantize(q, scale, offsets, out_dtype, stream)
+PyObject *fp4_dequantize(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 5, [&] {
+    const Tensor &q = tensor(a[0], "q"), &scale = tensor(a[1], "scale");
+    const int64_t ld = matrix4(q, "q"), rows = q.size(0), cols = 2 * q.size(1);
+    int64_t groups;
+    const int64_t *offsets = groups_of(a[2], q, groups);
+    dense(scale, "scale", kPower, {scale_tiles(rows, groups), (cols + 127) / 128, 32, 4, 4}, q);
+    const int out = small(a[3]);
+    const Place place(a[4], q);
+    const Tensor y = make({rows, cols}, out == TUNA_DTYPE_F32 ? at::kFloat : at::kBFloat16, q);
+    check(p_tuna_fp4_dequantize(at_of(q), ld, at_of(scale), rows, clip(cols), clip(groups), offsets, at_of(y), out, std::max<int64_t>(cols, 1),
+                                place.stream()),
+          "tuna_fp4_dequantize");
+    return THPVariable_Wrap(place.out(y));
+  });
+}
+
+// fp4_matmul(a, a_scale, b, b_scale, offsets, out_dtype, stream)
+PyObject *fp4_matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 7, [&] {
+    const Tensor &left = tensor(a[0], "a"), &sa = tensor(a[1], "a_scale"), &right = tensor(a[2], "b"), &sb = tensor(a[3], "b_scale");
+    if (right.device() != left.device()) refuse("b: on another device than its fellow");
+    int64_t groups;
+    const int64_t *offsets = groups_of(a[4], left, groups);
+    const int out = small(a[5]);
+    const Place place(a[6], left);
+    int64_t lda = 0, ldb = 0, cols, kb;
+    const Tensor x = operand4(left, "a", lda);
+    const int64_t m = left.size(0), k = 2 * left.size(1), runs = (k + 127) / 128;
+    Tensor w;
+    if (offsets) {
+      if (right.dim() != 3 || !right.is_contiguous() || right.size(0) != groups) refuse("b: contiguous matrices [%lld, n, k / 2] go with these offsets", (long long)groups);
+      cols = right.size(1), kb = 2 * right.size(2);
+      w = operand4(right.view({groups * cols, right.size(2)}), "b", ldb);
+      dense(sb, "b_scale", kPower, {groups, (cols + 127) / 128, runs, 32, 4, 4}, left);
+    } else {
+      w = operand4(right, "b", ldb);
+      cols = right.size(0), kb = 2 * right.size(1);
+      dense(sb, "b_scale", kPower, {(cols + 127) / 128, runs, 32, 4, 4}, left);
+    }
+    if (kb != k) refuse("a has %lld columns, b %lld", (long long)k, (long long)kb);
+    dense(sa, "a_scale", kPower, {scale_tiles(m, groups), runs, 32, 4, 4}, left);
+    const Tensor y = make({m, cols}, out == TUNA_DTYPE_F32 ? at::kFloat : at::kBFloat16, left);
+    check(p_tuna_fp4_matmul(at_of(x), at_of(sa), m, lda, at_of(w), at_of(sb), clip(cols), ldb, clip(k), clip(groups), offsets, at_of(y), out,
+                            std::max<int64_t>(cols, 1), place.stream()),
+          "tuna_fp4_matmul");
+    return THPVariable_Wrap(place.out(y));
+  });
+}
+
+// Checked 4-bit expert weights; (experts, inter) of them.
+std::pair<int64_t, int64_t> weights4(PyObject *const *w, int64_t hidden, const Tensor &with) {
+  const Tensor &w13 = tensor(w[0], "w13"), &s13 = tensor(w[1], "s13"), &w2 = tensor(w[2], "w2"), &s2 = tensor(w[3], "s2");
+  if (w13.dim() != 4) refuse("w13: [experts, 2, inter, hidden / 2] is wanted");
+  if (hidden % 2) refuse("x: an even number of columns is wanted");
+  const int64_t e = w13.size(0), i = w13.size(2), bi = (i + 127) / 128, bd = (hidden + 127) / 128;
+  dense(w13, "w13", kFp4, {e, 2, i, hidden / 2}, with);
+  dense(s13, "s13", kPower, {e, 2, bi, bd, 32, 4, 4}, with);
+  dense(w2, "w2", kFp4, {e, hidden, i / 2}, with);
+  dense(s2, "s2", kPower, {e, bd, bi, 32, 4, 4}, with);
+  return {e, i};
+}
+// A workspace: the caller's, or one of the call's own.
+Tensor space(PyObject *given, size_t need, const Tensor &with) {
+  if (given == Py_None) return make({(int64_t)std::max<size_t>(need, 256)}, at::kByte, with);
+  const Tensor &t = tensor(given, "workspace");
+  if (!t.is_contiguous()) refuse("workspace: a contiguous tensor is wanted");
+  if (t.device() != with.device()) refuse("workspace: on another device than its fellow");
+  return t;
+}
+
+// fp4_expert_rows(x, offsets, w13, s13, w2, s2, workspace, stream)
+PyObject *fp4_expert_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 8, [&] {
+    const Tensor &x = tensor(a[0], "x"), &offsets = tensor(a[1], "offsets");
+    const int64_t ld = matrix(x, "x", false, true, false), rows = x.size(0), d = x.size(1);
+    const auto [e, i] = weights4(a + 2, d, x);
+    dense(offsets, "offsets", at::kLong, {e + 1}, x);
+    size_t need = 0;
+    const Place place(a[7], x);
+    check(p_tuna_fp4_expert_rows_workspace_bytes(rows, clip(e), clip(d), clip(i), &need), "tuna_fp4_expert_rows_workspace_bytes");
+    const Tensor ws = space(a[6], need, x), y = make({rows, d}, at::kBFloat16, x);
+    check(p_tuna_fp4_expert_rows(at_of(x), ld, rows, clip(e), (const int64_t *)at_of(offsets), clip(d), clip(i), at_of(tensor(a[2], "w13")),
+                                 at_of(tensor(a[3], "s13")), at_of(tensor(a[4], "w2")), at_of(tensor(a[5], "s2")), at_of(y), std::max<int64_t>(d, 1),
+                                 at_of(ws), ws.nbytes(), place.stream()),
+          "tuna_fp4_expert_rows");
+    return THPVariable_Wrap(place.out(y));
+  });
+}
+
+// fp4_experts(x, ids, weights, w13, s13, w2, s2, workspace, stream)
+PyObject *fp4_experts(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(n, 9, [&] {
+    const Tensor &x = tensor(a[0], "x"), &ids = tensor(a[1], "ids"), &weights = tensor(a[2], "weights");
+    const int64_t ld = matrix(x, "x", false, true, false), t = x.size(0), d = x.size(1);
+    if (ids.dim() != 2) refuse("ids: [tokens, k] is wanted");
+    const int64_t k = ids.size(1);
+    dense(ids, "ids", at::kInt, {t, k}, x);
+    dense(weights, "weights", at::kFloat, {t, k}, x);
+    const auto [e, i] = weights4(a + 3, d, x);
+    size_t need = 0;
+    const Place place(a[8], x);
+    check(p_tuna_fp4_experts_workspace_bytes(t, clip(e), clip(k), clip(d), clip(i), &need), "tuna_fp4_experts_workspace_bytes");
+    const Tensor ws = space(a[7], need, x), out = make({t, d}, at::kBFloat16, x);
+    check(p_tuna_fp4_experts(at_of(x), ld, t, (const int32_t *)at_of(ids), (const float *)at_of(weights), clip(k), clip(e), clip(d), clip(i),
+                             at_of(tensor(a[3], "w13")), at_of(tensor(a[4], "s13")), at_of(tensor(a[5], "w2")), at_of(tensor(a[6], "s2")), at_of(out),
+                             std::max<int64_t>(d, 1), at_of(ws), ws.nbytes(), place.stream()),
+          "tuna_fp4_experts");
+    return THPVariable_Wrap(place.out(out));
+  });
+}
+
 // bind(handle of the loaded library, raise_status)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return guarded(n, 2, [&]() -> PyObject * {
@@ -353,7 +587,8 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 
 #define F(f) {#f, (PyCFunction)(void (*)())f, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {F(route), F(route_backward), F(fp8_quantize), F(fp8_matmul), F(few), F(bind), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {F(route), F(route_backward), F(fp8_quantize), F(fp8_matmul), F(few), F(balance), F(balance_backward), F(fp4_quantize),
+                         F(fp4_dequantize), F(fp4_matmul), F(fp4_expert_rows), F(fp4_experts), F(bind), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "tuna_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,5 +1,5 @@
-"""Mixture-of-experts operators over torch tensors: router, 8-bit block-scaled products,
-experts, few-token layer.
+"""Mixture-of-experts operators over torch tensors: router and its balance loss, 8-bit block-scaled and
+4-bit microscaled products, experts, few-token layer.
 
 A thin layer over the C ABI in ``include/tuna.h``, like :mod:`binding`: arguments are
 checked and marshalled, outputs and workspaces come from torch's allocator, every
@@ -11,10 +11,10 @@ and copies are its own.  An input that was made on another stream is the caller'
 order, as with any torch operation, and so is an output before another stream reads it.
 
 Nothing here is recorded by autograd: outputs carry no gradient, whatever the inputs require.
-Gradients are calls of their own (:func:`route_backward`, :func:`combine_backward`, and
-:func:`fp8_matmul` on operands quantised along the other axis), which a
-``torch.autograd.Function`` of the caller's may make; :func:`experts`, :func:`expert_rows`
-and :func:`few` have none.
+Gradients are calls of their own (:func:`route_backward`, :func:`balance_backward`,
+:func:`combine_backward`, and :func:`fp8_matmul` or :func:`fp4_matmul` on operands quantised along the
+other axis), which a ``torch.autograd.Function`` of the caller's may make; :func:`experts`,
+:func:`expert_rows`, their 4-bit forms and :func:`few` have none.
 """
 from __future__ import annotations
 
@@ -33,6 +33,8 @@ from . import build as _build
 SOFTMAX, SIGMOID = 0, 1
 SCORING = {"softmax": SOFTMAX, "sigmoid": SIGMOID}
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2}
+FP4, POWER = torch.float4_e2m1fn_x2, torch.float8_e8m0fnu  # two values a byte; the scale of 32 values
+FP4_LAYOUTS = {"rows": 0, "columns": 1}
 LAYOUTS = {"rows": 0, "columns": 1, "tiles": 2, "tiles_t": 3}
 FLOATS = (torch.float32, torch.bfloat16)
 
@@ -45,6 +47,15 @@ class Routing(NamedTuple):
     offsets: torch.Tensor  # int64 [ranks * experts + 1]
     rows: torch.Tensor     # int64 [tokens * k]
     pos: torch.Tensor      # int64 [tokens, k]
+
+
+class Balance(NamedTuple):
+    """What :func:`balance` returns; see ``tuna_moe_balance`` for each."""
+    loss: torch.Tensor     # float32 [segments]
+    z: torch.Tensor        # float32 [segments]
+    counts: torch.Tensor   # int64 [segments, experts]
+    mass: torch.Tensor     # float32 [segments, experts]
+    tokens: torch.Tensor   # int64 [segments]: live tokens
 
 
 def _same(*tensors):
@@ -176,6 +187,19 @@ def route_backward(logits, ids, dweights, *, scoring="softmax", renormalize=Fals
     return (_marshal or _fast()).route_backward(logits, ids, dweights, _scoring(scoring), renormalize, scale, stream)
 
 
+def balance(logits, ids, *, scoring="softmax", offsets=None, stream=None) -> Balance:
+    """The balance loss of every segment of the tokens, the mean square of the logits' log-sum-exp, and what they are
+    made of (``tuna_moe_balance``).  ``ids`` as :func:`route` makes them; ``offsets`` (int64 [segments + 1]): the segments'
+    bounds, None for one segment."""
+    return Balance(*(_marshal or _fast()).balance(logits, ids, _scoring(scoring), offsets, stream))
+
+
+def balance_backward(logits, counts, tokens, k, dloss, dz=None, *, scoring="softmax", offsets=None, stream=None):
+    """Gradient of sum(dloss * loss + dz * z) of :func:`balance` with respect to the logits (``tuna_moe_balance_backward``);
+    ``k``: slots a token.  A row takes part if it has a logit that is not masked."""
+    return (_marshal or _fast()).balance_backward(logits, counts, tokens, k, dloss, dz, _scoring(scoring), offsets, stream)
+
+
 def combine(y, weights, pos, *, out_dtype=torch.bfloat16, stream=None):
     """out[t] = sum over s of weights[t, s] * y[pos[t, s]] (``tuna_moe_combine``)."""
     ld = _matrix(y, "y", FLOATS)
@@ -233,6 +257,49 @@ def fp8_matmul(a, a_scale, b, b_scale, *, offsets=None, b_blocks="tiles", out_dt
     if out_dtype not in FLOATS:
         raise ValueError(f"out_dtype: one of {FLOATS}")
     return (_marshal or _fast()).fp8_matmul(a, a_scale, b, b_scale, offsets, LAYOUTS[b_blocks], DTYPES[out_dtype], stream)
+
+
+def fp4_quantize(x, layout="rows", *, offsets=None, stream=None):
+    """(q, scale): ``x`` in 4 bits with a power of two for every 32 values along the row (``tuna_fp4_quantize``).
+
+    ``q`` (float4_e2m1fn_x2: two values an element, the first in its low half) is [rows, (cols + 1) // 2], of the layout "columns"
+    that of the transposed matrix.  ``scale`` (float8_e8m0fnu) is [row tiles, runs of 128 columns, 32, 4, 4]: that of row r and
+    block j of a run is at [r // 128, run, r % 32, r % 128 // 32, j].  With ``offsets`` (int64 [groups + 1]) the row tiles
+    are of rows of one group each, as :func:`fp4_matmul` with these offsets takes them."""
+    which = FP4_LAYOUTS.get(layout)
+    if which is None:
+        raise ValueError(f"layout: one of {', '.join(FP4_LAYOUTS)}, got {layout!r}")
+    return (_marshal or _fast()).fp4_quantize(x, which, offsets, stream)
+
+
+def fp4_dequantize(q, scale, *, offsets=None, out_dtype=torch.bfloat16, stream=None):
+    """The values that ``q`` stands for, [rows, 2 * q.shape[1]] (``tuna_fp4_dequantize``); a row outside every group is undefined."""
+    if out_dtype not in FLOATS:
+        raise ValueError(f"out_dtype: one of {FLOATS}")
+    return (_marshal or _fast()).fp4_dequantize(q, scale, offsets, DTYPES[out_dtype], stream)
+
+
+def fp4_matmul(a, a_scale, b, b_scale, *, offsets=None, out_dtype=torch.bfloat16, stream=None):
+    """a b^T of operands that :func:`fp4_quantize` made along the contracted axis (``tuna_fp4_matmul``).
+
+    ``b`` [n, k / 2], or [groups, n, k / 2] with ``offsets`` (int64 [groups + 1]): rows offsets[g] .. offsets[g + 1] of
+    ``a``, which was quantised with these offsets, meet ``b[g]``; a row of the result that is outside every group is undefined."""
+    if out_dtype not in FLOATS:
+        raise ValueError(f"out_dtype: one of {FLOATS}")
+    return (_marshal or _fast()).fp4_matmul(a, a_scale, b, b_scale, offsets, DTYPES[out_dtype], stream)
+
+
+def fp4_expert_rows(x, offsets, w13, s13, w2, s2, *, workspace=None, stream=None):
+    """:func:`expert_rows` with weights, x and h in 4 bits (``tuna_fp4_expert_rows``).
+
+    ``w13`` [experts, 2, inter, hidden / 2] and ``w2`` [experts, hidden, inter / 2] with ``s13`` and ``s2`` of every matrix
+    as :func:`fp4_quantize` makes them; hidden and inter are multiples of 32."""
+    return (_marshal or _fast()).fp4_expert_rows(x, offsets, w13, s13, w2, s2, workspace, stream)
+
+
+def fp4_experts(x, ids, weights, w13, s13, w2, s2, *, workspace=None, stream=None):
+    """:func:`experts` with weights, x and h in 4 bits (``tuna_fp4_experts``); weights as in :func:`fp4_expert_rows`."""
+    return (_marshal or _fast()).fp4_experts(x, ids, weights, w13, s13, w2, s2, workspace, stream)
 
 
 def _experts_weights(w13, s13, w2, s2, hidden, device):
