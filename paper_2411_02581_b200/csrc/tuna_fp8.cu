@@ -662,7 +662,7 @@ int run_tiles(const ProductArgs &p, cudaStream_t st, int parts = 1) {
     if (const int rc = make_map(&mb, 3, p.b, p.k, p.n, (int64_t)p.groups * (SWIGLU ? 2 : 1), p.ldb, SWIGLU ? 32 : BN)) return rc;
   }
   mo = ma;
-  a.store_tiles = S::kOutBytes && !SWIGLU && !p.out_f32 && aligned(p.out, 16) && p.ldo % 8 == 0;
+  a.store_tiles = S::kOutBytes && !SWIGLU && !p.out_f32 && aligned(p.out, 16) && p.ldo % 8 == 0 && p.n % 8 == 0;  // (a tensor copy's rows end on 16 bytes)
   if (a.store_tiles)
     if (const int rc = make_out_map(&mo, p.out, p.n, p.m, p.ldo, S::kRowBytes)) return rc;
   static bool set[64] = {}, fits = false;
