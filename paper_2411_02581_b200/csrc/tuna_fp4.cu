@@ -485,7 +485,7 @@ __global__ void __launch_bounds__(kThreads4, 1)
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             const float x = __uint_as_float(g[i]);
-            h[i] = x / (1.0f + expf(-x)) * __uint_as_float(u[i]);
+            h[i] = __fdividef(x, 1.0f + expf(-x)) * __uint_as_float(u[i]);  // (within 2^-21; 0 from x = -87 down)
             amax = max(amax, abs_bits(h[i]));
           }
           const uint32_t byte = fp4_scale(amax);
