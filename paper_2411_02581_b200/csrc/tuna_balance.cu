@@ -16,18 +16,17 @@
 namespace tuna_ops {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kSumThreads = 1024;
 
 struct BalanceArgs {
   const void *logits;
   const int32_t *ids;
   const int64_t *offsets;  // segments + 1, or nullptr: one segment of all tokens
   int64_t tokens, ld, ldd;
-  int experts, k, scoring, segments, vec;
+  int experts, k, scoring, segments;
   int64_t chunk;  // tokens of a block
   // a block's part of a segment, [block + segment]: both only rise along the tokens, so no two parts meet
-  float *part_mass;    // [slots][experts]
-  int *part_count;     // [slots][experts]
+  float2 *part;        // [slots][experts]: sum of probabilities; choices (as an int)
   float2 *part_token;  // [slots]: sum of lse^2; live tokens (as an int)
   float *loss, *z, *mass;
   int64_t *counts, *live;
@@ -62,8 +61,28 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
-// A token's probabilities from its logits: the softmax, its logarithm of sums, and with sigmoids their shares (in p) and
-// the complements 1 - sigmoid (in rest).  A masked logit (-inf, NaN) has none; a token without any other is not live.
+// A lane's logits of a token, VPL of them from `first` on; a masked one (NaN, or behind the last) is -inf.
+template <int VPL, typename T>
+struct Logits {
+  Eight<T> w[VPL / 8];
+  int left;
+  __device__ __forceinline__ void load(const BalanceArgs &a, int64_t t, int first, bool there) {
+    left = there ? a.experts - first : 0;
+    const T *p = reinterpret_cast<const T *>(a.logits) + (there ? t : 0) * a.ld + first;
+#pragma unroll
+    for (int i = 0; i < VPL / 8; ++i) w[i].load_any(p + 8 * i, left - 8 * i);
+  }
+  __device__ __forceinline__ void values(float (&z)[VPL]) const {
+#pragma unroll
+    for (int i = 0; i < VPL / 8; ++i) w[i].values(z + 8 * i);
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) z[i] = i < left ? logit_of(z[i]) : -INFINITY;
+  }
+};
+
+// A token's probabilities from its logits: the softmax, the logarithm of its sum, and with sigmoids their shares (in p) and
+// the complements 1 - sigmoid (in rest).  A masked logit has none; a token without any other is not live.
+// (__expf is within 2 + 1.2 |x| units of 2^-24, which is 2^-19 where a probability is over e^-25.)
 template <int LPT, int VPL>
 struct Token {
   float soft[VPL], p[VPL], rest[VPL];
@@ -75,42 +94,54 @@ struct Token {
     for (int i = 0; i < VPL; ++i) top = fmaxf(top, z[i]);
     top = group_max<LPT>(top);
     live = top != -INFINITY;
+    const bool endless = top == INFINITY;  // those that hold +inf share the softmax
+    const float base = live && !endless ? top : 0.0f;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+      soft[i] = __expf(z[i] - base);
+      if (endless) soft[i] = z[i] == INFINITY ? 1.0f : 0.0f;
+      sum += soft[i];
+    }
     if (want_soft || scoring == TUNA_MOE_SOFTMAX) {
-      float sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < VPL; ++i) soft[i] = z[i] == -INFINITY ? 0.0f : exp_of(z[i], top), sum += soft[i];
       sum = group_sum<LPT>(sum);
-      const float by = live ? 1.0f / sum : 0.0f;
+      const float by = live ? __fdividef(1.0f, sum) : 0.0f;
+      if (scoring == TUNA_MOE_SOFTMAX) {
 #pragma unroll
-      for (int i = 0; i < VPL; ++i) soft[i] *= by;
-      lse = live ? top + logf(sum) : 0.0f;
-    }
-    if (scoring == TUNA_MOE_SIGMOID) {
-      // sigmoid(z) e^-m = e^(min(z, 0) - m) / (1 + e^-|z|) with m = min(largest z, 0): no share of very negative
-      // logits is 0 / 0
-      const float m = fminf(top, 0.0f);
-      float sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < VPL; ++i) {
-        const float e = expf(-fabsf(z[i])), one = 1.0f / (1.0f + e);
-        p[i] = z[i] == -INFINITY ? 0.0f : expf(fminf(z[i], 0.0f) - m) * one;
-        rest[i] = z[i] >= 0.0f ? e * one : one;
-        sum += p[i];
+        for (int i = 0; i < VPL; ++i) p[i] = soft[i] = soft[i] * by;
+        lse = live ? top + __logf(sum) : 0.0f;
+        return;
       }
-      sum = group_sum<LPT>(sum);
-      const float by = live ? 1.0f / sum : 0.0f;
-#pragma unroll
-      for (int i = 0; i < VPL; ++i) p[i] *= by;
+      lse = live ? top + __logf(sum) : 0.0f;
+      shares(z, top, by);
     } else {
-#pragma unroll
-      for (int i = 0; i < VPL; ++i) p[i] = soft[i];
+      shares(z, top, 0.0f);
     }
+  }
+  // sigmoid(z) e^-m = e^(min(z, 0) - m) / (1 + e^-|z|) with m = min(top, 0): no share of very negative logits is 0 / 0.
+  // The first exponential is 1 or the second one where some logit is not negative, and the softmax's where none is.
+  __device__ __forceinline__ void shares(const float (&z)[VPL], float top, float by_soft) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+      const float e = __expf(-fabsf(z[i])), one = __fdividef(1.0f, 1.0f + e);
+      const bool up = z[i] >= 0.0f;
+      p[i] = (top < 0.0f ? soft[i] : up ? 1.0f : e) * one;
+      rest[i] = up ? e * one : one;
+      soft[i] *= by_soft;
+      sum += p[i];
+    }
+    sum = group_sum<LPT>(sum);
+    const float by = live ? __fdividef(1.0f, sum) : 0.0f;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) p[i] *= by;
   }
 };
 
-// loss and z of a segment by a whole block; thread e, e + kThreads, ... brings the sums of its experts
+// loss and z of a segment by a whole block, whose threads bring the products of their experts
+template <int THREADS>
 __device__ __forceinline__ void finish(const BalanceArgs &a, int g, double product, double squares, int64_t n) {
-  __shared__ double sum[kThreads / 32];
+  __shared__ double sum[THREADS / 32];
 #pragma unroll
   for (int d = 16; d; d >>= 1) product += __shfl_xor_sync(~0u, product, d);
   __syncthreads();
@@ -118,7 +149,7 @@ __device__ __forceinline__ void finish(const BalanceArgs &a, int g, double produ
   __syncthreads();
   if (threadIdx.x == 0) {
     double all = 0.0;
-    for (int w = 0; w < kThreads / 32; ++w) all += sum[w];
+    for (int w = 0; w < THREADS / 32; ++w) all += sum[w];
     a.loss[g] = n ? (float)(all * a.experts / ((double)a.k * n * n)) : 0.0f;
     if (a.z) a.z[g] = n ? (float)(squares / n) : 0.0f;
     a.live[g] = n;
@@ -153,15 +184,13 @@ __global__ void __launch_bounds__(kThreads) tuna_balance_kernel(BalanceArgs a) {
       const int id = a.ids[i];
       if (id >= 0 && id < a.experts) atomicAdd(count + id, 1);
     }
-    for (int64_t tb = t0; tb < t1; tb += kStep) {  // (uniform: the shuffles need whole warps)
-      const int64_t t = tb + threadIdx.x / LPT;
+    Logits<VPL, T> next;
+    int64_t t = t0 + threadIdx.x / LPT;
+    next.load(a, t, sub * VPL, t < t1);
+    for (int64_t tb = t0; tb < t1; tb += kStep, t += kStep) {  // (uniform: the shuffles need whole warps)
       float z[VPL];
-      if (t < t1) {
-        load_logits(reinterpret_cast<const T *>(a.logits) + t * a.ld, sub * VPL, a.experts, a.vec, z);
-      } else {
-#pragma unroll
-        for (int i = 0; i < VPL; ++i) z[i] = -INFINITY;
-      }
+      next.values(z);
+      next.load(a, t + kStep, sub * VPL, t + kStep < t1);  // on its way during this one
       Token<LPT, VPL> token;
       token.of(z, a.scoring, a.z != nullptr);
 #pragma unroll
@@ -198,40 +227,62 @@ __global__ void __launch_bounds__(kThreads) tuna_balance_kernel(BalanceArgs a) {
         a.mass[(int64_t)g * a.experts + e] = m, a.counts[(int64_t)g * a.experts + e] = count[e];
         product += (double)m * count[e];
       } else {
-        a.part_mass[slot * a.experts + e] = m, a.part_count[slot * a.experts + e] = count[e];
+        a.part[slot * a.experts + e] = make_float2(m, __int_as_float(count[e]));
       }
     }
-    if (ALONE) finish(a, g, product, all_squares, all_live);
+    if (ALONE) finish<kThreads>(a, g, product, all_squares, all_live);
     else if (threadIdx.x == 0) a.part_token[slot] = make_float2(all_squares, __int_as_float(all_live));
     __syncthreads();
   }
 }
 
-// A block a segment: the parts of the blocks that met it, in their order.
-__global__ void __launch_bounds__(kThreads) tuna_balance_sum_kernel(BalanceArgs a) {
+// A block a segment: the parts of the blocks that met it, every 8th (or 16th, 32nd ...) of them by one row of threads, then the
+// rows in order.
+__global__ void __launch_bounds__(kSumThreads) tuna_balance_sum_kernel(BalanceArgs a) {
+  __shared__ float mass[kSumThreads];
+  __shared__ int count[kSumThreads];
+  __shared__ double squares[kSumThreads / 32];
+  __shared__ int live[kSumThreads / 32];
   wait_previous();
   allow_next();
   const int g = blockIdx.x;
   const int64_t begin = bound_of(a, g), end = bound_of(a, g + 1);
   const int64_t s0 = begin / a.chunk + g, s1 = end > begin ? (end - 1) / a.chunk + g + 1 : s0;
-  double product = 0.0, squares = 0.0;
-  int64_t n = 0;
-  for (int e = threadIdx.x; e < a.experts; e += kThreads) {
-    float m = 0.0f;
-    int64_t c = 0;
-#pragma unroll 8
-    for (int64_t s = s0; s < s1; ++s) m += a.part_mass[s * a.experts + e], c += a.part_count[s * a.experts + e];
-    a.mass[(int64_t)g * a.experts + e] = m, a.counts[(int64_t)g * a.experts + e] = c;
-    product += (double)m * c;
-  }
-  if (threadIdx.x == 0) {
-#pragma unroll 8
-    for (int64_t s = s0; s < s1; ++s) {
-      const float2 v = a.part_token[s];
-      squares += v.x, n += __float_as_int(v.y);
+  const int lanes = a.experts <= 32 ? 32 : (a.experts + 31) / 32 * 32, rows = kSumThreads / lanes;  // (512 experts: 2 rows)
+  const int e = threadIdx.x % lanes, row = threadIdx.x / lanes;
+  float m = 0.0f;
+  int c = 0;
+  if (row < rows && e < a.experts) {
+#pragma unroll 4
+    for (int64_t s = s0 + row; s < s1; s += rows) {
+      const float2 v = a.part[s * a.experts + e];
+      m += v.x, c += __float_as_int(v.y);
     }
   }
-  finish(a, g, product, squares, n);
+  mass[threadIdx.x] = m, count[threadIdx.x] = c;
+  double q = 0.0;
+  int n = 0;
+  for (int64_t s = s0 + threadIdx.x; s < s1; s += kSumThreads) {
+    const float2 v = a.part_token[s];
+    q += v.x, n += __float_as_int(v.y);
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) q += __shfl_xor_sync(~0u, q, d), n += __shfl_xor_sync(~0u, n, d);
+  if (threadIdx.x % 32 == 0) squares[threadIdx.x / 32] = q, live[threadIdx.x / 32] = n;
+  __syncthreads();
+  double product = 0.0;
+  if (threadIdx.x < a.experts) {
+    int64_t all = 0;
+    m = 0.0f;
+    for (int r = 0; r < rows; ++r) m += mass[r * lanes + threadIdx.x], all += count[r * lanes + threadIdx.x];
+    a.mass[(int64_t)g * a.experts + threadIdx.x] = m, a.counts[(int64_t)g * a.experts + threadIdx.x] = all;
+    product = (double)m * all;
+  }
+  double all_squares = 0.0;
+  int64_t all_live = 0;
+  if (threadIdx.x == 0)
+    for (int w = 0; w < kSumThreads / 32; ++w) all_squares += squares[w], all_live += live[w];
+  finish<kSumThreads>(a, g, product, all_squares, all_live);
 }
 
 template <int LPT, int VPL, typename T>
@@ -244,15 +295,13 @@ __global__ void __launch_bounds__(kThreads) tuna_balance_grad_kernel(BalanceArgs
   float pull[VPL], pull_z = 0.0f;  // G, and dz 2 / n
   int g = segment_of(a, b0), known = -1;
   int64_t end = g >= 0 ? bound_of(a, g + 1) : bound_of(a, 0);
-  for (int64_t tb = b0; tb < b1; tb += kStep) {
-    const int64_t t = tb + threadIdx.x / LPT;
+  Logits<VPL, T> next;
+  int64_t t = b0 + threadIdx.x / LPT;
+  next.load(a, t, sub * VPL, t < b1);
+  for (int64_t tb = b0; tb < b1; tb += kStep, t += kStep) {
     float z[VPL];
-    if (t < b1) {
-      load_logits(reinterpret_cast<const T *>(a.logits) + t * a.ld, sub * VPL, a.experts, a.vec, z);
-    } else {
-#pragma unroll
-      for (int i = 0; i < VPL; ++i) z[i] = -INFINITY;
-    }
+    next.values(z);
+    next.load(a, t + kStep, sub * VPL, t + kStep < b1);  // on its way during this one
     while (t >= end && g < a.segments) ++g, end = g < a.segments ? bound_of(a, g + 1) : INT64_MAX;
     const bool inside = t < b1 && g >= 0 && g < a.segments;
     if (inside && g != known) {
@@ -279,13 +328,8 @@ __global__ void __launch_bounds__(kThreads) tuna_balance_grad_kernel(BalanceArgs
     }
     if (t < b1) {
       T *out = reinterpret_cast<T *>(a.dlogits) + t * a.ldd + sub * VPL;
-      if (a.vec && sub * VPL + VPL <= a.experts) {
-        store_row(out, d);
-      } else {
 #pragma unroll
-        for (int i = 0; i < VPL; ++i)
-          if (sub * VPL + i < a.experts) out[i] = from_f32<T>(d[i]);
-      }
+      for (int i = 0; i < VPL; i += 8) store_any(out + i, reinterpret_cast<const float(&)[8]>(d[i]), a.experts - sub * VPL - i);
     }
   }
 }
@@ -307,9 +351,11 @@ struct Rows {  // tokens that a block takes at a time
   int operator()() { return kThreads / LPT; }
 };
 
+// Tokens of a block: one step where that leaves four blocks a multiprocessor or fewer, as many as keep it at that otherwise; all of
+// them where one block is done with them before a second launch would be.
 int64_t chunk_of(int64_t tokens, int experts) {
-  const int64_t step = by_experts(experts, Rows{});
-  return std::max<int64_t>(1, ceil_div(ceil_div(tokens, 296), step)) * step;
+  const int64_t step = by_experts(experts, Rows{}), steps = ceil_div(tokens, step);
+  return std::max<int64_t>(1, steps <= 4 ? steps : ceil_div(steps, 592)) * step;
 }
 
 template <typename T>
@@ -322,7 +368,7 @@ struct BalanceLaunch {
     const int64_t blocks = ceil_div(a.tokens, a.chunk);
     if (blocks == 1) return launch(tuna_balance_kernel<LPT, VPL, true, T>, dim3(1), kThreads, smem, st, false, a);
     if (const int rc = launch(tuna_balance_kernel<LPT, VPL, false, T>, dim3((unsigned)blocks), kThreads, smem, st, false, a)) return rc;
-    return launch(tuna_balance_sum_kernel, dim3((unsigned)a.segments), kThreads, 0, st, false, a);
+    return launch(tuna_balance_sum_kernel, dim3((unsigned)a.segments), kSumThreads, 0, st, false, a);
   }
 };
 template <typename T>
@@ -344,8 +390,7 @@ int check_balance(int64_t tokens, int experts, int k, int segments) {
 }
 void carve(Carve &c, BalanceArgs &a) {
   const int64_t slots = ceil_div(a.tokens, a.chunk) + a.segments;
-  a.part_mass = c.take<float>(slots * a.experts);
-  a.part_count = c.take<int>(slots * a.experts);
+  a.part = c.take<float2>(slots * a.experts);
   a.part_token = c.take<float2>(slots);
 }
 
@@ -388,7 +433,7 @@ int tuna_moe_balance(const void *logits, int dtype, int64_t tokens, int experts,
   if (!logits || !ids || !aligned(logits, size) || !aligned(ids, 4)) return TUNA_ERR_INVALID_ARG;
   BalanceArgs a = {};
   a.logits = logits, a.ids = ids, a.offsets = offsets, a.tokens = tokens, a.ld = ld, a.experts = experts, a.k = k, a.scoring = scoring;
-  a.segments = segments, a.vec = aligned(logits, 16) && ld * size % 16 == 0, a.chunk = chunk_of(tokens, experts);
+  a.segments = segments, a.chunk = chunk_of(tokens, experts);
   a.loss = loss, a.z = z, a.counts = counts, a.mass = mass, a.live = live;
   if (tokens > a.chunk) {
     Carve c(workspace);
@@ -409,8 +454,7 @@ int tuna_moe_balance_backward(const void *logits, int dtype, int64_t tokens, int
   if (!logits || !counts || !live || !dloss || !dlogits || !aligned(logits, size) || !aligned(dlogits, size)) return TUNA_ERR_INVALID_ARG;
   BalanceArgs a = {};
   a.logits = logits, a.offsets = offsets, a.tokens = tokens, a.ld = ld, a.ldd = ldd, a.experts = experts, a.k = k, a.scoring = scoring;
-  a.segments = segments, a.vec = aligned(logits, 16) && aligned(dlogits, 16) && ld * size % 16 == 0 && ldd * size % 16 == 0;
-  a.chunk = chunk_of(tokens, experts);
+  a.segments = segments, a.chunk = chunk_of(tokens, experts);
   a.counts = (int64_t *)counts, a.live = (int64_t *)live, a.dloss = dloss, a.dz = dz, a.dlogits = dlogits;
   cudaStream_t st = (cudaStream_t)stream;
   return dtype == TUNA_DTYPE_F32 ? by_experts(experts, BalanceGradLaunch<float>{a, st}) : by_experts(experts, BalanceGradLaunch<__nv_bfloat16>{a, st});

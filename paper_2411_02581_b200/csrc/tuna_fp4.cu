@@ -51,11 +51,12 @@ __device__ __forceinline__ void fp4_values(uint32_t q, float (&v)[8]) {
 //
 // Bound by memory: two bytes (bf16) read and 17/32 written a value.  A warp takes 256 columns of four rows that are 32
 // apart, 8 columns a lane, so that a lane loads 16 bytes of bf16, a block's largest magnitude costs two shuffles, and
-// the four rows' scales of four blocks are 16 bytes in a row.
+// the four rows' scales of four blocks are 16 bytes in a row.  A block of threads takes eight such sets of rows, a quarter of a
+// tile, and `strips` times 256 columns of them, the next ones on their way during the present ones.
 struct Quant4Args {
   const void *x;
   int64_t rows, ldx, ldq, in_rows;
-  int cols, vec, runs;
+  int cols, runs, strips;
   const int64_t *gather;
   const int64_t *offsets;  // of groups; nullptr: none
   int groups;
@@ -88,23 +89,29 @@ template <typename T>
 __global__ void __launch_bounds__(256) tuna_quantize4_rows_kernel(Quant4Args a) {
   wait_previous();
   allow_next();
-  const int lane = threadIdx.x & 31, c = (int)blockIdx.y * 256 + lane * 8, run = (int)blockIdx.y * 2 + (lane >> 4);
-  const int64_t slot = blockIdx.x;
+  const int lane = threadIdx.x & 31, l = (blockIdx.x & 3) * 8 + (threadIdx.x >> 5);
+  const int64_t slot = blockIdx.x >> 2;
   int64_t row0, end;
   slot_rows(a.offsets, a.groups, a.rows, slot, row0, end);
-  for (int l = threadIdx.x >> 5; l < 32 && row0 + l < end; l += 8) {
-    Eight<T> x[4];
+  if (row0 + l >= end) return;
+  const T *from[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t r = row0 + l + 32 * i;
+    const int64_t at = r >= end ? -1 : a.gather ? __ldg(a.gather + r) : r;
+    from[i] = at >= 0 && at < a.in_rows ? reinterpret_cast<const T *>(a.x) + at * a.ldx : nullptr;
+  }
+  int c = (int)blockIdx.y * a.strips * 256 + lane * 8;
+  Eight<T> x[4];
+  auto fetch = [&](int c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i].load_any(from[i] + c, from[i] ? a.cols - c : 0);
+  };
+  fetch(c);
+  for (int n = 0; n < a.strips && c - lane * 8 < a.cols; ++n, c += 256) {
+    uint32_t words[4], q[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int64_t r = row0 + l + 32 * i;
-      const int64_t from = r >= end ? -1 : a.gather ? __ldg(a.gather + r) : r;
-      const bool there = from >= 0 && from < a.in_rows;
-      x[i].load(reinterpret_cast<const T *>(a.x) + (there ? from : 0) * a.ldx + c, a.vec, there ? a.cols - c : 0);
-    }
-    uint32_t words[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t r = row0 + l + 32 * i;
       uint32_t amax = Eight<T>::top_bits(x[i].top(0));
       amax = max(amax, __shfl_xor_sync(~0u, amax, 1));
       amax = max(amax, __shfl_xor_sync(~0u, amax, 2));
@@ -114,10 +121,17 @@ __global__ void __launch_bounds__(256) tuna_quantize4_rows_kernel(Quant4Args a) 
       x[i].values(v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] *= by;
-      if (r < end && c < (a.cols + 31) / 32 * 32) *reinterpret_cast<uint32_t *>(a.q + r * a.ldq + c / 2) = fp4_eight(v);
+      q[i] = fp4_eight(v);
       words[i] = byte << (lane & 12) * 2;
       words[i] |= __shfl_xor_sync(~0u, words[i], 4);
       words[i] |= __shfl_xor_sync(~0u, words[i], 8);
+    }
+    if (n + 1 < a.strips) fetch(c + 256);
+    const int run = c >> 7;
+    if (c < (a.cols + 31) / 32 * 32) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (row0 + l + 32 * i < end) *reinterpret_cast<uint32_t *>(a.q + (row0 + l + 32 * i) * a.ldq + c / 2) = q[i];
     }
     if ((lane & 15) == 0 && run < a.runs)
       *reinterpret_cast<uint4 *>(a.scale + (slot * a.runs + run) * kScaleTile + l * 16) = make_uint4(words[0], words[1], words[2], words[3]);
@@ -147,7 +161,7 @@ __global__ void __launch_bounds__(256) tuna_quantize4_columns_kernel(Quant4Args 
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t r = r0 + mine + i * 16;
-    x[i].load(reinterpret_cast<const T *>(a.x) + r * a.ldx + c0 + c, a.vec, r < a.rows ? a.cols - c0 - c : 0);
+    x[i].load_any(reinterpret_cast<const T *>(a.x) + r * a.ldx + c0 + c, r < a.rows ? a.cols - c0 - c : 0);
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i)
@@ -169,6 +183,8 @@ __global__ void __launch_bounds__(256) tuna_quantize4_columns_kernel(Quant4Args 
     }
     top[0] = max(top[0], abs_bits(t[0][r])), top[1] = max(top[1], abs_bits(t[1][r]));
   }
+  __syncthreads();  // the tile has been read: the values go out by way of its place, in whole sectors
+  uint4 *out = reinterpret_cast<uint4 *>(tile_raw);  // [128 columns][4 quarters], their pieces turned by column
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const uint32_t byte = fp4_scale(top[e]);
@@ -177,11 +193,15 @@ __global__ void __launch_bounds__(256) tuna_quantize4_columns_kernel(Quant4Args 
     scales[(col & 31) * 16 + (col >> 5) * 4 + quarter] = (uint8_t)byte;
 #pragma unroll
     for (int r = 0; r < 32; ++r) t[e][r] *= by;
-    if (c0 + col < a.cols && r0 + quarter * 32 < a.rows)
-      *reinterpret_cast<uint4 *>(a.q + (int64_t)(c0 + col) * a.ldq + (r0 + quarter * 32) / 2) =
-          make_uint4(fp4_eight(t[e]), fp4_eight(t[e] + 8), fp4_eight(t[e] + 16), fp4_eight(t[e] + 24));
+    out[col * 4 + (quarter ^ (col >> 1 & 3))] = make_uint4(fp4_eight(t[e]), fp4_eight(t[e] + 8), fp4_eight(t[e] + 16), fp4_eight(t[e] + 24));
   }
   __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int col = i * 64 + (tid >> 2), piece = tid & 3;
+    if (c0 + col < a.cols && r0 + piece * 32 < a.rows)
+      *reinterpret_cast<uint4 *>(a.q + (int64_t)(c0 + col) * a.ldq + (r0 + piece * 32) / 2) = out[col * 4 + (piece ^ (col >> 1 & 3))];
+  }
   if (tid < 32) reinterpret_cast<uint4 *>(a.scale + ((int64_t)col_tile * a.runs + run) * kScaleTile)[tid] = reinterpret_cast<const uint4 *>(scales)[tid];
 }
 
@@ -190,14 +210,14 @@ template <typename T>
 __global__ void __launch_bounds__(256) tuna_dequantize4_kernel(Quant4Args a, T *out, int64_t ldo) {
   wait_previous();
   allow_next();
-  const int lane = threadIdx.x & 31, c = (int)blockIdx.y * 256 + lane * 8, run = (int)blockIdx.y * 2 + (lane >> 4);
-  const int64_t slot = blockIdx.x;
+  const int lane = threadIdx.x & 31, l = (blockIdx.x & 3) * 8 + (threadIdx.x >> 5);
+  const int64_t slot = blockIdx.x >> 2;
   int64_t row0, end;
   slot_rows(a.offsets, a.groups, a.rows, slot, row0, end);
-  if (c >= a.cols) return;
-  const bool whole = c + 8 <= a.cols;
-  for (int l = threadIdx.x >> 5; l < 32 && row0 + l < end; l += 8) {
-    const uint4 s = *reinterpret_cast<const uint4 *>(a.scale + (slot * a.runs + run) * kScaleTile + l * 16);
+  if (row0 + l >= end) return;
+  int c = (int)blockIdx.y * a.strips * 256 + lane * 8;
+  for (int n = 0; n < a.strips && c < a.cols; ++n, c += 256) {
+    const uint4 s = __ldg(reinterpret_cast<const uint4 *>(a.scale + (slot * a.runs + (c >> 7)) * kScaleTile + l * 16));
     const uint32_t words[4] = {s.x, s.y, s.z, s.w};
     uint32_t q[4];
 #pragma unroll
@@ -206,7 +226,7 @@ __global__ void __launch_bounds__(256) tuna_dequantize4_kernel(Quant4Args a, T *
       const uint8_t *p = a.q + r * a.ldq + c / 2;
       q[i] = 0;
       if (r >= end) continue;
-      if (whole && a.vec) {
+      if (c + 8 <= a.cols && ((uintptr_t)p & 3) == 0) {
         q[i] = __ldg(reinterpret_cast<const uint32_t *>(p));
       } else {
 #pragma unroll
@@ -223,14 +243,7 @@ __global__ void __launch_bounds__(256) tuna_dequantize4_kernel(Quant4Args a, T *
       fp4_values(q[i], v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] *= by;
-      T *o = out + r * ldo + c;
-      if (whole && a.vec) {
-        store_row(o, v);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c + j < a.cols) o[j] = from_f32<T>(v[j]);
-      }
+      store_any(out + r * ldo + c, v, a.cols - c);
     }
   }
 }
@@ -662,13 +675,20 @@ int launch_product4(const Product4Args &p, cudaStream_t st) {
   return p.out_f32 ? run_tiles4<128, false, float>(p, st) : run_tiles4<128, false, __nv_bfloat16>(p, st);
 }
 
+// The grid over quarters of row tiles and strips of 256 columns: several strips a block where there are many (and then no more
+// than 65535 of the others: 2^24 columns are 2^16 strips), so that what finds its rows is shared by them.
+static dim3 strips_grid(int64_t tiles, int cols, int &strips) {
+  const int64_t quarters = tiles * 4, all = ceil_div(cols, 256);
+  strips = (int)std::max<int64_t>(1, std::min<int64_t>(all, quarters * all / (16 * sm_count())));
+  return dim3((unsigned)quarters, (unsigned)ceil_div(all, strips));
+}
+
 int launch_quantize4_rows(const void *x, bool f32, int64_t rows, int cols, int64_t ldx, const int64_t *gather, int64_t in_rows, int groups,
                           const int64_t *offsets, void *q, int64_t ldq, uint8_t *scale, cudaStream_t st) {
   Quant4Args a = {};
   a.x = x, a.rows = rows, a.cols = cols, a.ldx = ldx, a.gather = gather, a.in_rows = in_rows, a.groups = groups, a.offsets = offsets;
   a.q = (uint8_t *)q, a.ldq = ldq, a.scale = scale, a.runs = (int)ceil_div(cols, 128);
-  a.vec = aligned(x, 16) && ldx * (f32 ? 4 : 2) % 16 == 0;
-  const dim3 grid((unsigned)fp4_slots(rows, offsets ? groups : 0), (unsigned)ceil_div(cols, 256));
+  const dim3 grid = strips_grid(fp4_slots(rows, offsets ? groups : 0), cols, a.strips);
   return f32 ? launch(tuna_quantize4_rows_kernel<float>, grid, 256, 0, st, false, a)
              : launch(tuna_quantize4_rows_kernel<__nv_bfloat16>, grid, 256, 0, st, false, a);
 }
@@ -706,7 +726,6 @@ int tuna_fp4_quantize(const void *x, int dtype, int64_t rows, int cols, int64_t 
   if (layout == TUNA_FP4_ROWS) return launch_quantize4_rows(x, f32, rows, cols, ldx, nullptr, rows, groups, offsets, q, ldq, (uint8_t *)scale, st);
   Quant4Args a = {};
   a.x = x, a.rows = rows, a.cols = cols, a.ldx = ldx, a.q = (uint8_t *)q, a.ldq = ldq, a.scale = (uint8_t *)scale, a.runs = (int)ceil_div(rows, 128);
-  a.vec = aligned(x, 16) && ldx * size % 16 == 0;
   const dim3 grid((unsigned)(ceil_div(rows, 128) * ceil_div(cols, 128)));
   static bool set[2][64] = {};
   if (f32) {
@@ -727,8 +746,7 @@ int tuna_fp4_dequantize(const void *q, int64_t ldq, const void *scale, int64_t r
   Quant4Args a = {};
   a.rows = rows, a.cols = cols, a.groups = groups, a.offsets = offsets, a.q = (uint8_t *)q, a.ldq = ldq, a.scale = (uint8_t *)scale;
   a.runs = (int)ceil_div(cols, 128);
-  a.vec = aligned(q, 4) && ldq % 4 == 0 && aligned(out, 16) && ldo * size % 16 == 0;
-  const dim3 grid((unsigned)fp4_slots(rows, groups), (unsigned)ceil_div(cols, 256));
+  const dim3 grid = strips_grid(fp4_slots(rows, groups), cols, a.strips);
   cudaStream_t st = (cudaStream_t)stream;
   return out_dtype == TUNA_DTYPE_F32 ? launch(tuna_dequantize4_kernel<float>, grid, 256, 0, st, false, a, (float *)out, ldo)
                                      : launch(tuna_dequantize4_kernel<__nv_bfloat16>, grid, 256, 0, st, false, a, (__nv_bfloat16 *)out, ldo);

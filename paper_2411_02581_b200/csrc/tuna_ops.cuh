@@ -271,6 +271,32 @@ struct Eight {
       for (int i = 0; i < kWords; ++i) w[i] = x.u[i];
     }
   }
+  // The same from any address: in the widest pieces that its alignment allows.  (A bf16 row that starts between two
+  // words is taken as a half, three words and a half.)
+  __device__ __forceinline__ void load_any(const T *p, int left) {
+    const uint32_t at = (uint32_t)(uintptr_t)p & 15;
+    if (left >= 8 && at == 0) {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+    } else if (left >= 8 && (at & 7) == 0) {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) {
+        const uint2 a = __ldg(reinterpret_cast<const uint2 *>(p) + 2 * i), b = __ldg(reinterpret_cast<const uint2 *>(p) + 2 * i + 1);
+        w[i] = make_uint4(a.x, a.y, b.x, b.y);
+      }
+    } else if (left >= 8 && (at & 3) == 0) {
+      const uint32_t *u = reinterpret_cast<const uint32_t *>(p);
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = make_uint4(__ldg(u + 4 * i), __ldg(u + 4 * i + 1), __ldg(u + 4 * i + 2), __ldg(u + 4 * i + 3));
+    } else if (left >= 8 && sizeof(T) == 2) {
+      const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
+      const uint32_t *u = reinterpret_cast<const uint32_t *>(h + 1);
+      const uint32_t a = __ldg(h), b = __ldg(u), c = __ldg(u + 1), d = __ldg(u + 2), e = __ldg(h + 7);
+      w[0] = make_uint4(a | b << 16, __funnelshift_l(b, c, 16), __funnelshift_l(c, d, 16), d >> 16 | e << 16);
+    } else {
+      load(p, false, left);
+    }
+  }
   // the largest magnitude's bits, kept as `T` has them (two 16-bit values in a word for bf16)
   __device__ __forceinline__ uint32_t top(uint32_t so_far) const {
     constexpr uint32_t mask = sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu;
@@ -297,6 +323,43 @@ struct Eight {
     }
   }
 };
+
+// Eight consecutive values to any address, `left` of them there are, in the widest pieces that it allows.
+__device__ __forceinline__ void store_any(float *p, const float (&v)[8], int left) {
+  const uint32_t at = (uint32_t)(uintptr_t)p & 15;
+  if (left >= 8 && at == 0) {
+    store_row(p, v);
+  } else if (left >= 8 && (at & 7) == 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) reinterpret_cast<float2 *>(p)[i] = make_float2(v[2 * i], v[2 * i + 1]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < left) p[i] = v[i];
+  }
+}
+__device__ __forceinline__ void store_any(__nv_bfloat16 *p, const float (&v)[8], int left) {
+  const uint32_t at = (uint32_t)(uintptr_t)p & 15;
+  const uint32_t w[4] = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+  uint16_t *h = reinterpret_cast<uint16_t *>(p);
+  if (left >= 8 && at == 0) {
+    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  } else if (left >= 8 && (at & 7) == 0) {
+    reinterpret_cast<uint2 *>(p)[0] = make_uint2(w[0], w[1]), reinterpret_cast<uint2 *>(p)[1] = make_uint2(w[2], w[3]);
+  } else if (left >= 8 && (at & 3) == 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t *>(p)[i] = w[i];
+  } else if (left >= 8) {
+    uint32_t *u = reinterpret_cast<uint32_t *>(h + 1);
+    h[0] = (uint16_t)w[0], h[7] = (uint16_t)(w[3] >> 16);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) u[i] = __funnelshift_r(w[i], w[i + 1], 16);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < left) h[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+  }
+}
 
 // True in one lane of a whole warp.  What a warp issues to the tensor cores is issued so: the
 // operands stay in uniform registers, where a branch on the lane would move each of them there.
