@@ -5,7 +5,6 @@
 //
 // The tensor cores apply the scales themselves, so a product accumulates in tensor memory from the first step to the last.
 #include <algorithm>
-#include <mutex>
 
 #include "tuna_fp4.h"
 #include "tuna_ops.cuh"
@@ -270,11 +269,13 @@ constexpr int kThreads4 = 128 + kOutWarps * 32;
 constexpr int kSumPitch4 = 132;  // floats: rows of sums that a cluster joins, on 16-byte boundaries and four banks apart
 constexpr int kMaxGroups4 = TUNA_MOE_MAX_EXPERTS;
 
-template <int BN, bool STORES>
+template <int BN, bool STORES, bool PAIR>
 struct Shape4 {
-  static constexpr int kStages = BN == 256 ? 3 : 5;
+  static constexpr int kStages = PAIR ? 5 : BN == 256 ? 3 : 5;
+  static constexpr int kRowsB = PAIR ? BN / 2 : BN;            // of b in this block's shared memory
+  static constexpr int kOperandBytes = (128 + kRowsB) * 128;
   static constexpr int kScaleBytes = 1024 + BN / 128 * 1024;
-  static constexpr int kStageBytes = (128 + BN) * 128 + kScaleBytes;
+  static constexpr int kStageBytes = kOperandBytes + kScaleBytes;
   static constexpr int kAccs = BN == 256 ? 1 : 2;              // accumulators
   static constexpr int kScaleCols = 8 + BN / 128 * 8;          // tensor-memory columns of a stage's scales
   static constexpr int kCols = BN / 2;                         // accumulator columns of a warp of the results
@@ -284,20 +285,78 @@ struct Shape4 {
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kOutBytes + (kMaxGroups4 + 8) * 4 + 256;
 };
 
-__device__ __forceinline__ void tma_load_scales(uint32_t dst, const CUtensorMap *map, int run, int tile, uint32_t bar) { tma_load_3d(dst, map, 0, run, tile, bar); }
-// 512 bytes of scales to 4 columns of tensor memory, once for each quarter of the lanes
+// 512 bytes of scales to 4 columns of tensor memory, once for each quarter of the lanes; of a pair, in both of its blocks
+template <bool PAIR>
 __device__ __forceinline__ void tc_copy_scales(uint32_t to, uint32_t smem) {
   // rows of 16 bytes, 8 of them 128 bytes apart, no swizzle
   const uint64_t desc = (uint64_t)((smem & 0x3ffff) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(desc) : "memory");
+  if (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(desc) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(desc) : "memory");
 }
-// d[tmem] (+)= A (128 x 64) * B^T (N x 64), 4-bit values with a scale for each 32 of them
+// d[tmem] (+)= A (128 x 64, of a pair 256 x 64) * B^T (N x 64), 4-bit values with a scale for each 32 of them
+template <bool PAIR>
 __device__ __forceinline__ void tc_mma_fp4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, bool accumulate) {
-  asm volatile(
-      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%5], [%6], p;\n}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate), "r"(sa), "r"(sb)
-      : "memory");
+  if (PAIR)
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%5], [%6], p;\n}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate), "r"(sa), "r"(sb)
+        : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%5], [%6], p;\n}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate), "r"(sa), "r"(sb)
+        : "memory");
+}
+// Arrives, when all steps so far are done, at a barrier of this block, or at the same one in both blocks of a pair.
+template <bool PAIR>
+__device__ __forceinline__ void tc_commit_to(uint32_t bar) {
+  if (PAIR)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+  else
+    tc_commit(bar);
+}
+// Tensor copies into this block's shared memory; of a pair, the bytes are counted by the first block's barrier, which `bar` is in.
+template <bool PAIR>
+__device__ __forceinline__ void load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+  if (PAIR)
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+  else
+    tma_load_2d(dst, map, x, y, bar);
+}
+template <bool PAIR>
+__device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
+  if (PAIR)
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+  else
+    tma_load_3d(dst, map, x, y, z, bar);
+}
+__device__ __forceinline__ uint32_t in_first_block(uint32_t addr) {  // the same place in the shared memory of the cluster's first block
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+  return r;
+}
+// (No memory is handed over with it, only room in tensor memory: a release to the cluster would wait for all that the thread
+// has stored, 1600 cycles a tile.)
+__device__ __forceinline__ void mbar_arrive_far(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
+template <bool PAIR>
+__device__ __forceinline__ void tmem_take(uint32_t smem_dst) {
+  if (PAIR) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_dst) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  } else {
+    tmem_alloc(smem_dst, 512);
+  }
+}
+template <bool PAIR>
+__device__ __forceinline__ void tmem_give(uint32_t addr) {
+  if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(addr) : "memory");
+  else tmem_free(addr, 512);
 }
 // Instruction descriptor: e2m1 operands, e8m0 scales, n columns, m rows; `half`: which two of a word's four scales
 __host__ __device__ constexpr uint32_t fp4_idesc(int m, int n, int half) {
@@ -311,24 +370,33 @@ struct Walk4 {
   int slot;      // tile of the rows' scales
   int n0;
 };
+template <int ROWS>
 __device__ __forceinline__ void walk_to(Walk4 &w, int t, const Tile4Args &a, const int *tile_base, int bn) {
   while (t >= tile_base[w.g + 1] * a.n_tiles) ++w.g;
   const uint32_t mt = tile_base[w.g + 1] - tile_base[w.g], local = t - tile_base[w.g] * a.n_tiles;
   const uint32_t n = local / mt, m = local - n * mt;  // rows fastest: blocks that run together share b
   int64_t begin = 0, end = a.p.m;
   if (a.p.offsets) begin = max(a.p.offsets[w.g], (int64_t)0), end = min(a.p.offsets[w.g + 1], a.p.m);
-  w.row = (int)begin + (int)m * 128, w.end = (int)end;
-  w.slot = (int)begin / 128 + w.g + (int)m;
+  w.row = (int)begin + (int)m * ROWS, w.end = (int)end;
+  w.slot = (int)begin / 128 + w.g + (int)m * (ROWS / 128);
+  if (ROWS == 256 && cluster_rank()) w.row += 128, ++w.slot;  // this block's half
   w.n0 = n * bn;
 }
 
+// With PAIR a cluster of two blocks takes a tile of 256 rows: each has 128 of them and half of b's rows in its shared memory, all
+// scales of b, and the results of its own rows in its tensor memory.  The first block's elected lane issues the steps for
+// both; the copies of both are counted by its barriers.  A multiprocessor then takes 68 bytes a cycle of its tensor cores' rate in
+// copies where a block alone takes 102 (BN = 256), and b's half is read by both.
+//
 // With SPLIT a cluster of 2 or 4 blocks shares one tile: each adds up a part of k, leaves its sums in its shared memory,
 // and adds up the parts of some of the rows from all of them, in order of k.
-template <int BN, bool SWIGLU, bool SPLIT, typename TO>
+template <int BN, bool SWIGLU, bool SPLIT, bool PAIR, typename TO>
 __global__ void __launch_bounds__(kThreads4, 1)
     tuna_product4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_sa,
                          const __grid_constant__ CUtensorMap map_sb, const __grid_constant__ CUtensorMap map_out, const Tile4Args a) {
-  using S = Shape4<BN, !SWIGLU && !SPLIT && sizeof(TO) == 2>;
+  using S = Shape4<BN, !SWIGLU && !SPLIT && sizeof(TO) == 2, PAIR>;
+  static_assert(!PAIR || (BN == 256 && !SPLIT));
+  constexpr int kRows = PAIR ? 256 : 128;
   extern __shared__ char smem_raw[];
   char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   int *tile_base = (int *)(smem + (size_t)S::kStages * S::kStageBytes + S::kOutBytes);
@@ -338,15 +406,18 @@ __global__ void __launch_bounds__(kThreads4, 1)
   const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages, freed = done + 8 * S::kAccs, drained = freed + 8 * S::kAccs;
   const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
+  if (threadIdx.x == 32) {
+    for (const CUtensorMap *map : {&map_a, &map_b, &map_sa, &map_sb}) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+  }
   if (threadIdx.x == 0) {
     for (int s = 0; s < S::kStages; ++s) mbar_init(full + 8 * s, 1), mbar_init(empty + 8 * s, 1);
-    for (int s = 0; s < S::kAccs; ++s) mbar_init(done + 8 * s, 1), mbar_init(freed + 8 * s, kOutWarps);
+    for (int s = 0; s < S::kAccs; ++s) mbar_init(done + 8 * s, 1), mbar_init(freed + 8 * s, PAIR ? 2 * kOutWarps : kOutWarps);
     mbar_init(drained, 1);
     *given_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (warp == 2) tmem_alloc(smem_u32(tmem_at), 512);
+  if (warp == 2) tmem_take<PAIR>(smem_u32(tmem_at));
   wait_previous();
   allow_next();
   // Tiles of rows before each group, cut at most_rows, which groups that lie apart never come near.
@@ -357,7 +428,7 @@ __global__ void __launch_bounds__(kThreads4, 1)
       int64_t rows = 0;
       auto cut = [&](int64_t row) { return min(max(row, (int64_t)0), a.p.m); };
       if (g < a.p.groups) rows = a.p.offsets ? cut(a.p.offsets[g + 1]) - cut(a.p.offsets[g]) : a.p.m;
-      const uint32_t mt = rows > 0 ? (uint32_t)((rows + 127) / 128) : 0;  // (2^24 at most: 32 of them and most_rows fit 32 bits)
+      const uint32_t mt = rows > 0 ? (uint32_t)((rows + kRows - 1) / kRows) : 0;  // (2^24 at most: 32 of them and most_rows fit 32 bits)
       uint32_t x = mt;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
@@ -371,11 +442,13 @@ __global__ void __launch_bounds__(kThreads4, 1)
   }
   tc_fence_before();
   __syncthreads();
+  if constexpr (PAIR) cluster_meet();  // the barriers of both blocks are there
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(~0u, *tmem_at, 0);
   const int tiles = tile_base[a.p.groups] * a.n_tiles;
   const int parts = SPLIT ? (int)cluster_size() : 1, part = SPLIT ? (int)cluster_rank() : 0;
-  const int first = (int)(SPLIT ? blockIdx.x / parts : blockIdx.x), step = (int)(SPLIT ? gridDim.x / parts : gridDim.x);
+  const int sharers = PAIR ? 2 : parts, first = (int)blockIdx.x / sharers, step = (int)gridDim.x / sharers;
+  const int half_b = PAIR ? (int)cluster_rank() : 0;  // of b, and of the pair
   // this block's part of k
   const int s_first = SPLIT ? (int)((int64_t)a.stages * part / parts) : 0, stages = SPLIT ? (int)((int64_t)a.stages * (part + 1) / parts) - s_first : a.stages;
   constexpr int kTileN = SWIGLU ? BN / 2 : BN;
@@ -389,34 +462,39 @@ __global__ void __launch_bounds__(kThreads4, 1)
       Walk4 w;
       bool ok = true;
       for (int t = first; ok && t < tiles; t += step) {
-        walk_to(w, t, a, tile_base, kTileN);
+        walk_to<kRows>(w, t, a, tile_base, kTileN);
         for (int s = 0; s < stages; ++s) {
           if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, given_up))) break;
-          const uint32_t at = smem_u32(smem) + stage * S::kStageBytes, bar = full + 8 * stage, scales = at + (128 + BN) * 128;
-          mbar_expect(bar, S::kStageBytes);
+          const uint32_t at = smem_u32(smem) + stage * S::kStageBytes, scales = at + S::kOperandBytes;
+          const uint32_t bar = PAIR ? in_first_block(full + 8 * stage) : full + 8 * stage;
+          if (half_b == 0) mbar_expect(full + 8 * stage, (PAIR ? 2 : 1) * S::kStageBytes);
           const int col = (s_first + s) * 128, run = (s_first + s) * 2;
-          tma_load_2d(at, &map_a, col, w.row, bar);
-          tma_load_scales(scales, &map_sa, run, w.slot, bar);
+          load_2d<PAIR>(at, &map_a, col, w.row, bar);
+          load_3d<PAIR>(scales, &map_sa, 0, run, w.slot, bar);
           if (SWIGLU) {
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-              tma_load_3d(at + 128 * 128 + q * 128 * 128, &map_b, col, w.n0, w.g * 2 + q, bar);
-              tma_load_scales(scales + 1024 + q * 1024, &map_sb, run, (w.g * 2 + q) * tiles_n + w.n0 / 128, bar);
+              if (!PAIR || q == half_b) load_3d<PAIR>(at + 128 * 128 + (PAIR ? 0 : q * 128 * 128), &map_b, col, w.n0, w.g * 2 + q, bar);
+              load_3d<PAIR>(scales + 1024 + q * 1024, &map_sb, 0, run, (w.g * 2 + q) * tiles_n + w.n0 / 128, bar);
             }
           } else {
-            tma_load_3d(at + 128 * 128, &map_b, col, w.n0, w.g, bar);
-            tma_load_scales(scales + 1024, &map_sb, run, w.g * tiles_n + w.n0 / 128, bar);
+            load_3d<PAIR>(at + 128 * 128, &map_b, col, w.n0 + half_b * 128, w.g, bar);
+            load_3d<PAIR>(scales + 1024, &map_sb, 0, run, w.g * tiles_n + w.n0 / 128, bar);
           }
           ++issued;
           if (++stage == S::kStages) stage = 0, phase ^= 1;
         }
       }
       // nothing may land in shared memory after the block has gone, whichever warp gives up: the last copies are waited for
+      // (of a pair by its first block, which has the barriers; the other one stays until it comes to the meeting)
       int never = 0;
-      for (int64_t i = max((int64_t)0, issued - S::kStages); i < issued; ++i)
+      for (int64_t i = half_b ? issued : max((int64_t)0, issued - S::kStages); i < issued; ++i)
         mbar_wait(full + 8 * (int)(i % S::kStages), (uint32_t)((i / S::kStages) & 1), &never);
+      if (PAIR)  // nor may the first block's steps still report to a block that has gone
+        for (int64_t i = max((int64_t)0, issued - S::kStages); i < issued; ++i)
+          mbar_wait(empty + 8 * (int)(i % S::kStages), (uint32_t)((i / S::kStages) & 1), given_up);
     }
-  } else if (warp == 1) {
+  } else if (warp == 1 && half_b == 0) {
     // ---- tensor cores: the whole warp goes along, one lane issues
     int stage = 0, phase = 0, acc = 0, acc_phase = 0;
     bool ok = true;
@@ -425,21 +503,21 @@ __global__ void __launch_bounds__(kThreads4, 1)
       for (int s = 0; ok && s < stages; ++s) {
         if (!(ok = __all_sync(~0u, mbar_wait(full + 8 * stage, phase, given_up)))) break;
         tc_fence_after();
-        const uint32_t at = smem_u32(smem) + stage * S::kStageBytes, scales = at + (128 + BN) * 128;
+        const uint32_t at = smem_u32(smem) + stage * S::kStageBytes, scales = at + S::kOperandBytes;
         const uint64_t da = tc_desc(at), db = tc_desc(at + 128 * 128);
         const uint32_t ta = tmem + S::kAccs * BN + stage * S::kScaleCols, tb = ta + 8;
         if (elect_one()) {
 #pragma unroll
           for (int r = 0; r < 2; ++r) {  // runs of 128 along k
-            tc_copy_scales(ta + r * 4, scales + r * 512);
+            tc_copy_scales<PAIR>(ta + r * 4, scales + r * 512);
 #pragma unroll
-            for (int q = 0; q < BN / 128; ++q) tc_copy_scales(tb + r * (BN / 32) + q * 4, scales + 1024 + q * 1024 + r * 512);
+            for (int q = 0; q < BN / 128; ++q) tc_copy_scales<PAIR>(tb + r * (BN / 32) + q * 4, scales + 1024 + q * 1024 + r * 512);
           }
 #pragma unroll
           for (int i = 0; i < 4; ++i)  // 32 bytes along k
-            tc_mma_fp4(tmem + acc * BN, da + 2 * i, db + 2 * i, fp4_idesc(128, BN, i & 1), ta + (i >> 1) * 4, tb + (i >> 1) * (BN / 32), s > 0 || i > 0);
-          tc_commit(empty + 8 * stage);
-          if (s == stages - 1) tc_commit(done + 8 * acc);
+            tc_mma_fp4<PAIR>(tmem + acc * BN, da + 2 * i, db + 2 * i, fp4_idesc(kRows, BN, i & 1), ta + (i >> 1) * 4, tb + (i >> 1) * (BN / 32), s > 0 || i > 0);
+          tc_commit_to<PAIR>(empty + 8 * stage);
+          if (s == stages - 1) tc_commit_to<PAIR>(done + 8 * acc);
         }
         __syncwarp();
         if (++stage == S::kStages) stage = 0, phase ^= 1;
@@ -448,7 +526,10 @@ __global__ void __launch_bounds__(kThreads4, 1)
     }
     // and no step may be under way when tensor memory is freed
     int never = 0;
-    if (elect_one()) tc_commit(drained);
+    if (elect_one()) {
+      if (PAIR) asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(drained) : "memory");
+      else tc_commit(drained);
+    }
     __syncwarp();
     mbar_wait(drained, 0, &never);
   } else if (warp >= 4) {
@@ -458,14 +539,17 @@ __global__ void __launch_bounds__(kThreads4, 1)
     int acc = 0, acc_phase = 0;
     Walk4 w;
     for (int t = first; t < tiles; t += step) {
-      walk_to(w, t, a, tile_base, kTileN);
+      walk_to<kRows>(w, t, a, tile_base, kTileN);
       if (!__all_sync(~0u, mbar_wait(done + 8 * acc, acc_phase, given_up))) break;  // (and the warp is whole for the loads)
       tc_fence_after();
       const uint32_t at = from + acc * BN;
       auto release = [&] {  // everything is in registers: the accumulator may be filled again
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(freed + 8 * acc);
+        if (lane == 0) {
+          if (PAIR) mbar_arrive_far(in_first_block(freed + 8 * acc));
+          else mbar_arrive(freed + 8 * acc);
+        }
       };
       const int row = w.row + row_in;
       const bool there = row < w.end;
@@ -602,7 +686,7 @@ __global__ void __launch_bounds__(kThreads4, 1)
     cluster_meet();
     if (first < tiles && !*given_up) {
       Walk4 w;
-      walk_to(w, first, a, tile_base, BN);
+      walk_to<kRows>(w, first, a, tile_base, BN);
       const int rows = min(128, w.end - w.row);
       for (int i = threadIdx.x; i < (rows - part + parts - 1) / parts * (BN / 4); i += kThreads4) {
         const int r = part + i / (BN / 4) * parts, c = i % (BN / 4) * 4;
@@ -621,16 +705,20 @@ __global__ void __launch_bounds__(kThreads4, 1)
   }
   tc_fence_before();
   __syncthreads();
+  if constexpr (PAIR) cluster_meet();  // neither block's memory is used by the other one any more
   tc_fence_after();
-  if (warp == 2) tmem_free(tmem, 512);
+  if (warp == 2) tmem_give<PAIR>(tmem);
   if (threadIdx.x == 0 && *given_up) *a.error = 1;
 }
 
 // ---- host ------------------------------------------------------------------------------------
 
-template <int BN, bool SWIGLU, typename TO, bool SPLIT = false>
+enum { kAlone, kSplit, kPair };
+template <int BN, bool SWIGLU, typename TO, int HOW = kAlone>
 int run_tiles4(const Product4Args &p, cudaStream_t st, int parts = 1) {
-  using S = Shape4<BN, !SWIGLU && !SPLIT && sizeof(TO) == 2>;
+  constexpr bool SPLIT = HOW == kSplit, PAIR = HOW == kPair;
+  constexpr int kRows = PAIR ? 256 : 128;
+  using S = Shape4<BN, !SWIGLU && !SPLIT && sizeof(TO) == 2, PAIR>;
   Tile4Args a = {};
   a.p = p;
   const int64_t bytes = ceil_div(p.k, 2), runs = ceil_div(p.k, 128), tiles_n = ceil_div(p.n, 128), matrices = (int64_t)p.groups * (SWIGLU ? 2 : 1);
@@ -641,7 +729,7 @@ int run_tiles4(const Product4Args &p, cudaStream_t st, int parts = 1) {
   if (!a.error) return TUNA_ERR_CUDA;
   CUtensorMap ma, mb, msa, msb, mo;
   if (const int rc = make_map(&ma, 2, p.a, bytes, p.m, 1, p.lda, 128)) return rc;
-  if (const int rc = make_map(&mb, 3, p.b, bytes, p.n, matrices, p.ldb, SWIGLU ? 128 : BN)) return rc;
+  if (const int rc = make_map(&mb, 3, p.b, bytes, p.n, matrices, p.ldb, SWIGLU ? 128 : S::kRowsB)) return rc;
   if (const int rc = make_scale_map(&msa, p.sa, runs, fp4_slots(p.m, p.offsets ? p.groups : 0), 1)) return rc;
   if (const int rc = make_scale_map(&msb, p.sb, runs, matrices * tiles_n, SWIGLU ? 1 : BN / 128)) return rc;
   mo = ma;
@@ -649,9 +737,11 @@ int run_tiles4(const Product4Args &p, cudaStream_t st, int parts = 1) {
   if (a.store_tiles)
     if (const int rc = make_out_map(&mo, p.out, p.n, p.m, p.ldo, 128)) return rc;
   static bool set[64] = {};
-  auto kernel = tuna_product4_kernel<BN, SWIGLU, SPLIT, TO>;
+  auto kernel = tuna_product4_kernel<BN, SWIGLU, SPLIT, PAIR, TO>;
   if (const int rc = allow_smem(kernel, S::kSmem, set)) return rc;
-  const int64_t most = (ceil_div(p.m, 128) + (p.offsets ? p.groups : 0)) * a.n_tiles;
+  const int64_t most = (ceil_div(p.m, kRows) + (p.offsets ? p.groups : 0)) * a.n_tiles;
+  if (PAIR)
+    return launch_cluster(kernel, dim3((unsigned)std::min<int64_t>(most, std::max(sm_count() / 2, 1)) * 2), 2, kThreads4, S::kSmem, st, false, ma, mb, msa, msb, mo, a);
   if (SPLIT) return launch_cluster(kernel, dim3((unsigned)(most * parts)), parts, kThreads4, S::kSmem, st, false, ma, mb, msa, msb, mo, a);
   return launch(kernel, dim3((unsigned)std::min<int64_t>(most, sm_count())), kThreads4, S::kSmem, st, false, ma, mb, msa, msb, mo, a);
 }
@@ -661,6 +751,15 @@ size_t dtype_size(int dtype) { return dtype == TUNA_DTYPE_F32 ? 4 : dtype == TUN
 }  // namespace
 
 int launch_product4(const Product4Args &p, cudaStream_t st) {
+  // Pairs of blocks where they have two rounds of tiles or more, and groups whole tiles of rows on average.  (Pairs and blocks alone,
+  // us: 8192 x 4096 x 4096 52.9 and 62.5, 8192^3 180 and 210, 3000^3 19.5 and 20.8; with less than two rounds 2048 x 4096 x 4096 18.4 and 18.2,
+  // 1024 x 4096 x 4096 11.8 and 11.2.  64 groups of 4096 x 2048, rows of a group 128: 70 and 68, 256: 99 and 100, 512: 155 and 165, 1024:
+  // 268 and 294.)
+  const int64_t pairs = std::max(sm_count() / 2, 1), tiles = ceil_div(p.m, 256) * ceil_div(p.n, p.swiglu ? 128 : 256);
+  if (tiles >= 2 * pairs && (!p.offsets || p.m >= 256 * (int64_t)p.groups)) {
+    if (p.swiglu) return run_tiles4<256, true, uint8_t, kPair>(p, st);
+    return p.out_f32 ? run_tiles4<256, false, float, kPair>(p, st) : run_tiles4<256, false, __nv_bfloat16, kPair>(p, st);
+  }
   if (p.swiglu) return run_tiles4<256, true, uint8_t>(p, st);
   const int64_t rows = ceil_div(p.m, 128) + (p.offsets ? p.groups - 1 : 0);
   const int64_t wide = rows * ceil_div(p.n, 256), narrow = rows * ceil_div(p.n, 128);
@@ -670,7 +769,7 @@ int launch_product4(const Product4Args &p, cudaStream_t st) {
     const int64_t stages = ceil_div(p.k, 256);
     int parts = 4;
     while (parts > 1 && (narrow * parts > 128 || stages - stages / parts < 6)) parts /= 2;
-    if (parts > 1) return p.out_f32 ? run_tiles4<128, false, float, true>(p, st, parts) : run_tiles4<128, false, __nv_bfloat16, true>(p, st, parts);
+    if (parts > 1) return p.out_f32 ? run_tiles4<128, false, float, kSplit>(p, st, parts) : run_tiles4<128, false, __nv_bfloat16, kSplit>(p, st, parts);
   }
   return p.out_f32 ? run_tiles4<128, false, float>(p, st) : run_tiles4<128, false, __nv_bfloat16>(p, st);
 }

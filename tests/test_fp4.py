@@ -211,8 +211,8 @@ def grouped(sizes, n, k, first=0, spare=9):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("n,k", [(256, 512), (300, 144), (2048, 1024)])
-@pytest.mark.parametrize("sizes", GROUPS[:6] + [[700, 0, 513, 40]])
+@pytest.mark.parametrize("n,k", [(256, 512), (300, 144), (2048, 1024), (2400, 130)])
+@pytest.mark.parametrize("sizes", GROUPS[:6] + [[700, 0, 513, 40], [1500, 0, 2561, 700, 1]])
 def test_grouped_product(n, k, sizes):
     from paper_2411_02581_b200 import moe
     a, offsets, bounds, qb, sb = grouped(sizes, n, k, first=3)
