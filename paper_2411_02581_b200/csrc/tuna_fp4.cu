@@ -137,6 +137,46 @@ __global__ void __launch_bounds__(256) tuna_quantize4_rows_kernel(Quant4Args a) 
   }
 }
 
+// The same for a few rows an expert, whose tiles would be nearly empty: a block takes 2048 columns of one row, a warp 256 of them.
+template <typename T>
+__global__ void __launch_bounds__(256) tuna_quantize4_few_kernel(Quant4Args a) {
+  wait_previous();
+  allow_next();
+  const int lane = threadIdx.x & 31, c = ((int)blockIdx.y * 8 + (threadIdx.x >> 5)) * 256 + lane * 8;
+  const int64_t r = blockIdx.x;
+  // on their way together: where the row comes from, and every 32nd group's first row (there are 1024 groups at most)
+  const int64_t from = a.gather ? __ldg(a.gather + r) : r;
+  auto cut = [&](int g) { return min(max(a.offsets[g], (int64_t)0), a.rows); };
+  const uint32_t coarse = __ballot_sync(~0u, lane * 32 < a.groups && cut(min(lane * 32, a.groups - 1)) <= r);
+  if (!(coarse & 1)) return;
+  int g = (31 - __clz(coarse)) * 32 + lane;
+  const int64_t first = cut(min(g, a.groups));
+  const uint32_t fine = __ballot_sync(~0u, g < a.groups && first <= r);
+  if (!(fine & 1)) return;
+  g += 31 - __clz(fine) - lane;  // the last group that begins at r or before it
+  const int64_t begin = __shfl_sync(~0u, first, 31 - __clz(fine));
+  if (r >= cut(g + 1)) return;
+  const bool there = from >= 0 && from < a.in_rows;
+  Eight<T> x;
+  x.load_any(reinterpret_cast<const T *>(a.x) + (there ? from : 0) * a.ldx + c, there ? a.cols - c : 0);
+  uint32_t amax = Eight<T>::top_bits(x.top(0));
+  amax = max(amax, __shfl_xor_sync(~0u, amax, 1));
+  amax = max(amax, __shfl_xor_sync(~0u, amax, 2));
+  const uint32_t byte = fp4_scale(amax);
+  const float by = fp4_inverse(byte);
+  float v[8];
+  x.values(v);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] *= by;
+  if (c < (a.cols + 31) / 32 * 32) *reinterpret_cast<uint32_t *>(a.q + r * a.ldq + c / 2) = fp4_eight(v);
+  uint32_t word = byte << (lane & 12) * 2;
+  word |= __shfl_xor_sync(~0u, word, 4);
+  word |= __shfl_xor_sync(~0u, word, 8);
+  const int64_t slot = begin / 128 + g + (r - begin) / 128;
+  const int at = (int)((r - begin) % 128), run = c >> 7;
+  if ((lane & 15) == 0 && run < a.runs) *reinterpret_cast<uint32_t *>(a.scale + (slot * a.runs + run) * kScaleTile + (at & 31) * 16 + (at >> 5) * 4) = word;
+}
+
 // Blocks along the columns, for the turned matrix: a block of threads takes a 128 x 128 tile through shared memory in its
 // own type; a thread then has 32 rows, one scale block, of two columns, read as pairs.  The tile's scales are one tile of them.
 template <typename T>
@@ -266,12 +306,17 @@ struct Tile4Args {
 
 constexpr int kOutWarps = 8;
 constexpr int kThreads4 = 128 + kOutWarps * 32;
-constexpr int kSumPitch4 = 132;  // floats: rows of sums that a cluster joins, on 16-byte boundaries and four banks apart
 constexpr int kMaxGroups4 = TUNA_MOE_MAX_EXPERTS;
+
+// What the groups' bounds come to: first rows (and the end behind the last one), cut to the operand, and tiles of rows before each.
+struct Groups4 {
+  int row[kMaxGroups4 + 1], tile[kMaxGroups4 + 1];
+};
 
 template <int BN, bool STORES, bool PAIR>
 struct Shape4 {
-  static constexpr int kStages = PAIR ? 5 : BN == 256 ? 3 : 5;
+  // what is in flight hides the memory's latency, so the stages take the room that the results on their way out leave
+  static constexpr int kStages = PAIR ? (STORES ? 5 : 6) : BN == 256 ? 4 : (STORES ? 5 : 6);
   static constexpr int kRowsB = PAIR ? BN / 2 : BN;            // of b in this block's shared memory
   static constexpr int kOperandBytes = (128 + kRowsB) * 128;
   static constexpr int kScaleBytes = 1024 + BN / 128 * 1024;
@@ -279,10 +324,13 @@ struct Shape4 {
   static constexpr int kAccs = BN == 256 ? 1 : 2;              // accumulators
   static constexpr int kScaleCols = 8 + BN / 128 * 8;          // tensor-memory columns of a stage's scales
   static constexpr int kCols = BN / 2;                         // accumulator columns of a warp of the results
-  static constexpr int kOutBytes = STORES ? kOutWarps * 4096 : 0;  // 32 rows of 64 bf16 results a warp, on their way out
+  static constexpr int kSumPitch = BN + 4;  // floats: rows of sums that a cluster joins, on 16-byte boundaries and four banks apart
+  static_assert(128 * kSumPitch * 4 <= kStages * kStageBytes);
+  static constexpr int kOutCols = BN == 256 && !PAIR ? 32 : 64;    // bf16 results that a warp sends out at a time, of 32 rows
+  static constexpr int kOutBytes = STORES ? kOutWarps * 32 * kOutCols * 2 : 0;
   static_assert(kAccs * BN + kStages * kScaleCols <= 512);
   static_assert(kStageBytes % 1024 == 0);
-  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kOutBytes + (kMaxGroups4 + 8) * 4 + 256;
+  static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kOutBytes + sizeof(Groups4) + 256;
 };
 
 // 512 bytes of scales to 4 columns of tensor memory, once for each quarter of the lanes; of a pair, in both of its blocks
@@ -292,6 +340,11 @@ __device__ __forceinline__ void tc_copy_scales(uint32_t to, uint32_t smem) {
   const uint64_t desc = (uint64_t)((smem & 0x3ffff) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
   if (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(desc) : "memory");
   else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(desc) : "memory");
+}
+__device__ __forceinline__ float load_one(uint32_t addr, uint32_t rank) {  // from a block of the cluster
+  float v;
+  asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %1, %2;\n ld.shared::cluster.f32 %0, [a];\n}" : "=f"(v) : "r"(addr), "r"(rank) : "memory");
+  return v;
 }
 // d[tmem] (+)= A (128 x 64, of a pair 256 x 64) * B^T (N x 64), 4-bit values with a scale for each 32 of them
 template <bool PAIR>
@@ -371,14 +424,20 @@ struct Walk4 {
   int n0;
 };
 template <int ROWS>
-__device__ __forceinline__ void walk_to(Walk4 &w, int t, const Tile4Args &a, const int *tile_base, int bn) {
-  while (t >= tile_base[w.g + 1] * a.n_tiles) ++w.g;
-  const uint32_t mt = tile_base[w.g + 1] - tile_base[w.g], local = t - tile_base[w.g] * a.n_tiles;
+__device__ __forceinline__ void walk_to(Walk4 &w, int t, const Tile4Args &a, const Groups4 &at, int bn) {
+  if (t >= at.tile[w.g + 1] * a.n_tiles) {  // the last group that begins at t or before it
+    int high = a.p.groups;
+    while (high - w.g > 1) {
+      const int g = (w.g + high) >> 1;
+      if (at.tile[g] * a.n_tiles <= t) w.g = g;
+      else high = g;
+    }
+  }
+  const uint32_t mt = at.tile[w.g + 1] - at.tile[w.g], local = t - at.tile[w.g] * a.n_tiles;
   const uint32_t n = local / mt, m = local - n * mt;  // rows fastest: blocks that run together share b
-  int64_t begin = 0, end = a.p.m;
-  if (a.p.offsets) begin = max(a.p.offsets[w.g], (int64_t)0), end = min(a.p.offsets[w.g + 1], a.p.m);
-  w.row = (int)begin + (int)m * ROWS, w.end = (int)end;
-  w.slot = (int)begin / 128 + w.g + (int)m * (ROWS / 128);
+  const int begin = at.row[w.g];
+  w.row = begin + (int)m * ROWS, w.end = at.row[w.g + 1];
+  w.slot = begin / 128 + w.g + (int)m * (ROWS / 128);
   if (ROWS == 256 && cluster_rank()) w.row += 128, ++w.slot;  // this block's half
   w.n0 = n * bn;
 }
@@ -399,8 +458,8 @@ __global__ void __launch_bounds__(kThreads4, 1)
   constexpr int kRows = PAIR ? 256 : 128;
   extern __shared__ char smem_raw[];
   char *smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-  int *tile_base = (int *)(smem + (size_t)S::kStages * S::kStageBytes + S::kOutBytes);
-  uint64_t *bars = (uint64_t *)(tile_base + kMaxGroups4 + 8);
+  Groups4 &groups = *(Groups4 *)(smem + (size_t)S::kStages * S::kStageBytes + S::kOutBytes);
+  uint64_t *bars = (uint64_t *)(&groups + 1);
   volatile int *given_up = (volatile int *)(bars + 2 * S::kStages + 2 * S::kAccs + 1);
   uint32_t *tmem_at = (uint32_t *)(given_up + 1);
   const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages, freed = done + 8 * S::kAccs, drained = freed + 8 * S::kAccs;
@@ -420,14 +479,13 @@ __global__ void __launch_bounds__(kThreads4, 1)
   if (warp == 2) tmem_take<PAIR>(smem_u32(tmem_at));
   wait_previous();
   allow_next();
-  // Tiles of rows before each group, cut at most_rows, which groups that lie apart never come near.
+  // All bounds are fetched at once; a warp then sums up the tiles, cut at most_rows, which groups that lie apart never come near.
+  for (int g = threadIdx.x; g <= a.p.groups; g += kThreads4) groups.row[g] = (int)(a.p.offsets ? min(max(a.p.offsets[g], (int64_t)0), a.p.m) : g ? a.p.m : 0);
+  __syncthreads();
   if (warp == 1) {
     uint32_t sum = 0;
     for (int g0 = 0; g0 < a.p.groups; g0 += 32) {
-      const int g = g0 + lane;
-      int64_t rows = 0;
-      auto cut = [&](int64_t row) { return min(max(row, (int64_t)0), a.p.m); };
-      if (g < a.p.groups) rows = a.p.offsets ? cut(a.p.offsets[g + 1]) - cut(a.p.offsets[g]) : a.p.m;
+      const int g = g0 + lane, rows = g < a.p.groups ? groups.row[g + 1] - groups.row[g] : 0;
       const uint32_t mt = rows > 0 ? (uint32_t)((rows + kRows - 1) / kRows) : 0;  // (2^24 at most: 32 of them and most_rows fit 32 bits)
       uint32_t x = mt;
 #pragma unroll
@@ -435,17 +493,17 @@ __global__ void __launch_bounds__(kThreads4, 1)
         const uint32_t y = __shfl_up_sync(~0u, x, d);
         if (lane >= d) x += y;
       }
-      if (g < a.p.groups) tile_base[g] = (int)min(sum + x - mt, a.most_rows);
+      if (g < a.p.groups) groups.tile[g] = (int)min(sum + x - mt, a.most_rows);
       sum = min(sum + __shfl_sync(~0u, x, 31), a.most_rows);
     }
-    if (lane == 0) tile_base[a.p.groups] = (int)sum;
+    if (lane == 0) groups.tile[a.p.groups] = (int)sum;
   }
   tc_fence_before();
   __syncthreads();
   if constexpr (PAIR) cluster_meet();  // the barriers of both blocks are there
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(~0u, *tmem_at, 0);
-  const int tiles = tile_base[a.p.groups] * a.n_tiles;
+  const int tiles = groups.tile[a.p.groups] * a.n_tiles;
   const int parts = SPLIT ? (int)cluster_size() : 1, part = SPLIT ? (int)cluster_rank() : 0;
   const int sharers = PAIR ? 2 : parts, first = (int)blockIdx.x / sharers, step = (int)gridDim.x / sharers;
   const int half_b = PAIR ? (int)cluster_rank() : 0;  // of b, and of the pair
@@ -462,7 +520,7 @@ __global__ void __launch_bounds__(kThreads4, 1)
       Walk4 w;
       bool ok = true;
       for (int t = first; ok && t < tiles; t += step) {
-        walk_to<kRows>(w, t, a, tile_base, kTileN);
+        walk_to<kRows>(w, t, a, groups, kTileN);
         for (int s = 0; s < stages; ++s) {
           if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, given_up))) break;
           const uint32_t at = smem_u32(smem) + stage * S::kStageBytes, scales = at + S::kOperandBytes;
@@ -539,7 +597,7 @@ __global__ void __launch_bounds__(kThreads4, 1)
     int acc = 0, acc_phase = 0;
     Walk4 w;
     for (int t = first; t < tiles; t += step) {
-      walk_to<kRows>(w, t, a, tile_base, kTileN);
+      walk_to<kRows>(w, t, a, groups, kTileN);
       if (!__all_sync(~0u, mbar_wait(done + 8 * acc, acc_phase, given_up))) break;  // (and the warp is whole for the loads)
       tc_fence_after();
       const uint32_t at = from + acc * BN;
@@ -555,7 +613,7 @@ __global__ void __launch_bounds__(kThreads4, 1)
       const bool there = row < w.end;
       if constexpr (SPLIT) {
         // the sums to shared memory, where the stages were: every step that read them is done
-        float *red = (float *)smem + row_in * kSumPitch4 + half * S::kCols;
+        float *red = (float *)smem + row_in * S::kSumPitch + half * S::kCols;
 #pragma unroll
         for (int c = 0; c < S::kCols; c += 32) {
           uint32_t v[32];
@@ -569,20 +627,20 @@ __global__ void __launch_bounds__(kThreads4, 1)
         release();
       } else if constexpr (SWIGLU) {
         const int c0 = half * 64;
-        uint32_t packed[2][4], bytes = 0;
+        uint32_t g[2][32], u[2][32], packed[2][4], bytes = 0;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) tmem_load(at + c0 + b * 32, g[b]), tmem_load(at + 128 + c0 + b * 32, u[b]);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) tmem_wait(g[b]), tmem_wait(u[b]);
+        release();
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          uint32_t g[32], u[32];
-          tmem_load(at + c0 + b * 32, g);
-          tmem_load(at + 128 + c0 + b * 32, u);
-          tmem_wait(g), tmem_wait(u);
-          if (b == 1) release();
           float h[32];
           uint32_t amax = 0;
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
-            const float x = __uint_as_float(g[i]);
-            h[i] = __fdividef(x, 1.0f + expf(-x)) * __uint_as_float(u[i]);  // (within 2^-21; 0 from x = -87 down)
+            const float x = __uint_as_float(g[b][i]);
+            h[i] = __fdividef(x, 1.0f + expf(-x)) * __uint_as_float(u[b][i]);  // (within 2^-21; 0 from x = -87 down)
             amax = max(amax, abs_bits(h[i]));
           }
           const uint32_t byte = fp4_scale(amax);
@@ -610,20 +668,22 @@ __global__ void __launch_bounds__(kThreads4, 1)
           for (int i = 0; i < 16; ++i) packed[c / 2 + i] = pack_bf16(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
         }
         release();
-        // 64 columns at a time to shared memory, in 16-byte pieces swizzled by row.  32 whole rows leave from there by a tensor
-        // copy; rows that a group's end cuts, or that a tensor copy cannot reach (a pitch that is no multiple of 16 bytes),
-        // leave in whole rows as the warp reads them back.
-        const uint32_t to = smem_u32(smem) + S::kStages * S::kStageBytes + (warp - 4) * 4096;
+        // kOutCols columns at a time to shared memory, in 16-byte pieces swizzled by row.  32 whole rows leave from there by a
+        // tensor copy; rows that a group's end cuts, or that a tensor copy cannot reach (a pitch that is no multiple of 16
+        // bytes), leave in whole rows as the warp reads them back.
+        constexpr int kRowBytes = S::kOutCols * 2, kPieces = kRowBytes / 16;
+        auto place = [](int r, int piece) { return (uint32_t)(r * kRowBytes + (kPieces == 8 ? piece ^ (r & 7) : piece ^ ((r >> 1) & 3)) * 16); };
+        const uint32_t to = smem_u32(smem) + S::kStages * S::kStageBytes + (warp - 4) * 32 * kRowBytes;
         const int row0 = row - lane, valid = max(0, min(32, w.end - row0));
 #pragma unroll
-        for (int c = 0; c < S::kCols; c += 64) {
+        for (int c = 0; c < S::kCols; c += S::kOutCols) {
           const int c0 = w.n0 + half * S::kCols + c;
           if (lane == 0) tma_store_read();
           __syncwarp();
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + lane * 128 + (i ^ (lane & 7)) * 16), "r"(packed[c / 2 + i * 4]),
-                         "r"(packed[c / 2 + i * 4 + 1]), "r"(packed[c / 2 + i * 4 + 2]), "r"(packed[c / 2 + i * 4 + 3])
+          for (int i = 0; i < kPieces; ++i)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + place(lane, i)), "r"(packed[c / 2 + i * 4]), "r"(packed[c / 2 + i * 4 + 1]),
+                         "r"(packed[c / 2 + i * 4 + 2]), "r"(packed[c / 2 + i * 4 + 3])
                          : "memory");
           if (a.store_tiles && valid == 32) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -632,19 +692,19 @@ __global__ void __launch_bounds__(kThreads4, 1)
           } else {
             __syncwarp();
             __nv_bfloat16 *out = (__nv_bfloat16 *)a.p.out + (int64_t)row0 * a.p.ldo + c0;
-            if (a.store_tiles && c0 + 64 <= a.p.n) {
-              for (int i = lane; i < valid * 8; i += 32) {
-                const int r = i / 8, piece = i % 8;
+            if (a.store_tiles && c0 + S::kOutCols <= a.p.n) {
+              for (int i = lane; i < valid * kPieces; i += 32) {
+                const int r = i / kPieces, piece = i % kPieces;
                 uint4 u;
-                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(to + r * 128 + (piece ^ (r & 7)) * 16) : "memory");
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(to + place(r, piece)) : "memory");
                 *reinterpret_cast<uint4 *>(out + r * a.p.ldo + piece * 8) = u;
               }
             } else {
-              const int cols = min(64, a.p.n - c0);
+              const int cols = min(S::kOutCols, a.p.n - c0);
               for (int r = 0; r < valid; ++r)
                 for (int j = lane; j < cols; j += 32) {
                   uint16_t u;
-                  asm volatile("ld.shared.b16 %0, [%1];" : "=h"(u) : "r"(to + r * 128 + ((j >> 3) ^ (r & 7)) * 16 + (j & 7) * 2) : "memory");
+                  asm volatile("ld.shared.b16 %0, [%1];" : "=h"(u) : "r"(to + place(r, j >> 3) + (j & 7) * 2) : "memory");
                   reinterpret_cast<uint16_t *>(out)[r * a.p.ldo + j] = u;
                 }
             }
@@ -686,19 +746,39 @@ __global__ void __launch_bounds__(kThreads4, 1)
     cluster_meet();
     if (first < tiles && !*given_up) {
       Walk4 w;
-      walk_to<kRows>(w, first, a, tile_base, BN);
-      const int rows = min(128, w.end - w.row);
-      for (int i = threadIdx.x; i < (rows - part + parts - 1) / parts * (BN / 4); i += kThreads4) {
-        const int r = part + i / (BN / 4) * parts, c = i % (BN / 4) * 4;
-        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int q = 0; q < parts; ++q) {
-          const float4 x = load_from_block(smem_u32(smem) + (r * kSumPitch4 + c) * 4, q);
-          v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
-        }
-        TO *out = (TO *)a.p.out + (int64_t)(w.row + r) * a.p.ldo + w.n0 + c;
+      walk_to<kRows>(w, first, a, groups, kTileN);
+      const int rows = min(128, w.end - w.row), mine = (rows - part + parts - 1) / parts;
+      if constexpr (SWIGLU) {
+        // a warp a row and block of 32: a lane has a gate and an up sum
+        for (int i = warp; i < mine * 4; i += kThreads4 / 32) {
+          const int r = part + (i >> 2) * parts, c = (i & 3) * 32 + lane;
+          const uint32_t at = smem_u32(smem) + (r * S::kSumPitch + c) * 4;
+          float g = 0.0f, u = 0.0f;
+          for (int q = 0; q < parts; ++q) g += load_one(at, q), u += load_one(at + 128 * 4, q);
+          const float h = __fdividef(g, 1.0f + expf(-g)) * u;
+          const uint32_t byte = fp4_scale(__reduce_max_sync(~0u, abs_bits(h)));
+          float v = h * fp4_inverse(byte);
+          // eight neighbours' values to the first of them
+          float eight[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (w.n0 + c + j < a.p.n) out[j] = from_f32<TO>(v[j]);
+          for (int j = 0; j < 8; ++j) eight[j] = __shfl_down_sync(~0u, v, j);
+          if ((lane & 7) == 0) *reinterpret_cast<uint32_t *>((uint8_t *)a.p.out + (int64_t)(w.row + r) * a.p.ldo + (w.n0 + c) / 2) = fp4_eight(eight);
+          if (lane == 0)
+            a.p.hs[((int64_t)w.slot * a.n_tiles + w.n0 / 128) * kScaleTile + (r & 31) * 16 + (r >> 5) * 4 + (i & 3)] = (uint8_t)byte;
+        }
+      } else {
+        for (int i = threadIdx.x; i < mine * (BN / 4); i += kThreads4) {
+          const int r = part + i / (BN / 4) * parts, c = i % (BN / 4) * 4;
+          float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          for (int q = 0; q < parts; ++q) {
+            const float4 x = load_from_block(smem_u32(smem) + (r * S::kSumPitch + c) * 4, q);
+            v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+          }
+          TO *out = (TO *)a.p.out + (int64_t)(w.row + r) * a.p.ldo + w.n0 + c;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (w.n0 + c + j < a.p.n) out[j] = from_f32<TO>(v[j]);
+        }
       }
     }
     cluster_meet();  // no block leaves while its sums are read
@@ -714,6 +794,9 @@ __global__ void __launch_bounds__(kThreads4, 1)
 // ---- host ------------------------------------------------------------------------------------
 
 enum { kAlone, kSplit, kPair };
+// Tiles of `rows` rows, at most: every group may have one that is not full, and none more than it has rows.  (Offsets that make
+// groups overlap can ask for more; blocks that go on from tile to tile take those too, clusters that take one each do not reach them.)
+int64_t row_tiles(const Product4Args &p, int rows) { return p.offsets ? std::min(p.m, ceil_div(p.m, rows) + p.groups - 1) : ceil_div(p.m, rows); }
 template <int BN, bool SWIGLU, typename TO, int HOW = kAlone>
 int run_tiles4(const Product4Args &p, cudaStream_t st, int parts = 1) {
   constexpr bool SPLIT = HOW == kSplit, PAIR = HOW == kPair;
@@ -735,11 +818,11 @@ int run_tiles4(const Product4Args &p, cudaStream_t st, int parts = 1) {
   mo = ma;
   a.store_tiles = S::kOutBytes && aligned(p.out, 16) && p.ldo % 8 == 0 && p.n % 8 == 0;  // (a tensor copy's rows end on 16 bytes)
   if (a.store_tiles)
-    if (const int rc = make_out_map(&mo, p.out, p.n, p.m, p.ldo, 128)) return rc;
+    if (const int rc = make_out_map(&mo, p.out, p.n, p.m, p.ldo, S::kOutCols * 2)) return rc;
   static bool set[64] = {};
   auto kernel = tuna_product4_kernel<BN, SWIGLU, SPLIT, PAIR, TO>;
   if (const int rc = allow_smem(kernel, S::kSmem, set)) return rc;
-  const int64_t most = (ceil_div(p.m, kRows) + (p.offsets ? p.groups : 0)) * a.n_tiles;
+  const int64_t most = row_tiles(p, kRows) * a.n_tiles;
   if (PAIR)
     return launch_cluster(kernel, dim3((unsigned)std::min<int64_t>(most, std::max(sm_count() / 2, 1)) * 2), 2, kThreads4, S::kSmem, st, false, ma, mb, msa, msb, mo, a);
   if (SPLIT) return launch_cluster(kernel, dim3((unsigned)(most * parts)), parts, kThreads4, S::kSmem, st, false, ma, mb, msa, msb, mo, a);
@@ -751,26 +834,24 @@ size_t dtype_size(int dtype) { return dtype == TUNA_DTYPE_F32 ? 4 : dtype == TUN
 }  // namespace
 
 int launch_product4(const Product4Args &p, cudaStream_t st) {
-  // Pairs of blocks where they have two rounds of tiles or more, and groups whole tiles of rows on average.  (Pairs and blocks alone,
+  // Pairs of blocks where they have two rounds of tiles or more, and groups a tile and a half of rows on average.  (Pairs and blocks alone,
   // us: 8192 x 4096 x 4096 52.9 and 62.5, 8192^3 180 and 210, 3000^3 19.5 and 20.8; with less than two rounds 2048 x 4096 x 4096 18.4 and 18.2,
   // 1024 x 4096 x 4096 11.8 and 11.2.  64 groups of 4096 x 2048, rows of a group 128: 70 and 68, 256: 99 and 100, 512: 155 and 165, 1024:
   // 268 and 294.)
   const int64_t pairs = std::max(sm_count() / 2, 1), tiles = ceil_div(p.m, 256) * ceil_div(p.n, p.swiglu ? 128 : 256);
-  if (tiles >= 2 * pairs && (!p.offsets || p.m >= 256 * (int64_t)p.groups)) {
+  if (tiles >= 2 * pairs && (!p.offsets || p.m >= 384 * (int64_t)p.groups)) {
     if (p.swiglu) return run_tiles4<256, true, uint8_t, kPair>(p, st);
     return p.out_f32 ? run_tiles4<256, false, float, kPair>(p, st) : run_tiles4<256, false, __nv_bfloat16, kPair>(p, st);
   }
-  if (p.swiglu) return run_tiles4<256, true, uint8_t>(p, st);
-  const int64_t rows = ceil_div(p.m, 128) + (p.offsets ? p.groups - 1 : 0);
+  const int64_t rows = row_tiles(p, 128), stages = ceil_div(p.k, 256);
   const int64_t wide = rows * ceil_div(p.n, 256), narrow = rows * ceil_div(p.n, 128);
-  if (6 * ceil_div(wide, sm_count()) < 5 * ceil_div(narrow, sm_count()))
+  if (!p.swiglu && 6 * ceil_div(wide, sm_count()) < 5 * ceil_div(narrow, sm_count()))
     return p.out_f32 ? run_tiles4<256, false, float>(p, st) : run_tiles4<256, false, __nv_bfloat16>(p, st);
-  if (!p.offsets) {
-    const int64_t stages = ceil_div(p.k, 256);
-    int parts = 4;
-    while (parts > 1 && (narrow * parts > 128 || stages - stages / parts < 6)) parts /= 2;
-    if (parts > 1) return p.out_f32 ? run_tiles4<128, false, float, kSplit>(p, st, parts) : run_tiles4<128, false, __nv_bfloat16, kSplit>(p, st, parts);
-  }
+  // Few tiles: a cluster shares each.  (narrow: with SwiGLU too, whose tiles have 128 columns of the result)
+  int parts = 4;
+  while (parts > 1 && (narrow * parts > 128 || stages - stages / parts < 6)) parts /= 2;
+  if (p.swiglu) return parts > 1 ? run_tiles4<256, true, uint8_t, kSplit>(p, st, parts) : run_tiles4<256, true, uint8_t>(p, st);
+  if (parts > 1) return p.out_f32 ? run_tiles4<128, false, float, kSplit>(p, st, parts) : run_tiles4<128, false, __nv_bfloat16, kSplit>(p, st, parts);
   return p.out_f32 ? run_tiles4<128, false, float>(p, st) : run_tiles4<128, false, __nv_bfloat16>(p, st);
 }
 
@@ -787,6 +868,10 @@ int launch_quantize4_rows(const void *x, bool f32, int64_t rows, int cols, int64
   Quant4Args a = {};
   a.x = x, a.rows = rows, a.cols = cols, a.ldx = ldx, a.gather = gather, a.in_rows = in_rows, a.groups = groups, a.offsets = offsets;
   a.q = (uint8_t *)q, a.ldq = ldq, a.scale = scale, a.runs = (int)ceil_div(cols, 128);
+  if (offsets && rows < 32 * (int64_t)groups) {  // FEW
+    const dim3 grid((unsigned)rows, (unsigned)ceil_div(cols, 2048));
+    return f32 ? launch(tuna_quantize4_few_kernel<float>, grid, 256, 0, st, false, a) : launch(tuna_quantize4_few_kernel<__nv_bfloat16>, grid, 256, 0, st, false, a);
+  }
   const dim3 grid = strips_grid(fp4_slots(rows, offsets ? groups : 0), cols, a.strips);
   return f32 ? launch(tuna_quantize4_rows_kernel<float>, grid, 256, 0, st, false, a)
              : launch(tuna_quantize4_rows_kernel<__nv_bfloat16>, grid, 256, 0, st, false, a);

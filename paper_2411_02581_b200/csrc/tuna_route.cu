@@ -364,6 +364,37 @@ __global__ void __launch_bounds__(kSmallThreads) tuna_route_small_kernel(RouteAr
   for (int64_t j = sum + threadIdx.x; j < a.tokens * a.k; j += kSmallThreads) o.rows[j] = -1;
 }
 
+// The order of a few choices of one rank in one block and one launch.
+__global__ void __launch_bounds__(kSmallThreads) tuna_order_small_kernel(OrderArgs o) {
+  extern __shared__ __align__(16) char smem[];
+  int64_t *base = (int64_t *)smem;
+  int *count = (int *)(smem + (size_t)o.experts * 8);
+  for (int e = threadIdx.x; e < o.experts; e += kSmallThreads) count[e] = 0;
+  wait_previous();
+  allow_next();
+  __syncthreads();
+  const int64_t n = o.tokens * o.k;
+  for (int64_t i = threadIdx.x; i < n; i += kSmallThreads) {
+    const int id = o.ids[i];
+    if (id >= 0 && id < o.experts) atomicAdd(count + id, 1);
+  }
+  __syncthreads();
+  const int e = threadIdx.x;  // (experts <= TUNA_MOE_MAX_EXPERTS < kSmallThreads)
+  const int64_t c = e < o.experts ? count[e] : 0;
+  int64_t sum;
+  const int64_t x = block_scan(c, &sum);
+  if (e < o.experts) {
+    base[e] = x;
+    if (o.counts) o.counts[e] = c;
+    if (o.offsets) {
+      o.offsets[e] = x;
+      if (e == o.experts - 1) o.offsets[o.experts] = sum;
+    }
+  }
+  place_entries<kSmallThreads>(o, smem, 0, n);
+  for (int64_t j = sum + threadIdx.x; j < n; j += kSmallThreads) o.rows[j] = -1;
+}
+
 // Gradient of the weights with respect to the logits; the probabilities are computed anew
 // from the logits (one read of them) instead of being kept by the forward pass.
 //   softmax            dz_e = p_e (g_e - sum_s g_s p_s)          g: dw at the chosen, 0 elsewhere
@@ -650,6 +681,10 @@ struct Lanes {
 };
 int64_t small_tokens(int experts, int k) { return 2 * kSmallThreads / by_width(experts, k, Lanes{}); }
 
+// Choices that one block orders before two launches would be done.  (One block and two launches, us: 1 token, 64 experts, 2 slots 3.4 and 4.5;
+// 64 tokens 3.9 and 4.7; 64 tokens, 512 experts, 8 slots 4.8 and 6.7; 128 tokens, 64 experts, 8 slots 5.7 and 5.2; 1024 tokens, 2 slots 7.7 and 5.2.)
+constexpr int64_t kSmallEntries = 512;
+
 size_t dtype_size(int dtype) { return dtype == TUNA_DTYPE_F32 ? 4 : dtype == TUNA_DTYPE_BF16 ? 2 : 0; }
 
 }  // namespace
@@ -692,6 +727,11 @@ int tuna_moe_order(const int32_t *ids, int64_t tokens, int experts, int k, int r
   plan_order(o, tokens, experts, k, ranks);
   if (!workspace || !aligned(workspace, 256) || workspace_bytes < order_bytes(tokens, experts, k, ranks)) return TUNA_ERR_WORKSPACE;
   o.hist = (uint16_t *)workspace;
+  if (ranks == 1 && tokens * k <= kSmallEntries) {
+    static bool set[64] = {};
+    if (const int rc = allow_smem(tuna_order_small_kernel, order_smem(TUNA_MOE_MAX_EXPERTS, kSmallThreads), set)) return rc;
+    return launch(tuna_order_small_kernel, dim3(1), kSmallThreads, order_smem(experts, kSmallThreads), st, false, o);
+  }
   if (const int rc = launch(tuna_order_hist_kernel, dim3((unsigned)(o.rank_chunks * ranks)), 256, (size_t)experts * 4, st, false, o)) return rc;
   return launch_order(o, st);
 }
