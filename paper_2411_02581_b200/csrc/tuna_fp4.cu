@@ -46,12 +46,40 @@ __device__ __forceinline__ void fp4_values(uint32_t q, float (&v)[8]) {
   }
 }
 
+// The largest magnitude of values: an infinity or a NaN, if there is one.
+__device__ __forceinline__ float top_of(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// silu(g) * u of two values.  1 / (1 + 2^(-g log2 e)): the exponent's rounding makes it off by |g| 2^-23, the rest by 2^-21; from g = -88 down
+// it is 0.  (Six instructions a value: with expf and a division the results of a tile took longer than its steps.)
+__device__ __forceinline__ uint64_t swiglu2(float g0, float g1, float u0, float u1) {
+  const uint64_t g = pair(g0, g1);
+  float a, b, c, d;
+  unpair(mul2(g, pair(-1.4426950408889634f, -1.4426950408889634f)), a, b);
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(c) : "f"(a));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(b));
+  unpair(add2(pair(c, d), pair(1.0f, 1.0f)), a, b);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(c) : "f"(a));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(b));
+  return mul2(mul2(g, pair(c, d)), pair(u0, u1));
+}
+
 // ---- quantisation --------------------------------------------------------------------------
 //
 // Bound by memory: two bytes (bf16) read and 17/32 written a value.  A warp takes 256 columns of four rows that are 32
-// apart, 8 columns a lane, so that a lane loads 16 bytes of bf16, a block's largest magnitude costs two shuffles, and
-// the four rows' scales of four blocks are 16 bytes in a row.  A block of threads takes eight such sets of rows, a quarter of a
-// tile, and `strips` times 256 columns of them, the next ones on their way during the present ones.
+// apart, 8 columns a lane, so that a lane loads 16 bytes of bf16 a row, and the four rows' scales of four blocks are 16 bytes in a
+// row.  A block of threads takes eight such sets of rows, a quarter of a tile, and `strips` times 256 columns of them.  Rows on
+// 16-byte boundaries come by asynchronous copies, several strips ahead, each lane's to a place of its own in shared memory (so
+// that nobody waits for anybody); others by loads of what width they allow, one strip ahead.
+template <typename T>
+__host__ __device__ constexpr int ahead() { return sizeof(T) == 2 ? 3 : 2; }  // strips on their way and under way: 48 and 64 KB a block of threads
 struct Quant4Args {
   const void *x;
   int64_t rows, ldx, ldq, in_rows;
@@ -84,8 +112,44 @@ __device__ __forceinline__ void slot_rows(const int64_t *offsets, int groups, in
   row = begin + (slot - begin / 128 - g) * 128, end = min(row + 128, cut(g + 1));
 }
 
+// A lane's eight values of four rows: their 4-bit words, and in lane 4 j + i of the sixteen of a run the scales of row i.
 template <typename T>
+__device__ __forceinline__ void quantize_four(const Eight<T> (&x)[4], uint32_t (&q)[4], uint32_t &scales) {
+  float v[4][8];
+  uint32_t top[2];  // the upper halves of the largest magnitudes (their exponents are all that counts), two rows a word
+#pragma unroll
+  for (int i = 0; i < 4; i += 2) {
+    float t[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      x[i + j].values(v[i + j]);
+      const float(&w)[8] = v[i + j];
+      t[j] = top_of(top_of(top_of(top_of(w[0], w[1], w[2]), w[3], w[4]), w[5], w[6]), w[7], 0.0f);
+    }
+    top[i / 2] = __byte_perm(__float_as_uint(t[0]), __float_as_uint(t[1]), 0x7632) & 0x7fff7fffu;
+  }
+#pragma unroll
+  for (int d = 1; d < 4; d <<= 1)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) top[i] = __vmaxu2(top[i], __shfl_xor_sync(~0u, top[i], d));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t e = i & 1 ? top[i >> 1] >> 23 : top[i >> 1] >> 7 & 255;
+    const float inverse = __uint_as_float(min(256 - e, 254u) << 23);  // that of fp4_scale(e)
+    const uint64_t by = pair(inverse, inverse);
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) unpair(mul2(pair(v[i][j], v[i][j + 1]), by), v[i][j], v[i][j + 1]);
+    q[i] = fp4_eight(v[i]);
+  }
+  const uint32_t own = threadIdx.x & 2 ? top[1] : top[0];
+  uint32_t mine = fp4_scale(threadIdx.x & 1 ? own & 0xffff0000u : own << 16) << (threadIdx.x & 12) * 2;
+  mine |= __shfl_xor_sync(~0u, mine, 4);
+  scales = mine | __shfl_xor_sync(~0u, mine, 8);
+}
+template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(256) tuna_quantize4_rows_kernel(Quant4Args a) {
+  extern __shared__ __align__(16) uint4 ring[];  // [kAhead][4][kWords][256], a lane's pieces in its own column
+  constexpr int kAhead = ahead<T>(), kWords = Eight<T>::kWords;
   wait_previous();
   allow_next();
   const int lane = threadIdx.x & 31, l = (blockIdx.x & 3) * 8 + (threadIdx.x >> 5);
@@ -93,47 +157,70 @@ __global__ void __launch_bounds__(256) tuna_quantize4_rows_kernel(Quant4Args a) 
   int64_t row0, end;
   slot_rows(a.offsets, a.groups, a.rows, slot, row0, end);
   if (row0 + l >= end) return;
+  const int rows = (int)min((end - row0 - l + 31) / 32, (int64_t)4);
+  int c0 = (int)blockIdx.y * a.strips * 256;                        // first column of the strip
+  const int last = min(a.cols, c0 + a.strips * 256);                // end of this block's columns
   const T *from[4];
+  uint32_t *to[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int64_t r = row0 + l + 32 * i;
-    const int64_t at = r >= end ? -1 : a.gather ? __ldg(a.gather + r) : r;
-    from[i] = at >= 0 && at < a.in_rows ? reinterpret_cast<const T *>(a.x) + at * a.ldx : nullptr;
+    const int64_t r = row0 + l + 32 * min(i, rows - 1);  // (a row that is not there: the last one again, which nobody stores)
+    const int64_t at = a.gather ? min(max(__ldg(a.gather + r), (int64_t)0), a.in_rows - 1) : r;
+    from[i] = reinterpret_cast<const T *>(a.x) + at * a.ldx + c0 + lane * 8;
+    to[i] = reinterpret_cast<uint32_t *>(a.q + r * a.ldq + c0 / 2) + lane;
   }
-  int c = (int)blockIdx.y * a.strips * 256 + lane * 8;
+  uint32_t *scale = reinterpret_cast<uint32_t *>(a.scale + (slot * a.runs + (c0 >> 7) + (lane >> 4)) * kScaleTile + l * 16) + (lane & 3);
   Eight<T> x[4];
-  auto fetch = [&](int c) {
+  auto fetch = [&](int ahead, int stage) {  // `ahead`: strips from the present one
+    const int left = a.cols - c0 - ahead * 256 - lane * 8;
+    if (!ALIGNED) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i].load_any(from[i] + c, from[i] ? a.cols - c : 0);
-  };
-  fetch(c);
-  for (int n = 0; n < a.strips && c - lane * 8 < a.cols; ++n, c += 256) {
-    uint32_t words[4], q[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t amax = Eight<T>::top_bits(x[i].top(0));
-      amax = max(amax, __shfl_xor_sync(~0u, amax, 1));
-      amax = max(amax, __shfl_xor_sync(~0u, amax, 2));
-      const uint32_t byte = fp4_scale(amax);
-      const float by = fp4_inverse(byte);
-      float v[8];
-      x[i].values(v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] *= by;
-      q[i] = fp4_eight(v);
-      words[i] = byte << (lane & 12) * 2;
-      words[i] |= __shfl_xor_sync(~0u, words[i], 4);
-      words[i] |= __shfl_xor_sync(~0u, words[i], 8);
+      for (int i = 0; i < 4; ++i) x[i].load_any(from[i] + ahead * 256, left);
+      return;
     }
-    if (n + 1 < a.strips) fetch(c + 256);
-    const int run = c >> 7;
-    if (c < (a.cols + 31) / 32 * 32) {
+    if (c0 + ahead * 256 < last) {
+      const uint32_t at = smem_u32(ring + stage * 4 * kWords * 256 + threadIdx.x);
+#pragma unroll
+      for (int w = 0; w < kWords; ++w) {
+        const int bytes = max(0, min(16, (left - w * (8 / kWords)) * (int)sizeof(T)));  // (the rest of the 16 is zero)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + (i * kWords + w) * 4096),
+                       "l"(from[i] + (bytes ? ahead * 256 + w * (8 / kWords) : -lane * 8)), "r"(bytes)
+                       : "memory");
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if (ALIGNED) {
+#pragma unroll
+    for (int n = 0; n < kAhead - 1; ++n) fetch(n, n);
+  } else {
+    fetch(0, 0);
+  }
+  int stage = 0;
+  for (; c0 < last; c0 += 256) {
+    if (ALIGNED) {
+      fetch(kAhead - 1, stage == 0 ? kAhead - 1 : stage - 1);
+      asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (row0 + l + 32 * i < end) *reinterpret_cast<uint32_t *>(a.q + (row0 + l + 32 * i) * a.ldq + c / 2) = q[i];
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) x[i].w[w] = ring[((stage * 4 + i) * kWords + w) * 256 + threadIdx.x];
+      if (++stage == kAhead) stage = 0;
     }
-    if ((lane & 15) == 0 && run < a.runs)
-      *reinterpret_cast<uint4 *>(a.scale + (slot * a.runs + run) * kScaleTile + l * 16) = make_uint4(words[0], words[1], words[2], words[3]);
+    uint32_t q[4], scales;
+    quantize_four(x, q, scales);
+    if (!ALIGNED && c0 + 256 < last) fetch(1, 0);
+    if (c0 + lane * 8 < (a.cols + 31) / 32 * 32) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < rows) *to[i] = q[i];
+    }
+    if ((lane & 12) == 0 && (c0 >> 7) + (lane >> 4) < a.runs) *scale = scales;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) from[i] += 256, to[i] += 32;
+    scale += 2 * kScaleTile / 4;
   }
 }
 
@@ -300,6 +387,7 @@ struct Tile4Args {
   int stages;   // of k: 256 values each
   int n_tiles;
   int store_tiles;     // bf16 results leave through map_out
+  int box_a;           // rows of a that a copy brings
   uint32_t most_rows;  // row tiles, at most: their number times n_tiles, and a step beyond, fits 31 bits
   int *error;
 };
@@ -521,13 +609,20 @@ __global__ void __launch_bounds__(kThreads4, 1)
       bool ok = true;
       for (int t = first; ok && t < tiles; t += step) {
         walk_to<kRows>(w, t, a, groups, kTileN);
+        // of a, the boxes that hold rows of the group (at least one, so that every block of a pair brings something); what stands
+        // in the others' place ends in rows that nobody stores
+        const int boxes = max(1, (min(128, w.end - w.row) + a.box_a - 1) / a.box_a);
+        const uint32_t left_out = (128 - boxes * a.box_a) * 128;
+        // a pair's first block expects what both bring
+        const int other = PAIR ? max(1, (min(128, w.end - w.row - 128) + a.box_a - 1) / a.box_a) : 0;
+        const uint32_t expected = S::kStageBytes - left_out + (PAIR ? S::kStageBytes - (128 - other * a.box_a) * 128 : 0);
         for (int s = 0; s < stages; ++s) {
           if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1, given_up))) break;
           const uint32_t at = smem_u32(smem) + stage * S::kStageBytes, scales = at + S::kOperandBytes;
           const uint32_t bar = PAIR ? in_first_block(full + 8 * stage) : full + 8 * stage;
-          if (half_b == 0) mbar_expect(full + 8 * stage, (PAIR ? 2 : 1) * S::kStageBytes);
+          if (half_b == 0) mbar_expect(full + 8 * stage, expected);
           const int col = (s_first + s) * 128, run = (s_first + s) * 2;
-          load_2d<PAIR>(at, &map_a, col, w.row, bar);
+          for (int q = 0; q < boxes; ++q) load_2d<PAIR>(at + q * a.box_a * 128, &map_a, col, w.row + q * a.box_a, bar);
           load_3d<PAIR>(scales, &map_sa, 0, run, w.slot, bar);
           if (SWIGLU) {
 #pragma unroll
@@ -635,18 +730,16 @@ __global__ void __launch_bounds__(kThreads4, 1)
         release();
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          float h[32];
-          uint32_t amax = 0;
+          float h[32], top = 0.0f;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const float x = __uint_as_float(g[b][i]);
-            h[i] = __fdividef(x, 1.0f + expf(-x)) * __uint_as_float(u[b][i]);  // (within 2^-21; 0 from x = -87 down)
-            amax = max(amax, abs_bits(h[i]));
+          for (int i = 0; i < 32; i += 2) {
+            unpair(swiglu2(__uint_as_float(g[b][i]), __uint_as_float(g[b][i + 1]), __uint_as_float(u[b][i]), __uint_as_float(u[b][i + 1])), h[i], h[i + 1]);
+            top = top_of(top, h[i], h[i + 1]);
           }
-          const uint32_t byte = fp4_scale(amax);
-          const float by = fp4_inverse(byte);
+          const uint32_t byte = fp4_scale(__float_as_uint(top) & 0x7fffffffu);
+          const uint64_t by = pair(fp4_inverse(byte), fp4_inverse(byte));
 #pragma unroll
-          for (int i = 0; i < 32; ++i) h[i] *= by;
+          for (int i = 0; i < 32; i += 2) unpair(mul2(pair(h[i], h[i + 1]), by), h[i], h[i + 1]);
 #pragma unroll
           for (int i = 0; i < 4; ++i) packed[b][i] = fp4_eight(h + i * 8);
           bytes |= byte << (8 * b);
@@ -755,9 +848,10 @@ __global__ void __launch_bounds__(kThreads4, 1)
           const uint32_t at = smem_u32(smem) + (r * S::kSumPitch + c) * 4;
           float g = 0.0f, u = 0.0f;
           for (int q = 0; q < parts; ++q) g += load_one(at, q), u += load_one(at + 128 * 4, q);
-          const float h = __fdividef(g, 1.0f + expf(-g)) * u;
+          float h, unused;
+          unpair(swiglu2(g, g, u, u), h, unused);
           const uint32_t byte = fp4_scale(__reduce_max_sync(~0u, abs_bits(h)));
-          float v = h * fp4_inverse(byte);
+          const float v = h * fp4_inverse(byte);
           // eight neighbours' values to the first of them
           float eight[8];
 #pragma unroll
@@ -811,7 +905,8 @@ int run_tiles4(const Product4Args &p, cudaStream_t st, int parts = 1) {
   a.error = error_word();
   if (!a.error) return TUNA_ERR_CUDA;
   CUtensorMap ma, mb, msa, msb, mo;
-  if (const int rc = make_map(&ma, 2, p.a, bytes, p.m, 1, p.lda, 128)) return rc;
+  a.box_a = p.offsets ? 32 : 128;
+  if (const int rc = make_map(&ma, 2, p.a, bytes, p.m, 1, p.lda, a.box_a)) return rc;
   if (const int rc = make_map(&mb, 3, p.b, bytes, p.n, matrices, p.ldb, SWIGLU ? 128 : S::kRowsB)) return rc;
   if (const int rc = make_scale_map(&msa, p.sa, runs, fp4_slots(p.m, p.offsets ? p.groups : 0), 1)) return rc;
   if (const int rc = make_scale_map(&msb, p.sb, runs, matrices * tiles_n, SWIGLU ? 1 : BN / 128)) return rc;
@@ -834,12 +929,12 @@ size_t dtype_size(int dtype) { return dtype == TUNA_DTYPE_F32 ? 4 : dtype == TUN
 }  // namespace
 
 int launch_product4(const Product4Args &p, cudaStream_t st) {
-  // Pairs of blocks where they have two rounds of tiles or more, and groups a tile and a half of rows on average.  (Pairs and blocks alone,
+  // Pairs of blocks where they have two rounds of tiles or more, and groups three tiles of rows on average.  (Pairs and blocks alone,
   // us: 8192 x 4096 x 4096 52.9 and 62.5, 8192^3 180 and 210, 3000^3 19.5 and 20.8; with less than two rounds 2048 x 4096 x 4096 18.4 and 18.2,
-  // 1024 x 4096 x 4096 11.8 and 11.2.  64 groups of 4096 x 2048, rows of a group 128: 70 and 68, 256: 99 and 100, 512: 155 and 165, 1024:
-  // 268 and 294.)
+  // 1024 x 4096 x 4096 11.8 and 11.2.  64 groups of 4096 x 2048, of sizes that differ by half, rows of a group 256: 109 and 102, 512: 175 and 170;
+  // of nearly equal sizes 512: 155 and 165, 1024: 268 and 294.)
   const int64_t pairs = std::max(sm_count() / 2, 1), tiles = ceil_div(p.m, 256) * ceil_div(p.n, p.swiglu ? 128 : 256);
-  if (tiles >= 2 * pairs && (!p.offsets || p.m >= 384 * (int64_t)p.groups)) {
+  if (tiles >= 2 * pairs && (!p.offsets || p.m >= 768 * (int64_t)p.groups)) {
     if (p.swiglu) return run_tiles4<256, true, uint8_t, kPair>(p, st);
     return p.out_f32 ? run_tiles4<256, false, float, kPair>(p, st) : run_tiles4<256, false, __nv_bfloat16, kPair>(p, st);
   }
@@ -855,12 +950,22 @@ int launch_product4(const Product4Args &p, cudaStream_t st) {
   return p.out_f32 ? run_tiles4<128, false, float>(p, st) : run_tiles4<128, false, __nv_bfloat16>(p, st);
 }
 
-// The grid over quarters of row tiles and strips of 256 columns: several strips a block where there are many (and then no more
-// than 65535 of the others: 2^24 columns are 2^16 strips), so that what finds its rows is shared by them.
-static dim3 strips_grid(int64_t tiles, int cols, int &strips) {
+// The grid over quarters of row tiles and strips of 256 columns: as many strips a block as leave `blocks` of them a multiprocessor, so
+// that what finds its rows is shared, and what is ahead is on its way (2^24 columns are 2^16 strips, of which a block takes several then).
+static dim3 strips_grid(int64_t tiles, int cols, int blocks, int &strips) {
   const int64_t quarters = tiles * 4, all = ceil_div(cols, 256);
-  strips = (int)std::max<int64_t>(1, std::min<int64_t>(all, quarters * all / (16 * sm_count())));
+  strips = (int)std::max<int64_t>(1, std::min<int64_t>(all, quarters * all / (blocks * sm_count())));
   return dim3((unsigned)quarters, (unsigned)ceil_div(all, strips));
+}
+
+template <typename T>
+static int run_quantize_rows(Quant4Args a, int64_t tiles, cudaStream_t st) {
+  const dim3 grid = strips_grid(tiles, a.cols, 6, a.strips);
+  if (!aligned(a.x, 16) || a.ldx * sizeof(T) % 16) return launch(tuna_quantize4_rows_kernel<T, false>, grid, 256, 0, st, false, a);
+  static bool set[64] = {};
+  constexpr size_t smem = ahead<T>() * 4 * Eight<T>::kWords * 256 * 16;
+  if (const int rc = allow_smem(tuna_quantize4_rows_kernel<T, true>, smem, set)) return rc;
+  return launch(tuna_quantize4_rows_kernel<T, true>, grid, 256, smem, st, false, a);
 }
 
 int launch_quantize4_rows(const void *x, bool f32, int64_t rows, int cols, int64_t ldx, const int64_t *gather, int64_t in_rows, int groups,
@@ -868,13 +973,13 @@ int launch_quantize4_rows(const void *x, bool f32, int64_t rows, int cols, int64
   Quant4Args a = {};
   a.x = x, a.rows = rows, a.cols = cols, a.ldx = ldx, a.gather = gather, a.in_rows = in_rows, a.groups = groups, a.offsets = offsets;
   a.q = (uint8_t *)q, a.ldq = ldq, a.scale = scale, a.runs = (int)ceil_div(cols, 128);
-  if (offsets && rows < 32 * (int64_t)groups) {  // FEW
+  // A few rows a group.  (64 groups, 4096 columns of bf16, us: 16 rows a group 5.6 and 13.6 in tiles, 32 rows 10.0 and 14.3, 64 rows 18 and 14.4.)
+  if (offsets && rows < 48 * (int64_t)groups) {
     const dim3 grid((unsigned)rows, (unsigned)ceil_div(cols, 2048));
     return f32 ? launch(tuna_quantize4_few_kernel<float>, grid, 256, 0, st, false, a) : launch(tuna_quantize4_few_kernel<__nv_bfloat16>, grid, 256, 0, st, false, a);
   }
-  const dim3 grid = strips_grid(fp4_slots(rows, offsets ? groups : 0), cols, a.strips);
-  return f32 ? launch(tuna_quantize4_rows_kernel<float>, grid, 256, 0, st, false, a)
-             : launch(tuna_quantize4_rows_kernel<__nv_bfloat16>, grid, 256, 0, st, false, a);
+  const int64_t tiles = fp4_slots(rows, offsets ? groups : 0);
+  return f32 ? run_quantize_rows<float>(a, tiles, st) : run_quantize_rows<__nv_bfloat16>(a, tiles, st);
 }
 
 }  // namespace tuna_ops
@@ -930,7 +1035,7 @@ int tuna_fp4_dequantize(const void *q, int64_t ldq, const void *scale, int64_t r
   Quant4Args a = {};
   a.rows = rows, a.cols = cols, a.groups = groups, a.offsets = offsets, a.q = (uint8_t *)q, a.ldq = ldq, a.scale = (uint8_t *)scale;
   a.runs = (int)ceil_div(cols, 128);
-  const dim3 grid = strips_grid(fp4_slots(rows, groups), cols, a.strips);
+  const dim3 grid = strips_grid(fp4_slots(rows, groups), cols, 16, a.strips);
   cudaStream_t st = (cudaStream_t)stream;
   return out_dtype == TUNA_DTYPE_F32 ? launch(tuna_dequantize4_kernel<float>, grid, 256, 0, st, false, a, (float *)out, ldo)
                                      : launch(tuna_dequantize4_kernel<__nv_bfloat16>, grid, 256, 0, st, false, a, (__nv_bfloat16 *)out, ldo);

@@ -1,8 +1,9 @@
 """Experts with 4-bit weights against a plain implementation in 64 bits.
 
 The bound follows the values.  A gate or up sum is within (d / 64 + 8) * 2^-23 of its terms' magnitude (test_fp4.py), so h =
-silu(gate) * up moves by at most 1.1 eg |u| + |silu(g)| eu + 1.1 eg eu (silu rises by 1.1 at most), and by 2^-19 of itself for the
-exponential and the division.  What its 4-bit form may then be lies between those of h a little larger and a little smaller, in
+silu(gate) * up moves by at most 1.1 eg |u| + |silu(g)| eu + 1.1 eg eu (silu rises by 1.1 at most), by 2^-19 of itself for the
+exponential and the division, and by |g| 2^-23 of itself for the exponential's argument, g log2(e) with a constant that is off by 2^-25 and a
+product by 2^-24 of themselves: e^-g is off by |g| 1.5 * 2^-24 of itself, 1 / (1 + e^-g) by no more.  What its 4-bit form may then be lies between those of h a little larger and a little smaller, in
 either of the scales that they give; a row of the down product moves linearly with it, by its own sum's share and by its rounding to
 bf16 (2^-8), the weighted sum by those of its slots, by k + 1 roundings of 2^-24, and by its own rounding to bf16.
 """
@@ -45,7 +46,7 @@ def plain_rows(x, w13, s13, w2, s2):
     eg, eu = ((d / 64 + 8) * 2.0 ** -23 * (a.abs() @ m.abs().t()) for m in (gate, up))
     s = torch.nn.functional.silu(g)
     h = s * u
-    off = 1.1 * eg * u.abs() + s.abs() * eu + 1.1 * eg * eu + 2.0 ** -19 * h.abs()
+    off = 1.1 * eg * u.abs() + s.abs() * eu + 1.1 * eg * eu + (2.0 ** -19 + 2.0 ** -23 * g.abs()) * h.abs()
     more, less = h + off * h.sign(), torch.where(off < h.abs(), h - off * h.sign(), torch.zeros_like(h))
     held = stored(h)
     slack = torch.stack([(rounded(v, by) - held).abs() for v in (more, less) for by in (more, less)]).amax(0)
