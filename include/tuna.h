@@ -586,10 +586,10 @@ int tuna_moe_route_backward(const void *logits, int dtype, int64_t tokens, int e
  * tuna_moe_balance_backward - dlogits (the logits' type, pitch ldd) of sum over g of dloss[g] * loss[g] +
  * dz[g] * z[g] (dz NULL: no such part); counts, the choice itself, are constant.  counts and live are those
  * of the loss (of all GPUs, where they were added up).  Masked logits, rows without live logits and tokens
- * of no segment get zeros.
+ * of no segment get zeros; a row that holds +inf gets no part of z's gradient.
  * Limits (TUNA_ERR_RANGE): those of tuna_moe_route, segments <= TUNA_MOE_MAX_SEGMENTS.
  */
-#define TUNA_MOE_MAX_SEGMENTS 65536
+#define TUNA_MOE_MAX_SEGMENTS 32768
 int tuna_moe_balance_workspace_bytes(int64_t tokens, int experts, int segments, size_t *bytes);
 int tuna_moe_balance(const void *logits, int dtype, int64_t tokens, int experts, int64_t ld,
                      const int32_t *ids, int k, int scoring, int segments, const int64_t *offsets,

@@ -37,15 +37,27 @@ struct BalanceArgs {
 __device__ __forceinline__ int64_t bound_of(const BalanceArgs &a, int g) {
   return a.offsets ? min(max(a.offsets[g], (int64_t)0), a.tokens) : g ? a.tokens : 0;
 }
-// The last segment that begins at t or before it (empty ones before it are passed over), -1 if none does.
-__device__ __forceinline__ int segment_of(const BalanceArgs &a, int64_t t) {
-  int low = -1, high = a.segments;
-  while (high - low > 1) {
-    const int g = (low + high) >> 1;
-    if (bound_of(a, g) <= t) low = g;
-    else high = g;
+// The last segment that begins at t or before it (empty ones before it are passed over), -1 if none does; its bounds.  The whole
+// warp looks at 32 segments at a time.
+__device__ __forceinline__ int segment_of(const BalanceArgs &a, int64_t t, int64_t &begin, int64_t &end) {
+  begin = 0, end = a.tokens;
+  if (!a.offsets) return 0;
+  const int lane = threadIdx.x & 31;
+  int base = 0;
+  for (int step = a.segments > 1024 ? 1024 : a.segments > 32 ? 32 : 1; step; step >>= 5) {
+    const int g = base + lane * step;
+    const int64_t at = bound_of(a, min(g, a.segments));
+    const uint32_t before = __ballot_sync(~0u, g < a.segments && at <= t);
+    if (!before) {
+      end = bound_of(a, 0);
+      return -1;
+    }
+    const int last = 31 - __clz(before);
+    base += last * step;
+    begin = __shfl_sync(~0u, at, last), end = __shfl_sync(~0u, at, min(last + 1, 31));
+    if (last == 31 && step == 1) end = bound_of(a, base + 1);
   }
-  return low;
+  return base;
 }
 
 template <int LPT>
@@ -61,7 +73,7 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
-// A lane's logits of a token, VPL of them from `first` on; a masked one (NaN, or behind the last) is -inf.
+// A lane's logits of a token, VPL of them from `first` on; those behind the last are -inf.
 template <int VPL, typename T>
 struct Logits {
   Eight<T> w[VPL / 8];
@@ -75,93 +87,148 @@ struct Logits {
   __device__ __forceinline__ void values(float (&z)[VPL]) const {
 #pragma unroll
     for (int i = 0; i < VPL / 8; ++i) w[i].values(z + 8 * i);
+    if (left < VPL) {
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) z[i] = i < left ? logit_of(z[i]) : -INFINITY;
+      for (int i = 0; i < VPL; ++i)
+        if (i >= left) z[i] = -INFINITY;
+    }
   }
 };
 
-// A token's probabilities from its logits: the softmax, the logarithm of its sum, and with sigmoids their shares (in p) and
-// the complements 1 - sigmoid (in rest).  A masked logit has none; a token without any other is not live.
-// (__expf is within 2 + 1.2 |x| units of 2^-24, which is 2^-19 where a probability is over e^-25.)
-template <int LPT, int VPL>
+// A token's probabilities from its logits.  p = x by; with sigmoids also the softmax, s by_s, and the complements 1 - sigmoid, rest
+// (both where they are wanted).  lse is the logarithm of the softmax's sum.  A masked logit (-inf, NaN) has no probability; a token
+// without any other is not live.
+//
+// Per value and exponential: a multiply-add and the power of two, 2^(z log2 e - top log2 e).  The rounding of top log2 e is
+// common to the token and cancels while |top| <= 2^16; 2^-20 remains (the exponent's own rounding, at most 2^-23 |z - top|, counts
+// where a probability is over e^-8).  Tokens for which that does not do are looked at again with more care: NaN, +inf, larger
+// logits, and with sigmoids no logit over 0, where the shares might be 0 / 0.
+template <int LPT, int VPL, bool SIGMOID>
 struct Token {
-  float soft[VPL], p[VPL], rest[VPL];
-  float lse;
-  bool live;
-  __device__ __forceinline__ void of(const float (&z)[VPL], int scoring, bool want_soft) {
-    float top = -INFINITY;
+  static constexpr int kMore = SIGMOID ? VPL : 2;
+  float x[VPL], s[kMore], rest[kMore];
+  float by, by_s, lse;
+  bool live, endless;
+  __device__ __forceinline__ void of(const float (&z)[VPL], bool want_soft, bool want_rest) {
+    float top = z[0];
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) top = fmaxf(top, z[i]);
+    for (int i = 1; i < VPL; ++i) top = fmaxf(top, z[i]);
     top = group_max<LPT>(top);
-    live = top != -INFINITY;
-    const bool endless = top == INFINITY;  // those that hold +inf share the softmax
-    const float base = live && !endless ? top : 0.0f;
+    live = top != -INFINITY, endless = false;
     float sum = 0.0f;
+    if (!SIGMOID || want_soft) {
+      const float shift = live ? -top * kLog2E : 0.0f;
+      uint64_t all = 0;
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-      soft[i] = __expf(z[i] - base);
-      if (endless) soft[i] = z[i] == INFINITY ? 1.0f : 0.0f;
-      sum += soft[i];
-    }
-    if (want_soft || scoring == TUNA_MOE_SOFTMAX) {
-      sum = group_sum<LPT>(sum);
-      const float by = live ? __fdividef(1.0f, sum) : 0.0f;
-      if (scoring == TUNA_MOE_SOFTMAX) {
-#pragma unroll
-        for (int i = 0; i < VPL; ++i) p[i] = soft[i] = soft[i] * by;
-        lse = live ? top + __logf(sum) : 0.0f;
-        return;
+      for (int i = 0; i < VPL; i += 2) {
+        float a, b;
+        unpair(fma2(pair(z[i], z[i + 1]), pair(kLog2E, kLog2E), pair(shift, shift)), a, b);
+        a = exp2_fast(a), b = exp2_fast(b);
+        if constexpr (SIGMOID) s[i] = a, s[i + 1] = b;
+        else x[i] = a, x[i + 1] = b;
+        all = add2(all, pair(a, b));
       }
-      lse = live ? top + __logf(sum) : 0.0f;
-      shares(z, top, by);
-    } else {
-      shares(z, top, 0.0f);
+      float a, b;
+      unpair(all, a, b);
+      sum = group_sum<LPT>(a + b);
+      by_s = by = live ? reciprocal_fast(sum) : 0.0f, lse = live ? top + __logf(sum) : 0.0f;
     }
+    bool careful = !(sum < INFINITY) || (live && fabsf(top) > 65536.0f);  // (the lanes of a row of NaN may find no largest logit)
+    if constexpr (SIGMOID) {
+      uint64_t all = 0;
+#pragma unroll
+      for (int i = 0; i < VPL; i += 2) {
+        float a, b, c, d;
+        unpair(mul2(pair(z[i], z[i + 1]), pair(-kLog2E, -kLog2E)), a, b);
+        a = exp2_fast(fminf(a, 127.0f)), b = exp2_fast(fminf(b, 127.0f));  // (finite; the reciprocal of 2^127 is taken for 0)
+        unpair(add2(pair(a, b), pair(1.0f, 1.0f)), c, d);
+        x[i] = reciprocal_fast(c), x[i + 1] = reciprocal_fast(d);
+        if (want_rest) unpair(mul2(pair(a, b), pair(x[i], x[i + 1])), rest[i], rest[i + 1]);
+        all = add2(all, pair(x[i], x[i + 1]));
+      }
+      float a, b;
+      unpair(all, a, b);
+      sum = group_sum<LPT>(a + b);
+      by = live ? reciprocal_fast(sum) : 0.0f;
+      careful |= !(sum < INFINITY) || (live && !(top >= 0.0f));
+    }
+    if (__any_sync(~0u, careful)) again(z, careful);  // (the warp goes together; what a token gets does not depend on its neighbours)
   }
-  // sigmoid(z) e^-m = e^(min(z, 0) - m) / (1 + e^-|z|) with m = min(top, 0): no share of very negative logits is 0 / 0.
-  // The first exponential is 1 or the second one where some logit is not negative, and the softmax's where none is.
-  __device__ __forceinline__ void shares(const float (&z)[VPL], float top, float by_soft) {
-    float sum = 0.0f;
+  __device__ __forceinline__ void again(const float (&given)[VPL], bool careful) {
+    float z[VPL], top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-      const float e = __expf(-fabsf(z[i])), one = __fdividef(1.0f, 1.0f + e);
-      const bool up = z[i] >= 0.0f;
-      p[i] = (top < 0.0f ? soft[i] : up ? 1.0f : e) * one;
-      rest[i] = up ? e * one : one;
-      soft[i] *= by_soft;
-      sum += p[i];
-    }
+    for (int i = 0; i < VPL; ++i) z[i] = logit_of(given[i]), top = fmaxf(top, z[i]);
+    top = group_max<LPT>(top);
+    const bool some = top != -INFINITY, infinite = top == INFINITY;  // those that hold +inf share the softmax
+    const float base = some && !infinite ? top : 0.0f;
+    float soft[VPL], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) soft[i] = infinite ? (z[i] == INFINITY ? 1.0f : 0.0f) : exp2_fast((z[i] - base) * kLog2E), sum += soft[i];
     sum = group_sum<LPT>(sum);
-    const float by = live ? __fdividef(1.0f, sum) : 0.0f;
+    if (careful) {
+      live = some, endless = infinite;
+      by_s = by = some ? reciprocal_fast(sum) : 0.0f, lse = some ? top + __logf(sum) : 0.0f;
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) p[i] *= by;
+      for (int i = 0; i < VPL; ++i) {
+        if constexpr (SIGMOID) s[i] = soft[i];
+        else x[i] = soft[i];
+      }
+    }
+    if constexpr (SIGMOID) {
+      // sigmoid(z) e^-m = e^(min(z, 0) - m) / (1 + e^-|z|) with m = min(top, 0); the first factor is the softmax's where no logit is over 0
+      sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) {
+        const float e = exp2_fast(-fabsf(z[i]) * kLog2E), one = reciprocal_fast(1.0f + e);
+        const bool up = z[i] >= 0.0f;
+        const float v = z[i] == -INFINITY ? 0.0f : (top < 0.0f ? soft[i] : up ? 1.0f : e) * one;
+        sum += v;
+        if (careful) x[i] = v, rest[i] = up ? e * one : one;
+      }
+      sum = group_sum<LPT>(sum);
+      if (careful) by = some ? reciprocal_fast(sum) : 0.0f;
+    }
   }
 };
 
-// loss and z of a segment by a whole block, whose threads bring the products of their experts
-template <int THREADS>
-__device__ __forceinline__ void finish(const BalanceArgs &a, int g, double product, double squares, int64_t n) {
-  __shared__ double sum[THREADS / 32];
+// Sums over a warp or, by way of `part`, over a block.
+template <typename T>
+__device__ __forceinline__ T warp_sum(T v) {
 #pragma unroll
-  for (int d = 16; d; d >>= 1) product += __shfl_xor_sync(~0u, product, d);
+  for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
+  return v;
+}
+// loss and z of a segment by a whole block, whose threads bring the products of their experts; of squares and n, the first warp's lanes
+// bring parts (others nothing that counts)
+template <int THREADS>
+__device__ __forceinline__ void finish(const BalanceArgs &a, int g, float product, float squares, uint32_t n) {
+  __shared__ float sum[THREADS / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  product = warp_sum(product);
+  if (lane == 0) sum[warp] = product;
   __syncthreads();
-  if (threadIdx.x % 32 == 0) sum[threadIdx.x / 32] = product;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    double all = 0.0;
-    for (int w = 0; w < THREADS / 32; ++w) all += sum[w];
-    a.loss[g] = n ? (float)(all * a.experts / ((double)a.k * n * n)) : 0.0f;
-    if (a.z) a.z[g] = n ? (float)(squares / n) : 0.0f;
-    a.live[g] = n;
+  if (warp == 0) {
+    const float all = warp_sum(lane < THREADS / 32 ? sum[lane] : 0.0f);
+    squares = warp_sum(squares), n = warp_sum(n);
+    if (lane == 0) {
+      // (E / k / n / n in this order: n^2 may have 62 bits)
+      a.loss[g] = n ? all * ((float)a.experts / a.k) / n / n : 0.0f;
+      if (a.z) a.z[g] = n ? squares / n : 0.0f;
+      a.live[g] = n;
+    }
   }
 }
 
-// A block's tokens, segment by segment.  ALONE: there is no other block, and what it finds is the answer.
-template <int LPT, int VPL, bool ALONE, typename T>
+// A block's tokens.  The steps do not mind the segments: what a step's tokens bring is added to the segments that they are in, and
+// a segment's sums leave at its end.  So the first logits are asked for before the segment is known.  ALONE: there is no other
+// block, and what it finds is the answer.
+constexpr int kIdsHeld = 2048;  // of a block's choices, in shared memory; more are read when they are counted
+template <int LPT, int VPL, bool ALONE, bool SIGMOID, typename T>
 __global__ void __launch_bounds__(kThreads) tuna_balance_kernel(BalanceArgs a) {
   extern __shared__ __align__(16) char smem[];
-  float *mass = (float *)smem;                    // [warps][experts]
+  float *mass = (float *)smem;                             // [warps][experts]
   int *count = (int *)(mass + kThreads / 32 * a.experts);  // [experts]
+  __shared__ int held[kIdsHeld];
   __shared__ float warp_squares[kThreads / 32];
   __shared__ int warp_live[kThreads / 32];
   wait_previous();
@@ -169,43 +236,36 @@ __global__ void __launch_bounds__(kThreads) tuna_balance_kernel(BalanceArgs a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = threadIdx.x % LPT;
   constexpr int kStep = kThreads / LPT;
   const int64_t b0 = blockIdx.x * a.chunk, b1 = min(b0 + a.chunk, a.tokens);
-  const int first = ALONE ? 0 : max(segment_of(a, b0), 0);
-  for (int g = first; g < a.segments; ++g) {
-    const int64_t begin = bound_of(a, g), t0 = max(begin, b0), t1 = min(bound_of(a, g + 1), b1);
-    if (!ALONE && begin >= b1) break;
-    if (!ALONE && t0 >= t1) continue;
-    for (int e = threadIdx.x; e < a.experts; e += kThreads) count[e] = 0;
-    float sum[VPL], squares = 0.0f;
-    int live = 0;
+  Logits<VPL, T> next;
+  int64_t t = b0 + threadIdx.x / LPT;
+  next.load(a, t, sub * VPL, t < b1);
+  const bool hold = (b1 - b0) * a.k <= kIdsHeld;
+  if (hold)
+    for (int i = threadIdx.x; i < (int)(b1 - b0) * a.k; i += kThreads)
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(held + i)), "l"(a.ids + b0 * a.k + i) : "memory");
+  for (int e = threadIdx.x; e < a.experts; e += kThreads) count[e] = 0;
+  int64_t begin, end;
+  int g = segment_of(a, b0, begin, end);
+  if (ALONE || g < 0) g = 0, begin = bound_of(a, 0), end = bound_of(a, 1);
+  float sum[VPL], squares = 0.0f;
+  int live = 0;
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) sum[i] = 0.0f;
-    __syncthreads();
+  for (int i = 0; i < VPL; ++i) sum[i] = 0.0f;
+  // what this block has of segment g; the sums begin anew
+  auto leave = [&] {
+    const int64_t t0 = max(begin, b0), t1 = min(end, b1);
+    if (!ALONE && t0 >= t1) return;
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();  // the choices are there, and the counts are zero
     for (int64_t i = t0 * a.k + threadIdx.x; i < t1 * a.k; i += kThreads) {
-      const int id = a.ids[i];
+      const int id = hold ? held[i - b0 * a.k] : a.ids[i];
       if (id >= 0 && id < a.experts) atomicAdd(count + id, 1);
-    }
-    Logits<VPL, T> next;
-    int64_t t = t0 + threadIdx.x / LPT;
-    next.load(a, t, sub * VPL, t < t1);
-    for (int64_t tb = t0; tb < t1; tb += kStep, t += kStep) {  // (uniform: the shuffles need whole warps)
-      float z[VPL];
-      next.values(z);
-      next.load(a, t + kStep, sub * VPL, t + kStep < t1);  // on its way during this one
-      Token<LPT, VPL> token;
-      token.of(z, a.scoring, a.z != nullptr);
-#pragma unroll
-      for (int i = 0; i < VPL; ++i) sum[i] += token.p[i];
-      if (token.live && sub == 0) {
-        ++live;
-        if (a.z) squares = fmaf(token.lse, token.lse, squares);
-      }
     }
 #pragma unroll
     for (int d = LPT; d < 32; d <<= 1)
 #pragma unroll
       for (int i = 0; i < VPL; ++i) sum[i] += __shfl_xor_sync(~0u, sum[i], d);
-#pragma unroll
-    for (int d = LPT; d < 32; d <<= 1) squares += __shfl_xor_sync(~0u, squares, d), live += __shfl_xor_sync(~0u, live, d);
+    squares = warp_sum(squares), live = warp_sum(live);
     if (lane < LPT) {
 #pragma unroll
       for (int i = 0; i < VPL; ++i)
@@ -213,11 +273,7 @@ __global__ void __launch_bounds__(kThreads) tuna_balance_kernel(BalanceArgs a) {
     }
     if (lane == 0) warp_squares[warp] = squares, warp_live[warp] = live;
     __syncthreads();
-    float all_squares = 0.0f;
-    int all_live = 0;
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) all_squares += warp_squares[w], all_live += warp_live[w];
-    double product = 0.0;
+    float product = 0.0f;
     const int64_t slot = (int64_t)blockIdx.x + g;
     for (int e = threadIdx.x; e < a.experts; e += kThreads) {
       float m = 0.0f;
@@ -225,79 +281,109 @@ __global__ void __launch_bounds__(kThreads) tuna_balance_kernel(BalanceArgs a) {
       for (int w = 0; w < kThreads / 32; ++w) m += mass[w * a.experts + e];
       if (ALONE) {
         a.mass[(int64_t)g * a.experts + e] = m, a.counts[(int64_t)g * a.experts + e] = count[e];
-        product += (double)m * count[e];
+        product = fmaf(m, count[e], product);
       } else {
         a.part[slot * a.experts + e] = make_float2(m, __int_as_float(count[e]));
       }
+      count[e] = 0;
     }
-    if (ALONE) finish<kThreads>(a, g, product, all_squares, all_live);
-    else if (threadIdx.x == 0) a.part_token[slot] = make_float2(all_squares, __int_as_float(all_live));
+    squares = lane < kThreads / 32 ? warp_squares[lane] : 0.0f, live = lane < kThreads / 32 ? warp_live[lane] : 0;
+    if (ALONE) {
+      finish<kThreads>(a, g, product, squares, live);
+    } else if (warp == 0) {
+      squares = warp_sum(squares), live = warp_sum(live);
+      if (lane == 0) a.part_token[slot] = make_float2(squares, __int_as_float(live));
+    }
     __syncthreads();
+    squares = 0.0f, live = 0;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) sum[i] = 0.0f;
+  };
+  for (int64_t tb = b0; tb < b1; tb += kStep, t += kStep) {  // (uniform: the shuffles need whole warps)
+    float z[VPL];
+    next.values(z);
+    next.load(a, t + kStep, sub * VPL, t + kStep < b1);  // on its way during this one
+    Token<LPT, VPL, SIGMOID> token;
+    token.of(z, a.z != nullptr, false);
+    const int64_t stop = min(tb + kStep, b1);
+    while (g < a.segments && begin < stop) {
+      if (t >= begin && t < min(end, stop) && token.live) {
+#pragma unroll
+        for (int i = 0; i < VPL; i += 2) unpair(fma2(pair(token.x[i], token.x[i + 1]), pair(token.by, token.by), pair(sum[i], sum[i + 1])), sum[i], sum[i + 1]);
+        if (sub == 0) {
+          ++live;
+          if (a.z) squares = fmaf(token.lse, token.lse, squares);
+        }
+      }
+      if (end > stop) break;
+      leave();
+      if (++g < a.segments) begin = end, end = max(begin, bound_of(a, g + 1));
+    }
+  }
+  for (; g < a.segments; ++g) {  // the segment that goes on behind this block; ALONE: those without tokens behind it too
+    leave();
+    if (!ALONE) break;
+    if (g + 1 < a.segments) begin = end, end = max(begin, bound_of(a, g + 2));
   }
 }
 
 // A block a segment: the parts of the blocks that met it, every 8th (or 16th, 32nd ...) of them by one row of threads, then the
 // rows in order.
 __global__ void __launch_bounds__(kSumThreads) tuna_balance_sum_kernel(BalanceArgs a) {
-  __shared__ float mass[kSumThreads];
-  __shared__ int count[kSumThreads];
-  __shared__ double squares[kSumThreads / 32];
-  __shared__ int live[kSumThreads / 32];
+  __shared__ float2 sums[kSumThreads];
+  __shared__ float2 tokens[kSumThreads / 32];
   wait_previous();
   allow_next();
-  const int g = blockIdx.x;
+  const int g = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t begin = bound_of(a, g), end = bound_of(a, g + 1);
   const int64_t s0 = begin / a.chunk + g, s1 = end > begin ? (end - 1) / a.chunk + g + 1 : s0;
-  const int lanes = a.experts <= 32 ? 32 : (a.experts + 31) / 32 * 32, rows = kSumThreads / lanes;  // (512 experts: 2 rows)
-  const int e = threadIdx.x % lanes, row = threadIdx.x / lanes;
-  float m = 0.0f;
-  int c = 0;
+  const int lanes = (a.experts + 31) / 32 * 32, rows = kSumThreads / lanes;  // (512 experts: 2 rows)
+  const int row = threadIdx.x / lanes, e = threadIdx.x - row * lanes;
+  float m = 0.0f, q = 0.0f;
+  uint32_t c = 0, n = 0;  // (2^31 at most)
   if (row < rows && e < a.experts) {
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t s = s0 + row; s < s1; s += rows) {
       const float2 v = a.part[s * a.experts + e];
       m += v.x, c += __float_as_int(v.y);
     }
   }
-  mass[threadIdx.x] = m, count[threadIdx.x] = c;
-  double q = 0.0;
-  int n = 0;
   for (int64_t s = s0 + threadIdx.x; s < s1; s += kSumThreads) {
     const float2 v = a.part_token[s];
     q += v.x, n += __float_as_int(v.y);
   }
-#pragma unroll
-  for (int d = 16; d; d >>= 1) q += __shfl_xor_sync(~0u, q, d), n += __shfl_xor_sync(~0u, n, d);
-  if (threadIdx.x % 32 == 0) squares[threadIdx.x / 32] = q, live[threadIdx.x / 32] = n;
+  sums[threadIdx.x] = make_float2(m, __int_as_float(c));
+  q = warp_sum(q), n = warp_sum(n);
+  if (lane == 0) tokens[warp] = make_float2(q, __int_as_float(n));
   __syncthreads();
-  double product = 0.0;
+  float product = 0.0f;
   if (threadIdx.x < a.experts) {
-    int64_t all = 0;
-    m = 0.0f;
-    for (int r = 0; r < rows; ++r) m += mass[r * lanes + threadIdx.x], all += count[r * lanes + threadIdx.x];
-    a.mass[(int64_t)g * a.experts + threadIdx.x] = m, a.counts[(int64_t)g * a.experts + threadIdx.x] = all;
-    product = (double)m * all;
+    m = 0.0f, c = 0;
+#pragma unroll 4
+    for (int r = 0; r < rows; ++r) {
+      const float2 v = sums[r * lanes + threadIdx.x];
+      m += v.x, c += __float_as_int(v.y);
+    }
+    a.mass[(int64_t)g * a.experts + threadIdx.x] = m, a.counts[(int64_t)g * a.experts + threadIdx.x] = c;
+    product = m * (float)c;
   }
-  double all_squares = 0.0;
-  int64_t all_live = 0;
-  if (threadIdx.x == 0)
-    for (int w = 0; w < kSumThreads / 32; ++w) all_squares += squares[w], all_live += live[w];
-  finish<kSumThreads>(a, g, product, all_squares, all_live);
+  const float2 mine = tokens[lane];
+  finish<kSumThreads>(a, g, product, mine.x, __float_as_int(mine.y));
 }
 
-template <int LPT, int VPL, typename T>
+template <int LPT, int VPL, bool SIGMOID, typename T>
 __global__ void __launch_bounds__(kThreads) tuna_balance_grad_kernel(BalanceArgs a) {
   wait_previous();
   allow_next();
   const int sub = threadIdx.x % LPT;
   constexpr int kStep = kThreads / LPT;
   const int64_t b0 = blockIdx.x * a.chunk, b1 = min(b0 + a.chunk, a.tokens);
-  float pull[VPL], pull_z = 0.0f;  // G, and dz 2 / n
-  int g = segment_of(a, b0), known = -1;
-  int64_t end = g >= 0 ? bound_of(a, g + 1) : bound_of(a, 0);
   Logits<VPL, T> next;
   int64_t t = b0 + threadIdx.x / LPT;
   next.load(a, t, sub * VPL, t < b1);
+  float pull[VPL] = {}, pull_z = 0.0f;  // G, and dz 2 / n
+  int64_t begin, end;
+  int g = segment_of(a, b0, begin, end), known = -1;
   for (int64_t tb = b0; tb < b1; tb += kStep, t += kStep) {
     float z[VPL];
     next.values(z);
@@ -306,25 +392,38 @@ __global__ void __launch_bounds__(kThreads) tuna_balance_grad_kernel(BalanceArgs
     const bool inside = t < b1 && g >= 0 && g < a.segments;
     if (inside && g != known) {
       const int64_t n = a.live[g];
-      const float by = n > 0 ? (float)((double)a.dloss[g] * a.experts / ((double)a.k * n * n)) : 0.0f;
-      pull_z = a.dz && n > 0 ? a.dz[g] * 2.0f / (float)n : 0.0f;
+      int64_t c[VPL];
 #pragma unroll
-      for (int i = 0; i < VPL; ++i) pull[i] = sub * VPL + i < a.experts ? by * (float)a.counts[(int64_t)g * a.experts + sub * VPL + i] : 0.0f;
+      for (int i = 0; i < VPL; ++i) c[i] = sub * VPL + i < a.experts ? a.counts[(int64_t)g * a.experts + sub * VPL + i] : 0;
+      const float over = n > 0 ? 1.0f / (float)n : 0.0f, by = a.dloss[g] * ((float)a.experts / a.k) * over * over;
+      pull_z = a.dz ? a.dz[g] * 2.0f * over : 0.0f;
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) pull[i] = by * (float)c[i];
       known = g;
     }
-    Token<LPT, VPL> token;
-    token.of(z, a.scoring, a.dz != nullptr);
-    float dot = 0.0f;
+    Token<LPT, VPL, SIGMOID> token;
+    token.of(z, a.dz != nullptr, true);
+    const bool part = inside && token.live;
+    const float by = part ? token.by : 0.0f;
+    uint64_t dots = 0;
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) dot = fmaf(token.p[i], inside ? pull[i] : 0.0f, dot);
-    dot = group_sum<LPT>(dot);
+    for (int i = 0; i < VPL; i += 2) dots = fma2(pair(token.x[i], token.x[i + 1]), pair(pull[i], pull[i + 1]), dots);
+    float dot, other;
+    unpair(dots, dot, other);
+    dot = group_sum<LPT>(dot + other) * by;
+    // (a token that holds +inf has an infinite z whatever moves: it gets no part of its gradient)
+    const float of_z = part && pull_z != 0.0f && !token.endless ? pull_z * token.lse : 0.0f;
     float d[VPL];
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-      float v = token.p[i] * (pull[i] - dot);
-      if (a.scoring == TUNA_MOE_SIGMOID) v *= token.rest[i];
-      if (pull_z != 0.0f && token.soft[i] != 0.0f) v = fmaf(pull_z * token.lse, token.soft[i], v);
-      d[i] = inside && token.live && z[i] != -INFINITY ? v : 0.0f;
+    for (int i = 0; i < VPL; i += 2) {
+      const uint64_t p = mul2(pair(token.x[i], token.x[i + 1]), pair(by, by));
+      if constexpr (SIGMOID) {
+        uint64_t v = mul2(mul2(p, pair(token.rest[i], token.rest[i + 1])), add2(pair(pull[i], pull[i + 1]), pair(-dot, -dot)));
+        if (a.dz) v = fma2(pair(token.s[i], token.s[i + 1]), pair(of_z * token.by_s, of_z * token.by_s), v);
+        unpair(v, d[i], d[i + 1]);
+      } else {
+        unpair(mul2(p, add2(pair(pull[i], pull[i + 1]), pair(of_z - dot, of_z - dot))), d[i], d[i + 1]);
+      }
     }
     if (t < b1) {
       T *out = reinterpret_cast<T *>(a.dlogits) + t * a.ldd + sub * VPL;
@@ -366,8 +465,10 @@ struct BalanceLaunch {
   int operator()() {
     const size_t smem = (size_t)(kThreads / 32 + 1) * a.experts * 4;
     const int64_t blocks = ceil_div(a.tokens, a.chunk);
-    if (blocks == 1) return launch(tuna_balance_kernel<LPT, VPL, true, T>, dim3(1), kThreads, smem, st, false, a);
-    if (const int rc = launch(tuna_balance_kernel<LPT, VPL, false, T>, dim3((unsigned)blocks), kThreads, smem, st, false, a)) return rc;
+    const bool sigmoid = a.scoring == TUNA_MOE_SIGMOID;
+    if (blocks == 1) return launch(sigmoid ? tuna_balance_kernel<LPT, VPL, true, true, T> : tuna_balance_kernel<LPT, VPL, true, false, T>, dim3(1), kThreads, smem, st, false, a);
+    if (const int rc = launch(sigmoid ? tuna_balance_kernel<LPT, VPL, false, true, T> : tuna_balance_kernel<LPT, VPL, false, false, T>, dim3((unsigned)blocks), kThreads, smem, st, false, a))
+      return rc;
     return launch(tuna_balance_sum_kernel, dim3((unsigned)a.segments), kSumThreads, 0, st, false, a);
   }
 };
@@ -377,7 +478,8 @@ struct BalanceGradLaunch {
   cudaStream_t st;
   template <int LPT, int VPL>
   int operator()() {
-    return launch(tuna_balance_grad_kernel<LPT, VPL, T>, dim3((unsigned)ceil_div(a.tokens, a.chunk)), kThreads, 0, st, false, a);
+    return launch(a.scoring == TUNA_MOE_SIGMOID ? tuna_balance_grad_kernel<LPT, VPL, true, T> : tuna_balance_grad_kernel<LPT, VPL, false, T>,
+                  dim3((unsigned)ceil_div(a.tokens, a.chunk)), kThreads, 0, st, false, a);
   }
 };
 

@@ -52,22 +52,14 @@ __device__ __forceinline__ float top_of(float a, float b, float c) {
   asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 // silu(g) * u of two values.  1 / (1 + 2^(-g log2 e)): the exponent's rounding makes it off by |g| 2^-23, the rest by 2^-21; from g = -88 down
 // it is 0.  (Six instructions a value: with expf and a division the results of a tile took longer than its steps.)
 __device__ __forceinline__ uint64_t swiglu2(float g0, float g1, float u0, float u1) {
   const uint64_t g = pair(g0, g1);
   float a, b, c, d;
-  unpair(mul2(g, pair(-1.4426950408889634f, -1.4426950408889634f)), a, b);
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(c) : "f"(a));
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(b));
-  unpair(add2(pair(c, d), pair(1.0f, 1.0f)), a, b);
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(c) : "f"(a));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(b));
+  unpair(mul2(g, pair(-kLog2E, -kLog2E)), a, b);
+  unpair(add2(pair(exp2_fast(a), exp2_fast(b)), pair(1.0f, 1.0f)), a, b);
+  c = reciprocal_fast(a), d = reciprocal_fast(b);
   return mul2(mul2(g, pair(c, d)), pair(u0, u1));
 }
 
@@ -940,7 +932,9 @@ int launch_product4(const Product4Args &p, cudaStream_t st) {
   }
   const int64_t rows = row_tiles(p, 128), stages = ceil_div(p.k, 256);
   const int64_t wide = rows * ceil_div(p.n, 256), narrow = rows * ceil_div(p.n, 128);
-  if (!p.swiglu && 6 * ceil_div(wide, sm_count()) < 5 * ceil_div(narrow, sm_count()))
+  // Tiles of 256 columns where they take fewer rounds.  (Of 256 and of 128, us: 1024 x 4096 x 4096, one round and two, 10.5 and 16.2; 777 x 2000 x
+  // 2896, one of either, 11.7 and 8.9; 1024 x 4736 x 4096, two of either, 16.3 and 16.5; 64 groups of 4096 x 2048 with 16 rows each, 7 and 14: 49 and 53.)
+  if (!p.swiglu && ceil_div(wide, sm_count()) < ceil_div(narrow, sm_count()))
     return p.out_f32 ? run_tiles4<256, false, float>(p, st) : run_tiles4<256, false, __nv_bfloat16>(p, st);
   // Few tiles: a cluster shares each.  (narrow: with SwiGLU too, whose tiles have 128 columns of the result)
   int parts = 4;

@@ -376,7 +376,7 @@ def test_balance_refusals():
     assert loss(dtype=2) == -1 and loss(ld=15) == -1 and loss(scoring=2) == -1 and loss(seg=2) == -1 and loss(seg=0) == -1 and loss(k=0) == -1
     assert loss(z=None) == -1 and loss(z=258) == -1 and loss(ids=None) == -1 and loss(out=None) == -1 and loss(counts=None) == -1 and loss(mass=None) == -1
     assert loss(live=None) == -1 and loss(t=-1) == -1 and loss(e=0, ld=0) == -1
-    assert loss(e=513, ld=513) == -9 and loss(k=33) == -9 and loss(seg=65537, off=256) == -9 and loss(t=1 << 31) == -9
+    assert loss(e=513, ld=513) == -9 and loss(k=33) == -9 and loss(seg=32769, off=256) == -9 and loss(t=1 << 31) == -9
     assert loss(t=1 << 20, ws=None) == -6 and loss(t=1 << 20, n=100) == -6 and loss(t=1 << 20, ws=264) == -6
 
     def grad(z=256, dtype=0, t=8, e=16, ld=16, k=2, scoring=0, seg=1, off=None, counts=256, live=256, dloss=256, out=256, ldd=16):
