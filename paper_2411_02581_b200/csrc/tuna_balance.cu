@@ -198,25 +198,13 @@ __device__ __forceinline__ T warp_sum(T v) {
   for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
   return v;
 }
-// loss and z of a segment by a whole block, whose threads bring the products of their experts; of squares and n, the first warp's lanes
-// bring parts (others nothing that counts)
-template <int THREADS>
-__device__ __forceinline__ void finish(const BalanceArgs &a, int g, float product, float squares, uint32_t n) {
-  __shared__ float sum[THREADS / 32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  product = warp_sum(product);
-  if (lane == 0) sum[warp] = product;
-  __syncthreads();
-  if (warp == 0) {
-    const float all = warp_sum(lane < THREADS / 32 ? sum[lane] : 0.0f);
-    squares = warp_sum(squares), n = warp_sum(n);
-    if (lane == 0) {
-      // (E / k / n / n in this order: n^2 may have 62 bits)
-      a.loss[g] = n ? all * ((float)a.experts / a.k) / n / n : 0.0f;
-      if (a.z) a.z[g] = n ? squares / n : 0.0f;
-      a.live[g] = n;
-    }
-  }
+// loss and z of a segment, by the first lane of a warp
+__device__ __forceinline__ void leave_loss(const BalanceArgs &a, int g, float product, float squares, uint32_t n) {
+  if ((threadIdx.x & 31) != 0) return;
+  // (E / k / n / n in this order: n^2 may have 62 bits)
+  a.loss[g] = n ? product * ((float)a.experts / a.k) / n / n : 0.0f;
+  if (a.z) a.z[g] = n ? squares / n : 0.0f;
+  a.live[g] = n;
 }
 
 // A block's tokens.  The steps do not mind the segments: what a step's tokens bring is added to the segments that they are in, and
@@ -231,6 +219,7 @@ __global__ void __launch_bounds__(kThreads) tuna_balance_kernel(BalanceArgs a) {
   __shared__ int held[kIdsHeld];
   __shared__ float warp_squares[kThreads / 32];
   __shared__ int warp_live[kThreads / 32];
+  __shared__ float products[kThreads / 32];
   wait_previous();
   allow_next();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = threadIdx.x % LPT;
@@ -289,10 +278,14 @@ __global__ void __launch_bounds__(kThreads) tuna_balance_kernel(BalanceArgs a) {
     }
     squares = lane < kThreads / 32 ? warp_squares[lane] : 0.0f, live = lane < kThreads / 32 ? warp_live[lane] : 0;
     if (ALONE) {
-      finish<kThreads>(a, g, product, squares, live);
-    } else if (warp == 0) {
+      product = warp_sum(product);
+      if (lane == 0) products[warp] = product;
+      __syncthreads();
+    }
+    if (warp == 0) {
       squares = warp_sum(squares), live = warp_sum(live);
-      if (lane == 0) a.part_token[slot] = make_float2(squares, __int_as_float(live));
+      if (ALONE) leave_loss(a, g, warp_sum(lane < kThreads / 32 ? products[lane] : 0.0f), squares, live);
+      else if (lane == 0) a.part_token[slot] = make_float2(squares, __int_as_float(live));
     }
     __syncthreads();
     squares = 0.0f, live = 0;
@@ -327,11 +320,12 @@ __global__ void __launch_bounds__(kThreads) tuna_balance_kernel(BalanceArgs a) {
   }
 }
 
-// A block a segment: the parts of the blocks that met it, every 8th (or 16th, 32nd ...) of them by one row of threads, then the
+// A block a segment: the parts of the blocks that met it, every 2nd (or 16th, 32nd ...) of them by one row of threads, then the
 // rows in order.
 __global__ void __launch_bounds__(kSumThreads) tuna_balance_sum_kernel(BalanceArgs a) {
   __shared__ float2 sums[kSumThreads];
   __shared__ float2 tokens[kSumThreads / 32];
+  __shared__ float products[kSumThreads / 32];
   wait_previous();
   allow_next();
   const int g = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -367,8 +361,70 @@ __global__ void __launch_bounds__(kSumThreads) tuna_balance_sum_kernel(BalanceAr
     a.mass[(int64_t)g * a.experts + threadIdx.x] = m, a.counts[(int64_t)g * a.experts + threadIdx.x] = c;
     product = m * (float)c;
   }
-  const float2 mine = tokens[lane];
-  finish<kSumThreads>(a, g, product, mine.x, __float_as_int(mine.y));
+  product = warp_sum(product);
+  if (lane == 0) products[warp] = product;
+  __syncthreads();
+  if (warp == 0) leave_loss(a, g, warp_sum(products[lane]), warp_sum(tokens[lane].x), warp_sum((uint32_t)__float_as_int(tokens[lane].y)));
+}
+
+// A cluster a segment, a block its share of the experts: the parts of the blocks that met the segment, every 16th (or 32nd, 64th ...)
+// of them by one row of threads, then the rows in order.  The first block joins the shares of the loss.
+__global__ void __launch_bounds__(kSumThreads) tuna_balance_sum_wide_kernel(BalanceArgs a) {
+  __shared__ float2 sums[kSumThreads];
+  __shared__ float2 tokens[kSumThreads / 32];
+  __shared__ float products[kSumThreads / 32];
+  __shared__ __align__(16) float share[4];
+  wait_previous();
+  allow_next();
+  const int blocks = (int)cluster_size(), rank = (int)cluster_rank();
+  const int g = blockIdx.x / blocks, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t begin = bound_of(a, g), end = bound_of(a, g + 1);
+  const int64_t s0 = begin / a.chunk + g, s1 = end > begin ? (end - 1) / a.chunk + g + 1 : s0;
+  const int mine = (a.experts + blocks - 1) / blocks, e0 = rank * mine, count = max(0, min(mine, a.experts - e0));
+  int lanes = 4;
+  while (lanes < mine) lanes *= 2;  // (512 at most)
+  const int rows = kSumThreads / lanes, row = threadIdx.x / lanes, e = threadIdx.x & (lanes - 1);
+  float m = 0.0f, q = 0.0f;
+  uint32_t c = 0, n = 0;  // (2^31 at most)
+  if (e < count) {
+#pragma unroll 8
+    for (int64_t s = s0 + row; s < s1; s += rows) {
+      const float2 v = a.part[s * a.experts + e0 + e];
+      m += v.x, c += __float_as_int(v.y);
+    }
+  }
+  if (rank == 0)
+    for (int64_t s = s0 + threadIdx.x; s < s1; s += kSumThreads) {
+      const float2 v = a.part_token[s];
+      q += v.x, n += __float_as_int(v.y);
+    }
+  sums[threadIdx.x] = make_float2(m, __int_as_float(c));
+  q = warp_sum(q), n = warp_sum(n);
+  if (lane == 0) tokens[warp] = make_float2(q, __int_as_float(n));
+  __syncthreads();
+  float product = 0.0f;
+  if (threadIdx.x < count) {
+    m = 0.0f, c = 0;
+#pragma unroll 8
+    for (int r = 0; r < rows; ++r) {
+      const float2 v = sums[r * lanes + threadIdx.x];
+      m += v.x, c += __float_as_int(v.y);
+    }
+    a.mass[(int64_t)g * a.experts + e0 + threadIdx.x] = m, a.counts[(int64_t)g * a.experts + e0 + threadIdx.x] = c;
+    product = m * (float)c;
+  }
+  product = warp_sum(product);
+  if (lane == 0) products[warp] = product;
+  __syncthreads();
+  if (warp == 0) product = warp_sum(lane < kSumThreads / 32 ? products[lane] : 0.0f);
+  if (threadIdx.x == 0) share[0] = product;
+  cluster_meet();
+  if (rank == 0 && warp == 0) {
+    product = lane < blocks ? load_from_block(smem_u32(share), lane).x : 0.0f;
+    const float2 v = lane < kSumThreads / 32 ? tokens[lane] : make_float2(0.0f, 0.0f);
+    leave_loss(a, g, warp_sum(product), warp_sum(v.x), warp_sum((uint32_t)__float_as_int(v.y)));
+  }
+  cluster_meet();  // no block leaves while its share is read
 }
 
 template <int LPT, int VPL, bool SIGMOID, typename T>
@@ -451,7 +507,8 @@ struct Rows {  // tokens that a block takes at a time
 };
 
 // Tokens of a block: one step where that leaves four blocks a multiprocessor or fewer, as many as keep it at that otherwise; all of
-// them where one block is done with them before a second launch would be.
+// them where one block is done with them before a second launch would be.  (65536 x 64 with gradient, inputs from memory: four blocks a
+// multiprocessor 20.8 us, six 24.3, two 24.6; 20011 x 160 40.3, 41.6, 41.0.)
 int64_t chunk_of(int64_t tokens, int experts) {
   const int64_t step = by_experts(experts, Rows{}), steps = ceil_div(tokens, step);
   return std::max<int64_t>(1, steps <= 4 ? steps : ceil_div(steps, 592)) * step;
@@ -469,6 +526,9 @@ struct BalanceLaunch {
     if (blocks == 1) return launch(sigmoid ? tuna_balance_kernel<LPT, VPL, true, true, T> : tuna_balance_kernel<LPT, VPL, true, false, T>, dim3(1), kThreads, smem, st, false, a);
     if (const int rc = launch(sigmoid ? tuna_balance_kernel<LPT, VPL, false, true, T> : tuna_balance_kernel<LPT, VPL, false, false, T>, dim3((unsigned)blocks), kThreads, smem, st, false, a))
       return rc;
+    // Eight blocks a segment where it has many parts of many experts.  (Eight and one, us, the blocks' kernel with it: one segment of 8192 x 256 12.4
+    // and 18.7, four of 16384 x 256 18.4 and 23.1; one of 8192 x 64 8.3 and 8.5; eight of 65536 x 64 13.3 and 11.6.)
+    if (blocks / a.segments * a.experts > 16384) return launch_cluster(tuna_balance_sum_wide_kernel, dim3((unsigned)(a.segments * 8)), 8, kSumThreads, 0, st, false, a);
     return launch(tuna_balance_sum_kernel, dim3((unsigned)a.segments), kSumThreads, 0, st, false, a);
   }
 };
