@@ -427,8 +427,9 @@ __global__ void __launch_bounds__(kSumThreads) tuna_balance_sum_wide_kernel(Bala
   cluster_meet();  // no block leaves while its share is read
 }
 
+// (Four blocks a multiprocessor, at a few spilled registers with sigmoids: 20011 x 160 14.9 us, with two 17.7.)
 template <int LPT, int VPL, bool SIGMOID, typename T>
-__global__ void __launch_bounds__(kThreads) tuna_balance_grad_kernel(BalanceArgs a) {
+__global__ void __launch_bounds__(kThreads, VPL > 8 ? 2 : 4) tuna_balance_grad_kernel(BalanceArgs a) {
   wait_previous();
   allow_next();
   const int sub = threadIdx.x % LPT;

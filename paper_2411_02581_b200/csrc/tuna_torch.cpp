@@ -421,16 +421,18 @@ int64_t matrix4(const Tensor &t, const char *name) {
   return rows > 1 ? t.stride(0) : std::max<int64_t>(cols, 1);
 }
 // The same for a product: rows on 16-byte boundaries, the tensor itself or a copy.
-Tensor operand4(const Tensor &q, const char *name, int64_t &ld) {
+Tensor operand4(const Tensor &q, const char *name, int64_t &ld, void *stream) {
   ld = matrix4(q, name);
   if (q.size(0) <= 1) ld = (q.size(1) + 15) / 16 * 16;  // the pitch of a single row is free
   if (ld % 16 == 0 && (uintptr_t)q.data_ptr() % 16 == 0) {
     ld = std::max<int64_t>(ld, 16);
     return q;
   }
+  const int64_t pitch = ld;
   ld = std::max<int64_t>((q.size(1) + 15) / 16 * 16, 16);
-  Tensor p = make({q.size(0), ld}, at::kByte, q).zero_();
-  p.narrow(1, 0, q.size(1)).copy_(q.view(at::kByte));
+  Tensor p = make({q.size(0), ld}, at::kByte, q);  // (what stands behind the rows is not read)
+  if (q.numel() && cudaMemcpy2DAsync(p.data_ptr(), ld, q.data_ptr(), pitch, q.size(1), q.size(0), cudaMemcpyDeviceToDevice, (cudaStream_t)stream) != cudaSuccess)
+    throw std::runtime_error("cudaMemcpy2DAsync failed");
   return p;
 }
 
@@ -483,16 +485,16 @@ PyObject *fp4_matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {
     const int out = small(a[5]);
     const Place place(a[6], left);
     int64_t lda = 0, ldb = 0, cols, kb;
-    const Tensor x = operand4(left, "a", lda);
+    const Tensor x = operand4(left, "a", lda, place.stream());
     const int64_t m = left.size(0), k = 2 * left.size(1), runs = (k + 127) / 128;
     Tensor w;
     if (offsets) {
       if (right.dim() != 3 || !right.is_contiguous() || right.size(0) != groups) refuse("b: contiguous matrices [%lld, n, k / 2] go with these offsets", (long long)groups);
       cols = right.size(1), kb = 2 * right.size(2);
-      w = operand4(right.view({groups * cols, right.size(2)}), "b", ldb);
+      w = operand4(right.view({groups * cols, right.size(2)}), "b", ldb, place.stream());
       dense(sb, "b_scale", kPower, {groups, (cols + 127) / 128, runs, 32, 4, 4}, left);
     } else {
-      w = operand4(right, "b", ldb);
+      w = operand4(right, "b", ldb, place.stream());
       cols = right.size(0), kb = 2 * right.size(1);
       dense(sb, "b_scale", kPower, {(cols + 127) / 128, runs, 32, 4, 4}, left);
     }
