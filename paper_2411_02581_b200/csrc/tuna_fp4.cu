@@ -68,8 +68,8 @@ __device__ __forceinline__ uint64_t swiglu2(float g0, float g1, float u0, float 
 // Bound by memory: two bytes (bf16) read and 17/32 written a value.  A warp takes 256 columns of four rows that are 32
 // apart, 8 columns a lane, so that a lane loads 16 bytes of bf16 a row, and the four rows' scales of four blocks are 16 bytes in a
 // row.  A block of threads takes eight such sets of rows, a quarter of a tile, and `strips` times 256 columns of them.  Rows on
-// 16-byte boundaries come by asynchronous copies, several strips ahead, each lane's to a place of its own in shared memory (so
-// that nobody waits for anybody); others by loads of what width they allow, one strip ahead.
+// 16-byte boundaries come by asynchronous copies, several strips ahead, to a place of the warp's own in shared memory (so that
+// no warp waits for another); others by loads of what width they allow, one strip ahead.
 template <typename T>
 __host__ __device__ constexpr int ahead() { return sizeof(T) == 2 ? 3 : 2; }  // strips on their way and under way: 48 and 64 KB a block of threads
 struct Quant4Args {
@@ -140,8 +140,8 @@ __device__ __forceinline__ void quantize_four(const Eight<T> (&x)[4], uint32_t (
 }
 template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(256) tuna_quantize4_rows_kernel(Quant4Args a) {
-  extern __shared__ __align__(16) uint4 ring[];  // [kAhead][4][kWords][256], a lane's pieces in its own column
-  constexpr int kAhead = ahead<T>(), kWords = Eight<T>::kWords;
+  extern __shared__ __align__(16) uint4 ring[];  // [kAhead][4][warps][a row's 256 values]
+  constexpr int kAhead = ahead<T>(), kWords = Eight<T>::kWords, kPiece = 8 / kWords;  // (16 bytes)
   wait_previous();
   allow_next();
   const int lane = threadIdx.x & 31, l = (blockIdx.x & 3) * 8 + (threadIdx.x >> 5);
@@ -158,27 +158,28 @@ __global__ void __launch_bounds__(256) tuna_quantize4_rows_kernel(Quant4Args a) 
   for (int i = 0; i < 4; ++i) {
     const int64_t r = row0 + l + 32 * min(i, rows - 1);  // (a row that is not there: the last one again, which nobody stores)
     const int64_t at = a.gather ? min(max(__ldg(a.gather + r), (int64_t)0), a.in_rows - 1) : r;
-    from[i] = reinterpret_cast<const T *>(a.x) + at * a.ldx + c0 + lane * 8;
+    from[i] = reinterpret_cast<const T *>(a.x) + at * a.ldx + c0 + lane * (ALIGNED ? kPiece : 8);
     to[i] = reinterpret_cast<uint32_t *>(a.q + r * a.ldq + c0 / 2) + lane;
   }
   uint32_t *scale = reinterpret_cast<uint32_t *>(a.scale + (slot * a.runs + (c0 >> 7) + (lane >> 4)) * kScaleTile + l * 16) + (lane & 3);
   Eight<T> x[4];
   auto fetch = [&](int ahead, int stage) {  // `ahead`: strips from the present one
-    const int left = a.cols - c0 - ahead * 256 - lane * 8;
     if (!ALIGNED) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i].load_any(from[i] + ahead * 256, left);
+      for (int i = 0; i < 4; ++i) x[i].load_any(from[i] + ahead * 256, a.cols - c0 - ahead * 256 - lane * 8);
       return;
     }
     if (c0 + ahead * 256 < last) {
-      const uint32_t at = smem_u32(ring + stage * 4 * kWords * 256 + threadIdx.x);
+      // (a warp's 32 pieces are next to each other, so that whole sectors are asked for)
+      const uint32_t at = smem_u32(ring + (stage * 4 * 8 + (threadIdx.x >> 5)) * 32 * kWords + lane);
 #pragma unroll
       for (int w = 0; w < kWords; ++w) {
-        const int bytes = max(0, min(16, (left - w * (8 / kWords)) * (int)sizeof(T)));  // (the rest of the 16 is zero)
+        const int from_here = a.cols - c0 - ahead * 256 - (w * 32 + lane) * kPiece;
+        const int bytes = max(0, min(16, from_here * (int)sizeof(T)));  // (the rest of the 16 is zero)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + (i * kWords + w) * 4096),
-                       "l"(from[i] + (bytes ? ahead * 256 + w * (8 / kWords) : -lane * 8)), "r"(bytes)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + (i * 8 * 32 * kWords + w * 32) * 16),
+                       "l"(from[i] + (bytes ? ahead * 256 + w * 32 * kPiece : -lane * kPiece)), "r"(bytes)
                        : "memory");
       }
     }
@@ -193,12 +194,14 @@ __global__ void __launch_bounds__(256) tuna_quantize4_rows_kernel(Quant4Args a) 
   int stage = 0;
   for (; c0 < last; c0 += 256) {
     if (ALIGNED) {
+      if (kWords > 1) __syncwarp();  // (a lane reads what two others brought: all have read the strip whose place is taken)
       fetch(kAhead - 1, stage == 0 ? kAhead - 1 : stage - 1);
       asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+      if (kWords > 1) __syncwarp();
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int w = 0; w < kWords; ++w) x[i].w[w] = ring[((stage * 4 + i) * kWords + w) * 256 + threadIdx.x];
+        for (int w = 0; w < kWords; ++w) x[i].w[w] = ring[((stage * 4 + i) * 8 + (threadIdx.x >> 5)) * 32 * kWords + lane * kWords + w];
       if (++stage == kAhead) stage = 0;
     }
     uint32_t q[4], scales;
@@ -286,32 +289,47 @@ __global__ void __launch_bounds__(256) tuna_quantize4_columns_kernel(Quant4Args 
 #pragma unroll
     for (int q = 0; q < Eight<T>::kWords; ++q) *reinterpret_cast<uint4 *>(tile + (mine + i * 16) * kPitch + c + q * (8 / Eight<T>::kWords)) = x[i].w[q];
   __syncthreads();
-  const int two = (tid & 63) * 2, quarter = tid >> 6;  // columns two, two + 1; rows quarter * 32 ..
-  float t[2][32];
-  uint32_t top[2] = {0, 0};
+  const int quarter = tid >> 6;  // rows quarter * 32 .. of two columns: next to each other in bf16, whose words they share, else 64 apart
+  auto column = [&](int e) { return sizeof(T) == 2 ? (tid & 63) * 2 + e : (tid & 63) + 64 * e; };
+  uint32_t t[2][sizeof(T) == 2 ? 1 : 32], pairs[sizeof(T) == 2 ? 32 : 1], top[2] = {0, 0};
 #pragma unroll
   for (int r = 0; r < 32; ++r) {
-    const T *p = tile + (quarter * 32 + r) * kPitch + two;
+    const T *p = tile + (quarter * 32 + r) * kPitch;
     if constexpr (sizeof(T) == 2) {
-      const uint32_t u = *reinterpret_cast<const uint32_t *>(p);
-      t[0][r] = __uint_as_float(u << 16), t[1][r] = __uint_as_float(u & 0xffff0000u);
+      pairs[r] = *reinterpret_cast<const uint32_t *>(p + column(0));
+      top[0] = __vmaxu2(top[0], pairs[r] & 0x7fff7fffu);
     } else {
-      const float2 u = *reinterpret_cast<const float2 *>(p);
-      t[0][r] = u.x, t[1][r] = u.y;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) t[e][r] = __float_as_uint(p[column(e)]), top[e] = max(top[e], t[e][r] & 0x7fffffffu);
     }
-    top[0] = max(top[0], abs_bits(t[0][r])), top[1] = max(top[1], abs_bits(t[1][r]));
   }
+  if (sizeof(T) == 2) top[1] = top[0] & 0xffff0000u, top[0] <<= 16;
   __syncthreads();  // the tile has been read: the values go out by way of its place, in whole sectors
   uint4 *out = reinterpret_cast<uint4 *>(tile_raw);  // [128 columns][4 quarters], their pieces turned by column
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const uint32_t byte = fp4_scale(top[e]);
-    const float by = fp4_inverse(byte);
-    const int col = two + e;
+    const uint64_t by = pair(fp4_inverse(byte), fp4_inverse(byte));
+    const int col = column(e);
     scales[(col & 31) * 16 + (col >> 5) * 4 + quarter] = (uint8_t)byte;
+    uint32_t q[4];
 #pragma unroll
-    for (int r = 0; r < 32; ++r) t[e][r] *= by;
-    out[col * 4 + (quarter ^ (col >> 1 & 3))] = make_uint4(fp4_eight(t[e]), fp4_eight(t[e] + 8), fp4_eight(t[e] + 16), fp4_eight(t[e] + 24));
+    for (int w = 0; w < 4; ++w) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) {
+        float at[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int r = w * 8 + j + h;
+          if constexpr (sizeof(T) == 2) at[h] = __uint_as_float(e ? pairs[r] & 0xffff0000u : pairs[r] << 16);
+          else at[h] = __uint_as_float(t[e][r]);
+        }
+        unpair(mul2(pair(at[0], at[1]), by), v[j], v[j + 1]);
+      }
+      q[w] = fp4_eight(v);
+    }
+    out[col * 4 + (quarter ^ (col >> 1 & 3))] = make_uint4(q[0], q[1], q[2], q[3]);
   }
   __syncthreads();
 #pragma unroll
@@ -323,8 +341,9 @@ __global__ void __launch_bounds__(256) tuna_quantize4_columns_kernel(Quant4Args 
   if (tid < 32) reinterpret_cast<uint4 *>(a.scale + ((int64_t)col_tile * a.runs + run) * kScaleTile)[tid] = reinterpret_cast<const uint4 *>(scales)[tid];
 }
 
-// The values that 4-bit rows stand for, in the quantisation's arrangement.
-template <typename T>
+// The values that 4-bit rows stand for, in the quantisation's arrangement.  ALIGNED: words of q, and eight values of the
+// result, can be taken whole.
+template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(256) tuna_dequantize4_kernel(Quant4Args a, T *out, int64_t ldo) {
   wait_previous();
   allow_next();
@@ -333,36 +352,56 @@ __global__ void __launch_bounds__(256) tuna_dequantize4_kernel(Quant4Args a, T *
   int64_t row0, end;
   slot_rows(a.offsets, a.groups, a.rows, slot, row0, end);
   if (row0 + l >= end) return;
+  const int rows = (int)min((end - row0 - l + 31) / 32, (int64_t)4);
   int c = (int)blockIdx.y * a.strips * 256 + lane * 8;
-  for (int n = 0; n < a.strips && c < a.cols; ++n, c += 256) {
-    const uint4 s = __ldg(reinterpret_cast<const uint4 *>(a.scale + (slot * a.runs + (c >> 7)) * kScaleTile + l * 16));
+  const int last = min(a.cols, (int)(blockIdx.y + 1) * a.strips * 256);
+  const uint8_t *from[4];
+  T *to[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t r = row0 + l + 32 * min(i, rows - 1);  // (a row that is not there: the last one again, written only once)
+    from[i] = a.q + r * a.ldq + c / 2, to[i] = out + r * ldo + c;
+  }
+  const uint4 *scale = reinterpret_cast<const uint4 *>(a.scale + (slot * a.runs + (c >> 7)) * kScaleTile + l * 16);
+  for (; c < last; c += 256) {
+    const uint4 s = __ldg(scale);
     const uint32_t words[4] = {s.x, s.y, s.z, s.w};
+    const bool whole = ALIGNED && c + 8 <= a.cols;
     uint32_t q[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int64_t r = row0 + l + 32 * i;
-      const uint8_t *p = a.q + r * a.ldq + c / 2;
-      q[i] = 0;
-      if (r >= end) continue;
-      if (c + 8 <= a.cols && ((uintptr_t)p & 3) == 0) {
-        q[i] = __ldg(reinterpret_cast<const uint32_t *>(p));
+      if (whole || (c + 8 <= a.cols && ((uintptr_t)from[i] & 3) == 0)) {
+        q[i] = __ldg(reinterpret_cast<const uint32_t *>(from[i]));
       } else {
+        q[i] = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (c + 2 * j < a.cols) q[i] |= (uint32_t)p[j] << (8 * j);
+          if (c + 2 * j < a.cols) q[i] |= (uint32_t)from[i][j] << (8 * j);
       }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int64_t r = row0 + l + 32 * i;
-      if (r >= end) continue;
-      const float by = fp4_power((words[i] >> (lane & 12) * 2) & 255);
+      if (i >= rows) break;
+      const float by = fp4_power(__byte_perm(words[i], 0, 0x4440 | (lane >> 2 & 3)));
       float v[8];
       fp4_values(q[i], v);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] *= by;
-      store_any(out + r * ldo + c, v, a.cols - c);
+      for (int j = 0; j < 8; j += 2) unpair(mul2(pair(v[j], v[j + 1]), pair(by, by)), v[j], v[j + 1]);
+      if constexpr (sizeof(T) == 4) {
+        if (whole) {
+          uint32_t u[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(v[j]);
+          store32(to[i], u);
+          continue;
+        }
+      }
+      if (whole) store_row(to[i], v);
+      else store_any(to[i], v, a.cols - c);
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) from[i] += 128, to[i] += 256;
+    scale += 2 * kScaleTile / 16;
   }
 }
 
@@ -1029,10 +1068,12 @@ int tuna_fp4_dequantize(const void *q, int64_t ldq, const void *scale, int64_t r
   Quant4Args a = {};
   a.rows = rows, a.cols = cols, a.groups = groups, a.offsets = offsets, a.q = (uint8_t *)q, a.ldq = ldq, a.scale = (uint8_t *)scale;
   a.runs = (int)ceil_div(cols, 128);
-  const dim3 grid = strips_grid(fp4_slots(rows, groups), cols, 16, a.strips);
+  const dim3 grid = strips_grid(fp4_slots(rows, groups), cols, 8, a.strips);
   cudaStream_t st = (cudaStream_t)stream;
-  return out_dtype == TUNA_DTYPE_F32 ? launch(tuna_dequantize4_kernel<float>, grid, 256, 0, st, false, a, (float *)out, ldo)
-                                     : launch(tuna_dequantize4_kernel<__nv_bfloat16>, grid, 256, 0, st, false, a, (__nv_bfloat16 *)out, ldo);
+  const bool whole = aligned(q, 4) && ldq % 4 == 0 && aligned(out, 8 * size) && ldo % 8 == 0;
+  if (out_dtype == TUNA_DTYPE_F32)
+    return launch(whole ? tuna_dequantize4_kernel<float, true> : tuna_dequantize4_kernel<float, false>, grid, 256, 0, st, false, a, (float *)out, ldo);
+  return launch(whole ? tuna_dequantize4_kernel<__nv_bfloat16, true> : tuna_dequantize4_kernel<__nv_bfloat16, false>, grid, 256, 0, st, false, a, (__nv_bfloat16 *)out, ldo);
 }
 
 int tuna_fp4_matmul(const void *a, const void *a_scale, int64_t m, int64_t lda, const void *b, const void *b_scale, int n, int64_t ldb, int k, int groups,
