@@ -960,12 +960,12 @@ size_t dtype_size(int dtype) { return dtype == TUNA_DTYPE_F32 ? 4 : dtype == TUN
 }  // namespace
 
 int launch_product4(const Product4Args &p, cudaStream_t st) {
-  // Pairs of blocks where they have two rounds of tiles or more, and groups three tiles of rows on average.  (Pairs and blocks alone,
-  // us: 8192 x 4096 x 4096 52.9 and 62.5, 8192^3 180 and 210, 3000^3 19.5 and 20.8; with less than two rounds 2048 x 4096 x 4096 18.4 and 18.2,
-  // 1024 x 4096 x 4096 11.8 and 11.2.  64 groups of 4096 x 2048, of sizes that differ by half, rows of a group 256: 109 and 102, 512: 175 and 170;
-  // of nearly equal sizes 512: 155 and 165, 1024: 268 and 294.)
+  // Pairs of blocks where they have six rounds of tiles or more, and groups four tiles of rows on average.  (Pairs and blocks alone, us: 8192 x 8192 x
+  // 4096 101.6 and 105.7, 8192 x 4096 x 2048 33.1 and 34.2, 16384 x 4096 x 512 28.7 and 29.6; with fewer rounds 4096 x 4096 x 2048 20.4 and 19.8, 3000^3 19.6
+  // and 17.7.  64 experts of 4096 x 2048, both products and what is around them, rows of an expert 512: 561 and 524, 1024: 964 and 961, 1536: 1406
+  // and 1430.)
   const int64_t pairs = std::max(sm_count() / 2, 1), tiles = ceil_div(p.m, 256) * ceil_div(p.n, p.swiglu ? 128 : 256);
-  if (tiles >= 2 * pairs && (!p.offsets || p.m >= 768 * (int64_t)p.groups)) {
+  if (tiles >= 6 * pairs && (!p.offsets || p.m >= 1024 * (int64_t)p.groups)) {
     if (p.swiglu) return run_tiles4<256, true, uint8_t, kPair>(p, st);
     return p.out_f32 ? run_tiles4<256, false, float, kPair>(p, st) : run_tiles4<256, false, __nv_bfloat16, kPair>(p, st);
   }

@@ -171,7 +171,7 @@ def test_quantize_in_groups(sizes):
 
 PRODUCTS = [(1, 1, 2), (1, 128, 128), (1, 4096, 512), (2, 100, 300), (17, 640, 2064), (64, 256, 128), (65, 1000, 1040), (128, 256, 4096),
             (129, 257, 130), (300, 2000, 272), (1000, 96, 1024), (2500, 2304, 256), (20000, 517, 144), (0, 64, 64), (5, 7, 0), (3, 130, 2895),
-            (513, 4000, 2894), (700, 5000, 66), (2049, 1025, 4096)]
+            (513, 4000, 2894), (700, 5000, 66), (2049, 1025, 4096), (8201, 3585, 290), (57000, 517, 130)]
 
 
 @pytest.mark.gpu
@@ -211,8 +211,8 @@ def grouped(sizes, n, k, first=0, spare=9):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("n,k", [(256, 512), (300, 144), (2048, 1024), (2400, 130)])
-@pytest.mark.parametrize("sizes", GROUPS[:6] + [[700, 0, 513, 40], [1500, 0, 2561, 700, 1]])
+@pytest.mark.parametrize("n,k", [(256, 512), (300, 144), (2048, 1024), (2800, 130)])
+@pytest.mark.parametrize("sizes", GROUPS[:6] + [[700, 0, 513, 40], [1500, 0, 2561, 700, 1], [5000, 3000, 2600]])
 def test_grouped_product(n, k, sizes):
     from paper_2411_02581_b200 import moe
     a, offsets, bounds, qb, sb = grouped(sizes, n, k, first=3)
