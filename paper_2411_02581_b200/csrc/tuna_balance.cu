@@ -508,11 +508,11 @@ struct Rows {  // tokens that a block takes at a time
 };
 
 // Tokens of a block: one step where that leaves four blocks a multiprocessor or fewer, as many as keep it at that otherwise; all of
-// them where one block is done with them before a second launch would be.  (65536 x 64 with gradient, inputs from memory: four blocks a
+// them where one block is done with them before a second launch would be (a segment's end costs it 1.5 us).  (65536 x 64 with gradient, inputs from memory: four blocks a
 // multiprocessor 20.8 us, six 24.3, two 24.6; 20011 x 160 40.3, 41.6, 41.0.)
-int64_t chunk_of(int64_t tokens, int experts) {
+int64_t chunk_of(int64_t tokens, int experts, int segments) {
   const int64_t step = by_experts(experts, Rows{}), steps = ceil_div(tokens, step);
-  return std::max<int64_t>(1, steps <= 4 ? steps : ceil_div(steps, 592)) * step;
+  return std::max<int64_t>(1, steps <= 4 && segments <= 8 ? steps : ceil_div(steps, 592)) * step;
 }
 
 template <typename T>
@@ -569,7 +569,7 @@ int tuna_moe_balance_workspace_bytes(int64_t tokens, int experts, int segments, 
   if (const int rc = check_balance(tokens, experts, 1, segments)) return rc;
   *bytes = 0;
   BalanceArgs a = {};
-  a.tokens = tokens, a.experts = experts, a.segments = segments, a.chunk = chunk_of(tokens, experts);
+  a.tokens = tokens, a.experts = experts, a.segments = segments, a.chunk = chunk_of(tokens, experts, segments);
   if (tokens <= a.chunk) return TUNA_OK;
   Carve c(nullptr);
   carve(c, a);
@@ -596,7 +596,7 @@ int tuna_moe_balance(const void *logits, int dtype, int64_t tokens, int experts,
   if (!logits || !ids || !aligned(logits, size) || !aligned(ids, 4)) return TUNA_ERR_INVALID_ARG;
   BalanceArgs a = {};
   a.logits = logits, a.ids = ids, a.offsets = offsets, a.tokens = tokens, a.ld = ld, a.experts = experts, a.k = k, a.scoring = scoring;
-  a.segments = segments, a.chunk = chunk_of(tokens, experts);
+  a.segments = segments, a.chunk = chunk_of(tokens, experts, segments);
   a.loss = loss, a.z = z, a.counts = counts, a.mass = mass, a.live = live;
   if (tokens > a.chunk) {
     Carve c(workspace);
@@ -617,7 +617,7 @@ int tuna_moe_balance_backward(const void *logits, int dtype, int64_t tokens, int
   if (!logits || !counts || !live || !dloss || !dlogits || !aligned(logits, size) || !aligned(dlogits, size)) return TUNA_ERR_INVALID_ARG;
   BalanceArgs a = {};
   a.logits = logits, a.offsets = offsets, a.tokens = tokens, a.ld = ld, a.ldd = ldd, a.experts = experts, a.k = k, a.scoring = scoring;
-  a.segments = segments, a.chunk = chunk_of(tokens, experts);
+  a.segments = segments, a.chunk = chunk_of(tokens, experts, segments);
   a.counts = (int64_t *)counts, a.live = (int64_t *)live, a.dloss = dloss, a.dz = dz, a.dlogits = dlogits;
   cudaStream_t st = (cudaStream_t)stream;
   return dtype == TUNA_DTYPE_F32 ? by_experts(experts, BalanceGradLaunch<float>{a, st}) : by_experts(experts, BalanceGradLaunch<__nv_bfloat16>{a, st});

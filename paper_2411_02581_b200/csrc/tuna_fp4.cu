@@ -450,6 +450,9 @@ struct Shape4 {
   static_assert(kAccs * BN + kStages * kScaleCols <= 512);
   static_assert(kStageBytes % 1024 == 0);
   static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kOutBytes + sizeof(Groups4) + 256;
+  // One block a multiprocessor: a launch that begins early takes its tensor memory before it waits for the one before it, which must
+  // not be without its own then.
+  static_assert(kSmem > 116 * 1024 && kSmem <= 227 * 1024);
 };
 
 // 512 bytes of scales to 4 columns of tensor memory, once for each quarter of the lanes; of a pair, in both of its blocks

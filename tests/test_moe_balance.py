@@ -85,7 +85,7 @@ def cut_at(t, segments, seed=1):
 
 
 SIZES = [(1, 1, 1, 1), (1, 8, 2, 1), (2, 3, 3, 2), (63, 60, 4, 5), (500, 8, 2, 1), (257, 33, 5, 4), (1000, 64, 2, 8), (5003, 160, 6, 37), (20000, 64, 8, 3),
-         (700, 128, 4, 700), (333, 256, 8, 2), (90, 300, 10, 3), (40, 512, 32, 4), (65, 511, 1, 1), (30011, 9, 2, 1)]
+         (700, 128, 4, 700), (333, 256, 8, 2), (90, 300, 10, 3), (40, 512, 32, 4), (65, 511, 1, 1), (30011, 9, 2, 1), (100, 64, 2, 9), (100, 64, 2, 8), (50, 16, 2, 3000), (9000, 24, 2, 4000), (8200, 256, 4, 2)]
 
 
 @pytest.mark.gpu
