@@ -220,6 +220,28 @@ __global__ void __launch_bounds__(256) tuna_quantize4_rows_kernel(Quant4Args a) 
   }
 }
 
+// A warp's 256 columns of a row, from c on (a lane's), `have` of which are read: to the row's values and to its place in a tile's scales.
+template <typename T>
+__device__ __forceinline__ void quantize_piece(const T *row, int have, int c, int cols, uint8_t *q, uint8_t *tile, int at, int runs) {
+  const int lane = threadIdx.x & 31, run = c >> 7;
+  Eight<T> x;
+  x.load_any(row + c, have - c);
+  uint32_t amax = Eight<T>::top_bits(x.top(0));
+  amax = max(amax, __shfl_xor_sync(~0u, amax, 1));
+  amax = max(amax, __shfl_xor_sync(~0u, amax, 2));
+  const uint32_t byte = fp4_scale(amax);
+  const float by = fp4_inverse(byte);
+  float v[8];
+  x.values(v);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] *= by;
+  if (c < (cols + 31) / 32 * 32) *reinterpret_cast<uint32_t *>(q + c / 2) = fp4_eight(v);
+  uint32_t word = byte << (lane & 12) * 2;
+  word |= __shfl_xor_sync(~0u, word, 4);
+  word |= __shfl_xor_sync(~0u, word, 8);
+  if ((lane & 15) == 0 && run < runs) *reinterpret_cast<uint32_t *>(tile + run * kScaleTile + (at & 31) * 16 + (at >> 5) * 4) = word;
+}
+
 // The same for a few rows an expert, whose tiles would be nearly empty: a block takes 2048 columns of one row, a warp 256 of them.
 template <typename T>
 __global__ void __launch_bounds__(256) tuna_quantize4_few_kernel(Quant4Args a) {
@@ -240,24 +262,44 @@ __global__ void __launch_bounds__(256) tuna_quantize4_few_kernel(Quant4Args a) {
   const int64_t begin = __shfl_sync(~0u, first, 31 - __clz(fine));
   if (r >= cut(g + 1)) return;
   const bool there = from >= 0 && from < a.in_rows;
-  Eight<T> x;
-  x.load_any(reinterpret_cast<const T *>(a.x) + (there ? from : 0) * a.ldx + c, there ? a.cols - c : 0);
-  uint32_t amax = Eight<T>::top_bits(x.top(0));
-  amax = max(amax, __shfl_xor_sync(~0u, amax, 1));
-  amax = max(amax, __shfl_xor_sync(~0u, amax, 2));
-  const uint32_t byte = fp4_scale(amax);
-  const float by = fp4_inverse(byte);
-  float v[8];
-  x.values(v);
-#pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] *= by;
-  if (c < (a.cols + 31) / 32 * 32) *reinterpret_cast<uint32_t *>(a.q + r * a.ldq + c / 2) = fp4_eight(v);
-  uint32_t word = byte << (lane & 12) * 2;
-  word |= __shfl_xor_sync(~0u, word, 4);
-  word |= __shfl_xor_sync(~0u, word, 8);
-  const int64_t slot = begin / 128 + g + (r - begin) / 128;
-  const int at = (int)((r - begin) % 128), run = c >> 7;
-  if ((lane & 15) == 0 && run < a.runs) *reinterpret_cast<uint32_t *>(a.scale + (slot * a.runs + run) * kScaleTile + (at & 31) * 16 + (at >> 5) * 4) = word;
+  quantize_piece(reinterpret_cast<const T *>(a.x) + (there ? from : 0) * a.ldx, there ? a.cols : 0, c, a.cols, a.q + r * a.ldq,
+                 a.scale + (begin / 128 + g + (r - begin) / 128) * a.runs * kScaleTile, (int)((r - begin) % 128), a.runs);
+}
+
+// The same for the choices of a few tokens, which it puts in their experts' order itself: a block counts the choices before its own (of
+// lower experts, and earlier ones of the same), which is its row.  The first block also leaves the experts' first rows.
+constexpr int kPlaceMost = 128;  // choices: a tile's rows, so that an expert has one tile at most
+struct Place4Args {
+  Quant4Args quant;
+  const int32_t *ids;
+  int n, k, experts;
+  int64_t *first, *pos;  // experts + 1; n: a choice's row, -1 where there is no such expert
+};
+__global__ void __launch_bounds__(256) tuna_place_quantize4_kernel(Place4Args a) {
+  __shared__ int ids[kPlaceMost];
+  wait_previous();
+  allow_next();
+  const int lane = threadIdx.x & 31, c = ((int)blockIdx.y * 8 + (threadIdx.x >> 5)) * 256 + lane * 8, i = blockIdx.x;
+  if (threadIdx.x < a.n) {
+    const int id = a.ids[threadIdx.x];
+    ids[threadIdx.x] = id >= 0 && id < a.experts ? id : INT32_MAX;
+  }
+  __syncthreads();
+  if (i == 0 && blockIdx.y == 0)
+    for (int e = threadIdx.x; e <= a.experts; e += 256) {
+      int before = 0;
+      for (int j = 0; j < a.n; ++j) before += ids[j] < e;
+      a.first[e] = before;
+    }
+  const int mine = ids[i];
+  int begin = 0, rank = 0;
+  for (int j = lane; j < a.n; j += 32) begin += ids[j] < mine, rank += j < i && ids[j] == mine;
+  begin = __reduce_add_sync(~0u, begin), rank = __reduce_add_sync(~0u, rank);
+  if (threadIdx.x == 0 && blockIdx.y == 0) a.pos[i] = mine == INT32_MAX ? -1 : begin + rank;
+  if (mine == INT32_MAX) return;
+  const Quant4Args &q = a.quant;
+  quantize_piece(reinterpret_cast<const __nv_bfloat16 *>(q.x) + (i / a.k) * q.ldx, q.cols, c, q.cols, q.q + (int64_t)(begin + rank) * q.ldq,
+                 q.scale + (int64_t)(begin / 128 + mine) * q.runs * kScaleTile, rank, q.runs);
 }
 
 // Blocks along the columns, for the turned matrix: a block of threads takes a 128 x 128 tile through shared memory in its
@@ -986,9 +1028,11 @@ int launch_product4(const Product4Args &p, cudaStream_t st) {
   // 2896, one of either, 11.7 and 8.9; 1024 x 4736 x 4096, two of either, 16.3 and 16.5; 64 groups of 4096 x 2048 with 16 rows each, 7 and 14: 49 and 53.)
   if (!p.swiglu && ceil_div(wide, sm_count()) < ceil_div(narrow, sm_count()))
     return p.out_f32 ? run_tiles4<256, false, float>(p, st) : run_tiles4<256, false, __nv_bfloat16>(p, st);
-  // Few tiles: a cluster shares each.  (narrow: with SwiGLU too, whose tiles have 128 columns of the result)
+  // Few tiles: a cluster shares each, while its blocks find room at once and every one is spared six stages, which pay for the meeting
+  // (and every one has some).  (narrow: with SwiGLU too, whose tiles have 128 columns of the result.  One row in fours, twos, alone, us: 4096 x
+  // 4096 6.7, 6.6, 8.2; 2048 x 2048 4.6, 5.2, 5.5; 512 x 8192 6.1, 8.2, 13.1; 4096 x 1024 4.6, 4.6, 4.3; 128 rows, 2048 x 1536 6.8, 6.8, 5.3.)
   int parts = 4;
-  while (parts > 1 && (narrow * parts > 128 || stages - stages / parts < 6)) parts /= 2;
+  while (parts > 1 && (narrow * parts > 128 || stages - stages / parts < 6 || stages < 2 * parts)) parts /= 2;
   if (p.swiglu) return parts > 1 ? run_tiles4<256, true, uint8_t, kSplit>(p, st, parts) : run_tiles4<256, true, uint8_t>(p, st);
   if (parts > 1) return p.out_f32 ? run_tiles4<128, false, float, kSplit>(p, st, parts) : run_tiles4<128, false, __nv_bfloat16, kSplit>(p, st, parts);
   return p.out_f32 ? run_tiles4<128, false, float>(p, st) : run_tiles4<128, false, __nv_bfloat16>(p, st);
@@ -1024,6 +1068,16 @@ int launch_quantize4_rows(const void *x, bool f32, int64_t rows, int cols, int64
   }
   const int64_t tiles = fp4_slots(rows, offsets ? groups : 0);
   return f32 ? run_quantize_rows<float>(a, tiles, st) : run_quantize_rows<__nv_bfloat16>(a, tiles, st);
+}
+
+bool places_quantize4(int64_t choices) { return choices <= kPlaceMost; }
+int launch_place_quantize4(const void *x, int64_t tokens, int cols, int64_t ldx, const int32_t *ids, int k, int experts, void *q, int64_t ldq,
+                           uint8_t *scale, int64_t *first, int64_t *pos, cudaStream_t st) {
+  Place4Args a = {};
+  a.quant.x = x, a.quant.cols = cols, a.quant.ldx = ldx, a.quant.q = (uint8_t *)q, a.quant.ldq = ldq, a.quant.scale = scale;
+  a.quant.runs = (int)ceil_div(cols, 128);
+  a.ids = ids, a.n = (int)(tokens * k), a.k = k, a.experts = experts, a.first = first, a.pos = pos;
+  return launch(tuna_place_quantize4_kernel, dim3((unsigned)a.n, (unsigned)ceil_div(cols, 2048)), 256, 0, st, false, a);
 }
 
 }  // namespace tuna_ops

@@ -36,5 +36,11 @@ int launch_product4(const Product4Args &p, cudaStream_t st);
 int launch_quantize4_rows(const void *x, bool f32, int64_t rows, int cols, int64_t ldx, const int64_t *gather, int64_t in_rows, int groups,
                           const int64_t *offsets, void *q, int64_t ldq, uint8_t *scale, cudaStream_t st);
 
+// The same for the choices of a few tokens (as many as places_quantize4 allows), bf16, put in their experts' order on the way: `first`
+// receives the experts' first rows (experts + 1), `pos` each choice's row, -1 where there is no such expert.
+bool places_quantize4(int64_t choices);
+int launch_place_quantize4(const void *x, int64_t tokens, int cols, int64_t ldx, const int32_t *ids, int k, int experts, void *q, int64_t ldq,
+                           uint8_t *scale, int64_t *first, int64_t *pos, cudaStream_t st);
+
 }  // namespace tuna_ops
 #endif

@@ -100,10 +100,9 @@ int check_experts4(int64_t rows, int experts, int hidden, int inter) {
   return check_experts(rows, experts, hidden, inter);
 }
 
-int run_rows4(const void *x, int64_t ldx, int64_t rows, const int64_t *gather, int64_t in_rows, int experts, const int64_t *offsets, int hidden,
-              int inter, const void *w13, const void *s13, const void *w2, const void *s2, void *y, int64_t ldy, const Rows4Space &w,
-              cudaStream_t st) {
-  if (const int rc = launch_quantize4_rows(x, false, rows, hidden, ldx, gather, in_rows, experts, offsets, w.q, w.ldq, w.qs, st)) return rc;
+// The two products of quantised rows.
+int run_products4(int64_t rows, int experts, const int64_t *offsets, int hidden, int inter, const void *w13, const void *s13, const void *w2,
+                  const void *s2, void *y, int64_t ldy, const Rows4Space &w, cudaStream_t st) {
   Product4Args p = {};
   p.a = w.q, p.sa = w.qs, p.b = w13, p.sb = (const uint8_t *)s13, p.m = rows, p.n = inter, p.k = hidden, p.lda = w.ldq, p.ldb = hidden / 2;
   p.groups = experts, p.offsets = offsets, p.out = w.h, p.ldo = w.ldh, p.hs = w.hs, p.swiglu = true;
@@ -213,7 +212,9 @@ int tuna_fp4_expert_rows(const void *x, int64_t ldx, int64_t rows, int experts, 
   Carve c(workspace);
   const Rows4Space w = carve_rows4(c, rows, experts, hidden, inter);
   if (!workspace || !aligned(workspace, 256) || workspace_bytes < c.used) return TUNA_ERR_WORKSPACE;
-  return run_rows4(x, ldx, rows, nullptr, rows, experts, offsets, hidden, inter, w13, s13, w2, s2, y, ldy, w, (cudaStream_t)stream);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (const int rc = launch_quantize4_rows(x, false, rows, hidden, ldx, nullptr, rows, experts, offsets, w.q, w.ldq, w.qs, st)) return rc;
+  return run_products4(rows, experts, offsets, hidden, inter, w13, s13, w2, s2, y, ldy, w, st);
 }
 
 int tuna_fp4_experts_workspace_bytes(int64_t tokens, int experts, int k, int hidden, int inter, size_t *bytes) {
@@ -239,10 +240,15 @@ int tuna_fp4_experts(const void *x, int64_t ldx, int64_t tokens, const int32_t *
   if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return TUNA_ERR_WORKSPACE;
   Carve c(workspace);
   const Token4Space w = carve_tokens4(c, tokens, experts, k, hidden, inter);
-  if (const int rc = tuna_moe_order(ids, tokens, experts, k, 1, nullptr, w.offsets, w.order, w.pos, w.sort, w.sort_bytes, stream)) return rc;
-  if (const int rc = run_rows4(x, ldx, tokens * k, w.order, tokens, experts, w.offsets, hidden, inter, w13, s13, w2, s2, w.y, hidden, w.rows,
-                               (cudaStream_t)stream))
-    return rc;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (places_quantize4(tokens * k)) {
+    if (const int rc = launch_place_quantize4(x, tokens, hidden, ldx, ids, k, experts, w.rows.q, w.rows.ldq, w.rows.qs, w.offsets, w.pos, st)) return rc;
+  } else {
+    if (const int rc = tuna_moe_order(ids, tokens, experts, k, 1, nullptr, w.offsets, w.order, w.pos, w.sort, w.sort_bytes, stream)) return rc;
+    if (const int rc = launch_quantize4_rows(x, false, tokens * k, hidden, ldx, w.order, tokens, experts, w.offsets, w.rows.q, w.rows.ldq, w.rows.qs, st))
+      return rc;
+  }
+  if (const int rc = run_products4(tokens * k, experts, w.offsets, hidden, inter, w13, s13, w2, s2, w.y, hidden, w.rows, st)) return rc;
   return tuna_moe_combine(w.y, TUNA_DTYPE_BF16, tokens * k, hidden, hidden, weights, w.pos, tokens, k, out, TUNA_DTYPE_BF16, ldo, stream);
 }
 

@@ -72,7 +72,7 @@ def near(got, want, off):
 
 
 SIZES = [(1, 4, 2, 128, 128), (1, 64, 2, 1024, 512), (3, 8, 2, 256, 160), (70, 16, 4, 288, 416), (300, 5, 1, 512, 256), (513, 60, 6, 1024, 96),
-         (0, 4, 2, 128, 128), (1000, 3, 3, 160, 512), (2, 4, 4, 32, 32), (900, 2, 1, 4096, 64), (260, 4, 2, 64, 2080), (1500, 3, 2, 1056, 800), (4000, 4, 2, 288, 1056), (6000, 3, 1, 160, 2592)]
+         (0, 4, 2, 128, 128), (1000, 3, 3, 160, 512), (2, 4, 4, 32, 32), (900, 2, 1, 4096, 64), (260, 4, 2, 64, 2080), (1500, 3, 2, 1056, 800), (4000, 4, 2, 288, 1056), (6000, 3, 1, 160, 2592), (64, 512, 2, 96, 64), (40, 300, 3, 2080, 32), (32, 3, 3, 64, 64), (128, 1, 1, 128, 96), (43, 5, 3, 64, 32)]
 
 
 @pytest.mark.gpu
