@@ -675,6 +675,9 @@ int tuna_fp8_matmul(const void *a, const float *a_scale, int64_t m, int64_t lda,
  * tuna_fp4_dequantize - the values that rows x cols of q (pitch ldq bytes, any alignment) stand for, f32 or bf16;
  * rows outside every group are not written.
  *
+ * tuna_fp4_align - rows of `bytes` bytes, of any pitch and alignment, to rows on 16-byte boundaries (pitch ldo, a multiple of
+ * 16), as tuna_fp4_matmul wants them: for operands that somebody else laid; what stands behind the rows is not written.
+ *
  * tuna_fp4_matmul - out[m][n] = sum over k of a[m][k] * b[n][k], in 32 bits, to f32 or bf16; a: m x k, b: n x k, k even,
  * both quantised along k, pitches in bytes, multiples of 16.  A layer y = x w^T and its gradients are the same
  * product on operands quantised along the contracted axis:  y = (x ROWS) (w ROWS);  dx = (dy ROWS) (w COLUMNS);
@@ -694,6 +697,8 @@ int tuna_fp4_quantize(const void *x, int dtype, int64_t rows, int cols, int64_t 
 int tuna_fp4_dequantize(const void *q, int64_t ldq, const void *scale, int64_t rows, int cols,
                         int groups, const int64_t *offsets, void *out, int out_dtype, int64_t ldo,
                         void *stream);
+int tuna_fp4_align(const void *q, int64_t ldq, int64_t rows, int64_t bytes, void *out, int64_t ldo,
+                   void *stream);
 int tuna_fp4_matmul(const void *a, const void *a_scale, int64_t m, int64_t lda, const void *b,
                     const void *b_scale, int n, int64_t ldb, int k, int groups,
                     const int64_t *offsets, void *out, int out_dtype, int64_t ldo, void *stream);

@@ -103,6 +103,7 @@ SIGNATURES = {
     "tuna_fp4_scale_tiles": (ctypes.c_int, [_I64, _INT, _I64P]),
     "tuna_fp4_quantize": (ctypes.c_int, [_VP, _INT, _I64, _INT, _I64, _INT, _INT, _VP, _VP, _I64, _VP, _VP]),
     "tuna_fp4_dequantize": (ctypes.c_int, [_VP, _I64, _VP, _I64, _INT, _INT, _VP, _VP, _INT, _I64, _VP]),
+    "tuna_fp4_align": (ctypes.c_int, [_VP, _I64, _I64, _I64, _VP, _I64, _VP]),
     "tuna_fp4_matmul": (ctypes.c_int, [_VP, _VP, _I64, _I64, _VP, _VP, _INT, _I64, _INT, _INT, _VP, _VP, _INT, _I64, _VP]),
     "tuna_fp4_expert_rows_workspace_bytes": (ctypes.c_int, [_I64, _INT, _INT, _INT, _SZP]),
     "tuna_fp4_expert_rows": (ctypes.c_int, [_VP, _I64, _I64, _INT, _VP, _INT, _INT] + [_VP] * 5 + [_I64, _VP, ctypes.c_size_t, _VP]),

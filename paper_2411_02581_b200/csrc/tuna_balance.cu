@@ -509,12 +509,14 @@ struct Rows {  // tokens that a block takes at a time
 };
 
 // Tokens of a block: one step where that leaves four blocks a multiprocessor or fewer, as many as keep it at that otherwise; all of
-// them where one block is done with them before a second launch would be (a segment's end costs it 1.5 us).  (65536 x 64 with gradient, inputs from memory: four blocks a
-// multiprocessor 20.8 us, six 24.3, two 24.6; 20011 x 160 40.3, 41.6, 41.0.)
+// them where one block is done with them before a second launch would be (a segment's end costs it 1.5 us).  (65536 x 64 with
+// gradient, inputs from memory: four blocks a multiprocessor 20.8 us, six 24.3, two 24.6; 20011 x 160 40.3, 41.6, 41.0.)
+constexpr int kAloneSegments = 8;
 int64_t chunk_of(int64_t tokens, int experts, int segments) {
   const int64_t step = by_experts(experts, Rows{}), steps = ceil_div(tokens, step);
-  return std::max<int64_t>(1, steps <= 4 && segments <= 8 ? steps : ceil_div(steps, 592)) * step;
+  return std::max<int64_t>(1, steps <= 4 && segments <= kAloneSegments ? steps : ceil_div(steps, 592)) * step;
 }
+bool alone(const BalanceArgs &a) { return a.tokens <= a.chunk && a.segments <= kAloneSegments; }
 
 template <typename T>
 struct BalanceLaunch {
@@ -525,7 +527,7 @@ struct BalanceLaunch {
     const size_t smem = (size_t)(kThreads / 32 + 1) * a.experts * 4;
     const int64_t blocks = ceil_div(a.tokens, a.chunk);
     const bool sigmoid = a.scoring == TUNA_MOE_SIGMOID;
-    if (blocks == 1) return launch(sigmoid ? tuna_balance_kernel<LPT, VPL, true, true, T> : tuna_balance_kernel<LPT, VPL, true, false, T>, dim3(1), kThreads, smem, st, false, a);
+    if (alone(a)) return launch(sigmoid ? tuna_balance_kernel<LPT, VPL, true, true, T> : tuna_balance_kernel<LPT, VPL, true, false, T>, dim3(1), kThreads, smem, st, false, a);
     if (const int rc = launch(sigmoid ? tuna_balance_kernel<LPT, VPL, false, true, T> : tuna_balance_kernel<LPT, VPL, false, false, T>, dim3((unsigned)blocks), kThreads, smem, st, false, a))
       return rc;
     // Eight blocks a segment where it has many parts of many experts.  (Eight and one, us, the blocks' kernel with it: one segment of 8192 x 256 12.4
@@ -571,7 +573,7 @@ int tuna_moe_balance_workspace_bytes(int64_t tokens, int experts, int segments, 
   *bytes = 0;
   BalanceArgs a = {};
   a.tokens = tokens, a.experts = experts, a.segments = segments, a.chunk = chunk_of(tokens, experts, segments);
-  if (tokens <= a.chunk) return TUNA_OK;
+  if (alone(a)) return TUNA_OK;
   Carve c(nullptr);
   carve(c, a);
   *bytes = c.used;
@@ -599,7 +601,7 @@ int tuna_moe_balance(const void *logits, int dtype, int64_t tokens, int experts,
   a.logits = logits, a.ids = ids, a.offsets = offsets, a.tokens = tokens, a.ld = ld, a.experts = experts, a.k = k, a.scoring = scoring;
   a.segments = segments, a.chunk = chunk_of(tokens, experts, segments);
   a.loss = loss, a.z = z, a.counts = counts, a.mass = mass, a.live = live;
-  if (tokens > a.chunk) {
+  if (!alone(a)) {
     Carve c(workspace);
     carve(c, a);
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < c.used) return TUNA_ERR_WORKSPACE;

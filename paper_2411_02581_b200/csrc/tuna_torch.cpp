@@ -22,7 +22,7 @@ namespace {
 #define TUNA_CALLS(X)                                                                                       \
   X(tuna_moe_route_workspace_bytes) X(tuna_moe_route) X(tuna_moe_route_backward) X(tuna_fp8_quantize) \
   X(tuna_fp8_matmul) X(tuna_moe_few) X(tuna_moe_balance_workspace_bytes) X(tuna_moe_balance) X(tuna_moe_balance_backward)  \
-  X(tuna_fp4_quantize) X(tuna_fp4_dequantize) X(tuna_fp4_matmul) X(tuna_fp4_expert_rows_workspace_bytes) X(tuna_fp4_expert_rows) \
+  X(tuna_fp4_quantize) X(tuna_fp4_dequantize) X(tuna_fp4_align) X(tuna_fp4_matmul) X(tuna_fp4_expert_rows_workspace_bytes) X(tuna_fp4_expert_rows) \
   X(tuna_fp4_experts_workspace_bytes) X(tuna_fp4_experts)
 #define X(f) decltype(&f) p_##f = nullptr;
 TUNA_CALLS(X)
@@ -431,8 +431,7 @@ Tensor operand4(const Tensor &q, const char *name, int64_t &ld, void *stream) {
   const int64_t pitch = ld;
   ld = std::max<int64_t>((q.size(1) + 15) / 16 * 16, 16);
   Tensor p = make({q.size(0), ld}, at::kByte, q);  // (what stands behind the rows is not read)
-  if (q.numel() && cudaMemcpy2DAsync(p.data_ptr(), ld, q.data_ptr(), pitch, q.size(1), q.size(0), cudaMemcpyDeviceToDevice, (cudaStream_t)stream) != cudaSuccess)
-    throw std::runtime_error("cudaMemcpy2DAsync failed");
+  check(p_tuna_fp4_align(at_of(q), pitch, q.size(0), q.size(1), at_of(p), ld, stream), "tuna_fp4_align");
   return p;
 }
 

@@ -335,6 +335,18 @@ def test_operands_off_16_bytes_and_results_of_any_pitch():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,count,pitch,at", [(1, 1, 1, 0), (7, 15, 15, 0), (200, 33, 37, 1), (300, 1448, 1448, 0), (33, 64, 66, 2), (50, 100, 104, 4), (9, 4097, 5000, 3)])
+def test_rows_laid_on_16_bytes(rows, count, pitch, at):
+    g = torch.Generator().manual_seed(rows)
+    src = torch.randint(0, 256, (rows * pitch + at + 16,), dtype=torch.uint8, generator=g).cuda()
+    ldo = (count + 15) // 16 * 16 + 16
+    out = torch.full((rows, ldo), 7, dtype=torch.uint8, device="cuda")
+    assert B.lib().tuna_fp4_align(src[at:].data_ptr(), pitch, rows, count, out.data_ptr(), ldo, None) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(out[:, :count], src[at:at + rows * pitch].view(rows, pitch)[:, :count]) and bool((out[:, count:] == 7).all())
+
+
+@pytest.mark.gpu
 def test_more_values_than_32_bits_count():
     """2^31 + values: the last rows of the operand and of the result are where they should be."""
     from paper_2411_02581_b200 import moe
@@ -457,6 +469,11 @@ def test_fp4_refusals():
         return L.tuna_fp4_dequantize(q, ldq, s, rows, cols, groups, off, out, dt, ldo, None)
     assert back(ldq=31) == -1 and back(ldo=63) == -1 and back(dt=2) == -1 and back(groups=1) == -1 and back(s=264) == -1 and back(out=257) == -1
     assert back(q=None) == -1 and back(rows=0) == 0 and back(cols=0) == 0 and back(rows=-1) == -1 and back(groups=600, off=256) == -9
+
+    def align(q=256, ldq=32, rows=4, count=32, out=256, ldo=32):
+        return L.tuna_fp4_align(q, ldq, rows, count, out, ldo, None)
+    assert align(ldq=31) == -1 and align(ldo=40) == -1 and align(ldo=16) == -1 and align(q=None) == -1 and align(out=264) == -1 and align(rows=-1) == -1
+    assert align(rows=0) == 0 and align(count=0) == 0 and align(rows=1 << 32) == -9 and align(count=1 << 25, ldq=1 << 25, ldo=1 << 25) == -9
 
     def product(a=256, sa=256, m=4, lda=32, b=256, sb=256, n=8, ldb=32, k=64, groups=0, off=None, out=256, dt=1, ldo=8):
         return L.tuna_fp4_matmul(a, sa, m, lda, b, sb, n, ldb, k, groups, off, out, dt, ldo, None)
