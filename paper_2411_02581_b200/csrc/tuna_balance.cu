@@ -319,6 +319,7 @@ __global__ void __launch_bounds__(kThreads) tuna_balance_kernel(BalanceArgs a) {
     if (!ALONE) break;
     if (g + 1 < a.segments) begin = end, end = max(begin, bound_of(a, g + 2));
   }
+  asm volatile("cp.async.wait_all;" ::: "memory");  // (a block whose tokens are nobody's has not waited for its choices yet)
 }
 
 // A block a segment: the parts of the blocks that met it, every 2nd (or 16th, 32nd ...) of them by one row of threads, then the
