@@ -472,6 +472,13 @@ __global__ void __launch_bounds__(kThreads, VPL > 8 ? 2 : 4) tuna_balance_grad_k
     dot = group_sum<LPT>(dot + other) * by;
     // (a token that holds +inf has an infinite z whatever moves: it gets no part of its gradient)
     const float of_z = part && pull_z != 0.0f && !token.endless ? pull_z * token.lse : 0.0f;
+    // Where a gradient of the segment is not finite, neither is dot (0 times it is NaN): what has no probability, and who is nobody's, gets
+    // zeros all the same.  (A sigmoid that is 0 has no part of the softmax either.)
+    uint32_t none = 0;
+    if (!(fabsf(of_z - dot) < INFINITY)) {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) none |= (uint32_t)(!part || token.x[i] == 0.0f) << i;
+    }
     float d[VPL];
 #pragma unroll
     for (int i = 0; i < VPL; i += 2) {
@@ -483,6 +490,11 @@ __global__ void __launch_bounds__(kThreads, VPL > 8 ? 2 : 4) tuna_balance_grad_k
       } else {
         unpair(mul2(p, add2(pair(pull[i], pull[i + 1]), pair(of_z - dot, of_z - dot))), d[i], d[i + 1]);
       }
+    }
+    if (none) {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i)
+        if (none >> i & 1) d[i] = 0.0f;
     }
     if (t < b1) {
       T *out = reinterpret_cast<T *>(a.dlogits) + t * a.ldd + sub * VPL;

@@ -27,3 +27,33 @@ def test_blocks_of_nobodys_tokens(scoring):
     assert bool((d[:29000] == 0).all()) and bool((d[30001:] == 0).all())
     none = moe.balance(z, ids, scoring=scoring, offsets=torch.tensor([t, t, t], device="cuda"))
     assert all(bool((p == 0).all()) for p in none)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scoring", SCORINGS)
+@pytest.mark.parametrize("e", [5, 24, 64, 160, 300])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("which", ["loss", "z"])
+def test_a_gradient_that_is_not_finite_stays_in_its_segment(which, bad, e, scoring):
+    """Masked logits, masked rows and tokens of no segment get zeros, and other segments what they get without it."""
+    from paper_2411_02581_b200 import moe
+    t, k = 3000, 3
+    z, ids = made(t, e, k, F32, 4)
+    z[700:760], z[1500], z[2500:] = -float("inf"), float("nan"), -float("inf")
+    z[::7, 1], z[3::11, 4], ids[2500:] = -float("inf"), float("nan"), -1
+    z, ids = z.cuda(), ids.cuda()
+    offsets = torch.tensor([100, 600, 2000, 2600], device="cuda")
+    got = moe.balance(z, ids, scoring=scoring, offsets=offsets)
+    fine = torch.tensor([1.0, 2.0, 3.0], device="cuda")
+    odd = fine.clone()
+    odd[1] = bad
+    args = dict(scoring=scoring, offsets=offsets)
+    for dz in ((None, fine) if which == "loss" else (odd,)):
+        d = moe.balance_backward(z, got.counts, got.tokens, k, odd if which == "loss" else fine, dz, **args)
+        want = moe.balance_backward(z, got.counts, got.tokens, k, fine, None if dz is None else fine, **args)
+        inside = torch.zeros(t, dtype=torch.bool, device="cuda")
+        inside[600:2000] = True
+        assert torch.equal(d[~inside], want[~inside])
+        masked = torch.isnan(z) | (z == -float("inf"))
+        assert bool((d[masked] == 0).all())
+        assert not bool(torch.isfinite(d[inside][~masked[inside]]).any())
