@@ -1183,10 +1183,10 @@ int tuna_fp4_matmul(const void *a, const void *a_scale, int64_t m, int64_t lda, 
   const int matrices = std::max(groups, 1);
   if (matrices * (ceil_div(m, 128) + 1) * ceil_div(n, 128) > INT32_MAX) return TUNA_ERR_RANGE;  // tiles, whatever the offsets hold
   if (m == 0 || n == 0) return TUNA_OK;
-  if (!out || !aligned(out, so)) return TUNA_ERR_INVALID_ARG;
+  if (!out || !aligned(out, so) || !aligned(offsets, 8)) return TUNA_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
-  if (k == 0) return note_cuda(cudaMemset2DAsync(out, ldo * so, 0, n * so, m, st));  // an empty sum
-  if (!a || !b || !a_scale || !b_scale || !aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 16) || !aligned(b_scale, 16) || !aligned(offsets, 8))
+  if (k == 0) return launch_empty_sums(out, out_dtype == TUNA_DTYPE_F32, m, n, ldo, groups, offsets, st);
+  if (!a || !b || !a_scale || !b_scale || !aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 16) || !aligned(b_scale, 16))
     return TUNA_ERR_INVALID_ARG;
   Product4Args p = {};
   p.a = a, p.b = b, p.sa = (const uint8_t *)a_scale, p.sb = (const uint8_t *)b_scale, p.m = m, p.n = n, p.k = k, p.lda = lda, p.ldb = ldb, p.ldo = ldo;

@@ -638,6 +638,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   if (threadIdx.x == 0 && *given_up) *a.error = 1;
 }
 
+template <typename T>
+__global__ void __launch_bounds__(256) tuna_empty_sums_kernel(T *out, int64_t m, int n, int64_t ldo, const int64_t *offsets) {
+  wait_previous();
+  allow_next();
+  auto cut = [&](int g) { return min(max(offsets[g], (int64_t)0), m); };
+  const int64_t end = cut(blockIdx.x + 1);
+  for (int64_t r = cut(blockIdx.x) + blockIdx.y; r < end; r += gridDim.y)
+    for (int c = threadIdx.x; c < n; c += 256) out[r * ldo + c] = from_f32<T>(0.0f);
+}
+
 // ---- host ------------------------------------------------------------------------------------
 
 template <int BN, bool SWIGLU, bool B_ROWS, typename TO, bool SPLIT = false>
@@ -721,6 +731,14 @@ int make_map(CUtensorMap *map, int rank, const void *p, int64_t k, int64_t rows,
                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? TUNA_OK : note_cuda(cudaErrorInvalidValue);
+}
+
+int launch_empty_sums(void *out, bool f32, int64_t m, int n, int64_t ldo, int groups, const int64_t *offsets, cudaStream_t st) {
+  const size_t size = f32 ? 4 : 2;
+  if (!offsets) return note_cuda(cudaMemset2DAsync(out, ldo * size, 0, n * size, m, st));
+  const dim3 grid((unsigned)groups, (unsigned)std::min<int64_t>(m, 64));
+  if (f32) return launch(tuna_empty_sums_kernel<float>, grid, 256, 0, st, false, (float *)out, m, n, ldo, offsets);
+  return launch(tuna_empty_sums_kernel<__nv_bfloat16>, grid, 256, 0, st, false, (__nv_bfloat16 *)out, m, n, ldo, offsets);
 }
 
 int make_out_map(CUtensorMap *map, void *p, int64_t cols, int64_t rows, int64_t ld, int row_bytes) {
@@ -836,9 +854,9 @@ int tuna_fp8_matmul(const void *a, const float *a_scale, int64_t m, int64_t lda,
   if (groups > TUNA_MOE_MAX_EXPERTS || n > kMaxDim || k > kMaxDim || m > INT32_MAX - 256) return TUNA_ERR_RANGE;
   if (groups * (ceil_div(m, 128) + 1) * ceil_div(n, 128) > INT32_MAX) return TUNA_ERR_RANGE;  // tiles, whatever the offsets hold
   if (m == 0 || n == 0) return TUNA_OK;
-  if (!out || !aligned(out, so)) return TUNA_ERR_INVALID_ARG;
+  if (!out || !aligned(out, so) || !aligned(offsets, 8)) return TUNA_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
-  if (k == 0) return note_cuda(cudaMemset2DAsync(out, ldo * so, 0, n * so, m, st));  // an empty sum
+  if (k == 0) return launch_empty_sums(out, out_dtype == TUNA_DTYPE_F32, m, n, ldo, groups, offsets, st);
   if (!a || !b || !a_scale || !b_scale || !aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 4) || !aligned(b_scale, 4)) return TUNA_ERR_INVALID_ARG;
   ProductArgs p = {};
   p.a = a, p.b = b, p.sa = a_scale, p.sb = b_scale, p.m = m, p.n = n, p.k = k, p.lda = lda, p.ldb = ldb, p.ldo = ldo;

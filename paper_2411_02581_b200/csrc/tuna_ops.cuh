@@ -82,6 +82,10 @@ int make_out_map(CUtensorMap *map, void *p, int64_t cols, int64_t rows, int64_t 
 // Scales of 4-bit operands: tiles x runs x 512 bytes; boxes of 512 bytes x 2 runs x `box` tiles (tuna_fp4.cu).
 int make_scale_map(CUtensorMap *map, const void *p, int64_t runs, int64_t tiles, int box);
 
+// Zeros for the results of a product whose contracted axis is empty (f32 or bf16, n columns of pitch ldo), in the rows of the
+// groups alone (offsets: device, groups + 1, or nullptr: all m rows) (tuna_fp8.cu).
+int launch_empty_sums(void *out, bool f32, int64_t m, int n, int64_t ldo, int groups, const int64_t *offsets, cudaStream_t st);
+
 // Carves a caller's workspace into 256-byte aligned pieces; with base == nullptr it only adds up.
 struct Carve {
   char *base;

@@ -1,7 +1,9 @@
-"""4-bit operands where they end: scales behind the last row."""
+"""4-bit operands where they end: scales behind the last row, rows outside every group."""
 import pytest
 import torch
 
+from paper_2411_02581_b200 import binding as B
+from paper_2411_02581_b200 import build as build_mod
 from test_fp4_experts import layer
 from test_fp8 import activations
 
@@ -36,3 +38,32 @@ def test_scales_behind_the_last_row_may_be_nan(form):
     w = torch.rand(rows, 1, generator=torch.Generator().manual_seed(1)).cuda()
     assert torch.equal(moe.fp4_experts(x, ids, w, w13, bad, w2, s2), moe.fp4_experts(x, ids, w, w13, s13, w2, s2))
     assert moe.device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,code", [(torch.float32, 0), (torch.bfloat16, 1)])
+@pytest.mark.parametrize("entry", ["fp4", "fp8"])
+@pytest.mark.parametrize("offsets", [None, [30, 200, 200, 471], [-5, 1, 1, 1 << 40], [499, 500, 500, 500], [0, 0, 0, 0]])
+def test_an_empty_sum_leaves_rows_of_no_group_alone(entry, offsets, dtype, code):
+    """k = 0: rows of the groups are zero, others as they were."""
+    m, n, pitch, groups = 500, 37, 41, 3
+    y = torch.full((m + 2, pitch), 7.0, dtype=dtype, device="cuda")
+    off = None if offsets is None else torch.tensor(offsets, device="cuda")
+    at, out = None if off is None else off.data_ptr(), y[1:].data_ptr()
+    if entry == "fp4":
+        rc = B.lib().tuna_fp4_matmul(None, None, m, 16, None, None, n, 16, 0, 0 if off is None else groups, at, out, code, pitch, None)
+    else:
+        rc = B.lib().tuna_fp8_matmul(None, None, m, 16, None, None, 2, n, 16, 0, 1 if off is None else groups, at, out, code, pitch, None)
+    torch.cuda.synchronize()
+    lo, hi = (0, m) if offsets is None else (max(offsets[0], 0), min(offsets[-1], m))
+    want = torch.full_like(y, 7.0)
+    want[1 + lo:1 + hi, :n] = 0
+    assert rc == 0 and torch.equal(y, want)
+
+
+def test_offsets_off_eight_bytes_are_refused():
+    """On the host, before any GPU work (pointers are never followed), with an empty sum too."""
+    build_mod.build()
+    for k in (0, 64):
+        assert B.lib().tuna_fp4_matmul(256, 256, 5, 64, 256, 256, 7, 64, k, 2, 260, 256, 0, 8, None) == -1
+        assert B.lib().tuna_fp8_matmul(256, 256, 5, 64, 256, 256, 2, 7, 64, k, 2, 260, 256, 0, 8, None) == -1
