@@ -599,7 +599,9 @@ int tuna_moe_balance(const void *logits, int dtype, int64_t tokens, int experts,
   if (const int rc = check_balance(tokens, experts, k, segments)) return rc;
   const size_t size = dtype_size(dtype);
   if (!size || (scoring != TUNA_MOE_SOFTMAX && scoring != TUNA_MOE_SIGMOID) || ld < experts || (segments > 1 && !offsets)) return TUNA_ERR_INVALID_ARG;
-  if (!loss || !counts || !mass || !live) return TUNA_ERR_INVALID_ARG;
+  if (!loss || !counts || !mass || !live || !aligned(loss, 4) || !aligned(z, 4) || !aligned(counts, 8) || !aligned(mass, 4) || !aligned(live, 8) ||
+      !aligned(offsets, 8))
+    return TUNA_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
   if (tokens == 0) {
     const size_t n = (size_t)segments * experts;
@@ -630,7 +632,9 @@ int tuna_moe_balance_backward(const void *logits, int dtype, int64_t tokens, int
   if (!size || (scoring != TUNA_MOE_SOFTMAX && scoring != TUNA_MOE_SIGMOID) || ld < experts || ldd < experts || (segments > 1 && !offsets))
     return TUNA_ERR_INVALID_ARG;
   if (tokens == 0) return TUNA_OK;
-  if (!logits || !counts || !live || !dloss || !dlogits || !aligned(logits, size) || !aligned(dlogits, size)) return TUNA_ERR_INVALID_ARG;
+  if (!logits || !counts || !live || !dloss || !dlogits || !aligned(logits, size) || !aligned(dlogits, size) || !aligned(counts, 8) || !aligned(live, 8) ||
+      !aligned(dloss, 4) || !aligned(dz, 4) || !aligned(offsets, 8))
+    return TUNA_ERR_INVALID_ARG;
   BalanceArgs a = {};
   a.logits = logits, a.offsets = offsets, a.tokens = tokens, a.ld = ld, a.ldd = ldd, a.experts = experts, a.k = k, a.scoring = scoring;
   a.segments = segments, a.chunk = chunk_of(tokens, experts, segments);

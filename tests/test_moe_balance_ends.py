@@ -2,6 +2,8 @@
 import pytest
 import torch
 
+from paper_2411_02581_b200 import binding as B
+from paper_2411_02581_b200 import build as build_mod
 from test_moe_balance import F32, agree, agree_gradient, made, plain
 
 SCORINGS = ["softmax", "sigmoid"]
@@ -57,3 +59,17 @@ def test_a_gradient_that_is_not_finite_stays_in_its_segment(which, bad, e, scori
         masked = torch.isnan(z) | (z == -float("inf"))
         assert bool((d[masked] == 0).all())
         assert not bool(torch.isfinite(d[inside][~masked[inside]]).any())
+
+
+def test_pointers_off_their_values_boundaries_are_refused():
+    """On the host, before any GPU work (pointers are never followed)."""
+    build_mod.build()
+    L = B.lib()
+
+    def loss(off=256, out=256, z=256, counts=256, mass=256, live=256):
+        return L.tuna_moe_balance(256, 0, 8, 16, 16, 256, 2, 0, 2, off, out, z, counts, mass, live, 256, 0, None)
+    assert [loss(off=260), loss(out=258), loss(z=257), loss(counts=260), loss(mass=258), loss(live=252)] == [-1] * 6
+
+    def grad(off=256, counts=256, live=256, dloss=256, dz=256):
+        return L.tuna_moe_balance_backward(256, 0, 8, 16, 16, 2, 0, 2, off, counts, live, dloss, dz, 256, 16, None)
+    assert [grad(off=260), grad(counts=260), grad(live=252), grad(dloss=258), grad(dz=257)] == [-1] * 5
