@@ -120,8 +120,9 @@ int64_t integer(PyObject *o) {
   if (v == -1 && PyErr_Occurred()) throw Refused();
   return v;
 }
+int clip(int64_t n) { return (int)std::min<int64_t>(std::max<int64_t>(n, INT32_MIN), INT32_MAX); }
 int small(PyObject *o) {  // what does not fit an int is beyond every limit of the library: let it say so
-  return (int)std::min<int64_t>(std::max<int64_t>(integer(o), INT32_MIN), INT32_MAX);
+  return clip(integer(o));
 }
 double number(PyObject *o) {
   const double v = PyFloat_AsDouble(o);
@@ -143,7 +144,6 @@ void check(int rc, const char *what) {
 }
 
 void *at_of(const Tensor &t) { return t.data_ptr(); }
-int clip(int64_t n) { return (int)std::min<int64_t>(n, INT32_MAX); }
 
 template <typename... T>
 PyObject *pack(const T &...t) {

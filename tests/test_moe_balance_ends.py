@@ -73,3 +73,16 @@ def test_pointers_off_their_values_boundaries_are_refused():
     def grad(off=256, counts=256, live=256, dloss=256, dz=256):
         return L.tuna_moe_balance_backward(256, 0, 8, 16, 16, 2, 0, 2, off, counts, live, dloss, dz, 256, 16, None)
     assert [grad(off=260), grad(counts=260), grad(live=252), grad(dloss=258), grad(dz=257)] == [-1] * 5
+
+
+@pytest.mark.gpu
+def test_slots_a_token_are_not_wrapped():
+    """An integer that does not fit 32 bits is refused, below as above."""
+    from paper_2411_02581_b200 import moe
+    z, ids = (p.cuda() for p in made(8, 16, 2, F32))
+    b = moe.balance(z, ids)
+    one = torch.ones(1, device="cuda")
+    with pytest.raises(B.TunaError, match="TUNA_ERR_INVALID_ARG"):
+        moe.balance_backward(z, b.counts, b.tokens, 2 - (1 << 32), one)
+    with pytest.raises(B.TunaError, match="TUNA_ERR_RANGE"):
+        moe.balance_backward(z, b.counts, b.tokens, 2 + (1 << 32), one)
