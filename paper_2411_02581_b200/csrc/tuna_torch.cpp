@@ -10,6 +10,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <dlfcn.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/version.h>
 
 #include <algorithm>
 #include <optional>
@@ -398,7 +399,15 @@ PyObject *balance_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// A torch without the types of 4-bit operands (before 2.8) has the other operators all the same.
+#ifndef TUNA_TORCH_FP4
+#define TUNA_TORCH_FP4 (TORCH_VERSION_MAJOR > 2 || (TORCH_VERSION_MAJOR == 2 && TORCH_VERSION_MINOR >= 8))
+#endif
+#if TUNA_TORCH_FP4
 constexpr at::ScalarType kFp4 = at::ScalarType::Float4_e2m1fn_x2, kPower = at::ScalarType::Float8_e8m0fnu;
+#else
+constexpr at::ScalarType kFp4 = at::ScalarType::Undefined, kPower = at::ScalarType::Undefined;
+#endif
 
 // The groups' bounds: int64 [groups + 1], or None (0 groups).
 const int64_t *groups_of(PyObject *o, const Tensor &with, int64_t &groups) {
@@ -438,6 +447,7 @@ Tensor operand4(const Tensor &q, const char *name, int64_t &ld, void *stream) {
 // fp4_quantize(x, layout, offsets, stream)
 PyObject *fp4_quantize(PyObject *, PyObject *const *a, Py_ssize_t n) {
   return guarded(n, 4, [&] {
+    if (kFp4 == at::ScalarType::Undefined) refuse("this torch has no float4_e2m1fn_x2");
     const Tensor &x = tensor(a[0], "x");
     const int64_t ld = matrix(x, "x", true, true, false), rows = x.size(0), cols = x.size(1);
     const int layout = small(a[1]);

@@ -33,7 +33,8 @@ from . import build as _build
 SOFTMAX, SIGMOID = 0, 1
 SCORING = {"softmax": SOFTMAX, "sigmoid": SIGMOID}
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2}
-FP4, POWER = torch.float4_e2m1fn_x2, torch.float8_e8m0fnu  # two values a byte; the scale of 32 values
+# two values a byte; the scale of 32 values (None: a torch without them, which has the other operators)
+FP4, POWER = getattr(torch, "float4_e2m1fn_x2", None), getattr(torch, "float8_e8m0fnu", None)
 FP4_LAYOUTS = {"rows": 0, "columns": 1}
 LAYOUTS = {"rows": 0, "columns": 1, "tiles": 2, "tiles_t": 3}
 FLOATS = (torch.float32, torch.bfloat16)
