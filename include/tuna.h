@@ -571,10 +571,12 @@ int tuna_moe_route_backward(const void *logits, int dtype, int64_t tokens, int e
  * packed batch, or all of it), over its n live tokens, those with a logit that is neither -inf nor NaN,
  *   loss[g] = experts / (k n^2) * sum over e of counts[g][e] * mass[g][e],
  *   z[g]    = (1 / n) * sum over t of (log of the sum over e of exp(logit))^2,
- *   counts[g][e] = how often ids names e in the segment (ids outside [0, experts) are left out),
+ *   counts[g][e] = how often ids names e in the segment (ids outside [0, experts) are left out; those of a token
+ *                  that is not live count as any other: tuna_moe_route gives it -1, and who chooses in another
+ *                  way does the same, or the shares counts / (k n) add up to more than 1),
  *   mass[g][e]   = sum over t of the probability of e: TUNA_MOE_SOFTMAX the softmax over the experts,
  *                  TUNA_MOE_SIGMOID 1/(1+exp(-logit)) divided by the token's sum of them,
- *   live[g] = n.  An even choice has a loss of 1; a segment without live tokens one of 0.
+ *   live[g] = n.  An even choice of the live tokens has a loss of 1; a segment without live tokens one of 0.
  *   logits   tokens x experts, f32 or bf16, pitch ld; masked logits (-inf, NaN) have probability 0,
  *            logits of +inf share the softmax (z is then +inf).  ids: tokens x k (int32), as
  *            tuna_moe_route makes them.

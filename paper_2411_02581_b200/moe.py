@@ -190,7 +190,8 @@ def route_backward(logits, ids, dweights, *, scoring="softmax", renormalize=Fals
 
 def balance(logits, ids, *, scoring="softmax", offsets=None, stream=None) -> Balance:
     """The balance loss of every segment of the tokens, the mean square of the logits' log-sum-exp, and what they are
-    made of (``tuna_moe_balance``).  ``ids`` as :func:`route` makes them; ``offsets`` (int64 [segments + 1]): the segments'
+    made of (``tuna_moe_balance``).  ``ids`` as :func:`route` makes them (-1 for a row without live logits: other ids
+    of such a row are counted); ``offsets`` (int64 [segments + 1]): the segments'
     bounds, None for one segment."""
     return Balance(*(_marshal or _fast()).balance(logits, ids, _scoring(scoring), offsets, stream))
 

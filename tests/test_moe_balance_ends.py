@@ -86,3 +86,20 @@ def test_slots_a_token_are_not_wrapped():
         moe.balance_backward(z, b.counts, b.tokens, 2 - (1 << 32), one)
     with pytest.raises(B.TunaError, match="TUNA_ERR_RANGE"):
         moe.balance_backward(z, b.counts, b.tokens, 2 + (1 << 32), one)
+
+
+@pytest.mark.gpu
+def test_choices_of_masked_rows_are_counted():
+    """ids may come from another choice than route's and name experts for rows without live logits: they are counted as any other, and the loss is
+    that of the formula, over 1 when all is even.  With -1 there (as route has it) they are not."""
+    from paper_2411_02581_b200 import moe
+    t, e, k = 640, 8, 2
+    z = torch.zeros(t, e)
+    z[::4] = -float("inf")
+    ids = torch.stack([torch.arange(t) % e, (torch.arange(t) + 3) % e], 1).to(torch.int32)
+    got = moe.balance(z.cuda(), ids.cuda())
+    agree(got, plain(z, ids, k, "softmax", [0, t]))
+    assert abs(float(got.loss) - 4 / 3) < 1e-6 and int(got.counts.sum()) == t * k and int(got.tokens) == t * 3 // 4
+    ids[::4] = -1
+    got = moe.balance(z.cuda(), ids.cuda())
+    agree(got, plain(z, ids, k, "softmax", [0, t]))
