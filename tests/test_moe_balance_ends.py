@@ -103,3 +103,63 @@ def test_choices_of_masked_rows_are_counted():
     ids[::4] = -1
     got = moe.balance(z.cuda(), ids.cuda())
     agree(got, plain(z, ids, k, "softmax", [0, t]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scoring", SCORINGS)
+def test_infinite_logits_have_no_part_of_z(scoring):
+    """A row that holds +inf gets the loss's gradient and none of z's; the others get both."""
+    from paper_2411_02581_b200 import moe
+    t, e, k = 500, 40, 2
+    z, ids = made(t, e, k, F32, 5)
+    z[3, 7], z[3, 30], z[400, 0] = float("inf"), float("inf"), float("inf")
+    one = torch.ones(1)
+    calm = torch.where(torch.isinf(z), torch.full_like(z, 200.0), z)              # (the same shares, and a finite z)
+    want = plain(calm, ids, k, scoring, [0, t], one, 0.3 * one)
+    alone = plain(calm, ids, k, scoring, [0, t], one)
+    got = moe.balance(z.cuda(), ids.cuda(), scoring=scoring)
+    assert float(got.z) == float("inf") and int(got.tokens) == t and torch.equal(got.counts.cpu(), want[2])
+    d = moe.balance_backward(z.cuda(), got.counts, got.tokens, k, one.cuda(), 0.3 * one.cuda(), scoring=scoring).cpu()
+    rows = torch.ones(t, dtype=torch.bool)
+    rows[[3, 400]] = False
+    agree_gradient(d[rows], want[5][rows], want[6][rows], F32)
+    agree_gradient(d[~rows], alone[5][~rows], alone[6][~rows], F32)
+
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scoring", SCORINGS)
+@pytest.mark.parametrize("t,segments", [(200, 3), (9000, 4)])
+def test_without_z(t, segments, scoring):
+    """The C entry without a place for z: the rest is the same, bit for bit."""
+    from paper_2411_02581_b200 import moe
+    e, k = 50, 2
+    z, ids = (p.cuda() for p in made(t, e, k, F32, 6))
+    offsets = torch.linspace(0, t, segments + 1).long().cuda()
+    want = moe.balance(z, ids, scoring=scoring, offsets=offsets)
+    loss, counts, mass, live = (torch.empty_like(p) for p in (want.loss, want.counts, want.mass, want.tokens))
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    assert B.lib().tuna_moe_balance(z.data_ptr(), 0, t, e, e, ids.data_ptr(), k, SCORINGS.index(scoring), segments, offsets.data_ptr(), loss.data_ptr(),
+                                    None, counts.data_ptr(), mass.data_ptr(), live.data_ptr(), ws.data_ptr(), ws.numel(), None) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(loss, want.loss) and torch.equal(counts, want.counts) and torch.equal(mass, want.mass) and torch.equal(live, want.tokens)
+
+
+
+@pytest.mark.gpu
+def test_sums_of_a_huge_segment():
+    """4 million tokens of even logits: each adds 2^-9 to every expert, so that a lane's sums (of 900 tokens at most) and a block's are exact, and
+    the sum of 600 blocks' is off by 600 * 2^-24 of itself at most; the first one's choices are counted to the last."""
+    from paper_2411_02581_b200 import moe
+    t, e, k = (1 << 22) + 777, 512, 2
+    z = torch.zeros(t, e, dtype=torch.bfloat16, device="cuda")
+    ids = torch.zeros(t, k, dtype=torch.int32, device="cuda")
+    ids[:, 1] = torch.arange(t, device="cuda") % e
+    got = moe.balance(z, ids)
+    want = torch.bincount(ids[:, 1].long(), minlength=e)
+    want[0] += t
+    assert torch.equal(got.counts[0], want) and int(got.tokens) == t
+    assert bool(((got.mass[0].double() - t / e).abs() <= 2.0 ** -14 * t / e).all())
+    assert abs(float(got.loss) - 1) <= 2.0 ** -13
+    del z
+    torch.cuda.empty_cache()
