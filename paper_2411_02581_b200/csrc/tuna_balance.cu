@@ -527,7 +527,7 @@ struct Rows {  // tokens that a block takes at a time
 constexpr int kAloneSegments = 8;
 int64_t chunk_of(int64_t tokens, int experts, int segments) {
   const int64_t step = by_experts(experts, Rows{}), steps = ceil_div(tokens, step);
-  return std::max<int64_t>(1, steps <= 4 && segments <= kAloneSegments ? steps : ceil_div(steps, 592)) * step;
+  return std::max<int64_t>(1, steps <= 4 && segments <= kAloneSegments ? steps : ceil_div(steps, 4 * sm_count())) * step;
 }
 bool alone(const BalanceArgs &a) { return a.tokens <= a.chunk && a.segments <= kAloneSegments; }
 
