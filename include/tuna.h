@@ -734,7 +734,8 @@ int tuna_moe_experts(const void *x, int64_t ldx, int64_t tokens, const int32_t *
                      int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
- * tuna_fp4_experts, tuna_fp4_expert_rows - the same with weights, x and h in 4 bits (tuna_fp4_quantize):
+ * tuna_fp4_experts, tuna_fp4_expert_rows - the same with weights, x and h in 4 bits (tuna_fp4_quantize), and each
+ *   expert's row rounded to bf16 before the sum as well:
  *   w13      experts x 2 x inter x hidden / 2 bytes; s13: experts x 2 x ceil(inter/128) x ceil(hidden/128) x 512;
  *   w2, s2   experts x hidden x inter / 2 and experts x ceil(hidden/128) x ceil(inter/128) x 512.
  *   hidden and inter are multiples of 32; weights and scales start on 16-byte boundaries.  Limits as above.

@@ -7,6 +7,10 @@
 //
 //   dz = p (G - sum p G) [sigmoid: times 1 - sigmoid(z)] + dz_g 2 lse / n softmax(z),   G = dloss_g E / (k n^2) c
 //
+// Probabilities and all sums are in 32 bits; a sum goes over a lane's tokens, a block's warps, then the blocks, so that a mass of 4 million
+// tokens adds 900 terms, 8 and 600 one after the other: off by 1500 * 2^-24 of itself at the very worst (65536 x 64: 9e-8 measured, 8.4e-8
+// with sums in 64 bits), where 64 bits would take two more registers a value and the packed instructions.
+//
 // Of 65536 x 64 f32 logits the loss takes 11.6 us and the gradient 7.7 (memory alone: 2.6 and 5.1): instructions, the chain of loads at a
 // block's start, and for the loss a second launch.
 #include <algorithm>

@@ -53,7 +53,8 @@ __device__ __forceinline__ float top_of(float a, float b, float c) {
   return r;
 }
 // silu(g) * u of two values.  1 / (1 + 2^(-g log2 e)): the exponent's rounding makes it off by |g| 2^-23, the rest by 2^-21; from g = -88 down
-// it is 0.  (Six instructions a value: with expf and a division the results of a tile took longer than its steps.)
+// it is 0.  (Six instructions a value: with expf and a division the results of a tile took longer than its steps.  An h that is so near to
+// the middle of two 4-bit values may become the other one, as it may by the order of the sums that g and u are: one in some 2^16 of them.)
 __device__ __forceinline__ uint64_t swiglu2(float g0, float g1, float u0, float u1) {
   const uint64_t g = pair(g0, g1);
   float a, b, c, d;

@@ -4,7 +4,7 @@ import torch
 
 from paper_2411_02581_b200 import binding as B
 from paper_2411_02581_b200 import build as build_mod
-from test_fp4_experts import layer
+from test_fp4_experts import layer, plain_rows
 from test_fp8 import activations
 
 
@@ -67,3 +67,26 @@ def test_offsets_off_eight_bytes_are_refused():
     for k in (0, 64):
         assert B.lib().tuna_fp4_matmul(256, 256, 5, 64, 256, 256, 7, 64, k, 2, 260, 256, 0, 8, None) == -1
         assert B.lib().tuna_fp8_matmul(256, 256, 5, 64, 256, 256, 2, 7, 64, k, 2, 260, 256, 0, 8, None) == -1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("t,e,k,d,i", [(1, 8, 2, 1024, 256), (1, 4, 1, 512, 128), (16, 6, 2, 512, 256), (130, 5, 4, 256, 64)])
+def test_experts_rows_are_rounded_once_before_the_sum(t, e, k, d, i):
+    """The weighted sum adds rows of bf16 in 32 bits.  Against those of 64 bits, rounded, a value differs only where the 32-bit sums cross the middle of two
+    bf16 values (a product's sum is off by some 2^-22 of its terms, so one in 2^10 at most, and then by 2^-8: 2^-13 in all) or of two 4-bit ones (one in
+    2^16 of h, by a quarter of itself: 2^-10 of all rows, if there is one at all)."""
+    from paper_2411_02581_b200 import moe
+    parts = layer(e, d, i, 11)
+    x = activations(t, d, 12).cuda()
+    g = torch.Generator().manual_seed(13)
+    ids = torch.rand(t, e, generator=g).argsort(1)[:, :k].to(torch.int32)
+    w = torch.rand(t, k, generator=g)
+    want = torch.zeros(t, d, dtype=torch.float64)
+    for j in range(e):
+        at, slot = (ids == j).nonzero(as_tuple=True)
+        if at.numel():
+            y, _ = plain_rows(x[at].cpu(), *[p[j] for p in parts])
+            want.index_add_(0, at, y.to(torch.bfloat16).double() * w[at, slot].double()[:, None])
+    want = want.to(torch.bfloat16).double()
+    got = moe.fp4_experts(x, ids.cuda(), w.cuda(), *parts).cpu().double()
+    assert float((got - want).norm()) <= 2.0 ** -10 * float(want.norm())
