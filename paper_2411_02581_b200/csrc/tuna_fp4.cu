@@ -484,8 +484,8 @@ __global__ void __launch_bounds__(256) tuna_align4_kernel(const uint8_t *q, int6
 //
 // With `swiglu` the 256 columns are 128 rows of the gate matrix and the same 128 of the up matrix, so that a thread reads
 // both values of a place from its own row of the accumulator, and 32 of them are one block of the 4-bit result.  Blocks behind the
-// last column are zero with the scale 0: b's values are zero there, but its scales may be anything, NaN too, and the next product reads
-// the blocks' scales to the end of the run.
+// last column get the scale 0: b's values are zero there, but its scales may be anything, NaN too, and the next product reads the scales
+// to the end of the run (and no values).
 struct Tile4Args {
   Product4Args p;
   int stages;   // of k: 256 values each
@@ -843,13 +843,12 @@ __global__ void __launch_bounds__(kThreads4, 1)
             unpair(swiglu2(__uint_as_float(g[b][i]), __uint_as_float(g[b][i + 1]), __uint_as_float(u[b][i]), __uint_as_float(u[b][i + 1])), h[i], h[i + 1]);
             top = top_of(top, h[i], h[i + 1]);
           }
-          const bool real = w.n0 + c0 + b * 32 < a.p.n;  // (n is whole blocks)
-          const uint32_t byte = real ? fp4_scale(__float_as_uint(top) & 0x7fffffffu) : 0;
+          const uint32_t byte = w.n0 + c0 + b * 32 < a.p.n ? fp4_scale(__float_as_uint(top) & 0x7fffffffu) : 0;  // (n is whole blocks)
           const uint64_t by = pair(fp4_inverse(byte), fp4_inverse(byte));
 #pragma unroll
           for (int i = 0; i < 32; i += 2) unpair(mul2(pair(h[i], h[i + 1]), by), h[i], h[i + 1]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) packed[b][i] = real ? fp4_eight(h + i * 8) : 0;
+          for (int i = 0; i < 4; ++i) packed[b][i] = fp4_eight(h + i * 8);
           bytes |= byte << (8 * b);
         }
         if (there) {
@@ -958,8 +957,7 @@ __global__ void __launch_bounds__(kThreads4, 1)
           for (int q = 0; q < parts; ++q) g += load_one(at, q), u += load_one(at + 128 * 4, q);
           float h, unused;
           unpair(swiglu2(g, g, u, u), h, unused);
-          if (w.n0 + (i & 3) * 32 >= a.p.n) h = 0.0f;
-          const uint32_t byte = fp4_scale(__reduce_max_sync(~0u, abs_bits(h)));
+          const uint32_t most = __reduce_max_sync(~0u, abs_bits(h)), byte = w.n0 + (i & 3) * 32 < a.p.n ? fp4_scale(most) : 0;
           const float v = h * fp4_inverse(byte);
           // eight neighbours' values to the first of them
           float eight[8];
