@@ -476,11 +476,12 @@ __global__ void __launch_bounds__(256) tuna_align4_kernel(const uint8_t *q, int6
 // into a ring of stages; one elected lane moves a stage's scales into tensor memory, to columns that belong to the stage,
 // and issues its four tensor-core steps; eight warps read a finished accumulator back and store it.
 //
-// What bounds it: the 1000 W limit.  8192 x 4096 x 4096 takes 54 to 60 us (4600 to 5100 TFLOP/s) at a clock of 1.4 to 1.5 GHz, the tensor
-// pipe busy for 63 % of the cycles, and that time does not change when b is shared by pairs, when the next tile's steps begin
+// What bounds it: the 1000 W limit.  8192 x 4096 x 4096 takes 55 us in bursts with pauses between them (5000 TFLOP/s) and 61 in long runs
+// (4500) at a clock of 1.4 to 1.5 GHz, the tensor pipe busy for 57 to 63 % of the cycles, and that time does not change when b is shared by pairs, when the next tile's steps begin
 // before an accumulator has been read out, or when the copies of the scales are left out.  A few rows are bound by memory: 64
 // matrices of 4096 x 2048 with 4 rows each 45.3 us, 96 % of the copy rate.  (SwiGLU's tiles were bound by their results: with exact division 511 us for
-// the first product of 64 experts of 4096 x 2048 and 16384 rows, 150 us as it is.)
+// the first product of 64 experts of 4096 x 2048 and 16384 uneven rows; now 188 in bursts and 222 in long runs, 156 in bursts with 256 rows each, as
+// much as two products of its two halves without it.)
 //
 // With `swiglu` the 256 columns are 128 rows of the gate matrix and the same 128 of the up matrix, so that a thread reads
 // both values of a place from its own row of the accumulator, and 32 of them are one block of the 4-bit result.  Blocks behind the

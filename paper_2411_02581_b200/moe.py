@@ -285,7 +285,9 @@ def fp4_matmul(a, a_scale, b, b_scale, *, offsets=None, out_dtype=torch.bfloat16
     """a b^T of operands that :func:`fp4_quantize` made along the contracted axis (``tuna_fp4_matmul``).
 
     ``b`` [n, k / 2], or [groups, n, k / 2] with ``offsets`` (int64 [groups + 1]): rows offsets[g] .. offsets[g + 1] of
-    ``a``, which was quantised with these offsets, meet ``b[g]``; a row of the result that is outside every group is undefined."""
+    ``a``, which was quantised with these offsets, meet ``b[g]``; a row of the result that is outside every group is undefined.
+    Operands lie as :func:`fp4_quantize` returns them, each row on a 16-byte boundary; others (a contiguous copy of rows
+    whose bytes are no multiple of 16) are laid so in every call."""
     if out_dtype not in FLOATS:
         raise ValueError(f"out_dtype: one of {FLOATS}")
     return (_marshal or _fast()).fp4_matmul(a, a_scale, b, b_scale, offsets, DTYPES[out_dtype], stream)
